@@ -488,6 +488,33 @@ size_t sp_mha_value_refit_workspace_bytes(int64_t d, int64_t n_heads, int64_t T,
                                           int32_t dtype);
 
 /* ---------------------------------------------------------------------------------------------------------------
+ * sp_token_logprobs, sp_token_logprobs_grad — how well a model predicts given tokens (the paper's measure, Section 4, is the
+ * perplexity exp(-mean log p)), and the gradient of that.
+ * With z = scale * logits (row by row):  lse = log sum_v e^z_v,  logp = z_target - lse,  entropy = -sum_v p_v log p_v with
+ * p = e^(z - lse).  logits: [T, V], SP_BF16 or SP_F32, any ld and alignment.  All sums in fp32, one read of the logits.
+ * targets: int64 [T] or NULL.  A negative target: the row is not scored, logp = 0 (its lse, entropy and alternatives are
+ * written).  A target >= V: logp = NaN, and SP_ERR_SHAPE with the row through status_dev (may be NULL).
+ * alt_ids int32 / alt_logp fp32 [T, n_alts]: the n_alts largest logits of each row in falling order, equal ones by the lower
+ * index, NaN lowest.  Any output may be NULL (alt_ids and alt_logp go with n_alts > 0).
+ * A logit of -infinity has p = 0 and adds nothing to the entropy; a row of nothing else has lse = logp = -infinity and
+ * entropy 0 (alternatives: indices 0, 1, ... and -infinity).  A NaN or +infinity among the logits makes logp, lse and entropy NaN.
+ * sp_token_logprobs_grad: dlogits = scale (g_logp (1{v = target} - p) - g_entropy p (log p + entropy)), the gradient of
+ * sum_t g_logp logp + g_entropy entropy, from the lse and entropy of the forward call (entropy is read only with g_entropy).
+ * g_logp, g_entropy: fp32 [T], either may be NULL (zero), g_logp needs targets.  A row that is not scored has no g_logp part;
+ * a target >= V is taken as not scored; a row of nothing but -infinity has gradient 0.  dlogits: [T, V], dtype of logits, it
+ * may be logits itself (same pointer and ld).
+ * Errors: SP_ERR_INVALID_ARG (null logits or outputs, scale not positive and finite, all gradients NULL), SP_ERR_SHAPE
+ * (V < 1 with rows, n_alts outside [0, min(V, SP_MAX_ALTS)], V > 2^30), SP_ERR_DTYPE.
+ */
+#define SP_MAX_ALTS 32
+sp_status sp_token_logprobs(const sp_mat* logits, const int64_t* targets, double scale, int32_t n_alts, float* logp,
+                            float* lse, float* entropy, int32_t* alt_ids, float* alt_logp, int32_t* status_dev,
+                            void* stream);
+sp_status sp_token_logprobs_grad(const sp_mat* logits, const int64_t* targets, double scale, const float* lse,
+                                 const float* entropy, const float* g_logp, const float* g_entropy,
+                                 const sp_mat* dlogits, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
  * Helpers.
  * sp_ridge_solve   — W[m,n] = R[m,n] (G[n,n] + rho_eff I)^-1 by Cholesky and two triangular solves (weight
  *                    recovery of Appendix A.1).  G, R, W fp32; factorisation in fp64 when precise != 0, else fp32.

@@ -22,6 +22,7 @@ SP_ACT_RELU, SP_ACT_SWIGLU = 0, 1
 SP_Z_PAPER, SP_Z_EXACT = 0, 1
 SP_SCORE_WANDA_L2, SP_SCORE_WANDA_L1, SP_SCORE_LEMMA1 = 0, 1, 2
 SP_ALLOC_SOFTMAX, SP_ALLOC_INVERSE, SP_ALLOC_UNIFORM = 0, 1, 2
+SP_MAX_ALTS = 32
 (SP_WS_GRAM, SP_WS_ADMM_STEP, SP_WS_SCORES, SP_WS_APPLY_MASK, SP_WS_FFN_INIT, SP_WS_LINEAR_REFIT, SP_WS_GEMM,
  SP_WS_RIDGE_SOLVE) = range(8)
 
@@ -33,7 +34,8 @@ EXPORTS = ["sp_gram_accumulate", "sp_ffn_init", "sp_admm_step", "sp_admm_scores"
            "sp_profile_kind_name", "sp_launch_count", "sp_mha_init", "sp_mha_step", "sp_mha_workspace_bytes",
            "sp_set_reproducible", "sp_get_reproducible", "sp_allocate_sparsity_grid", "sp_apply_mask_global",
            "sp_apply_mask_global_bytes", "sp_objective_accumulate", "sp_ffn_cache_input_inverse",
-           "sp_set_wait_budget", "sp_mha_value_refit", "sp_mha_value_refit_workspace_bytes"]
+           "sp_set_wait_budget", "sp_mha_value_refit", "sp_mha_value_refit_workspace_bytes",
+           "sp_token_logprobs", "sp_token_logprobs_grad"]
 
 
 class SpError(RuntimeError):
@@ -141,6 +143,8 @@ def lib() -> C.CDLL:
         L.sp_apply_mask_global_bytes.restype = C.c_size_t
         L.sp_apply_mask_global_bytes.argtypes = [i64, i32]
         L.sp_objective_accumulate.argtypes = [vp, dbl, vp, i32, vp]
+        L.sp_token_logprobs.argtypes = [pm, vp, dbl, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.sp_token_logprobs_grad.argtypes = [pm, vp, dbl, vp, vp, vp, vp, pm, vp]
         L.sp_set_reproducible.argtypes = [i32]
         L.sp_set_wait_budget.argtypes = [i64]
         L.sp_get_reproducible.restype = i32
@@ -451,6 +455,74 @@ def sp_distribute_importance(head_stats, fc_stats, rho, gamma):
                                           float(rho), float(gamma), _ptr(Ia), _ptr(Im), _stream()),
            "sp_distribute_importance")
     return Ia, Im
+
+
+# ---------------------------------------------------------------------------------- forward of a layer, scoring
+def _on_one_device(*tensors):
+    """CUDA tensors of one device, which has to be the current one (the kernels run on its current stream)."""
+    _require_cuda(*tensors)
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError("the tensors of a call must be on the current CUDA device")
+
+
+def _vector(t, dtype, n, what):
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{what} must be contiguous {str(dtype)[6:]} with {n} entries")
+
+
+def _dtype_of(t, what):
+    if t.dim() != 2 or t.dtype not in _DTYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be a row-major 2-D tensor of fp32 or bf16")
+    return _DTYPES[t.dtype]
+
+
+@dataclass
+class TokenLogprobs:
+    logp: torch.Tensor | None           # fp32 [T] log probability of the target (None without targets)
+    lse: torch.Tensor                   # fp32 [T] log sum_v e^(scale logit_v)
+    entropy: torch.Tensor | None        # fp32 [T]
+    alt_ids: torch.Tensor | None        # int32 [T, n_alts]
+    alt_logp: torch.Tensor | None       # fp32 [T, n_alts]
+
+
+def sp_token_logprobs(logits, targets=None, n_alts=0, scale=1.0, want_entropy=True, status=None) -> TokenLogprobs:
+    """Log probabilities of the target tokens with entropies and the n_alts best alternatives of every row (see sp.h).
+    logits [T, V] bf16 or fp32, any row pitch; targets int64 [T] (negative: the row is not scored)."""
+    _on_one_device(logits, targets, status)
+    _dtype_of(logits, "logits")
+    T, n_alts = logits.shape[0], int(n_alts)
+    _vector(targets, torch.int64, T, "targets")
+    _vector(status, torch.int32, 4, "status")
+    f32 = dict(dtype=torch.float32, device=logits.device)
+    keep = 0 < n_alts <= SP_MAX_ALTS                    # (else the library's refusal, with its code)
+    r = TokenLogprobs(torch.empty(T, **f32) if targets is not None else None, torch.empty(T, **f32),
+                      torch.empty(T, **f32) if want_entropy else None,
+                      torch.empty(T, n_alts, dtype=torch.int32, device=logits.device) if keep else None,
+                      torch.empty(T, n_alts, **f32) if keep else None)
+    x = mat(logits)
+    _check(lib().sp_token_logprobs(C.byref(x), _ptr(targets), float(scale), n_alts, _ptr(r.logp), _ptr(r.lse),
+                                   _ptr(r.entropy), _ptr(r.alt_ids), _ptr(r.alt_logp), _ptr(status), _stream()),
+           "sp_token_logprobs")
+    return r
+
+
+def sp_token_logprobs_grad(logits, targets, lse, g_logp, entropy=None, g_entropy=None, scale=1.0, out=None):
+    """Gradient of sum_t g_logp logp + g_entropy entropy with respect to the logits (see sp.h), in their dtype; lse and
+    entropy as sp_token_logprobs left them.  out may be logits itself.  Returns it."""
+    _on_one_device(logits, targets, lse, g_logp, entropy, g_entropy, out)
+    _dtype_of(logits, "logits")
+    T = logits.shape[0]
+    _vector(targets, torch.int64, T, "targets")
+    for name, t in (("lse", lse), ("g_logp", g_logp), ("entropy", entropy), ("g_entropy", g_entropy)):
+        _vector(t, torch.float32, T, name)
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _dtype_of(out, "out")
+    x, d = mat(logits), mat(out)
+    _check(lib().sp_token_logprobs_grad(C.byref(x), _ptr(targets), float(scale), _ptr(lse), _ptr(entropy), _ptr(g_logp),
+                                        _ptr(g_entropy), C.byref(d), _stream()), "sp_token_logprobs_grad")
+    return out
 
 
 # ---------------------------------------------------------------------------------------------- module driver

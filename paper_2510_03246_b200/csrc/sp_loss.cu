@@ -1,0 +1,480 @@
+// Log probabilities of given tokens with entropy and best alternatives, and their gradient with respect to the logits.
+//
+// With t_v = log2(e) scale x_v and any reference r:  s = sum_v 2^(t_v - r), w = sum_v (t_v - r) 2^(t_v - r) give
+//   lse = ln2 (r + log2 s),   log p_v = ln2 (t_v - r - log2 s),   entropy = ln2 (log2 s - w / s),
+// and (r, s, w) of two parts of a row join by shifting both to the larger r.  So one pass over the logits suffices: every
+// thread keeps its own (r, s, w) with r its running maximum, and they are joined at the end.  All of it is held in fp32.
+#include <math.h>
+
+#include "sp_common.cuh"
+
+namespace sp {
+namespace {
+
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kLossThreads = 256;
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// 16 bytes of a row as floats
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(const uint4& q, float (&x)[4]) {
+    x[0] = __uint_as_float(q.x); x[1] = __uint_as_float(q.y); x[2] = __uint_as_float(q.z); x[3] = __uint_as_float(q.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ float one(float v) { return v; }
+  static __device__ __forceinline__ float to(float v) { return v; }
+};
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void unpack(const uint4& q, float (&x)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float one(__nv_bfloat16 v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ __nv_bfloat16 to(float v) { return __float2bfloat16_rn(v); }
+};
+
+// (r, s, w) of a part of a row; r = -infinity: nothing but -infinity so far
+struct Part {
+  float r, s, w;
+};
+__device__ __forceinline__ Part join(const Part& a, const Part& b) {
+  const float r = fmaxf(a.r, b.r);
+  if (r == -INFINITY) return Part{r, a.s + b.s, a.w + b.w};     // (zeros, or the NaN of a NaN logit)
+  // a part with r = -infinity holds zeros: its shift is taken as zero (0 * infinity)
+  const float da = a.r == -INFINITY ? 0.f : a.r - r, db = b.r == -INFINITY ? 0.f : b.r - r;
+  const float fa = exp2f(da), fb = exp2f(db);
+  return Part{r, a.s * fa + b.s * fb, (a.w + da * a.s) * fa + (b.w + db * b.s) * fb};
+}
+
+// Keys of the selection: larger value first, then the lower index; NaN below everything, zeros equal.
+__device__ __forceinline__ uint32_t order_bits(float x) {
+  if (x != x) return 0u;
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float order_value(uint32_t k) {
+  if (k == 0u) return __uint_as_float(0x7fffffffu);
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+__device__ __forceinline__ unsigned long long make_key(float x, uint32_t index) {
+  return ((unsigned long long)order_bits(x) << 32) | (uint32_t)~index;
+}
+
+// The n best keys a warp has seen, one per lane in falling order (0: none yet).  floor_key: keys up to it are of no use, since
+// n larger ones are known (to this warp or another one of the row).
+struct WarpBest {
+  unsigned long long key;
+  // every lane calls; keys of the lanes in `offer` are inserted
+  __device__ __forceinline__ void insert(bool offer, unsigned long long k, int n, unsigned long long& floor_key, int lane) {
+    uint32_t m = __ballot_sync(0xffffffffu, offer && k > floor_key);
+    while (m) {
+      const unsigned long long c = __shfl_sync(0xffffffffu, k, __ffs(m) - 1);
+      m &= m - 1;
+      if (c <= floor_key) continue;                       // the same in every lane
+      const int at = __popc(__ballot_sync(0xffffffffu, key > c));
+      const unsigned long long up = __shfl_up_sync(0xffffffffu, key, 1);
+      if (lane == at) key = c;
+      else if (lane > at) key = up;
+      const unsigned long long last = __shfl_sync(0xffffffffu, key, n - 1);
+      if (last > floor_key) floor_key = last;
+    }
+  }
+};
+
+struct LogprobParams {
+  const void* x;
+  int64_t ld, T;
+  int32_t V, n_alts;
+  float scale;
+  const int64_t* targets;
+  float* logp;
+  float* lse;
+  float* entropy;
+  int32_t* alt_ids;
+  float* alt_logp;
+  int32_t* status;
+};
+
+// A row belongs to WARPS warps (one: eight rows a block) of each of the CTAs of a cluster (gridDim.x = rows x cluster).
+template <typename T, int WARPS, bool ENT, bool ALTS>
+__global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const LogprobParams p, int cluster) {
+  kernel_begin();
+  constexpr int kWarps = kLossThreads / 32, N = Vec<T>::N, U = 4;     // U vectors in flight per thread
+  static_assert(WARPS == 1 || WARPS == kWarps, "rows per block");
+  __shared__ Part s_part[kWarps];
+  __shared__ unsigned long long s_best[ALTS ? kWarps * SP_MAX_ALTS : 1];
+  __shared__ unsigned long long s_floor;
+  __shared__ Part s_all[kMaxCluster];
+  __shared__ unsigned long long s_all_best[ALTS ? kMaxCluster * SP_MAX_ALTS : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rank = WARPS == 1 ? 0 : (int)(blockIdx.x % cluster);
+  const int64_t row = WARPS == 1 ? (int64_t)blockIdx.x * kWarps + warp : (int64_t)(blockIdx.x / cluster);
+  const bool live = row < p.T;
+  const int wl = WARPS == 1 ? 0 : warp;                // warp within the row
+  // (the other CTAs of a cluster write into the first one's shared memory: all have started once they meet)
+  if (WARPS > 1 && cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  if (ALTS && WARPS > 1) {
+    if (threadIdx.x == 0) s_floor = 0ull;
+    __syncthreads();
+  }
+  const float c = p.scale * kLog2E;
+  Part a{-INFINITY, 0.f, 0.f};
+  float rc = 0.f;                                      // a.r, or 0 while that is -infinity
+  WarpBest best{0ull};
+  unsigned long long floor_key = 0ull;
+
+  // values x[0 .. n) into (r, s, w)
+  auto take = [&](const float* x, int n, float m) {
+    const float mt = m * c;
+    if (mt > a.r) {
+      const float d = a.r - mt, f = exp2_fast(d);      // a.r = -infinity: f = 0, and s = w = 0
+      if (ENT) a.w = a.r == -INFINITY ? a.w : f * fmaf(d, a.s, a.w);
+      a.s *= f;
+      a.r = mt;
+      rc = mt;
+    }
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float t = fmaf(x[i], c, -rc), e = exp2_fast(t);
+      a.s += e;
+      // (a logit of -infinity: e = 0, and 0 times a finite number is added)
+      if (ENT) a.w = fmaf(e, fmaxf(t, -10000.f), a.w);
+    }
+  };
+
+  if (live) {
+    const T* xr = reinterpret_cast<const T*>(p.x) + row * p.ld;
+    // whole vectors of the row, which start on 16 bytes, and the values before and behind them; this CTA's vectors: [v0, v1)
+    const int head = (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(xr) & 15u)) & 15u) / sizeof(T));
+    const int first = head < p.V ? head : p.V;
+    const int nvec = (p.V - first) / N;
+    const int per = (nvec + cluster - 1) / cluster;
+    const int v0 = min(rank * per, nvec), v1 = min(v0 + per, nvec);
+    const uint4* xv = reinterpret_cast<const uint4*>(xr + first);
+    auto scalar = [&](int i, bool in) {                // one value per lane (loose ends)
+      const float v = in ? Vec<T>::one(xr[i]) : -INFINITY;
+      if (in) take(&v, 1, v);
+      if (ALTS) best.insert(in, make_key(v, (uint32_t)i), p.n_alts, floor_key, lane);
+    };
+    if (wl == 0 && rank == 0) scalar(lane, lane < first);
+    constexpr int STEP = WARPS * 32;
+    for (int v = v0 + wl * 32; v < v1; v += STEP * U) {         // the warp's first vector: the same trips in every lane
+      uint4 q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (v + u * STEP + lane < v1) q[u] = __ldcs(xv + v + u * STEP + lane);
+      if (ALTS && WARPS > 1) {
+        const unsigned long long f = *reinterpret_cast<volatile unsigned long long*>(&s_floor);
+        if (f > floor_key) floor_key = f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = v + u * STEP + lane;
+        const bool in = at < v1;
+        float x[N];
+        Vec<T>::unpack(q[u], x);
+        float m = -INFINITY;
+        if (in) {
+          m = x[0];
+#pragma unroll
+          for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+          take(x, N, m);
+        }
+        if (ALTS) {
+          // (fmaxf skips NaN; a vector of nothing else has m = NaN, the lowest value)
+          const bool may = in && !(order_bits(m) < (uint32_t)(floor_key >> 32));
+          if (__any_sync(0xffffffffu, may)) {
+            const unsigned long long before = floor_key;
+#pragma unroll 1
+            for (int i = 0; i < N; ++i) {
+              float xi = x[0];
+#pragma unroll
+              for (int j = 1; j < N; ++j) xi = i == j ? x[j] : xi;
+              best.insert(in, make_key(xi, (uint32_t)(first + at * N + i)), p.n_alts, floor_key, lane);
+            }
+            if (WARPS > 1 && lane == 0 && floor_key > before) atomicMax(&s_floor, floor_key);
+          }
+        }
+      }
+    }
+    if (wl == WARPS - 1 && rank == cluster - 1) {
+      const int tail0 = first + nvec * N;
+      scalar(tail0 + lane, tail0 + lane < p.V);
+    }
+  }
+
+  // join the lanes, then the warps of the row, then the CTAs of the cluster
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const Part b{__shfl_xor_sync(0xffffffffu, a.r, o), __shfl_xor_sync(0xffffffffu, a.s, o),
+                 __shfl_xor_sync(0xffffffffu, a.w, o)};
+    a = lane & o ? join(b, a) : join(a, b);            // the same order in both lanes
+  }
+  if (WARPS > 1) {
+    if (lane == 0) s_part[warp] = a;
+    if (ALTS && lane < p.n_alts) s_best[warp * SP_MAX_ALTS + lane] = best.key;
+    __syncthreads();
+    if (warp == 0) {
+      a = s_part[0];
+      for (int i = 1; i < kWarps; ++i) a = join(a, s_part[i]);
+      if (ALTS) {
+        floor_key = __shfl_sync(0xffffffffu, best.key, p.n_alts - 1);
+        for (int i = 1; i < kWarps; ++i) {
+          const unsigned long long k = lane < p.n_alts ? s_best[i * SP_MAX_ALTS + lane] : 0ull;
+          best.insert(k != 0ull, k, p.n_alts, floor_key, lane);
+        }
+      }
+    }
+    if (cluster > 1) {
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+      uint32_t dst = (uint32_t)__cvta_generic_to_shared(&s_all[rank]), dst_best = 0u;
+      asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(dst));
+      if (warp == 0) {
+        if (lane == 0)
+          asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\t"
+                       "st.shared::cluster.f32 [%0+8], %3;" ::"r"(dst), "f"(a.r), "f"(a.s), "f"(a.w) : "memory");
+        if (ALTS && lane < p.n_alts) {
+          dst_best = (uint32_t)__cvta_generic_to_shared(&s_all_best[rank * SP_MAX_ALTS + lane]);
+          asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(dst_best));
+          asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(dst_best), "l"(best.key) : "memory");
+        }
+      }
+      asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+      if (rank != 0) return;
+      if (warp == 0) {
+        a = s_all[0];
+        for (int i = 1; i < cluster; ++i) a = join(a, s_all[i]);
+        if (ALTS) {
+          floor_key = __shfl_sync(0xffffffffu, best.key, p.n_alts - 1);
+          for (int i = 1; i < cluster; ++i) {
+            const unsigned long long k = lane < p.n_alts ? s_all_best[i * SP_MAX_ALTS + lane] : 0ull;
+            best.insert(k != 0ull, k, p.n_alts, floor_key, lane);
+          }
+        }
+      }
+    }
+    if (warp != 0) return;
+  }
+  if (!live) return;
+  // (all -infinity: s = 0, unless a NaN made it NaN)
+  const bool none = a.r == -INFINITY && a.s == 0.f;
+  const float r = a.r == -INFINITY ? 0.f : a.r;
+  const float l2 = none ? -INFINITY : log2f(a.s);
+  // a logit of +infinity makes r infinite and s NaN
+  auto logp_of = [&](float x) { return none ? -INFINITY : kLn2 * (fmaf(x, c, -r) - l2); };
+  if (lane == 0) {
+    if (p.lse) p.lse[row] = none ? -INFINITY : kLn2 * (r + l2);
+    if (ENT && p.entropy) p.entropy[row] = none ? 0.f : kLn2 * (l2 - a.w / a.s);
+    if (p.logp && p.targets) {
+      const int64_t t = p.targets[row];
+      float v = 0.f;
+      if (t >= p.V) {
+        v = NAN;
+        report_status(p.status, SP_ERR_SHAPE, (int32_t)row, 0);
+      } else if (t >= 0) {
+        v = logp_of(Vec<T>::one(reinterpret_cast<const T*>(p.x)[row * p.ld + t]));
+      }
+      p.logp[row] = v;
+    }
+  }
+  if (ALTS && lane < p.n_alts) {
+    const int64_t o = row * p.n_alts + lane;
+    if (p.alt_ids) p.alt_ids[o] = (int32_t)~(uint32_t)best.key;
+    if (p.alt_logp) p.alt_logp[o] = logp_of(order_value((uint32_t)(best.key >> 32)));
+  }
+}
+
+struct GradParams {
+  const void* x;
+  void* d;
+  int64_t ld_x, ld_d, T;
+  int32_t V, chunks;
+  float scale;
+  const int64_t* targets;
+  const float* lse;
+  const float* entropy;
+  const float* g_logp;
+  const float* g_entropy;
+};
+constexpr int kGradVecs = 4;       // vectors of 16 bytes per thread
+
+// d_v = p_v (A + B u_v) + (v == target) scale g,  u = scale x - lse = log p,  A = -scale (g + h H), B = -scale h.
+// One read and one write of the row: 8 elementary operations per value, bound by DRAM.
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads) token_logprobs_grad_kernel(const GradParams p) {
+  kernel_begin();
+  constexpr int N = Vec<T>::N;
+  const int64_t row = blockIdx.x / p.chunks;
+  const int chunk = (int)(blockIdx.x % p.chunks);
+  const T* xr = reinterpret_cast<const T*>(p.x) + row * p.ld_x;
+  T* dr = reinterpret_cast<T*>(p.d) + row * p.ld_d;
+  const int64_t target64 = p.targets ? p.targets[row] : -1;
+  const int target = target64 >= 0 && target64 < p.V ? (int)target64 : -1;
+  float lse = p.lse[row];
+  float g = target >= 0 && p.g_logp ? p.g_logp[row] : 0.f;
+  float A = -p.scale * g, B = 0.f;
+  if (p.g_entropy) {
+    const float h = p.g_entropy[row];
+    A = -p.scale * fmaf(h, p.entropy[row], g);
+    B = -p.scale * h;
+  }
+  if (lse == -INFINITY) A = B = g = lse = 0.f;           // nothing but -infinity: p = 0 below
+  const float add = p.scale * g;
+  auto one = [&](float x) {
+    const float u = fmaf(x, p.scale, -lse);
+    return exp2_fast(u * kLog2E) * fmaf(B, fmaxf(u, -10000.f), A);
+  };
+  const uint32_t phase = (uint32_t)(reinterpret_cast<uintptr_t>(xr) & 15u);
+  const bool same = phase == (uint32_t)(reinterpret_cast<uintptr_t>(dr) & 15u);
+  const int head = same ? (int)(((16u - phase) & 15u) / sizeof(T)) : p.V;     // rows of two phases go value by value
+  const int first = head < p.V ? head : p.V;
+  constexpr int kPer = kLossThreads * kGradVecs;
+  if (same) {
+    const int nvec = (p.V - first) / N;
+    uint4 q[kGradVecs];
+#pragma unroll
+    for (int i = 0; i < kGradVecs; ++i) {
+      const int v = chunk * kPer + i * kLossThreads + (int)threadIdx.x;
+      if (v < nvec) q[i] = __ldcs(reinterpret_cast<const uint4*>(xr + first) + v);
+    }
+#pragma unroll
+    for (int i = 0; i < kGradVecs; ++i) {
+      const int v = chunk * kPer + i * kLossThreads + (int)threadIdx.x;
+      if (v < nvec) {
+        float x[N];
+        Vec<T>::unpack(q[i], x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          x[j] = one(x[j]);
+          if (first + v * N + j == target) x[j] += add;
+        }
+        __stcs(reinterpret_cast<uint4*>(dr + first) + v, Vec<T>::pack(x));
+      }
+    }
+    if (chunk == 0) {
+      const int loose = first + (p.V - first) % N;       // before the first and behind the last vector
+      for (int i = threadIdx.x; i < loose; i += kLossThreads) {
+        const int at = i < first ? i : first + nvec * N + (i - first);
+        dr[at] = Vec<T>::to(one(Vec<T>::one(xr[at])) + (at == target ? add : 0.f));
+      }
+    }
+  } else {
+    const int lo = chunk * kPer * N;
+    for (int i = lo + (int)threadIdx.x; i < p.V && i < lo + kPer * N; i += kLossThreads)
+      dr[i] = Vec<T>::to(one(Vec<T>::one(xr[i])) + (i == target ? add : 0.f));
+  }
+}
+
+template <typename T, int WARPS>
+cudaError_t launch_logprobs(const LogprobParams& p, int cluster, cudaStream_t stream) {
+  const bool ent = p.entropy != nullptr, alts = p.n_alts > 0;
+  const auto kernel = ent ? (alts ? token_logprobs_kernel<T, WARPS, true, true> : token_logprobs_kernel<T, WARPS, true, false>)
+                          : (alts ? token_logprobs_kernel<T, WARPS, false, true> : token_logprobs_kernel<T, WARPS, false, false>);
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  const int64_t blocks = WARPS == 1 ? ceil_div(p.T, kLossThreads / 32) : p.T * cluster;
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kLossThreads);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = cluster > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, p, cluster);
+}
+
+bool positive_finite(double v) { return v > 0.0 && v <= 3.0e38; }
+
+}  // namespace
+}  // namespace sp
+
+extern "C" {
+
+sp_status sp_token_logprobs(const sp_mat* logits, const int64_t* targets, double scale, int32_t n_alts, float* logp,
+                            float* lse, float* entropy, int32_t* alt_ids, float* alt_logp, int32_t* status_dev,
+                            void* stream) {
+  using namespace sp;
+  if (!logits) return SP_ERR_INVALID_ARG;
+  if (logits->dtype != SP_F32 && logits->dtype != SP_BF16) return SP_ERR_DTYPE;
+  const int64_t T = logits->rows, V = logits->cols;
+  if (T < 0 || V < 0 || V > (1 << 30) || (T > 1 && logits->ld < V)) return SP_ERR_SHAPE;
+  if (n_alts < 0 || n_alts > SP_MAX_ALTS || n_alts > V) return SP_ERR_SHAPE;
+  if (!positive_finite(scale)) return SP_ERR_INVALID_ARG;
+  if (n_alts > 0 ? !alt_ids && !alt_logp : alt_ids != nullptr || alt_logp != nullptr) return SP_ERR_INVALID_ARG;
+  if (logp && !targets) return SP_ERR_INVALID_ARG;
+  if (!logp && !lse && !entropy && n_alts == 0) return SP_ERR_INVALID_ARG;
+  if (T == 0) return SP_OK;
+  if (V < 1 || T * kMaxCluster > 0x7fffffff) return SP_ERR_SHAPE;
+  if (!logits->ptr) return SP_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const LogprobParams p{logits->ptr, logits->ld, T, (int32_t)V, n_alts, (float)scale, targets, logp, lse, entropy,
+                        alt_ids, alt_logp, status_dev};
+  // Short rows: a warp each.  Long ones: a block, or a cluster of blocks while there are too few rows to fill the SMs.
+  const bool narrow = V <= 4096;
+  int cluster = 1;
+  while (!narrow && cluster < kMaxCluster && T * cluster * 2 <= (int64_t)sm_count() * 4 && V / (cluster * 2) >= 2048) cluster *= 2;
+  count_launch();
+  ProfScope prof(PK_SCORES, 0.0, (double)T * V * dtype_size(logits->dtype), s);
+  const cudaError_t e =
+      logits->dtype == SP_F32
+          ? (narrow ? launch_logprobs<float, 1>(p, 1, s) : launch_logprobs<float, kLossThreads / 32>(p, cluster, s))
+          : (narrow ? launch_logprobs<__nv_bfloat16, 1>(p, 1, s)
+                    : launch_logprobs<__nv_bfloat16, kLossThreads / 32>(p, cluster, s));
+  return e == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+}
+
+sp_status sp_token_logprobs_grad(const sp_mat* logits, const int64_t* targets, double scale, const float* lse,
+                                 const float* entropy, const float* g_logp, const float* g_entropy,
+                                 const sp_mat* dlogits, void* stream) {
+  using namespace sp;
+  if (!logits || !dlogits) return SP_ERR_INVALID_ARG;
+  if ((logits->dtype != SP_F32 && logits->dtype != SP_BF16) || dlogits->dtype != logits->dtype) return SP_ERR_DTYPE;
+  const int64_t T = logits->rows, V = logits->cols;
+  if (T < 0 || V < 0 || V > (1 << 30) || (T > 1 && (logits->ld < V || dlogits->ld < V))) return SP_ERR_SHAPE;
+  if (dlogits->rows != T || dlogits->cols != V) return SP_ERR_SHAPE;
+  if (!positive_finite(scale) || (!g_logp && !g_entropy)) return SP_ERR_INVALID_ARG;
+  if (T == 0) return SP_OK;
+  const int n = 16 / (int)dtype_size(logits->dtype);
+  const int64_t chunks = ceil_div(ceil_div(V, (int64_t)n), (int64_t)kLossThreads * kGradVecs);
+  if (V < 1 || T > 0x7fffffff || T * chunks > 0x7fffffff) return SP_ERR_SHAPE;
+  if (!logits->ptr || !dlogits->ptr || !lse || (g_logp && !targets) || (g_entropy && !entropy)) return SP_ERR_INVALID_ARG;
+  // the same values at another pitch would be overwritten before they are read
+  if (logits->ptr == dlogits->ptr && T > 1 && logits->ld != dlogits->ld) return SP_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const GradParams p{logits->ptr, dlogits->ptr, logits->ld, dlogits->ld, T, (int32_t)V, (int32_t)chunks, (float)scale,
+                     targets, lse, entropy, g_logp, g_entropy};
+  count_launch();
+  ProfScope prof(PK_ELEMENTWISE, 0.0, 2.0 * T * V * dtype_size(logits->dtype), s);
+  const dim3 grid((unsigned)(T * chunks));
+  const cudaError_t e = logits->dtype == SP_F32
+                            ? launch(token_logprobs_grad_kernel<float>, grid, dim3(kLossThreads), 0, s, p)
+                            : launch(token_logprobs_grad_kernel<__nv_bfloat16>, grid, dim3(kLossThreads), 0, s, p);
+  return e == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+}
+
+}  // extern "C"

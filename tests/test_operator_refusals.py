@@ -1,0 +1,69 @@
+"""What sp_token_logprobs and sp_token_logprobs_grad refuse, on the host and before any launch: the pointers below are never
+followed."""
+import ctypes as C
+
+import pytest
+
+from paper_2510_03246_b200 import api, build
+
+F32, BF16, F64 = api.SP_F32, api.SP_BF16, api.SP_F64
+OK, INVALID, SHAPE, DTYPE, ALIGN, WORKSPACE, UNSUPPORTED = 0, 1, 2, 3, 4, 5, 9
+P = 0x1000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return api.lib()
+
+
+def m(rows, cols, dtype=F32, ld=None, ptr=P):
+    return api.SpMat(ptr, dtype, 0, rows, cols, cols if ld is None else ld)
+
+
+def logprobs(lib, x, targets=P, scale=1.0, n_alts=0, logp=P, lse=P, entropy=None, ids=None, alts=None):
+    return lib.sp_token_logprobs(C.byref(x), targets, scale, n_alts, logp, lse, entropy, ids, alts, None, None)
+
+
+def test_logprob_refusals(lib):
+    assert lib.sp_token_logprobs(None, P, 1.0, 0, P, P, None, None, None, None, None) == INVALID
+    assert logprobs(lib, m(4, 100, F64)) == DTYPE
+    assert logprobs(lib, m(4, 100, ld=99)) == SHAPE and logprobs(lib, m(-1, 100)) == SHAPE
+    assert logprobs(lib, m(4, 0)) == SHAPE and logprobs(lib, m(4, (1 << 30) + 1)) == SHAPE
+    assert logprobs(lib, m(1 << 29, 10)) == SHAPE
+    for n in (-1, 33):
+        assert logprobs(lib, m(4, 100), n_alts=n, ids=P) == SHAPE
+    assert logprobs(lib, m(4, 3), n_alts=4, ids=P) == SHAPE                    # more alternatives than logits
+    assert logprobs(lib, m(4, 100), n_alts=2) == INVALID and logprobs(lib, m(4, 100), ids=P) == INVALID
+    for scale in (0.0, -2.0, float("nan"), float("inf")):
+        assert logprobs(lib, m(4, 100), scale=scale) == INVALID
+    assert logprobs(lib, m(4, 100), targets=None) == INVALID
+    assert logprobs(lib, m(4, 100), logp=None, lse=None) == INVALID
+    assert logprobs(lib, m(4, 100, ptr=None)) == INVALID
+    assert logprobs(lib, m(0, 100, ptr=None)) == OK
+
+
+def grad(lib, x, d, targets=P, scale=1.0, lse=P, entropy=P, gl=P, gh=None):
+    return lib.sp_token_logprobs_grad(C.byref(x), targets, scale, lse, entropy, gl, gh, C.byref(d), None)
+
+
+def test_gradient_refusals(lib):
+    x = m(4, 100)
+    assert lib.sp_token_logprobs_grad(None, P, 1.0, P, P, P, P, None, None) == INVALID
+    assert grad(lib, m(4, 100, F64), m(4, 100, F64)) == DTYPE and grad(lib, x, m(4, 100, BF16)) == DTYPE
+    assert grad(lib, x, m(4, 99)) == SHAPE and grad(lib, x, m(3, 100)) == SHAPE and grad(lib, x, m(4, 100, ld=10)) == SHAPE
+    assert grad(lib, x, x, gl=None) == INVALID and grad(lib, x, x, targets=None) == INVALID
+    assert grad(lib, x, x, lse=None) == INVALID and grad(lib, x, x, gh=P, entropy=None) == INVALID
+    assert grad(lib, x, m(4, 100, ptr=None)) == INVALID
+    assert grad(lib, x, m(4, 100, ld=104)) == INVALID                          # in place at another pitch
+    for scale in (0.0, -2.0, float("nan"), float("inf")):
+        assert grad(lib, x, x, scale=scale) == INVALID
+    assert grad(lib, m(0, 100, ptr=None), m(0, 100, ptr=None)) == OK
+
+
+def test_binding_refuses_cpu_tensors_in_logprobs(lib):
+    import torch
+    x = torch.zeros(4, 8)
+    for call in (lambda: api.sp_token_logprobs(x), lambda: api.sp_token_logprobs_grad(x, None, x[:, 0], x[:, 0])):
+        with pytest.raises(RuntimeError):
+            call()
