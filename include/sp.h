@@ -488,6 +488,26 @@ size_t sp_mha_value_refit_workspace_bytes(int64_t d, int64_t n_heads, int64_t T,
                                           int32_t dtype);
 
 /* ---------------------------------------------------------------------------------------------------------------
+ * sp_linear — a projection with what follows it in a layer, in one kernel:
+ *     Y = act(X W^T + bias) + other      (SP_COMBINE_ADD: residual)
+ *     Y = act(X W^T + bias) * other      (SP_COMBINE_MUL, elementwise: the other branch of a gated module)
+ * X: [T, in], W: [out, in], Y: [T, out], bias: fp32 [out] or NULL, other: [T, out] or NULL.  act: SP_LINEAR_NONE, _RELU
+ * (max(y, 0)), _SILU (y / (1 + e^-y)), _GELU (y Phi(y), Phi the normal distribution function).  X and W have one dtype
+ * (SP_BF16 or SP_F32); Y has it too or is SP_F32; other has Y's.  other may be Y itself (same pointer and ld); other
+ * overlaps of Y with an input are not allowed.
+ * bf16 mode: tensor cores, fp32 accumulation, one rounding at the end.  Needs leading dimensions of X and W that are multiples
+ * of 8 and 16-byte aligned pointers, else the CUDA cores serve, slower; in and out may be any numbers (a pruned module's
+ * k_keep).  fp32 mode: fp64 accumulation.
+ * The gradients of X W^T are plain products: dX = dY W, dW = dY^T X (sp_gemm, sp_gram_accumulate).
+ * Errors: SP_ERR_INVALID_ARG (null pointers, unknown act or combine), SP_ERR_SHAPE (sizes that do not match, ld too small,
+ * in < 1, T > 65535 * 64, in or out > 2^30), SP_ERR_DTYPE.  Time-outs of the tensor-core kernel through status_dev (may be NULL).
+ */
+typedef enum { SP_LINEAR_NONE = 0, SP_LINEAR_RELU = 1, SP_LINEAR_SILU = 2, SP_LINEAR_GELU = 3 } sp_linear_act;
+typedef enum { SP_COMBINE_ADD = 0, SP_COMBINE_MUL = 1 } sp_linear_combine;
+sp_status sp_linear(const sp_mat* X, const sp_mat* W, const float* bias, int32_t act, const sp_mat* other,
+                    int32_t combine, const sp_mat* Y, int32_t* status_dev, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
  * sp_token_logprobs, sp_token_logprobs_grad — how well a model predicts given tokens (the paper's measure, Section 4, is the
  * perplexity exp(-mean log p)), and the gradient of that.
  * With z = scale * logits (row by row):  lse = log sum_v e^z_v,  logp = z_target - lse,  entropy = -sum_v p_v log p_v with

@@ -22,6 +22,8 @@ SP_ACT_RELU, SP_ACT_SWIGLU = 0, 1
 SP_Z_PAPER, SP_Z_EXACT = 0, 1
 SP_SCORE_WANDA_L2, SP_SCORE_WANDA_L1, SP_SCORE_LEMMA1 = 0, 1, 2
 SP_ALLOC_SOFTMAX, SP_ALLOC_INVERSE, SP_ALLOC_UNIFORM = 0, 1, 2
+SP_LINEAR_NONE, SP_LINEAR_RELU, SP_LINEAR_SILU, SP_LINEAR_GELU = 0, 1, 2, 3
+SP_COMBINE_ADD, SP_COMBINE_MUL = 0, 1
 SP_MAX_ALTS = 32
 (SP_WS_GRAM, SP_WS_ADMM_STEP, SP_WS_SCORES, SP_WS_APPLY_MASK, SP_WS_FFN_INIT, SP_WS_LINEAR_REFIT, SP_WS_GEMM,
  SP_WS_RIDGE_SOLVE) = range(8)
@@ -35,7 +37,7 @@ EXPORTS = ["sp_gram_accumulate", "sp_ffn_init", "sp_admm_step", "sp_admm_scores"
            "sp_set_reproducible", "sp_get_reproducible", "sp_allocate_sparsity_grid", "sp_apply_mask_global",
            "sp_apply_mask_global_bytes", "sp_objective_accumulate", "sp_ffn_cache_input_inverse",
            "sp_set_wait_budget", "sp_mha_value_refit", "sp_mha_value_refit_workspace_bytes",
-           "sp_token_logprobs", "sp_token_logprobs_grad"]
+           "sp_linear", "sp_token_logprobs", "sp_token_logprobs_grad"]
 
 
 class SpError(RuntimeError):
@@ -143,6 +145,7 @@ def lib() -> C.CDLL:
         L.sp_apply_mask_global_bytes.restype = C.c_size_t
         L.sp_apply_mask_global_bytes.argtypes = [i64, i32]
         L.sp_objective_accumulate.argtypes = [vp, dbl, vp, i32, vp]
+        L.sp_linear.argtypes = [pm, pm, vp, i32, pm, i32, pm, vp, vp]
         L.sp_token_logprobs.argtypes = [pm, vp, dbl, i32, vp, vp, vp, vp, vp, vp, vp]
         L.sp_token_logprobs_grad.argtypes = [pm, vp, dbl, vp, vp, vp, vp, pm, vp]
         L.sp_set_reproducible.argtypes = [i32]
@@ -475,6 +478,33 @@ def _dtype_of(t, what):
     if t.dim() != 2 or t.dtype not in _DTYPES or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{what} must be a row-major 2-D tensor of fp32 or bf16")
     return _DTYPES[t.dtype]
+
+
+def rows_of_16_bytes(rows, cols, dtype, device):
+    """Uninitialised [rows, cols] whose rows start on 16 bytes (a view of a wider buffer where cols needs it): the layout
+    that the tensor-core kernels read, for widths such as a pruned module's k_keep."""
+    per = 16 // torch.empty(0, dtype=dtype).element_size()
+    return torch.empty(rows, (cols + per - 1) // per * per, dtype=dtype, device=device)[:, :cols]
+
+
+def sp_linear(X, W, bias=None, act=SP_LINEAR_NONE, other=None, combine=SP_COMBINE_ADD, out=None, out_dtype=None,
+              status=None):
+    """act(X W^T + bias), then other added or multiplied (see sp.h).  X [T, in], W [out, in] of one dtype; bias fp32 [out].
+    out may be `other` itself.  A result allocated here has rows that start on 16 bytes (rows_of_16_bytes)."""
+    _on_one_device(X, W, bias, other, out, status)
+    for name, t in (("X", X), ("W", W), ("other", other), ("out", out)):
+        if t is not None:
+            _dtype_of(t, name)
+    n = W.shape[0]
+    _vector(bias, torch.float32, n, "bias")
+    _vector(status, torch.int32, 4, "status")
+    if out is None:
+        out = rows_of_16_bytes(X.shape[0], n, out_dtype or X.dtype, X.device)
+    x, w, y = mat(X), mat(W), mat(out)
+    o = mat(other) if other is not None else None
+    _check(lib().sp_linear(C.byref(x), C.byref(w), _ptr(bias), int(act), C.byref(o) if o is not None else None,
+                           int(combine), C.byref(y), _ptr(status), _stream()), "sp_linear")
+    return out
 
 
 @dataclass

@@ -464,6 +464,41 @@ sp_status sp_gemm(int32_t transA, int32_t transB, int64_t M, int64_t N, int64_t 
   return contract(M, N, K, alpha, a, a_kmajor, b, b_kmajor, beta, c, c, lower_only != 0, acc64, false, status_dev, s);
 }
 
+sp_status sp_linear(const sp_mat* X, const sp_mat* W, const float* bias, int32_t act, const sp_mat* other,
+                    int32_t combine, const sp_mat* Y, int32_t* status_dev, void* stream) {
+  if (!X || !W || !Y) return SP_ERR_INVALID_ARG;
+  if (act < SP_LINEAR_NONE || act > SP_LINEAR_GELU) return SP_ERR_INVALID_ARG;
+  if (combine != SP_COMBINE_ADD && combine != SP_COMBINE_MUL) return SP_ERR_INVALID_ARG;
+  if (!valid_act_dtype(X->dtype) || W->dtype != X->dtype) return SP_ERR_DTYPE;
+  if (Y->dtype != X->dtype && Y->dtype != SP_F32) return SP_ERR_DTYPE;
+  if (other && other->dtype != Y->dtype) return SP_ERR_DTYPE;
+  const int64_t T = X->rows, K = X->cols, N = W->rows;
+  if (T < 0 || N < 0 || K < 1 || W->cols != K || Y->rows != T || Y->cols != N) return SP_ERR_SHAPE;
+  if (other && (other->rows != T || other->cols != N)) return SP_ERR_SHAPE;
+  // (rows: the CUDA-core forms have a block row per 64 of them; 2^30: the extents of a tensor map and the tile counts)
+  if (T > 65535 * 64 || N > (1 << 30) || K > (1 << 30) || ceil_div(T, (int64_t)128) * ceil_div(N, (int64_t)128) > 0x7fffffff)
+    return SP_ERR_SHAPE;
+  if ((T > 1 && (X->ld < K || Y->ld < N || (other && other->ld < N))) || (N > 1 && W->ld < K)) return SP_ERR_SHAPE;
+  if (T == 0 || N == 0) return SP_OK;
+  if (!X->ptr || !W->ptr || !Y->ptr || (other && !other->ptr)) return SP_ERR_INVALID_ARG;
+  // (the same values at another pitch would be overwritten before they are read)
+  if (other && other->ptr == Y->ptr && T > 1 && other->ld != Y->ld) return SP_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  LinearEpi epi;
+  epi.bias = bias;
+  epi.act = act;
+  epi.combine = combine;
+  const Operand o = other ? Operand{other->ptr, other->dtype, other->ld, 1} : Operand{nullptr, Y->dtype, 0, 1};
+  const OutOperand y{Y->ptr, Y->dtype, Y->ld};
+  if (X->dtype == SP_BF16) {
+    TcOperand ta{X->ptr, X->ld, true}, tb{W->ptr, W->ld, true};
+    if (gemm_tc_supported(T, N, K, ta, tb))
+      return gemm_tc(T, N, K, 1.f, ta, tb, other ? 1.f : 0.f, o, y, false, status_dev, s, nullptr, -1.0, 0, nullptr, &epi);
+  }
+  CU(linear_simt(T, N, K, Operand{X->ptr, X->dtype, X->ld, 1}, Operand{W->ptr, W->dtype, W->ld, 1}, epi, o, y, s));
+  return SP_OK;
+}
+
 sp_status sp_symmetrize(float* G, int64_t n, int64_t ldg, void* stream) {
   if (!G) return SP_ERR_INVALID_ARG;
   if (n < 0 || ldg < n) return SP_ERR_SHAPE;

@@ -258,6 +258,31 @@ struct OutOperand {
   int64_t lo_off = 0;
 };
 
+// What follows a product in sp_linear: v -> act(v + bias[j]); the caller's `other` is then added or multiplied.
+struct LinearEpi {
+  const float* bias = nullptr;
+  int32_t act = SP_LINEAR_NONE, combine = SP_COMBINE_ADD;
+};
+#ifdef __CUDACC__
+__device__ __forceinline__ float linear_act(float v, int32_t act) {
+  if (act == SP_LINEAR_RELU) return v < 0.f ? 0.f : v;                 // (a NaN stays one)
+  if (act == SP_LINEAR_SILU) return v == -INFINITY ? 0.f : v / (1.f + __expf(-v));      // (-inf / inf is NaN)
+  // v Phi(v) with Phi(v) = erfc(-v / sqrt 2) / 2, which keeps its relative accuracy where Phi is small
+  if (act == SP_LINEAR_GELU) return v == -INFINITY ? 0.f : 0.5f * v * erfcf(-0.7071067811865476f * v);
+  return v;
+}
+__device__ __forceinline__ double linear_act(double v, int32_t act) {
+  if (act == SP_LINEAR_RELU) return v < 0.0 ? 0.0 : v;
+  if (act == SP_LINEAR_SILU) return v == -INFINITY ? 0.0 : v / (1.0 + exp(-v));
+  if (act == SP_LINEAR_GELU) return v == -INFINITY ? 0.0 : 0.5 * v * erfc(-0.70710678118654752440 * v);
+  return v;
+}
+template <typename Acc>
+__device__ __forceinline__ Acc linear_combine(Acc v, Acc other, int32_t combine) {
+  return combine == SP_COMBINE_MUL ? v * other : v + other;
+}
+#endif
+
 // C[M,N] (row-major) = alpha * sum_k A(i,k) B(k,j) + beta * Cin[i,j].  Cin may alias C or be another matrix of
 // another dtype; beta == 0 never reads Cin.  lower_only skips tiles that lie strictly above the diagonal.
 // acc64: accumulate in fp64 (else fp32).  k_tri: B(k, j) = 0 for k < j and (kTriBoth) A(i, k) = 0 for k < i, so that a tile may
@@ -265,6 +290,9 @@ struct OutOperand {
 constexpr int kTriBoth = 1, kTriColumns = 2;
 cudaError_t gemm_simt(int64_t M, int64_t N, int64_t K, double alpha, Operand A, Operand B, double beta,
                       Operand Cin, OutOperand C, bool lower_only, bool acc64, cudaStream_t stream, int k_tri = 0);
+// C = act(A W^T + bias), then (+ or *) other unless other.ptr is null: A [M,K], W [N,K], K contiguous in both, bf16 or fp32.
+cudaError_t linear_simt(int64_t M, int64_t N, int64_t K, Operand A, Operand W, const LinearEpi& epi, Operand other, OutOperand C,
+                        cudaStream_t stream);
 
 // tcgen05 path: bf16 operands, fp32 accumulation in tensor memory.
 //   a_kmajor: A is stored [M, K] row-major (K contiguous) ; else [K, M] row-major (M contiguous).
@@ -310,7 +338,8 @@ constexpr int64_t kTcTileRows = 256;
 sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcOperand B, float beta, Operand Cin,
                   OutOperand C, bool lower_only, int32_t* status_dev, cudaStream_t stream,
                   const TcSegments* segs = nullptr, double alg_flops = -1.0, int max_pairs = 0,
-                  const TcBatch* batch = nullptr);
+                  const TcBatch* batch = nullptr, const LinearEpi* lin = nullptr);
+// lin: C = act(A B + bias), then (+ or *) Cin when beta is not 0 (alpha = 1, beta = 0 or 1; neither batched nor lower_only).
 bool gemm_tc_supported(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand B);
 
 struct SolveAssist;

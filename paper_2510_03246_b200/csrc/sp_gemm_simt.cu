@@ -28,10 +28,11 @@ __device__ __forceinline__ void store_elem(void* p, int32_t dt, int64_t idx, Acc
 
 constexpr int BK = 16;
 
-template <typename Acc, int BM, int BN, int TM, int TN>
+// LIN: what follows the product is LinearEpi's, and `beta` only tells whether there is a Cin to combine with
+template <typename Acc, int BM, int BN, int TM, int TN, bool LIN = false>
 __global__ void __launch_bounds__((BM / TM) * (BN / TN))
 gemm_simt_kernel(int64_t M, int64_t N, int64_t K, Acc alpha, Operand A, Operand B, Acc beta, Operand Cin,
-                 OutOperand C, int lower_only) {
+                 OutOperand C, int lower_only, LinearEpi epi) {
   kernel_begin();
   constexpr int NT = (BM / TM) * (BN / TN);
   constexpr int EA = BM * BK / NT;
@@ -120,7 +121,11 @@ gemm_simt_kernel(int64_t M, int64_t N, int64_t K, Acc alpha, Operand A, Operand 
       const int64_t gj = col0 + tx * TN + j;
       if (gj >= N) continue;
       Acc v = alpha * acc[i][j];
-      if (beta != (Acc)0) v += beta * load_elem<Acc>(Cin.ptr, Cin.dtype, gi * Cin.s0 + gj * Cin.s1);
+      if constexpr (LIN) {
+        v = linear_act(epi.bias ? v + (Acc)epi.bias[gj] : v, epi.act);
+        if (beta != (Acc)0)
+          v = linear_combine(v, load_elem<Acc>(Cin.ptr, Cin.dtype, gi * Cin.s0 + gj * Cin.s1), epi.combine);
+      } else if (beta != (Acc)0) v += beta * load_elem<Acc>(Cin.ptr, Cin.dtype, gi * Cin.s0 + gj * Cin.s1);
       store_elem<Acc>(C.ptr, C.dtype, gi * C.ld + gj, v);
     }
   }
@@ -187,10 +192,10 @@ struct DmmaSlab {
   }
 };
 
-template <typename T, bool A_KFAST, bool B_KFAST, int BM>
+template <typename T, bool A_KFAST, bool B_KFAST, int BM, bool LIN = false>
 __global__ void __launch_bounds__(DM_THREADS, 3)
 gemm_dmma_kernel(int64_t M, int64_t N, int64_t K, double alpha, const T* A, int64_t lda,
-                 const T* B, int64_t ldb, double beta, Operand Cin, OutOperand C, int lower_only, int k_tri) {
+                 const T* B, int64_t ldb, double beta, Operand Cin, OutOperand C, int lower_only, int k_tri, LinearEpi epi) {
   kernel_begin();
   using SlabA = DmmaSlab<T, A_KFAST, BM>;
   using SlabB = DmmaSlab<T, B_KFAST, DM_BN>;
@@ -285,7 +290,11 @@ gemm_dmma_kernel(int64_t M, int64_t N, int64_t K, double alpha, const T* A, int6
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           o[q] = alpha * acc[i][j][2 * h + q];
-          if (beta != 0.0) o[q] += beta * v[j][q];
+          if constexpr (LIN) {
+            if (epi.bias && gj + q < N) o[q] += (double)epi.bias[gj + q];
+            o[q] = linear_act(o[q], epi.act);
+            if (beta != 0.0) o[q] = linear_combine(o[q], v[j][q], epi.combine);
+          } else if (beta != 0.0) o[q] += beta * v[j][q];
         }
         if (vc && gj + 2 <= N && C.dtype != SP_BF16) {
           if (c64) *reinterpret_cast<double2*>(reinterpret_cast<double*>(C.ptr) + gi * C.ld + gj) = make_double2(o[0], o[1]);
@@ -447,10 +456,10 @@ void launch_dmma(int64_t M, int64_t N, int64_t K, double alpha, const Operand& A
   const T* a = reinterpret_cast<const T*>(A.ptr);
   const T* b = reinterpret_cast<const T*>(B.ptr);
   const int lo = lower_only ? 1 : 0;
-  if (ak && bk) launch(gemm_dmma_kernel<T, true, true, BM>, grid, DM_THREADS, 0, stream, M, N, K, alpha, a, lda, b, ldb, beta, Cin, C, lo, tri);
-  else if (ak) launch(gemm_dmma_kernel<T, true, false, BM>, grid, DM_THREADS, 0, stream, M, N, K, alpha, a, lda, b, ldb, beta, Cin, C, lo, tri);
-  else if (bk) launch(gemm_dmma_kernel<T, false, true, BM>, grid, DM_THREADS, 0, stream, M, N, K, alpha, a, lda, b, ldb, beta, Cin, C, lo, tri);
-  else launch(gemm_dmma_kernel<T, false, false, BM>, grid, DM_THREADS, 0, stream, M, N, K, alpha, a, lda, b, ldb, beta, Cin, C, lo, tri);
+  if (ak && bk) launch(gemm_dmma_kernel<T, true, true, BM>, grid, DM_THREADS, 0, stream, M, N, K, alpha, a, lda, b, ldb, beta, Cin, C, lo, tri, LinearEpi{});
+  else if (ak) launch(gemm_dmma_kernel<T, true, false, BM>, grid, DM_THREADS, 0, stream, M, N, K, alpha, a, lda, b, ldb, beta, Cin, C, lo, tri, LinearEpi{});
+  else if (bk) launch(gemm_dmma_kernel<T, false, true, BM>, grid, DM_THREADS, 0, stream, M, N, K, alpha, a, lda, b, ldb, beta, Cin, C, lo, tri, LinearEpi{});
+  else launch(gemm_dmma_kernel<T, false, false, BM>, grid, DM_THREADS, 0, stream, M, N, K, alpha, a, lda, b, ldb, beta, Cin, C, lo, tri, LinearEpi{});
 }
 
 }  // namespace
@@ -483,14 +492,32 @@ cudaError_t gemm_simt(int64_t M, int64_t N, int64_t K, double alpha, Operand A, 
     constexpr int BM = 64, BN = 64;
     dim3 grid((unsigned)ceil_div(N, BN), (unsigned)ceil_div(M, BM));
     launch(gemm_simt_kernel<double, BM, BN, 4, 4>, grid, 256, 0, stream, M, N, K, alpha, A, B, beta, Cin, C,
-                                                                      lower_only ? 1 : 0);
+                                                                      lower_only ? 1 : 0, LinearEpi{});
   } else {
     constexpr int BM = 128, BN = 128;
     dim3 grid((unsigned)ceil_div(N, BN), (unsigned)ceil_div(M, BM));
     launch(gemm_simt_kernel<float, BM, BN, 8, 8>, grid, 256, 0, stream, M, N, K, (float)alpha, A, B, (float)beta, Cin, C,
-                                                                     lower_only ? 1 : 0);
+                                                                     lower_only ? 1 : 0, LinearEpi{});
   }
   return cudaGetLastError();
+}
+
+cudaError_t linear_simt(int64_t M, int64_t N, int64_t K, Operand A, Operand W, const LinearEpi& epi, Operand other, OutOperand C,
+                        cudaStream_t stream) {
+  if (M <= 0 || N <= 0) return cudaSuccess;
+  count_launch();
+  ProfScope prof(PK_GEMM_SIMT, 2.0 * (double)M * (double)N * (double)K, 0.0, stream);
+  const double beta = other.ptr ? 1.0 : 0.0;
+  if (A.dtype == SP_F32) {
+    const float *a = reinterpret_cast<const float*>(A.ptr), *w = reinterpret_cast<const float*>(W.ptr);
+    if (ceil_div(M, 64) * ceil_div(N, (int64_t)DM_BN) < sm_count())
+      return launch(gemm_dmma_kernel<float, true, true, 32, true>, dim3((unsigned)ceil_div(N, DM_BN), (unsigned)ceil_div(M, 32)),
+                    DM_THREADS, 0, stream, M, N, K, 1.0, a, A.s0, w, W.s0, beta, other, C, 0, 0, epi);
+    return launch(gemm_dmma_kernel<float, true, true, 64, true>, dim3((unsigned)ceil_div(N, DM_BN), (unsigned)ceil_div(M, 64)),
+                  DM_THREADS, 0, stream, M, N, K, 1.0, a, A.s0, w, W.s0, beta, other, C, 0, 0, epi);
+  }
+  return launch(gemm_simt_kernel<float, 128, 128, 8, 8, true>, dim3((unsigned)ceil_div(N, 128), (unsigned)ceil_div(M, 128)), 256, 0,
+                stream, M, N, K, 1.f, A, Operand{W.ptr, W.dtype, 1, W.s0}, (float)beta, other, C, 0, epi);
 }
 
 }  // namespace sp

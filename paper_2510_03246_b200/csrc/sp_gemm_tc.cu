@@ -91,6 +91,7 @@ struct TcParams {
   long long wait_budget;   // clock cycles a role may wait on one barrier before it gives up (SP_ERR_TIMEOUT)
   int32_t* status;
   const int32_t* skip;     // conditional launch: every CTA returns at once when *skip != 0 (see SkipScope)
+  LinearEpi lin;           // sp_linear's epilogue (the LIN form of the kernel only)
 };
 
 struct Coord5 {
@@ -199,6 +200,19 @@ __device__ __forceinline__ void tc_commit_local(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// act(acc + bias) of a 32-column block: lane l fetches the bias of column gj0 + l, every lane needs all 32.
+__device__ __forceinline__ void linear_block(const TcParams& p, int64_t gj0, uint32_t (&r)[32]) {
+  const int lane = threadIdx.x & 31;
+  if (p.lin.bias) {
+    const float b = gj0 + lane < p.N ? p.lin.bias[gj0 + lane] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __shfl_sync(0xffffffffu, b, i));
+  }
+  if (p.lin.act == SP_LINEAR_NONE) return;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(linear_act(__uint_as_float(r[i]), p.lin.act));
+}
+
 // BATCHED = false is the plain two-dimensional form (the products of the FFN path); BATCHED = true adds the batch
 // and plane coordinates (five-dimensional tensor maps).  Two instantiations, so that the plain form carries none of
 // the batched form's instructions.
@@ -206,7 +220,9 @@ __device__ __forceinline__ void tc_commit_local(uint32_t bar) {
 // main loop (0.3 us per 64 values of K at 256 columns) and epilogue are the whole time (3072 x 256, K = 768: 11.1 -> 9.9 us;
 // 256 x 256, K = 64: 7.2 -> 5.9), and for products of at most 128 columns, which the wide tile would do twice over with
 // zeros.  The sum over K runs in the same order either way.
-template <bool BATCHED, int TN>
+// LIN: sp_linear's epilogue, act(acc + bias) and then Cin added or multiplied, in each of the epilogue's forms; an instantiation of its
+// own, so that the others carry none of its instructions.
+template <bool BATCHED, int TN, bool LIN = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmCin, const TcParams p) {
@@ -428,6 +444,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           uint32_t r[32];
           tc_ld32(taddr + (uint32_t)(sl * 32), r);
           tc_wait_ld();
+          if constexpr (LIN) linear_block(p, gj0, r);
           if (rows_ok) {
             if (lane == 0 && sl + 1 < nsl) {     // next block of Cin into the other half (its last reader is done)
               fence_async_smem();
@@ -450,8 +467,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const __nv_bfloat162 c2 = *reinterpret_cast<const __nv_bfloat162*>(&cwv[e]);
-                const float v0 = fmaf(p.beta, __low2float(c2), p.alpha * __uint_as_float(r[8 * j + 2 * e]));
-                const float v1 = fmaf(p.beta, __high2float(c2), p.alpha * __uint_as_float(r[8 * j + 2 * e + 1]));
+                float v0, v1;
+                if constexpr (LIN) {
+                  v0 = linear_combine(__uint_as_float(r[8 * j + 2 * e]), __low2float(c2), p.lin.combine);
+                  v1 = linear_combine(__uint_as_float(r[8 * j + 2 * e + 1]), __high2float(c2), p.lin.combine);
+                } else {
+                  v0 = fmaf(p.beta, __low2float(c2), p.alpha * __uint_as_float(r[8 * j + 2 * e]));
+                  v1 = fmaf(p.beta, __high2float(c2), p.alpha * __uint_as_float(r[8 * j + 2 * e + 1]));
+                }
                 const __nv_bfloat162 o2 = __floats2bfloat162_rn(v0, v1);
                 ow[e] = *reinterpret_cast<const uint32_t*>(&o2);
               }
@@ -480,6 +503,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           uint32_t r[32];
           tc_ld32(taddr + (uint32_t)c0, r);
           tc_wait_ld();
+          if constexpr (LIN) linear_block(p, gj0, r);
           if (lane == 0) bulk_wait_read_1();      // the copies that last read this half (two blocks ago) are done
           __syncwarp();
           uint8_t* out_row = wstg_ptr + buf * 4096 + lane * 64;
@@ -527,6 +551,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           uint32_t r[32];
           tc_ld32(taddr + (uint32_t)c0, r);
           tc_wait_ld();
+          if constexpr (LIN) linear_block(p, gj0, r);
           if (lane == 0) bulk_wait_read_1();      // the copy that last read this tile (two blocks ago) is done
           __syncwarp();
           uint8_t* tile = wstg_ptr + buf * 4096 + lane * 128;
@@ -579,6 +604,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           uint32_t r[32];
           tc_ld32(taddr + (uint32_t)c0, r);
           tc_wait_ld();
+          if constexpr (LIN) linear_block(p, gj0, r);
 #pragma unroll
           for (int i = 0; i < 32; ++i) stg[lane][i] = p.alpha * __uint_as_float(r[i]);
           __syncwarp();
@@ -588,7 +614,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             for (int rr = 0; rr < 32; ++rr) {
               if (rr < rows_here) {
                 float v = stg[rr][lane];
-                if (has_cin) v = fmaf(p.beta, cv[rr], v);
+                if (has_cin) v = LIN ? linear_combine(v, cv[rr], p.lin.combine) : fmaf(p.beta, cv[rr], v);
                 const int64_t o = c_off + (int64_t)rr * p.c_ld;
                 if (c_f32) {
                   reinterpret_cast<float*>(p.c)[o] = v;
@@ -731,8 +757,9 @@ bool gemm_tc_supported(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand B
 
 sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcOperand B, float beta, Operand Cin,
                   OutOperand C, bool lower_only, int32_t* status_dev, cudaStream_t stream, const TcSegments* segs,
-                  double alg_flops, int max_pairs, const TcBatch* batch) {
+                  double alg_flops, int max_pairs, const TcBatch* batch, const LinearEpi* lin) {
   const bool batched = batch != nullptr;
+  if (lin && (batched || lower_only || segs || alpha != 1.f || (beta != 0.f && beta != 1.f))) return SP_ERR_INVALID_ARG;
   if (batched && (batch->nb0 < 1 || batch->nb1 < 1 || batch->a_planes < 1 || batch->b_planes < 1))
     return SP_ERR_INVALID_ARG;
   TcSegments sg;
@@ -762,7 +789,7 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
   // below), and for a lower triangle only where one wide tile covers all columns, so that the same entries are written.
   const int64_t wide_tiles = ceil_div(M, (int64_t)TILE_M) * ceil_div(N, (int64_t)TILE_N) *
                              (batched ? (int64_t)batch->nb0 * batch->nb1 : 1);
-  const bool narrow = (batched || num_kb < kMinCutKb * 2) && (!lower_only || N <= TILE_N) &&
+  const bool narrow = (batched || lin || num_kb < kMinCutKb * 2) && (!lower_only || N <= TILE_N) &&
                       (N <= kNarrowN || 2 * wide_tiles <= pairs_max);
   const int tile_n = narrow ? kNarrowN : TILE_N;
 
@@ -822,7 +849,8 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
   bool c_tma = C.dtype == SP_F32 && C.ld % 4 == 0 && N % 4 == 0 && (reinterpret_cast<uintptr_t>(C.ptr) & 15u) == 0;
   if (batched && ((batch->nb0 > 1 && batch->c_s0 % 4 != 0) || (batch->nb1 > 1 && batch->c_s1 % 4 != 0))) c_tma = false;
   if (c_tma && beta == 0.f) p.epi_mode = EPI_TMA_STORE;
-  if (c_tma && beta == 1.f && Cin.ptr == C.ptr && Cin.dtype == SP_F32 && Cin.s0 == C.ld &&
+  if (lin) p.lin = *lin;
+  if (!lin && c_tma && beta == 1.f && Cin.ptr == C.ptr && Cin.dtype == SP_F32 && Cin.s0 == C.ld &&
       (!batched || (batch->cin_s0 == batch->c_s0 && batch->cin_s1 == batch->c_s1)))
     p.epi_mode = EPI_TMA_ADD;
   if (p.epi_mode != EPI_DIRECT) {
@@ -885,7 +913,7 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
   // order that is not fixed, so the last bits of such sums can differ between runs).  A plain store into an fp32 C
   // is turned into "clear C, then accumulate" when that pays.
   p.ksplit = 1;
-  const bool may_cut = !batched && !reproducible_mode();   // partial products of a cut tile add in no fixed order
+  const bool may_cut = !batched && !lin && !reproducible_mode();   // partial products of a cut tile add in no fixed order
   if (may_cut && (p.epi_mode == EPI_TMA_STORE || p.epi_mode == EPI_TMA_ADD) && p.num_tiles > 0) {
     auto eff = [&](int ks) {
       const double u = (double)p.num_tiles * ks;
@@ -927,7 +955,8 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
   static PerDeviceOnce attr_once;
   if (attr_once.run([] {
         for (auto k : {gemm_tc_kernel<false, TILE_N>, gemm_tc_kernel<true, TILE_N>, gemm_tc_kernel<false, kNarrowN>,
-                       gemm_tc_kernel<true, kNarrowN>}) {
+                       gemm_tc_kernel<true, kNarrowN>, gemm_tc_kernel<false, TILE_N, true>,
+                       gemm_tc_kernel<false, kNarrowN, true>}) {
           const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES);
           if (e != cudaSuccess) return e;
         }
@@ -942,7 +971,8 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
   ProfScope prof(p.skip != nullptr ? PK_CONDITIONAL : max_pairs > 0 ? PK_GEMM_TC_SHARED : PK_GEMM_TC,
                  p.skip != nullptr ? 0.0 : flops, 0.0, stream);
   const int pairs = p.num_units < pairs_max ? p.num_units : pairs_max;
-  const auto kernel = batched ? (narrow ? gemm_tc_kernel<true, kNarrowN> : gemm_tc_kernel<true, TILE_N>)
+  const auto kernel = lin     ? (narrow ? gemm_tc_kernel<false, kNarrowN, true> : gemm_tc_kernel<false, TILE_N, true>)
+                      : batched ? (narrow ? gemm_tc_kernel<true, kNarrowN> : gemm_tc_kernel<true, TILE_N>)
                               : (narrow ? gemm_tc_kernel<false, kNarrowN> : gemm_tc_kernel<false, TILE_N>);
   // (programmatic launch only for one wave of tiles with the GPU to itself, see launch())
   if (p.num_units <= pairs && max_pairs == 0) launch(kernel, 2 * pairs, NUM_THREADS, SMEM_BYTES, stream, tmA, tmB, tmC, tmCin, p);

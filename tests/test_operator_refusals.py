@@ -1,4 +1,4 @@
-"""What sp_token_logprobs and sp_token_logprobs_grad refuse, on the host and before any launch: the pointers below are never
+"""What sp_linear, sp_token_logprobs and sp_token_logprobs_grad refuse, on the host and before any launch: the pointers below are never
 followed."""
 import ctypes as C
 
@@ -19,6 +19,29 @@ def lib():
 
 def m(rows, cols, dtype=F32, ld=None, ptr=P):
     return api.SpMat(ptr, dtype, 0, rows, cols, cols if ld is None else ld)
+
+
+def linear(lib, X=None, W=None, other=None, Y=None, bias=None, act=0, combine=0):
+    X, W, Y = X or m(10, 64), W or m(32, 64), Y or m(10, 32)
+    return lib.sp_linear(C.byref(X), C.byref(W), bias, act, C.byref(other) if other else None, combine, C.byref(Y), None, None)
+
+
+def test_linear_refusals(lib):
+    assert lib.sp_linear(None, None, None, 0, None, 0, None, None, None) == INVALID
+    assert linear(lib, act=4) == INVALID and linear(lib, act=-1) == INVALID
+    assert linear(lib, combine=2) == INVALID and linear(lib, combine=-1) == INVALID
+    assert linear(lib, X=m(10, 64, F64)) == DTYPE and linear(lib, W=m(32, 64, BF16)) == DTYPE
+    assert linear(lib, Y=m(10, 32, BF16)) == DTYPE and linear(lib, other=m(10, 32, BF16)) == DTYPE
+    assert linear(lib, W=m(32, 63)) == SHAPE and linear(lib, Y=m(9, 32)) == SHAPE and linear(lib, Y=m(10, 31)) == SHAPE
+    assert linear(lib, other=m(10, 31)) == SHAPE and linear(lib, other=m(9, 32)) == SHAPE
+    assert linear(lib, X=m(10, 64, ld=63)) == SHAPE and linear(lib, W=m(32, 64, ld=10)) == SHAPE
+    assert linear(lib, Y=m(10, 32, ld=31)) == SHAPE and linear(lib, other=m(10, 32, ld=31)) == SHAPE
+    assert linear(lib, X=m(10, 0), W=m(32, 0)) == SHAPE
+    assert linear(lib, X=m((1 << 22) + 1, 64), Y=m((1 << 22) + 1, 32)) == SHAPE
+    assert linear(lib, X=m(10, 64, ptr=None)) == INVALID and linear(lib, W=m(32, 64, ptr=None)) == INVALID
+    assert linear(lib, Y=m(10, 32, ptr=None)) == INVALID and linear(lib, other=m(10, 32, ptr=None)) == INVALID
+    assert linear(lib, other=m(10, 32, ld=40), Y=m(10, 32, ld=48)) == INVALID  # the same values at another pitch
+    assert linear(lib, X=m(0, 64, ptr=None), Y=m(0, 32, ptr=None)) == OK
 
 
 def logprobs(lib, x, targets=P, scale=1.0, n_alts=0, logp=P, lse=P, entropy=None, ids=None, alts=None):
@@ -59,6 +82,12 @@ def test_gradient_refusals(lib):
     for scale in (0.0, -2.0, float("nan"), float("inf")):
         assert grad(lib, x, x, scale=scale) == INVALID
     assert grad(lib, m(0, 100, ptr=None), m(0, 100, ptr=None)) == OK
+
+
+def test_binding_refuses_cpu_tensors_in_linear(lib):
+    import torch
+    with pytest.raises(RuntimeError):
+        api.sp_linear(torch.zeros(4, 8), torch.zeros(4, 8))
 
 
 def test_binding_refuses_cpu_tensors_in_logprobs(lib):
