@@ -488,6 +488,42 @@ size_t sp_mha_value_refit_workspace_bytes(int64_t d, int64_t n_heads, int64_t T,
                                           int32_t dtype);
 
 /* ---------------------------------------------------------------------------------------------------------------
+ * sp_attention — attention forward over packed sequences: the head outputs of a calibration set (the input of the W_O
+ * recovery and of the head scores) or of a text to be scored, without the probabilities that sp_mha_init keeps.
+ *   Sequence s holds query rows [cu_q[s], cu_q[s+1]) and key rows [cu_k[s], cu_k[s+1]).  With n_q and n_k their numbers,
+ *   g = n_heads / n_kv_heads and query head h reading key / value head h / g:
+ *     O_i = sum_j p_ij V_j,  p_ij = exp(scale <Q_i, K_j> - lse_i),  lse_i = log sum_j exp(scale <Q_i, K_j>),
+ *   the sums over the sequence's keys (causal == 0) or over its keys j <= i + n_k - n_q (causal != 0: the last query sees
+ *   every key, so that the next tokens of a text attend to those that are there already; n_q = n_k is the usual triangle,
+ *   n_q = 1 a single new token).  A query without a visible key gets O_i = 0 and lse_i = -infinity.
+ * Q, O: [Nq, n_heads * d_head], K, V: [Nk, n_kv_heads * d_head], token-major, head h owns columns [h d_head, ...); any
+ * leading dimension, so that Q, K, V may be column slices of one matrix.  One dtype for all four (SP_BF16 or SP_F32).
+ * O may not overlap Q, K or V.  lse: optional fp32 [Nq, n_heads], natural logarithm.
+ * cu_q, cu_k: int32 [n_seq + 1] on the DEVICE, not decreasing; entries outside [0, Nq] / [0, Nk] are taken as the nearest
+ * bound.  Rows of O and lse that belong to no sequence are left as they were, and what stands in rows of K and V outside a
+ * sequence does not reach it (infinities and NaN included).  Inside a sequence a NaN or an infinity in K or V at a key that the
+ * causal mask hides from some queries does not reach those either.
+ * Softmax and sums in fp32 in both modes; fp32 mode: products in fp32.  Equal calls give equal bits.
+ * Few rows: the keys of a sequence are cut into parts that run side by side and are joined by their lse; the workspace of
+ * sp_attention_workspace_bytes (0 when no cut is made) holds their results, scratch of this call alone (two calls that may
+ * overlap on the GPU need two).  status_dev may be NULL.
+ * Errors: SP_ERR_INVALID_ARG (null pointers, scale not positive and finite), SP_ERR_SHAPE (n_kv_heads does not divide
+ * n_heads, column counts, ld, n_seq < 0, more than 2^30 rows), SP_ERR_DTYPE, SP_ERR_UNSUPPORTED (d_head > 128),
+ * SP_ERR_WORKSPACE, SP_ERR_ALIGNMENT (workspace not 256-byte aligned).
+ */
+typedef struct {
+  sp_mat Q, K, V, O;
+  const int32_t* cu_q;
+  const int32_t* cu_k;
+  float* lse;              /* [Nq, n_heads] or NULL */
+  int32_t n_seq, n_heads, n_kv_heads, causal;
+  double scale;            /* usually 1 / sqrt(d_head) */
+} sp_attention_args;
+sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream);
+size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
+                                    int32_t d_head, int32_t dtype);
+
+/* ---------------------------------------------------------------------------------------------------------------
  * sp_linear — a projection with what follows it in a layer, in one kernel:
  *     Y = act(X W^T + bias) + other      (SP_COMBINE_ADD: residual)
  *     Y = act(X W^T + bias) * other      (SP_COMBINE_MUL, elementwise: the other branch of a gated module)

@@ -37,7 +37,7 @@ EXPORTS = ["sp_gram_accumulate", "sp_ffn_init", "sp_admm_step", "sp_admm_scores"
            "sp_set_reproducible", "sp_get_reproducible", "sp_allocate_sparsity_grid", "sp_apply_mask_global",
            "sp_apply_mask_global_bytes", "sp_objective_accumulate", "sp_ffn_cache_input_inverse",
            "sp_set_wait_budget", "sp_mha_value_refit", "sp_mha_value_refit_workspace_bytes",
-           "sp_linear", "sp_token_logprobs", "sp_token_logprobs_grad"]
+           "sp_attention", "sp_attention_workspace_bytes", "sp_linear", "sp_token_logprobs", "sp_token_logprobs_grad"]
 
 
 class SpError(RuntimeError):
@@ -90,6 +90,12 @@ class SpMhaState(C.Structure):
 class SpMhaParams(C.Structure):
     _fields_ = [("alpha", C.c_double), ("beta", C.c_double), ("a_steps", C.c_int32), ("z_steps", C.c_int32),
                 ("eta_z", C.c_double), ("causal", C.c_int32), ("reserved", C.c_int32), ("seq_chunk", C.c_int64)]
+
+
+class SpAttentionArgs(C.Structure):
+    _fields_ = [("Q", SpMat), ("K", SpMat), ("V", SpMat), ("O", SpMat), ("cu_q", C.c_void_p), ("cu_k", C.c_void_p),
+                ("lse", C.c_void_p), ("n_seq", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("causal", C.c_int32), ("scale", C.c_double)]
 
 
 REPORT_FIELDS = ["res_act", "res_out", "res_in", "z_sq", "a_sq", "rho1_eff", "rho2_eff", "kept", "factor_reused",
@@ -145,6 +151,9 @@ def lib() -> C.CDLL:
         L.sp_apply_mask_global_bytes.restype = C.c_size_t
         L.sp_apply_mask_global_bytes.argtypes = [i64, i32]
         L.sp_objective_accumulate.argtypes = [vp, dbl, vp, i32, vp]
+        L.sp_attention.argtypes = [C.POINTER(SpAttentionArgs), vp, vp, sz, vp]
+        L.sp_attention_workspace_bytes.restype = C.c_size_t
+        L.sp_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32, i32]
         L.sp_linear.argtypes = [pm, pm, vp, i32, pm, i32, pm, vp, vp]
         L.sp_token_logprobs.argtypes = [pm, vp, dbl, i32, vp, vp, vp, vp, vp, vp, vp]
         L.sp_token_logprobs_grad.argtypes = [pm, vp, dbl, vp, vp, vp, vp, pm, vp]
@@ -160,7 +169,7 @@ def lib() -> C.CDLL:
         for name in EXPORTS:
             if name not in ("sp_workspace_bytes", "sp_admm_overlap_bytes", "sp_mha_workspace_bytes",
                             "sp_mha_value_refit_workspace_bytes",
-                            "sp_apply_mask_global_bytes", "sp_status_string", "sp_version", "sp_profile_kinds",
+                            "sp_apply_mask_global_bytes", "sp_attention_workspace_bytes", "sp_status_string", "sp_version", "sp_profile_kinds",
                             "sp_profile_kind_name", "sp_launch_count"):
                 getattr(L, name).restype = C.c_int32
         _lib = L
@@ -485,6 +494,42 @@ def rows_of_16_bytes(rows, cols, dtype, device):
     that the tensor-core kernels read, for widths such as a pruned module's k_keep."""
     per = 16 // torch.empty(0, dtype=dtype).element_size()
     return torch.empty(rows, (cols + per - 1) // per * per, dtype=dtype, device=device)[:, :cols]
+
+
+def sp_attention(Q, K, V, cu_q, cu_k, n_heads, n_kv_heads=None, causal=True, scale=None, out=None, lse=None,
+                 want_lse=False, ws=None, status=None):
+    """Attention over packed sequences (see sp.h).  Q [Nq, n_heads * d_head], K, V [Nk, n_kv_heads * d_head]: row-major, any
+    leading dimension; cu_q, cu_k: int32 [n_seq + 1] on the device.  Returns (O, lse or None).  out: where to write O (rows
+    of no sequence stay as they are there; in a buffer allocated here they are undefined); lse: fp32 [Nq, n_heads] to
+    write, want_lse: allocate it."""
+    _on_one_device(Q, K, V, cu_q, cu_k, out, lse, ws, status)
+    for name, t in (("Q", Q), ("K", K), ("V", V), ("out", out)):
+        if t is not None:
+            _dtype_of(t, name)
+    n_heads = int(n_heads)
+    n_kv = n_heads if n_kv_heads is None else int(n_kv_heads)
+    n_seq = cu_q.numel() - 1
+    if n_seq < 0:
+        raise ValueError("cu_q and cu_k hold n_seq + 1 offsets")
+    _vector(cu_q, torch.int32, n_seq + 1, "cu_q")
+    _vector(cu_k, torch.int32, n_seq + 1, "cu_k")
+    _vector(status, torch.int32, 4, "status")
+    Nq, Nk, d_head = Q.shape[0], K.shape[0], Q.shape[1] // max(n_heads, 1)
+    if out is None:
+        out = torch.empty(Nq, Q.shape[1], dtype=Q.dtype, device=Q.device)
+    if lse is None and want_lse:
+        lse = torch.empty(Nq, n_heads, dtype=torch.float32, device=Q.device)
+    _vector(lse, torch.float32, Nq * n_heads, "lse")
+    if scale is None:
+        scale = max(d_head, 1) ** -0.5
+    args = SpAttentionArgs(mat(Q), mat(K), mat(V), mat(out), cu_q.data_ptr(), cu_k.data_ptr(), _ptr(lse), n_seq, n_heads,
+                           n_kv, int(bool(causal)), float(scale))
+    if ws is None:
+        need = lib().sp_attention_workspace_bytes(Nq, Nk, n_seq, n_heads, n_kv, d_head, _dt(Q))
+        ws = _ws(need, Q.device) if need else None
+    _check(lib().sp_attention(C.byref(args), _ptr(status), _ptr(ws), ws.nbytes if ws is not None else 0, _stream()),
+           "sp_attention")
+    return out, lse
 
 
 def sp_linear(X, W, bias=None, act=SP_LINEAR_NONE, other=None, combine=SP_COMBINE_ADD, out=None, out_dtype=None,

@@ -1,0 +1,358 @@
+// Attention forward over packed sequences: entry points, the CUDA-core kernel, and the join of a key axis that was cut into
+// parts.
+//
+// O_i = sum_j p_ij V_j with p = softmax(scale Q K^T): one pass over the keys, tile by tile, with the running maximum r and
+// sum l of a row: when r rises to r', l and the row of O are scaled by 2^(r - r').  Logits are held in base 2.
+#include <math.h>
+
+#include "sp_attention.cuh"
+
+namespace sp {
+namespace {
+
+constexpr int kBN = 64;                // keys per tile
+constexpr int kSimtThreads = 256;
+
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// A tile of BM rows (queries x the heads that share a key head) against tiles of 64 keys.  256 threads as 16 x 16: a thread
+// has BM / 16 rows x 4 keys of the logits and BM / 16 rows x DH / 16 columns of O.  All operands lie in shared memory as
+// fp32 with the index that a thread's own values run along innermost (Q and K turned: [d][row], [d][key]; P as [key][row]),
+// so that both products read 16-byte pieces.
+template <typename T, int DH, int BM>
+struct SimtTile {
+  static constexpr int PQ = BM + 4, PK = kBN + 4, PV = DH, PP = BM + 4;
+  static constexpr int kQ = DH * PQ, kK = DH * PK, kV = kBN * PV, kP = kBN * PP;
+  static constexpr size_t SMEM = (size_t)(kQ + kK + kV + kP) * sizeof(float);
+};
+
+template <typename T, int DH, int BM>
+__global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const AttnParams p) {
+  kernel_begin();
+  using L = SimtTile<T, DH, BM>;
+  constexpr int TM = BM / 16, TD = DH / 16;
+  extern __shared__ __align__(16) float sm[];
+  float* sq = sm;
+  float* sk = sq + L::kQ;
+  float* sv = sk + L::kK;
+  float* sp_ = sv + L::kV;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const T* Q = reinterpret_cast<const T*>(p.q);
+  const T* K = reinterpret_cast<const T*>(p.k);
+  const T* V = reinterpret_cast<const T*>(p.v);
+  AttnDealer dealer;
+  AttnItem it;
+  for (int64_t item = blockIdx.x; dealer.find(p, item, BM, p.g, p.n_kv, it); item += gridDim.x) {
+    const int rows = (int)min((int64_t)BM, (int64_t)it.nq * p.g - (int64_t)it.tile * BM);
+    const int64_t r0 = (int64_t)it.tile * BM;
+    const int64_t shift = p.causal ? (int64_t)it.nk - it.nq : (int64_t)it.nk;       // query i sees keys j <= i + shift
+    const int last_q = (int)((r0 + rows - 1) / p.g);
+    const int seen = (int)max((int64_t)0, min((int64_t)it.nk, last_q + shift + 1));
+    const bool cut = p.part > 0 && it.nk > p.part;
+    const int kb = cut ? it.c * p.part : 0;
+    const int ke = cut && seen - kb > p.part ? kb + p.part : seen;
+    __syncthreads();
+    for (int e = threadIdx.x; e < BM * DH; e += kSimtThreads) {
+      const int r = e / DH, d = e % DH;
+      float v = 0.f;
+      if (r < rows && d < p.dh) {
+        const int64_t rr = r0 + r;
+        v = load1(Q + (it.q0 + rr / p.g) * p.ldq + (it.head * p.g + rr % p.g) * (int64_t)p.dh + d) * p.scale_log2;
+      }
+      sq[d * L::PQ + r] = v;
+    }
+    float o[TM][TD], m[TM], l[TM];
+    int lim[TM];                      // keys [0, lim) are visible to the row
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+      const int64_t qi = (r0 + ty * TM + i) / p.g;
+      lim[i] = (int)max((int64_t)0, min((int64_t)it.nk, qi + shift + 1));
+#pragma unroll
+      for (int j = 0; j < TD; ++j) o[i][j] = 0.f;
+    }
+    for (int kt = kb; kt < ke; kt += kBN) {
+      __syncthreads();                // the tile before has been read
+      for (int e = threadIdx.x; e < kBN * DH; e += kSimtThreads) {
+        const int j = e / DH, d = e % DH;
+        const bool in = j < ke - kt && d < p.dh;
+        const int64_t at = (int64_t)it.k0 + kt + j;
+        sk[d * L::PK + j] = in ? load1(K + at * p.ldk + it.head * (int64_t)p.dh + d) : 0.f;
+        sv[j * L::PV + d] = in ? load1(V + at * p.ldv + it.head * (int64_t)p.dh + d) : 0.f;
+      }
+      __syncthreads();
+      float s[TM][4];
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+      for (int d = 0; d < DH; ++d) {
+        const float4 kv = *reinterpret_cast<const float4*>(sk + d * L::PK + tx * 4);
+        float qv[TM];
+        if constexpr (TM == 4) {
+          const float4 t = *reinterpret_cast<const float4*>(sq + d * L::PQ + ty * 4);
+          qv[0] = t.x; qv[1] = t.y; qv[2] = t.z; qv[3] = t.w;
+        } else {
+#pragma unroll
+          for (int i = 0; i < TM; ++i) qv[i] = sq[d * L::PQ + ty * TM + i];
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          s[i][0] = fmaf(qv[i], kv.x, s[i][0]);
+          s[i][1] = fmaf(qv[i], kv.y, s[i][1]);
+          s[i][2] = fmaf(qv[i], kv.z, s[i][2]);
+          s[i][3] = fmaf(qv[i], kv.w, s[i][3]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (kt + tx * 4 + j >= lim[i] || tx * 4 + j >= ke - kt) s[i][j] = -INFINITY;
+          mx = fmaxf(mx, s[i][j]);    // (a NaN is passed over here and stays one in the exponential)
+        }
+#pragma unroll
+        for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+        const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.f : mn;
+        const float f = exp2f(m[i] - ref);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[i][j] = exp2f(s[i][j] - ref);
+          sum += s[i][j];
+        }
+#pragma unroll
+        for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+        l[i] = fmaf(l[i], f, sum);
+        m[i] = mn;
+#pragma unroll
+        for (int j = 0; j < TD; ++j) o[i][j] *= f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sp_[(tx * 4 + j) * L::PP + ty * TM + i] = s[i][j];
+      }
+      __syncwarp();                   // a warp's rows of P are its own: two values of ty
+      // In a tile that the mask cuts, a key beyond a row's limit is not touched at all: 0 times a NaN in V is no 0.
+      const bool whole = kt + kBN <= lim[0];     // (rows rise with i and see no fewer keys)
+      const int jend = min(kBN, ke - kt);
+      for (int j = 0; j < jend; ++j) {
+        float pv[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) pv[i] = sp_[j * L::PP + ty * TM + i];
+#pragma unroll
+        for (int c = 0; c < TD; c += 4) {
+          const float4 vv = *reinterpret_cast<const float4*>(sv + j * L::PV + (c / 4) * 64 + tx * 4);
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+            if (whole || kt + j < lim[i]) {
+              o[i][c] = fmaf(pv[i], vv.x, o[i][c]);
+              o[i][c + 1] = fmaf(pv[i], vv.y, o[i][c + 1]);
+              o[i][c + 2] = fmaf(pv[i], vv.z, o[i][c + 2]);
+              o[i][c + 3] = fmaf(pv[i], vv.w, o[i][c + 3]);
+            }
+        }
+      }
+      __syncwarp();
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      if (ty * TM + i >= rows) continue;
+      const int64_t rr = r0 + ty * TM + i, row = it.q0 + rr / p.g;
+      const int h = it.head * p.g + (int)(rr % p.g);
+      // a row without a visible key: l = 0
+      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+      const float lse2 = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
+      float* po = cut ? p.part_o + ((int64_t)it.c * p.Nq + row) * ((int64_t)p.n_heads * p.dh) + (int64_t)h * p.dh : nullptr;
+      T* out = reinterpret_cast<T*>(p.o) + row * p.ldo + (int64_t)h * p.dh;
+#pragma unroll
+      for (int c = 0; c < TD; ++c) {
+        const int d = (c / 4) * 64 + tx * 4 + c % 4;
+        if (d >= p.dh) continue;
+        if (cut) po[d] = o[i][c] * inv;
+        else store1(out + d, o[i][c] * inv);
+      }
+      if (tx == 0) {
+        if (cut) p.part_lse[((int64_t)it.c * p.Nq + row) * p.n_heads + h] = lse2;
+        else if (p.lse) p.lse[row * p.n_heads + h] = lse2 == -INFINITY ? lse2 : lse2 * 0.6931471805599453f;
+      }
+    }
+  }
+}
+
+// O_i = sum_c w_c O_ic / sum_c w_c with w_c = 2^(lse_ic - max): one warp per row and head.  Rows of sequences that are not
+// cut have their result already.
+template <typename T>
+__global__ void __launch_bounds__(256) attention_join_kernel(const AttnParams p) {
+  kernel_begin();
+  const int64_t idx = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (idx >= (int64_t)p.Nq * p.n_heads) return;
+  const int32_t row = (int32_t)(idx / p.n_heads), h = (int32_t)(idx % p.n_heads);
+  if (row < AttnDealer::bound(p.cu_q[0], p.Nq) || row >= AttnDealer::bound(p.cu_q[p.n_seq], p.Nq)) return;
+  int lo = 0, hi = p.n_seq;           // the last sequence that starts at or before the row
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (AttnDealer::bound(p.cu_q[mid], p.Nq) <= row) lo = mid;
+    else hi = mid;
+  }
+  const int nk = AttnDealer::bound(p.cu_k[lo + 1], p.Nk) - AttnDealer::bound(p.cu_k[lo], p.Nk);
+  if (nk <= p.part) return;
+  const int parts = (nk - 1) / p.part + 1;
+  float mx = -INFINITY;
+  bool bad = false;                   // (fmaxf passes over a NaN)
+  for (int c = lane; c < parts; c += 32) {
+    const float lc = p.part_lse[((int64_t)c * p.Nq + row) * p.n_heads + h];
+    mx = fmaxf(mx, lc);
+    bad |= lc != lc;
+  }
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  bad = __any_sync(0xffffffffu, bad);
+  float acc[4] = {0.f, 0.f, 0.f, 0.f}, total = 0.f;
+  for (int c = 0; c < parts; ++c) {
+    const float lc = p.part_lse[((int64_t)c * p.Nq + row) * p.n_heads + h];
+    if (lc == -INFINITY) continue;       // nothing visible there
+    const float w = exp2f(lc - ref);
+    total += w;
+    const float* po = p.part_o + ((int64_t)c * p.Nq + row) * ((int64_t)p.n_heads * p.dh) + (int64_t)h * p.dh;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (lane + 32 * q < p.dh) acc[q] = fmaf(w, po[lane + 32 * q], acc[q]);
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  T* out = reinterpret_cast<T*>(p.o) + (int64_t)row * p.ldo + (int64_t)h * p.dh;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (lane + 32 * q < p.dh) store1(out + lane + 32 * q, bad ? NAN : acc[q] * inv);
+  if (lane == 0 && p.lse)
+    p.lse[(int64_t)row * p.n_heads + h] = bad ? NAN : total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
+}
+
+template <typename T, int DH, int BM>
+cudaError_t launch_simt(const AttnParams& p, cudaStream_t stream) {
+  using L = SimtTile<T, DH, BM>;
+  static PerDeviceOnce attr_once;
+  const auto kernel = attention_simt_kernel<T, DH, BM>;
+  const cudaError_t e = attr_once.run(
+      [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::SMEM); });
+  if (e != cudaSuccess) return e;
+  // as many blocks as can be resident and have work
+  const int64_t rows = (int64_t)p.Nq * p.g;
+  const int64_t tiles = min(rows / BM + p.n_seq, (int64_t)p.Nq * ceil_div((int64_t)p.g, (int64_t)BM));
+  const int64_t work = tiles * p.n_kv * (p.part > 0 ? p.max_parts : 1);
+  const int64_t resident = (int64_t)sm_count() * (L::SMEM > 110 * 1024 ? 1 : L::SMEM > 72 * 1024 ? 2 : 3);
+  const dim3 grid((unsigned)(work < resident ? work : resident));
+  return launch(kernel, grid, dim3(kSimtThreads), L::SMEM, stream, p);
+}
+
+template <typename T>
+cudaError_t launch_simt(const AttnParams& p, cudaStream_t stream) {
+  // 16 rows where the sequences have no more on average (single tokens): a tile's products are the bound there
+  const bool few = (int64_t)p.Nq * p.g <= (int64_t)16 * p.n_seq;
+  if (p.dh <= 64) return few ? launch_simt<T, 64, 16>(p, stream) : launch_simt<T, 64, 64>(p, stream);
+  return few ? launch_simt<T, 128, 16>(p, stream) : launch_simt<T, 128, 64>(p, stream);
+}
+
+struct Cut {
+  int32_t part = 0, max_parts = 1;
+  size_t bytes = 0;
+};
+// Whether and how the key axis is cut.  Without a cut there are about Nq g / 128 tiles of rows, at least one for every sequence
+// that has queries, times the key heads; fewer than the SMs (148) leave SMs idle.  Parts are then as long as gives four for every SM
+// (so that sequences of different lengths even out), at least 256 keys (a part costs its result's way through memory and
+// a second launch).
+Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh) {
+  Cut cut;
+  if (Nq < 1 || Nk < 1 || n_seq < 1) return cut;
+  const int64_t g = n_heads / n_kv, sms = 148;
+  const int64_t seqs = n_seq < Nq ? n_seq : Nq;
+  const int64_t tiles = (Nq * g / 128 > seqs ? Nq * g / 128 : seqs) * n_kv;
+  if (tiles >= 2 * sms) return cut;
+  const int64_t per_tile = ceil_div(Nk, seqs);                 // keys of a tile, on average
+  int64_t part = (int64_t)align_up((size_t)ceil_div(tiles * per_tile, sms * 4), 128);
+  if (part < 256) part = 256;
+  if (part >= Nk) return cut;                                   // nothing is longer
+  const int64_t parts = ceil_div(Nk, part);
+  const int64_t elems = parts * Nq * n_heads;
+  if (elems * (dh + 1) * 4 > (int64_t)1 << 30) return cut;
+  cut.part = (int32_t)part;
+  cut.max_parts = (int32_t)parts;
+  cut.bytes = align_up((size_t)(elems * dh * 4), 256) + (size_t)(elems * 4);
+  return cut;
+}
+
+}  // namespace
+}  // namespace sp
+
+extern "C" {
+
+size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
+                                    int32_t d_head, int32_t dtype) {
+  (void)dtype;
+  if (Nq < 0 || Nk < 0 || n_seq < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || d_head < 1) return 0;
+  return sp::plan_cut(Nq, Nk, n_seq, n_heads, n_kv_heads, d_head).bytes;
+}
+
+sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream) {
+  using namespace sp;
+  if (!a) return SP_ERR_INVALID_ARG;
+  const int32_t dt = a->Q.dtype;
+  if (dt != SP_F32 && dt != SP_BF16) return SP_ERR_DTYPE;
+  if (a->K.dtype != dt || a->V.dtype != dt || a->O.dtype != dt) return SP_ERR_DTYPE;
+  if (a->n_heads < 1 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads != 0 || a->n_seq < 0) return SP_ERR_SHAPE;
+  const int64_t Nq = a->Q.rows, Nk = a->K.rows;
+  if (Nq < 0 || Nk < 0 || Nq > (1 << 30) || Nk > (1 << 30)) return SP_ERR_SHAPE;
+  if (a->Q.cols < 1 || a->Q.cols % a->n_heads != 0 || a->Q.cols > (1 << 30)) return SP_ERR_SHAPE;
+  const int64_t dh = a->Q.cols / a->n_heads;
+  if (dh > 128) return SP_ERR_UNSUPPORTED;
+  if (a->O.rows != Nq || a->O.cols != a->Q.cols || a->V.rows != Nk || a->K.cols != dh * a->n_kv_heads ||
+      a->V.cols != a->K.cols)
+    return SP_ERR_SHAPE;
+  if ((Nq > 1 && (a->Q.ld < a->Q.cols || a->O.ld < a->O.cols)) || (Nk > 1 && (a->K.ld < a->K.cols || a->V.ld < a->V.cols)))
+    return SP_ERR_SHAPE;
+  if (Nq * a->n_heads > ((int64_t)1 << 33)) return SP_ERR_SHAPE;       // (blocks of the join)
+  if (!(a->scale > 0.0) || !(a->scale <= 1.0e38)) return SP_ERR_INVALID_ARG;
+  if (Nq == 0 || a->n_seq == 0) return SP_OK;
+  if (!a->Q.ptr || !a->O.ptr || !a->cu_q || !a->cu_k || (Nk > 0 && (!a->K.ptr || !a->V.ptr))) return SP_ERR_INVALID_ARG;
+  const Cut cut = plan_cut(Nq, Nk, a->n_seq, a->n_heads, a->n_kv_heads, (int32_t)dh);
+  if (cut.part > 0) {
+    if (!ws || ws_bytes < cut.bytes) return SP_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) & 255u) return SP_ERR_ALIGNMENT;
+  }
+  AttnParams p = {};
+  p.q = a->Q.ptr; p.k = a->K.ptr; p.v = a->V.ptr; p.o = a->O.ptr;
+  p.ldq = a->Q.ld; p.ldk = a->K.ld; p.ldv = a->V.ld; p.ldo = a->O.ld;
+  p.lse = a->lse;
+  p.cu_q = a->cu_q; p.cu_k = a->cu_k;
+  p.Nq = (int32_t)Nq; p.Nk = (int32_t)Nk;
+  p.n_seq = a->n_seq; p.n_heads = a->n_heads; p.n_kv = a->n_kv_heads; p.g = a->n_heads / a->n_kv_heads;
+  p.dh = (int32_t)dh; p.causal = a->causal != 0;
+  p.scale_log2 = (float)(a->scale * 1.4426950408889634);
+  p.part = cut.part; p.max_parts = cut.max_parts;
+  if (cut.part > 0) {
+    p.part_o = reinterpret_cast<float*>(ws);
+    p.part_lse = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(ws) +
+                                          align_up((size_t)cut.max_parts * Nq * a->n_heads * dh * 4, 256));
+  }
+  p.status = status_dev;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope prof(PK_GEMM_SIMT, 0.0, 0.0, s);
+  count_launch();
+  if ((dt == SP_F32 ? launch_simt<float>(p, s) : launch_simt<__nv_bfloat16>(p, s)) != cudaSuccess) return SP_ERR_CUDA;
+  if (cut.part > 0) {
+    count_launch();
+    const dim3 grid((unsigned)ceil_div(Nq * a->n_heads, (int64_t)8));
+    const cudaError_t e = dt == SP_F32 ? launch(attention_join_kernel<float>, grid, dim3(256), 0, s, p)
+                                       : launch(attention_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, p);
+    if (e != cudaSuccess) return SP_ERR_CUDA;
+  }
+  return SP_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,90 @@
+// Shared by the attention kernels: their arguments, and how the work of a call is dealt out.
+#pragma once
+#include "sp_common.cuh"
+
+namespace sp {
+
+struct AttnParams {
+  const void *q, *k, *v;
+  void* o;
+  int64_t ldq, ldk, ldv, ldo;
+  float* lse;
+  const int32_t* cu_q;
+  const int32_t* cu_k;
+  int32_t Nq, Nk, n_seq, n_heads, n_kv, g, dh, causal;
+  float scale_log2;            // scale * log2(e): softmax in base 2
+  // Key axis in parts of `part` keys (a multiple of the key tile; 0: not cut).  Part c of row i leaves its normalised
+  // result and lse (base 2) at [c][i] of these; a sequence of n_k keys has max(1, ceil(n_k / part)) parts.
+  int32_t part, max_parts;
+  float* part_o;               // [max_parts, Nq, n_heads * dh]
+  float* part_lse;             // [max_parts, Nq, n_heads]
+  int32_t* status;
+  long long wait_budget;
+};
+
+// One piece of work: a tile of a sequence's rows (queries x the heads that share a key head, head fastest), one key / value
+// head, one part of the keys.
+struct AttnItem {
+  int32_t q0, nq, k0, nk;           // first row of the sequence in Q and K, their numbers
+  int32_t head, tile, c;            // key / value head, tile of rows, part of keys
+};
+
+// Deals the items of a call in a fixed order: sequence by sequence; within one, tiles from the last (which sees the most
+// keys) to the first, heads, parts.  An item is found by walking the sequences, 32 at a time, from where the last one was
+// found, so a caller asks for rising item numbers.  Every warp keeps a dealer of its own; all lanes of the warp call.
+struct AttnDealer {
+  int32_t base;          // sequences before this group of 32 are passed
+  int64_t passed;        // items of those
+  __device__ __forceinline__ AttnDealer() : base(0), passed(0) {}
+  static __device__ __forceinline__ int32_t bound(int32_t x, int32_t n) { return x < 0 ? 0 : x > n ? n : x; }
+  // row_mul: rows per query; rows_per_tile counts those
+  __device__ __forceinline__ bool find(const AttnParams& p, int64_t item, int rows_per_tile, int row_mul, int heads,
+                                       AttnItem& it) {
+    const int lane = threadIdx.x & 31;
+    while (base < p.n_seq) {
+      const int s = base + lane;
+      int q0 = 0, nq = 0, k0 = 0, nk = 0, tiles = 0, parts = 1;
+      if (s < p.n_seq) {
+        q0 = bound(p.cu_q[s], p.Nq);
+        nq = bound(p.cu_q[s + 1], p.Nq) - q0;
+        k0 = bound(p.cu_k[s], p.Nk);
+        nk = bound(p.cu_k[s + 1], p.Nk) - k0;
+        if (nq < 0) nq = 0;
+        if (nk < 0) nk = 0;
+        tiles = (int)(((int64_t)nq * row_mul + rows_per_tile - 1) / rows_per_tile);
+        if (p.part > 0 && nk > p.part) parts = (nk - 1) / p.part + 1;
+      }
+      const int64_t mine = (int64_t)tiles * heads * parts;
+      int64_t upto = mine;                                   // inclusive sums over the lanes
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t t = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += t;
+      }
+      const int64_t total = __shfl_sync(0xffffffffu, upto, 31);
+      if (item < passed + total) {
+        const uint32_t beyond = __ballot_sync(0xffffffffu, item < passed + upto);
+        const int l = __ffs(beyond) - 1;
+        int64_t rest = item - passed - (upto - mine);
+        rest = __shfl_sync(0xffffffffu, rest, l);
+        it.q0 = __shfl_sync(0xffffffffu, q0, l);
+        it.nq = __shfl_sync(0xffffffffu, nq, l);
+        it.k0 = __shfl_sync(0xffffffffu, k0, l);
+        it.nk = __shfl_sync(0xffffffffu, nk, l);
+        tiles = __shfl_sync(0xffffffffu, tiles, l);
+        parts = __shfl_sync(0xffffffffu, parts, l);
+        const int64_t hp = (int64_t)heads * parts;
+        it.tile = tiles - 1 - (int)(rest / hp);
+        rest %= hp;
+        it.head = (int)(rest / parts);
+        it.c = (int)(rest % parts);
+        return true;
+      }
+      passed += total;
+      base += 32;
+    }
+    return false;
+  }
+};
+
+}  // namespace sp

@@ -1,4 +1,4 @@
-"""What sp_linear, sp_token_logprobs and sp_token_logprobs_grad refuse, on the host and before any launch: the pointers below are never
+"""What sp_attention, sp_linear, sp_token_logprobs and sp_token_logprobs_grad refuse, on the host and before any launch: the pointers below are never
 followed."""
 import ctypes as C
 
@@ -19,6 +19,54 @@ def lib():
 
 def m(rows, cols, dtype=F32, ld=None, ptr=P):
     return api.SpMat(ptr, dtype, 0, rows, cols, cols if ld is None else ld)
+
+
+def attention(lib, ws=None, ws_bytes=0, **kw):
+    f = dict(Q=m(1024, 256), K=m(1024, 128), V=m(1024, 128), O=m(1024, 256), cu_q=P, cu_k=P, lse=None, n_seq=600, n_heads=4,
+             n_kv_heads=2, causal=1, scale=0.125)
+    f.update(kw)
+    return lib.sp_attention(C.byref(api.SpAttentionArgs(**f)), None, ws, ws_bytes, None)
+
+
+def test_attention_refusals(lib):
+    assert lib.sp_attention(None, None, None, 0, None) == INVALID
+    for name in "QKVO":
+        shape = (1024, 256) if name in "QO" else (1024, 128)
+        assert attention(lib, **{name: m(*shape, dtype=BF16)}) == DTYPE
+        assert attention(lib, **{name: m(*shape, ld=shape[1] - 1)}) == SHAPE
+        assert attention(lib, **{name: m(*shape, ptr=None)}) == INVALID
+        assert attention(lib, **{name: m(shape[0], shape[1] + 4)}) == SHAPE
+    assert attention(lib, Q=m(1024, 256, F64)) == DTYPE
+    assert attention(lib, O=m(1000, 256)) == SHAPE and attention(lib, V=m(1000, 128)) == SHAPE
+    assert attention(lib, n_kv_heads=3) == SHAPE and attention(lib, n_heads=0) == SHAPE
+    assert attention(lib, n_kv_heads=0) == SHAPE and attention(lib, n_seq=-1) == SHAPE
+    assert attention(lib, n_heads=3, n_kv_heads=3) == SHAPE                    # 256 columns are not 3 heads
+    assert attention(lib, Q=m((1 << 30) + 1, 256), O=m((1 << 30) + 1, 256)) == SHAPE
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 1e39):
+        assert attention(lib, scale=scale) == INVALID
+    assert attention(lib, cu_q=None) == INVALID and attention(lib, cu_k=None) == INVALID
+    wide = dict(Q=m(8, 129), O=m(8, 129), K=m(8, 129), V=m(8, 129), n_heads=1, n_kv_heads=1)
+    assert attention(lib, **wide) == UNSUPPORTED
+    # a call whose keys are cut needs its workspace, aligned
+    long = dict(Q=m(1, 256), O=m(1, 256), K=m(9000, 128), V=m(9000, 128), n_seq=1)
+    need = lib.sp_attention_workspace_bytes(1, 9000, 1, 4, 2, 64, F32)
+    assert need > 0
+    assert attention(lib, **long) == WORKSPACE
+    assert attention(lib, ws=C.c_void_p(0x1000), ws_bytes=need - 1, **long) == WORKSPACE
+    assert attention(lib, ws=C.c_void_p(0x1010), ws_bytes=need, **long) == ALIGN
+    # nothing to do: no pointer is needed
+    none = m(0, 256, ptr=None)
+    assert attention(lib, Q=none, O=none, cu_q=None) == OK
+    assert attention(lib, n_seq=0, cu_q=None, cu_k=None) == OK
+
+
+def test_attention_workspace(lib):
+    w = lambda *a: lib.sp_attention_workspace_bytes(*a, BF16)
+    assert w(128 * 2048, 128 * 2048, 128, 32, 32, 128) == 0                    # rows enough to fill the GPU
+    assert w(16, 16 * 32768, 16, 32, 8, 128) > 0
+    assert w(0, 100, 1, 8, 8, 64) == 0 and w(1, 0, 1, 8, 8, 64) == 0 and w(1, 200, 1, 8, 8, 64) == 0
+    assert w(1, 1 << 24, 0, 8, 8, 64) == 0 and w(1, 1 << 24, 1, 8, 3, 64) == 0 and w(-1, 100, 1, 8, 8, 64) == 0
+    assert w(64, 1 << 30, 64, 32, 8, 128) < 2 << 30
 
 
 def linear(lib, X=None, W=None, other=None, Y=None, bias=None, act=0, combine=0):
@@ -82,6 +130,13 @@ def test_gradient_refusals(lib):
     for scale in (0.0, -2.0, float("nan"), float("inf")):
         assert grad(lib, x, x, scale=scale) == INVALID
     assert grad(lib, m(0, 100, ptr=None), m(0, 100, ptr=None)) == OK
+
+
+def test_binding_refuses_cpu_tensors_in_attention(lib):
+    import torch
+    x, cu = torch.zeros(4, 8), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(RuntimeError):
+        api.sp_attention(x, x, x, cu, cu, 1)
 
 
 def test_binding_refuses_cpu_tensors_in_linear(lib):
