@@ -342,9 +342,13 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
   }
   p.status = status_dev;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  ProfScope prof(PK_GEMM_SIMT, 0.0, 0.0, s);
+  const bool tc = dt == SP_BF16 && attention_tc_supported(p);
+  ProfScope prof(tc ? PK_GEMM_TC : PK_GEMM_SIMT, 0.0, 0.0, s);
   count_launch();
-  if ((dt == SP_F32 ? launch_simt<float>(p, s) : launch_simt<__nv_bfloat16>(p, s)) != cudaSuccess) return SP_ERR_CUDA;
+  if (tc) {
+    const sp_status st = attention_tc(p, s);
+    if (st != SP_OK) return st;
+  } else if ((dt == SP_F32 ? launch_simt<float>(p, s) : launch_simt<__nv_bfloat16>(p, s)) != cudaSuccess) return SP_ERR_CUDA;
   if (cut.part > 0) {
     count_launch();
     const dim3 grid((unsigned)ceil_div(Nq * a->n_heads, (int64_t)8));

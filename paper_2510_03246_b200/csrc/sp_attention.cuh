@@ -87,4 +87,8 @@ struct AttnDealer {
   }
 };
 
+// tcgen05 form (sp_attention_tc.cu): layouts that tensor maps can describe
+bool attention_tc_supported(const AttnParams& a);
+sp_status attention_tc(const AttnParams& a, cudaStream_t stream);
+
 }  // namespace sp

@@ -1,0 +1,602 @@
+// bf16 attention on the tensor cores of sm_100a: S = Q K^T and O += P V as tcgen05.mma with fp32 accumulators in tensor
+// memory, operands brought in by TMA, softmax on the CUDA cores in between.
+//
+// A CTA (one per SM, persistent) works on two tiles of up to 128 rows at a time, "half" 0 and 1, that share every key and value tile:
+// while the softmax warps of one half turn its S into P, the tensor core multiplies for the other.  Rows of a tile are queries x the heads
+// that share a key head (head fastest), so that grouped heads read K and V once; a 3-D tensor map (channel, head, token) lands them in
+// that order.  Per half and key tile of 128:
+//   S (128 columns of tensor memory) -> registers, one row per thread; row maximum; P = 2^(c S - c r) in bf16, written back over the
+//   first 64 columns of S; O += P V with P read from tensor memory.
+// The reference r of a row follows its running maximum only when that has risen by more than 2^8 in P's scale: O is then rescaled in tensor
+// memory by the same threads.  P and its sum l stay relative to r, so nothing is approximated by waiting, and l <= 2^8 n holds in fp32.
+// Masked values: S is replaced by -infinity.  V is not touched by that: 0 times what stands there would be NaN for an infinity.  So in tiles
+// that some row does not see whole, two warps clear the rows of V that no row sees, and set non-finite values in rows that only some see to
+// zero; those rows then get them back at the end (rows_with_bad_values).
+//
+// Warps: 0-3 and 4-7 softmax of half 0 and 1 (lane and warp give the row), 8 TMA, 9 MMA issue and tensor memory, 10-11 edge tiles of V.
+// Waits for copies, the tensor core and other warps are bounded by a clock budget (SP_ERR_TIMEOUT through status).
+#include <math.h>
+#include <string.h>
+
+#include "sp_attention.cuh"
+#include "sp_tc.cuh"
+
+namespace sp {
+namespace {
+
+constexpr int kRows = 128, kKeys = 128;
+constexpr int kThreads = 384;
+constexpr long long kWaitBudget = 4000000000LL, kDrainBudget = 200000000LL;    // clock cycles: ~2 s, ~0.1 s
+constexpr int kBadSlots = 32;       // items between the edge warps and the epilogue: less than the stages of the ring
+
+template <int DH>
+struct Cfg {
+  static constexpr int CH = DH / 64;                       // 128-byte wide chunks of a row
+  static constexpr int CHUNK = 128 * 128;                  // bytes of one: 128 rows of 128 bytes
+  static constexpr int TILE = CH * CHUNK;
+  static constexpr int STAGES = DH == 128 ? 5 : 8;
+  static constexpr int BARS = 4 * STAGES + 12;
+  static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE + 1024 + 8 * BARS;
+  static constexpr uint32_t S_COL = 0, O_COL = 256;        // tensor memory: S0 S1 | O0 O1
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_commit_one(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+        "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+        "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// bf16 operands, fp32 accumulator, 128 x n; B K-major or (V: keys are K, channels contiguous) MN-major
+__device__ __forceinline__ uint32_t instr_desc(bool b_kmajor, int n) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((b_kmajor ? 0u : 1u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+}
+
+struct TcAttnParams {
+  AttnParams a;
+  int32_t gp, tokens;        // heads in a tile's rows, tokens of a half: gp * tokens <= 128
+  int32_t heads;             // items' heads: key heads, or query heads when these are not packed (gp = 1)
+  int32_t vec_out;           // rows of O can be stored 16 bytes at a time
+};
+
+// What all warps derive from an item.
+struct Work {
+  int t0;                    // first token of the tile within its sequence
+  int kb;                    // first key of the part
+  int n[2];                  // key tiles of each half
+  int sure;                  // keys [0, sure) are seen by every row
+  int seen;                  // keys [0, seen) are seen by some row (no later one is in the part either)
+  __device__ __forceinline__ int tiles() const { return n[0] > n[1] ? n[0] : n[1]; }
+  __device__ __forceinline__ bool edge(int i) const { return kb + (i + 1) * kKeys > sure; }
+};
+__device__ __forceinline__ int visible(const AttnItem& it, int causal, int token) {
+  if (!causal) return it.nk;
+  const int64_t v = (int64_t)token + it.nk - it.nq + 1;
+  return v < 0 ? 0 : v < it.nk ? (int)v : it.nk;
+}
+__device__ __forceinline__ Work work_of(const TcAttnParams& p, const AttnItem& it) {
+  Work w;
+  w.t0 = it.tile * 2 * p.tokens;
+  const bool cut = p.a.part > 0 && it.nk > p.a.part;
+  w.kb = cut ? it.c * p.a.part : 0;
+  const int end = cut && it.nk - w.kb > p.a.part ? w.kb + p.a.part : it.nk;
+  w.sure = visible(it, p.a.causal, w.t0);
+  w.seen = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int first = w.t0 + h * p.tokens;
+    int last = first + p.tokens - 1;
+    if (last > it.nq - 1) last = it.nq - 1;
+    int v = first < it.nq ? visible(it, p.a.causal, last) : 0;
+    if (v > end) v = end;
+    if (v > w.seen) w.seen = v;
+    w.n[h] = v > w.kb ? (v - w.kb + kKeys - 1) / kKeys : 0;
+  }
+  return w;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                    const __grid_constant__ CUtensorMap tmV, const TcAttnParams p) {
+  using C = Cfg<DH>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint32_t s_tmem_base;
+  __shared__ int s_abort;
+  __shared__ int s_bad[kBadSlots];       // slot of an item: its number where V had non-finite values behind the mask
+
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t q_smem = (raw + 1023u) & ~1023u;
+  const uint32_t ring = q_smem + 2 * C::TILE;
+  const uint32_t bars = ring + C::STAGES * C::TILE;
+  auto full_bar = [&](int s) { return bars + 8u * s; };                         // a K tile, or a V tile seen whole
+  auto edge_bar = [&](int s) { return bars + 8u * (C::STAGES + s); };           // a V tile that the edge warps look at first
+  auto ready_bar = [&](int s) { return bars + 8u * (2 * C::STAGES + s); };      // they have
+  auto empty_bar = [&](int s) { return bars + 8u * (3 * C::STAGES + s); };
+  const uint32_t misc = bars + 8u * 4 * C::STAGES;
+  const uint32_t q_full = misc, q_empty = misc + 8, drain_bar = misc + 16;
+  auto s_full = [&](int h) { return misc + 24u + 8u * h; };
+  auto p_full = [&](int h) { return misc + 40u + 8u * h; };
+  auto o_full = [&](int h) { return misc + 56u + 8u * h; };
+  auto o_empty = [&](int h) { return misc + 72u + 8u * h; };
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abort_flag = &s_abort;
+  const long long budget = p.a.wait_budget;
+
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int s = 0; s < C::STAGES; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(edge_bar(s), 1);
+      mbar_init(ready_bar(s), 2);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
+    mbar_init(drain_bar, 1);
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(s_full(h), 1);
+      mbar_init(p_full(h), 4);
+      mbar_init(o_full(h), 1);
+      mbar_init(o_empty(h), 4);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (threadIdx.x < kBadSlots) s_bad[threadIdx.x] = -1;
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem_base)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem_base;
+  kernel_begin();
+
+  AttnDealer dealer;
+  AttnItem it;
+  int seq = 0;                // number of the item within this CTA
+  if (warp == 8) {
+    // ------------------------------------------------------------------------------------------------ TMA
+    uint32_t pos = 0;         // tiles loaded so far
+    int loaded = 0;           // items with keys so far (their Q was loaded)
+    bool ok = true;
+    for (int64_t item = blockIdx.x; dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x) {
+      const Work w = work_of(p, it);
+      const int n = w.tiles();
+      if (n == 0) continue;
+      if (lane == 0) {
+        const int kvh = p.gp == 1 ? it.head / p.a.g : it.head;
+        if (loaded > 0) ok = mbar_wait(q_empty, (uint32_t)(loaded - 1) & 1u, abort_flag, budget);
+        if (ok) {
+          const int halves = w.t0 + p.tokens < it.nq ? 2 : 1;
+          mbar_expect_tx(q_full, (uint32_t)(halves * C::CH * p.gp * p.tokens * 128));
+          for (int h = 0; h < halves; ++h)
+#pragma unroll
+            for (int c = 0; c < C::CH; ++c)
+              tma_load_3d(q_smem + h * C::TILE + c * C::CHUNK, &tmQ, c * 64, it.head * p.gp, it.q0 + w.t0 + h * p.tokens, q_full);
+        }
+        for (int i = 0; i < 2 * n && ok; ++i) {
+          const int s = (int)(pos % C::STAGES);
+          if (!mbar_wait(empty_bar(s), (pos / C::STAGES + 1) & 1u, abort_flag, budget)) { ok = false; break; }
+          const bool v = i & 1;
+          const uint32_t bar = v && w.edge(i >> 1) ? edge_bar(s) : full_bar(s);
+          mbar_expect_tx(bar, C::TILE);
+#pragma unroll
+          for (int c = 0; c < C::CH; ++c)
+            tma_load_3d(ring + s * C::TILE + c * C::CHUNK, v ? &tmV : &tmK, c * 64, kvh, it.k0 + w.kb + (i >> 1) * kKeys, bar);
+          ++pos;
+        }
+      }
+      ++loaded;
+      ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+      if (!ok) break;
+    }
+    if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 11);
+  } else if (warp == 9) {
+    // ------------------------------------------------------------------------------------------------ MMA
+    const uint32_t id_s = instr_desc(true, kKeys), id_o = instr_desc(false, DH);
+    uint32_t pos = 0, full_ph = 0, ready_ph = 0;      // phases of the barriers of a stage: a bit each
+    uint32_t p_ph = 0, oe_ph = 0;                     // of a half: a bit each
+    int loaded = 0;
+    bool ok = true, issued = false;
+    uint32_t wrote_o = 0;                             // halves that have had an output
+    for (int64_t item = blockIdx.x; dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x) {
+      const Work w = work_of(p, it);
+      const int n = w.tiles();
+      if (n == 0) continue;
+      if (lane == 0) {
+        auto stage_at = [&](uint32_t x) { return (int)(x % C::STAGES); };
+        auto wait_full = [&](int s) {
+          const bool got = mbar_wait(full_bar(s), (full_ph >> s) & 1u, abort_flag, budget);
+          full_ph ^= 1u << s;
+          return got;
+        };
+        auto scores = [&](int h, int s) {
+          const uint32_t a0 = q_smem + h * C::TILE, b0 = ring + s * C::TILE;
+#pragma unroll
+          for (int k = 0; k < DH / 16; ++k) {
+            const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32);
+            tc_mma_ss(tmem + C::S_COL + 128u * h, make_smem_desc(a0 + off, true, 0), make_smem_desc(b0 + off, true, 0), id_s, k > 0);
+          }
+          tc_commit_one(s_full(h));
+        };
+        ok = mbar_wait(q_full, (uint32_t)loaded & 1u, abort_flag, budget) && wait_full(stage_at(pos));
+        if (ok) {
+          tc_fence_after();
+          for (int h = 0; h < 2; ++h)
+            if (w.n[h] > 0) scores(h, stage_at(pos));
+          issued = true;
+          tc_commit_one(empty_bar(stage_at(pos)));
+          if (n == 1) tc_commit_one(q_empty);
+        }
+        for (int i = 0; i < n && ok; ++i) {
+          const int sv = stage_at(pos + 1), sk = stage_at(pos + 2);
+          const bool more = i + 1 < n;
+          if (w.edge(i)) {
+            ok = mbar_wait(ready_bar(sv), (ready_ph >> sv) & 1u, abort_flag, budget);
+            ready_ph ^= 1u << sv;
+          } else {
+            ok = wait_full(sv);
+          }
+          if (ok && more) ok = wait_full(sk);
+          for (int h = 0; h < 2 && ok; ++h) {
+            if (i >= w.n[h]) continue;
+            ok = mbar_wait(p_full(h), (p_ph >> h) & 1u, abort_flag, budget);
+            p_ph ^= 1u << h;
+            if (ok && i == 0 && ((wrote_o >> h) & 1u)) {        // the item before has left O
+              ok = mbar_wait(o_empty(h), (oe_ph >> h) & 1u, abort_flag, budget);
+              oe_ph ^= 1u << h;
+            }
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k)
+              tc_mma_ts(tmem + C::O_COL + 128u * h, tmem + C::S_COL + 128u * h + 8u * k,
+                        make_smem_desc(ring + sv * C::TILE + (uint32_t)k * 2048u, false, C::CHUNK), id_o, i > 0 || k > 0);
+            if (i + 1 < w.n[h]) {
+              scores(h, sk);
+            } else {
+              tc_commit_one(o_full(h));
+              wrote_o |= 1u << h;
+            }
+          }
+          if (!ok) break;
+          tc_commit_one(empty_bar(sv));
+          if (more) {
+            tc_commit_one(empty_bar(sk));
+            if (i + 2 == n) tc_commit_one(q_empty);
+          }
+          pos += 2;
+        }
+      }
+      ++loaded;
+      ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+      if (!ok) break;
+    }
+    if (lane == 0) {
+      if (!ok) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 12);
+      // (in a complete run the epilogues have seen the last products; this matters when a role gave up)
+      if (issued && (!ok || *abort_flag)) {
+        tc_commit_one(drain_bar);
+        const long long t0 = clock64();
+        while (!mbar_try(drain_bar, 0u) && clock64() - t0 < kDrainBudget) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 10) {
+    // ------------------------------------------------------------------------------------------------ edge tiles of V
+    const int tid = threadIdx.x - 320;               // 0 .. 63
+    uint32_t pos = 0, edge_ph = 0;
+    bool ok = true;
+    for (int64_t item = blockIdx.x; ok && dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x, ++seq) {
+      const Work w = work_of(p, it);
+      const int n = w.tiles();
+      for (int i = 0; i < n && ok; ++i, pos += 2) {
+        if (!w.edge(i)) continue;
+        const int s = (int)((pos + 1) % C::STAGES);
+        const bool got = mbar_wait(edge_bar(s), (edge_ph >> s) & 1u, abort_flag, budget);
+        edge_ph ^= 1u << s;
+        ok = __all_sync(0xffffffffu, got);
+        if (!ok) break;
+        const int k0 = w.kb + i * kKeys;
+        uint8_t* tile = smem_raw + (ring - raw) + (size_t)s * C::TILE;
+        bool found = false;
+        for (int j = tid; j < kKeys; j += 64) {
+          if (k0 + j < w.sure) continue;             // seen by every row
+          const bool clear = k0 + j >= w.seen;
+#pragma unroll
+          for (int c = 0; c < C::CH; ++c)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              uint4* at = reinterpret_cast<uint4*>(tile + c * C::CHUNK + j * 128 + ((x + j) & 7) * 16);
+              if (clear) {
+                *at = make_uint4(0u, 0u, 0u, 0u);
+              } else {
+                const uint4 v = *at;
+                // a bf16 of all-ones exponent: its magnitude plus 0x80 reaches the sign bit
+                auto mark = [](uint32_t u) { return ((u & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; };
+                if (mark(v.x) | mark(v.y) | mark(v.z) | mark(v.w)) {
+                  auto fix = [&](uint32_t u) {
+                    const uint32_t b = mark(u);
+                    return u & ~((b & 0x8000u ? 0xffffu : 0u) | (b & 0x80000000u ? 0xffff0000u : 0u));
+                  };
+                  *at = make_uint4(fix(v.x), fix(v.y), fix(v.z), fix(v.w));
+                  found = true;
+                }
+              }
+            }
+        }
+        if (found) *reinterpret_cast<volatile int*>(&s_bad[seq % kBadSlots]) = seq;
+        fence_async_smem();                          // the tensor core reads what was written here
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ready_bar(s));
+      }
+    }
+    if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 13);
+  } else {
+    // ------------------------------------------------------------------------------------------------ softmax and output
+    const int h = warp >> 2, q = warp & 3;
+    const int row = q * 32 + lane;                   // of the half, and lane of tensor memory
+    const uint32_t lanes = (uint32_t)(q * 32) << 16;
+    const uint32_t t_s = tmem + C::S_COL + 128u * h + lanes, t_o = tmem + C::O_COL + 128u * h + lanes;
+    const float c = p.a.scale_log2;
+    uint32_t s_ph = 0, o_ph = 0;
+    bool ok = true;
+    for (int64_t item = blockIdx.x; ok && dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x, ++seq) {
+      const Work w = work_of(p, it);
+      const int token = w.t0 + h * p.tokens + row / p.gp;
+      const bool valid = row < p.gp * p.tokens && token < it.nq;
+      const int lim = valid ? min(visible(it, p.a.causal, token), w.seen) : 0;       // keys [0, lim)
+      const bool busy = __any_sync(0xffffffffu, valid);
+      const int n = w.n[h];
+      float r = -INFINITY, l = 0.f;                  // reference (not yet times c) and sum
+      for (int i = 0; i < n; ++i) {
+        const bool got = mbar_wait(s_full(h), s_ph, abort_flag, budget);
+        s_ph ^= 1u;
+        ok = __all_sync(0xffffffffu, got);
+        if (!ok) break;
+        if (busy) {
+          tc_fence_after();
+          uint32_t x[128];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) tc_ld32(t_s + 32u * b, x + 32 * b);
+          tc_wait_ld();
+          const int left = lim - (w.kb + i * kKeys); // keys of this tile that the row sees
+          if (__any_sync(0xffffffffu, left < kKeys)) {
+#pragma unroll
+            for (int j = 0; j < kKeys; ++j)
+              if (j >= left) x[j] = 0xff800000u;
+          }
+          float m4[4];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) m4[b] = __uint_as_float(x[b]);
+#pragma unroll
+          for (int j = 4; j < kKeys; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(x[j]));
+          const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+          // the reference follows a maximum that has risen by more than 2^8 (from -infinity: by anything)
+          const bool rise = m > r && (m - r) * c > 8.f;
+          if (__any_sync(0xffffffffu, rise)) {
+            const float f = rise ? exp2_fast((r - m) * c) : 1.f;       // r = -infinity: 0
+            if (rise) r = m;
+            l *= f;
+            if (i > 0) {
+#pragma unroll 1
+              for (int b = 0; b < DH / 32; ++b) {
+                uint32_t o[32];
+                tc_ld32(t_o + 32u * b, o);
+                tc_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                tc_st32(t_o + 32u * b, o);
+              }
+            }
+          }
+          const float shift = r == -INFINITY ? 0.f : -r * c;
+          float l2[2] = {0.f, 0.f};
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            uint32_t w16[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float e0 = exp2_fast(fmaf(__uint_as_float(x[32 * b + 2 * j]), c, shift));
+              const float e1 = exp2_fast(fmaf(__uint_as_float(x[32 * b + 2 * j + 1]), c, shift));
+              l2[0] += e0;
+              l2[1] += e1;
+              const __nv_bfloat162 e = __floats2bfloat162_rn(e0, e1);
+              w16[j] = *reinterpret_cast<const uint32_t*>(&e);
+            }
+            tc_st16(t_s + 16u * b, w16);
+          }
+          l += l2[0] + l2[1];
+          tc_wait_st();
+          tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(h));
+      }
+      if (!ok) break;
+      // ---- output of the item
+      const int64_t out_row = (int64_t)it.q0 + token;
+      const int head = p.gp == 1 ? it.head : it.head * p.gp + row % p.gp;
+      const bool cut = p.a.part > 0 && it.nk > p.a.part;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float lse2 = l == 0.f ? -INFINITY : fmaf(r, c, log2f(l));
+      __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.o) + out_row * p.a.ldo + (int64_t)head * p.a.dh;
+      float* part = cut ? p.a.part_o + ((int64_t)it.c * p.a.Nq + out_row) * ((int64_t)p.a.n_heads * p.a.dh) + (int64_t)head * p.a.dh
+                        : nullptr;
+      bool bad = false;
+      if (n > 0) {
+        const bool got = mbar_wait(o_full(h), o_ph, abort_flag, budget);
+        o_ph ^= 1u;
+        ok = __all_sync(0xffffffffu, got);
+        if (!ok) break;
+        tc_fence_after();
+        bad = *reinterpret_cast<volatile int*>(&s_bad[seq % kBadSlots]) == seq;
+      }
+      if (busy) {
+#pragma unroll 1
+        for (int b = 0; b < DH / 32; ++b) {
+          uint32_t o[32];
+          __syncwarp();                              // (lanes without a row skipped the rest of the round before)
+          if (n > 0) {
+            tc_ld32(t_o + 32u * b, o);
+            tc_wait_ld();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = 0u;
+          }
+          if (!valid || 32 * b >= p.a.dh) continue;
+          float f[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) f[j] = l == 0.f ? 0.f : __uint_as_float(o[j]) * inv;
+          if (bad) {
+            // values of V that the edge warps set to zero, for the rows that do see them
+            const int kvh = p.gp == 1 ? it.head / p.a.g : it.head;
+            const __nv_bfloat16* V = reinterpret_cast<const __nv_bfloat16*>(p.a.v) + (int64_t)kvh * p.a.dh + 32 * b;
+            for (int key = max(w.sure, w.kb); key < lim; ++key)
+#pragma unroll 1
+              for (int j = 0; j < 32 && 32 * b + j < p.a.dh; ++j) {
+                const float v = __bfloat162float(V[((int64_t)it.k0 + key) * p.a.ldv + j]);
+                if (!(fabsf(v) < INFINITY)) {
+#pragma unroll
+                  for (int y = 0; y < 32; ++y)
+                    if (y == j) f[y] += v;
+                }
+              }
+          }
+          if (cut) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              if (32 * b + j < p.a.dh) *reinterpret_cast<float4*>(part + 32 * b + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+          } else if (p.vec_out) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8)
+              if (32 * b + j < p.a.dh) {
+                uint32_t u[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                  const __nv_bfloat162 e = __floats2bfloat162_rn(f[j + 2 * y], f[j + 2 * y + 1]);
+                  u[y] = *reinterpret_cast<const uint32_t*>(&e);
+                }
+                *reinterpret_cast<uint4*>(out + 32 * b + j) = make_uint4(u[0], u[1], u[2], u[3]);
+              }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (32 * b + j < p.a.dh) out[32 * b + j] = __float2bfloat16_rn(f[j]);
+          }
+        }
+        if (valid) {
+          if (cut) p.a.part_lse[((int64_t)it.c * p.a.Nq + out_row) * p.a.n_heads + head] = lse2;
+          else if (p.a.lse) p.a.lse[out_row * p.a.n_heads + head] = lse2 == -INFINITY ? lse2 : lse2 * 0.6931471805599453f;
+        }
+      }
+      if (n > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(o_empty(h));
+      }
+    }
+    if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 14);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (s_abort) {              // a role gave up: copies that another one had in flight land before shared memory is released
+    const long long t0 = clock64();
+    while (clock64() - t0 < kDrainBudget) {}
+  }
+  if (warp == 9) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+template <int DH>
+sp_status launch_tc(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const TcAttnParams& p, int64_t work,
+                    cudaStream_t stream) {
+  static PerDeviceOnce attr_once;
+  const auto kernel = attention_tc_kernel<DH>;
+  if (attr_once.run([&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<DH>::SMEM);
+      }) != cudaSuccess)
+    return SP_ERR_CUDA;
+  const dim3 grid((unsigned)(work < sm_count() ? work : sm_count()));
+  return launch(kernel, grid, dim3(kThreads), Cfg<DH>::SMEM, stream, tmQ, tmK, tmV, p) == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+}
+
+}  // namespace
+
+bool attention_tc_supported(const AttnParams& a) {
+  const auto fits = [](const void* ptr, int64_t ld) { return ld % 8 == 0 && (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; };
+  return a.dh % 8 == 0 && a.dh <= 128 && a.Nk > 0 && fits(a.q, a.ldq) && fits(a.k, a.ldk) && fits(a.v, a.ldv);
+}
+
+sp_status attention_tc(const AttnParams& a, cudaStream_t stream) {
+  TcAttnParams p;
+  p.a = a;
+  p.a.wait_budget = wait_budget_cycles() > 0 ? wait_budget_cycles() : kWaitBudget;
+  // Heads that share a key head fill the rows of a tile together.  Groups of more than half a tile would leave too many rows
+  // empty: their heads go one by one.
+  p.gp = a.g <= kRows / 2 ? a.g : 1;
+  p.tokens = kRows / p.gp;
+  p.heads = p.gp == 1 ? a.n_heads : a.n_kv;
+  p.vec_out = a.ldo % 8 == 0 && (reinterpret_cast<uintptr_t>(a.o) & 15u) == 0;
+  CUtensorMap tmQ, tmK, tmV;
+  if (!make_map3(&tmQ, a.q, a.dh, a.n_heads, a.Nq, a.dh, a.ldq, 64, p.gp, p.tokens) ||
+      !make_map3(&tmK, a.k, a.dh, a.n_kv, a.Nk, a.dh, a.ldk, 64, 1, kKeys) ||
+      !make_map3(&tmV, a.v, a.dh, a.n_kv, a.Nk, a.dh, a.ldv, 64, 1, kKeys))
+    return SP_ERR_CUDA;
+  const int64_t tiles = min((int64_t)a.Nq / (2 * p.tokens) + a.n_seq, (int64_t)a.Nq);
+  const int64_t work = tiles * p.heads * (a.part > 0 ? a.max_parts : 1);
+  return a.dh <= 64 ? launch_tc<64>(tmQ, tmK, tmV, p, work, stream) : launch_tc<128>(tmQ, tmK, tmV, p, work, stream);
+}
+
+}  // namespace sp

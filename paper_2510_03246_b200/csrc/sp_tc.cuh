@@ -151,5 +151,8 @@ __device__ __forceinline__ uint64_t make_smem_desc(uint32_t addr, bool kmajor, u
 // Tensor map of a row-major matrix (sp_gemm_tc.cu).
 bool make_map(CUtensorMap* map, bool f32, const void* ptr, int64_t inner, int64_t outer, int64_t ld, int box_inner,
               int box_outer, bool swizzle64 = false);
+// bf16 [n2, n1, n0] with strides ld2, ld1 (elements) of the outer dimensions, 128-byte swizzle, boxes [b2, b1, b0].
+bool make_map3(CUtensorMap* map, const void* ptr, int64_t n0, int64_t n1, int64_t n2, int64_t ld1, int64_t ld2, int b0, int b1,
+               int b2);
 
 }  // namespace sp
