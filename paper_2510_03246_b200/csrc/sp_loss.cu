@@ -4,6 +4,10 @@
 //   lse = ln2 (r + log2 s),   log p_v = ln2 (t_v - r - log2 s),   entropy = ln2 (log2 s - w / s),
 // and (r, s, w) of two parts of a row join by shifting both to the larger r.  So one pass over the logits suffices: every
 // thread keeps its own (r, s, w) with r its running maximum, and they are joined at the end.  All of it is held in fp32.
+//
+// The n best logits need no list during that pass.  The k-th largest of a warp's 32 thread maxima, k = ceil(n / warps of the row), taken
+// over the warps' least, is a floor that at least n logits reach; few more do (some 20 of 50257 for n = 8).  Afterwards only the vectors of
+// threads whose maximum reaches the floor are looked at again, a warp at a time and out of L2.
 #include <math.h>
 
 #include "sp_common.cuh"
@@ -89,7 +93,7 @@ __device__ __forceinline__ unsigned long long make_key(float x, uint32_t index) 
 struct WarpBest {
   unsigned long long key;
   // every lane calls; keys of the lanes in `offer` are inserted
-  __device__ __forceinline__ void insert(bool offer, unsigned long long k, int n, unsigned long long& floor_key, int lane) {
+  __device__ __noinline__ void insert(bool offer, unsigned long long k, int n, unsigned long long& floor_key, int lane) {
     uint32_t m = __ballot_sync(0xffffffffu, offer && k > floor_key);
     while (m) {
       const unsigned long long c = __shfl_sync(0xffffffffu, k, __ffs(m) - 1);
@@ -127,7 +131,7 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
   static_assert(WARPS == 1 || WARPS == kWarps, "rows per block");
   __shared__ Part s_part[kWarps];
   __shared__ unsigned long long s_best[ALTS ? kWarps * SP_MAX_ALTS : 1];
-  __shared__ unsigned long long s_floor;
+  __shared__ uint32_t s_floor[kWarps];
   __shared__ Part s_all[kMaxCluster];
   __shared__ unsigned long long s_all_best[ALTS ? kMaxCluster * SP_MAX_ALTS : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -137,15 +141,13 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
   const int wl = WARPS == 1 ? 0 : warp;                // warp within the row
   // (the other CTAs of a cluster write into the first one's shared memory: all have started once they meet)
   if (WARPS > 1 && cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-  if (ALTS && WARPS > 1) {
-    if (threadIdx.x == 0) s_floor = 0ull;
-    __syncthreads();
-  }
   const float c = p.scale * kLog2E;
   Part a{-INFINITY, 0.f, 0.f};
   float rc = 0.f;                                      // a.r, or 0 while that is -infinity
   WarpBest best{0ull};
   unsigned long long floor_key = 0ull;
+  float top = -INFINITY;                               // largest value of this thread's vectors
+  bool any = false;                                    // it has had one that is a number
 
   // values x[0 .. n) into (r, s, w)
   auto take = [&](const float* x, int n, float m) {
@@ -175,55 +177,73 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
     const int per = (nvec + cluster - 1) / cluster;
     const int v0 = min(rank * per, nvec), v1 = min(v0 + per, nvec);
     const uint4* xv = reinterpret_cast<const uint4*>(xr + first);
+    const int tail0 = first + nvec * N;
     auto scalar = [&](int i, bool in) {                // one value per lane (loose ends)
       const float v = in ? Vec<T>::one(xr[i]) : -INFINITY;
       if (in) take(&v, 1, v);
-      if (ALTS) best.insert(in, make_key(v, (uint32_t)i), p.n_alts, floor_key, lane);
+      return v;
     };
-    if (wl == 0 && rank == 0) scalar(lane, lane < first);
+    float lead = 0.f, rear = 0.f;
+    const bool has_lead = wl == 0 && rank == 0, has_rear = wl == WARPS - 1 && rank == cluster - 1;
+    if (has_lead) lead = scalar(lane, lane < first);
     constexpr int STEP = WARPS * 32;
-    for (int v = v0 + wl * 32; v < v1; v += STEP * U) {         // the warp's first vector: the same trips in every lane
+    for (int v = v0 + wl * 32 + lane; v < v1; v += STEP * U) {
       uint4 q[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (v + u * STEP + lane < v1) q[u] = __ldcs(xv + v + u * STEP + lane);
-      if (ALTS && WARPS > 1) {
-        const unsigned long long f = *reinterpret_cast<volatile unsigned long long*>(&s_floor);
-        if (f > floor_key) floor_key = f;
-      }
+      for (int u = 0; u < U; ++u)                      // (with alternatives some are read again: they stay in L2)
+        if (v + u * STEP < v1) q[u] = ALTS ? __ldcg(xv + v + u * STEP) : __ldcs(xv + v + u * STEP);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int at = v + u * STEP + lane;
-        const bool in = at < v1;
-        float x[N];
-        Vec<T>::unpack(q[u], x);
-        float m = -INFINITY;
-        if (in) {
-          m = x[0];
+        if (v + u * STEP < v1) {
+          float x[N];
+          Vec<T>::unpack(q[u], x);
+          float m = x[0];
 #pragma unroll
-          for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+          for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);      // (passes over NaN)
           take(x, N, m);
-        }
-        if (ALTS) {
-          // (fmaxf skips NaN; a vector of nothing else has m = NaN, the lowest value)
-          const bool may = in && !(order_bits(m) < (uint32_t)(floor_key >> 32));
-          if (__any_sync(0xffffffffu, may)) {
-            const unsigned long long before = floor_key;
-#pragma unroll 1
-            for (int i = 0; i < N; ++i) {
-              float xi = x[0];
-#pragma unroll
-              for (int j = 1; j < N; ++j) xi = i == j ? x[j] : xi;
-              best.insert(in, make_key(xi, (uint32_t)(first + at * N + i)), p.n_alts, floor_key, lane);
-            }
-            if (WARPS > 1 && lane == 0 && floor_key > before) atomicMax(&s_floor, floor_key);
+          if (ALTS) {
+            any |= m == m;
+            top = fmaxf(top, m);
           }
         }
       }
     }
-    if (wl == WARPS - 1 && rank == cluster - 1) {
-      const int tail0 = first + nvec * N;
-      scalar(tail0 + lane, tail0 + lane < p.V);
+    if (has_rear) rear = scalar(tail0 + lane, tail0 + lane < p.V);
+    if (ALTS) {
+      const uint32_t mine = any ? order_bits(top) : 0u;        // 0: nothing that is a number
+      uint32_t left = mine, kth = 0u;
+      const int k = (p.n_alts + WARPS - 1) / WARPS;
+      for (int i = 0; i < k; ++i) {                    // the k-th largest of the lanes
+        kth = __reduce_max_sync(0xffffffffu, left);
+        const uint32_t who = __ballot_sync(0xffffffffu, left == kth);
+        if (lane == __ffs(who) - 1) left = 0u;
+      }
+      if (WARPS > 1) {
+        if (lane == 0) s_floor[warp] = kth;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) kth = min(kth, s_floor[i]);
+      }
+      // keys above floor_key: values that reach the floor (0: every key)
+      floor_key = kth == 0u ? 0ull : ((unsigned long long)kth << 32) - 1ull;
+      if (has_lead) best.insert(lane < first, make_key(lead, (uint32_t)lane), p.n_alts, floor_key, lane);
+      if (has_rear) best.insert(tail0 + lane < p.V, make_key(rear, (uint32_t)(tail0 + lane)), p.n_alts, floor_key, lane);
+      uint32_t hot = __ballot_sync(0xffffffffu, mine >= kth);
+      while (hot) {                                    // the vectors of one thread, a lane each
+        const int l = __ffs(hot) - 1;
+        hot &= hot - 1;
+        for (int v = v0 + wl * 32 + l; v < v1; v += STEP * 32) {
+          const int at = v + STEP * lane;
+          const bool in = at < v1;
+          float x[N];
+          Vec<T>::unpack(in ? __ldcg(xv + at) : make_uint4(0u, 0u, 0u, 0u), x);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const unsigned long long key = make_key(x[i], (uint32_t)(first + at * N + i));
+            if (__any_sync(0xffffffffu, in && key > floor_key)) best.insert(in, key, p.n_alts, floor_key, lane);
+          }
+        }
+      }
     }
   }
 
