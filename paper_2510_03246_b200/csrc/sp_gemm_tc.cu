@@ -213,6 +213,17 @@ __device__ __forceinline__ void linear_block(const TcParams& p, int64_t gj0, uin
   for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(linear_act(__uint_as_float(r[i]), p.lin.act));
 }
 
+// A bulk store moves whole 16-byte pieces: where N is no multiple of 8, the map of C ends at the last one, and the up to seven
+// columns behind it (of the last block) are stored here.
+__device__ __forceinline__ void linear_loose_columns(const TcParams& p, int64_t gj0, int64_t row, bool live, const uint32_t (&r)[32]) {
+  const int64_t whole = p.N & ~(int64_t)7;
+  if (gj0 + 32 <= whole || whole == p.N) return;
+  __nv_bfloat16* c = reinterpret_cast<__nv_bfloat16*>(p.c) + row * p.c_ld;
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (live && gj0 + i >= whole && gj0 + i < p.N) c[gj0 + i] = __float2bfloat16_rn(__uint_as_float(r[i]));
+}
+
 // BATCHED = false is the plain two-dimensional form (the products of the FFN path); BATCHED = true adds the batch
 // and plane coordinates (five-dimensional tensor maps).  Two instantiations, so that the plain form carries none of
 // the batched form's instructions.
@@ -477,13 +488,19 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 }
                 const __nv_bfloat162 o2 = __floats2bfloat162_rn(v0, v1);
                 ow[e] = *reinterpret_cast<const uint32_t*>(&o2);
+                if constexpr (LIN) {
+                  r[8 * j + 2 * e] = __float_as_uint(v0);
+                  r[8 * j + 2 * e + 1] = __float_as_uint(v1);
+                }
               }
               *reinterpret_cast<uint4*>(out_row + ((j ^ sw) << 4)) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
             }
+            if constexpr (LIN) linear_loose_columns(p, gj0, row0 + lane, lane < rows_here, r);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
-              tma_store_2d(&tmC, (int32_t)gj0, (int32_t)row0, wstg + 4096 + buf * 2048);
+              if (!LIN || gj0 + 8 <= p.N)      // (some whole piece is in the block)
+                tma_store_2d(&tmC, (int32_t)gj0, (int32_t)row0, wstg + 4096 + buf * 2048);
               bulk_commit();
             }
             cph ^= 1u << cbuf;
@@ -523,10 +540,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             if (p.c_lo_off > 0)
               *reinterpret_cast<uint4*>(out_row + 2048 + ((j ^ sw) << 4)) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
           }
+          if constexpr (LIN) linear_loose_columns(p, gj0, row0 + lane, lane < rows_here, r);
           fence_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (rows_here > 0) {
+            if (rows_here > 0 && (!LIN || gj0 + 8 <= p.N)) {      // (some whole piece is in the block)
               const uint32_t src = wstg + buf * 4096;
               if constexpr (BATCHED) {
                 const Coord5 cc = make_coord(p.c_ord, (int32_t)gj0, (int32_t)row0, b0, b1, 0);
@@ -877,22 +895,23 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
   }
   // bf16 C = beta * Cin + alpha * acc with a bf16 Cin: both through TMA
   if (p.epi_mode == EPI_DIRECT && !batched && p.c_lo_off == 0 && beta != 0.f && C.dtype == SP_BF16 && Cin.dtype == SP_BF16 &&
-      C.ld % 8 == 0 && N % 8 == 0 &&
+      C.ld % 8 == 0 && (N % 8 == 0 || (lin && N > 8)) &&
       Cin.s0 % 8 == 0 && (reinterpret_cast<uintptr_t>(C.ptr) & 15u) == 0 &&
       (reinterpret_cast<uintptr_t>(Cin.ptr) & 15u) == 0) {
-    if (!make_map(&tmC, false, C.ptr, N, M, C.ld, 32, 32, true) ||
+    if (!make_map(&tmC, false, C.ptr, N & ~(int64_t)7, M, C.ld, 32, 32, true) ||
         !make_map(&tmCin, false, Cin.ptr, N, M, Cin.s0, 32, 32, true))
       return SP_ERR_CUDA;
     p.epi_mode = EPI_TMA_BF16_CIN;
   }
   // bf16 C without Cin (one part, or hi and lo parts through a map each)
-  if (p.epi_mode == EPI_DIRECT && C.dtype == SP_BF16 && beta == 0.f && C.ld % 8 == 0 && N % 8 == 0 && C.lo_off % 8 == 0 &&
+  if (p.epi_mode == EPI_DIRECT && C.dtype == SP_BF16 && beta == 0.f && C.ld % 8 == 0 && (N % 8 == 0 || (lin && N > 8)) &&
+      C.lo_off % 8 == 0 &&
       (reinterpret_cast<uintptr_t>(C.ptr) & 15u) == 0 &&
       (!batched || ((batch->nb0 == 1 || batch->c_s0 % 8 == 0) && (batch->nb1 == 1 || batch->c_s1 % 8 == 0)))) {
     auto describe = [&](CUtensorMap* map, void* ptr) {
       return batched ? make_map5(map, false, ptr, N, 32, M, C.ld, 32, batch->nb0, batch->c_s0, batch->nb1, batch->c_s1, 1, 0,
                                  true, p.c_ord)
-                     : make_map(map, false, ptr, N, M, C.ld, 32, 32, true);
+                     : make_map(map, false, ptr, N & ~(int64_t)7, M, C.ld, 32, 32, true);
     };
     if (describe(&tmC, C.ptr) &&
         (p.c_lo_off == 0 || describe(&tmCin, reinterpret_cast<__nv_bfloat16*>(C.ptr) + p.c_lo_off)))
