@@ -13,6 +13,9 @@
 // that some row does not see whole, two warps clear the rows of V that no row sees, and set non-finite values in rows that only some see to
 // zero; those rows then get them back at the end (rows_with_bad_values).
 //
+// A tile of which only half 0 has rows (few queries, the end of a sequence) uses the tensor memory of both halves for its own key
+// tiles in turn ("alone"): the next S is computed while the softmax works on this one.
+//
 // Warps: 0-3 and 4-7 softmax of half 0 and 1 (lane and warp give the row), 8 TMA, 9 MMA issue and tensor memory, 10-11 edge tiles of V.
 // Waits for copies, the tensor core and other warps are bounded by a clock budget (SP_ERR_TIMEOUT through status).
 #include <math.h>
@@ -27,6 +30,9 @@ namespace {
 constexpr int kRows = 128, kKeys = 128;
 constexpr int kThreads = 384;
 constexpr long long kWaitBudget = 4000000000LL, kDrainBudget = 200000000LL;    // clock cycles: ~2 s, ~0.1 s
+// Registers of a thread: 168 at launch (384 threads); the eight softmax warps hold a whole row of S and take what the others leave.
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
+static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * 168, "shares of the registers at launch");
 constexpr int kBadSlots = 32;       // items between the edge warps and the epilogue: less than the stages of the ring
 
 template <int DH>
@@ -35,11 +41,12 @@ struct Cfg {
   static constexpr int CHUNK = 128 * 128;                  // bytes of one: 128 rows of 128 bytes
   static constexpr int TILE = CH * CHUNK;
   static constexpr int STAGES = DH == 128 ? 5 : 8;
-  static constexpr int BARS = 4 * STAGES + 12;
+  static constexpr int BARS = 4 * STAGES + 16;
   static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE + 1024 + 8 * BARS;
   static constexpr uint32_t S_COL = 0, O_COL = 256;        // tensor memory: S0 S1 | O0 O1
 };
 
+constexpr float kExp2C1 = 0.6931241750f, kExp2C2 = 0.2402409911f, kExp2C3 = 0.0559064261f, kExp2C4 = 0.0095828529f;
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -90,6 +97,48 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+// two fp32 operations per instruction
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {       // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// 2^t of two values on the fused multiply-add units: t = n + f with n the nearest whole number (an addition of 1.5 2^23 leaves it
+// in the low bits), 2^f on [-1/2, 1/2] by a polynomial of degree 4 with p(0) = 1, fitted for the least relative error (2.8e-06), n added to
+// the exponent.  t below -127 is taken as -127, where the sum of the exponents is zero: 2^-infinity = 0 exactly.  Not for NaN.
+__device__ __forceinline__ void exp2_poly(uint64_t t, float& e0, float& e1) {
+  float t0, t1;
+  unpack2(t, t0, t1);
+  t = pack2(fmaxf(t0, -127.f), fmaxf(t1, -127.f));
+  const uint64_t z = add2(t, pack2(12582912.f, 12582912.f));
+  const uint64_t f = fma2(add2(z, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), t);
+  uint64_t p = pack2(kExp2C4, kExp2C4);
+  p = fma2(p, f, pack2(kExp2C3, kExp2C3));
+  p = fma2(p, f, pack2(kExp2C2, kExp2C2));
+  p = fma2(p, f, pack2(kExp2C1, kExp2C1));
+  p = fma2(p, f, pack2(1.f, 1.f));
+  float z0, z1, p0, p1;
+  unpack2(z, z0, z1);
+  unpack2(p, p0, p1);
+  e0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(z0) << 23));
+  e1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(z1) << 23));
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // bf16 operands, fp32 accumulator, 128 x n; B K-major or (V: keys are K, channels contiguous) MN-major
@@ -109,6 +158,7 @@ struct Work {
   int t0;                    // first token of the tile within its sequence
   int kb;                    // first key of the part
   int n[2];                  // key tiles of each half
+  bool alone;                // half 1 has no rows
   int sure;                  // keys [0, sure) are seen by every row
   int seen;                  // keys [0, seen) are seen by some row (no later one is in the part either)
   __device__ __forceinline__ int tiles() const { return n[0] > n[1] ? n[0] : n[1]; }
@@ -127,6 +177,7 @@ __device__ __forceinline__ Work work_of(const TcAttnParams& p, const AttnItem& i
   const int end = cut && it.nk - w.kb > p.a.part ? w.kb + p.a.part : it.nk;
   w.sure = visible(it, p.a.causal, w.t0);
   w.seen = 0;
+  w.alone = w.t0 + p.tokens >= it.nq;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int first = w.t0 + h * p.tokens;
@@ -139,6 +190,10 @@ __device__ __forceinline__ Work work_of(const TcAttnParams& p, const AttnItem& i
   }
   return w;
 }
+
+// One pair of exponentials in kPolyEvery goes through exp2_poly: the special function unit alone would take as long per tile (1024 cycles for
+// a half) as the two products of 128 x 128 x 128.
+constexpr int kPolyEvery = 3;
 
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -164,6 +219,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   auto p_full = [&](int h) { return misc + 40u + 8u * h; };
   auto o_full = [&](int h) { return misc + 56u + 8u * h; };
   auto o_empty = [&](int h) { return misc + 72u + 8u * h; };
+  auto s1_full = [&](int x) { return misc + 88u + 8u * x; };      // a tile alone: S and P in the tensor memory of half x
+  auto p1_full = [&](int x) { return misc + 104u + 8u * x; };
+  const uint32_t pv_done = misc + 120u;                           // a tile alone: O += P V of a key tile
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = &s_abort;
@@ -180,11 +238,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     mbar_init(drain_bar, 1);
+    mbar_init(pv_done, 1);
     for (int h = 0; h < 2; ++h) {
       mbar_init(s_full(h), 1);
       mbar_init(p_full(h), 4);
       mbar_init(o_full(h), 1);
       mbar_init(o_empty(h), 4);
+      mbar_init(s1_full(h), 1);
+      mbar_init(p1_full(h), 4);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -203,193 +264,241 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   AttnDealer dealer;
   AttnItem it;
   int seq = 0;                // number of the item within this CTA
-  if (warp == 8) {
-    // ------------------------------------------------------------------------------------------------ TMA
-    uint32_t pos = 0;         // tiles loaded so far
-    int loaded = 0;           // items with keys so far (their Q was loaded)
-    bool ok = true;
-    for (int64_t item = blockIdx.x; dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x) {
-      const Work w = work_of(p, it);
-      const int n = w.tiles();
-      if (n == 0) continue;
-      if (lane == 0) {
-        const int kvh = p.gp == 1 ? it.head / p.a.g : it.head;
-        if (loaded > 0) ok = mbar_wait(q_empty, (uint32_t)(loaded - 1) & 1u, abort_flag, budget);
-        if (ok) {
-          const int halves = w.t0 + p.tokens < it.nq ? 2 : 1;
-          mbar_expect_tx(q_full, (uint32_t)(halves * C::CH * p.gp * p.tokens * 128));
-          for (int h = 0; h < halves; ++h)
-#pragma unroll
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == 8) {
+      // ------------------------------------------------------------------------------------------------ TMA
+      uint32_t pos = 0;         // tiles loaded so far
+      int loaded = 0;           // items with keys so far (their Q was loaded)
+      bool ok = true;
+      for (int64_t item = blockIdx.x; dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x) {
+        const Work w = work_of(p, it);
+        const int n = w.tiles();
+        if (n == 0) continue;
+        if (lane == 0) {
+          const int kvh = p.gp == 1 ? it.head / p.a.g : it.head;
+          if (loaded > 0) ok = mbar_wait(q_empty, (uint32_t)(loaded - 1) & 1u, abort_flag, budget);
+          if (ok) {
+            const int halves = w.alone ? 1 : 2;
+            mbar_expect_tx(q_full, (uint32_t)(halves * C::CH * p.gp * p.tokens * 128));
+            for (int h = 0; h < halves; ++h)
+  #pragma unroll
+              for (int c = 0; c < C::CH; ++c)
+                tma_load_3d(q_smem + h * C::TILE + c * C::CHUNK, &tmQ, c * 64, it.head * p.gp, it.q0 + w.t0 + h * p.tokens, q_full);
+          }
+          for (int i = 0; i < 2 * n && ok; ++i) {
+            const int s = (int)(pos % C::STAGES);
+            if (!mbar_wait(empty_bar(s), (pos / C::STAGES + 1) & 1u, abort_flag, budget)) { ok = false; break; }
+            const bool v = i & 1;
+            const uint32_t bar = v && w.edge(i >> 1) ? edge_bar(s) : full_bar(s);
+            mbar_expect_tx(bar, C::TILE);
+  #pragma unroll
             for (int c = 0; c < C::CH; ++c)
-              tma_load_3d(q_smem + h * C::TILE + c * C::CHUNK, &tmQ, c * 64, it.head * p.gp, it.q0 + w.t0 + h * p.tokens, q_full);
-        }
-        for (int i = 0; i < 2 * n && ok; ++i) {
-          const int s = (int)(pos % C::STAGES);
-          if (!mbar_wait(empty_bar(s), (pos / C::STAGES + 1) & 1u, abort_flag, budget)) { ok = false; break; }
-          const bool v = i & 1;
-          const uint32_t bar = v && w.edge(i >> 1) ? edge_bar(s) : full_bar(s);
-          mbar_expect_tx(bar, C::TILE);
-#pragma unroll
-          for (int c = 0; c < C::CH; ++c)
-            tma_load_3d(ring + s * C::TILE + c * C::CHUNK, v ? &tmV : &tmK, c * 64, kvh, it.k0 + w.kb + (i >> 1) * kKeys, bar);
-          ++pos;
-        }
-      }
-      ++loaded;
-      ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-      if (!ok) break;
-    }
-    if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 11);
-  } else if (warp == 9) {
-    // ------------------------------------------------------------------------------------------------ MMA
-    const uint32_t id_s = instr_desc(true, kKeys), id_o = instr_desc(false, DH);
-    uint32_t pos = 0, full_ph = 0, ready_ph = 0;      // phases of the barriers of a stage: a bit each
-    uint32_t p_ph = 0, oe_ph = 0;                     // of a half: a bit each
-    int loaded = 0;
-    bool ok = true, issued = false;
-    uint32_t wrote_o = 0;                             // halves that have had an output
-    for (int64_t item = blockIdx.x; dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x) {
-      const Work w = work_of(p, it);
-      const int n = w.tiles();
-      if (n == 0) continue;
-      if (lane == 0) {
-        auto stage_at = [&](uint32_t x) { return (int)(x % C::STAGES); };
-        auto wait_full = [&](int s) {
-          const bool got = mbar_wait(full_bar(s), (full_ph >> s) & 1u, abort_flag, budget);
-          full_ph ^= 1u << s;
-          return got;
-        };
-        auto scores = [&](int h, int s) {
-          const uint32_t a0 = q_smem + h * C::TILE, b0 = ring + s * C::TILE;
-#pragma unroll
-          for (int k = 0; k < DH / 16; ++k) {
-            const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32);
-            tc_mma_ss(tmem + C::S_COL + 128u * h, make_smem_desc(a0 + off, true, 0), make_smem_desc(b0 + off, true, 0), id_s, k > 0);
+              tma_load_3d(ring + s * C::TILE + c * C::CHUNK, v ? &tmV : &tmK, c * 64, kvh, it.k0 + w.kb + (i >> 1) * kKeys, bar);
+            ++pos;
           }
-          tc_commit_one(s_full(h));
-        };
-        ok = mbar_wait(q_full, (uint32_t)loaded & 1u, abort_flag, budget) && wait_full(stage_at(pos));
-        if (ok) {
-          tc_fence_after();
-          for (int h = 0; h < 2; ++h)
-            if (w.n[h] > 0) scores(h, stage_at(pos));
-          issued = true;
-          tc_commit_one(empty_bar(stage_at(pos)));
-          if (n == 1) tc_commit_one(q_empty);
         }
-        for (int i = 0; i < n && ok; ++i) {
-          const int sv = stage_at(pos + 1), sk = stage_at(pos + 2);
-          const bool more = i + 1 < n;
-          if (w.edge(i)) {
-            ok = mbar_wait(ready_bar(sv), (ready_ph >> sv) & 1u, abort_flag, budget);
-            ready_ph ^= 1u << sv;
-          } else {
-            ok = wait_full(sv);
-          }
-          if (ok && more) ok = wait_full(sk);
-          for (int h = 0; h < 2 && ok; ++h) {
-            if (i >= w.n[h]) continue;
-            ok = mbar_wait(p_full(h), (p_ph >> h) & 1u, abort_flag, budget);
-            p_ph ^= 1u << h;
-            if (ok && i == 0 && ((wrote_o >> h) & 1u)) {        // the item before has left O
-              ok = mbar_wait(o_empty(h), (oe_ph >> h) & 1u, abort_flag, budget);
-              oe_ph ^= 1u << h;
-            }
-            if (!ok) break;
-            tc_fence_after();
-#pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k)
-              tc_mma_ts(tmem + C::O_COL + 128u * h, tmem + C::S_COL + 128u * h + 8u * k,
-                        make_smem_desc(ring + sv * C::TILE + (uint32_t)k * 2048u, false, C::CHUNK), id_o, i > 0 || k > 0);
-            if (i + 1 < w.n[h]) {
-              scores(h, sk);
-            } else {
-              tc_commit_one(o_full(h));
-              wrote_o |= 1u << h;
-            }
-          }
-          if (!ok) break;
-          tc_commit_one(empty_bar(sv));
-          if (more) {
-            tc_commit_one(empty_bar(sk));
-            if (i + 2 == n) tc_commit_one(q_empty);
-          }
-          pos += 2;
-        }
-      }
-      ++loaded;
-      ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-      if (!ok) break;
-    }
-    if (lane == 0) {
-      if (!ok) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 12);
-      // (in a complete run the epilogues have seen the last products; this matters when a role gave up)
-      if (issued && (!ok || *abort_flag)) {
-        tc_commit_one(drain_bar);
-        const long long t0 = clock64();
-        while (!mbar_try(drain_bar, 0u) && clock64() - t0 < kDrainBudget) {}
-      }
-    }
-    __syncwarp();
-  } else if (warp >= 10) {
-    // ------------------------------------------------------------------------------------------------ edge tiles of V
-    const int tid = threadIdx.x - 320;               // 0 .. 63
-    uint32_t pos = 0, edge_ph = 0;
-    bool ok = true;
-    for (int64_t item = blockIdx.x; ok && dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x, ++seq) {
-      const Work w = work_of(p, it);
-      const int n = w.tiles();
-      for (int i = 0; i < n && ok; ++i, pos += 2) {
-        if (!w.edge(i)) continue;
-        const int s = (int)((pos + 1) % C::STAGES);
-        const bool got = mbar_wait(edge_bar(s), (edge_ph >> s) & 1u, abort_flag, budget);
-        edge_ph ^= 1u << s;
-        ok = __all_sync(0xffffffffu, got);
+        ++loaded;
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
         if (!ok) break;
-        const int k0 = w.kb + i * kKeys;
-        uint8_t* tile = smem_raw + (ring - raw) + (size_t)s * C::TILE;
-        bool found = false;
-        for (int j = tid; j < kKeys; j += 64) {
-          if (k0 + j < w.sure) continue;             // seen by every row
-          const bool clear = k0 + j >= w.seen;
-#pragma unroll
-          for (int c = 0; c < C::CH; ++c)
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              uint4* at = reinterpret_cast<uint4*>(tile + c * C::CHUNK + j * 128 + ((x + j) & 7) * 16);
-              if (clear) {
-                *at = make_uint4(0u, 0u, 0u, 0u);
-              } else {
-                const uint4 v = *at;
-                // a bf16 of all-ones exponent: its magnitude plus 0x80 reaches the sign bit
-                auto mark = [](uint32_t u) { return ((u & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; };
-                if (mark(v.x) | mark(v.y) | mark(v.z) | mark(v.w)) {
-                  auto fix = [&](uint32_t u) {
-                    const uint32_t b = mark(u);
-                    return u & ~((b & 0x8000u ? 0xffffu : 0u) | (b & 0x80000000u ? 0xffff0000u : 0u));
-                  };
-                  *at = make_uint4(fix(v.x), fix(v.y), fix(v.z), fix(v.w));
-                  found = true;
-                }
+      }
+      if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 11);
+    } else if (warp == 9) {
+      // ------------------------------------------------------------------------------------------------ MMA
+      const uint32_t id_s = instr_desc(true, kKeys), id_o = instr_desc(false, DH);
+      uint32_t pos = 0, full_ph = 0, ready_ph = 0;      // phases of the barriers of a stage: a bit each
+      uint32_t p_ph = 0, p1_ph = 0, oe_ph = 0;          // of a half: a bit each
+      int loaded = 0;
+      bool ok = true, issued = false;
+      uint32_t wrote_o = 0;                             // halves that have had an output
+      for (int64_t item = blockIdx.x; dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x) {
+        const Work w = work_of(p, it);
+        const int n = w.tiles();
+        if (n == 0) continue;
+        if (lane == 0) {
+          auto stage_at = [&](uint32_t x) { return (int)(x % C::STAGES); };
+          auto wait_full = [&](int s) {
+            const bool got = mbar_wait(full_bar(s), (full_ph >> s) & 1u, abort_flag, budget);
+            full_ph ^= 1u << s;
+            return got;
+          };
+          auto scores = [&](int h, int s, int at, uint32_t bar) {     // S of half h in the tensor memory of `at`
+            const uint32_t a0 = q_smem + h * C::TILE, b0 = ring + s * C::TILE;
+  #pragma unroll
+            for (int k = 0; k < DH / 16; ++k) {
+              const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32);
+              tc_mma_ss(tmem + C::S_COL + 128u * at, make_smem_desc(a0 + off, true, 0), make_smem_desc(b0 + off, true, 0), id_s, k > 0);
+            }
+            tc_commit_one(bar);
+          };
+          auto values = [&](int h, int s, int at, bool first) {       // O of half h += P V with P in the tensor memory of `at`
+  #pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k)
+              tc_mma_ts(tmem + C::O_COL + 128u * h, tmem + C::S_COL + 128u * at + 8u * k,
+                        make_smem_desc(ring + s * C::TILE + (uint32_t)k * 2048u, false, C::CHUNK), id_o, !first || k > 0);
+          };
+          auto wait_v = [&](int i, int s) {
+            if (!w.edge(i)) return wait_full(s);
+            const bool got = mbar_wait(ready_bar(s), (ready_ph >> s) & 1u, abort_flag, budget);
+            ready_ph ^= 1u << s;
+            return got;
+          };
+          ok = mbar_wait(q_full, (uint32_t)loaded & 1u, abort_flag, budget) && wait_full(stage_at(pos));
+          if (ok && w.alone) {
+            // S of tile i + 2 takes the place of P of tile i, behind the product that reads it
+            tc_fence_after();
+            scores(0, stage_at(pos), 0, s1_full(0));
+            issued = true;
+            tc_commit_one(empty_bar(stage_at(pos)));
+            if (n == 1) tc_commit_one(q_empty);
+            if (n > 1) {
+              ok = wait_full(stage_at(pos + 2));
+              if (ok) {
+                tc_fence_after();
+                scores(0, stage_at(pos + 2), 1, s1_full(1));
+                tc_commit_one(empty_bar(stage_at(pos + 2)));
+                if (n == 2) tc_commit_one(q_empty);
               }
             }
+            for (int i = 0; i < n && ok; ++i, pos += 2) {
+              const int x = i & 1, sv = stage_at(pos + 1), sk = stage_at(pos + 4);
+              ok = wait_v(i, sv) && mbar_wait(p1_full(x), (p1_ph >> x) & 1u, abort_flag, budget);
+              p1_ph ^= 1u << x;
+              if (ok && i == 0 && (wrote_o & 1u)) {
+                ok = mbar_wait(o_empty(0), oe_ph & 1u, abort_flag, budget);
+                oe_ph ^= 1u;
+              }
+              if (!ok) break;
+              tc_fence_after();
+              values(0, sv, x, i == 0);
+              tc_commit_one(pv_done);
+              tc_commit_one(empty_bar(sv));
+              wrote_o |= 1u;
+              if (i + 2 < n) {
+                ok = wait_full(sk);
+                if (!ok) break;
+                tc_fence_after();
+                scores(0, sk, x, s1_full(x));
+                tc_commit_one(empty_bar(sk));
+                if (i + 3 == n) tc_commit_one(q_empty);
+              }
+            }
+          } else if (ok) {
+            tc_fence_after();
+            for (int h = 0; h < 2; ++h)
+              if (w.n[h] > 0) scores(h, stage_at(pos), h, s_full(h));
+            issued = true;
+            tc_commit_one(empty_bar(stage_at(pos)));
+            if (n == 1) tc_commit_one(q_empty);
+          }
+          for (int i = 0; i < n && ok && !w.alone; ++i) {
+            const int sv = stage_at(pos + 1), sk = stage_at(pos + 2);
+            const bool more = i + 1 < n;
+            ok = wait_v(i, sv);
+            if (ok && more) ok = wait_full(sk);
+            for (int h = 0; h < 2 && ok; ++h) {
+              if (i >= w.n[h]) continue;
+              ok = mbar_wait(p_full(h), (p_ph >> h) & 1u, abort_flag, budget);
+              p_ph ^= 1u << h;
+              if (ok && i == 0 && ((wrote_o >> h) & 1u)) {        // the item before has left O
+                ok = mbar_wait(o_empty(h), (oe_ph >> h) & 1u, abort_flag, budget);
+                oe_ph ^= 1u << h;
+              }
+              if (!ok) break;
+              tc_fence_after();
+              values(h, sv, h, i == 0);
+              if (i + 1 < w.n[h]) {
+                scores(h, sk, h, s_full(h));
+              } else {
+                tc_commit_one(o_full(h));
+                wrote_o |= 1u << h;
+              }
+            }
+            if (!ok) break;
+            tc_commit_one(empty_bar(sv));
+            if (more) {
+              tc_commit_one(empty_bar(sk));
+              if (i + 2 == n) tc_commit_one(q_empty);
+            }
+            pos += 2;
+          }
         }
-        if (found) *reinterpret_cast<volatile int*>(&s_bad[seq % kBadSlots]) = seq;
-        fence_async_smem();                          // the tensor core reads what was written here
-        __syncwarp();
-        if (lane == 0) mbar_arrive(ready_bar(s));
+        ++loaded;
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (!ok) break;
       }
+      if (lane == 0) {
+        if (!ok) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 12);
+        // (in a complete run the epilogues have seen the last products; this matters when a role gave up)
+        if (issued && (!ok || *abort_flag)) {
+          tc_commit_one(drain_bar);
+          const long long t0 = clock64();
+          while (!mbar_try(drain_bar, 0u) && clock64() - t0 < kDrainBudget) {}
+        }
+      }
+      __syncwarp();
+    } else {
+      // ------------------------------------------------------------------------------------------------ edge tiles of V
+      const int tid = threadIdx.x - 320;               // 0 .. 63
+      uint32_t pos = 0, edge_ph = 0;
+      bool ok = true;
+      for (int64_t item = blockIdx.x; ok && dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x, ++seq) {
+        const Work w = work_of(p, it);
+        const int n = w.tiles();
+        for (int i = 0; i < n && ok; ++i, pos += 2) {
+          if (!w.edge(i)) continue;
+          const int s = (int)((pos + 1) % C::STAGES);
+          const bool got = mbar_wait(edge_bar(s), (edge_ph >> s) & 1u, abort_flag, budget);
+          edge_ph ^= 1u << s;
+          ok = __all_sync(0xffffffffu, got);
+          if (!ok) break;
+          const int k0 = w.kb + i * kKeys;
+          uint8_t* tile = smem_raw + (ring - raw) + (size_t)s * C::TILE;
+          bool found = false;
+          for (int j = tid; j < kKeys; j += 64) {
+            if (k0 + j < w.sure) continue;             // seen by every row
+            const bool clear = k0 + j >= w.seen;
+  #pragma unroll
+            for (int c = 0; c < C::CH; ++c)
+  #pragma unroll
+              for (int x = 0; x < 8; ++x) {
+                uint4* at = reinterpret_cast<uint4*>(tile + c * C::CHUNK + j * 128 + ((x + j) & 7) * 16);
+                if (clear) {
+                  *at = make_uint4(0u, 0u, 0u, 0u);
+                } else {
+                  const uint4 v = *at;
+                  // a bf16 of all-ones exponent: its magnitude plus 0x80 reaches the sign bit
+                  auto mark = [](uint32_t u) { return ((u & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; };
+                  if (mark(v.x) | mark(v.y) | mark(v.z) | mark(v.w)) {
+                    auto fix = [&](uint32_t u) {
+                      const uint32_t b = mark(u);
+                      return u & ~((b & 0x8000u ? 0xffffu : 0u) | (b & 0x80000000u ? 0xffff0000u : 0u));
+                    };
+                    *at = make_uint4(fix(v.x), fix(v.y), fix(v.z), fix(v.w));
+                    found = true;
+                  }
+                }
+              }
+          }
+          if (found) *reinterpret_cast<volatile int*>(&s_bad[seq % kBadSlots]) = seq;
+          fence_async_smem();                          // the tensor core reads what was written here
+          __syncwarp();
+          if (lane == 0) mbar_arrive(ready_bar(s));
+        }
+      }
+      if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 13);
     }
-    if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 13);
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     // ------------------------------------------------------------------------------------------------ softmax and output
     const int h = warp >> 2, q = warp & 3;
     const int row = q * 32 + lane;                   // of the half, and lane of tensor memory
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
-    const uint32_t t_s = tmem + C::S_COL + 128u * h + lanes, t_o = tmem + C::O_COL + 128u * h + lanes;
+    const uint32_t t_o = tmem + C::O_COL + 128u * h + lanes;
     const float c = p.a.scale_log2;
-    uint32_t s_ph = 0, o_ph = 0;
+    uint32_t s_ph = 0, o_ph = 0, s1_ph = 0, pv_ph = 0;
     bool ok = true;
+    const uint64_t c2 = pack2(c, c);
     for (int64_t item = blockIdx.x; ok && dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x, ++seq) {
       const Work w = work_of(p, it);
       const int token = w.t0 + h * p.tokens + row / p.gp;
@@ -399,10 +508,22 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const int n = w.n[h];
       float r = -INFINITY, l = 0.f;                  // reference (not yet times c) and sum
       for (int i = 0; i < n; ++i) {
-        const bool got = mbar_wait(s_full(h), s_ph, abort_flag, budget);
-        s_ph ^= 1u;
+        const int at = w.alone ? i & 1 : h;          // whose tensor memory holds S and takes P
+        const uint32_t t_s = tmem + C::S_COL + 128u * at + lanes;
+        bool got = mbar_wait(w.alone ? s1_full(at) : s_full(h), w.alone ? (s1_ph >> at) & 1u : s_ph, abort_flag, budget);
+        if (w.alone) s1_ph ^= 1u << at;
+        else s_ph ^= 1u;
         ok = __all_sync(0xffffffffu, got);
         if (!ok) break;
+        // (a tile alone: the product of the tile before may still add to O, unlike with two halves, where S follows it)
+        bool o_still = !(w.alone && i > 0);
+        auto wait_o_still = [&] {
+          if (o_still) return;
+          got = mbar_wait(pv_done, pv_ph, abort_flag, budget);
+          pv_ph ^= 1u;
+          o_still = true;
+          ok = __all_sync(0xffffffffu, got);
+        };
         if (busy) {
           tc_fence_after();
           uint32_t x[128];
@@ -419,15 +540,18 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
           for (int b = 0; b < 4; ++b) m4[b] = __uint_as_float(x[b]);
 #pragma unroll
-          for (int j = 4; j < kKeys; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(x[j]));
-          const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-          // the reference follows a maximum that has risen by more than 2^8 (from -infinity: by anything)
-          const bool rise = m > r && (m - r) * c > 8.f;
+          for (int j = 4; j < kKeys; ++j) m4[j & 3] = max_nan(m4[j & 3], __uint_as_float(x[j]));
+          const float m = max_nan(max_nan(m4[0], m4[1]), max_nan(m4[2], m4[3]));
+          // the reference follows a maximum that has risen by more than 2^8 (from -infinity: by anything), and a NaN
+          const bool rise = m != -INFINITY && !((m - r) * c <= 8.f);
           if (__any_sync(0xffffffffu, rise)) {
             const float f = rise ? exp2_fast((r - m) * c) : 1.f;       // r = -infinity: 0
             if (rise) r = m;
             l *= f;
             if (i > 0) {
+              wait_o_still();
+              if (!ok) break;
+              tc_fence_after();
 #pragma unroll 1
               for (int b = 0; b < DH / 32; ++b) {
                 uint32_t o[32];
@@ -440,27 +564,38 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
           }
           const float shift = r == -INFINITY ? 0.f : -r * c;
-          float l2[2] = {0.f, 0.f};
+          const uint64_t shift2 = pack2(shift, shift);
+          uint64_t l2 = pack2(l, 0.f);
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             uint32_t w16[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-              const float e0 = exp2_fast(fmaf(__uint_as_float(x[32 * b + 2 * j]), c, shift));
-              const float e1 = exp2_fast(fmaf(__uint_as_float(x[32 * b + 2 * j + 1]), c, shift));
-              l2[0] += e0;
-              l2[1] += e1;
+              const uint64_t t = fma2(pack2(__uint_as_float(x[32 * b + 2 * j]), __uint_as_float(x[32 * b + 2 * j + 1])), c2, shift2);
+              float e0, e1;
+              if (j % kPolyEvery == kPolyEvery - 1) {
+                exp2_poly(t, e0, e1);
+              } else {
+                unpack2(t, e0, e1);
+                e0 = exp2_fast(e0);
+                e1 = exp2_fast(e1);
+              }
+              l2 = add2(l2, pack2(e0, e1));
               const __nv_bfloat162 e = __floats2bfloat162_rn(e0, e1);
               w16[j] = *reinterpret_cast<const uint32_t*>(&e);
             }
             tc_st16(t_s + 16u * b, w16);
           }
-          l += l2[0] + l2[1];
+          float l0, l1;
+          unpack2(l2, l0, l1);
+          l = l0 + l1;
           tc_wait_st();
           tc_fence_before();
         }
+        wait_o_still();      // at the latest here, so that no phase of the barrier is passed over
+        if (!ok) break;
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(h));
+        if (lane == 0) mbar_arrive(w.alone ? p1_full(at) : p_full(h));
       }
       if (!ok) break;
       // ---- output of the item
@@ -474,8 +609,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         : nullptr;
       bool bad = false;
       if (n > 0) {
-        const bool got = mbar_wait(o_full(h), o_ph, abort_flag, budget);
-        o_ph ^= 1u;
+        const bool got = mbar_wait(w.alone ? pv_done : o_full(h), w.alone ? pv_ph : o_ph, abort_flag, budget);
+        if (w.alone) pv_ph ^= 1u;
+        else o_ph ^= 1u;
         ok = __all_sync(0xffffffffu, got);
         if (!ok) break;
         tc_fence_after();
