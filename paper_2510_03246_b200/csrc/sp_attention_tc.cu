@@ -46,7 +46,6 @@ struct Cfg {
   static constexpr uint32_t S_COL = 0, O_COL = 256;        // tensor memory: S0 S1 | O0 O1
 };
 
-constexpr float kExp2C1 = 0.6931241750f, kExp2C2 = 0.2402409911f, kExp2C3 = 0.0559064261f, kExp2C4 = 0.0095828529f;
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -114,30 +113,10 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {       // NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b, float c) {       // NaN if one of them is
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-// 2^t of two values on the fused multiply-add units: t = n + f with n the nearest whole number (an addition of 1.5 2^23 leaves it
-// in the low bits), 2^f on [-1/2, 1/2] by a polynomial of degree 4 with p(0) = 1, fitted for the least relative error (2.8e-06), n added to
-// the exponent.  t below -127 is taken as -127, where the sum of the exponents is zero: 2^-infinity = 0 exactly.  Not for NaN.
-__device__ __forceinline__ void exp2_poly(uint64_t t, float& e0, float& e1) {
-  float t0, t1;
-  unpack2(t, t0, t1);
-  t = pack2(fmaxf(t0, -127.f), fmaxf(t1, -127.f));
-  const uint64_t z = add2(t, pack2(12582912.f, 12582912.f));
-  const uint64_t f = fma2(add2(z, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), t);
-  uint64_t p = pack2(kExp2C4, kExp2C4);
-  p = fma2(p, f, pack2(kExp2C3, kExp2C3));
-  p = fma2(p, f, pack2(kExp2C2, kExp2C2));
-  p = fma2(p, f, pack2(kExp2C1, kExp2C1));
-  p = fma2(p, f, pack2(1.f, 1.f));
-  float z0, z1, p0, p1;
-  unpack2(z, z0, z1);
-  unpack2(p, p0, p1);
-  e0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(z0) << 23));
-  e1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(z1) << 23));
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -191,9 +170,11 @@ __device__ __forceinline__ Work work_of(const TcAttnParams& p, const AttnItem& i
   return w;
 }
 
-// One pair of exponentials in kPolyEvery goes through exp2_poly: the special function unit alone would take as long per tile (1024 cycles for
-// a half) as the two products of 128 x 128 x 128.
-constexpr int kPolyEvery = 3;
+// The k-th item of this CTA.  Items of a sequence get lighter; every other round is dealt backwards, so that no CTA always has the
+// heavier ones (one prompt of 8192: busy cycles of the SMs from 0.86 to 1.14 of their mean without).
+__device__ __forceinline__ int64_t item_of(int k) {
+  return (int64_t)k * gridDim.x + (k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+}
 
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -271,7 +252,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       uint32_t pos = 0;         // tiles loaded so far
       int loaded = 0;           // items with keys so far (their Q was loaded)
       bool ok = true;
-      for (int64_t item = blockIdx.x; dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x) {
+      for (int k = 0; dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
         const Work w = work_of(p, it);
         const int n = w.tiles();
         if (n == 0) continue;
@@ -311,7 +292,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       int loaded = 0;
       bool ok = true, issued = false;
       uint32_t wrote_o = 0;                             // halves that have had an output
-      for (int64_t item = blockIdx.x; dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x) {
+      for (int k = 0; dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
         const Work w = work_of(p, it);
         const int n = w.tiles();
         if (n == 0) continue;
@@ -442,7 +423,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const int tid = threadIdx.x - 320;               // 0 .. 63
       uint32_t pos = 0, edge_ph = 0;
       bool ok = true;
-      for (int64_t item = blockIdx.x; ok && dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x, ++seq) {
+      for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k, ++seq) {
         const Work w = work_of(p, it);
         const int n = w.tiles();
         for (int i = 0; i < n && ok; ++i, pos += 2) {
@@ -499,7 +480,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     uint32_t s_ph = 0, o_ph = 0, s1_ph = 0, pv_ph = 0;
     bool ok = true;
     const uint64_t c2 = pack2(c, c);
-    for (int64_t item = blockIdx.x; ok && dealer.find(p.a, item, 2 * p.tokens, 1, p.heads, it); item += gridDim.x, ++seq) {
+    for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k, ++seq) {
       const Work w = work_of(p, it);
       const int token = w.t0 + h * p.tokens + row / p.gp;
       const bool valid = row < p.gp * p.tokens && token < it.nq;
@@ -540,8 +521,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
           for (int b = 0; b < 4; ++b) m4[b] = __uint_as_float(x[b]);
 #pragma unroll
-          for (int j = 4; j < kKeys; ++j) m4[j & 3] = max_nan(m4[j & 3], __uint_as_float(x[j]));
-          const float m = max_nan(max_nan(m4[0], m4[1]), max_nan(m4[2], m4[3]));
+          for (int j = 4; j + 8 <= kKeys; j += 8)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) m4[b] = max_nan(m4[b], __uint_as_float(x[j + 2 * b]), __uint_as_float(x[j + 2 * b + 1]));
+#pragma unroll
+          for (int b = 0; b < 4; ++b) m4[b] = max_nan(m4[b], __uint_as_float(x[kKeys - 4 + b]), m4[b]);
+          const float m = max_nan(max_nan(m4[0], m4[1], m4[2]), m4[3], m4[3]);
           // the reference follows a maximum that has risen by more than 2^8 (from -infinity: by anything), and a NaN
           const bool rise = m != -INFINITY && !((m - r) * c <= 8.f);
           if (__any_sync(0xffffffffu, rise)) {
@@ -573,13 +558,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             for (int j = 0; j < 16; ++j) {
               const uint64_t t = fma2(pack2(__uint_as_float(x[32 * b + 2 * j]), __uint_as_float(x[32 * b + 2 * j + 1])), c2, shift2);
               float e0, e1;
-              if (j % kPolyEvery == kPolyEvery - 1) {
-                exp2_poly(t, e0, e1);
-              } else {
-                unpack2(t, e0, e1);
-                e0 = exp2_fast(e0);
-                e1 = exp2_fast(e1);
-              }
+              unpack2(t, e0, e1);
+              e0 = exp2_fast(e0);
+              e1 = exp2_fast(e1);
               l2 = add2(l2, pack2(e0, e1));
               const __nv_bfloat162 e = __floats2bfloat162_rn(e0, e1);
               w16[j] = *reinterpret_cast<const uint32_t*>(&e);
