@@ -41,7 +41,7 @@ struct Cfg {
   static constexpr int CHUNK = 128 * 128;                  // bytes of one: 128 rows of 128 bytes
   static constexpr int TILE = CH * CHUNK;
   static constexpr int STAGES = DH == 128 ? 5 : 8;
-  static constexpr int BARS = 4 * STAGES + 16;
+  static constexpr int BARS = 4 * STAGES + 18;
   static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE + 1024 + 8 * BARS;
   static constexpr uint32_t S_COL = 0, O_COL = 256;        // tensor memory: S0 S1 | O0 O1
 };
@@ -63,18 +63,22 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 __device__ __forceinline__ void tc_commit_one(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// Shared-memory descriptors (make_smem_desc of sp_tc.cuh) in two words: the upper one is the same for all tiles here, the lower
+// one moves with the address in units of 16 bytes, so that an instruction's descriptors cost an addition.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t leading) { return ((addr & 0x3ffffu) >> 4) | ((leading >> 4) << 16); }
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+      ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
       : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b_low, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b_low), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
       : "memory");
 }
 __device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* r) {
@@ -117,6 +121,13 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {       // N
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
+}
+// One lane of a converged warp, chosen by the hardware.  Behind this branch the compiler knows that one lane is active and keeps the
+// operands of the matrix instructions in uniform registers; behind lane == 0 every issue cost 75 cycles.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t pred;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
+  return pred != 0;
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -202,6 +213,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   auto o_empty = [&](int h) { return misc + 72u + 8u * h; };
   auto s1_full = [&](int x) { return misc + 88u + 8u * x; };      // a tile alone: S and P in the tensor memory of half x
   auto p1_full = [&](int x) { return misc + 104u + 8u * x; };
+  auto p_half = [&](int h) { return misc + 128u + 8u * h; };      // the first 64 columns of P
   const uint32_t pv_done = misc + 120u;                           // a tile alone: O += P V of a key tile
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -223,6 +235,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     for (int h = 0; h < 2; ++h) {
       mbar_init(s_full(h), 1);
       mbar_init(p_full(h), 4);
+      mbar_init(p_half(h), 4);
       mbar_init(o_full(h), 1);
       mbar_init(o_empty(h), 4);
       mbar_init(s1_full(h), 1);
@@ -296,7 +309,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const Work w = work_of(p, it);
         const int n = w.tiles();
         if (n == 0) continue;
-        if (lane == 0) {
+        if (elect_one()) {
           auto stage_at = [&](uint32_t x) { return (int)(x % C::STAGES); };
           auto wait_full = [&](int s) {
             const bool got = mbar_wait(full_bar(s), (full_ph >> s) & 1u, abort_flag, budget);
@@ -304,19 +317,20 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             return got;
           };
           auto scores = [&](int h, int s, int at, uint32_t bar) {     // S of half h in the tensor memory of `at`
-            const uint32_t a0 = q_smem + h * C::TILE, b0 = ring + s * C::TILE;
+            const uint32_t a0 = desc_low(q_smem + h * C::TILE, 16), b0 = desc_low(ring + s * C::TILE, 16);
   #pragma unroll
             for (int k = 0; k < DH / 16; ++k) {
-              const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32);
-              tc_mma_ss(tmem + C::S_COL + 128u * at, make_smem_desc(a0 + off, true, 0), make_smem_desc(b0 + off, true, 0), id_s, k > 0);
+              const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
+              tc_mma_ss(tmem + C::S_COL + 128u * at, a0 + off, b0 + off, id_s, k > 0);
             }
             tc_commit_one(bar);
           };
-          auto values = [&](int h, int s, int at, bool first) {       // O of half h += P V with P in the tensor memory of `at`
-  #pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k)
-              tc_mma_ts(tmem + C::O_COL + 128u * h, tmem + C::S_COL + 128u * at + 8u * k,
-                        make_smem_desc(ring + s * C::TILE + (uint32_t)k * 2048u, false, C::CHUNK), id_o, !first || k > 0);
+          // O of half h += P V over half `part` of the keys, P in the tensor memory of `at`
+          auto values = [&](int h, int s, int at, bool first, int part) {
+            const uint32_t v0 = desc_low(ring + s * C::TILE + part * (kKeys / 2 * 128), C::CHUNK);
+            const uint32_t d = tmem + C::O_COL + 128u * h, a0 = tmem + C::S_COL + 128u * at + 32u * part;
+#pragma unroll
+            for (int k = 0; k < kKeys / 32; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, !first || k > 0);
           };
           auto wait_v = [&](int i, int s) {
             if (!w.edge(i)) return wait_full(s);
@@ -351,7 +365,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               }
               if (!ok) break;
               tc_fence_after();
-              values(0, sv, x, i == 0);
+              values(0, sv, x, i == 0, 0);
+              values(0, sv, x, false, 1);
               tc_commit_one(pv_done);
               tc_commit_one(empty_bar(sv));
               wrote_o |= 1u;
@@ -379,15 +394,19 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             if (ok && more) ok = wait_full(sk);
             for (int h = 0; h < 2 && ok; ++h) {
               if (i >= w.n[h]) continue;
-              ok = mbar_wait(p_full(h), (p_ph >> h) & 1u, abort_flag, budget);
-              p_ph ^= 1u << h;
+              ok = mbar_wait(p_half(h), (p_ph >> h) & 1u, abort_flag, budget);
               if (ok && i == 0 && ((wrote_o >> h) & 1u)) {        // the item before has left O
                 ok = mbar_wait(o_empty(h), (oe_ph >> h) & 1u, abort_flag, budget);
                 oe_ph ^= 1u << h;
               }
               if (!ok) break;
               tc_fence_after();
-              values(h, sv, h, i == 0);
+              values(h, sv, h, i == 0, 0);
+              ok = mbar_wait(p_full(h), (p_ph >> h) & 1u, abort_flag, budget);
+              p_ph ^= 1u << h;
+              if (!ok) break;
+              tc_fence_after();
+              values(h, sv, h, false, 1);
               if (i + 1 < w.n[h]) {
                 scores(h, sk, h, s_full(h));
               } else {
@@ -405,7 +424,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           }
         }
         ++loaded;
-        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
       }
       if (lane == 0) {
@@ -517,16 +536,19 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             for (int j = 0; j < kKeys; ++j)
               if (j >= left) x[j] = 0xff800000u;
           }
-          float m4[4];
+          float m8[8];
 #pragma unroll
-          for (int b = 0; b < 4; ++b) m4[b] = __uint_as_float(x[b]);
+          for (int y = 0; y < 8; ++y)
+            m8[y] = max_nan(__uint_as_float(x[3 * y]), __uint_as_float(x[3 * y + 1]), __uint_as_float(x[3 * y + 2]));
 #pragma unroll
-          for (int j = 4; j + 8 <= kKeys; j += 8)
+          for (int j = 24; j + 16 <= kKeys; j += 16)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) m4[b] = max_nan(m4[b], __uint_as_float(x[j + 2 * b]), __uint_as_float(x[j + 2 * b + 1]));
+            for (int y = 0; y < 8; ++y) m8[y] = max_nan(m8[y], __uint_as_float(x[j + 2 * y]), __uint_as_float(x[j + 2 * y + 1]));
+          static_assert((kKeys - 24) % 16 == 8, "the last eight");
 #pragma unroll
-          for (int b = 0; b < 4; ++b) m4[b] = max_nan(m4[b], __uint_as_float(x[kKeys - 4 + b]), m4[b]);
-          const float m = max_nan(max_nan(m4[0], m4[1], m4[2]), m4[3], m4[3]);
+          for (int y = 0; y < 4; ++y)
+            m8[y] = max_nan(m8[y], __uint_as_float(x[kKeys - 8 + 2 * y]), __uint_as_float(x[kKeys - 7 + 2 * y]));
+          const float m = max_nan(max_nan(m8[0], m8[1], m8[2]), max_nan(m8[3], m8[4], m8[5]), max_nan(m8[6], m8[7], m8[7]));
           // the reference follows a maximum that has risen by more than 2^8 (from -infinity: by anything), and a NaN
           const bool rise = m != -INFINITY && !((m - r) * c <= 8.f);
           if (__any_sync(0xffffffffu, rise)) {
@@ -566,6 +588,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               w16[j] = *reinterpret_cast<const uint32_t*>(&e);
             }
             tc_st16(t_s + 16u * b, w16);
+            if (b == 1 && !w.alone) {                // the tensor core starts on these keys
+              tc_wait_st();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(p_half(h));
+            }
           }
           float l0, l1;
           unpack2(l2, l0, l1);
@@ -573,6 +601,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           tc_wait_st();
           tc_fence_before();
         }
+        if (!busy && !w.alone && lane == 0) mbar_arrive(p_half(h));
         wait_o_still();      // at the latest here, so that no phase of the barrier is passed over
         if (!ok) break;
         __syncwarp();
