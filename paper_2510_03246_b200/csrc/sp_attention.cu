@@ -254,7 +254,7 @@ cudaError_t launch_simt(const AttnParams& p, cudaStream_t stream) {
 template <typename T>
 cudaError_t launch_simt(const AttnParams& p, cudaStream_t stream) {
   // 16 rows where the sequences have no more on average (single tokens): a tile's products are the bound there
-  const bool few = (int64_t)p.Nq * p.g <= (int64_t)16 * p.n_seq;
+  const bool few = attention_few_rows(p.Nq, p.g, p.n_seq);
   if (p.dh <= 64) return few ? launch_simt<T, 64, 16>(p, stream) : launch_simt<T, 64, 64>(p, stream);
   return few ? launch_simt<T, 128, 16>(p, stream) : launch_simt<T, 128, 64>(p, stream);
 }
@@ -265,17 +265,18 @@ struct Cut {
 };
 // Whether and how the key axis is cut.  Without a cut there are about Nq g / 128 tiles of rows, at least one for every sequence
 // that has queries, times the key heads; fewer than the SMs (148) leave SMs idle.  Parts are then as long as gives four for every SM
-// (so that sequences of different lengths even out), at least 256 keys (a part costs its result's way through memory and
-// a second launch).
+// (so that sequences of different lengths even out), eight with few rows, at least 256 keys (a part costs its
+// result's way through memory and a second launch).
 Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh) {
   Cut cut;
   if (Nq < 1 || Nk < 1 || n_seq < 1) return cut;
   const int64_t g = n_heads / n_kv, sms = 148;
   const int64_t seqs = n_seq < Nq ? n_seq : Nq;
   const int64_t tiles = (Nq * g / 128 > seqs ? Nq * g / 128 : seqs) * n_kv;
-  if (tiles >= 2 * sms) return cut;
+  const int64_t per_sm = attention_few_rows(Nq, g, n_seq) ? 8 : 4;
+  if (tiles >= sms * per_sm / 2) return cut;
   const int64_t per_tile = ceil_div(Nk, seqs);                 // keys of a tile, on average
-  int64_t part = (int64_t)align_up((size_t)ceil_div(tiles * per_tile, sms * 4), 128);
+  int64_t part = (int64_t)align_up((size_t)ceil_div(tiles * per_tile, sms * per_sm), 128);
   if (part < 256) part = 256;
   if (part >= Nk) return cut;                                   // nothing is longer
   const int64_t parts = ceil_div(Nk, part);
@@ -345,7 +346,10 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
   const bool tc = dt == SP_BF16 && attention_tc_supported(p);
   ProfScope prof(tc ? PK_GEMM_TC : PK_GEMM_SIMT, 0.0, 0.0, s);
   count_launch();
-  if (tc) {
+  if (tc && attention_few_rows(Nq, p.g, a->n_seq)) {
+    const sp_status st = attention_rows(p, s);
+    if (st != SP_OK) return st;
+  } else if (tc) {
     const sp_status st = attention_tc(p, s);
     if (st != SP_OK) return st;
   } else if ((dt == SP_F32 ? launch_simt<float>(p, s) : launch_simt<__nv_bfloat16>(p, s)) != cudaSuccess) return SP_ERR_CUDA;
