@@ -492,8 +492,13 @@ sp_status sp_linear(const sp_mat* X, const sp_mat* W, const float* bias, int32_t
   const OutOperand y{Y->ptr, Y->dtype, Y->ld};
   if (X->dtype == SP_BF16) {
     TcOperand ta{X->ptr, X->ld, true}, tb{W->ptr, W->ld, true};
-    if (gemm_tc_supported(T, N, K, ta, tb))
+    if (gemm_tc_supported(T, N, K, ta, tb)) {
+      if (T <= kLinearFewRows) {
+        CU(linear_few(T, N, K, ta, tb, epi, o, y, s));
+        return SP_OK;
+      }
       return gemm_tc(T, N, K, 1.f, ta, tb, other ? 1.f : 0.f, o, y, false, status_dev, s, nullptr, -1.0, 0, nullptr, &epi);
+    }
   }
   CU(linear_simt(T, N, K, Operand{X->ptr, X->dtype, X->ld, 1}, Operand{W->ptr, W->dtype, W->ld, 1}, epi, o, y, s));
   return SP_OK;

@@ -19,15 +19,37 @@ __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // A tile of BM rows (queries x the heads that share a key head) against tiles of 64 keys.  256 threads as 16 x 16: a thread
-// has BM / 16 rows x 4 keys of the logits and BM / 16 rows x DH / 16 columns of O.  All operands lie in shared memory as
-// fp32 with the index that a thread's own values run along innermost (Q and K turned: [d][row], [d][key]; P as [key][row]),
-// so that both products read 16-byte pieces.
+// has BM / 16 rows x 4 keys (tx, tx + 16, ...) of the logits and BM / 16 rows x DH / 16 columns of O.  Operands lie in shared memory as fp32
+// in rows of a pitch 4 beyond a multiple of 32, so that both products read 16-byte pieces along their inner index, eight lanes on
+// eight rows without a bank twice: two such reads for 16 fused multiply-adds.
 template <typename T, int DH, int BM>
 struct SimtTile {
-  static constexpr int PQ = BM + 4, PK = kBN + 4, PV = DH, PP = BM + 4;
-  static constexpr int kQ = DH * PQ, kK = DH * PK, kV = kBN * PV, kP = kBN * PP;
+  static constexpr int P = DH + 4, PP = kBN + 4;
+  static constexpr int kQ = BM * P, kK = kBN * P, kV = kBN * P, kP = BM * PP;
   static constexpr size_t SMEM = (size_t)(kQ + kK + kV + kP) * sizeof(float);
 };
+// rows [0, n) of a [.., dh] head into shared memory, zero beyond n and dh; row(i): where row i starts
+template <typename T, int DH, int ROWS, typename F>
+__device__ __forceinline__ void load_rows(float* dst, int n, int dh, bool vec, float scale, F&& row) {
+  constexpr int P = DH + 4;
+  for (int e = threadIdx.x; e < ROWS * (DH / 4); e += kSimtThreads) {
+    const int i = e / (DH / 4), d = e % (DH / 4) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < n && d < dh) {
+      const T* src = row(i) + d;
+      if (sizeof(T) == 4 && vec) {
+        v = *reinterpret_cast<const float4*>(src);
+      } else {
+        v.x = load1(src);
+        if (d + 1 < dh) v.y = load1(src + 1);
+        if (d + 2 < dh) v.z = load1(src + 2);
+        if (d + 3 < dh) v.w = load1(src + 3);
+      }
+      v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
+    }
+    *reinterpret_cast<float4*>(dst + i * P + d) = v;
+  }
+}
 
 template <typename T, int DH, int BM>
 __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const AttnParams p) {
@@ -43,6 +65,10 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const Attn
   const T* Q = reinterpret_cast<const T*>(p.q);
   const T* K = reinterpret_cast<const T*>(p.k);
   const T* V = reinterpret_cast<const T*>(p.v);
+  const auto aligned = [&](const void* ptr, int64_t ld) {
+    return p.dh % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0;
+  };
+  const bool vq = aligned(Q, p.ldq), vk = aligned(K, p.ldk), vv = aligned(V, p.ldv);
   AttnDealer dealer;
   AttnItem it;
   for (int64_t item = blockIdx.x; dealer.find(p, item, BM, p.g, p.n_kv, it); item += gridDim.x) {
@@ -55,15 +81,10 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const Attn
     const int kb = cut ? it.c * p.part : 0;
     const int ke = cut && seen - kb > p.part ? kb + p.part : seen;
     __syncthreads();
-    for (int e = threadIdx.x; e < BM * DH; e += kSimtThreads) {
-      const int r = e / DH, d = e % DH;
-      float v = 0.f;
-      if (r < rows && d < p.dh) {
-        const int64_t rr = r0 + r;
-        v = load1(Q + (it.q0 + rr / p.g) * p.ldq + (it.head * p.g + rr % p.g) * (int64_t)p.dh + d) * p.scale_log2;
-      }
-      sq[d * L::PQ + r] = v;
-    }
+    load_rows<T, DH, BM>(sq, rows, p.dh, vq, p.scale_log2, [&](int i) {
+      const int64_t rr = r0 + i;
+      return Q + (it.q0 + rr / p.g) * p.ldq + (it.head * p.g + rr % p.g) * (int64_t)p.dh;
+    });
     float o[TM][TD], m[TM], l[TM];
     int lim[TM];                      // keys [0, lim) are visible to the row
 #pragma unroll
@@ -77,13 +98,12 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const Attn
     }
     for (int kt = kb; kt < ke; kt += kBN) {
       __syncthreads();                // the tile before has been read
-      for (int e = threadIdx.x; e < kBN * DH; e += kSimtThreads) {
-        const int j = e / DH, d = e % DH;
-        const bool in = j < ke - kt && d < p.dh;
-        const int64_t at = (int64_t)it.k0 + kt + j;
-        sk[d * L::PK + j] = in ? load1(K + at * p.ldk + it.head * (int64_t)p.dh + d) : 0.f;
-        sv[j * L::PV + d] = in ? load1(V + at * p.ldv + it.head * (int64_t)p.dh + d) : 0.f;
-      }
+      load_rows<T, DH, kBN>(sk, ke - kt, p.dh, vk, 1.f, [&](int j) {
+        return K + ((int64_t)it.k0 + kt + j) * p.ldk + it.head * (int64_t)p.dh;
+      });
+      load_rows<T, DH, kBN>(sv, ke - kt, p.dh, vv, 1.f, [&](int j) {
+        return V + ((int64_t)it.k0 + kt + j) * p.ldv + it.head * (int64_t)p.dh;
+      });
       __syncthreads();
       float s[TM][4];
 #pragma unroll
@@ -91,22 +111,16 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const Attn
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 4
-      for (int d = 0; d < DH; ++d) {
-        const float4 kv = *reinterpret_cast<const float4*>(sk + d * L::PK + tx * 4);
-        float qv[TM];
-        if constexpr (TM == 4) {
-          const float4 t = *reinterpret_cast<const float4*>(sq + d * L::PQ + ty * 4);
-          qv[0] = t.x; qv[1] = t.y; qv[2] = t.z; qv[3] = t.w;
-        } else {
+      for (int d = 0; d < DH; d += 4) {
+        float4 kf[4];
 #pragma unroll
-          for (int i = 0; i < TM; ++i) qv[i] = sq[d * L::PQ + ty * TM + i];
-        }
+        for (int j = 0; j < 4; ++j) kf[j] = *reinterpret_cast<const float4*>(sk + (tx + 16 * j) * L::P + d);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-          s[i][0] = fmaf(qv[i], kv.x, s[i][0]);
-          s[i][1] = fmaf(qv[i], kv.y, s[i][1]);
-          s[i][2] = fmaf(qv[i], kv.z, s[i][2]);
-          s[i][3] = fmaf(qv[i], kv.w, s[i][3]);
+          const float4 qf = *reinterpret_cast<const float4*>(sq + (ty * TM + i) * L::P + d);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            s[i][j] = fmaf(qf.w, kf[j].w, fmaf(qf.z, kf[j].z, fmaf(qf.y, kf[j].y, fmaf(qf.x, kf[j].x, s[i][j]))));
         }
       }
 #pragma unroll
@@ -114,7 +128,7 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const Attn
         float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (kt + tx * 4 + j >= lim[i] || tx * 4 + j >= ke - kt) s[i][j] = -INFINITY;
+          if (kt + tx + 16 * j >= lim[i] || tx + 16 * j >= ke - kt) s[i][j] = -INFINITY;
           mx = fmaxf(mx, s[i][j]);    // (a NaN is passed over here and stays one in the exponential)
         }
 #pragma unroll
@@ -134,27 +148,49 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const Attn
 #pragma unroll
         for (int j = 0; j < TD; ++j) o[i][j] *= f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sp_[(tx * 4 + j) * L::PP + ty * TM + i] = s[i][j];
+        for (int j = 0; j < 4; ++j) sp_[(ty * TM + i) * L::PP + tx + 16 * j] = s[i][j];
       }
       __syncwarp();                   // a warp's rows of P are its own: two values of ty
       // In a tile that the mask cuts, a key beyond a row's limit is not touched at all: 0 times a NaN in V is no 0.
-      const bool whole = kt + kBN <= lim[0];     // (rows rise with i and see no fewer keys)
-      const int jend = min(kBN, ke - kt);
-      for (int j = 0; j < jend; ++j) {
-        float pv[TM];
+      if (kt + kBN <= lim[0]) {          // (rows rise with i and see no fewer keys)
+#pragma unroll 2
+        for (int j = 0; j < kBN; j += 4) {
+          float4 pf[TM];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) pv[i] = sp_[j * L::PP + ty * TM + i];
+          for (int i = 0; i < TM; ++i) pf[i] = *reinterpret_cast<const float4*>(sp_ + (ty * TM + i) * L::PP + j);
 #pragma unroll
-        for (int c = 0; c < TD; c += 4) {
-          const float4 vv = *reinterpret_cast<const float4*>(sv + j * L::PV + (c / 4) * 64 + tx * 4);
+          for (int c = 0; c < TD; c += 4)
 #pragma unroll
-          for (int i = 0; i < TM; ++i)
-            if (whole || kt + j < lim[i]) {
-              o[i][c] = fmaf(pv[i], vv.x, o[i][c]);
-              o[i][c + 1] = fmaf(pv[i], vv.y, o[i][c + 1]);
-              o[i][c + 2] = fmaf(pv[i], vv.z, o[i][c + 2]);
-              o[i][c + 3] = fmaf(pv[i], vv.w, o[i][c + 3]);
+            for (int y = 0; y < 4; ++y) {
+              const float4 vf = *reinterpret_cast<const float4*>(sv + (j + y) * L::P + (c / 4) * 64 + tx * 4);
+#pragma unroll
+              for (int i = 0; i < TM; ++i) {
+                const float pv = y == 0 ? pf[i].x : y == 1 ? pf[i].y : y == 2 ? pf[i].z : pf[i].w;
+                o[i][c] = fmaf(pv, vf.x, o[i][c]);
+                o[i][c + 1] = fmaf(pv, vf.y, o[i][c + 1]);
+                o[i][c + 2] = fmaf(pv, vf.z, o[i][c + 2]);
+                o[i][c + 3] = fmaf(pv, vf.w, o[i][c + 3]);
+              }
             }
+        }
+      } else {
+        const int jend = min(kBN, ke - kt);
+        for (int j = 0; j < jend; ++j) {
+          float pv[TM];
+#pragma unroll
+          for (int i = 0; i < TM; ++i) pv[i] = sp_[(ty * TM + i) * L::PP + j];
+#pragma unroll
+          for (int c = 0; c < TD; c += 4) {
+            const float4 vf = *reinterpret_cast<const float4*>(sv + j * L::P + (c / 4) * 64 + tx * 4);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+              if (kt + j < lim[i]) {
+                o[i][c] = fmaf(pv[i], vf.x, o[i][c]);
+                o[i][c + 1] = fmaf(pv[i], vf.y, o[i][c + 1]);
+                o[i][c + 2] = fmaf(pv[i], vf.z, o[i][c + 2]);
+                o[i][c + 3] = fmaf(pv[i], vf.w, o[i][c + 3]);
+              }
+          }
         }
       }
       __syncwarp();
@@ -203,10 +239,12 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnParams p)
   const int nk = AttnDealer::bound(p.cu_k[lo + 1], p.Nk) - AttnDealer::bound(p.cu_k[lo], p.Nk);
   if (nk <= p.part) return;
   const int parts = (nk - 1) / p.part + 1;
+  const float* lses = p.part_lse + (int64_t)row * p.n_heads + h;
+  const int64_t lse_step = (int64_t)p.Nq * p.n_heads, o_step = lse_step * p.dh;
   float mx = -INFINITY;
   bool bad = false;                   // (fmaxf passes over a NaN)
   for (int c = lane; c < parts; c += 32) {
-    const float lc = p.part_lse[((int64_t)c * p.Nq + row) * p.n_heads + h];
+    const float lc = lses[c * lse_step];
     mx = fmaxf(mx, lc);
     bad |= lc != lc;
   }
@@ -214,22 +252,27 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnParams p)
   for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
   const float ref = mx == -INFINITY ? 0.f : mx;
   bad = __any_sync(0xffffffffu, bad);
+  // a lane has channels 4 lane ..; what a part without a visible key left (lse -infinity) is zeros
+  const int d = 4 * lane;
   float acc[4] = {0.f, 0.f, 0.f, 0.f}, total = 0.f;
-  for (int c = 0; c < parts; ++c) {
-    const float lc = p.part_lse[((int64_t)c * p.Nq + row) * p.n_heads + h];
-    if (lc == -INFINITY) continue;       // nothing visible there
-    const float w = exp2f(lc - ref);
-    total += w;
-    const float* po = p.part_o + ((int64_t)c * p.Nq + row) * ((int64_t)p.n_heads * p.dh) + (int64_t)h * p.dh;
+  const float* po = p.part_o + ((int64_t)row * p.n_heads + h) * p.dh + d;
+  for (int c0 = 0; c0 < parts; c0 += 32) {
+    const float wl = c0 + lane < parts ? exp2f(lses[(c0 + lane) * lse_step] - ref) : 0.f;
+    const int m = min(32, parts - c0);
+#pragma unroll 8
+    for (int c = 0; c < m; ++c) {
+      const float w = __shfl_sync(0xffffffffu, wl, c);
+      total += w;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (lane + 32 * q < p.dh) acc[q] = fmaf(w, po[lane + 32 * q], acc[q]);
+      for (int x = 0; x < 4; ++x)
+        if (d + x < p.dh) acc[x] = fmaf(w, po[(c0 + c) * o_step + x], acc[x]);
+    }
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
-  T* out = reinterpret_cast<T*>(p.o) + (int64_t)row * p.ldo + (int64_t)h * p.dh;
+  T* out = reinterpret_cast<T*>(p.o) + (int64_t)row * p.ldo + (int64_t)h * p.dh + d;
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
-    if (lane + 32 * q < p.dh) store1(out + lane + 32 * q, bad ? NAN : acc[q] * inv);
+  for (int x = 0; x < 4; ++x)
+    if (d + x < p.dh) store1(out + x, bad ? NAN : acc[x] * inv);
   if (lane == 0 && p.lse)
     p.lse[(int64_t)row * p.n_heads + h] = bad ? NAN : total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
 }
@@ -265,19 +308,20 @@ struct Cut {
 };
 // Whether and how the key axis is cut.  Without a cut there are about Nq g / 128 tiles of rows, at least one for every sequence
 // that has queries, times the key heads; fewer than the SMs (148) leave SMs idle.  Parts are then as long as gives four for every SM
-// (so that sequences of different lengths even out), eight with few rows, at least 256 keys (a part costs its
-// result's way through memory and a second launch).
+// (so that sequences of different lengths even out), at least 256 keys.  With few rows an SM reads 1024 keys of a head in 5 us, about what a second
+// launch and the results' way through memory cost: shorter parts do not pay, up to 4096 keys for an SM it gets one part, beyond eight.
 Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh) {
   Cut cut;
   if (Nq < 1 || Nk < 1 || n_seq < 1) return cut;
   const int64_t g = n_heads / n_kv, sms = 148;
   const int64_t seqs = n_seq < Nq ? n_seq : Nq;
   const int64_t tiles = (Nq * g / 128 > seqs ? Nq * g / 128 : seqs) * n_kv;
-  const int64_t per_sm = attention_few_rows(Nq, g, n_seq) ? 8 : 4;
-  if (tiles >= sms * per_sm / 2) return cut;
   const int64_t per_tile = ceil_div(Nk, seqs);                 // keys of a tile, on average
+  const bool few = attention_few_rows(Nq, g, n_seq);
+  const int64_t per_sm = !few ? 4 : tiles * per_tile <= sms * 4096 ? 1 : 8;
+  if (tiles >= (per_sm > 1 ? sms * per_sm / 2 : sms)) return cut;
   int64_t part = (int64_t)align_up((size_t)ceil_div(tiles * per_tile, sms * per_sm), 128);
-  if (part < 256) part = 256;
+  if (part < (few ? 1024 : 256)) part = few ? 1024 : 256;
   if (part >= Nk) return cut;                                   // nothing is longer
   const int64_t parts = ceil_div(Nk, part);
   const int64_t elems = parts * Nq * n_heads;
@@ -355,6 +399,7 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
   } else if ((dt == SP_F32 ? launch_simt<float>(p, s) : launch_simt<__nv_bfloat16>(p, s)) != cudaSuccess) return SP_ERR_CUDA;
   if (cut.part > 0) {
     count_launch();
+    const OverlapScope overlap(true);       // its blocks start while the parts end
     const dim3 grid((unsigned)ceil_div(Nq * a->n_heads, (int64_t)8));
     const cudaError_t e = dt == SP_F32 ? launch(attention_join_kernel<float>, grid, dim3(256), 0, s, p)
                                        : launch(attention_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, p);

@@ -341,6 +341,10 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
                   const TcBatch* batch = nullptr, const LinearEpi* lin = nullptr);
 // lin: C = act(A B + bias), then (+ or *) Cin when beta is not 0 (alpha = 1, beta = 0 or 1; neither batched nor lower_only).
 bool gemm_tc_supported(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand B);
+// The same for up to kLinearFewRows rows (sp_linear_few.cu), layouts as gemm_tc_supported, both K-major.
+constexpr int64_t kLinearFewRows = 16;
+cudaError_t linear_few(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand W, const LinearEpi& epi, Operand other, OutOperand C,
+                       cudaStream_t stream);
 
 struct SolveAssist;
 // fp64 factorisation and solves (sp_linalg.cu), block columns of kCholNB.
