@@ -310,6 +310,7 @@ struct Cut {
 // that has queries, times the key heads; fewer than the SMs (148) leave SMs idle.  Parts are then as long as gives four for every SM
 // (so that sequences of different lengths even out), at least 256 keys.  With few rows an SM reads 1024 keys of a head in 5 us, about what a second
 // launch and the results' way through memory cost: shorter parts do not pay, up to 4096 keys for an SM it gets one part, beyond eight.
+// Sequences that are no longer than a part on average are not cut.
 Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh) {
   Cut cut;
   if (Nq < 1 || Nk < 1 || n_seq < 1) return cut;
@@ -322,7 +323,7 @@ Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_k
   if (tiles >= (per_sm > 1 ? sms * per_sm / 2 : sms)) return cut;
   int64_t part = (int64_t)align_up((size_t)ceil_div(tiles * per_tile, sms * per_sm), 128);
   if (part < (few ? 1024 : 256)) part = few ? 1024 : 256;
-  if (part >= Nk) return cut;                                   // nothing is longer
+  if (part >= per_tile) return cut;                             // (a longer sequence among many short ones is not worth it)
   const int64_t parts = ceil_div(Nk, part);
   const int64_t elems = parts * Nq * n_heads;
   if (elems * (dh + 1) * 4 > (int64_t)1 << 30) return cut;

@@ -264,12 +264,31 @@ struct LinearEpi {
   int32_t act = SP_LINEAR_NONE, combine = SP_COMBINE_ADD;
 };
 #ifdef __CUDACC__
+__device__ __forceinline__ float act_relu(float v) { return v < 0.f ? 0.f : v; }      // (a NaN stays one)
+// (the quotient by a reciprocal: 2 units in the last place, 0 from a denominator of 2^126 on; -inf / inf would be NaN)
+__device__ __forceinline__ float act_silu(float v) {
+  const float y = __fdividef(v, 1.f + __expf(-v));      // (selections, no branches, here and below: 32 of these run side by side)
+  return v == -INFINITY ? 0.f : y;
+}
+// v Phi(v).  Phi(-|v|) = erfc(a) / 2 with a = |v| / sqrt 2, and erfc(a) = t exp(q(t) - a^2) with t = 1 / (1 + a / 2): the smooth
+// q(t) = log(erfc(a) exp(a^2) / t) is a polynomial of degree 7, interpolated at Chebyshev nodes for a up to 12 (within 1e-6, so that
+// small Phi keep their relative accuracy).  A tenth of erfcf's instructions, 32 copies of which no longer fit the instruction cache.
+__device__ __forceinline__ float act_gelu(float v) {
+  const float a = 0.7071067811865476f * fabsf(v), t = __fdividef(1.f, fmaf(0.5f, a, 1.f));
+  float q = fmaf(-0.19117627f, t, 0.76572722f);
+  q = fmaf(q, t, -1.0253474f);
+  q = fmaf(q, t, 0.37195718f);
+  q = fmaf(q, t, -0.051072314f);
+  q = fmaf(q, t, 0.39727193f);
+  q = fmaf(q, t, 0.99808556f);
+  q = fmaf(q, t, -1.2654468f);
+  const float e = 0.5f * t * __expf(fmaf(-a, a, q));
+  // (e = 0 for infinities, too)
+  const float base = v < 0.f ? 0.f : v, share = e == 0.f ? 0.f : fabsf(v) * e;
+  return base - share;
+}
 __device__ __forceinline__ float linear_act(float v, int32_t act) {
-  if (act == SP_LINEAR_RELU) return v < 0.f ? 0.f : v;                 // (a NaN stays one)
-  if (act == SP_LINEAR_SILU) return v == -INFINITY ? 0.f : v / (1.f + __expf(-v));      // (-inf / inf is NaN)
-  // v Phi(v) with Phi(v) = erfc(-v / sqrt 2) / 2, which keeps its relative accuracy where Phi is small
-  if (act == SP_LINEAR_GELU) return v == -INFINITY ? 0.f : 0.5f * v * erfcf(-0.7071067811865476f * v);
-  return v;
+  return act == SP_LINEAR_RELU ? act_relu(v) : act == SP_LINEAR_SILU ? act_silu(v) : act == SP_LINEAR_GELU ? act_gelu(v) : v;
 }
 __device__ __forceinline__ double linear_act(double v, int32_t act) {
   if (act == SP_LINEAR_RELU) return v < 0.0 ? 0.0 : v;
