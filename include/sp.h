@@ -531,7 +531,7 @@ size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32
  * (max(y, 0)), _SILU (y / (1 + e^-y)), _GELU (y Phi(y), Phi the normal distribution function).  X and W have one dtype
  * (SP_BF16 or SP_F32); Y has it too or is SP_F32; other has Y's.  other may be Y itself (same pointer and ld); other
  * overlaps of Y with an input are not allowed.
- * bf16 mode: tensor cores, fp32 accumulation, one rounding at the end; up to 16 rows a kernel that streams W.  Needs leading dimensions of X and W that are multiples
+ * bf16 mode: tensor cores, fp32 accumulation, one rounding at the end; few rows by a kernel that streams W.  Needs leading dimensions of X and W that are multiples
  * of 8 and 16-byte aligned pointers, else the CUDA cores serve, slower; in and out may be any numbers (a pruned module's
  * k_keep).  fp32 mode: fp64 accumulation.
  * The gradients of X W^T are plain products: dX = dY W, dW = dY^T X (sp_gemm, sp_gram_accumulate).

@@ -493,7 +493,7 @@ sp_status sp_linear(const sp_mat* X, const sp_mat* W, const float* bias, int32_t
   if (X->dtype == SP_BF16) {
     TcOperand ta{X->ptr, X->ld, true}, tb{W->ptr, W->ld, true};
     if (gemm_tc_supported(T, N, K, ta, tb)) {
-      if (T <= kLinearFewRows) {
+      if (linear_few_rows(T, N)) {
         CU(linear_few(T, N, K, ta, tb, epi, o, y, s));
         return SP_OK;
       }

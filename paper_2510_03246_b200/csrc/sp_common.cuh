@@ -360,8 +360,10 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
                   const TcBatch* batch = nullptr, const LinearEpi* lin = nullptr);
 // lin: C = act(A B + bias), then (+ or *) Cin when beta is not 0 (alpha = 1, beta = 0 or 1; neither batched nor lower_only).
 bool gemm_tc_supported(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand B);
-// The same for up to kLinearFewRows rows (sp_linear_few.cu), layouts as gemm_tc_supported, both K-major.
-constexpr int64_t kLinearFewRows = 16;
+// The same for few rows (sp_linear_few.cu, up to 32), layouts as gemm_tc_supported, both K-major.  Where it is the faster one: up to 16
+// rows, and up to 32 where the tiles of 128 outputs leave many SM pairs idle.  Tiles / this, us: 4096 -> 4096 16 rows 32.8 / 16.4, 32 rows
+// 34.8 / 20.5, 48 rows 32.8 / 30.7; 4096 -> 16384 16 rows 46 / 41, 32 rows 45 / 63; 768 -> 1536 32 rows 16.4 / 10.2.
+inline bool linear_few_rows(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 8192); }
 cudaError_t linear_few(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand W, const LinearEpi& epi, Operand other, OutOperand C,
                        cudaStream_t stream);
 

@@ -1,4 +1,4 @@
-// sp_linear for up to 16 rows in bf16: Y = act(X W^T + bias) (+|*) other, bound by reading W once.
+// sp_linear for up to 32 rows in bf16: Y = act(X W^T + bias) (+|*) other, bound by reading W once.
 //
 // A 128-row tile of the tensor-core product would be nearly empty, and a call has few of them: its time is that of a few SMs reading W
 // (16 x 768 -> 1536 took 32 us from cold caches).  Here a block takes 16 outputs and all of K, its eight warps every eighth piece of 32
@@ -10,7 +10,7 @@
 namespace sp {
 namespace {
 
-constexpr int kWarps = 8, kOut = 16, kPiece = 32, kUnroll = 4;
+constexpr int kWarps = 8, kOut = 16, kPiece = 32;
 
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -42,8 +42,9 @@ struct FewParams {
 
 // NT: groups of eight rows of X
 template <int NT>
-__global__ void __launch_bounds__(kWarps * 32, 3) linear_few_kernel(const FewParams p) {
+__global__ void __launch_bounds__(kWarps * 32, NT > 1 ? 2 : 3) linear_few_kernel(const FewParams p) {
   kernel_begin();
+  constexpr int kUnroll = NT > 2 ? 2 : 4;
   __shared__ float s_acc[kWarps][NT * 8][kOut + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g4 = lane >> 2, t4 = lane & 3;
   const int64_t o0 = (int64_t)blockIdx.x * kOut;
@@ -117,7 +118,8 @@ cudaError_t linear_few(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand W
   ProfScope prof(PK_GEMM_SIMT, 2.0 * (double)M * (double)N * (double)K, 0.0, stream);
   const dim3 grid((unsigned)ceil_div(N, (int64_t)kOut));
   return M <= 8 ? launch(linear_few_kernel<1>, grid, dim3(kWarps * 32), 0, stream, p)
-                : launch(linear_few_kernel<2>, grid, dim3(kWarps * 32), 0, stream, p);
+       : M <= 16 ? launch(linear_few_kernel<2>, grid, dim3(kWarps * 32), 0, stream, p)
+                : launch(linear_few_kernel<4>, grid, dim3(kWarps * 32), 0, stream, p);
 }
 
 }  // namespace sp
