@@ -11,6 +11,7 @@
 #include <math.h>
 
 #include "sp_attention.cuh"
+#include "sp_f32x2.cuh"
 #include "sp_tc.cuh"
 
 namespace sp {
@@ -34,11 +35,6 @@ struct RowsCfg {
   static constexpr size_t SMEM = (size_t)STAGES * 2 * TILE + JOIN + 16 * STAGES + 1024;
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"

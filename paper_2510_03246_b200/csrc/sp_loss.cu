@@ -11,6 +11,7 @@
 #include <math.h>
 
 #include "sp_common.cuh"
+#include "sp_f32x2.cuh"
 
 namespace sp {
 namespace {
@@ -18,12 +19,6 @@ namespace {
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kLossThreads = 256;
 constexpr int kMaxCluster = 8;
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 // 16 bytes of a row as floats
 template <typename T> struct Vec;
@@ -34,6 +29,11 @@ template <> struct Vec<float> {
   }
   static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  // largest and smallest of them (NaN passed over)
+  static __device__ __forceinline__ void range(const uint4&, const float (&x)[4], float& hi, float& lo) {
+    hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
   }
   static __device__ __forceinline__ float one(float v) { return v; }
   static __device__ __forceinline__ float to(float v) { return v; }
@@ -57,6 +57,12 @@ template <> struct Vec<__nv_bfloat16> {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
+  static __device__ __forceinline__ void range(const uint4& q, const float (&)[8], float& hi, float& lo) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&q);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])), n = __hmin2(__hmin2(h[0], h[1]), __hmin2(h[2], h[3]));
+    hi = fmaxf(__low2float(m), __high2float(m));
+    lo = fminf(__low2float(n), __high2float(n));
+  }
   static __device__ __forceinline__ float one(__nv_bfloat16 v) { return __bfloat162float(v); }
   static __device__ __forceinline__ __nv_bfloat16 to(float v) { return __float2bfloat16_rn(v); }
 };
@@ -70,7 +76,7 @@ __device__ __forceinline__ Part join(const Part& a, const Part& b) {
   if (r == -INFINITY) return Part{r, a.s + b.s, a.w + b.w};     // (zeros, or the NaN of a NaN logit)
   // a part with r = -infinity holds zeros: its shift is taken as zero (0 * infinity)
   const float da = a.r == -INFINITY ? 0.f : a.r - r, db = b.r == -INFINITY ? 0.f : b.r - r;
-  const float fa = exp2f(da), fb = exp2f(db);
+  const float fa = exp2_fast(da), fb = exp2_fast(db);
   return Part{r, a.s * fa + b.s * fb, (a.w + da * a.s) * fa + (b.w + db * b.s) * fb};
 }
 
@@ -149,8 +155,8 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
   float top = -INFINITY;                               // largest value of this thread's vectors
   bool any = false;                                    // it has had one that is a number
 
-  // values x[0 .. n) into (r, s, w)
-  auto take = [&](const float* x, int n, float m) {
+  // the reference follows a larger value
+  auto raise = [&](float m) {
     const float mt = m * c;
     if (mt > a.r) {
       const float d = a.r - mt, f = exp2_fast(d);      // a.r = -infinity: f = 0, and s = w = 0
@@ -159,12 +165,38 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
       a.r = mt;
       rc = mt;
     }
+  };
+  const uint64_t c2 = pack2(c, c);
+  // Values x[0 .. n) into (r, s, w), the largest and smallest of which are given.  Two at a time; a logit of -infinity, which
+  // would add 0 times infinity to w, goes alone.
+  auto take = [&](const float (&x)[N], float hi, float lo) {
+    raise(hi);
+    if (ENT && lo == -INFINITY) {
 #pragma unroll
-    for (int i = 0; i < n; ++i) {
-      const float t = fmaf(x[i], c, -rc), e = exp2_fast(t);
-      a.s += e;
-      // (a logit of -infinity: e = 0, and 0 times a finite number is added)
-      if (ENT) a.w = fmaf(e, fmaxf(t, -10000.f), a.w);
+      for (int i = 0; i < N; ++i) {
+        const float t = fmaf(x[i], c, -rc), e = exp2_fast(t);
+        a.s += e;
+        a.w = fmaf(e, fmaxf(t, -10000.f), a.w);
+      }
+      return;
+    }
+    const uint64_t r2 = pack2(-rc, -rc);
+    uint64_t s2 = pack2(a.s, 0.f), w2 = pack2(a.w, 0.f);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const uint64_t t = fma2(pack2(x[i], x[i + 1]), c2, r2);
+      float e0, e1;
+      unpack2(t, e0, e1);
+      const uint64_t e = pack2(exp2_fast(e0), exp2_fast(e1));
+      s2 = add2(s2, e);
+      if (ENT) w2 = fma2(e, t, w2);
+    }
+    float u, v;
+    unpack2(s2, u, v);
+    a.s = u + v;
+    if (ENT) {
+      unpack2(w2, u, v);
+      a.w = u + v;
     }
   };
 
@@ -180,7 +212,12 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
     const int tail0 = first + nvec * N;
     auto scalar = [&](int i, bool in) {                // one value per lane (loose ends)
       const float v = in ? Vec<T>::one(xr[i]) : -INFINITY;
-      if (in) take(&v, 1, v);
+      if (in) {
+        raise(v);
+        const float t = fmaf(v, c, -rc), e = exp2_fast(t);
+        a.s += e;
+        if (ENT) a.w = fmaf(e, fmaxf(t, -10000.f), a.w);
+      }
       return v;
     };
     float lead = 0.f, rear = 0.f;
@@ -197,13 +234,12 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
         if (v + u * STEP < v1) {
           float x[N];
           Vec<T>::unpack(q[u], x);
-          float m = x[0];
-#pragma unroll
-          for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);      // (passes over NaN)
-          take(x, N, m);
+          float hi, lo;
+          Vec<T>::range(q[u], x, hi, lo);
+          take(x, hi, lo);
           if (ALTS) {
-            any |= m == m;
-            top = fmaxf(top, m);
+            any |= hi == hi;
+            top = fmaxf(top, hi);
           }
         }
       }
@@ -228,6 +264,7 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
       floor_key = kth == 0u ? 0ull : ((unsigned long long)kth << 32) - 1ull;
       if (has_lead) best.insert(lane < first, make_key(lead, (uint32_t)lane), p.n_alts, floor_key, lane);
       if (has_rear) best.insert(tail0 + lane < p.V, make_key(rear, (uint32_t)(tail0 + lane)), p.n_alts, floor_key, lane);
+      const float floor_value = kth == 0u ? NAN : order_value(kth);      // (nothing is less than a NaN: all go on to their keys)
       uint32_t hot = __ballot_sync(0xffffffffu, mine >= kth);
       while (hot) {                                    // the vectors of one thread, a lane each
         const int l = __ffs(hot) - 1;
@@ -239,8 +276,8 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
           Vec<T>::unpack(in ? __ldcg(xv + at) : make_uint4(0u, 0u, 0u, 0u), x);
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const unsigned long long key = make_key(x[i], (uint32_t)(first + at * N + i));
-            if (__any_sync(0xffffffffu, in && key > floor_key)) best.insert(in, key, p.n_alts, floor_key, lane);
+            if (__any_sync(0xffffffffu, in && !(x[i] < floor_value)))
+              best.insert(in, make_key(x[i], (uint32_t)(first + at * N + i)), p.n_alts, floor_key, lane);
           }
         }
       }
