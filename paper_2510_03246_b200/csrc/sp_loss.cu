@@ -7,7 +7,9 @@
 //
 // The n best logits need no list during that pass.  The k-th largest of a warp's 32 thread maxima, k = ceil(n / warps of the row), taken
 // over the warps' least, is a floor that at least n logits reach; few more do (some 20 of 50257 for n = 8).  Afterwards only the vectors of
-// threads whose maximum reaches the floor are looked at again, a warp at a time and out of L2.
+// threads whose maximum reaches the floor are looked at again, a warp at a time and out of L2, and what reaches it is gathered in shared
+// memory, where each one's place is the number of larger ones.  (Sorted lists in every warp, joined by one: 285 us for 8192 rows of 50257 with
+// eight alternatives; insertions follow one another.)  Where more are gathered than there is room for (many equal logits), such lists do serve.
 #include <math.h>
 
 #include "sp_common.cuh"
@@ -19,6 +21,8 @@ namespace {
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kLossThreads = 256;
 constexpr int kMaxCluster = 8;
+constexpr int kWideRoom = 512, kNarrowRoom = 256;      // keys gathered for a row of many warps, of one
+static_assert(kNarrowRoom >= SP_MAX_ALTS && kWideRoom >= kLossThreads / 32 * SP_MAX_ALTS && kWideRoom >= kMaxCluster * SP_MAX_ALTS, "lists");
 
 // 16 bytes of a row as floats
 template <typename T> struct Vec;
@@ -135,8 +139,10 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
   kernel_begin();
   constexpr int kWarps = kLossThreads / 32, N = Vec<T>::N, U = 4;     // U vectors in flight per thread
   static_assert(WARPS == 1 || WARPS == kWarps, "rows per block");
+  constexpr int kRoom = WARPS == 1 ? kNarrowRoom : kWideRoom, kRowsHere = WARPS == 1 ? kWarps : 1;
   __shared__ Part s_part[kWarps];
-  __shared__ unsigned long long s_best[ALTS ? kWarps * SP_MAX_ALTS : 1];
+  __shared__ unsigned long long s_keys[ALTS ? kRowsHere : 1][ALTS ? kRoom : 1];
+  __shared__ int s_count[kRowsHere];
   __shared__ uint32_t s_floor[kWarps];
   __shared__ Part s_all[kMaxCluster];
   __shared__ unsigned long long s_all_best[ALTS ? kMaxCluster * SP_MAX_ALTS : 1];
@@ -146,12 +152,21 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
   const bool live = row < p.T;
   const int wl = WARPS == 1 ? 0 : warp;                // warp within the row
   // (the other CTAs of a cluster write into the first one's shared memory: all have started once they meet)
-  if (WARPS > 1 && cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  if (WARPS > 1 && cluster > 1) {
+    if (ALTS)
+      for (int i = threadIdx.x; i < kMaxCluster * SP_MAX_ALTS; i += kLossThreads) s_all_best[i] = 0ull;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  }
+  const int tid = WARPS == 1 ? lane : (int)threadIdx.x;      // thread within the row
+  unsigned long long* keys = s_keys[WARPS == 1 && ALTS ? warp : 0];
+  int* count = &s_count[WARPS == 1 ? warp : 0];
+  auto row_sync = [&] {
+    if (WARPS > 1) __syncthreads();
+    else __syncwarp();
+  };
   const float c = p.scale * kLog2E;
   Part a{-INFINITY, 0.f, 0.f};
   float rc = 0.f;                                      // a.r, or 0 while that is -infinity
-  WarpBest best{0ull};
-  unsigned long long floor_key = 0ull;
   float top = -INFINITY;                               // largest value of this thread's vectors
   bool any = false;                                    // it has had one that is a number
 
@@ -254,32 +269,50 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
         const uint32_t who = __ballot_sync(0xffffffffu, left == kth);
         if (lane == __ffs(who) - 1) left = 0u;
       }
+      if (tid == 0) *count = 0;
+      if (WARPS > 1 && lane == 0) s_floor[warp] = kth;
+      row_sync();
       if (WARPS > 1) {
-        if (lane == 0) s_floor[warp] = kth;
-        __syncthreads();
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) kth = min(kth, s_floor[i]);
       }
-      // keys above floor_key: values that reach the floor (0: every key)
-      floor_key = kth == 0u ? 0ull : ((unsigned long long)kth << 32) - 1ull;
-      if (has_lead) best.insert(lane < first, make_key(lead, (uint32_t)lane), p.n_alts, floor_key, lane);
-      if (has_rear) best.insert(tail0 + lane < p.V, make_key(rear, (uint32_t)(tail0 + lane)), p.n_alts, floor_key, lane);
       const float floor_value = kth == 0u ? NAN : order_value(kth);      // (nothing is less than a NaN: all go on to their keys)
-      uint32_t hot = __ballot_sync(0xffffffffu, mine >= kth);
-      while (hot) {                                    // the vectors of one thread, a lane each
-        const int l = __ffs(hot) - 1;
-        hot &= hot - 1;
-        for (int v = v0 + wl * 32 + l; v < v1; v += STEP * 32) {
-          const int at = v + STEP * lane;
-          const bool in = at < v1;
-          float x[N];
-          Vec<T>::unpack(in ? __ldcg(xv + at) : make_uint4(0u, 0u, 0u, 0u), x);
+      auto gather = [&](bool in, float v, uint32_t index) {
+        if (in && !(v < floor_value)) {
+          const int at = atomicAdd(count, 1);
+          if (at < kRoom) keys[at] = make_key(v, index);
+        }
+      };
+      // f(in, value, index) for every value that may reach the floor, all lanes at once
+      auto for_hot = [&](auto&& f) {
+        if (has_lead) f(lane < first, lead, (uint32_t)lane);
+        if (has_rear) f(tail0 + lane < p.V, rear, (uint32_t)(tail0 + lane));
+        uint32_t hot = __ballot_sync(0xffffffffu, mine >= kth);
+        while (hot) {                                  // the vectors of one thread, a lane each
+          const int l = __ffs(hot) - 1;
+          hot &= hot - 1;
+          for (int v = v0 + wl * 32 + l; v < v1; v += STEP * 32) {
+            const int at = v + STEP * lane;
+            const bool in = at < v1;
+            float x[N];
+            Vec<T>::unpack(in ? __ldcg(xv + at) : make_uint4(0u, 0u, 0u, 0u), x);
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            if (__any_sync(0xffffffffu, in && !(x[i] < floor_value)))
-              best.insert(in, make_key(x[i], (uint32_t)(first + at * N + i)), p.n_alts, floor_key, lane);
+            for (int i = 0; i < N; ++i) f(in, x[i], (uint32_t)(first + at * N + i));
           }
         }
+      };
+      for_hot(gather);
+      row_sync();
+      if (*count > kRoom) {                            // the same in all threads of the row
+        WarpBest best{0ull};
+        unsigned long long floor_key = kth == 0u ? 0ull : ((unsigned long long)kth << 32) - 1ull;
+        for_hot([&](bool in, float v, uint32_t index) {
+          if (__any_sync(0xffffffffu, in && !(v < floor_value))) best.insert(in, make_key(v, index), p.n_alts, floor_key, lane);
+        });
+        row_sync();
+        if (lane < p.n_alts) keys[wl * p.n_alts + lane] = best.key;
+        if (tid == 0) *count = WARPS * p.n_alts;
+        row_sync();
       }
     }
   }
@@ -291,50 +324,54 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
                  __shfl_xor_sync(0xffffffffu, a.w, o)};
     a = lane & o ? join(b, a) : join(a, b);            // the same order in both lanes
   }
+  // every warp joins the parts of the row's warps
+  auto join_parts = [&](const Part* parts, int n) {
+    Part b = lane < n ? parts[lane] : Part{-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+      const Part d{__shfl_xor_sync(0xffffffffu, b.r, o), __shfl_xor_sync(0xffffffffu, b.s, o),
+                   __shfl_xor_sync(0xffffffffu, b.w, o)};
+      b = lane & o ? join(d, b) : join(b, d);
+    }
+    return Part{__shfl_sync(0xffffffffu, b.r, 0), __shfl_sync(0xffffffffu, b.s, 0), __shfl_sync(0xffffffffu, b.w, 0)};
+  };
+  // f(place, key) for the n best of m keys (0: none); no two are equal
+  auto for_best = [&](const unsigned long long* k, int m, auto&& f) {
+    for (int i = tid; i < m; i += WARPS * 32) {
+      const unsigned long long mine = k[i];
+      int place = 0;
+#pragma unroll 4
+      for (int j = 0; j < m; ++j) place += k[j] > mine;
+      if (mine != 0ull && place < p.n_alts) f(place, mine);
+    }
+  };
+  static_assert(kWarps == 8 && kMaxCluster == 8, "three rounds join the parts");
+  const unsigned long long* found = keys;
+  int n_found = ALTS && live ? *count : 0;
   if (WARPS > 1) {
     if (lane == 0) s_part[warp] = a;
-    if (ALTS && lane < p.n_alts) s_best[warp * SP_MAX_ALTS + lane] = best.key;
     __syncthreads();
-    if (warp == 0) {
-      a = s_part[0];
-      for (int i = 1; i < kWarps; ++i) a = join(a, s_part[i]);
-      if (ALTS) {
-        floor_key = __shfl_sync(0xffffffffu, best.key, p.n_alts - 1);
-        for (int i = 1; i < kWarps; ++i) {
-          const unsigned long long k = lane < p.n_alts ? s_best[i * SP_MAX_ALTS + lane] : 0ull;
-          best.insert(k != 0ull, k, p.n_alts, floor_key, lane);
-        }
-      }
-    }
+    a = join_parts(s_part, kWarps);
     if (cluster > 1) {
       asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-      uint32_t dst = (uint32_t)__cvta_generic_to_shared(&s_all[rank]), dst_best = 0u;
-      asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(dst));
-      if (warp == 0) {
-        if (lane == 0)
-          asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\t"
-                       "st.shared::cluster.f32 [%0+8], %3;" ::"r"(dst), "f"(a.r), "f"(a.s), "f"(a.w) : "memory");
-        if (ALTS && lane < p.n_alts) {
-          dst_best = (uint32_t)__cvta_generic_to_shared(&s_all_best[rank * SP_MAX_ALTS + lane]);
-          asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(dst_best));
-          asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(dst_best), "l"(best.key) : "memory");
-        }
+      if (threadIdx.x == 0) {
+        uint32_t dst = (uint32_t)__cvta_generic_to_shared(&s_all[rank]);
+        asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(dst));
+        asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\t"
+                     "st.shared::cluster.f32 [%0+8], %3;" ::"r"(dst), "f"(a.r), "f"(a.s), "f"(a.w) : "memory");
       }
+      if (ALTS)
+        for_best(found, n_found, [&](int place, unsigned long long key) {
+          uint32_t dst = (uint32_t)__cvta_generic_to_shared(&s_all_best[rank * SP_MAX_ALTS + place]);
+          asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(dst));
+          asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(dst), "l"(key) : "memory");
+        });
       asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
       if (rank != 0) return;
-      if (warp == 0) {
-        a = s_all[0];
-        for (int i = 1; i < cluster; ++i) a = join(a, s_all[i]);
-        if (ALTS) {
-          floor_key = __shfl_sync(0xffffffffu, best.key, p.n_alts - 1);
-          for (int i = 1; i < cluster; ++i) {
-            const unsigned long long k = lane < p.n_alts ? s_all_best[i * SP_MAX_ALTS + lane] : 0ull;
-            best.insert(k != 0ull, k, p.n_alts, floor_key, lane);
-          }
-        }
-      }
+      a = join_parts(s_all, cluster);
+      found = s_all_best;
+      n_found = cluster * SP_MAX_ALTS;
     }
-    if (warp != 0) return;
   }
   if (!live) return;
   // (all -infinity: s = 0, unless a NaN made it NaN)
@@ -343,7 +380,7 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
   const float l2 = none ? -INFINITY : log2f(a.s);
   // a logit of +infinity makes r infinite and s NaN
   auto logp_of = [&](float x) { return none ? -INFINITY : kLn2 * (fmaf(x, c, -r) - l2); };
-  if (lane == 0) {
+  if (tid == 0) {
     if (p.lse) p.lse[row] = none ? -INFINITY : kLn2 * (r + l2);
     if (ENT && p.entropy) p.entropy[row] = none ? 0.f : kLn2 * (l2 - a.w / a.s);
     if (p.logp && p.targets) {
@@ -358,11 +395,12 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logp
       p.logp[row] = v;
     }
   }
-  if (ALTS && lane < p.n_alts) {
-    const int64_t o = row * p.n_alts + lane;
-    if (p.alt_ids) p.alt_ids[o] = (int32_t)~(uint32_t)best.key;
-    if (p.alt_logp) p.alt_logp[o] = logp_of(order_value((uint32_t)(best.key >> 32)));
-  }
+  if (ALTS)
+    for_best(found, n_found, [&](int place, unsigned long long key) {
+      const int64_t o = row * p.n_alts + place;
+      if (p.alt_ids) p.alt_ids[o] = (int32_t)~(uint32_t)key;
+      if (p.alt_logp) p.alt_logp[o] = logp_of(order_value((uint32_t)(key >> 32)));
+    });
 }
 
 struct GradParams {
