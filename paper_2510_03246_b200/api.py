@@ -470,30 +470,58 @@ def sp_distribute_importance(head_stats, fc_stats, rho, gamma):
 
 
 # ---------------------------------------------------------------------------------- forward of a layer, scoring
-def _on_one_device(*tensors):
-    """CUDA tensors of one device, which has to be the current one (the kernels run on its current stream)."""
-    _require_cuda(*tensors)
-    for t in tensors:
-        if t is not None and t.device.index != torch.cuda.current_device():
-            raise ValueError("the tensors of a call must be on the current CUDA device")
+def _current_device(t):
+    """Index of the CUDA device of t, which has to be the current one (the kernels run on its current stream)."""
+    dev = t.get_device()
+    if dev < 0:
+        _require_cuda(t)
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError("the tensors of a call must be on the current CUDA device")
+    return dev
 
 
-def _vector(t, dtype, n, what):
-    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+def _elsewhere(t):
+    _require_cuda(t)
+    raise ValueError("the tensors of a call must be on one device")
+
+
+def _vector(t, dtype, n, dev, what):
+    """Address of a contiguous vector, None for None."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        _elsewhere(t)
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous {str(dtype)[6:]} with {n} entries")
+    return t.data_ptr()
 
 
-def _dtype_of(t, what):
-    if t.dim() != 2 or t.dtype not in _DTYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+def _rows(t, dev, what):
+    """Matrix view of a 2-D tensor whose rows are contiguous (mat(), with the checks of the calls below)."""
+    if t.get_device() != dev:
+        _elsewhere(t)
+    code = _DTYPES.get(t.dtype)
+    if code is None or t.dim() != 2:
         raise ValueError(f"{what} must be a row-major 2-D tensor of fp32 or bf16")
-    return _DTYPES[t.dtype]
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what} must be a row-major 2-D tensor of fp32 or bf16")
+    return SpMat(t.data_ptr(), code, 0, rows, cols, ld if rows > 1 else max(cols, ld))
 
 
 def rows_of_16_bytes(rows, cols, dtype, device):
     """Uninitialised [rows, cols] whose rows start on 16 bytes (a view of a wider buffer where cols needs it): the layout
     that the tensor-core kernels read, for widths such as a pruned module's k_keep."""
-    per = 16 // torch.empty(0, dtype=dtype).element_size()
-    return torch.empty(rows, (cols + per - 1) // per * per, dtype=dtype, device=device)[:, :cols]
+    per = 16 // dtype.itemsize
+    wide = (cols + per - 1) // per * per
+    t = torch.empty(rows, wide, dtype=dtype, device=device)
+    return t if wide == cols else t[:, :cols]
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_bytes(Nq, Nk, n_seq, n_heads, n_kv, d_head, dtype):      # (a function of the sizes alone)
+    return int(lib().sp_attention_workspace_bytes(Nq, Nk, n_seq, n_heads, n_kv, d_head, dtype))
 
 
 def sp_attention(Q, K, V, cu_q, cu_k, n_heads, n_kv_heads=None, causal=True, scale=None, out=None, lse=None,
@@ -502,33 +530,31 @@ def sp_attention(Q, K, V, cu_q, cu_k, n_heads, n_kv_heads=None, causal=True, sca
     leading dimension; cu_q, cu_k: int32 [n_seq + 1] on the device.  Returns (O, lse or None).  out: where to write O (rows
     of no sequence stay as they are there; in a buffer allocated here they are undefined); lse: fp32 [Nq, n_heads] to
     write, want_lse: allocate it."""
-    _on_one_device(Q, K, V, cu_q, cu_k, out, lse, ws, status)
-    for name, t in (("Q", Q), ("K", K), ("V", V), ("out", out)):
-        if t is not None:
-            _dtype_of(t, name)
+    dev = _current_device(Q)
     n_heads = int(n_heads)
     n_kv = n_heads if n_kv_heads is None else int(n_kv_heads)
     n_seq = cu_q.numel() - 1
     if n_seq < 0:
         raise ValueError("cu_q and cu_k hold n_seq + 1 offsets")
-    _vector(cu_q, torch.int32, n_seq + 1, "cu_q")
-    _vector(cu_k, torch.int32, n_seq + 1, "cu_k")
-    _vector(status, torch.int32, 4, "status")
-    Nq, Nk, d_head = Q.shape[0], K.shape[0], Q.shape[1] // max(n_heads, 1)
+    q, k, v = _rows(Q, dev, "Q"), _rows(K, dev, "K"), _rows(V, dev, "V")
+    d_head = q.cols // max(n_heads, 1)
     if out is None:
-        out = torch.empty(Nq, Q.shape[1], dtype=Q.dtype, device=Q.device)
+        out = torch.empty(q.rows, q.cols, dtype=Q.dtype, device=Q.device)
     if lse is None and want_lse:
-        lse = torch.empty(Nq, n_heads, dtype=torch.float32, device=Q.device)
-    _vector(lse, torch.float32, Nq * n_heads, "lse")
+        lse = torch.empty(q.rows, n_heads, dtype=torch.float32, device=Q.device)
     if scale is None:
         scale = max(d_head, 1) ** -0.5
-    args = SpAttentionArgs(mat(Q), mat(K), mat(V), mat(out), cu_q.data_ptr(), cu_k.data_ptr(), _ptr(lse), n_seq, n_heads,
-                           n_kv, int(bool(causal)), float(scale))
+    args = SpAttentionArgs(q, k, v, _rows(out, dev, "out"), _vector(cu_q, torch.int32, n_seq + 1, dev, "cu_q"),
+                           _vector(cu_k, torch.int32, n_seq + 1, dev, "cu_k"),
+                           _vector(lse, torch.float32, q.rows * n_heads, dev, "lse"), n_seq, n_heads, n_kv,
+                           int(bool(causal)), scale)
     if ws is None:
-        need = lib().sp_attention_workspace_bytes(Nq, Nk, n_seq, n_heads, n_kv, d_head, _dt(Q))
+        need = _attention_bytes(q.rows, k.rows, n_seq, n_heads, n_kv, d_head, q.dtype)
         ws = _ws(need, Q.device) if need else None
-    _check(lib().sp_attention(C.byref(args), _ptr(status), _ptr(ws), ws.nbytes if ws is not None else 0, _stream()),
-           "sp_attention")
+    elif ws.get_device() != dev:
+        _elsewhere(ws)
+    _check(lib().sp_attention(C.byref(args), _vector(status, torch.int32, 4, dev, "status"), _ptr(ws),
+                              ws.nbytes if ws is not None else 0, torch._C._cuda_getCurrentRawStream(dev)), "sp_attention")
     return out, lse
 
 
@@ -536,19 +562,14 @@ def sp_linear(X, W, bias=None, act=SP_LINEAR_NONE, other=None, combine=SP_COMBIN
               status=None):
     """act(X W^T + bias), then other added or multiplied (see sp.h).  X [T, in], W [out, in] of one dtype; bias fp32 [out].
     out may be `other` itself.  A result allocated here has rows that start on 16 bytes (rows_of_16_bytes)."""
-    _on_one_device(X, W, bias, other, out, status)
-    for name, t in (("X", X), ("W", W), ("other", other), ("out", out)):
-        if t is not None:
-            _dtype_of(t, name)
-    n = W.shape[0]
-    _vector(bias, torch.float32, n, "bias")
-    _vector(status, torch.int32, 4, "status")
+    dev = _current_device(X)
+    x, w = _rows(X, dev, "X"), _rows(W, dev, "W")
     if out is None:
-        out = rows_of_16_bytes(X.shape[0], n, out_dtype or X.dtype, X.device)
-    x, w, y = mat(X), mat(W), mat(out)
-    o = mat(other) if other is not None else None
-    _check(lib().sp_linear(C.byref(x), C.byref(w), _ptr(bias), int(act), C.byref(o) if o is not None else None,
-                           int(combine), C.byref(y), _ptr(status), _stream()), "sp_linear")
+        out = rows_of_16_bytes(x.rows, w.rows, out_dtype or X.dtype, X.device)
+    o = None if other is None else C.byref(_rows(other, dev, "other"))
+    _check(lib().sp_linear(C.byref(x), C.byref(w), _vector(bias, torch.float32, w.rows, dev, "bias"), act, o, combine,
+                           C.byref(_rows(out, dev, "out")), _vector(status, torch.int32, 4, dev, "status"),
+                           torch._C._cuda_getCurrentRawStream(dev)), "sp_linear")
     return out
 
 
@@ -564,39 +585,34 @@ class TokenLogprobs:
 def sp_token_logprobs(logits, targets=None, n_alts=0, scale=1.0, want_entropy=True, status=None) -> TokenLogprobs:
     """Log probabilities of the target tokens with entropies and the n_alts best alternatives of every row (see sp.h).
     logits [T, V] bf16 or fp32, any row pitch; targets int64 [T] (negative: the row is not scored)."""
-    _on_one_device(logits, targets, status)
-    _dtype_of(logits, "logits")
-    T, n_alts = logits.shape[0], int(n_alts)
-    _vector(targets, torch.int64, T, "targets")
-    _vector(status, torch.int32, 4, "status")
+    dev = _current_device(logits)
+    x = _rows(logits, dev, "logits")
+    T, n_alts = x.rows, int(n_alts)
     f32 = dict(dtype=torch.float32, device=logits.device)
     keep = 0 < n_alts <= SP_MAX_ALTS                    # (else the library's refusal, with its code)
     r = TokenLogprobs(torch.empty(T, **f32) if targets is not None else None, torch.empty(T, **f32),
                       torch.empty(T, **f32) if want_entropy else None,
                       torch.empty(T, n_alts, dtype=torch.int32, device=logits.device) if keep else None,
                       torch.empty(T, n_alts, **f32) if keep else None)
-    x = mat(logits)
-    _check(lib().sp_token_logprobs(C.byref(x), _ptr(targets), float(scale), n_alts, _ptr(r.logp), _ptr(r.lse),
-                                   _ptr(r.entropy), _ptr(r.alt_ids), _ptr(r.alt_logp), _ptr(status), _stream()),
-           "sp_token_logprobs")
+    _check(lib().sp_token_logprobs(C.byref(x), _vector(targets, torch.int64, T, dev, "targets"), scale, n_alts,
+                                   _ptr(r.logp), r.lse.data_ptr(), _ptr(r.entropy), _ptr(r.alt_ids), _ptr(r.alt_logp),
+                                   _vector(status, torch.int32, 4, dev, "status"),
+                                   torch._C._cuda_getCurrentRawStream(dev)), "sp_token_logprobs")
     return r
 
 
 def sp_token_logprobs_grad(logits, targets, lse, g_logp, entropy=None, g_entropy=None, scale=1.0, out=None):
     """Gradient of sum_t g_logp logp + g_entropy entropy with respect to the logits (see sp.h), in their dtype; lse and
     entropy as sp_token_logprobs left them.  out may be logits itself.  Returns it."""
-    _on_one_device(logits, targets, lse, g_logp, entropy, g_entropy, out)
-    _dtype_of(logits, "logits")
-    T = logits.shape[0]
-    _vector(targets, torch.int64, T, "targets")
-    for name, t in (("lse", lse), ("g_logp", g_logp), ("entropy", entropy), ("g_entropy", g_entropy)):
-        _vector(t, torch.float32, T, name)
+    dev = _current_device(logits)
+    x = _rows(logits, dev, "logits")
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _dtype_of(out, "out")
-    x, d = mat(logits), mat(out)
-    _check(lib().sp_token_logprobs_grad(C.byref(x), _ptr(targets), float(scale), _ptr(lse), _ptr(entropy), _ptr(g_logp),
-                                        _ptr(g_entropy), C.byref(d), _stream()), "sp_token_logprobs_grad")
+        out = torch.empty(x.rows, x.cols, dtype=logits.dtype, device=logits.device)
+    t, h, gl, gh = (_vector(v, torch.float32, x.rows, dev, name) for v, name in
+                    ((lse, "lse"), (entropy, "entropy"), (g_logp, "g_logp"), (g_entropy, "g_entropy")))
+    _check(lib().sp_token_logprobs_grad(C.byref(x), _vector(targets, torch.int64, x.rows, dev, "targets"), scale, t, h, gl,
+                                        gh, C.byref(_rows(out, dev, "out")), torch._C._cuda_getCurrentRawStream(dev)),
+           "sp_token_logprobs_grad")
     return out
 
 
