@@ -275,10 +275,16 @@ __global__ void __launch_bounds__(loss_threads(WARPS), WARPS == 1 ? 4 : 8) token
       for (int u = 0; u < U; ++u) q[u] = ALTS ? __ldcg(xv + v + u * STEP) : __ldcs(xv + v + u * STEP);      // (some are read again: from L2)
       take(q);
     }
-    for (; v < v1; v += STEP) {
-      const uint4 q[1] = {ALTS ? __ldcg(xv + v) : __ldcs(xv + v)};
-      take(q);
-    }
+    uint4 last[U - 1];                                 // what is left, in flight together
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (v + u * STEP < v1) last[u] = ALTS ? __ldcg(xv + v + u * STEP) : __ldcs(xv + v + u * STEP);
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (v + u * STEP < v1) {
+        const uint4 q[1] = {last[u]};
+        take(q);
+      }
     if (has_rear) rear = scalar(tail0 + lane, tail0 + lane < p.V);
     if (ALTS) {
       constexpr int kRowThreads = WARPS * 32;
