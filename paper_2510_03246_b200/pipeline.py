@@ -6,6 +6,10 @@ built from the library calls only (argument marshalling and loop control; all ar
     Step 3/4 per-module ADMM             sp_admm_step x K with the layer's kept count
     Step 5  loss L(T) = sum_l L_l        the module objectives reported by the last step (temperature_search)
 
+attention_head_outputs, prune_attention_module, kept_ffn_weights, ffn_forward and token_loss carry activations through (pruned)
+modules and score the model's predictions: they give a module its calibration input from the module before, and the
+perplexity of Section 4.
+
 plan_distribute covers Steps 1 and 2 of the "-distribute" variant (importances from weight statistics, attention and
 MLP modules allocated separately by inverse weighting).
 
@@ -15,6 +19,7 @@ the only exchange is the vector of importances before Step 2.
 """
 from __future__ import annotations
 
+import math
 import time
 from dataclasses import dataclass, field
 from typing import Callable
@@ -210,6 +215,104 @@ def prune_attention_heads(H: torch.Tensor, Ypre: torch.Tensor, W_O: torch.Tensor
     mask, _, _ = api.sp_apply_mask(scores, k_heads)
     W_new = api.sp_linear_refit(R, G, mask, k_heads, rho, group=d_head, rho_relative=True)
     return mask, W_new, scores
+
+
+def attention_head_outputs(X: torch.Tensor, Wqkv: torch.Tensor, cu: torch.Tensor, n_heads: int, n_kv_heads: int | None = None,
+                           bias: torch.Tensor | None = None, causal: bool = True) -> torch.Tensor:
+    """Concatenated head outputs H [N, n_heads * d_head] of an attention module over packed sequences (cu: int32 offsets [n_seq + 1]
+    on the device, X [N, d] token-major): the input of its output projection, and what prune_attention_heads takes.
+    Wqkv [(n_heads + 2 n_kv_heads) d_head, d]: the rows of W_Q, W_K, W_V one below the other, in X's dtype; bias fp32 or None.
+    Two library calls, and no probabilities in memory (sp_mha_init, which the auxiliary variables of Algorithm 2 start from, keeps
+    n_seq * n_heads * T * T of them)."""
+    n_kv = n_heads if n_kv_heads is None else n_kv_heads
+    d_head = Wqkv.shape[0] // (n_heads + 2 * n_kv)
+    qkv = api.sp_linear(X, Wqkv, bias=bias)
+    q, k = n_heads * d_head, n_kv * d_head
+    H, _ = api.sp_attention(qkv[:, :q], qkv[:, q:q + k], qkv[:, q + k:q + 2 * k], cu, cu, n_heads, n_kv, causal=causal)
+    return H
+
+
+def prune_attention_module(X: torch.Tensor, Wqkv: torch.Tensor, W_O: torch.Tensor, cu: torch.Tensor, n_heads: int, k_heads: int,
+                           rho: float = 0.1, token_chunk: int = 32768, bias: torch.Tensor | None = None, causal: bool = True):
+    """Head pruning of an attention module from its input (every head with a key head of its own): the head outputs over the packed
+    calibration sequences, the pre-trained module output Ypre = H W_O^T, then prune_attention_heads.  W_O fp32 [d, n_heads * d_head].
+    Returns (mask, W_O_new, scores, H, Ypre)."""
+    H = attention_head_outputs(X, Wqkv, cu, n_heads, bias=bias, causal=causal)
+    Ypre = api.sp_linear(H, W_O.to(X.dtype))
+    mask, W_new, scores = prune_attention_heads(H, Ypre, W_O, n_heads, k_heads, rho, token_chunk)
+    return mask, W_new, scores, H, Ypre
+
+
+def kept_ffn_weights(mask: torch.Tensor, W1: torch.Tensor, W2: torch.Tensor, Wg: torch.Tensor | None = None,
+                     b1: torch.Tensor | None = None, dtype=torch.bfloat16):
+    """The weights of a pruned FFN module on its kept channels, in the layout and dtype that ffn_forward reads (rows of W2 start on
+    16 bytes, whatever the number kept).  Returns (W1 [k, d], W2 [d, k], Wg [k, d] or None, b1 [k] or None)."""
+    idx = torch.nonzero(mask, as_tuple=False).flatten()
+    k = int(idx.numel())
+    up, down = (api.rows_of_16_bytes(r, c, dtype, W1.device) for r, c in ((k, W1.shape[1]), (W2.shape[0], k)))
+    up.copy_(W1[idx])
+    down.copy_(W2[:, idx])
+    gate = None
+    if Wg is not None:
+        gate = api.rows_of_16_bytes(k, Wg.shape[1], dtype, Wg.device)
+        gate.copy_(Wg[idx])
+    return up, down, gate, b1[idx].contiguous() if b1 is not None else None
+
+
+def ffn_forward(X: torch.Tensor, W1: torch.Tensor, W2: torch.Tensor, Wg: torch.Tensor | None = None,
+                b1: torch.Tensor | None = None, b2: torch.Tensor | None = None, residual: torch.Tensor | None = None) -> torch.Tensor:
+    """Output [N, d] of an FFN module: W2 relu(W1 x + b1) + b2 (+ residual), or with a gate projection W2 (silu(Wg x) * (W1 x + b1)) + b2
+    (+ residual).  Weights in X's dtype (kept_ffn_weights), biases fp32.  Two (three) library calls."""
+    if Wg is None:
+        A = api.sp_linear(X, W1, bias=b1, act=api.SP_LINEAR_RELU)
+    else:
+        A = api.sp_linear(X, W1, bias=b1)
+        A = api.sp_linear(X, Wg, act=api.SP_LINEAR_SILU, other=A, combine=api.SP_COMBINE_MUL, out=A)
+    return api.sp_linear(A, W2, bias=b2, other=residual)
+
+
+@dataclass
+class TokenLoss:
+    nll: float                          # sum of -log p over the scored tokens
+    tokens: int                         # number of scored tokens
+    logp: torch.Tensor                  # fp32 [N], 0 where not scored
+    d_hidden: torch.Tensor | None       # gradient of nll / tokens, dtype of hidden
+    d_W: torch.Tensor | None            # the same, fp32
+
+    @property
+    def perplexity(self) -> float:
+        return math.exp(self.nll / max(self.tokens, 1))
+
+
+def token_loss(hidden: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor, token_chunk: int = 8192, with_grad: bool = False) -> TokenLoss:
+    """Negative log likelihood of the target tokens under logits = hidden W_lm^T, chunk by chunk (one chunk of logits in memory):
+    the measure of Section 4 is its perplexity.  hidden [N, d], W_lm [V, d] of one dtype; targets int64 [N], negative: not
+    scored.  with_grad: also the gradient of the mean with respect to hidden and W_lm, written over the logits of each chunk and
+    multiplied from there."""
+    N, d = hidden.shape
+    V = W_lm.shape[0]
+    tokens = int((targets >= 0).sum().item())
+    logp = torch.empty(N, dtype=torch.float32, device=hidden.device)
+    status = api.new_status(hidden.device)
+    d_hidden = torch.empty(N, d, dtype=hidden.dtype, device=hidden.device) if with_grad else None
+    d_W = torch.zeros(V, d, dtype=torch.float32, device=hidden.device) if with_grad else None
+    tc = hidden.dtype == torch.bfloat16 and d % 8 == 0
+    logits = api.rows_of_16_bytes(min(token_chunk, N), V, hidden.dtype, hidden.device)
+    g = torch.full((min(token_chunk, N),), -1.0 / max(tokens, 1), dtype=torch.float32, device=hidden.device)
+    for t0 in range(0, N, token_chunk):
+        h, t = hidden[t0:t0 + token_chunk], targets[t0:t0 + token_chunk]
+        n = h.shape[0]
+        x = api.sp_linear(h, W_lm, out=logits[:n])
+        r = api.sp_token_logprobs(x, t, want_entropy=False, status=status)
+        logp[t0:t0 + n] = r.logp
+        if with_grad:
+            api.sp_token_logprobs_grad(x, t, r.lse, g[:n], out=x)
+            api.sp_gemm(x, W_lm, d_hidden[t0:t0 + n], use_tensor_cores=tc)
+            api.sp_gemm(x, h, d_W, transA=True, beta=1.0, use_tensor_cores=tc)
+    code = status.cpu().tolist()
+    if code[0] != 0:
+        raise api.SpError(code[0], f"device status (token {code[1]} of its chunk)")
+    return TokenLoss(-float(logp.double().sum().item()), tokens, logp, d_hidden, d_W)
 
 
 def mha_outer_iterations(mod: api.MhaModule, head_mask: torch.Tensor, iters: int, params: api.MhaParams | None = None,
