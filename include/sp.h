@@ -507,7 +507,7 @@ size_t sp_mha_value_refit_workspace_bytes(int64_t d, int64_t n_heads, int64_t T,
  * Few rows: the keys of a sequence are cut into parts that run side by side and are joined by their lse; the workspace of
  * sp_attention_workspace_bytes (0 when no cut is made) holds their results, scratch of this call alone (two calls that may
  * overlap on the GPU need two).  status_dev may be NULL.
- * Errors: SP_ERR_INVALID_ARG (null pointers, scale not positive and finite), SP_ERR_SHAPE (n_kv_heads does not divide
+ * Errors: SP_ERR_INVALID_ARG (null pointers, scale outside [1e-30, 1e30]), SP_ERR_SHAPE (n_kv_heads does not divide
  * n_heads, column counts, ld, n_seq < 0, more than 2^30 rows), SP_ERR_DTYPE, SP_ERR_UNSUPPORTED (d_head > 128),
  * SP_ERR_WORKSPACE, SP_ERR_ALIGNMENT (workspace not 256-byte aligned).
  */
@@ -559,7 +559,7 @@ sp_status sp_linear(const sp_mat* X, const sp_mat* W, const float* bias, int32_t
  * g_logp, g_entropy: fp32 [T], either may be NULL (zero), g_logp needs targets.  A row that is not scored has no g_logp part;
  * a target >= V is taken as not scored; a row of nothing but -infinity has gradient 0.  dlogits: [T, V], dtype of logits, it
  * may be logits itself (same pointer and ld).
- * Errors: SP_ERR_INVALID_ARG (null logits or outputs, scale not positive and finite, all gradients NULL), SP_ERR_SHAPE
+ * Errors: SP_ERR_INVALID_ARG (null logits or outputs, scale outside [1e-30, 1e30], all gradients NULL), SP_ERR_SHAPE
  * (V < 1 with rows, n_alts outside [0, min(V, SP_MAX_ALTS)], V > 2^30), SP_ERR_DTYPE.
  */
 #define SP_MAX_ALTS 32

@@ -363,7 +363,7 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
   if ((Nq > 1 && (a->Q.ld < a->Q.cols || a->O.ld < a->O.cols)) || (Nk > 1 && (a->K.ld < a->K.cols || a->V.ld < a->V.cols)))
     return SP_ERR_SHAPE;
   if (Nq * a->n_heads > ((int64_t)1 << 33)) return SP_ERR_SHAPE;       // (blocks of the join)
-  if (!(a->scale > 0.0) || !(a->scale <= 1.0e38)) return SP_ERR_INVALID_ARG;
+  if (!(a->scale >= 1e-30) || !(a->scale <= 1e30)) return SP_ERR_INVALID_ARG;
   if (Nq == 0 || a->n_seq == 0) return SP_OK;
   if (!a->Q.ptr || !a->O.ptr || !a->cu_q || !a->cu_k || (Nk > 0 && (!a->K.ptr || !a->V.ptr))) return SP_ERR_INVALID_ARG;
   const Cut cut = plan_cut(Nq, Nk, a->n_seq, a->n_heads, a->n_kv_heads, (int32_t)dh);

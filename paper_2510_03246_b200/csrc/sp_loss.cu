@@ -1,9 +1,10 @@
 // Log probabilities of given tokens with entropy and best alternatives, and their gradient with respect to the logits.
 //
-// With t_v = log2(e) scale x_v and any reference r:  s = sum_v 2^(t_v - r), w = sum_v (t_v - r) 2^(t_v - r) give
-//   lse = ln2 (r + log2 s),   log p_v = ln2 (t_v - r - log2 s),   entropy = ln2 (log2 s - w / s),
+// With c = log2(e) scale and any reference r:  t_v = c (x_v - r), s = sum_v 2^t_v, w = sum_v t_v 2^t_v give
+//   lse = scale r + ln2 log2 s,   log p_v = ln2 (t_v - log2 s),   entropy = ln2 (log2 s - w / s),
 // and (r, s, w) of two parts of a row join by shifting both to the larger r.  So one pass over the logits suffices: every
-// thread keeps its own (r, s, w) with r its running maximum, and they are joined at the end.  All of it is held in fp32.
+// thread keeps its own (r, s, w) with r near its running maximum, and they are joined at the end.  All of it is held in fp32.  (The
+// difference before the product: a row of nothing but the type's lowest value has finite t, while c x_v would not be.)
 //
 // The n best logits need no list during that pass, only every thread's largest value.  The n-th largest of those of a row is a floor that at
 // least n logits reach, and few more do; they stand in the vectors of the (about n) threads whose largest value reaches it.  These
@@ -86,11 +87,11 @@ template <> struct Vec<__nv_bfloat16> {
 struct Part {
   float r, s, w;
 };
-__device__ __forceinline__ Part join(const Part& a, const Part& b) {
+__device__ __forceinline__ Part join(const Part& a, const Part& b, float c) {
   const float r = fmaxf(a.r, b.r);
   if (r == -INFINITY) return Part{r, a.s + b.s, a.w + b.w};     // (zeros, or the NaN of a NaN logit)
-  // a part with r = -infinity holds zeros: its shift is taken as zero (0 * infinity)
-  const float da = a.r == -INFINITY ? 0.f : a.r - r, db = b.r == -INFINITY ? 0.f : b.r - r;
+  // a part with r = -infinity holds zeros: its shift is taken as zero (0 * infinity), and no shift is more than 2^t can tell from 0
+  const float da = a.r == -INFINITY ? 0.f : fmaxf((a.r - r) * c, -10000.f), db = b.r == -INFINITY ? 0.f : fmaxf((b.r - r) * c, -10000.f);
   const float fa = exp2_fast(da), fb = exp2_fast(db);
   return Part{r, a.s * fa + b.s * fb, (a.w + da * a.s) * fa + (b.w + db * b.s) * fb};
 }
@@ -184,20 +185,19 @@ __global__ void __launch_bounds__(loss_threads(WARPS), WARPS == 1 ? 4 : 8) token
   float top = -INFINITY;                               // largest value of this thread's vectors
   bool any = false;                                    // it has had one that is a number
 
-  // The reference follows a maximum that has risen by more than 2^16 (from -infinity: by anything): sums and terms stay far from
-  // the ends of fp32, and the rescaling is rare.
+  // The reference follows a maximum that has risen by more than 2^4 (from -infinity: by anything), so that rescaling is rare.  (Not
+  // much more: log2 s and w / s, the difference of which is the entropy, grow by as much.)
   auto raise = [&](float m) {
-    const float mt = m * c;
-    if (mt - a.r > 16.f) {
-      const float d = a.r - mt, f = exp2_fast(d);      // a.r = -infinity: f = 0, and s = w = 0
-      if (ENT) a.w = a.r == -INFINITY ? a.w : f * fmaf(d, a.s, a.w);
+    if ((m - a.r) * c > 4.f) {
+      const float d = fmaxf((a.r - m) * c, -10000.f), f = exp2_fast(d);      // a.r = -infinity: f = 0, and s = w = 0
+      if (ENT) a.w = f * fmaf(d, a.s, a.w);
       a.s *= f;
-      a.r = mt;
-      rc = mt;
+      a.r = m;
+      rc = m;
     }
   };
   auto take_one = [&](float v) {
-    const float t = fmaf(v, c, -rc), e = exp2_fast(t);
+    const float t = (v - rc) * c, e = exp2_fast(t);
     a.s += e;
     // (a logit of -infinity: e = 0, and 0 times a finite number is added)
     if (ENT) a.w = fmaf(e, fmaxf(t, -10000.f), a.w);
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(loss_threads(WARPS), WARPS == 1 ? 4 : 8) token
       Vec<T>::unpack(q[u], x);
 #pragma unroll
       for (int i = 0; i < N; i += 2) {
-        const uint64_t t = fma2(pack2(x[i], x[i + 1]), c2, r2);
+        const uint64_t t = mul2(add2(pack2(x[i], x[i + 1]), r2), c2);
         float e0, e1;
         unpack2(t, e0, e1);
         const uint64_t e = pack2(exp2_fast(e0), exp2_fast(e1));
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(loss_threads(WARPS), WARPS == 1 ? 4 : 8) token
   for (int o = 16; o > 0; o >>= 1) {
     const Part b{__shfl_xor_sync(0xffffffffu, a.r, o), __shfl_xor_sync(0xffffffffu, a.s, o),
                  __shfl_xor_sync(0xffffffffu, a.w, o)};
-    a = lane & o ? join(b, a) : join(a, b);            // the same order in both lanes
+    a = lane & o ? join(b, a, c) : join(a, b, c);            // the same order in both lanes
   }
   // every warp joins the parts of the row's warps
   auto join_parts = [&](const Part* parts, int n) {
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(loss_threads(WARPS), WARPS == 1 ? 4 : 8) token
     for (int o = 4; o > 0; o >>= 1) {
       const Part d{__shfl_xor_sync(0xffffffffu, b.r, o), __shfl_xor_sync(0xffffffffu, b.s, o),
                    __shfl_xor_sync(0xffffffffu, b.w, o)};
-      b = lane & o ? join(d, b) : join(b, d);
+      b = lane & o ? join(d, b, c) : join(b, d, c);
     }
     return Part{__shfl_sync(0xffffffffu, b.r, 0), __shfl_sync(0xffffffffu, b.s, 0), __shfl_sync(0xffffffffu, b.w, 0)};
   };
@@ -418,10 +418,10 @@ __global__ void __launch_bounds__(loss_threads(WARPS), WARPS == 1 ? 4 : 8) token
   const bool none = a.r == -INFINITY && a.s == 0.f;
   const float r = a.r == -INFINITY ? 0.f : a.r;
   const float l2 = none ? -INFINITY : log2f(a.s);
-  // a logit of +infinity makes r infinite and s NaN
-  auto logp_of = [&](float x) { return none ? -INFINITY : kLn2 * (fmaf(x, c, -r) - l2); };
+  // (a logit of +infinity makes r infinite and s NaN)
+  auto logp_of = [&](float x) { return none ? -INFINITY : kLn2 * ((x - r) * c - l2); };
   if (tid == 0) {
-    if (p.lse) p.lse[row] = none ? -INFINITY : kLn2 * (r + l2);
+    if (p.lse) p.lse[row] = none ? -INFINITY : fmaf(p.scale, r, kLn2 * l2);
     if (ENT && p.entropy) p.entropy[row] = none ? 0.f : kLn2 * (l2 - a.w / a.s);
     if (p.logp && p.targets) {
       const int64_t t = p.targets[row];
@@ -543,7 +543,7 @@ cudaError_t launch_logprobs(const LogprobParams& p, int cluster, cudaStream_t st
   return cudaLaunchKernelEx(&cfg, kernel, p, cluster);
 }
 
-bool positive_finite(double v) { return v > 0.0 && v <= 3.0e38; }
+bool scale_fits(double v) { return v >= 1e-30 && v <= 1e30; }
 
 }  // namespace
 }  // namespace sp
@@ -559,7 +559,7 @@ sp_status sp_token_logprobs(const sp_mat* logits, const int64_t* targets, double
   const int64_t T = logits->rows, V = logits->cols;
   if (T < 0 || V < 0 || V > (1 << 30) || (T > 1 && logits->ld < V)) return SP_ERR_SHAPE;
   if (n_alts < 0 || n_alts > SP_MAX_ALTS || n_alts > V) return SP_ERR_SHAPE;
-  if (!positive_finite(scale)) return SP_ERR_INVALID_ARG;
+  if (!scale_fits(scale)) return SP_ERR_INVALID_ARG;
   if (n_alts > 0 ? !alt_ids && !alt_logp : alt_ids != nullptr || alt_logp != nullptr) return SP_ERR_INVALID_ARG;
   if (logp && !targets) return SP_ERR_INVALID_ARG;
   if (!logp && !lse && !entropy && n_alts == 0) return SP_ERR_INVALID_ARG;
@@ -593,7 +593,7 @@ sp_status sp_token_logprobs_grad(const sp_mat* logits, const int64_t* targets, d
   const int64_t T = logits->rows, V = logits->cols;
   if (T < 0 || V < 0 || V > (1 << 30) || (T > 1 && (logits->ld < V || dlogits->ld < V))) return SP_ERR_SHAPE;
   if (dlogits->rows != T || dlogits->cols != V) return SP_ERR_SHAPE;
-  if (!positive_finite(scale) || (!g_logp && !g_entropy)) return SP_ERR_INVALID_ARG;
+  if (!scale_fits(scale) || (!g_logp && !g_entropy)) return SP_ERR_INVALID_ARG;
   if (T == 0) return SP_OK;
   const int n = 16 / (int)dtype_size(logits->dtype);
   const int64_t chunks = ceil_div(ceil_div(V, (int64_t)n), (int64_t)kLossThreads * kGradVecs);

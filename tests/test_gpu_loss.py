@@ -40,7 +40,7 @@ def reference(x, targets, scale):
         logp = torch.where(targets < 0, 0.0, lp.gather(1, targets.clamp_min(0)[:, None]).squeeze(1))
         logp = torch.where(empty & (targets >= 0), -math.inf, logp)
     V = x.shape[1]
-    zmax = torch.where(torch.isfinite(z), z.abs(), 0.0).amax(1)
+    zmax = torch.where(z.abs() < 1e30, z.abs(), 0.0).amax(1)       # (masked ones do not enter)
     e = 2.0 ** -24 * (12 * zmax + V / (32 if V <= 4096 else 256) + 64)
     return lse, logp, H, lp, p, e
 
@@ -115,6 +115,30 @@ def test_not_a_number_and_infinities(dtype, V):
     y = torch.full((1, 5), math.nan, dtype=dtype, device=DEV)      # only the indices are left
     y[0, 3] = -math.inf
     assert api.sp_token_logprobs(y, None, n_alts=5).alt_ids.tolist() == [[3, 0, 1, 2, 4]]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [40, 9001])
+def test_masks_of_the_lowest_value(dtype, V):
+    """A mask may be the type's lowest number instead of -infinity.  A row of nothing else is a uniform one: the lse is that number (log V
+    is lost beside it), the log probabilities are -log V."""
+    low = torch.finfo(dtype).min
+    x, t = logits_of(4, V, dtype)
+    x[0] = low
+    x[1, 3:] = low
+    x[2, ::2] = low
+    t[:] = 1
+    for scale in (1.0, 0.5):
+        r = api.sp_token_logprobs(x, t, scale=scale, n_alts=3)
+        assert abs(float(r.logp[0]) + math.log(V)) < 1e-5 and abs(float(r.entropy[0]) - math.log(V)) < 1e-4
+        assert float(r.lse[0]) == pytest.approx(low * scale, rel=1e-6) and r.alt_ids[0].tolist() == [0, 1, 2]
+        check(x[1:], t[1:], scale=scale, n_alts=3)
+    hidden = x.clone()
+    hidden[1, 3:] = -math.inf
+    hidden[2, ::2] = -math.inf
+    a, b = api.sp_token_logprobs(x[1:], t[1:]), api.sp_token_logprobs(hidden[1:], t[1:])
+    assert torch.equal(a.lse, b.lse) and torch.equal(a.logp, b.logp)
+    assert (a.entropy - b.entropy).abs().max() < 1e-5
 
 
 @pytest.mark.parametrize("dtype", DTYPES)

@@ -1,0 +1,29 @@
+"""A wait inside the attention kernels that runs out ends the call with SP_ERR_TIMEOUT in the status word; the context stays usable, and
+the next call is right.  (The budget is cut to a few cycles, so that the ordinary wait for the first copy already exceeds it.)"""
+import pytest
+import torch
+
+from paper_2510_03246_b200 import api
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.mark.parametrize("q,k", [([300, 40], [300, 90]), ([1, 1], [3000, 70])])      # tiles of many rows; single tokens
+def test_waits_that_run_out(q, k):
+    heads, dh = 8, 64
+    cu = lambda n: torch.tensor([sum(n[:i]) for i in range(len(n) + 1)], dtype=torch.int32, device=DEV)
+    Q, K, V = (torch.randn(sum(n), heads * dh, device=DEV).bfloat16() for n in (q, k, k))
+    want, _ = api.sp_attention(Q, K, V, cu(q), cu(k), heads)
+    status = api.new_status()
+    torch.cuda.synchronize()
+    api._check(api.lib().sp_set_wait_budget(8), "sp_set_wait_budget")
+    try:
+        api.sp_attention(Q, K, V, cu(q), cu(k), heads, status=status)
+        torch.cuda.synchronize()
+        assert int(status[0]) == 7
+    finally:
+        api._check(api.lib().sp_set_wait_budget(0), "sp_set_wait_budget")
+    status.zero_()
+    got, _ = api.sp_attention(Q, K, V, cu(q), cu(k), heads, status=status)
+    assert torch.equal(got, want) and int(status[0]) == 0

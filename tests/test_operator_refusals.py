@@ -42,7 +42,7 @@ def test_attention_refusals(lib):
     assert attention(lib, n_kv_heads=0) == SHAPE and attention(lib, n_seq=-1) == SHAPE
     assert attention(lib, n_heads=3, n_kv_heads=3) == SHAPE                    # 256 columns are not 3 heads
     assert attention(lib, Q=m((1 << 30) + 1, 256), O=m((1 << 30) + 1, 256)) == SHAPE
-    for scale in (0.0, -1.0, float("nan"), float("inf"), 1e39):
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 1e31, 1e-31):
         assert attention(lib, scale=scale) == INVALID
     assert attention(lib, cu_q=None) == INVALID and attention(lib, cu_k=None) == INVALID
     wide = dict(Q=m(8, 129), O=m(8, 129), K=m(8, 129), V=m(8, 129), n_heads=1, n_kv_heads=1)
@@ -106,7 +106,7 @@ def test_logprob_refusals(lib):
         assert logprobs(lib, m(4, 100), n_alts=n, ids=P) == SHAPE
     assert logprobs(lib, m(4, 3), n_alts=4, ids=P) == SHAPE                    # more alternatives than logits
     assert logprobs(lib, m(4, 100), n_alts=2) == INVALID and logprobs(lib, m(4, 100), ids=P) == INVALID
-    for scale in (0.0, -2.0, float("nan"), float("inf")):
+    for scale in (0.0, -2.0, float("nan"), float("inf"), 1e31, 1e-31):
         assert logprobs(lib, m(4, 100), scale=scale) == INVALID
     assert logprobs(lib, m(4, 100), targets=None) == INVALID
     assert logprobs(lib, m(4, 100), logp=None, lse=None) == INVALID
@@ -127,7 +127,7 @@ def test_gradient_refusals(lib):
     assert grad(lib, x, x, lse=None) == INVALID and grad(lib, x, x, gh=P, entropy=None) == INVALID
     assert grad(lib, x, m(4, 100, ptr=None)) == INVALID
     assert grad(lib, x, m(4, 100, ld=104)) == INVALID                          # in place at another pitch
-    for scale in (0.0, -2.0, float("nan"), float("inf")):
+    for scale in (0.0, -2.0, float("nan"), float("inf"), 1e31, 1e-31):
         assert grad(lib, x, x, scale=scale) == INVALID
     assert grad(lib, m(0, 100, ptr=None), m(0, 100, ptr=None)) == OK
 
