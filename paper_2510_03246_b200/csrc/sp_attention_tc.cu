@@ -551,7 +551,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           }
           const float shift = r == -INFINITY ? 0.f : -r * c;
           const uint64_t shift2 = pack2(shift, shift);
-          uint64_t l2 = pack2(l, 0.f);
+          uint64_t l2[2] = {pack2(l, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             uint32_t w16[16];
@@ -562,20 +562,21 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               unpack2(t, e0, e1);
               e0 = exp2_fast(e0);
               e1 = exp2_fast(e1);
-              l2 = add2(l2, pack2(e0, e1));
+              l2[j & 1] = add2(l2[j & 1], pack2(e0, e1));
               const __nv_bfloat162 e = __floats2bfloat162_rn(e0, e1);
               w16[j] = *reinterpret_cast<const uint32_t*>(&e);
             }
-            tc_st16(t_s + 16u * b, w16);
-            if (b == 1 && !w.alone) {                // the tensor core starts on these keys
+            if (b < 2) tc_st16(t_s + 16u * b, w16);
+            if (b == 2 && !w.alone) {                // the tensor core starts on the first half (stored while this quarter was computed)
               tc_wait_st();
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(p_half(h));
             }
+            if (b >= 2) tc_st16(t_s + 16u * b, w16);
           }
           float l0, l1;
-          unpack2(l2, l0, l1);
+          unpack2(add2(l2[0], l2[1]), l0, l1);
           l = l0 + l1;
           tc_wait_st();
           tc_fence_before();
