@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include "sp_attention.cuh"
+#include "sp_f32x2.cuh"
 
 namespace sp {
 namespace {
@@ -21,7 +22,8 @@ __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float
 // A tile of BM rows (queries x the heads that share a key head) against tiles of 64 keys.  256 threads as 16 x 16: a thread
 // has BM / 16 rows x 4 keys (tx, tx + 16, ...) of the logits and BM / 16 rows x DH / 16 columns of O.  Operands lie in shared memory as fp32
 // in rows of a pitch 4 beyond a multiple of 32, so that both products read 16-byte pieces along their inner index, eight lanes on
-// eight rows without a bank twice: two such reads for 16 fused multiply-adds.
+// eight rows without a bank twice.  What bounds it is those reads beside the multiply-adds: with 128 rows twelve for 128 (the logits' sums over
+// even and over odd channels side by side, two to an instruction), with 64 eight for 64.
 template <typename T, int DH, int BM>
 struct SimtTile {
   static constexpr int P = DH + 4, PP = kBN + 4;
@@ -106,22 +108,32 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const Attn
       });
       __syncthreads();
       float s[TM][4];
+      {
+        uint64_t s2[TM][4];
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+          for (int j = 0; j < 4; ++j) s2[i][j] = 0ull;
 #pragma unroll 4
-      for (int d = 0; d < DH; d += 4) {
-        float4 kf[4];
+        for (int d = 0; d < DH; d += 4) {
+          ulonglong2 kf[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kf[j] = *reinterpret_cast<const float4*>(sk + (tx + 16 * j) * L::P + d);
+          for (int j = 0; j < 4; ++j) kf[j] = *reinterpret_cast<const ulonglong2*>(sk + (tx + 16 * j) * L::P + d);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          const float4 qf = *reinterpret_cast<const float4*>(sq + (ty * TM + i) * L::P + d);
+          for (int i = 0; i < TM; ++i) {
+            const ulonglong2 qf = *reinterpret_cast<const ulonglong2*>(sq + (ty * TM + i) * L::P + d);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            s[i][j] = fmaf(qf.w, kf[j].w, fmaf(qf.z, kf[j].z, fmaf(qf.y, kf[j].y, fmaf(qf.x, kf[j].x, s[i][j]))));
+            for (int j = 0; j < 4; ++j) s2[i][j] = fma2(qf.y, kf[j].y, fma2(qf.x, kf[j].x, s2[i][j]));
+          }
         }
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float a, b;
+            unpack2(s2[i][j], a, b);
+            s[i][j] = a + b;
+          }
       }
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
@@ -134,11 +146,11 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const Attn
 #pragma unroll
         for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
         const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.f : mn;
-        const float f = exp2f(m[i] - ref);
+        const float f = exp2_fast(m[i] - ref);
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          s[i][j] = exp2f(s[i][j] - ref);
+          s[i][j] = exp2_fast(s[i][j] - ref);
           sum += s[i][j];
         }
 #pragma unroll
@@ -289,17 +301,19 @@ cudaError_t launch_simt(const AttnParams& p, cudaStream_t stream) {
   const int64_t rows = (int64_t)p.Nq * p.g;
   const int64_t tiles = min(rows / BM + p.n_seq, (int64_t)p.Nq * ceil_div((int64_t)p.g, (int64_t)BM));
   const int64_t work = tiles * p.n_kv * (p.part > 0 ? p.max_parts : 1);
-  const int64_t resident = (int64_t)sm_count() * (L::SMEM > 110 * 1024 ? 1 : L::SMEM > 72 * 1024 ? 2 : 3);
+  const int64_t resident = (int64_t)sm_count() * (L::SMEM > 113 * 1024 ? 1 : L::SMEM > 75 * 1024 ? 2 : 3);
   const dim3 grid((unsigned)(work < resident ? work : resident));
   return launch(kernel, grid, dim3(kSimtThreads), L::SMEM, stream, p);
 }
 
 template <typename T>
 cudaError_t launch_simt(const AttnParams& p, cudaStream_t stream) {
-  // 16 rows where the sequences have no more on average (single tokens): a tile's products are the bound there
-  const bool few = attention_few_rows(p.Nq, p.g, p.n_seq);
-  if (p.dh <= 64) return few ? launch_simt<T, 64, 16>(p, stream) : launch_simt<T, 64, 64>(p, stream);
-  return few ? launch_simt<T, 128, 16>(p, stream) : launch_simt<T, 128, 64>(p, stream);
+  // 16 rows where the sequences have no more on average (single tokens): a tile's products are the bound there.  128 rows where heads
+  // are wider than 64 and that leaves tiles enough for the SMs (4 x 2048, 64 / 128 rows: heads of 128 6.1 / 4.6 ms, of 64 1.2 / 1.3 ms).
+  const int64_t rows = (int64_t)p.Nq * p.g;
+  const int bm = attention_few_rows(p.Nq, p.g, p.n_seq) ? 16 : p.dh > 64 && rows / 128 * p.n_kv >= 4 * (int64_t)sm_count() ? 128 : 64;
+  if (p.dh <= 64) return bm == 16 ? launch_simt<T, 64, 16>(p, stream) : launch_simt<T, 64, 64>(p, stream);
+  return bm == 16 ? launch_simt<T, 128, 16>(p, stream) : bm == 64 ? launch_simt<T, 128, 64>(p, stream) : launch_simt<T, 128, 128>(p, stream);
 }
 
 struct Cut {
@@ -308,10 +322,10 @@ struct Cut {
 };
 // Whether and how the key axis is cut.  Without a cut there are about Nq g / 128 tiles of rows, at least one for every sequence
 // that has queries, times the key heads; fewer than the SMs (148) leave SMs idle.  Parts are then as long as gives four for every SM
-// (so that sequences of different lengths even out), at least 256 keys.  With few rows an SM reads 1024 keys of a head in 5 us, about what a second
+// (so that sequences of different lengths even out), at least 256 keys.  With few rows an SM reads 1024 keys of a bf16 head (512 in fp32) in 5 us, about what a second
 // launch and the results' way through memory cost: shorter parts do not pay, up to 4096 keys for an SM it gets one part, beyond eight.
 // Sequences that are no longer than a part on average are not cut.
-Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh) {
+Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype) {
   Cut cut;
   if (Nq < 1 || Nk < 1 || n_seq < 1) return cut;
   const int64_t g = n_heads / n_kv, sms = 148;
@@ -322,7 +336,8 @@ Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_k
   const int64_t per_sm = !few ? 4 : tiles * per_tile <= sms * 4096 ? 1 : 8;
   if (tiles >= (per_sm > 1 ? sms * per_sm / 2 : sms)) return cut;
   int64_t part = (int64_t)align_up((size_t)ceil_div(tiles * per_tile, sms * per_sm), 128);
-  if (part < (few ? 1024 : 256)) part = few ? 1024 : 256;
+  const int64_t least = !few ? 256 : dtype == SP_F32 ? 512 : 1024;
+  if (part < least) part = least;
   if (part >= per_tile) return cut;                             // (a longer sequence among many short ones is not worth it)
   const int64_t parts = ceil_div(Nk, part);
   const int64_t elems = parts * Nq * n_heads;
@@ -340,9 +355,8 @@ extern "C" {
 
 size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
                                     int32_t d_head, int32_t dtype) {
-  (void)dtype;
   if (Nq < 0 || Nk < 0 || n_seq < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || d_head < 1) return 0;
-  return sp::plan_cut(Nq, Nk, n_seq, n_heads, n_kv_heads, d_head).bytes;
+  return sp::plan_cut(Nq, Nk, n_seq, n_heads, n_kv_heads, d_head, dtype).bytes;
 }
 
 sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream) {
@@ -366,7 +380,7 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
   if (!(a->scale >= 1e-30) || !(a->scale <= 1e30)) return SP_ERR_INVALID_ARG;
   if (Nq == 0 || a->n_seq == 0) return SP_OK;
   if (!a->Q.ptr || !a->O.ptr || !a->cu_q || !a->cu_k || (Nk > 0 && (!a->K.ptr || !a->V.ptr))) return SP_ERR_INVALID_ARG;
-  const Cut cut = plan_cut(Nq, Nk, a->n_seq, a->n_heads, a->n_kv_heads, (int32_t)dh);
+  const Cut cut = plan_cut(Nq, Nk, a->n_seq, a->n_heads, a->n_kv_heads, (int32_t)dh, dt);
   if (cut.part > 0) {
     if (!ws || ws_bytes < cut.bytes) return SP_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(ws) & 255u) return SP_ERR_ALIGNMENT;
@@ -397,6 +411,8 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
   } else if (tc) {
     const sp_status st = attention_tc(p, s);
     if (st != SP_OK) return st;
+  } else if (dt == SP_F32 && attention_few_rows(Nq, p.g, a->n_seq) && attention_rows_f32_supported(p)) {
+    if (attention_rows_f32(p, s) != cudaSuccess) return SP_ERR_CUDA;
   } else if ((dt == SP_F32 ? launch_simt<float>(p, s) : launch_simt<__nv_bfloat16>(p, s)) != cudaSuccess) return SP_ERR_CUDA;
   if (cut.part > 0) {
     count_launch();

@@ -90,6 +90,8 @@ struct AttnDealer {
 // Few rows on average (single tokens): kernels that stream the keys past them.
 inline bool attention_few_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 16 * n_seq; }
 sp_status attention_rows(const AttnParams& p, cudaStream_t stream);      // bf16 (sp_attention_rows.cu), layouts as below
+bool attention_rows_f32_supported(const AttnParams& p);                     // fp32 (sp_attention_rows_f32.cu): rows that 16-byte copies can take
+cudaError_t attention_rows_f32(const AttnParams& p, cudaStream_t stream);
 // tcgen05 form (sp_attention_tc.cu): layouts that tensor maps can describe
 bool attention_tc_supported(const AttnParams& a);
 sp_status attention_tc(const AttnParams& a, cudaStream_t stream);
