@@ -323,8 +323,8 @@ struct Cut {
 // Whether and how the key axis is cut.  Without a cut there are about Nq g / 128 tiles of rows, at least one for every sequence
 // that has queries, times the key heads; fewer than the SMs (148) leave SMs idle.  Parts are then as long as gives four for every SM
 // (so that sequences of different lengths even out), at least 256 keys.  With few rows an SM reads 1024 keys of a bf16 head (512 in fp32) in 5 us, about what a second
-// launch and the results' way through memory cost: shorter parts do not pay, up to 4096 keys for an SM it gets one part, beyond eight.
-// Sequences that are no longer than a part on average are not cut.
+// launch and the results' way through memory cost: shorter parts do not pay, and beyond 4096 keys for an SM it gets eight.
+// Sequences that are no longer than a part on average are not cut; one of average length falls into equal parts.
 Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype) {
   Cut cut;
   if (Nq < 1 || Nk < 1 || n_seq < 1) return cut;
@@ -333,12 +333,13 @@ Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_k
   const int64_t tiles = (Nq * g / 128 > seqs ? Nq * g / 128 : seqs) * n_kv;
   const int64_t per_tile = ceil_div(Nk, seqs);                 // keys of a tile, on average
   const bool few = attention_few_rows(Nq, g, n_seq);
-  const int64_t per_sm = !few ? 4 : tiles * per_tile <= sms * 4096 ? 1 : 8;
-  if (tiles >= (per_sm > 1 ? sms * per_sm / 2 : sms)) return cut;
+  const int64_t per_sm = few && tiles * per_tile > sms * 4096 ? 8 : 4;
+  if (tiles >= sms * per_sm / 2) return cut;
   int64_t part = (int64_t)align_up((size_t)ceil_div(tiles * per_tile, sms * per_sm), 128);
   const int64_t least = !few ? 256 : dtype == SP_F32 ? 512 : 1024;
   if (part < least) part = least;
   if (part >= per_tile) return cut;                             // (a longer sequence among many short ones is not worth it)
+  part = (int64_t)align_up((size_t)ceil_div(per_tile, ceil_div(per_tile, part)), 128);
   const int64_t parts = ceil_div(Nk, part);
   const int64_t elems = parts * Nq * n_heads;
   if (elems * (dh + 1) * 4 > (int64_t)1 << 30) return cut;
