@@ -503,12 +503,14 @@ size_t sp_mha_value_refit_workspace_bytes(int64_t d, int64_t n_heads, int64_t T,
  * bound.  Rows of O and lse that belong to no sequence are left as they were, and what stands in rows of K and V outside a
  * sequence does not reach it (infinities and NaN included).  Inside a sequence a NaN or an infinity in K or V at a key that the
  * causal mask hides from some queries does not reach those either.
- * Softmax and sums in fp32 in both modes; fp32 mode: products in fp32.  Equal calls give equal bits.
+ * Softmax and sums in fp32 in both modes; fp32 mode: products in fp32.  bf16 mode: the probabilities are rounded to bf16 before
+ * the product with V, the result once; tensor cores where d_head and the leading dimensions of Q, K and V are multiples of 8 and
+ * their pointers 16-byte aligned, else the CUDA cores, slower.  Equal calls give equal bits.
  * Few rows: the keys of a sequence are cut into parts that run side by side and are joined by their lse; the workspace of
  * sp_attention_workspace_bytes (0 when no cut is made) holds their results, scratch of this call alone (two calls that may
  * overlap on the GPU need two).  status_dev may be NULL.
  * Errors: SP_ERR_INVALID_ARG (null pointers, scale outside [1e-30, 1e30]), SP_ERR_SHAPE (n_kv_heads does not divide
- * n_heads, column counts, ld, n_seq < 0, more than 2^30 rows), SP_ERR_DTYPE, SP_ERR_UNSUPPORTED (d_head > 128),
+ * n_heads, column counts, ld, n_seq < 0, more than 2^30 rows or 2^33 rows of heads), SP_ERR_DTYPE, SP_ERR_UNSUPPORTED (d_head > 128),
  * SP_ERR_WORKSPACE, SP_ERR_ALIGNMENT (workspace not 256-byte aligned).
  */
 typedef struct {

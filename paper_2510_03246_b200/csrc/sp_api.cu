@@ -491,7 +491,9 @@ sp_status sp_linear(const sp_mat* X, const sp_mat* W, const float* bias, int32_t
   const Operand o = other ? Operand{other->ptr, other->dtype, other->ld, 1} : Operand{nullptr, Y->dtype, 0, 1};
   const OutOperand y{Y->ptr, Y->dtype, Y->ld};
   if (X->dtype == SP_BF16) {
-    TcOperand ta{X->ptr, X->ld, true}, tb{W->ptr, W->ld, true};
+    // (a single row has no pitch: whatever stands there is not used)
+    const int64_t whole = (K + 7) / 8 * 8;
+    TcOperand ta{X->ptr, T > 1 ? X->ld : whole, true}, tb{W->ptr, N > 1 ? W->ld : whole, true};
     if (gemm_tc_supported(T, N, K, ta, tb)) {
       if (linear_few_rows(T, N)) {
         CU(linear_few(T, N, K, ta, tb, epi, o, y, s));

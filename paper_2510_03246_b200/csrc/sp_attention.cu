@@ -356,7 +356,8 @@ extern "C" {
 
 size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
                                     int32_t d_head, int32_t dtype) {
-  if (Nq < 0 || Nk < 0 || n_seq < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || d_head < 1) return 0;
+  if (Nq < 0 || Nk < 0 || Nq > (1 << 30) || Nk > (1 << 30)) return 0;
+  if (n_seq < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || d_head < 1 || d_head > 128) return 0;
   return sp::plan_cut(Nq, Nk, n_seq, n_heads, n_kv_heads, d_head, dtype).bytes;
 }
 
@@ -388,7 +389,9 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
   }
   AttnParams p = {};
   p.q = a->Q.ptr; p.k = a->K.ptr; p.v = a->V.ptr; p.o = a->O.ptr;
-  p.ldq = a->Q.ld; p.ldk = a->K.ld; p.ldv = a->V.ld; p.ldo = a->O.ld;
+  // (a single row has no pitch: whatever stands there is not used)
+  p.ldq = Nq > 1 ? a->Q.ld : a->Q.cols; p.ldk = Nk > 1 ? a->K.ld : a->K.cols;
+  p.ldv = Nk > 1 ? a->V.ld : a->V.cols; p.ldo = Nq > 1 ? a->O.ld : a->O.cols;
   p.lse = a->lse;
   p.cu_q = a->cu_q; p.cu_k = a->cu_k;
   p.Nq = (int32_t)Nq; p.Nk = (int32_t)Nk;

@@ -74,8 +74,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_f32_kernel(const A
         for (int e = tid; e < kKeys * (DH / 4); e += kThreads) {
           const int j = e / (DH / 4), d = e % (DH / 4) * 4, key = kb + i * kKeys + j;
           const bool in = key < seen && d < p.dh;
-          copy_async(kd + j * C::PK + d, in ? K + (int64_t)key * p.ldk + d : Q, in);
-          copy_async(vd + j * DH + d, in ? V + (int64_t)key * p.ldv + d : Q, in);
+          // (where nothing is read the address still has to be one of 16 bytes: K's first)
+          copy_async(kd + j * C::PK + d, in ? K + (int64_t)key * p.ldk + d : reinterpret_cast<const float*>(p.k), in);
+          copy_async(vd + j * DH + d, in ? V + (int64_t)key * p.ldv + d : reinterpret_cast<const float*>(p.k), in);
         }
       }
       commit_copies();

@@ -34,7 +34,7 @@ constexpr long long kWaitBudget = 4000000000LL, kDrainBudget = 200000000LL;    /
 // Registers of a thread: 168 at launch (384 threads); the eight softmax warps hold a whole row of S and take what the others leave.
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * 168, "shares of the registers at launch");
-constexpr int kBadSlots = 32;       // items between the edge warps and the epilogue: less than the stages of the ring
+constexpr int kBadSlots = 32;       // items with keys between the edge warps and the epilogue: less than the stages of the ring
 
 template <int DH>
 struct Cfg {
@@ -236,7 +236,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 
   AttnDealer dealer;
   AttnItem it;
-  int seq = 0;                // number of the item within this CTA
+  int seq = 0;                // number of the item among those of this CTA that have keys
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == 8) {
@@ -421,9 +421,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const int tid = threadIdx.x - 320;               // 0 .. 63
       uint32_t pos = 0, edge_ph = 0;
       bool ok = true;
-      for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k, ++seq) {
+      for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
         const Work w = work_of(p, it);
         const int n = w.tiles();
+        if (n == 0) continue;
         for (int i = 0; i < n && ok; ++i, pos += 2) {
           if (!w.edge(i)) continue;
           const int s = (int)((pos + 1) % C::STAGES);
@@ -464,6 +465,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           __syncwarp();
           if (lane == 0) mbar_arrive(ready_bar(s));
         }
+        ++seq;
       }
       if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 13);
     }
@@ -478,7 +480,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     uint32_t s_ph = 0, o_ph = 0, s1_ph = 0, pv_ph = 0;
     bool ok = true;
     const uint64_t c2 = pack2(c, c);
-    for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k, ++seq) {
+    for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
       const Work w = work_of(p, it);
       const int token = w.t0 + h * p.tokens + row / p.gp;
       const bool valid = row < p.gp * p.tokens && token < it.nq;
@@ -670,6 +672,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         __syncwarp();
         if (lane == 0) mbar_arrive(o_empty(h));
       }
+      if (w.tiles() > 0) ++seq;
     }
     if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 14);
   }

@@ -296,7 +296,8 @@ def token_loss(hidden: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor, 
     status = api.new_status(hidden.device)
     d_hidden = torch.empty(N, d, dtype=hidden.dtype, device=hidden.device) if with_grad else None
     d_W = torch.zeros(V, d, dtype=torch.float32, device=hidden.device) if with_grad else None
-    tc = hidden.dtype == torch.bfloat16 and d % 8 == 0
+    tc = hidden.dtype == torch.bfloat16 and d % 8 == 0 and all(       # (what the tensor-core product can read)
+        m.stride(0) % 8 == 0 and m.data_ptr() % 16 == 0 for m in (hidden, W_lm))
     logits = api.rows_of_16_bytes(min(token_chunk, N), V, hidden.dtype, hidden.device)
     g = torch.full((min(token_chunk, N),), -1.0 / max(tokens, 1), dtype=torch.float32, device=hidden.device)
     for t0 in range(0, N, token_chunk):

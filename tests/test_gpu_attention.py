@@ -264,3 +264,59 @@ def test_a_batch_gives_what_its_sequences_give_alone():
         a, _ = check(Q[rq], K[rk], V[rk], [q[s]], [k[s]], 32, 8)
         tol = reference(Q[rq], K[rk], V[rk], [q[s]], [k[s]], 32, 8, True, 128 ** -0.5)[2]
         assert ((a.double() - o[rq].double()).abs() <= 2 * tol).all()
+
+
+def test_bad_values_behind_the_mask_with_keyless_sequences_between():
+    """Work without keys does not wait for the tensor core: what is known of one tile's values must not be lost to a later one's.  Rounds of
+    as many equal sequences as there are SMs: infinite values, 31 rounds without keys, infinite values."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    nq, nk = 40, 30
+    k = [nk] * sms + [0] * (31 * sms) + [nk] * sms
+    q = [nq] * len(k)
+    Q, K, V = inputs(sum(q), sum(k), 1, 1, 64, torch.bfloat16)
+    good, _ = api.sp_attention(Q, K, V, cu(q), cu(k), 1)
+    V2 = V.clone()
+    V2.view(-1, nk, 64)[:, 20, 5] = math.inf                        # seen by queries 30 and later
+    o, _ = api.sp_attention(Q, K, V2, cu(q), cu(k), 1)
+    rows = torch.cat([o[:sms * nq], o[-sms * nq:]]).view(-1, nq, 64)
+    want = torch.cat([good[:sms * nq], good[-sms * nq:]]).view(-1, nq, 64).clone()
+    want[:, 30:, 5] = math.inf
+    assert torch.equal(rows, want)
+    assert (o[sms * nq:-sms * nq] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dh", [64, 72])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (3, 1), (8, 1), (10, 1), (16, 1)])
+def test_few_rows_of_each_group(dtype, dh, heads, kv):
+    """Single tokens with 1 to 16 rows per key head; a query matrix that starts anywhere; non-finite values in rows of no sequence."""
+    q, k = [1, 1, 1, 2, 0, 1], [1, 64, 700, 1601, 30, 0]
+    if heads // kv > 8:
+        q[3] = 1
+    n, m = sum(q), sum(k)
+    Q, K, V = inputs(n, m + 70, heads, kv, dh, dtype, seed=heads)
+    K[m:], V[m:] = math.nan, math.inf
+    check(Q, K, V, q, k, heads, kv)
+    check(Q, K, V, q, k, heads, kv, causal=False)
+    buf = torch.zeros(n, heads * dh + 9, dtype=dtype, device=DEV)
+    buf[:, 3:3 + heads * dh] = Q
+    check(buf[:, 3:3 + heads * dh], K, V, q, k, heads, kv)
+
+
+def test_wide_heads_of_long_fp32_sequences():
+    q = [2401, 2300, 2500, 2399]
+    Q, K, V = inputs(sum(q), sum(q), 8, 8, 72, torch.float32)
+    check(Q, K, V, q, q, 8, 8)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_single_row_has_no_pitch(dtype):
+    """One query and one key: the leading dimensions are not used, whatever they are."""
+    Q, K, V = inputs(1, 1, 2, 2, 64, dtype)
+    O = torch.zeros(1, 128, dtype=dtype, device=DEV)
+    c = cu([1])
+    code = api._DTYPES[dtype]
+    args = api.SpAttentionArgs(*(api.SpMat(t.data_ptr(), code, 0, 1, 128, ld) for t, ld in ((Q, 0), (K, 5), (V, 3), (O, 0))),
+                               c.data_ptr(), c.data_ptr(), None, 1, 2, 2, 1, 0.125)
+    assert api.lib().sp_attention(api.C.byref(args), None, None, 0, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(O, V)                                        # the one probability is 1

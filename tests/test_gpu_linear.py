@@ -155,3 +155,25 @@ def test_another_stream_and_a_captured_call(T):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(y, want) and torch.equal(z, want)
+
+
+@pytest.mark.parametrize("T,K,N", [(17, 768, 1536), (24, 1311, 520), (32, 2048, 8192), (32, 320, 8200), (25, 9, 3)])
+def test_up_to_32_rows(T, K, N):
+    x, w, o, b = inputs(T, K, N, torch.bfloat16, seed=T)
+    check(x, w)
+    check(x, w, bias=b, act=api.SP_LINEAR_SILU, other=o, combine=api.SP_COMBINE_MUL)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,N", [(1, 1), (1, 70), (50, 1)])
+def test_a_single_row_has_no_pitch(dtype, T, N):
+    K = 77
+    x, w, _, _ = inputs(T, K, N, dtype)
+    want = check(x, w)
+    y = torch.zeros(T, N, dtype=dtype, device=DEV)
+    code = api._DTYPES[dtype]
+    m = lambda t, r, c: api.SpMat(t.data_ptr(), code, 0, r, c, t.stride(0) if r > 1 else 3)
+    X, W, Y = m(x, T, K), m(w, N, K), m(y, T, N)
+    assert api.lib().sp_linear(api.C.byref(X), api.C.byref(W), None, 0, None, 0, api.C.byref(Y), None,
+                               torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(y, want)
