@@ -31,59 +31,72 @@ struct AttnItem {
 
 // Deals the items of a call in a fixed order: sequence by sequence; within one, tiles from the last (which sees the most
 // keys) to the first, heads, parts.  An item is found by walking the sequences, 32 at a time, from where the last one was
-// found, so a caller asks for rising item numbers.  Every warp keeps a dealer of its own; all lanes of the warp call.
+// found, so a caller asks for rising item numbers; the 32 at hand stay in registers, a lane each.  Every warp keeps a dealer of its own; all
+// lanes of the warp call.
 struct AttnDealer {
-  int32_t base;          // sequences before this group of 32 are passed
-  int64_t passed;        // items of those
-  __device__ __forceinline__ AttnDealer() : base(0), passed(0) {}
+  int32_t base = 0;            // sequences before this group of 32 are passed
+  bool at_hand = false;        // the group's are in the registers below
+  int32_t q0, nq, k0, nk, parts;
+  int64_t passed = 0;          // items of the sequences that are passed
+  int64_t upto, total;         // items of the group up to this lane's sequence, of all
   static __device__ __forceinline__ int32_t bound(int32_t x, int32_t n) { return x < 0 ? 0 : x > n ? n : x; }
   // row_mul: rows per query; rows_per_tile counts those
   __device__ __forceinline__ bool find(const AttnParams& p, int64_t item, int rows_per_tile, int row_mul, int heads,
                                        AttnItem& it) {
     const int lane = threadIdx.x & 31;
-    while (base < p.n_seq) {
-      const int s = base + lane;
-      int q0 = 0, nq = 0, k0 = 0, nk = 0, tiles = 0, parts = 1;
-      if (s < p.n_seq) {
-        q0 = bound(p.cu_q[s], p.Nq);
-        nq = bound(p.cu_q[s + 1], p.Nq) - q0;
-        k0 = bound(p.cu_k[s], p.Nk);
-        nk = bound(p.cu_k[s + 1], p.Nk) - k0;
-        if (nq < 0) nq = 0;
-        if (nk < 0) nk = 0;
-        tiles = (int)(((int64_t)nq * row_mul + rows_per_tile - 1) / rows_per_tile);
-        if (p.part > 0 && nk > p.part) parts = (nk - 1) / p.part + 1;
-      }
-      const int64_t mine = (int64_t)tiles * heads * parts;
-      int64_t upto = mine;                                   // inclusive sums over the lanes
+    while (true) {
+      if (!at_hand) {
+        if (base >= p.n_seq) return false;
+        const int s = base + lane;
+        int32_t tiles = 0;
+        q0 = nq = k0 = nk = 0;
+        parts = 1;
+        if (s < p.n_seq) {
+          q0 = bound(p.cu_q[s], p.Nq);
+          nq = bound(p.cu_q[s + 1], p.Nq) - q0;
+          k0 = bound(p.cu_k[s], p.Nk);
+          nk = bound(p.cu_k[s + 1], p.Nk) - k0;
+          if (nq < 0) nq = 0;
+          if (nk < 0) nk = 0;
+          tiles = (int)(((int64_t)nq * row_mul + rows_per_tile - 1) / rows_per_tile);
+          if (p.part > 0 && nk > p.part) parts = (nk - 1) / p.part + 1;
+        }
+        upto = (int64_t)tiles * heads * parts;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t t = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += t;
+        for (int o = 1; o < 32; o <<= 1) {
+          const int64_t t = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += t;
+        }
+        total = __shfl_sync(0xffffffffu, upto, 31);
+        at_hand = true;
       }
-      const int64_t total = __shfl_sync(0xffffffffu, upto, 31);
       if (item < passed + total) {
         const uint32_t beyond = __ballot_sync(0xffffffffu, item < passed + upto);
         const int l = __ffs(beyond) - 1;
-        int64_t rest = item - passed - (upto - mine);
-        rest = __shfl_sync(0xffffffffu, rest, l);
         it.q0 = __shfl_sync(0xffffffffu, q0, l);
         it.nq = __shfl_sync(0xffffffffu, nq, l);
         it.k0 = __shfl_sync(0xffffffffu, k0, l);
         it.nk = __shfl_sync(0xffffffffu, nk, l);
-        tiles = __shfl_sync(0xffffffffu, tiles, l);
-        parts = __shfl_sync(0xffffffffu, parts, l);
-        const int64_t hp = (int64_t)heads * parts;
-        it.tile = tiles - 1 - (int)(rest / hp);
-        rest %= hp;
-        it.head = (int)(rest / parts);
-        it.c = (int)(rest % parts);
+        const uint32_t of_parts = (uint32_t)__shfl_sync(0xffffffffu, parts, l);
+        // items left in the sequence behind this one: those of later parts, heads, and earlier tiles
+        const int64_t left = passed + __shfl_sync(0xffffffffu, upto, l) - 1 - item, hp = (int64_t)heads * of_parts;
+        uint32_t rest;
+        if (((left | hp) >> 32) == 0) {                        // (64-bit divisions take a thousand cycles)
+          it.tile = (int)((uint32_t)left / (uint32_t)hp);
+          rest = (uint32_t)left % (uint32_t)hp;
+        } else {
+          it.tile = (int)(left / hp);
+          rest = (uint32_t)(left % hp);
+        }
+        rest = (uint32_t)hp - 1 - rest;
+        it.head = (int)(rest / of_parts);
+        it.c = (int)(rest % of_parts);
         return true;
       }
       passed += total;
       base += 32;
+      at_hand = false;
     }
-    return false;
   }
 };
 

@@ -13,8 +13,9 @@
 // that some row does not see whole, two warps clear the rows of V that no row sees, and set non-finite values in rows that only some see to
 // zero; those rows then get them back at the end (rows_with_bad_values).
 //
-// A tile of which only half 0 has rows (few queries, the end of a sequence) uses the tensor memory of both halves for its own key
-// tiles in turn ("alone"): the next S is computed while the softmax works on this one.
+// S and P of a key tile and a half (a job) take one of BUFS buffers of tensor memory in turn: three for heads up to 64 (O is narrow there),
+// so that S of a half's next tile is there when its softmax ends, two for wider ones.  A tile of which only half 0 has rows (few queries, the
+// end of a sequence) has all of them for itself ("alone").
 //
 // Warps: 0-3 and 4-7 softmax of half 0 and 1 (lane and warp give the row), 8 TMA, 9 MMA issue and tensor memory, 10-11 edge tiles of V.
 // Waits for copies, the tensor core and other warps are bounded by a clock budget (SP_ERR_TIMEOUT through status).
@@ -42,9 +43,11 @@ struct Cfg {
   static constexpr int CHUNK = 128 * 128;                  // bytes of one: 128 rows of 128 bytes
   static constexpr int TILE = CH * CHUNK;
   static constexpr int STAGES = DH == 128 ? 5 : 8;
-  static constexpr int BARS = 4 * STAGES + 18;
+  static constexpr int BUFS = DH == 128 ? 2 : 3;           // tiles of S and P in tensor memory
+  static constexpr int BARS = 4 * STAGES + 17;
   static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE + 1024 + 8 * BARS;
-  static constexpr uint32_t S_COL = 0, O_COL = 256;        // tensor memory: S0 S1 | O0 O1
+  static constexpr uint32_t O_COL = 128 * BUFS, O_COLS = DH;      // tensor memory: BUFS x 128 columns of S, then O of both halves
+  static_assert(O_COL + 2 * O_COLS <= 512, "tensor memory");
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
@@ -108,6 +111,12 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
   return pred != 0;
 }
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {      // without suspending the thread
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // bf16 operands, fp32 accumulator, 128 x n; B K-major or (V: keys are K, channels contiguous) MN-major
@@ -166,6 +175,43 @@ __device__ __forceinline__ int64_t item_of(int k) {
   return (int64_t)k * gridDim.x + (k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
 }
 
+// What the thread that issues the matrix instructions has to know of an item (it is one lane, and an item is found by a warp: the TMA warp leaves
+// this in shared memory before the item's Q): key tiles of each half, 0 and 0 behind the last item, and the first edge tile.
+struct Brief {
+  int n0, n1, edge;
+};
+constexpr int kBriefs = 8;             // more than the buffers of S: items between the issue of S and of P V
+
+// A walk over the jobs of an item: key tile by key tile, the halves that see the tile.  (Half 1 has the later rows and sees no fewer tiles
+// than half 0; a tile of rows without half 1 is half 0 alone.)
+struct Cursor {
+  Brief w;
+  int i, h;                            // key tile, half
+  int b = 0;                           // buffer of S and P
+  uint32_t pos = 0;                    // of the tile's K in the ring
+  bool open = false;
+  __device__ __forceinline__ void start(const Brief& of) {
+    w = of;
+    i = 0;
+    h = w.n0 > 0 ? 0 : 1;
+    open = true;
+  }
+  __device__ __forceinline__ int tiles() const { return w.n0 > w.n1 ? w.n0 : w.n1; }
+  __device__ __forceinline__ bool first() const { return h == 0 || w.n0 <= i; }       // of the tile
+  __device__ __forceinline__ bool last() const { return h == 1 || w.n1 <= i; }
+  __device__ __forceinline__ void advance(int bufs) {
+    b = b + 1 == bufs ? 0 : b + 1;
+    if (!last()) {
+      h = 1;
+      return;
+    }
+    ++i;
+    pos += 2;
+    h = w.n0 > i ? 0 : 1;
+    open = i < tiles();
+  }
+};
+
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -174,6 +220,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort;
+  __shared__ Brief s_brief[kBriefs];
   __shared__ int s_bad[kBadSlots];       // slot of an item: its number where V had non-finite values behind the mask
 
   const uint32_t raw = smem_u32(smem_raw);
@@ -186,14 +233,11 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   auto empty_bar = [&](int s) { return bars + 8u * (3 * C::STAGES + s); };
   const uint32_t misc = bars + 8u * 4 * C::STAGES;
   const uint32_t q_full = misc, q_empty = misc + 8, drain_bar = misc + 16;
-  auto s_full = [&](int h) { return misc + 24u + 8u * h; };
-  auto p_full = [&](int h) { return misc + 40u + 8u * h; };
-  auto o_full = [&](int h) { return misc + 56u + 8u * h; };
-  auto o_empty = [&](int h) { return misc + 72u + 8u * h; };
-  auto s1_full = [&](int x) { return misc + 88u + 8u * x; };      // a tile alone: S and P in the tensor memory of half x
-  auto p1_full = [&](int x) { return misc + 104u + 8u * x; };
-  auto p_half = [&](int h) { return misc + 128u + 8u * h; };      // the first 64 columns of P
-  const uint32_t pv_done = misc + 120u;                           // a tile alone: O += P V of a key tile
+  auto pv_done = [&](int h) { return misc + 24u + 8u * h; };                    // O of half h += P V of a key tile
+  // S in buffer b, for half h.  (A wait tells a phase from the next one only: every phase of a barrier is waited for by the same warps.)
+  auto s_full = [&](int h, int b) { return misc + 40u + 8u * (3 * h + b); };
+  auto p_half = [&](int b) { return misc + 88u + 8u * b; };                     // the first 64 columns of P
+  auto p_full = [&](int b) { return misc + 112u + 8u * b; };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = &s_abort;
@@ -210,15 +254,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     mbar_init(drain_bar, 1);
-    mbar_init(pv_done, 1);
     for (int h = 0; h < 2; ++h) {
-      mbar_init(s_full(h), 1);
-      mbar_init(p_full(h), 4);
-      mbar_init(p_half(h), 4);
-      mbar_init(o_full(h), 1);
-      mbar_init(o_empty(h), 4);
-      mbar_init(s1_full(h), 1);
-      mbar_init(p1_full(h), 4);
+      mbar_init(pv_done(h), 1);
+      for (int b = 0; b < C::BUFS; ++b) mbar_init(s_full(h, b), 1);
+    }
+    for (int b = 0; b < C::BUFS; ++b) {
+      mbar_init(p_half(b), 4);
+      mbar_init(p_full(b), 4);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -253,6 +295,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           if (loaded > 0) ok = mbar_wait(q_empty, (uint32_t)(loaded - 1) & 1u, abort_flag, budget);
           if (ok) {
             const int halves = w.alone ? 1 : 2;
+            s_brief[loaded % kBriefs] = Brief{w.n[0], w.n[1], w.sure > w.kb ? (w.sure - w.kb) / kKeys : 0};
             mbar_expect_tx(q_full, (uint32_t)(halves * C::CH * p.gp * p.tokens * 128));
             for (int h = 0; h < halves; ++h)
   #pragma unroll
@@ -275,144 +318,113 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
         if (!ok) break;
       }
+      if (ok && lane == 0) {      // no more
+        if (loaded > 0) ok = mbar_wait(q_empty, (uint32_t)(loaded - 1) & 1u, abort_flag, budget);
+        s_brief[loaded % kBriefs] = Brief{0, 0, 0};
+        if (ok) mbar_arrive(q_full);
+      }
       if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 11);
     } else if (warp == 9) {
       // ------------------------------------------------------------------------------------------------ MMA
-      const uint32_t id_s = instr_desc(true, kKeys), id_o = instr_desc(false, DH);
-      uint32_t pos = 0, full_ph = 0, ready_ph = 0;      // phases of the barriers of a stage: a bit each
-      uint32_t p_ph = 0, p1_ph = 0, oe_ph = 0;          // of a half: a bit each
-      int loaded = 0;
-      bool ok = true, issued = false;
-      uint32_t wrote_o = 0;                             // halves that have had an output
-      for (int k = 0; dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
-        const Work w = work_of(p, it);
-        const int n = w.tiles();
-        if (n == 0) continue;
-        if (elect_one()) {
-          auto stage_at = [&](uint32_t x) { return (int)(x % C::STAGES); };
-          auto wait_full = [&](int s) {
-            const bool got = mbar_wait(full_bar(s), (full_ph >> s) & 1u, abort_flag, budget);
-            full_ph ^= 1u << s;
-            return got;
-          };
-          auto scores = [&](int h, int s, int at, uint32_t bar) {     // S of half h in the tensor memory of `at`
-            const uint32_t a0 = desc_low(q_smem + h * C::TILE, 16), b0 = desc_low(ring + s * C::TILE, 16);
-  #pragma unroll
-            for (int k = 0; k < DH / 16; ++k) {
-              const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
-              tc_mma_ss(tmem + C::S_COL + 128u * at, a0 + off, b0 + off, id_s, k > 0);
-            }
-            tc_commit_one(bar);
-          };
-          // O of half h += P V over half `part` of the keys, P in the tensor memory of `at`
-          auto values = [&](int h, int s, int at, bool first, int part) {
-            const uint32_t v0 = desc_low(ring + s * C::TILE + part * (kKeys / 2 * 128), C::CHUNK);
-            const uint32_t d = tmem + C::O_COL + 128u * h, a0 = tmem + C::S_COL + 128u * at + 32u * part;
-#pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, !first || k > 0);
-          };
-          auto wait_v = [&](int i, int s) {
-            if (!w.edge(i)) return wait_full(s);
-            const bool got = mbar_wait(ready_bar(s), (ready_ph >> s) & 1u, abort_flag, budget);
-            ready_ph ^= 1u << s;
-            return got;
-          };
-          ok = mbar_wait(q_full, (uint32_t)loaded & 1u, abort_flag, budget) && wait_full(stage_at(pos));
-          if (ok && w.alone) {
-            // S of tile i + 2 takes the place of P of tile i, behind the product that reads it
-            tc_fence_after();
-            scores(0, stage_at(pos), 0, s1_full(0));
-            issued = true;
-            tc_commit_one(empty_bar(stage_at(pos)));
-            if (n == 1) tc_commit_one(q_empty);
-            if (n > 1) {
-              ok = wait_full(stage_at(pos + 2));
-              if (ok) {
-                tc_fence_after();
-                scores(0, stage_at(pos + 2), 1, s1_full(1));
-                tc_commit_one(empty_bar(stage_at(pos + 2)));
-                if (n == 2) tc_commit_one(q_empty);
-              }
-            }
-            for (int i = 0; i < n && ok; ++i, pos += 2) {
-              const int x = i & 1, sv = stage_at(pos + 1), sk = stage_at(pos + 4);
-              ok = wait_v(i, sv) && mbar_wait(p1_full(x), (p1_ph >> x) & 1u, abort_flag, budget);
-              p1_ph ^= 1u << x;
-              if (ok && i == 0 && (wrote_o & 1u)) {
-                ok = mbar_wait(o_empty(0), oe_ph & 1u, abort_flag, budget);
-                oe_ph ^= 1u;
-              }
-              if (!ok) break;
-              tc_fence_after();
-              values(0, sv, x, i == 0, 0);
-              values(0, sv, x, false, 1);
-              tc_commit_one(pv_done);
-              tc_commit_one(empty_bar(sv));
-              wrote_o |= 1u;
-              if (i + 2 < n) {
-                ok = wait_full(sk);
-                if (!ok) break;
-                tc_fence_after();
-                scores(0, sk, x, s1_full(x));
-                tc_commit_one(empty_bar(sk));
-                if (i + 3 == n) tc_commit_one(q_empty);
-              }
-            }
-          } else if (ok) {
-            tc_fence_after();
-            for (int h = 0; h < 2; ++h)
-              if (w.n[h] > 0) scores(h, stage_at(pos), h, s_full(h));
-            issued = true;
-            tc_commit_one(empty_bar(stage_at(pos)));
-            if (n == 1) tc_commit_one(q_empty);
+      // Two cursors over the same jobs (key tile, half): one issues S of a job, the other O += P V.  S of the next jobs is issued as soon
+      // as a buffer, its keys and its rows are there, across the items; a buffer is free behind the product that reads its P, since the tensor
+      // core takes the instructions of a thread in order.
+      bool ok = true;
+      if (elect_one()) {
+        const uint32_t id_s = instr_desc(true, kKeys), id_o = instr_desc(false, DH);
+        uint32_t full_ph = 0, ready_ph = 0, p_ph = 0;    // phases of the barriers of a stage, of a buffer: a bit each
+        int items_s = 0, items_v = 0;                    // items that the cursors have been given
+        int ahead = 0;                                   // jobs whose S is issued and whose P V is not
+        bool end = false, issued = false;
+        Cursor cs, cv;
+        long long t0 = 0;                                // since when nothing could be issued (0: something was)
+        while (true) {
+          if (!cs.open && !end && mbar_test(q_full, (uint32_t)items_s & 1u)) {
+            const Brief w = s_brief[items_s % kBriefs];
+            ++items_s;
+            end = w.n0 == 0 && w.n1 == 0;
+            if (!end) cs.start(w);
           }
-          for (int i = 0; i < n && ok && !w.alone; ++i) {
-            const int sv = stage_at(pos + 1), sk = stage_at(pos + 2);
-            const bool more = i + 1 < n;
-            ok = wait_v(i, sv);
-            if (ok && more) ok = wait_full(sk);
-            for (int h = 0; h < 2 && ok; ++h) {
-              if (i >= w.n[h]) continue;
-              ok = mbar_wait(p_half(h), (p_ph >> h) & 1u, abort_flag, budget);
-              if (ok && i == 0 && ((wrote_o >> h) & 1u)) {        // the item before has left O
-                ok = mbar_wait(o_empty(h), (oe_ph >> h) & 1u, abort_flag, budget);
-                oe_ph ^= 1u << h;
+          if (cs.open && ahead < C::BUFS) {
+            const int s = (int)(cs.pos % C::STAGES);
+            bool ready = true;
+            if (cs.first()) {
+              ready = mbar_test(full_bar(s), (full_ph >> s) & 1u);
+              if (ready) full_ph ^= 1u << s;
+            }
+            if (ready) {
+              tc_fence_after();
+              const uint32_t a0 = desc_low(q_smem + cs.h * C::TILE, 16), b0 = desc_low(ring + s * C::TILE, 16);
+              const uint32_t d = tmem + 128u * cs.b;
+#pragma unroll
+              for (int k = 0; k < DH / 16; ++k) {
+                const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
+                tc_mma_ss(d, a0 + off, b0 + off, id_s, k > 0);
               }
+              tc_commit_one(s_full(cs.h, cs.b));
+              if (cs.last()) {
+                tc_commit_one(empty_bar(s));
+                if (cs.i + 1 == cs.tiles()) tc_commit_one(q_empty);
+              }
+              issued = true;
+              ++ahead;
+              cs.advance(C::BUFS);
+              t0 = 0;
+              continue;
+            }
+          }
+          if (ahead > 0) {
+            if (!cv.open) cv.start(s_brief[items_v++ % kBriefs]);
+            if (mbar_test(p_half(cv.b), (p_ph >> cv.b) & 1u)) {
+              const int s = (int)((cv.pos + 1) % C::STAGES);
+              if (cv.first()) {
+                if (cv.i >= cv.w.edge) {
+                  ok = mbar_wait(ready_bar(s), (ready_ph >> s) & 1u, abort_flag, budget);
+                  ready_ph ^= 1u << s;
+                } else {
+                  ok = mbar_wait(full_bar(s), (full_ph >> s) & 1u, abort_flag, budget);
+                  full_ph ^= 1u << s;
+                }
+                if (!ok) break;
+              }
+              // (P of a half's first key tile also says that its warps have read O of the item before)
+              const uint32_t d = tmem + C::O_COL + C::O_COLS * cv.h, a0 = tmem + 128u * cv.b;
+              const uint32_t v0 = desc_low(ring + s * C::TILE, C::CHUNK);
+              tc_fence_after();
+#pragma unroll
+              for (int k = 0; k < kKeys / 32; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, cv.i > 0 || k > 0);
+              ok = mbar_wait(p_full(cv.b), (p_ph >> cv.b) & 1u, abort_flag, budget);
+              p_ph ^= 1u << cv.b;
               if (!ok) break;
               tc_fence_after();
-              values(h, sv, h, i == 0, 0);
-              ok = mbar_wait(p_full(h), (p_ph >> h) & 1u, abort_flag, budget);
-              p_ph ^= 1u << h;
-              if (!ok) break;
-              tc_fence_after();
-              values(h, sv, h, false, 1);
-              if (i + 1 < w.n[h]) {
-                scores(h, sk, h, s_full(h));
-              } else {
-                tc_commit_one(o_full(h));
-                wrote_o |= 1u << h;
-              }
+#pragma unroll
+              for (int k = kKeys / 32; k < kKeys / 16; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, 1u);
+              tc_commit_one(pv_done(cv.h));
+              if (cv.last()) tc_commit_one(empty_bar(s));
+              --ahead;
+              cv.advance(C::BUFS);
+              t0 = 0;
+              continue;
             }
-            if (!ok) break;
-            tc_commit_one(empty_bar(sv));
-            if (more) {
-              tc_commit_one(empty_bar(sk));
-              if (i + 2 == n) tc_commit_one(q_empty);
-            }
-            pos += 2;
+          } else if (end) {
+            break;
+          }
+          if (t0 == 0) {
+            t0 = clock64();
+          } else if (clock64() - t0 > budget) {
+            *abort_flag = 1;
+          }
+          if (*abort_flag) {
+            ok = false;
+            break;
           }
         }
-        ++loaded;
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-      }
-      if (lane == 0) {
         if (!ok) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 12);
         // (in a complete run the epilogues have seen the last products; this matters when a role gave up)
         if (issued && (!ok || *abort_flag)) {
           tc_commit_one(drain_bar);
-          const long long t0 = clock64();
-          while (!mbar_try(drain_bar, 0u) && clock64() - t0 < kDrainBudget) {}
+          const long long t1 = clock64();
+          while (!mbar_try(drain_bar, 0u) && clock64() - t1 < kDrainBudget) {}
         }
       }
       __syncwarp();
@@ -475,9 +487,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const int h = warp >> 2, q = warp & 3;
     const int row = q * 32 + lane;                   // of the half, and lane of tensor memory
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
-    const uint32_t t_o = tmem + C::O_COL + 128u * h + lanes;
+    const uint32_t t_o = tmem + C::O_COL + C::O_COLS * h + lanes;
     const float c = p.a.scale_log2;
-    uint32_t s_ph = 0, o_ph = 0, s1_ph = 0, pv_ph = 0;
+    uint32_t s_ph = 0, pv_ph = 0, jobs = 0;          // (of a buffer: a bit each; jobs of the items before)
     bool ok = true;
     const uint64_t c2 = pack2(c, c);
     for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
@@ -486,21 +498,19 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const bool valid = row < p.gp * p.tokens && token < it.nq;
       const int lim = valid ? min(visible(it, p.a.causal, token), w.seen) : 0;       // keys [0, lim)
       const bool busy = __any_sync(0xffffffffu, valid);
-      const int n = w.n[h];
+      const int n = h ? w.n[1] : w.n[0];
       float r = -INFINITY, l = 0.f;                  // reference (not yet times c) and sum
       for (int i = 0; i < n; ++i) {
-        const int at = w.alone ? i & 1 : h;          // whose tensor memory holds S and takes P
-        const uint32_t t_s = tmem + C::S_COL + 128u * at + lanes;
-        bool got = mbar_wait(w.alone ? s1_full(at) : s_full(h), w.alone ? (s1_ph >> at) & 1u : s_ph, abort_flag, budget);
-        if (w.alone) s1_ph ^= 1u << at;
-        else s_ph ^= 1u;
+        const int b_ = (int)((jobs + (w.alone ? i : i < w.n[0] ? 2 * i + h : w.n[0] + i)) % C::BUFS);      // the buffer of the job
+        const uint32_t t_s = tmem + 128u * b_ + lanes;
+        bool got = mbar_wait(s_full(h, b_), (s_ph >> b_) & 1u, abort_flag, budget);
+        s_ph ^= 1u << b_;
         ok = __all_sync(0xffffffffu, got);
         if (!ok) break;
-        // (a tile alone: the product of the tile before may still add to O, unlike with two halves, where S follows it)
-        bool o_still = !(w.alone && i > 0);
+        bool o_still = i == 0;                       // the product of the tile before may still add to O
         auto wait_o_still = [&] {
           if (o_still) return;
-          got = mbar_wait(pv_done, pv_ph, abort_flag, budget);
+          got = mbar_wait(pv_done(h), pv_ph, abort_flag, budget);
           pv_ph ^= 1u;
           o_still = true;
           ok = __all_sync(0xffffffffu, got);
@@ -569,11 +579,11 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               w16[j] = *reinterpret_cast<const uint32_t*>(&e);
             }
             if (b < 2) tc_st16(t_s + 16u * b, w16);
-            if (b == 2 && !w.alone) {                // the tensor core starts on the first half (stored while this quarter was computed)
+            if (b == 2) {                            // the tensor core starts on the first half (stored while this quarter was computed)
               tc_wait_st();
               tc_fence_before();
               __syncwarp();
-              if (lane == 0) mbar_arrive(p_half(h));
+              if (lane == 0) mbar_arrive(p_half(b_));
             }
             if (b >= 2) tc_st16(t_s + 16u * b, w16);
           }
@@ -583,11 +593,11 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           tc_wait_st();
           tc_fence_before();
         }
-        if (!busy && !w.alone && lane == 0) mbar_arrive(p_half(h));
+        if (!busy && lane == 0) mbar_arrive(p_half(b_));
         wait_o_still();      // at the latest here, so that no phase of the barrier is passed over
         if (!ok) break;
         __syncwarp();
-        if (lane == 0) mbar_arrive(w.alone ? p1_full(at) : p_full(h));
+        if (lane == 0) mbar_arrive(p_full(b_));
       }
       if (!ok) break;
       // ---- output of the item
@@ -601,9 +611,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         : nullptr;
       bool bad = false;
       if (n > 0) {
-        const bool got = mbar_wait(w.alone ? pv_done : o_full(h), w.alone ? pv_ph : o_ph, abort_flag, budget);
-        if (w.alone) pv_ph ^= 1u;
-        else o_ph ^= 1u;
+        const bool got = mbar_wait(pv_done(h), pv_ph, abort_flag, budget);
+        pv_ph ^= 1u;
         ok = __all_sync(0xffffffffu, got);
         if (!ok) break;
         tc_fence_after();
@@ -667,11 +676,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           else if (p.a.lse) p.a.lse[out_row * p.a.n_heads + head] = lse2 == -INFINITY ? lse2 : lse2 * 0.6931471805599453f;
         }
       }
-      if (n > 0) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(o_empty(h));
-      }
+      tc_fence_before();                             // (the next P of this half says that O has been read)
+      jobs = (jobs + w.n[0] + w.n[1]) % C::BUFS;
       if (w.tiles() > 0) ++seq;
     }
     if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 14);
