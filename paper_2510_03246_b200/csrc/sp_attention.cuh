@@ -81,7 +81,7 @@ struct AttnDealer {
         // items left in the sequence behind this one: those of later parts, heads, and earlier tiles
         const int64_t left = passed + __shfl_sync(0xffffffffu, upto, l) - 1 - item, hp = (int64_t)heads * of_parts;
         uint32_t rest;
-        if (((left | hp) >> 32) == 0) {                        // (64-bit divisions take a thousand cycles)
+        if (((left | hp) >> 32) == 0) {                        // (64-bit divisions are slow)
           it.tile = (int)((uint32_t)left / (uint32_t)hp);
           rest = (uint32_t)left % (uint32_t)hp;
         } else {

@@ -17,7 +17,10 @@
 // so that S of a half's next tile is there when its softmax ends, two for wider ones.  A tile of which only half 0 has rows (few queries, the
 // end of a sequence) has all of them for itself ("alone").
 //
-// Warps: 0-3 and 4-7 softmax of half 0 and 1 (lane and warp give the row), 8 TMA, 9 MMA issue and tensor memory, 10-11 edge tiles of V.
+// Warps: 0-3 and 4-7 softmax of half 0 and 1 (lane and warp give the row), 8 finds the items and issues TMA, 9 MMA issue and tensor memory,
+// 10-11 edge tiles of V.  Items go to the other warps through shared memory (finding one takes two thousand cycles).
+// What bounds it: per half and tile 128 exponentials a row (1024 cycles of the pipe that two warps share) between two products (1024 cycles
+// together for heads of 128).  One prompt of 8192, 32 heads of 128 on 8: 479 us; 16 documents of up to 2048 tokens, 32 heads of 64 on 8: 176 us.
 // Waits for copies, the tensor core and other warps are bounded by a clock budget (SP_ERR_TIMEOUT through status).
 #include <math.h>
 #include <string.h>
@@ -36,6 +39,7 @@ constexpr long long kWaitBudget = 4000000000LL, kDrainBudget = 200000000LL;    /
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * 168, "shares of the registers at launch");
 constexpr int kBadSlots = 32;       // items with keys between the edge warps and the epilogue: less than the stages of the ring
+constexpr int kItems = 8;           // items handed from the TMA warp to the softmax and edge warps
 
 template <int DH>
 struct Cfg {
@@ -44,7 +48,7 @@ struct Cfg {
   static constexpr int TILE = CH * CHUNK;
   static constexpr int STAGES = DH == 128 ? 5 : 8;
   static constexpr int BUFS = DH == 128 ? 2 : 3;           // tiles of S and P in tensor memory
-  static constexpr int BARS = 4 * STAGES + 17;
+  static constexpr int BARS = 4 * STAGES + 17 + 2 * kItems;
   static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE + 1024 + 8 * BARS;
   static constexpr uint32_t O_COL = 128 * BUFS, O_COLS = DH;      // tensor memory: BUFS x 128 columns of S, then O of both halves
   static_assert(O_COL + 2 * O_COLS <= 512, "tensor memory");
@@ -188,7 +192,7 @@ struct Cursor {
   Brief w;
   int i, h;                            // key tile, half
   int b = 0;                           // buffer of S and P
-  uint32_t pos = 0;                    // of the tile's K in the ring
+  int stage = 0;                       // of the ring: the tile's K, its V is in the next one
   bool open = false;
   __device__ __forceinline__ void start(const Brief& of) {
     w = of;
@@ -199,14 +203,14 @@ struct Cursor {
   __device__ __forceinline__ int tiles() const { return w.n0 > w.n1 ? w.n0 : w.n1; }
   __device__ __forceinline__ bool first() const { return h == 0 || w.n0 <= i; }       // of the tile
   __device__ __forceinline__ bool last() const { return h == 1 || w.n1 <= i; }
-  __device__ __forceinline__ void advance(int bufs) {
+  __device__ __forceinline__ void advance(int bufs, int stages) {
     b = b + 1 == bufs ? 0 : b + 1;
     if (!last()) {
       h = 1;
       return;
     }
     ++i;
-    pos += 2;
+    stage = stage + 2 >= stages ? stage + 2 - stages : stage + 2;
     h = w.n0 > i ? 0 : 1;
     open = i < tiles();
   }
@@ -221,6 +225,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort;
   __shared__ Brief s_brief[kBriefs];
+  __shared__ AttnItem s_item[kItems];    // tile < 0: no more
   __shared__ int s_bad[kBadSlots];       // slot of an item: its number where V had non-finite values behind the mask
 
   const uint32_t raw = smem_u32(smem_raw);
@@ -238,6 +243,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   auto s_full = [&](int h, int b) { return misc + 40u + 8u * (3 * h + b); };
   auto p_half = [&](int b) { return misc + 88u + 8u * b; };                     // the first 64 columns of P
   auto p_full = [&](int b) { return misc + 112u + 8u * b; };
+  auto item_full = [&](int k) { return misc + 136u + 16u * (k % kItems); };
+  auto item_empty = [&](int k) { return misc + 144u + 16u * (k % kItems); };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = &s_abort;
@@ -254,6 +261,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     mbar_init(drain_bar, 1);
+    for (int k = 0; k < kItems; ++k) {
+      mbar_init(item_full(k), 1);
+      mbar_init(item_empty(k), 10);
+    }
     for (int h = 0; h < 2; ++h) {
       mbar_init(pv_done(h), 1);
       for (int b = 0; b < C::BUFS; ++b) mbar_init(s_full(h, b), 1);
@@ -276,17 +287,37 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const uint32_t tmem = s_tmem_base;
   kernel_begin();
 
-  AttnDealer dealer;
   AttnItem it;
   int seq = 0;                // number of the item among those of this CTA that have keys
+  // the k-th item of this CTA, for the softmax and edge warps; false behind the last one, or when a wait ran out
+  auto next_item = [&](int k, bool& ok) {
+    ok = __all_sync(0xffffffffu, mbar_wait(item_full(k), (uint32_t)(k / kItems) & 1u, abort_flag, budget));
+    if (!ok) return false;
+    it = s_item[k % kItems];
+    return it.tile >= 0;
+  };
+  auto item_read = [&](int k) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(item_empty(k));
+  };
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == 8) {
       // ------------------------------------------------------------------------------------------------ TMA
+      AttnDealer dealer;
       uint32_t pos = 0;         // tiles loaded so far
       int loaded = 0;           // items with keys so far (their Q was loaded)
       bool ok = true;
-      for (int k = 0; dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
+      for (int k = 0;; ++k) {
+        const bool more = dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it);
+        if (!more) it.tile = -1;
+        if (lane == 0) {
+          if (k >= kItems) ok = mbar_wait(item_empty(k), (uint32_t)(k / kItems - 1) & 1u, abort_flag, budget);
+          s_item[k % kItems] = it;
+          if (ok) mbar_arrive(item_full(k));
+        }
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (!ok || !more) break;
         const Work w = work_of(p, it);
         const int n = w.tiles();
         if (n == 0) continue;
@@ -328,16 +359,45 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       // ------------------------------------------------------------------------------------------------ MMA
       // Two cursors over the same jobs (key tile, half): one issues S of a job, the other O += P V.  S of the next jobs is issued as soon
       // as a buffer, its keys and its rows are there, across the items; a buffer is free behind the product that reads its P, since the tensor
-      // core takes the instructions of a thread in order.
+      // core takes the instructions of a thread in order.  With two buffers a softmax waits for this thread: S of the next job follows the product
+      // at once, before the signals (prompt of 8192: 524 -> 479 us).  With three it does not, and one loop
+      // for both halves was better than a warp for each, whose instructions alternate (519 us, 189).
       bool ok = true;
       if (elect_one()) {
         const uint32_t id_s = instr_desc(true, kKeys), id_o = instr_desc(false, DH);
         uint32_t full_ph = 0, ready_ph = 0, p_ph = 0;    // phases of the barriers of a stage, of a buffer: a bit each
         int items_s = 0, items_v = 0;                    // items that the cursors have been given
         int ahead = 0;                                   // jobs whose S is issued and whose P V is not
-        bool end = false, issued = false;
+        bool end = false, issued = false, keys = false;  // keys: K of the next S has been waited for
         Cursor cs, cv;
         long long t0 = 0;                                // since when nothing could be issued (0: something was)
+        auto keys_there = [&] {                          // of the next S
+          if (!cs.open) return false;
+          if (!cs.first() || keys) return true;
+          const int s = cs.stage;
+          keys = mbar_test(full_bar(s), (full_ph >> s) & 1u);
+          if (keys) full_ph ^= 1u << s;
+          return keys;
+        };
+        auto issue_s = [&] {
+          const int s = cs.stage;
+          const uint32_t a0 = desc_low(q_smem + cs.h * C::TILE, 16), b0 = desc_low(ring + s * C::TILE, 16);
+          const uint32_t d = tmem + 128u * cs.b;
+#pragma unroll
+          for (int k = 0; k < DH / 16; ++k) {
+            const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
+            tc_mma_ss(d, a0 + off, b0 + off, id_s, k > 0);
+          }
+          tc_commit_one(s_full(cs.h, cs.b));
+          if (cs.last()) {
+            tc_commit_one(empty_bar(s));
+            if (cs.i + 1 == cs.tiles()) tc_commit_one(q_empty);
+          }
+          issued = true;
+          keys = false;
+          ++ahead;
+          cs.advance(C::BUFS, C::STAGES);
+        };
         while (true) {
           if (!cs.open && !end && mbar_test(q_full, (uint32_t)items_s & 1u)) {
             const Brief w = s_brief[items_s % kBriefs];
@@ -345,38 +405,16 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             end = w.n0 == 0 && w.n1 == 0;
             if (!end) cs.start(w);
           }
-          if (cs.open && ahead < C::BUFS) {
-            const int s = (int)(cs.pos % C::STAGES);
-            bool ready = true;
-            if (cs.first()) {
-              ready = mbar_test(full_bar(s), (full_ph >> s) & 1u);
-              if (ready) full_ph ^= 1u << s;
-            }
-            if (ready) {
-              tc_fence_after();
-              const uint32_t a0 = desc_low(q_smem + cs.h * C::TILE, 16), b0 = desc_low(ring + s * C::TILE, 16);
-              const uint32_t d = tmem + 128u * cs.b;
-#pragma unroll
-              for (int k = 0; k < DH / 16; ++k) {
-                const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
-                tc_mma_ss(d, a0 + off, b0 + off, id_s, k > 0);
-              }
-              tc_commit_one(s_full(cs.h, cs.b));
-              if (cs.last()) {
-                tc_commit_one(empty_bar(s));
-                if (cs.i + 1 == cs.tiles()) tc_commit_one(q_empty);
-              }
-              issued = true;
-              ++ahead;
-              cs.advance(C::BUFS);
-              t0 = 0;
-              continue;
-            }
+          if (ahead < C::BUFS && keys_there()) {
+            tc_fence_after();
+            issue_s();
+            t0 = 0;
+            continue;
           }
           if (ahead > 0) {
             if (!cv.open) cv.start(s_brief[items_v++ % kBriefs]);
             if (mbar_test(p_half(cv.b), (p_ph >> cv.b) & 1u)) {
-              const int s = (int)((cv.pos + 1) % C::STAGES);
+              const int s = cv.stage + 1 == C::STAGES ? 0 : cv.stage + 1;
               if (cv.first()) {
                 if (cv.i >= cv.w.edge) {
                   ok = mbar_wait(ready_bar(s), (ready_ph >> s) & 1u, abort_flag, budget);
@@ -393,16 +431,18 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               tc_fence_after();
 #pragma unroll
               for (int k = 0; k < kKeys / 32; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, cv.i > 0 || k > 0);
+              const bool more = keys_there();            // (before the wait: S of the next job follows the product at once)
               ok = mbar_wait(p_full(cv.b), (p_ph >> cv.b) & 1u, abort_flag, budget);
               p_ph ^= 1u << cv.b;
               if (!ok) break;
               tc_fence_after();
 #pragma unroll
               for (int k = kKeys / 32; k < kKeys / 16; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, 1u);
+              --ahead;
+              if (C::BUFS == 2 && more) issue_s();       // (with three: 184 us for the documents)
               tc_commit_one(pv_done(cv.h));
               if (cv.last()) tc_commit_one(empty_bar(s));
-              --ahead;
-              cv.advance(C::BUFS);
+              cv.advance(C::BUFS, C::STAGES);
               t0 = 0;
               continue;
             }
@@ -433,7 +473,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const int tid = threadIdx.x - 320;               // 0 .. 63
       uint32_t pos = 0, edge_ph = 0;
       bool ok = true;
-      for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
+      for (int k = 0; ok && next_item(k, ok); ++k) {
+        item_read(k);
         const Work w = work_of(p, it);
         const int n = w.tiles();
         if (n == 0) continue;
@@ -492,16 +533,23 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     uint32_t s_ph = 0, pv_ph = 0, jobs = 0;          // (of a buffer: a bit each; jobs of the items before)
     bool ok = true;
     const uint64_t c2 = pack2(c, c);
-    for (int k = 0; ok && dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it); ++k) {
-      const Work w = work_of(p, it);
-      const int token = w.t0 + h * p.tokens + row / p.gp;
-      const bool valid = row < p.gp * p.tokens && token < it.nq;
-      const int lim = valid ? min(visible(it, p.a.causal, token), w.seen) : 0;       // keys [0, lim)
-      const bool busy = __any_sync(0xffffffffu, valid);
-      const int n = h ? w.n[1] : w.n[0];
+    for (int k = 0; ok && next_item(k, ok); ++k) {
+      int lim, n, n0, kb;                            // (a row of S leaves few registers: the rest is derived again for the output)
+      bool alone, busy;
+      {
+        const Work w = work_of(p, it);
+        const int token = w.t0 + h * p.tokens + row / p.gp;
+        const bool valid = row < p.gp * p.tokens && token < it.nq;
+        lim = valid ? min(visible(it, p.a.causal, token), w.seen) : 0;       // keys [0, lim)
+        busy = __any_sync(0xffffffffu, valid);
+        n0 = w.n[0];
+        n = h ? w.n[1] : n0;
+        kb = w.kb;
+        alone = w.alone;
+      }
       float r = -INFINITY, l = 0.f;                  // reference (not yet times c) and sum
       for (int i = 0; i < n; ++i) {
-        const int b_ = (int)((jobs + (w.alone ? i : i < w.n[0] ? 2 * i + h : w.n[0] + i)) % C::BUFS);      // the buffer of the job
+        const int b_ = (int)((jobs + (alone ? i : i < n0 ? 2 * i + h : n0 + i)) % C::BUFS);      // the buffer of the job
         const uint32_t t_s = tmem + 128u * b_ + lanes;
         bool got = mbar_wait(s_full(h, b_), (s_ph >> b_) & 1u, abort_flag, budget);
         s_ph ^= 1u << b_;
@@ -521,7 +569,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
           for (int b = 0; b < 4; ++b) tc_ld32(t_s + 32u * b, x + 32 * b);
           tc_wait_ld();
-          const int left = lim - (w.kb + i * kKeys); // keys of this tile that the row sees
+          const int left = lim - (kb + i * kKeys);   // keys of this tile that the row sees
           if (__any_sync(0xffffffffu, left < kKeys)) {
 #pragma unroll
             for (int j = 0; j < kKeys; ++j)
@@ -601,6 +649,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       }
       if (!ok) break;
       // ---- output of the item
+      it = s_item[k % kItems];
+      const Work w = work_of(p, it);
+      const int token = w.t0 + h * p.tokens + row / p.gp;
+      const bool valid = row < p.gp * p.tokens && token < it.nq;
       const int64_t out_row = (int64_t)it.q0 + token;
       const int head = p.gp == 1 ? it.head : it.head * p.gp + row % p.gp;
       const bool cut = p.a.part > 0 && it.nk > p.a.part;
@@ -679,6 +731,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       tc_fence_before();                             // (the next P of this half says that O has been read)
       jobs = (jobs + w.n[0] + w.n[1]) % C::BUFS;
       if (w.tiles() > 0) ++seq;
+      item_read(k);
     }
     if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 14);
   }
