@@ -502,6 +502,10 @@ sp_status sp_linear(const sp_mat* X, const sp_mat* W, const float* bias, int32_t
       return gemm_tc(T, N, K, 1.f, ta, tb, other ? 1.f : 0.f, o, y, false, status_dev, s, nullptr, -1.0, 0, nullptr, &epi);
     }
   }
+  if (X->dtype == SP_F32 && linear_few_rows_f32(T, K)) {
+    CU(linear_few_f32(T, N, K, Operand{X->ptr, X->dtype, X->ld, 1}, Operand{W->ptr, W->dtype, W->ld, 1}, epi, o, y, s));
+    return SP_OK;
+  }
   CU(linear_simt(T, N, K, Operand{X->ptr, X->dtype, X->ld, 1}, Operand{W->ptr, W->dtype, W->ld, 1}, epi, o, y, s));
   return SP_OK;
 }

@@ -361,11 +361,18 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
 // lin: C = act(A B + bias), then (+ or *) Cin when beta is not 0 (alpha = 1, beta = 0 or 1; neither batched nor lower_only).
 bool gemm_tc_supported(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand B);
 // The same for few rows (sp_linear_few.cu, up to 32), layouts as gemm_tc_supported, both K-major.  Where it is the faster one: up to 16
-// rows, and up to 32 where the tiles of 128 outputs leave many SM pairs idle.  Tiles / this, us: 4096 -> 4096 16 rows 32.8 / 16.4, 32 rows
-// 34.8 / 20.5, 48 rows 32.8 / 30.7; 4096 -> 16384 16 rows 46 / 41, 32 rows 45 / 63; 768 -> 1536 32 rows 16.4 / 10.2.
+// rows, and up to 32 where the tiles of 128 outputs leave many SM pairs idle.  Tiles / this, us: 4096 -> 4096 16 rows 32.8 / 14.3, 32 rows
+// 34.8 / 16.4; 4096 -> 16384 16 rows 46 / 35, 32 rows 45 / 63; 768 -> 1536 32 rows 16.4 / 8.2.
 inline bool linear_few_rows(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 8192); }
 cudaError_t linear_few(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand W, const LinearEpi& epi, Operand other, OutOperand C,
                        cudaStream_t stream);
+
+// fp32, any layout with K-major rows.  The general form has 32 or 64 rows x 64 outputs a block and all of K, the few-row form 32 x 16 with K over its
+// warps: faster while blocks are few.  General / this, us: 4096 -> 4096 1 row 213 / 23, 32 rows 207 / 51, 128 rows 190 / 149, 512 rows
+// 739 / 545, 2048 rows 2009 / 2121; 768 -> 1536 1 row 45 / 10, 512 rows 68 / 51; 401 -> 2053 128 rows 27 / 20, 256 rows 28 / 33.
+inline bool linear_few_rows_f32(int64_t M, int64_t K) { return M <= 128 || (M <= 512 && K >= 512); }
+cudaError_t linear_few_f32(int64_t M, int64_t N, int64_t K, Operand A, Operand W, const LinearEpi& epi, Operand other, OutOperand C,
+                           cudaStream_t stream);
 
 struct SolveAssist;
 // fp64 factorisation and solves (sp_linalg.cu), block columns of kCholNB.

@@ -177,3 +177,27 @@ def test_a_single_row_has_no_pitch(dtype, T, N):
     assert api.lib().sp_linear(api.C.byref(X), api.C.byref(W), None, 0, None, 0, api.C.byref(Y), None,
                                torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("T,K,N", [(1, 5, 1), (8, 16, 17), (9, 512, 33), (16, 2047, 100), (33, 700, 65), (64, 4096, 48), (129, 512, 96),
+                                   (512, 530, 40), (513, 530, 40), (200, 511, 70)])
+def test_few_rows_in_fp32(T, K, N):
+    """Every group of rows, whole and ragged pieces of K, on both sides of the choice of form."""
+    for wide in (True, False):
+        x, w, o, b = inputs(T, K, N, torch.float32, seed=T, wide=wide)
+        check(x, w)
+        check(x, w, bias=b, act=api.SP_LINEAR_GELU, other=o, combine=api.SP_COMBINE_MUL)
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_infinities_and_subnormal_values_in_fp32(T):
+    x, w, _, _ = inputs(T, 600, 20, torch.float32)
+    tiny = 2.0 ** -140
+    x.zero_()
+    x[:, 3], x[:, 599] = tiny, 1.0
+    w[:, 3], w[:, 599] = 2.0 ** 20, 0.0
+    assert (api.sp_linear(x, w) == 2.0 ** -120).all()                # exact: one product, its sum in fp64
+    w[5, 599], w[6, 599], w[7, 3] = math.inf, -math.inf, math.nan
+    y = api.sp_linear(x, w)
+    assert (y[:, 5] == math.inf).all() and (y[:, 6] == -math.inf).all() and torch.isnan(y[:, 7]).all()
+    assert (y[:, :5] == 2.0 ** -120).all() and (y[:, 8:] == 2.0 ** -120).all()
