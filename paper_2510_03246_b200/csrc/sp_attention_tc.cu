@@ -173,7 +173,7 @@ __device__ __forceinline__ Work work_of(const TcAttnParams& p, const AttnItem& i
   return w;
 }
 
-// The k-th item of this CTA.  Items of a sequence get lighter; every other round is dealt backwards, so that no CTA always has the
+// The k-th item of this CTA.  Items get lighter (of 32 sequences); every other round is dealt backwards, so that no CTA always has the
 // heavier ones (one prompt of 8192: busy cycles of the SMs from 0.86 to 1.14 of their mean without).
 __device__ __forceinline__ int64_t item_of(int k) {
   return (int64_t)k * gridDim.x + (k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);

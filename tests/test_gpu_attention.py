@@ -320,3 +320,24 @@ def test_a_single_row_has_no_pitch(dtype):
                                c.data_ptr(), c.data_ptr(), None, 1, 2, 2, 1, 0.125)
     assert api.lib().sp_attention(api.C.byref(args), None, None, 0, torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(O, V)                                        # the one probability is 1
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_many_sequences_of_any_length(dtype, causal, dh):
+    """More than 32 of them, of very different lengths, some empty: every row is written once, by its own keys."""
+    q = [(i * 37) % 151 for i in range(75)]
+    k = [(i * 53) % 211 for i in range(75)]
+    q[40], k[40], q[64], k[64] = 700, 900, 0, 300
+    Q, K, V = inputs(sum(q), sum(k), 4, 2, dh, dtype)
+    check(Q, K, V, q, k, 4, 2, causal)
+
+
+def test_many_tiles_of_many_heads():
+    """Several rounds of work for every SM, tiles of one and of two halves in turn."""
+    q = [65, 700, 1, 129, 33, 1025, 64, 300, 97, 16] * 2
+    Q, K, V = inputs(sum(q), sum(q), 24, 12, 128, torch.bfloat16)
+    check(Q, K, V, q, q, 24, 12)
+    Q, K, V = inputs(sum(q), sum(q), 24, 12, 64, torch.bfloat16)
+    check(Q, K, V, q, q, 24, 12)
