@@ -290,8 +290,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   AttnItem it;
   int seq = 0;                // number of the item among those of this CTA that have keys
   // the k-th item of this CTA, for the softmax and edge warps; false behind the last one, or when a wait ran out
-  auto next_item = [&](int k, bool& ok) {
-    ok = __all_sync(0xffffffffu, mbar_wait(item_full(k), (uint32_t)(k / kItems) & 1u, abort_flag, budget));
+  auto next_item = [&](int k, bool& ok, long long patience) {
+    ok = __all_sync(0xffffffffu, mbar_wait(item_full(k), (uint32_t)(k / kItems) & 1u, abort_flag, patience));
     if (!ok) return false;
     it = s_item[k % kItems];
     return it.tile >= 0;
@@ -473,15 +473,17 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const int tid = threadIdx.x - 320;               // 0 .. 63
       uint32_t pos = 0, edge_ph = 0;
       bool ok = true;
-      for (int k = 0; ok && next_item(k, ok); ++k) {
+      long long patience = budget;                     // (these warps wait for as long as the others work on an item)
+      for (int k = 0; ok && next_item(k, ok, patience); ++k) {
         item_read(k);
         const Work w = work_of(p, it);
         const int n = w.tiles();
         if (n == 0) continue;
+        patience = budget + 20000ll * n;
         for (int i = 0; i < n && ok; ++i, pos += 2) {
           if (!w.edge(i)) continue;
           const int s = (int)((pos + 1) % C::STAGES);
-          const bool got = mbar_wait(edge_bar(s), (edge_ph >> s) & 1u, abort_flag, budget);
+          const bool got = mbar_wait(edge_bar(s), (edge_ph >> s) & 1u, abort_flag, patience);
           edge_ph ^= 1u << s;
           ok = __all_sync(0xffffffffu, got);
           if (!ok) break;
@@ -533,7 +535,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     uint32_t s_ph = 0, pv_ph = 0, jobs = 0;          // (of a buffer: a bit each; jobs of the items before)
     bool ok = true;
     const uint64_t c2 = pack2(c, c);
-    for (int k = 0; ok && next_item(k, ok); ++k) {
+    int waits = 0;                                   // key tiles of the item before: half 1 waits for as long as half 0 works on one alone
+    for (int k = 0; ok && next_item(k, ok, budget + 20000ll * waits); ++k) {
       int lim, n, n0, kb;                            // (a row of S leaves few registers: the rest is derived again for the output)
       bool alone, busy;
       {
@@ -730,7 +733,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       }
       tc_fence_before();                             // (the next P of this half says that O has been read)
       jobs = (jobs + w.n[0] + w.n[1]) % C::BUFS;
-      if (w.tiles() > 0) ++seq;
+      waits = w.tiles();
+      if (waits > 0) ++seq;
       item_read(k);
     }
     if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 14);
