@@ -341,3 +341,21 @@ def test_many_tiles_of_many_heads():
     check(Q, K, V, q, q, 24, 12)
     Q, K, V = inputs(sum(q), sum(q), 24, 12, 64, torch.bfloat16)
     check(Q, K, V, q, q, 24, 12)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_calls_side_by_side_on_two_streams(dtype):
+    """Each has a workspace of its own: the bits of a call by itself."""
+    q, k = [1, 1, 1], [5000, 3000, 700]
+    sets = [inputs(3, 8700, 8, 2, 64, dtype, seed=i) for i in range(2)]
+    cq, ck = cu(q), cu(k)
+    want = [api.sp_attention(*t, cq, ck, 8, 2)[0] for t in sets]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for stream, t in zip(streams, sets):
+            with torch.cuda.stream(stream):
+                got.append(api.sp_attention(*t, cq, ck, 8, 2)[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -201,3 +201,18 @@ def test_infinities_and_subnormal_values_in_fp32(T):
     y = api.sp_linear(x, w)
     assert (y[:, 5] == math.inf).all() and (y[:, 6] == -math.inf).all() and torch.isnan(y[:, 7]).all()
     assert (y[:, :5] == 2.0 ** -120).all() and (y[:, 8:] == 2.0 ** -120).all()
+
+
+@pytest.mark.parametrize("T", [1, 20, 600])
+def test_captured_calls_in_fp32(T):
+    x, w, o, b = inputs(T, 300, 90, torch.float32)
+    want = check(x, w, bias=b, act=api.SP_LINEAR_RELU, other=o)
+    out = torch.zeros(T, 90, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        api.sp_linear(x, w, bias=b, act=api.SP_LINEAR_RELU, other=o, out=out)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
