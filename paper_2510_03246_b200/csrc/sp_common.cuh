@@ -360,10 +360,11 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
                   const TcBatch* batch = nullptr, const LinearEpi* lin = nullptr);
 // lin: C = act(A B + bias), then (+ or *) Cin when beta is not 0 (alpha = 1, beta = 0 or 1; neither batched nor lower_only).
 bool gemm_tc_supported(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand B);
-// The same for few rows (sp_linear_few.cu, up to 32), layouts as gemm_tc_supported, both K-major.  Where it is the faster one: up to 16
-// rows, and up to 32 where the tiles of 128 outputs leave many SM pairs idle.  Tiles / this, us: 4096 -> 4096 16 rows 32.8 / 14.3, 32 rows
-// 34.8 / 16.4; 4096 -> 16384 16 rows 46 / 35, 32 rows 45 / 63; 768 -> 1536 32 rows 16.4 / 8.2.
-inline bool linear_few_rows(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 8192); }
+// The same for few rows (sp_linear_few.cu), layouts as gemm_tc_supported, both K-major.  Where it is the faster one: up to 16 rows, and up to
+// 192 while rows times outputs are at most 2^18 (a block has 32 x 16 of them and all of K; the tiles' time is that of one or two tiles of 128 x 256).
+// Tiles / this, us: 4096 -> 4096 16 rows 33 / 14, 64 rows 35 / 29, 96 rows 35 / 38; 1024 -> 8192 32 rows 18 / 14, 48 rows 18 / 21; 4096 -> 16384 16
+// rows 46 / 35, 32 rows 45 / 49; 2048 -> 2048 128 rows 23 / 18, 192 rows 23 / 25; 768 -> 1536 192 rows 16 / 14.
+inline bool linear_few_rows(int64_t M, int64_t N) { return M <= 16 || (M <= 192 && M * N <= (1 << 18)); }
 cudaError_t linear_few(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand W, const LinearEpi& epi, Operand other, OutOperand C,
                        cudaStream_t stream);
 

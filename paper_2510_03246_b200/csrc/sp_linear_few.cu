@@ -1,4 +1,4 @@
-// sp_linear for few rows, up to 32 in bf16, some hundred in fp32: Y = act(X W^T + bias) (+|*) other, bound by reading W once.
+// sp_linear for few rows, up to some hundred: Y = act(X W^T + bias) (+|*) other, bound by reading W once.
 //
 // A 128-row tile of the tensor-core product would be nearly empty, and a call has few of them: its time is that of a few SMs reading W
 // (16 x 768 -> 1536 took 32 us from cold caches).  Here a block takes 16 outputs and all of K, its eight warps every eighth piece of 32
@@ -51,13 +51,13 @@ __global__ void __launch_bounds__(kWarps * 32, NT > 1 ? 2 : 3) linear_few_kernel
   constexpr int kUnroll = NT > 2 ? 2 : 4;
   __shared__ float s_acc[kWarps][NT * 8][kOut + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g4 = lane >> 2, t4 = lane & 3;
-  const int64_t o0 = (int64_t)blockIdx.x * kOut;
+  const int64_t o0 = (int64_t)blockIdx.x * kOut, t0 = (int64_t)blockIdx.y * (NT * 8);
   // (rows behind the last one: any values, not stored)
   const __nv_bfloat16* w0 = p.w + min(o0 + g4, p.N - 1) * p.ldw;
   const __nv_bfloat16* w1 = p.w + min(o0 + g4 + 8, p.N - 1) * p.ldw;
   const __nv_bfloat16* xr[NT];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) xr[n] = p.x + min((int64_t)(8 * n + g4), p.T - 1) * p.ldx;
+  for (int n = 0; n < NT; ++n) xr[n] = p.x + min(t0 + 8 * n + g4, p.T - 1) * p.ldx;
   float acc[NT][4];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -98,12 +98,11 @@ __global__ void __launch_bounds__(kWarps * 32, NT > 1 ? 2 : 3) linear_few_kernel
     for (int i = 0; i < 4; ++i) s_acc[warp][8 * n + 2 * t4 + (i & 1)][g4 + 8 * (i >> 1)] = acc[n][i];
   __syncthreads();
   for (int e = threadIdx.x; e < NT * 8 * kOut; e += kWarps * 32) {
-    const int row = e / kOut, out = e % kOut;
-    const int64_t j = o0 + out;
+    const int64_t row = t0 + e / kOut, j = o0 + e % kOut;
     if (row >= p.T || j >= p.N) continue;
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) v += s_acc[w][row][out];
+    for (int w = 0; w < kWarps; ++w) v += s_acc[w][e / kOut][e % kOut];
     v = linear_act(p.epi.bias ? v + p.epi.bias[j] : v, p.epi.act);
     if (p.y_f32) {
       if (p.other) v = linear_combine(v, reinterpret_cast<const float*>(p.other)[row * p.ldo + j], p.epi.combine);
@@ -256,7 +255,7 @@ cudaError_t linear_few(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand W
   p.y_f32 = C.dtype == SP_F32 ? 1 : 0;
   count_launch();
   ProfScope prof(PK_GEMM_SIMT, 2.0 * (double)M * (double)N * (double)K, 0.0, stream);
-  const dim3 grid((unsigned)ceil_div(N, (int64_t)kOut));
+  const dim3 grid((unsigned)ceil_div(N, (int64_t)kOut), (unsigned)ceil_div(M, (int64_t)32));
   return M <= 8 ? launch(linear_few_kernel<1>, grid, dim3(kWarps * 32), 0, stream, p)
        : M <= 16 ? launch(linear_few_kernel<2>, grid, dim3(kWarps * 32), 0, stream, p)
                 : launch(linear_few_kernel<4>, grid, dim3(kWarps * 32), 0, stream, p);

@@ -216,3 +216,23 @@ def test_captured_calls_in_fp32(T):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("T,K,N", [(33, 768, 1536), (64, 1000, 4096), (65, 64, 4033), (192, 333, 1365), (192, 64, 1366), (193, 777, 100)])
+def test_bf16_on_both_sides_of_the_choice_of_form(T, K, N):
+    x, w, o, b = inputs(T, K, N, torch.bfloat16, seed=N)
+    check(x, w)
+    check(x, w, bias=b, act=api.SP_LINEAR_SILU, other=o, combine=api.SP_COMBINE_MUL)
+    y = check(x, w, bias=b, act=api.SP_LINEAR_GELU, out_dtype=torch.float32)
+    assert y.dtype == torch.float32
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_tiles_of_many_rows(dtype):
+    """What the tests above ask of few rows, of the general forms: in place, odd pitches, what stands beside ragged rows."""
+    test_other_in_place(dtype, 600, api.SP_COMBINE_ADD)
+    test_other_in_place(dtype, 600, api.SP_COMBINE_MUL)
+    test_pitches_and_what_lies_beside_the_result(dtype, 600)
+    test_values_beside_a_ragged_width_do_not_enter(dtype, 600)
+    test_fp32_result_of_bf16_operands(api.SP_LINEAR_GELU, 600)
+    test_infinities_and_nan(600)
