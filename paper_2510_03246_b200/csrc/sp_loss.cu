@@ -35,10 +35,10 @@ template <> struct Vec<float> {
   static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
   }
-  // largest value of n vectors (NaN passed over)
+  // largest value of n vectors, NaN passed over; of nothing but NaN: NaN, which is not to be taken for the number -infinity
   template <int n>
   static __device__ __forceinline__ float largest(const uint4 (&q)[n]) {
-    float m = -INFINITY;
+    float m = __uint_as_float(q[0].x);
 #pragma unroll
     for (int i = 0; i < n; ++i) {
       float x[4];
