@@ -557,7 +557,8 @@ sp_status sp_linear(const sp_mat* X, const sp_mat* W, const float* bias, int32_t
  * A logit of -infinity has p = 0 and adds nothing to the entropy; a row of nothing else has lse = logp = -infinity and
  * entropy 0 (alternatives: indices 0, 1, ... and -infinity).  A NaN or +infinity among the logits makes logp, lse and entropy NaN.
  * sp_token_logprobs_grad: dlogits = scale (g_logp (1{v = target} - p) - g_entropy p (log p + entropy)), the gradient of
- * sum_t g_logp logp + g_entropy entropy, from the lse and entropy of the forward call (entropy is read only with g_entropy).
+ * sum_t g_logp logp + g_entropy entropy, from the lse and entropy of the forward call (entropy is read only with g_entropy).  In rows whose lse is
+ * beyond +-1024 or not finite, where fp32 does not hold it exactly enough for p, p is formed from the row's logits alone.
  * g_logp, g_entropy: fp32 [T], either may be NULL (zero), g_logp needs targets.  A row that is not scored has no g_logp part;
  * a target >= V is taken as not scored; a row of nothing but -infinity has gradient 0.  dlogits: [T, V], dtype of logits, it
  * may be logits itself (same pointer and ld).

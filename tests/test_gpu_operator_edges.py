@@ -10,6 +10,7 @@ from paper_2510_03246_b200 import api
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 DTYPES = [torch.bfloat16, torch.float32]
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
 
 
 def best(x, n):
@@ -43,3 +44,87 @@ def test_alternatives_of_rows_of_few_numbers(dtype, V, n_alts):
                                        torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(ids.long(), best(x, n_alts))
     assert torch.isnan(alt).all()                                  # a row with a NaN has no log probabilities
+
+
+def far_rows(V, dtype, seed=0):
+    """Rows whose lse is far from zero, beside ordinary ones."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    n = torch.randn(9, V, generator=g, device=DEV)
+    low = torch.finfo(dtype).min
+    x = n.to(dtype)
+    x[1] = low                                                     # a mask that leaves nothing
+    x[2] = low
+    x[2, V // 2:] = -math.inf
+    x[3] = (300 * n[3] + 5e4).to(dtype)
+    x[4] = (n[4] - 3000).to(dtype)
+    x[5] = (1e30 * n[5]).to(dtype)
+    x[6] = torch.finfo(dtype).max
+    x[7] = -math.inf                                               # nothing at all
+    x[8] = (-1e37 * n[8].abs()).to(dtype)
+    x[8, ::2] = low
+    return x, torch.randint(0, (V + 1) // 2, (9,), generator=g, device=DEV)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [1.0, 0.5, 1.6])
+@pytest.mark.parametrize("V", [1, 7, 1000, 4099, 50257])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_gradient_of_rows_far_from_zero(dtype, scale, V, in_place):
+    """fp32 does not hold the lse of such rows as exactly as p = e^(z - lse) needs it (in a row of nothing but the type's lowest value, log V
+    is lost beside it, and with a scale above 1 it overflows).
+
+    Tolerance: with the row's largest logit r, z - z_r is formed from a difference and a scale, each rounded once (with log2(e) once more), and
+    the product: 4 half steps of 2^-24 of |z - z_r|; the log of the sum adds one per value of a thread (V / 256) and 16 for the joins;
+    the exponential 2^-21.  That is e, the error of log p; p is off by a factor within 1 +- 1.1 e, p log p by p (e + 1.1 e |log p|), and
+    the result is rounded once."""
+    x, t = far_rows(V, dtype)
+    r = api.sp_token_logprobs(x, t, scale=scale)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    gl, gh = torch.randn(9, generator=g, device=DEV), torch.randn(9, generator=g, device=DEV)
+    z = x.double() * scale
+    empty = (x == -math.inf).all(1)
+    zr = torch.where(empty, 0.0, z.amax(1))[:, None]
+    lp = torch.where(empty[:, None], -math.inf, torch.log_softmax(z, 1))
+    p = lp.exp()
+    plp = torch.where(p > 0, p * lp, 0.0)
+    one = torch.zeros_like(p)
+    one[torch.arange(9, device=DEV), t] = 1.0
+    gap = torch.where(p > 0, (z - zr).abs(), 0.0)
+    e = 2.0 ** -22 * gap + 2.0 ** -24 * (V / 256 + 16) + 2.0 ** -21
+    e = torch.where(r.lse.abs()[:, None] < 1024, e + 2.0 ** -24 * 6 * torch.where(p > 0, z.abs() + lp.abs(), 0.0), e)     # from the lse as given
+    for ent in (False, True):
+        buf = x.clone()
+        d = api.sp_token_logprobs_grad(buf, t, r.lse, gl, entropy=r.entropy if ent else None, g_entropy=gh if ent else None, scale=scale,
+                                       out=buf if in_place else None)
+        a, h = gl.double()[:, None], (gh.double()[:, None] if ent else torch.zeros(9, 1, dtype=torch.float64, device=DEV))
+        H = r.entropy.double()[:, None]
+        want = scale * (a * (one - p) - h * (plp + p * H))
+        want[empty] = 0.0
+        tol = scale * (1.1 * e * p * a.abs() + h.abs() * (p * e + 1.1 * e * (plp.abs() + p * H)))
+        tol = tol + 2.0 ** -22 * scale * (a.abs() * (one + p) + h.abs() * (plp.abs() + p * H)) + HALF[dtype] * want.abs() + 1e-37
+        # a p below 2^-126 becomes 0: p |log p| rises with p there, so at most 2^-126 times 126 log 2 < 88 is lost (4e-37 where it was first seen)
+        tol = tol + 2.0 ** -126 * scale * (a.abs() + h.abs() * (88 + H))
+        err = (d.double() - want).abs()
+        assert torch.isfinite(d).all() and (err <= tol).all(), (float((err / tol).max()), (err / tol).argmax().item() // V)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_gradient_of_far_rows_with_pitches_and_nan(dtype):
+    V = 1001
+    x, t = far_rows(V, dtype)
+    r = api.sp_token_logprobs(x, t)
+    gl = torch.ones(9, device=DEV)
+    want = api.sp_token_logprobs_grad(x, t, r.lse, gl)
+    src = torch.full((9, 1200), math.nan, dtype=dtype, device=DEV)
+    src[:, 5:5 + V] = x
+    for start in (5, 3):                                           # rows of the same phase, and of another one
+        out = torch.full((9, 1200), 7.0, dtype=dtype, device=DEV)
+        d = api.sp_token_logprobs_grad(src[:, 5:5 + V], t, r.lse, gl, out=out[:, start:start + V])
+        # (the row's sum is taken in the same order, wherever it starts)
+        assert torch.equal(d, want)
+        assert (out[:, :start] == 7).all() and (out[:, start + V:] == 7).all()
+    x[3, 17] = math.nan
+    x[1, 17] = math.inf
+    r = api.sp_token_logprobs(x, t)
+    d = api.sp_token_logprobs_grad(x, t, r.lse, gl)
+    assert torch.isnan(d[[1, 3]]).all() and torch.equal(d[[0, 2, 4, 5, 6, 7, 8]], want[[0, 2, 4, 5, 6, 7, 8]])
