@@ -222,13 +222,15 @@ def attention_head_outputs(X: torch.Tensor, Wqkv: torch.Tensor, cu: torch.Tensor
     """Concatenated head outputs H [N, n_heads * d_head] of an attention module over packed sequences (cu: int32 offsets [n_seq + 1]
     on the device, X [N, d] token-major): the input of its output projection, and what prune_attention_heads takes.
     Wqkv [(n_heads + 2 n_kv_heads) d_head, d]: the rows of W_Q, W_K, W_V one below the other, in X's dtype; bias fp32 or None.
+    Rows of X before the first and behind the last sequence (padding; whatever stands there) have zero rows in H: nothing in sums over tokens.
     Two library calls, and no probabilities in memory (sp_mha_init, which the auxiliary variables of Algorithm 2 start from, keeps
     n_seq * n_heads * T * T of them)."""
     n_kv = n_heads if n_kv_heads is None else n_kv_heads
     d_head = Wqkv.shape[0] // (n_heads + 2 * n_kv)
     qkv = api.sp_linear(X, Wqkv, bias=bias)
     q, k = n_heads * d_head, n_kv * d_head
-    H, _ = api.sp_attention(qkv[:, :q], qkv[:, q:q + k], qkv[:, q + k:q + 2 * k], cu, cu, n_heads, n_kv, causal=causal)
+    H = torch.zeros(X.shape[0], q, dtype=X.dtype, device=X.device)
+    api.sp_attention(qkv[:, :q], qkv[:, q:q + k], qkv[:, q + k:q + 2 * k], cu, cu, n_heads, n_kv, causal=causal, out=H)
     return H
 
 

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from paper_2510_03246_b200 import api
+from paper_2510_03246_b200 import api, pipeline
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -128,3 +128,26 @@ def test_gradient_of_far_rows_with_pitches_and_nan(dtype):
     r = api.sp_token_logprobs(x, t)
     d = api.sp_token_logprobs_grad(x, t, r.lse, gl)
     assert torch.isnan(d[[1, 3]]).all() and torch.equal(d[[0, 2, 4, 5, 6, 7, 8]], want[[0, 2, 4, 5, 6, 7, 8]])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_padded_calibration_batch(dtype):
+    """Rows before the first and behind the last sequence: no head outputs, and no part in the scores, the mask and the weights."""
+    g = torch.Generator(device=DEV).manual_seed(4)
+    n, d, heads, lead, tail = 300, 128, 4, 9, 55
+    X = torch.randn(n, d, generator=g, device=DEV).to(dtype)
+    W = (torch.randn(3 * d, d, generator=g, device=DEV) / math.sqrt(d)).to(dtype)
+    Wo = torch.randn(d, d, generator=g, device=DEV) / math.sqrt(d)
+    padded = torch.full((lead + n + tail, d), math.nan, dtype=dtype, device=DEV)
+    padded[lead:lead + n] = X
+    cu = lambda o: torch.tensor([o, o + 120, o + n], dtype=torch.int32, device=DEV)
+    hold = [torch.full((lead + n + tail, d), math.nan, dtype=dtype, device=DEV) for _ in range(4)]      # what the allocator gives out next
+    del hold
+    H = pipeline.attention_head_outputs(padded, W, cu(lead), heads)
+    alone = pipeline.attention_head_outputs(X, W, cu(0), heads)
+    assert torch.equal(H[lead:lead + n], alone) and (H[:lead] == 0).all() and (H[lead + n:] == 0).all()
+    a = pipeline.prune_attention_module(X, W, Wo, cu(0), heads, 2)
+    b = pipeline.prune_attention_module(padded, W, Wo, cu(lead), heads, 2)
+    assert torch.equal(a[0], b[0]) and torch.isfinite(b[1]).all() and torch.isfinite(b[2]).all()
+    # sums of the same n products of storage type in another order: n 2^-23 of their magnitudes, which the squares of the scores equal
+    assert ((a[2] - b[2]).abs() <= 2 * n * 2.0 ** -23 * a[2].abs()).all()

@@ -1,0 +1,79 @@
+"""What the layer-forward and scoring functions of the pipeline do on the host, with the library's calls replaced by stand-ins: no GPU."""
+import math
+
+import pytest
+import torch
+
+from paper_2510_03246_b200 import api, pipeline
+
+D, HEADS = 8, 2
+
+
+class Calls:
+    """Stand-ins that record their status words; the call named `late` reports a wait that ran out."""
+
+    def __init__(self, monkeypatch, late=None):
+        self.late, self.seen = late, []
+        for name in ("sp_linear", "sp_attention", "sp_token_logprobs", "sp_token_logprobs_grad", "sp_gemm", "sp_gram_accumulate",
+                     "sp_symmetrize", "sp_struct_scores", "sp_apply_mask", "sp_linear_refit"):
+            monkeypatch.setattr(api, name, getattr(self, name))
+        monkeypatch.setattr(api, "new_status", lambda device="cpu": torch.zeros(4, dtype=torch.int32, device=device))
+
+    def note(self, name, status):
+        self.seen.append((name, status))
+        if name == self.late and status is not None:
+            status[0], status[1] = 7, 3
+
+    def sp_linear(self, X, W, bias=None, act=0, other=None, combine=0, out=None, out_dtype=None, status=None):
+        self.note("sp_linear", status)
+        return torch.zeros(X.shape[0], W.shape[0], dtype=X.dtype) if out is None else out
+
+    def sp_attention(self, Q, K, V, cu_q, cu_k, n_heads, n_kv_heads=None, causal=True, scale=None, out=None, lse=None, want_lse=False,
+                     ws=None, status=None):
+        self.note("sp_attention", status)
+        out = torch.full_like(Q, math.nan) if out is None else out
+        out[int(cu_q[0]):int(cu_q[-1])] = 1.0                      # rows of the sequences, and no others
+        return out, lse
+
+    def sp_token_logprobs(self, logits, targets=None, n_alts=0, scale=1.0, want_entropy=True, status=None):
+        self.note("sp_token_logprobs", status)
+        z = torch.zeros(logits.shape[0])
+        return api.TokenLogprobs(z, z, None, None, None)
+
+    def sp_token_logprobs_grad(self, logits, targets, lse, g_logp, entropy=None, g_entropy=None, scale=1.0, out=None):
+        return out
+
+    def sp_gemm(self, A, B, C_, status=None, **kw):
+        self.note("sp_gemm", status)
+
+    def sp_gram_accumulate(self, Xc, Yc, G, R=None, rowstats=None, status=None, ws=None):
+        self.note("sp_gram_accumulate", status)
+
+    def sp_symmetrize(self, G):
+        pass
+
+    def sp_struct_scores(self, kind, n_units, *a, **kw):
+        return torch.zeros(n_units), None, None
+
+    def sp_apply_mask(self, scores, k, **kw):
+        return torch.ones(scores.numel(), dtype=torch.uint8), None, None
+
+    def sp_linear_refit(self, R, G, mask, k_keep, rho, status=None, **kw):
+        self.note("sp_linear_refit", status)
+        return R
+
+
+def tensors():
+    return dict(X=torch.zeros(6, D), Wqkv=torch.zeros(3 * D, D), W_O=torch.zeros(D, D), cu=torch.tensor([0, 4, 6], dtype=torch.int32))
+
+
+def head_outputs(t, **kw):
+    return pipeline.attention_head_outputs(t["X"], t["Wqkv"], t["cu"], HEADS, **kw)
+
+
+def test_head_outputs_of_rows_outside_the_sequences_are_zero(monkeypatch):
+    Calls(monkeypatch)
+    t = tensors()
+    t["cu"] = torch.tensor([1, 3, 5], dtype=torch.int32)
+    H = head_outputs(t)
+    assert H.shape == (6, D) and (H[1:5] == 1).all() and (H[0] == 0).all() and (H[5] == 0).all()
