@@ -22,17 +22,19 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// 8 values of a row from k on, zero from K on (what stands there, to align the rows, is no part of the product)
+// 8 values of a row from k on, zero from K on.  A piece that K cuts is read value by value: what stands behind the last value of a matrix may not be
+// the caller's.
 __device__ __forceinline__ uint4 row_piece(const __nv_bfloat16* row, int64_t k, int64_t K, bool stream) {
-  if (k >= K) return make_uint4(0u, 0u, 0u, 0u);
-  const uint4* at = reinterpret_cast<const uint4*>(row + k);
-  uint4 v = stream ? __ldcs(at) : *at;
-  if (k + 8 > K) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] &= (k + 2 * i < K ? 0xffffu : 0u) | (k + 2 * i + 1 < K ? 0xffff0000u : 0u);
+  if (k + 8 <= K) {
+    const uint4* at = reinterpret_cast<const uint4*>(row + k);
+    return stream ? __ldcs(at) : *at;
   }
-  return v;
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+  const uint16_t* bits = reinterpret_cast<const uint16_t*>(row);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (k + i < K) w[i / 2] |= (uint32_t)bits[k + i] << (16 * (i & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 struct FewParams {
@@ -129,25 +131,18 @@ __device__ __forceinline__ void dmma_16x8x8(double (&d)[4], double a0, double a1
       : "+d"(d[0]), "+d"(d[1]), "+d"(d[2]), "+d"(d[3])
       : "d"(a0), "d"(a1), "d"(a2), "d"(a3), "d"(b0), "d"(b1));
 }
-// 4 values of a row from k on, zero from K on; VEC: rows start on 16 bytes
+// the same for 4 values of fp32; VEC: rows start on 16 bytes
 template <bool VEC>
 __device__ __forceinline__ float4 row_piece(const float* row, int64_t k, int64_t K, bool stream) {
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (k >= K) return v;
-  if (VEC) {
+  if (VEC && k + 4 <= K) {
     const float4* at = reinterpret_cast<const float4*>(row + k);
-    v = stream ? __ldcs(at) : *at;
-    if (k + 4 > K) {                   // (a branch, so that nothing else waits for the value here)
-      if (k + 1 >= K) v.y = 0.f;
-      if (k + 2 >= K) v.z = 0.f;
-      v.w = 0.f;
-    }
-  } else {
-    v.x = row[k];
-    if (k + 1 < K) v.y = row[k + 1];
-    if (k + 2 < K) v.z = row[k + 2];
-    if (k + 3 < K) v.w = row[k + 3];
+    return stream ? __ldcs(at) : *at;
   }
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (k < K) v.x = row[k];
+  if (k + 1 < K) v.y = row[k + 1];
+  if (k + 2 < K) v.z = row[k + 2];
+  if (k + 3 < K) v.w = row[k + 3];
   return v;
 }
 

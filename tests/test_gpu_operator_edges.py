@@ -151,3 +151,17 @@ def test_a_padded_calibration_batch(dtype):
     assert torch.equal(a[0], b[0]) and torch.isfinite(b[1]).all() and torch.isfinite(b[2]).all()
     # sums of the same n products of storage type in another order: n 2^-23 of their magnitudes, which the squares of the scores equal
     assert ((a[2] - b[2]).abs() <= 2 * n * 2.0 ** -23 * a[2].abs()).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [1, 5, 77, 401, 777])
+def test_one_row_that_ends_with_its_storage(dtype, K):
+    """A single row has no pitch: what stands behind its K values belongs to somebody else."""
+    g = torch.Generator(device=DEV).manual_seed(K)
+    for T, N in ((1, 300), (1, 1), (7, 1)):
+        x = torch.randn(T, (K + 7) // 8 * 8, generator=g, device=DEV).to(dtype)[:, :K] if T > 1 else torch.randn(1, K, generator=g, device=DEV).to(dtype)
+        w = torch.randn(N, (K + 7) // 8 * 8, generator=g, device=DEV).to(dtype)[:, :K] if N > 1 else torch.randn(1, K, generator=g, device=DEV).to(dtype)
+        y = api.sp_linear(x, w, out_dtype=torch.float32)
+        want = x.double() @ w.double().T
+        tol = (x.double().abs() @ w.double().abs().T) * K * 2.0 ** (-23 if dtype == torch.bfloat16 else -52) + 2.0 ** -23 * want.abs() + 1e-30
+        assert ((y.double() - want).abs() <= tol).all()

@@ -39,3 +39,16 @@ def test_flags_acquired_by_other_lanes_are_ordered_before_the_loads():
     wait = text[text.index("auto wait_tiles"):text.index("uint32_t kl = kc;")]
     after = wait[wait.rindex("__ballot_sync"):]
     assert re.search(r"__syncwarp\(\);\s*asm volatile\(\"fence\.proxy\.async", after)
+
+
+def test_few_row_products_read_whole_pieces_only_where_k_has_them():
+    """row_piece of sp_linear_few.cu reads 16 bytes of a row behind a check that all of them lie below K, and nothing else unchecked: a single row
+    may end with the caller's storage."""
+    text = re.sub(r"//[^\n]*", "", (CSRC / "sp_linear_few.cu").read_text())
+    bodies = re.findall(r"\w+ row_piece\(([^)]*)\)\s*\{(.*?)\n\}", text, re.S)
+    assert len(bodies) == 2
+    for args, body in bodies:
+        n = 8 if "bfloat16" in args else 4
+        wide = re.search(r"if \((VEC && )?k \+ %d <= K\) \{.*?\n  \}" % n, body, re.S)
+        assert wide and body.count("reinterpret_cast<const %s*>" % ("uint4" if n == 8 else "float4")) == 1
+        assert "*at" in wide.group(0) and "*at" not in body.replace(wide.group(0), "")
