@@ -233,6 +233,13 @@ def new_status(device="cuda") -> torch.Tensor:
     return torch.zeros(4, dtype=torch.int32, device=device)
 
 
+def raise_status(status: torch.Tensor, what: str = "index"):
+    """Waits for the device and raises what the calls that were given `status` reported."""
+    s = status.cpu().tolist()
+    if s[0] != 0:
+        raise SpError(s[0], f"device status ({what} {s[1]}, aux {s[2]})")
+
+
 def sp_set_reproducible(on: bool):
     """Process-wide switch: fixed summation order everywhere (bit-identical results for equal inputs)."""
     _check(lib().sp_set_reproducible(int(bool(on))), "sp_set_reproducible")
@@ -801,9 +808,7 @@ class FfnModule:
         return dict(zip(REPORT_FIELDS, self.report.cpu().tolist()))
 
     def check_status(self):
-        s = self.status.cpu().tolist()
-        if s[0] != 0:
-            raise SpError(s[0], f"device status (index {s[1]}, aux {s[2]})")
+        raise_status(self.status)
 
 
 @dataclass

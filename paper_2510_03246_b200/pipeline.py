@@ -194,7 +194,7 @@ def expand_weights(cmod: api.FfnModule, idx: torch.Tensor, n: int):
 
 
 def prune_attention_heads(H: torch.Tensor, Ypre: torch.Tensor, W_O: torch.Tensor, n_heads: int, k_heads: int,
-                          rho: float = 0.1, token_chunk: int = 32768):
+                          rho: float = 0.1, token_chunk: int = 32768, status: torch.Tensor | None = None):
     """Head pruning of one attention module with its head outputs held fixed (Algorithm 2, attention branch, W_O part;
     Algorithm 1 Step 3 with heads as units).  H [N, d]: concatenated head outputs (the input of the output
     projection), Ypre [N, d]: the pre-trained module output, W_O [d, d] fp32.  Head h owns columns
@@ -203,45 +203,65 @@ def prune_attention_heads(H: torch.Tensor, Ypre: torch.Tensor, W_O: torch.Tensor
       head scores                       sp_struct_scores, Wanda-l2 over the head's column block of W_O
       keep the k_heads best             sp_apply_mask
       W_O[:, S] = R[:, S](G_H[S,S] + rho_eff I)^-1, other heads zero     sp_linear_refit (ridge of the full system)
-    Returns (mask u8 [n_heads], W_O_new fp32 [d, d], scores fp32 [n_heads])."""
+    status: int32 [4] (api.new_status) for what the device reports, or None.  Returns (mask u8 [n_heads], W_O_new fp32 [d, d], scores fp32 [n_heads])."""
     N, d = H.shape
     d_head = d // n_heads
     G = torch.zeros(d, d, dtype=torch.float32, device=H.device)
     R = torch.zeros(d, d, dtype=torch.float32, device=H.device)
     for t0 in range(0, N, token_chunk):
-        api.sp_gram_accumulate(H[t0:t0 + token_chunk], Ypre[t0:t0 + token_chunk], G, R)
+        api.sp_gram_accumulate(H[t0:t0 + token_chunk], Ypre[t0:t0 + token_chunk], G, R, status=status)
     api.sp_symmetrize(G)
     scores, _, _ = api.sp_struct_scores(api.SP_SCORE_WANDA_L2, n_heads, d_head, W=W_O, colsq=G, colsq_stride=d + 1)
     mask, _, _ = api.sp_apply_mask(scores, k_heads)
-    W_new = api.sp_linear_refit(R, G, mask, k_heads, rho, group=d_head, rho_relative=True)
+    W_new = api.sp_linear_refit(R, G, mask, k_heads, rho, group=d_head, rho_relative=True, status=status)
     return mask, W_new, scores
 
 
+class _Status:
+    """The status word of a function's calls.  A caller's own is passed on and left to the caller (api.raise_status); without one the function
+    waits for the device at its end and raises.  While a CUDA graph is captured nothing can be waited for: there only a caller's tells."""
+
+    def __init__(self, given: torch.Tensor | None, device):
+        self.own = given is None
+        self.word = api.new_status(device) if self.own else given
+
+    def __enter__(self):
+        return self.word
+
+    def __exit__(self, error, *_):
+        if self.own and error is None and not (self.word.is_cuda and torch.cuda.is_current_stream_capturing()):
+            api.raise_status(self.word)
+
+
 def attention_head_outputs(X: torch.Tensor, Wqkv: torch.Tensor, cu: torch.Tensor, n_heads: int, n_kv_heads: int | None = None,
-                           bias: torch.Tensor | None = None, causal: bool = True) -> torch.Tensor:
+                           bias: torch.Tensor | None = None, causal: bool = True, status: torch.Tensor | None = None) -> torch.Tensor:
     """Concatenated head outputs H [N, n_heads * d_head] of an attention module over packed sequences (cu: int32 offsets [n_seq + 1]
     on the device, X [N, d] token-major): the input of its output projection, and what prune_attention_heads takes.
     Wqkv [(n_heads + 2 n_kv_heads) d_head, d]: the rows of W_Q, W_K, W_V one below the other, in X's dtype; bias fp32 or None.
     Rows of X before the first and behind the last sequence (padding; whatever stands there) have zero rows in H: nothing in sums over tokens.
     Two library calls, and no probabilities in memory (sp_mha_init, which the auxiliary variables of Algorithm 2 start from, keeps
-    n_seq * n_heads * T * T of them)."""
+    n_seq * n_heads * T * T of them).  status: int32 [4] (api.new_status) that the calls report through; without one the function waits for them
+    and raises SpError itself."""
     n_kv = n_heads if n_kv_heads is None else n_kv_heads
     d_head = Wqkv.shape[0] // (n_heads + 2 * n_kv)
-    qkv = api.sp_linear(X, Wqkv, bias=bias)
-    q, k = n_heads * d_head, n_kv * d_head
-    H = torch.zeros(X.shape[0], q, dtype=X.dtype, device=X.device)
-    api.sp_attention(qkv[:, :q], qkv[:, q:q + k], qkv[:, q + k:q + 2 * k], cu, cu, n_heads, n_kv, causal=causal, out=H)
+    with _Status(status, X.device) as word:
+        qkv = api.sp_linear(X, Wqkv, bias=bias, status=word)
+        q, k = n_heads * d_head, n_kv * d_head
+        H = torch.zeros(X.shape[0], q, dtype=X.dtype, device=X.device)
+        api.sp_attention(qkv[:, :q], qkv[:, q:q + k], qkv[:, q + k:q + 2 * k], cu, cu, n_heads, n_kv, causal=causal, out=H, status=word)
     return H
 
 
 def prune_attention_module(X: torch.Tensor, Wqkv: torch.Tensor, W_O: torch.Tensor, cu: torch.Tensor, n_heads: int, k_heads: int,
-                           rho: float = 0.1, token_chunk: int = 32768, bias: torch.Tensor | None = None, causal: bool = True):
+                           rho: float = 0.1, token_chunk: int = 32768, bias: torch.Tensor | None = None, causal: bool = True,
+                           status: torch.Tensor | None = None):
     """Head pruning of an attention module from its input (every head with a key head of its own): the head outputs over the packed
     calibration sequences, the pre-trained module output Ypre = H W_O^T, then prune_attention_heads.  W_O fp32 [d, n_heads * d_head].
-    Returns (mask, W_O_new, scores, H, Ypre)."""
-    H = attention_head_outputs(X, Wqkv, cu, n_heads, bias=bias, causal=causal)
-    Ypre = api.sp_linear(H, W_O.to(X.dtype))
-    mask, W_new, scores = prune_attention_heads(H, Ypre, W_O, n_heads, k_heads, rho, token_chunk)
+    status as attention_head_outputs.  Returns (mask, W_O_new, scores, H, Ypre)."""
+    with _Status(status, X.device) as word:
+        H = attention_head_outputs(X, Wqkv, cu, n_heads, bias=bias, causal=causal, status=word)
+        Ypre = api.sp_linear(H, W_O.to(X.dtype), status=word)
+        mask, W_new, scores = prune_attention_heads(H, Ypre, W_O, n_heads, k_heads, rho, token_chunk, status=word)
     return mask, W_new, scores, H, Ypre
 
 
@@ -262,15 +282,18 @@ def kept_ffn_weights(mask: torch.Tensor, W1: torch.Tensor, W2: torch.Tensor, Wg:
 
 
 def ffn_forward(X: torch.Tensor, W1: torch.Tensor, W2: torch.Tensor, Wg: torch.Tensor | None = None,
-                b1: torch.Tensor | None = None, b2: torch.Tensor | None = None, residual: torch.Tensor | None = None) -> torch.Tensor:
+                b1: torch.Tensor | None = None, b2: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                status: torch.Tensor | None = None) -> torch.Tensor:
     """Output [N, d] of an FFN module: W2 relu(W1 x + b1) + b2 (+ residual), or with a gate projection W2 (silu(Wg x) * (W1 x + b1)) + b2
-    (+ residual).  Weights in X's dtype (kept_ffn_weights), biases fp32.  Two (three) library calls."""
-    if Wg is None:
-        A = api.sp_linear(X, W1, bias=b1, act=api.SP_LINEAR_RELU)
-    else:
-        A = api.sp_linear(X, W1, bias=b1)
-        A = api.sp_linear(X, Wg, act=api.SP_LINEAR_SILU, other=A, combine=api.SP_COMBINE_MUL, out=A)
-    return api.sp_linear(A, W2, bias=b2, other=residual)
+    (+ residual).  Weights in X's dtype (kept_ffn_weights), biases fp32.  Two (three) library calls.  status: int32 [4] (api.new_status) that the
+    calls report through; without one the function waits for them and raises SpError itself."""
+    with _Status(status, X.device) as word:
+        if Wg is None:
+            A = api.sp_linear(X, W1, bias=b1, act=api.SP_LINEAR_RELU, status=word)
+        else:
+            A = api.sp_linear(X, W1, bias=b1, status=word)
+            A = api.sp_linear(X, Wg, act=api.SP_LINEAR_SILU, other=A, combine=api.SP_COMBINE_MUL, out=A, status=word)
+        return api.sp_linear(A, W2, bias=b2, other=residual, status=word)
 
 
 @dataclass
@@ -305,16 +328,14 @@ def token_loss(hidden: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor, 
     for t0 in range(0, N, token_chunk):
         h, t = hidden[t0:t0 + token_chunk], targets[t0:t0 + token_chunk]
         n = h.shape[0]
-        x = api.sp_linear(h, W_lm, out=logits[:n])
+        x = api.sp_linear(h, W_lm, out=logits[:n], status=status)
         r = api.sp_token_logprobs(x, t, want_entropy=False, status=status)
         logp[t0:t0 + n] = r.logp
         if with_grad:
             api.sp_token_logprobs_grad(x, t, r.lse, g[:n], out=x)
-            api.sp_gemm(x, W_lm, d_hidden[t0:t0 + n], use_tensor_cores=tc)
-            api.sp_gemm(x, h, d_W, transA=True, beta=1.0, use_tensor_cores=tc)
-    code = status.cpu().tolist()
-    if code[0] != 0:
-        raise api.SpError(code[0], f"device status (token {code[1]} of its chunk)")
+            api.sp_gemm(x, W_lm, d_hidden[t0:t0 + n], use_tensor_cores=tc, status=status)
+            api.sp_gemm(x, h, d_W, transA=True, beta=1.0, use_tensor_cores=tc, status=status)
+    api.raise_status(status, "token of its chunk, or of a wait the block,")
     return TokenLoss(-float(logp.double().sum().item()), tokens, logp, d_hidden, d_W)
 
 

@@ -165,3 +165,45 @@ def test_one_row_that_ends_with_its_storage(dtype, K):
         want = x.double() @ w.double().T
         tol = (x.double().abs() @ w.double().abs().T) * K * 2.0 ** (-23 if dtype == torch.bfloat16 else -52) + 2.0 ** -23 * want.abs() + 1e-30
         assert ((y.double() - want).abs() <= tol).all()
+
+
+def test_pipeline_functions_in_a_captured_graph():
+    """With a status word of the caller nothing waits for the device; without one the wait is left out while a graph is captured."""
+    g = torch.Generator(device=DEV).manual_seed(7)
+    r = lambda *s: (torch.randn(*s, generator=g, device=DEV) / 8).bfloat16()
+    X, Wqkv, W1, W2, Wg = r(200, 64), r(192, 64), r(96, 64), r(64, 96), r(96, 64)
+    cu = torch.tensor([0, 150, 200], dtype=torch.int32, device=DEV)
+
+    def layer(status):
+        H = pipeline.attention_head_outputs(X, Wqkv, cu, 2, status=status)
+        return pipeline.ffn_forward(H, W1, W2, Wg, residual=X, status=status)
+    want = layer(None)
+    for status in (api.new_status(), None):
+        assert torch.equal(layer(status), want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = layer(status)
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+
+
+def test_a_wait_that_runs_out_under_a_pipeline_function_is_raised():
+    """(With a budget of a few cycles ordinary waits run out, nothing is withheld.)"""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    X = torch.randn(4096, 512, generator=g, device=DEV).bfloat16()
+    Wqkv = (torch.randn(1536, 512, generator=g, device=DEV) / 22).bfloat16()
+    cu = torch.tensor([0, 4096], dtype=torch.int32, device=DEV)
+    want = pipeline.attention_head_outputs(X, Wqkv, cu, 8)
+    status = api.new_status()
+    assert api.lib().sp_set_wait_budget(8) == 0
+    try:
+        with pytest.raises(api.SpError) as e:
+            pipeline.attention_head_outputs(X, Wqkv, cu, 8)
+        assert e.value.code == 7
+        pipeline.attention_head_outputs(X, Wqkv, cu, 8, status=status)
+        assert int(status[0]) == 7
+    finally:
+        assert api.lib().sp_set_wait_budget(0) == 0
+    assert torch.equal(pipeline.attention_head_outputs(X, Wqkv, cu, 8), want)

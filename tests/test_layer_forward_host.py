@@ -71,6 +71,51 @@ def head_outputs(t, **kw):
     return pipeline.attention_head_outputs(t["X"], t["Wqkv"], t["cu"], HEADS, **kw)
 
 
+def module(t, **kw):
+    return pipeline.prune_attention_module(t["X"], t["Wqkv"], t["W_O"], t["cu"], HEADS, 1, **kw)
+
+
+def ffn(t, **kw):
+    return pipeline.ffn_forward(t["X"], torch.zeros(5, D), torch.zeros(D, 5), **kw)
+
+
+def gated(t, **kw):
+    return pipeline.ffn_forward(t["X"], torch.zeros(5, D), torch.zeros(D, 5), torch.zeros(5, D), **kw)
+
+
+def loss(t):
+    return pipeline.token_loss(t["X"], torch.zeros(9, D), torch.zeros(6, dtype=torch.int64), with_grad=True)
+
+
+USED = [(head_outputs, ["sp_linear", "sp_attention"]), (module, ["sp_linear", "sp_attention", "sp_gram_accumulate", "sp_linear_refit"]),
+        (ffn, ["sp_linear"]), (gated, ["sp_linear"]), (loss, ["sp_linear", "sp_token_logprobs", "sp_gemm"])]
+
+
+@pytest.mark.parametrize("call,name", [(c, n) for c, names in USED for n in names])
+def test_waits_that_ran_out_in_a_call_are_raised(monkeypatch, call, name):
+    seen = Calls(monkeypatch, late=name).seen
+    with pytest.raises(api.SpError) as e:
+        call(tensors())
+    assert e.value.code == 7
+    assert {n for n, _ in seen} == set(dict((c, names) for c, names in USED)[call])
+
+
+@pytest.mark.parametrize("call", [c for c, _ in USED])
+def test_every_call_has_the_same_status_word(monkeypatch, call):
+    seen = Calls(monkeypatch).seen
+    call(tensors())
+    assert all(s is not None and s is seen[0][1] for _, s in seen)
+
+
+@pytest.mark.parametrize("call", [head_outputs, module, ffn, gated])
+def test_a_status_word_of_the_caller_is_left_to_the_caller(monkeypatch, call):
+    """Nothing is raised then, and nothing waits for the device."""
+    seen = Calls(monkeypatch, late="sp_linear").seen
+    status = torch.zeros(4, dtype=torch.int32)
+    call(tensors(), status=status)
+    assert int(status[0]) == 7 and all(s is status for _, s in seen)
+
+
 def test_head_outputs_of_rows_outside_the_sequences_are_zero(monkeypatch):
     Calls(monkeypatch)
     t = tensors()
