@@ -306,7 +306,13 @@ class TokenLoss:
 
     @property
     def perplexity(self) -> float:
-        return math.exp(self.nll / max(self.tokens, 1))
+        """e^(nll / tokens); NaN where no token was scored, infinite beyond the range of a double."""
+        if self.tokens == 0:
+            return math.nan
+        try:
+            return math.exp(self.nll / self.tokens)
+        except OverflowError:
+            return math.inf
 
 
 def token_loss(hidden: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor, token_chunk: int = 8192, with_grad: bool = False) -> TokenLoss:

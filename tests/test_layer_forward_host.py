@@ -122,3 +122,11 @@ def test_head_outputs_of_rows_outside_the_sequences_are_zero(monkeypatch):
     t["cu"] = torch.tensor([1, 3, 5], dtype=torch.int32)
     H = head_outputs(t)
     assert H.shape == (6, D) and (H[1:5] == 1).all() and (H[0] == 0).all() and (H[5] == 0).all()
+
+
+def test_perplexity():
+    def of(nll, tokens):
+        return pipeline.TokenLoss(nll, tokens, torch.zeros(1), None, None).perplexity
+    assert of(6.0, 2) == math.exp(3.0)
+    assert math.isnan(of(0.0, 0))                                  # of no tokens there is none
+    assert of(2000.0, 1) == math.inf and of(math.inf, 3) == math.inf and math.isnan(of(math.nan, 3))
