@@ -270,11 +270,12 @@ __device__ __forceinline__ float act_silu(float v) {
   const float y = __fdividef(v, 1.f + __expf(-v));      // (selections, no branches, here and below: 32 of these run side by side)
   return v == -INFINITY ? 0.f : y;
 }
-// v Phi(v).  Phi(-|v|) = erfc(a) / 2 with a = |v| / sqrt 2, and erfc(a) = t exp(q(t) - a^2) with t = 1 / (1 + a / 2): the smooth
-// q(t) = log(erfc(a) exp(a^2) / t) is a polynomial of degree 7, interpolated at Chebyshev nodes for a up to 12 (within 1e-6, so that
-// small Phi keep their relative accuracy).  A tenth of erfcf's instructions, 32 copies of which no longer fit the instruction cache.
+// v Phi(v).  Phi(-|v|) = erfc(a) / 2 with a = |v| / sqrt 2, and erfc(a) = t exp(q(t) - a^2) with t = 1 / (1 + a / 2), the form that Press et al., Numerical
+// Recipes, give for erfc; the smooth q(t) = log(erfc(a) exp(a^2) / t) is a polynomial of degree 7 here, interpolated at Chebyshev nodes for a up to 12
+// (within 1e-6, so that small Phi keep their relative accuracy).  a^2 is v v / 2 in one rounding with q: squared, a's own rounding would double the error at
+// v = -12 (1.6e-5 of the value there; so at most 1e-5).  A tenth of erfcf's instructions, 32 copies of which no longer fit the instruction cache.
 __device__ __forceinline__ float act_gelu(float v) {
-  const float a = 0.7071067811865476f * fabsf(v), t = __fdividef(1.f, fmaf(0.5f, a, 1.f));
+  const float t = __fdividef(1.f, fmaf(0.35355339059327373f, fabsf(v), 1.f));
   float q = fmaf(-0.19117627f, t, 0.76572722f);
   q = fmaf(q, t, -1.0253474f);
   q = fmaf(q, t, 0.37195718f);
@@ -282,7 +283,7 @@ __device__ __forceinline__ float act_gelu(float v) {
   q = fmaf(q, t, 0.39727193f);
   q = fmaf(q, t, 0.99808556f);
   q = fmaf(q, t, -1.2654468f);
-  const float e = 0.5f * t * __expf(fmaf(-a, a, q));
+  const float e = 0.5f * t * __expf(fmaf(-0.5f * v, v, q));
   // (e = 0 for infinities, too)
   const float base = v < 0.f ? 0.f : v, share = e == 0.f ? 0.f : fabsf(v) * e;
   return base - share;

@@ -207,3 +207,17 @@ def test_a_wait_that_runs_out_under_a_pipeline_function_is_raised():
     finally:
         assert api.lib().sp_set_wait_budget(0) == 0
     assert torch.equal(pipeline.attention_head_outputs(X, Wqkv, cu, 8), want)
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+def test_gelu_keeps_its_relative_accuracy(out_dtype):
+    """Down to where y Phi(y) leaves the normal range: within 2^-16 of its value (and half a step of storage)."""
+    v = torch.cat([-torch.linspace(0.001, 13.0, 40000), torch.linspace(0.001, 13.0, 1001)]).to(DEV)
+    for T in (1, 300):                                             # both forms
+        x = torch.zeros(T, 16, dtype=torch.bfloat16, device=DEV)
+        w = torch.zeros(v.numel(), 16, dtype=torch.bfloat16, device=DEV)
+        y = api.sp_linear(x, w, bias=v, act=api.SP_LINEAR_GELU, out_dtype=out_dtype)
+        want = v.double() * torch.special.log_ndtr(v.double()).exp()
+        tol = (2.0 ** -16 + HALF[out_dtype] * (1 + 2.0 ** -16)) * want.abs() + 2.0 ** -126
+        err = (y.double() - want).abs()
+        assert (err <= tol).all(), (float((err / tol).max()), float(v[(err / tol).amax(0).argmax()]))
