@@ -503,6 +503,8 @@ size_t sp_mha_value_refit_workspace_bytes(int64_t d, int64_t n_heads, int64_t T,
  * bound.  Rows of O and lse that belong to no sequence are left as they were, and what stands in rows of K and V outside a
  * sequence does not reach it (infinities and NaN included).  Inside a sequence a NaN or an infinity in K or V at a key that the
  * causal mask hides from some queries does not reach those either.
+ * A scaled logit beyond the range of fp32 makes its row NaN; below that range the row is NaN or the key counts as hidden.  (So does a key whose
+ * logit is -infinity: a row of nothing else is one without a visible key.)
  * Softmax and sums in fp32 in both modes; fp32 mode: products in fp32.  bf16 mode: the probabilities are rounded to bf16 before
  * the product with V, the result once; tensor cores where d_head and the leading dimensions of Q, K and V are multiples of 8 and
  * their pointers 16-byte aligned, else the CUDA cores, slower.  Equal calls give equal bits.

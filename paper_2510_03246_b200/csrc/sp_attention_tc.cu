@@ -659,8 +659,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const int64_t out_row = (int64_t)it.q0 + token;
       const int head = p.gp == 1 ? it.head : it.head * p.gp + row % p.gp;
       const bool cut = p.a.part > 0 && it.nk > p.a.part;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const float lse2 = l == 0.f ? -INFINITY : fmaf(r, c, log2f(l));
+      // no key seen: no reference r.  With one, 2^(c (x - r)) of the row's largest logit is 1 or more, unless c r is beyond fp32: then the row is NaN.
+      const bool none = r == -INFINITY;
+      const float inv = l == 0.f ? NAN : 1.f / l;
+      const float lse2 = none ? -INFINITY : l == 0.f ? NAN : fmaf(r, c, log2f(l));
       __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.o) + out_row * p.a.ldo + (int64_t)head * p.a.dh;
       float* part = cut ? p.a.part_o + ((int64_t)it.c * p.a.Nq + out_row) * ((int64_t)p.a.n_heads * p.a.dh) + (int64_t)head * p.a.dh
                         : nullptr;
@@ -688,7 +690,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           if (!valid || 32 * b >= p.a.dh) continue;
           float f[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) f[j] = l == 0.f ? 0.f : __uint_as_float(o[j]) * inv;
+          for (int j = 0; j < 32; ++j) f[j] = none ? 0.f : __uint_as_float(o[j]) * inv;
           if (bad) {
             // values of V that the edge warps set to zero, for the rows that do see them
             const int kvh = p.gp == 1 ? it.head / p.a.g : it.head;

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2510_03246_b200 import api, pipeline
+from tests import test_gpu_attention as att
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -221,3 +222,16 @@ def test_gelu_keeps_its_relative_accuracy(out_dtype):
         tol = (2.0 ** -16 + HALF[out_dtype] * (1 + 2.0 ** -16)) * want.abs() + 2.0 ** -126
         err = (y.double() - want).abs()
         assert (err <= tol).all(), (float((err / tol).max()), float(v[(err / tol).amax(0).argmax()]))
+
+
+@pytest.mark.parametrize("q,k", [([1, 1], [700, 40]), ([300], [300])])     # single tokens; tiles of many rows
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_scaled_logits_beyond_fp32_are_not_taken_for_a_mask(dtype, q, k):
+    """scale <q, k> = +2^136 at every key: beyond fp32.  No probability can be told, so the rows are NaN: not 0, which says that a row sees
+    no key."""
+    Q, K, V = att.inputs(sum(q), sum(k), 2, 2, 64, dtype)
+    Q.zero_()
+    K.zero_()
+    Q[:, ::64], K[:, ::64] = 2.0 ** 60, 2.0 ** 66
+    o, lse = api.sp_attention(Q, K, V, att.cu(q), att.cu(k), 2, scale=2.0 ** 10, want_lse=True)
+    assert torch.isnan(o).all() and not (lse == -math.inf).any()
