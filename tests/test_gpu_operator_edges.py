@@ -235,3 +235,28 @@ def test_scaled_logits_beyond_fp32_are_not_taken_for_a_mask(dtype, q, k):
     Q[:, ::64], K[:, ::64] = 2.0 ** 60, 2.0 ** 66
     o, lse = api.sp_attention(Q, K, V, att.cu(q), att.cu(k), 2, scale=2.0 ** 10, want_lse=True)
     assert torch.isnan(o).all() and not (lse == -math.inf).any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dh", [64, 72])
+@pytest.mark.parametrize("q", [[1] * 100 + [500] + [1] * 60, [0] * 90 + [600, 1] + [0] * 40, [3000] + [1] * 255])
+def test_one_long_sequence_among_many_short_or_empty_ones(dtype, dh, q):
+    """By the average these are few rows: the kernels that stream keys past some rows take the long sequence tile by tile."""
+    k = [n if n > 1 else (37 * i) % 301 for i, n in enumerate(q)]
+    Q, K, V = att.inputs(sum(q), sum(k), 2, 2, dh, dtype)
+    assert sum(q) <= 16 * len(q)
+    att.check(Q, K, V, q, k, 2, 2)
+    att.check(Q, K, V, q, k, 2, 2, causal=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv", [(64, 1), (40, 2), (96, 1)])
+def test_groups_wider_than_a_few_row_tile(dtype, heads, kv):
+    """Slots of which most are empty: few rows on average, and more heads to a key head than a tile of them has rows."""
+    q, k = [0] * 200, [0] * 200
+    for at, n in ((3, 700), (77, 1), (140, 2100), (199, 64)):
+        q[at], k[at] = 1, n
+    q[150], k[150] = 2, 65
+    Q, K, V = att.inputs(sum(q), sum(k), heads, kv, 64, dtype, seed=heads)
+    assert sum(q) * heads // kv <= 16 * len(q)
+    att.check(Q, K, V, q, k, heads, kv)
