@@ -507,8 +507,11 @@ size_t sp_mha_value_refit_workspace_bytes(int64_t d, int64_t n_heads, int64_t T,
  * logit is -infinity: a row of nothing else is one without a visible key.)
  * Softmax and sums in fp32 in both modes; fp32 mode: products in fp32.  bf16 mode: the probabilities are rounded to bf16 before
  * the product with V, the result once; tensor cores where d_head and the leading dimensions of Q, K and V are multiples of 8 and
- * their pointers 16-byte aligned, else the CUDA cores, slower.  Equal calls give equal bits.
- * Few rows: the keys of a sequence are cut into parts that run side by side and are joined by their lse; the workspace of
+ * their pointers 16-byte aligned, else the CUDA cores, slower (there the probabilities stay in fp32, so that the same values in another layout
+ * may round otherwise).  Equal calls give equal bits.
+ * Few rows (at most 16 queries x heads of a key head per sequence, on average over n_seq, empty sequences among them) take kernels that stream the
+ * keys past the rows; a long sequence among many short or empty ones is right there, but takes several times as long as by itself.  With few
+ * tiles for the SMs the keys of a sequence are cut into parts that run side by side and are joined by their lse; the workspace of
  * sp_attention_workspace_bytes (0 when no cut is made) holds their results, scratch of this call alone (two calls that may
  * overlap on the GPU need two).  status_dev may be NULL.
  * Errors: SP_ERR_INVALID_ARG (null pointers, scale outside [1e-30, 1e30]), SP_ERR_SHAPE (n_kv_heads does not divide

@@ -324,6 +324,9 @@ struct Cut {
 // that has queries, times the key heads; fewer than the SMs (148) leave SMs idle.  Parts are then as long as gives four for every SM
 // (so that sequences of different lengths even out), at least 256 keys.  With few rows an SM reads 1024 keys of a bf16 head (512 in fp32) in 5 us, about what a second
 // launch and the results' way through memory cost: shorter parts do not pay, and beyond 4096 keys for an SM it gets eight.
+// Least keys of a part halved / as here / doubled, us with cold caches: bf16, 1 token after 16384 keys, 32 heads of 128 on 8: 39 / 33 / 31, 4 after 8192
+// 51 / 45 / 43, 16 after 4096 74 / 72 / 70; fp32, 4 after 2048 39 / 33 / 47; tiles, 128 after 8064 (8 heads of 128) 59 / 41 / 31, 300 after 700 (4 of
+// 64) 23 / 23 / 25.  Four / eight parts for an SM: 16 after 16384 191 / 195, 16 after 2048 .. 31013 equal.
 // Sequences that are no longer than a part on average are not cut; one of average length falls into equal parts.
 Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype) {
   Cut cut;

@@ -20,7 +20,8 @@
 // Warps: 0-3 and 4-7 softmax of half 0 and 1 (lane and warp give the row), 8 finds the items and issues TMA, 9 MMA issue and tensor memory,
 // 10-11 edge tiles of V.  Items go to the other warps through shared memory (finding one takes two thousand cycles).
 // What bounds it: per half and tile 128 exponentials a row (1024 cycles of the pipe that two warps share) between two products (1024 cycles
-// together for heads of 128).  One prompt of 8192, 32 heads of 128 on 8: 479 us; 16 documents of up to 2048 tokens, 32 heads of 64 on 8: 176 us.
+// together for heads of 128).  One prompt of 8192, 32 heads of 128 on 8: 488 us after a pause, 531 in a row of calls (power cap); 16 documents of up to
+// 2048 tokens, 32 heads of 64 on 8: 167 and 156 us.  (Figures beside the steps below are of the kernel of that time.)
 // Waits for copies, the tensor core and other warps are bounded by a clock budget (SP_ERR_TIMEOUT through status).
 #include <math.h>
 #include <string.h>

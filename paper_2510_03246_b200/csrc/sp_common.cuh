@@ -364,7 +364,8 @@ bool gemm_tc_supported(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand B
 // The same for few rows (sp_linear_few.cu), layouts as gemm_tc_supported, both K-major.  Where it is the faster one: up to 16 rows, and up to
 // 192 while rows times outputs are at most 2^18 (a block has 32 x 16 of them and all of K; the tiles' time is that of one or two tiles of 128 x 256).
 // Tiles / this, us: 4096 -> 4096 16 rows 33 / 14, 64 rows 35 / 29, 96 rows 35 / 38; 1024 -> 8192 32 rows 18 / 14, 48 rows 18 / 21; 4096 -> 16384 16
-// rows 46 / 35, 32 rows 45 / 49; 2048 -> 2048 128 rows 23 / 18, 192 rows 23 / 25; 768 -> 1536 192 rows 16 / 14.
+// rows 46 / 35, 32 rows 45 / 49; 2048 -> 2048 128 rows 23 / 18, 192 rows 23 / 25; 768 -> 1536 192 rows 16 / 14.  (Measured for K of 768 .. 4096; it
+// does not enter the rule.)
 inline bool linear_few_rows(int64_t M, int64_t N) { return M <= 16 || (M <= 192 && M * N <= (1 << 18)); }
 cudaError_t linear_few(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand W, const LinearEpi& epi, Operand other, OutOperand C,
                        cudaStream_t stream);

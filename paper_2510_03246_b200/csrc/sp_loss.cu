@@ -619,6 +619,9 @@ sp_status sp_token_logprobs(const sp_mat* logits, const int64_t* targets, double
                         alt_ids, alt_logp, status_dev};
   // Short rows: a warp each.  Long ones: a block of four warps, so that the rows of an SM are many and at different places (8192 x 50257, warps
   // per row 8 / 4: 182 / 161 us, with eight alternatives 245 / 229), or a cluster of blocks while there are too few rows to fill the SMs.
+  // Border of the short rows at 2048 / here, us: 4096 x 2500 25 / 14, 8192 x 3000 in fp32 43 / 29; here / at 8192: 4096 x 6000 29 / 23, with five
+  // alternatives 43 / 29 (this border could lie higher).  Two / four / eight blocks for an SM: 100 x 50257 in fp32 21 / 17 / 16, 64 x 32000 with five
+  // alternatives 16 / 25 / 25, 300 x 32000 equal.  Least values of a block 1024 / 2048 / 4096: equal within 2 us but 64 x 32000 with five (25, 25, 16).
   const bool narrow = V <= 4096;
   int cluster = 1;
   while (!narrow && cluster < kMaxCluster && T * cluster * 2 <= (int64_t)sm_count() * 4 && V / (cluster * 2) >= 2048) cluster *= 2;

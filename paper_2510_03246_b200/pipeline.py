@@ -285,7 +285,8 @@ def ffn_forward(X: torch.Tensor, W1: torch.Tensor, W2: torch.Tensor, Wg: torch.T
                 b1: torch.Tensor | None = None, b2: torch.Tensor | None = None, residual: torch.Tensor | None = None,
                 status: torch.Tensor | None = None) -> torch.Tensor:
     """Output [N, d] of an FFN module: W2 relu(W1 x + b1) + b2 (+ residual), or with a gate projection W2 (silu(Wg x) * (W1 x + b1)) + b2
-    (+ residual).  Weights in X's dtype (kept_ffn_weights), biases fp32.  Two (three) library calls.  status: int32 [4] (api.new_status) that the
+    (+ residual).  Weights in X's dtype (kept_ffn_weights), biases fp32.  Two (three) library calls, each with its result in X's dtype: W1 x + b1 is
+    rounded to it before the gate multiplies it, and the product again.  status: int32 [4] (api.new_status) that the
     calls report through; without one the function waits for them and raises SpError itself."""
     with _Status(status, X.device) as word:
         if Wg is None:
@@ -317,8 +318,9 @@ class TokenLoss:
 
 def token_loss(hidden: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor, token_chunk: int = 8192, with_grad: bool = False) -> TokenLoss:
     """Negative log likelihood of the target tokens under logits = hidden W_lm^T, chunk by chunk (one chunk of logits in memory):
-    the measure of Section 4 is its perplexity.  hidden [N, d], W_lm [V, d] of one dtype; targets int64 [N], negative: not
-    scored.  with_grad: also the gradient of the mean with respect to hidden and W_lm, written over the logits of each chunk and
+    the measure of Section 4 is its perplexity.  hidden [N, d], W_lm [V, d] of one dtype, to which the logits are rounded (bf16: half a step is 0.03
+    of a logit between 8 and 16, 0.06 of one up to 32; log p is off by as much at the target, on average by far less); targets int64 [N], negative:
+    not scored.  with_grad: also the gradient of the mean with respect to hidden and W_lm, written over the logits of each chunk and
     multiplied from there."""
     N, d = hidden.shape
     V = W_lm.shape[0]
