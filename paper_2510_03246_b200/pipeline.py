@@ -206,6 +206,7 @@ def prune_attention_heads(H: torch.Tensor, Ypre: torch.Tensor, W_O: torch.Tensor
     status: int32 [4] (api.new_status) for what the device reports, or None.  Returns (mask u8 [n_heads], W_O_new fp32 [d, d], scores fp32 [n_heads])."""
     N, d = H.shape
     d_head = d // n_heads
+    api._vector(status, torch.int32, 4, H.get_device(), "status")      # (refused here: the calls below take its address as it is)
     G = torch.zeros(d, d, dtype=torch.float32, device=H.device)
     R = torch.zeros(d, d, dtype=torch.float32, device=H.device)
     for t0 in range(0, N, token_chunk):

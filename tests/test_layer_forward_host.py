@@ -130,3 +130,14 @@ def test_perplexity():
     assert of(6.0, 2) == math.exp(3.0)
     assert math.isnan(of(0.0, 0))                                  # of no tokens there is none
     assert of(2000.0, 1) == math.inf and of(math.inf, 3) == math.inf and math.isnan(of(math.nan, 3))
+
+
+def test_status_words_of_another_kind_are_refused(monkeypatch):
+    Calls(monkeypatch)
+    t = tensors()
+    H = torch.zeros(6, D)
+    for bad in (torch.zeros(4), torch.zeros(3, dtype=torch.int32), torch.zeros(8, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError):
+            pipeline.prune_attention_heads(H, H, t["W_O"], HEADS, 1, status=bad)
+    pipeline.prune_attention_heads(H, H, t["W_O"], HEADS, 1, status=torch.zeros(4, dtype=torch.int32))
+    pipeline.prune_attention_heads(H, H, t["W_O"], HEADS, 1)
