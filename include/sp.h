@@ -72,7 +72,7 @@ typedef enum {
   SP_ERR_STATIC_LIMIT = 10
 } sp_status;
 
-typedef enum { SP_F32 = 0, SP_BF16 = 1, SP_F64 = 2 } sp_dtype;
+typedef enum { SP_F32 = 0, SP_BF16 = 1, SP_F64 = 2, SP_E4M3 = 3 } sp_dtype;   /* SP_E4M3: 8 bits, sp_rms_norm and sp_linear_e4m3 only */
 typedef enum { SP_ACT_RELU = 0, SP_ACT_SWIGLU = 1 } sp_act_kind;
 typedef enum { SP_Z_PAPER = 0, SP_Z_EXACT = 1 } sp_z_rule;
 typedef enum { SP_SCORE_WANDA_L2 = 0, SP_SCORE_WANDA_L1 = 1, SP_SCORE_LEMMA1 = 2 } sp_score_kind;
@@ -577,6 +577,102 @@ sp_status sp_token_logprobs(const sp_mat* logits, const int64_t* targets, double
 sp_status sp_token_logprobs_grad(const sp_mat* logits, const int64_t* targets, double scale, const float* lse,
                                  const float* entropy, const float* g_logp, const float* g_entropy,
                                  const sp_mat* dlogits, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * sp_rms_norm, sp_rms_norm_grad — root-mean-square norm of the residual stream between two modules, and its gradient.
+ *     h = x + r,   rstd = (mean_j h_j^2 + eps)^-1/2,   y_j = weight_j h_j rstd
+ * X: [T, d] (a module's output), R: [T, d] the stream, or NULL (h = x).  H: [T, d] where the new stream is written, or NULL; it may be R or X
+ * itself, and has R's dtype.  Y: [T, d] of X's dtype, or SP_E4M3: y8 = e4m3(y / scale) with scale[t] = max_j |y_j| / 448 (a row's maximum counts as
+ * at least 1e-30): operands of sp_linear_e4m3.  Y may be X itself.  weight: fp32 [d] or NULL (ones).  scale: fp32 [T], given exactly with SP_E4M3.
+ * rstd: fp32 [T] or NULL.  Every dtype, ld and alignment of SP_BF16 and SP_F32; widths up to 32768 with 16-byte rows read each value once, others
+ * again for each pass.  y comes from the unrounded sum h.  Sums in fp32: a row whose sum of squares leaves its range has rstd 0.
+ * A NaN or an infinity in a row makes its y NaN where the formula does.
+ * sp_rms_norm_grad: dX = rstd (weight dy - h rstd^2 mean(weight dy h)) + dH: the gradient of x and of r alike.  H as sp_rms_norm left it;
+ * rstd as it left it, or NULL (then formed again from H).  dH: the gradient that arrives at h through the stream itself, or NULL.  dX may be dH, or
+ * dY or H of its dtype; H, dH and dX have one dtype.  dweight: fp32 [d] = sum_t dy h rstd (written, not added to) or NULL, which needs the
+ * workspace of sp_rms_norm_grad_bytes(T, d), scratch of this call alone.  Sums in a fixed order: equal calls give equal bits.
+ * Errors: SP_ERR_INVALID_ARG (null pointers, eps outside [0, 1e30], scale without SP_E4M3 or the other way round, an output in the place of an
+ * input of another dtype or ld), SP_ERR_SHAPE (sizes that do not match, ld too small, d < 1, T > 2^31 - 1, d > 2^30), SP_ERR_DTYPE, SP_ERR_WORKSPACE,
+ * SP_ERR_ALIGNMENT (workspace not 256-byte aligned).
+ */
+sp_status sp_rms_norm(const sp_mat* X, const sp_mat* R, const float* weight, double eps, const sp_mat* H, const sp_mat* Y,
+                      float* scale, float* rstd, void* stream);
+sp_status sp_rms_norm_grad(const sp_mat* dY, const sp_mat* H, const float* weight, const float* rstd, double eps, const sp_mat* dH,
+                           const sp_mat* dX, float* dweight, void* ws, size_t ws_bytes, void* stream);
+size_t sp_rms_norm_grad_bytes(int64_t T, int64_t d);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * sp_linear_e4m3 — sp_linear with operands held in 8 bits:
+ *     Y = act(x_scale_t w_scale_o sum_k X8[t,k] W8[o,k] + bias) + other  (or * other)
+ * X: [T, in], W: [out, in], SP_E4M3, leading dimensions that are multiples of 16 and 16-byte aligned pointers (SP_ERR_ALIGNMENT else; in and out
+ * may be any numbers).  x_scale: fp32 [T], w_scale: fp32 [out].  Y: SP_BF16 or SP_F32, other has Y's dtype; bias, act, combine, other and the
+ * places that they may share as sp_linear.  Products are exact, sums in fp32, one rounding at the end.
+ * Errors: as sp_linear (T > 2^30 there), SP_ERR_ALIGNMENT.  Time-outs of the tensor-core kernel through status_dev (may be NULL).
+ */
+sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const sp_mat* W, const float* w_scale, const float* bias, int32_t act,
+                         const sp_mat* other, int32_t combine, const sp_mat* Y, int32_t* status_dev, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * sp_cache_append, sp_cache_read, sp_cache_attention — keys and values in a cache of pages that grows with its texts.
+ *
+ * A page holds page_len tokens (a multiple of 16) of all key heads; table[s * table_ld + e] is the page of tokens [e page_len, (e + 1) page_len) of
+ * sequence s, lens[s] the number of its tokens WITH those of the call.  Both are read on the device.
+ *   SP_CACHE_BF16: k, v: bf16 [n_pages, n_kv_heads, page_len, d_head], d_head a multiple of 16, at most 128.
+ *   SP_CACHE_4BIT: k, v: bytes [n_pages, n_kv_heads, page_len, d_head / 2], channel 2 i in the low half of byte i; k_scale, v_scale: bf16
+ *     [n_pages, n_kv_heads, page_len, d_head / 64, 2], scale and zero of every 64 channels: a number n stands for scale n + zero.  d_head 64 or 128.
+ *     zero = bf16(least), scale = bf16((largest - zero) / 15), n = (x - zero) / scale rounded to the nearest of 0 .. 15 (halves to even; 0 where
+ *     scale is 0).  A group with a NaN or an infinity reads back as NaN.
+ * The *_step are the bytes from a page to the next (multiples of 16), so that the pages of several layers may lie in one buffer.
+ * A token whose place has no page (a place before 0 or behind the table, an entry outside [0, n_pages)) is reported through status_dev (may be
+ * NULL) as SP_ERR_SHAPE with the sequence, and nothing outside the pages is touched: it is not appended, reads back as NaN, and makes the queries NaN
+ * that see it.  Pages that sequences share may be read by all; one slot that two tokens of a call are put into holds either.
+ *
+ * sp_cache_append: rows [cu[s], cu[s+1]) of K, V (and Q) are the last tokens of sequence s: row cu[s] + i has place p = lens[s] - n + i, n their
+ * number.  K, V: [N, n_kv_heads * d_head], Q: [N, n_heads * d_head] or none (ptr NULL), one dtype (SP_BF16 or SP_F32), any ld, so that they may be column
+ * slices of one matrix.  The first `turned` channels (a multiple of 16, 0 .. d_head) of every query and key head are turned by their position: pair
+ * i of channels (i, i + turned / 2), with neighbours != 0 (2 i, 2 i + 1), by the angle position * inv_freq[i], (a, b) -> (a cos - b sin,
+ * b cos + a sin); inv_freq: fp32 [turned / 2]; the angle and what goes to 4 bits in fp64, the rest in fp32.  position is p, or positions[row] (int32
+ * [N]) where given.  Q_out [N, n_heads * d_head]: the turned queries, may be Q itself.  K_out: the turned keys, or none; not K itself.
+ * A cache without pages (k NULL; then lens may be NULL, p = i, and V is not read) only turns.  Rows of no sequence are left alone.
+ * sp_cache_read: the values that the cache holds for the last n = cu[s+1] - cu[s] tokens of every sequence, rows as above, into K, V
+ * [N, n_kv_heads * d_head] (SP_BF16: rounded, or SP_F32).
+ * sp_cache_attention: sp_attention with the keys and values [0, lens[s]) of the cache: rows [cu_q[s], cu_q[s+1]) of Q and O, [Nq, n_heads * d_head], query i
+ * of n_q sees keys j <= i + lens[s] - n_q (causal != 0) or all.  d_head and head h / g of a query head as there, a query without a visible key gets
+ * O = 0 and lse = -infinity, rows of no sequence are left as they were, and what stands in slots that a query does not see does not reach it.
+ * 4 bits or 16, the values are those the cache stands for, products in fp32 of them (SP_BF16: probabilities, or their products with the scales, are
+ * rounded to bf16; with many rows per sequence the values themselves, too).  Softmax and sums in fp32.  Equal calls give equal bits.
+ * Many rows per sequence (more than 64 queries x heads of a key head, on average) open the pages in the workspace: max_keys tells how many keys all
+ * sequences with queries have at most (0: as many as the table holds); sequences that do not fit are reported like tokens without a page.
+ * Workspace: sp_cache_attention_bytes of the same numbers, scratch of this call alone.
+ * Errors: SP_ERR_INVALID_ARG (null pointers, unknown kind, scale outside [1e-30, 1e30], K_out in K's place), SP_ERR_SHAPE (sizes that do not match, ld or
+ * a step too small or odd, page_len, turned, more than 2^30 rows, tokens of a table or opened keys), SP_ERR_DTYPE, SP_ERR_UNSUPPORTED (d_head),
+ * SP_ERR_ALIGNMENT (pages and scales on 16 bytes, workspace on 256), SP_ERR_WORKSPACE.
+ */
+typedef enum { SP_CACHE_BF16 = 0, SP_CACHE_4BIT = 1 } sp_cache_kind;
+#define SP_CACHE_GROUP 64
+typedef struct {
+  void *k, *v;
+  void *k_scale, *v_scale;           /* SP_CACHE_4BIT */
+  int64_t k_step, v_step, k_scale_step, v_scale_step;
+  const int32_t* table;              /* [n_seq, max_pages], device */
+  const int32_t* lens;               /* [n_seq], device */
+  int64_t table_ld;
+  int32_t max_pages, n_seq, kind, n_pages, page_len, n_kv_heads, d_head, reserved;
+} sp_kv_cache;
+typedef struct {
+  sp_mat Q, K, V, Q_out, K_out;
+  const int32_t* cu;                 /* [n_seq + 1], device */
+  const int32_t* positions;          /* [N], device, or NULL */
+  const float* inv_freq;             /* [turned / 2], device */
+  int32_t n_heads, turned, neighbours, reserved;
+} sp_cache_append_args;
+sp_status sp_cache_append(const sp_kv_cache* cache, const sp_cache_append_args* a, int32_t* status_dev, void* stream);
+sp_status sp_cache_read(const sp_kv_cache* cache, const int32_t* cu, const sp_mat* K, const sp_mat* V, int32_t* status_dev,
+                        void* stream);
+sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const int32_t* cu_q, int32_t n_heads, int32_t causal, double scale,
+                             int64_t max_keys, const sp_mat* O, float* lse, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream);
+size_t sp_cache_attention_bytes(int64_t Nq, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t dtype,
+                                int32_t max_pages, int32_t page_len, int64_t max_keys);
 
 /* ---------------------------------------------------------------------------------------------------------------
  * Helpers.

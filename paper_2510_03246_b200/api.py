@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsp.so")
 
 SP_OK = 0
-SP_F32, SP_BF16, SP_F64 = 0, 1, 2
+SP_F32, SP_BF16, SP_F64, SP_E4M3 = 0, 1, 2, 3
 SP_ACT_RELU, SP_ACT_SWIGLU = 0, 1
 SP_Z_PAPER, SP_Z_EXACT = 0, 1
 SP_SCORE_WANDA_L2, SP_SCORE_WANDA_L1, SP_SCORE_LEMMA1 = 0, 1, 2
@@ -25,6 +25,8 @@ SP_ALLOC_SOFTMAX, SP_ALLOC_INVERSE, SP_ALLOC_UNIFORM = 0, 1, 2
 SP_LINEAR_NONE, SP_LINEAR_RELU, SP_LINEAR_SILU, SP_LINEAR_GELU = 0, 1, 2, 3
 SP_COMBINE_ADD, SP_COMBINE_MUL = 0, 1
 SP_MAX_ALTS = 32
+SP_CACHE_BF16, SP_CACHE_4BIT = 0, 1
+SP_CACHE_GROUP = 64
 (SP_WS_GRAM, SP_WS_ADMM_STEP, SP_WS_SCORES, SP_WS_APPLY_MASK, SP_WS_FFN_INIT, SP_WS_LINEAR_REFIT, SP_WS_GEMM,
  SP_WS_RIDGE_SOLVE) = range(8)
 
@@ -37,7 +39,9 @@ EXPORTS = ["sp_gram_accumulate", "sp_ffn_init", "sp_admm_step", "sp_admm_scores"
            "sp_set_reproducible", "sp_get_reproducible", "sp_allocate_sparsity_grid", "sp_apply_mask_global",
            "sp_apply_mask_global_bytes", "sp_objective_accumulate", "sp_ffn_cache_input_inverse",
            "sp_set_wait_budget", "sp_mha_value_refit", "sp_mha_value_refit_workspace_bytes",
-           "sp_attention", "sp_attention_workspace_bytes", "sp_linear", "sp_token_logprobs", "sp_token_logprobs_grad"]
+           "sp_attention", "sp_attention_workspace_bytes", "sp_linear", "sp_token_logprobs", "sp_token_logprobs_grad",
+           "sp_rms_norm", "sp_rms_norm_grad", "sp_rms_norm_grad_bytes", "sp_linear_e4m3", "sp_cache_append", "sp_cache_read",
+           "sp_cache_attention", "sp_cache_attention_bytes"]
 
 
 class SpError(RuntimeError):
@@ -96,6 +100,20 @@ class SpAttentionArgs(C.Structure):
     _fields_ = [("Q", SpMat), ("K", SpMat), ("V", SpMat), ("O", SpMat), ("cu_q", C.c_void_p), ("cu_k", C.c_void_p),
                 ("lse", C.c_void_p), ("n_seq", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("causal", C.c_int32), ("scale", C.c_double)]
+
+
+class SpKvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_step", C.c_int64),
+                ("v_step", C.c_int64), ("k_scale_step", C.c_int64), ("v_scale_step", C.c_int64), ("table", C.c_void_p),
+                ("lens", C.c_void_p), ("table_ld", C.c_int64), ("max_pages", C.c_int32), ("n_seq", C.c_int32), ("kind", C.c_int32),
+                ("n_pages", C.c_int32), ("page_len", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class SpCacheAppendArgs(C.Structure):
+    _fields_ = [("Q", SpMat), ("K", SpMat), ("V", SpMat), ("Q_out", SpMat), ("K_out", SpMat), ("cu", C.c_void_p),
+                ("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("n_heads", C.c_int32), ("turned", C.c_int32),
+                ("neighbours", C.c_int32), ("reserved", C.c_int32)]
 
 
 REPORT_FIELDS = ["res_act", "res_out", "res_in", "z_sq", "a_sq", "rho1_eff", "rho2_eff", "kept", "factor_reused",
@@ -157,6 +175,17 @@ def lib() -> C.CDLL:
         L.sp_linear.argtypes = [pm, pm, vp, i32, pm, i32, pm, vp, vp]
         L.sp_token_logprobs.argtypes = [pm, vp, dbl, i32, vp, vp, vp, vp, vp, vp, vp]
         L.sp_token_logprobs_grad.argtypes = [pm, vp, dbl, vp, vp, vp, vp, pm, vp]
+        L.sp_rms_norm.argtypes = [pm, pm, vp, dbl, pm, pm, vp, vp, vp]
+        L.sp_rms_norm_grad.argtypes = [pm, pm, vp, vp, dbl, pm, pm, vp, vp, sz, vp]
+        L.sp_rms_norm_grad_bytes.restype = C.c_size_t
+        L.sp_rms_norm_grad_bytes.argtypes = [i64, i64]
+        L.sp_linear_e4m3.argtypes = [pm, vp, pm, vp, vp, i32, pm, i32, pm, vp, vp]
+        pc = C.POINTER(SpKvCache)
+        L.sp_cache_append.argtypes = [pc, C.POINTER(SpCacheAppendArgs), vp, vp]
+        L.sp_cache_read.argtypes = [pc, vp, pm, pm, vp, vp]
+        L.sp_cache_attention.argtypes = [pc, pm, vp, i32, i32, dbl, i64, pm, vp, vp, vp, sz, vp]
+        L.sp_cache_attention_bytes.restype = C.c_size_t
+        L.sp_cache_attention_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32, i32, i64]
         L.sp_set_reproducible.argtypes = [i32]
         L.sp_set_wait_budget.argtypes = [i64]
         L.sp_get_reproducible.restype = i32
@@ -169,7 +198,8 @@ def lib() -> C.CDLL:
         for name in EXPORTS:
             if name not in ("sp_workspace_bytes", "sp_admm_overlap_bytes", "sp_mha_workspace_bytes",
                             "sp_mha_value_refit_workspace_bytes",
-                            "sp_apply_mask_global_bytes", "sp_attention_workspace_bytes", "sp_status_string", "sp_version", "sp_profile_kinds",
+                            "sp_apply_mask_global_bytes", "sp_attention_workspace_bytes", "sp_rms_norm_grad_bytes",
+                            "sp_cache_attention_bytes", "sp_status_string", "sp_version", "sp_profile_kinds",
                             "sp_profile_kind_name", "sp_launch_count"):
                 getattr(L, name).restype = C.c_int32
         _lib = L
@@ -621,6 +651,239 @@ def sp_token_logprobs_grad(logits, targets, lse, g_logp, entropy=None, g_entropy
                                         gh, C.byref(_rows(out, dev, "out")), torch._C._cuda_getCurrentRawStream(dev)),
            "sp_token_logprobs_grad")
     return out
+
+
+# ------------------------------------------------------------- norm, 8-bit projections, paged caches of keys and values
+_F8 = torch.float8_e4m3fn
+
+
+def _eight(t, dev, what):
+    """Matrix view of a 2-D e4m3 tensor whose rows are contiguous."""
+    if t.get_device() != dev:
+        _elsewhere(t)
+    if t.dtype != _F8 or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what} must be a row-major 2-D tensor of float8_e4m3fn")
+    rows, cols = t.shape
+    return SpMat(t.data_ptr(), SP_E4M3, 0, rows, cols, t.stride(0) if rows > 1 else max(cols, t.stride(0)))
+
+
+@dataclass
+class RmsNorm:
+    Y: torch.Tensor                     # [T, d] normed, of X's dtype or float8_e4m3fn
+    H: torch.Tensor | None              # [T, d] the stream, x + r (None without a residual)
+    scale: torch.Tensor | None          # fp32 [T] with float8_e4m3fn: y = Y * scale
+    rstd: torch.Tensor | None           # fp32 [T]
+
+
+def sp_rms_norm(X, weight=None, eps=1e-5, residual=None, h_out=None, out=None, out_dtype=None, want_rstd=False) -> RmsNorm:
+    """h = X + residual, y = weight h / sqrt(mean h^2 + eps) (see sp.h).  X [T, d] bf16 or fp32, residual of either, weight fp32 [d].
+    h_out: where to write h (residual or X itself: in place; allocated where there is a residual).  out_dtype
+    torch.float8_e4m3fn: 8 bits with a scale per row, rows that start on 16 bytes, as sp_linear_e4m3 reads them."""
+    dev = _current_device(X)
+    x = _rows(X, dev, "X")
+    r = None if residual is None else _rows(residual, dev, "residual")
+    if out is None:
+        out = rows_of_16_bytes(x.rows, x.cols, out_dtype or X.dtype, X.device)
+    if h_out is None and residual is not None:
+        h_out = torch.empty(x.rows, x.cols, dtype=residual.dtype, device=X.device)
+    eight = out.dtype == _F8
+    y = _eight(out, dev, "out") if eight else _rows(out, dev, "out")
+    h = None if h_out is None else _rows(h_out, dev, "h_out")
+    scale = torch.empty(x.rows, dtype=torch.float32, device=X.device) if eight else None
+    rstd = torch.empty(x.rows, dtype=torch.float32, device=X.device) if want_rstd else None
+    _check(lib().sp_rms_norm(C.byref(x), None if r is None else C.byref(r), _vector(weight, torch.float32, x.cols, dev, "weight"), eps,
+                             None if h is None else C.byref(h), C.byref(y), _ptr(scale), _ptr(rstd),
+                             torch._C._cuda_getCurrentRawStream(dev)), "sp_rms_norm")
+    return RmsNorm(out, h_out, scale, rstd)
+
+
+def sp_rms_norm_grad(dY, H, weight=None, rstd=None, eps=1e-5, d_stream=None, want_weight=True, out=None, ws=None):
+    """Gradient of sp_rms_norm with respect to h (so to x and to the residual) and to the weight (see sp.h): dY [T, d] the gradient of
+    y, H and rstd as the forward call left them (rstd None: formed again), d_stream the gradient that arrives at h by itself.  out may be
+    d_stream.  Returns (dX of H's dtype, dweight fp32 [d] or None)."""
+    dev = _current_device(dY)
+    g, h = _rows(dY, dev, "dY"), _rows(H, dev, "H")
+    if out is None:
+        out = torch.empty(g.rows, g.cols, dtype=H.dtype, device=dY.device)
+    d = None if d_stream is None else _rows(d_stream, dev, "d_stream")
+    dw = torch.empty(g.cols, dtype=torch.float32, device=dY.device) if want_weight else None
+    if ws is None:
+        ws = _ws(lib().sp_rms_norm_grad_bytes(g.rows, g.cols), dY.device) if want_weight else None
+    elif ws.get_device() != dev:
+        _elsewhere(ws)
+    _check(lib().sp_rms_norm_grad(C.byref(g), C.byref(h), _vector(weight, torch.float32, g.cols, dev, "weight"),
+                                  _vector(rstd, torch.float32, g.rows, dev, "rstd"), eps, None if d is None else C.byref(d),
+                                  C.byref(_rows(out, dev, "out")), _ptr(dw), _ptr(ws), ws.nbytes if ws is not None else 0,
+                                  torch._C._cuda_getCurrentRawStream(dev)), "sp_rms_norm_grad")
+    return out, dw
+
+
+def sp_linear_e4m3(X, x_scale, W, w_scale, bias=None, act=SP_LINEAR_NONE, other=None, combine=SP_COMBINE_ADD, out=None,
+                   out_dtype=torch.bfloat16, status=None):
+    """act(x_scale w_scale X W^T + bias), then other added or multiplied (see sp.h).  X [T, in], W [out, in]: float8_e4m3fn, rows that start
+    on 16 bytes; x_scale fp32 [T] (sp_rms_norm), w_scale fp32 [out].  The result is bf16 or fp32."""
+    dev = _current_device(X)
+    x, w = _eight(X, dev, "X"), _eight(W, dev, "W")
+    if out is None:
+        out = rows_of_16_bytes(x.rows, w.rows, out_dtype, X.device)
+    o = None if other is None else C.byref(_rows(other, dev, "other"))
+    _check(lib().sp_linear_e4m3(C.byref(x), _vector(x_scale, torch.float32, x.rows, dev, "x_scale"), C.byref(w),
+                                _vector(w_scale, torch.float32, w.rows, dev, "w_scale"),
+                                _vector(bias, torch.float32, w.rows, dev, "bias"), act, o, combine, C.byref(_rows(out, dev, "out")),
+                                _vector(status, torch.int32, 4, dev, "status"), torch._C._cuda_getCurrentRawStream(dev)),
+           "sp_linear_e4m3")
+    return out
+
+
+@dataclass
+class KvPages:
+    """Pages of keys and values of one module: bf16 [n_pages, n_kv_heads, page_len, d_head], or 4 bits: uint8 [.., d_head / 2] with
+    bf16 scales [n_pages, n_kv_heads, page_len, d_head / 64, 2] (see sp.h).  A page's entries are contiguous; pages may lie any multiple of 16
+    bytes apart, so that those of several modules can be slices of one buffer."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor | None = None
+    v_scale: torch.Tensor | None = None
+
+    @staticmethod
+    def empty(n_pages, n_kv_heads, page_len, d_head, four_bits=False, device="cuda") -> "KvPages":
+        """Uninitialised pages (what is not appended is not read)."""
+        def of(*last, dtype):
+            return torch.empty(n_pages, n_kv_heads, page_len, *last, dtype=dtype, device=device)
+        if not four_bits:
+            return KvPages(of(d_head, dtype=torch.bfloat16), of(d_head, dtype=torch.bfloat16))
+        g = d_head // SP_CACHE_GROUP
+        return KvPages(of(d_head // 2, dtype=torch.uint8), of(d_head // 2, dtype=torch.uint8), of(g, 2, dtype=torch.bfloat16),
+                       of(g, 2, dtype=torch.bfloat16))
+
+    def view(self, dev, table, lens) -> SpKvCache:
+        k, v = self.k, self.v
+        four = k.dtype == torch.uint8
+        if not four and k.dtype != torch.bfloat16:
+            raise ValueError("pages are bf16 or uint8")
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("k and v must be [n_pages, n_kv_heads, page_len, d_head] of one shape and dtype")
+        n_pages, n_kv, page_len, d = k.shape
+        d_head = 2 * d if four else d
+        pages = [k, v]
+        if four:
+            want = (n_pages, n_kv, page_len, d_head // SP_CACHE_GROUP, 2)
+            for t in (self.k_scale, self.v_scale):
+                if t is None or t.shape != want or t.dtype != torch.bfloat16:
+                    raise ValueError(f"k_scale and v_scale must be bf16 {list(want)}")
+            pages += [self.k_scale, self.v_scale]
+        steps = []
+        for t in pages:
+            if t.get_device() != dev:
+                _elsewhere(t)
+            inner, stride, shape = 1, t.stride(), t.shape
+            for i in range(len(shape) - 1, 0, -1):
+                if stride[i] != inner and shape[i] > 1:
+                    raise ValueError("the entries of a page must be contiguous")
+                inner *= shape[i]
+            steps.append((stride[0] if n_pages > 1 else inner) * t.element_size())
+        if not four:
+            steps += [0, 0]
+        if table.dim() != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and table.shape[1] > 1):
+            raise ValueError("table must be int32 [n_seq, pages] with contiguous rows")
+        if table.get_device() != dev:
+            _elsewhere(table)
+        n_seq, max_pages = table.shape
+        return SpKvCache(k.data_ptr(), v.data_ptr(), _ptr(self.k_scale) if four else None, _ptr(self.v_scale) if four else None, *steps,
+                         table.data_ptr(), _vector(lens, torch.int32, n_seq, dev, "lens"),
+                         table.stride(0) if n_seq > 1 else max_pages, max_pages, n_seq, SP_CACHE_4BIT if four else SP_CACHE_BF16,
+                         n_pages, page_len, n_kv, d_head, 0)
+
+
+def sp_cache_append(pages, K, V, cu, table, lens, Q=None, inv_freq=None, neighbours=False, positions=None, q_out=None, k_out=None,
+                    want_k=False, status=None, d_head=None):
+    """Puts the rows [cu[s], cu[s+1]) of K, V [N, n_kv_heads * d_head], the last tokens of sequence s, into its pages, keys (and the queries Q
+    [N, n_heads * d_head]) turned by their positions on the way (see sp.h).  table int32 [n_seq, pages of a sequence], lens int32
+    [n_seq] with these tokens.  inv_freq fp32 [turned / 2]: frequencies of the turned channels, None: nothing is turned; pairs are halves apart,
+    or neighbours.  positions int32 [N]: others than the places.  q_out: where the turned queries go (Q itself: in place; allocated otherwise);
+    k_out, want_k: the turned keys, too.  pages None (then d_head is needed, table and V may be None): turns only.
+    Returns the turned queries (None without Q), and with want_k or k_out (queries, keys)."""
+    dev = _current_device(K)
+    k = _rows(K, dev, "K")
+    N = k.rows
+    n_seq = cu.numel() - 1
+    if n_seq < 0:
+        raise ValueError("cu holds n_seq + 1 offsets")
+    if pages is not None:
+        c = pages.view(dev, table, lens)
+        if c.n_seq != n_seq:
+            raise ValueError("cu, table and lens are of one number of sequences")
+        d_head, v = c.d_head, _rows(V, dev, "V")
+    else:
+        if not d_head or k.cols % d_head:
+            raise ValueError("d_head of the keys")
+        c = SpKvCache(lens=_vector(lens, torch.int32, n_seq, dev, "lens"), n_seq=n_seq, n_kv_heads=k.cols // d_head, d_head=d_head)
+        v = SpMat()
+    q = qo = ko = SpMat()
+    n_heads = 0
+    if Q is not None:
+        if q_out is None:
+            q_out = torch.empty(N, Q.shape[1], dtype=Q.dtype, device=Q.device)
+        q, qo, n_heads = _rows(Q, dev, "Q"), _rows(q_out, dev, "q_out"), Q.shape[1] // max(d_head, 1)
+    if k_out is None and want_k:
+        k_out = torch.empty(N, k.cols, dtype=K.dtype, device=K.device)
+    if k_out is not None:
+        ko = _rows(k_out, dev, "k_out")
+    turned = 0 if inv_freq is None else 2 * inv_freq.numel()
+    args = SpCacheAppendArgs(q, k, v, qo, ko, _vector(cu, torch.int32, n_seq + 1, dev, "cu"),
+                             _vector(positions, torch.int32, N, dev, "positions"),
+                             _vector(inv_freq, torch.float32, turned // 2, dev, "inv_freq") if turned else None, n_heads, turned,
+                             int(bool(neighbours)), 0)
+    _check(lib().sp_cache_append(C.byref(c), C.byref(args), _vector(status, torch.int32, 4, dev, "status"),
+                                 torch._C._cuda_getCurrentRawStream(dev)), "sp_cache_append")
+    return (q_out, k_out) if k_out is not None else q_out
+
+
+def sp_cache_read(pages, cu, table, lens, rows, dtype=torch.bfloat16, K=None, V=None, status=None):
+    """The values that the cache holds for the last cu[s+1] - cu[s] tokens of every sequence (see sp.h).  Returns (K, V) [rows, n_kv_heads *
+    d_head] of bf16 or fp32; rows of no sequence stay as they are (in buffers allocated here they are undefined)."""
+    dev = _current_device(pages.k)
+    c = pages.view(dev, table, lens)
+    if cu.numel() - 1 != c.n_seq:
+        raise ValueError("cu, table and lens are of one number of sequences")
+    cols = c.n_kv_heads * c.d_head
+    K, V = (torch.empty(rows, cols, dtype=dtype, device=pages.k.device) if t is None else t for t in (K, V))
+    _check(lib().sp_cache_read(C.byref(c), _vector(cu, torch.int32, c.n_seq + 1, dev, "cu"), C.byref(_rows(K, dev, "K")),
+                               C.byref(_rows(V, dev, "V")), _vector(status, torch.int32, 4, dev, "status"),
+                               torch._C._cuda_getCurrentRawStream(dev)), "sp_cache_read")
+    return K, V
+
+
+@functools.lru_cache(maxsize=256)
+def _cache_attention_bytes(*sizes):      # (a function of the sizes alone)
+    return int(lib().sp_cache_attention_bytes(*sizes))
+
+
+def sp_cache_attention(Q, pages, cu_q, table, lens, n_heads, causal=True, scale=None, max_keys=0, out=None, lse=None, want_lse=False,
+                       ws=None, status=None):
+    """sp_attention over the keys and values of a paged cache (see sp.h): rows [cu_q[s], cu_q[s+1]) of Q [Nq, n_heads * d_head] against the
+    lens[s] tokens of sequence s.  max_keys: how many keys all sequences have together, at most, as the caller knows it (0: as many as the
+    table holds); calls with many rows per sequence size their workspace by it.  Returns (O, lse or None)."""
+    dev = _current_device(Q)
+    c = pages.view(dev, table, lens)
+    q = _rows(Q, dev, "Q")
+    if out is None:
+        out = torch.empty(q.rows, q.cols, dtype=Q.dtype, device=Q.device)
+    if lse is None and want_lse:
+        lse = torch.empty(q.rows, n_heads, dtype=torch.float32, device=Q.device)
+    if scale is None:
+        scale = max(c.d_head, 1) ** -0.5
+    if ws is None:
+        need = _cache_attention_bytes(q.rows, c.n_seq, n_heads, c.n_kv_heads, c.d_head, q.dtype, c.max_pages, c.page_len, max_keys)
+        ws = _ws(need, Q.device) if need else None
+    elif ws.get_device() != dev:
+        _elsewhere(ws)
+    _check(lib().sp_cache_attention(C.byref(c), C.byref(q), _vector(cu_q, torch.int32, c.n_seq + 1, dev, "cu_q"), n_heads,
+                                    int(bool(causal)), scale, max_keys, C.byref(_rows(out, dev, "out")),
+                                    _vector(lse, torch.float32, q.rows * n_heads, dev, "lse"),
+                                    _vector(status, torch.int32, 4, dev, "status"), _ptr(ws), ws.nbytes if ws is not None else 0,
+                                    torch._C._cuda_getCurrentRawStream(dev)), "sp_cache_attention")
+    return out, lse
 
 
 # ---------------------------------------------------------------------------------------------- module driver

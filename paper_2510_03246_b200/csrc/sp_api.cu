@@ -446,6 +446,8 @@ sp_status sp_gemm(int32_t transA, int32_t transB, int64_t M, int64_t N, int64_t 
                   int32_t* status_dev, void* stream) {
   if (!A || !B || !C || !A->ptr || !B->ptr || !C->ptr) return SP_ERR_INVALID_ARG;
   if (M < 0 || N < 0 || K < 0) return SP_ERR_SHAPE;
+  for (const sp_mat* m : {A, B, C})
+    if (m->dtype < SP_F32 || m->dtype > SP_F64) return SP_ERR_DTYPE;
   // op(A) is M x K: stored [M,K] when !transA (K-major), [K,M] when transA.
   // op(B) is K x N: stored [K,N] when !transB (N contiguous), [N,K] when transB (K-major).
   const bool a_kmajor = !transA, b_kmajor = transB != 0;

@@ -1,0 +1,467 @@
+// Appending to a paged cache with the rotation of positions on the way, and reading it back.
+//
+// Token i of the n that a call brings to sequence s stands at p = lens[s] - n + i and goes to slot p % page_len of page table[s][p / page_len].
+// Rotation: channels (a, b) of a pair with frequency f become (a cos - b sin, b cos + a sin), angle p f.  The angle is taken in 64 bits and
+// in whole turns away first: at p = 10^5 an angle in 32 bits would be off by 10^-2.
+// 4 bits: of every 64 channels of a head, zero = bf16(least), scale = bf16((largest - zero) / 15), n = (x - zero) / scale rounded to the
+// nearest of 0 .. 15.  Rotated keys are kept in 64 bits up to there: a value next to the border of two steps falls on the side on which the
+// formula has it, whatever order the sums were taken in.
+//
+// Both kernels are bound by memory (append: 16384 x (32 + 2 x 8) heads of 128: 200 MB in, 150 MB out); a thread has eight channels at a time,
+// 16 bytes of bf16, four bytes of a page in 4 bits; the eight lanes of a group find its bounds by shuffles.
+#include <math.h>
+
+#include "sp_cache.cuh"
+
+namespace sp {
+namespace {
+
+constexpr int kAppendThreads = 256;
+constexpr int kMaxTurned = 128;
+
+struct AppendParams {
+  CacheView c;
+  const void *q, *k, *v;
+  void *q_out, *k_out;
+  int64_t ldq, ldk, ldv, ldqo, ldko;
+  const int32_t* cu;
+  const int32_t* positions;
+  const float* inv_freq;
+  int32_t rows, n_heads, turned, neighbours;
+  int32_t q_vec, k_vec, v_vec;             // rows start on 16 bytes
+  int32_t* status;
+};
+
+// eight values from p on, in fp32
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, bool vec, float (&x)[8]);
+template <>
+__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, bool vec, float (&x)[8]) {
+  if (vec) {
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
+  }
+}
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, bool vec, float (&x)[8]) {
+  if (vec) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = p[i];
+  }
+}
+__device__ __forceinline__ void put8(__nv_bfloat16* p, bool vec, const float (&x)[8]) {
+  if (vec) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 e = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      u[i] = *reinterpret_cast<const uint32_t*>(&e);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(x[i]);
+  }
+}
+__device__ __forceinline__ void put8(float* p, bool vec, const float (&x)[8]) {
+  if (vec) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = x[i];
+  }
+}
+
+// The eight lanes of a group hold eight channels each: their 4-bit numbers packed, and the group's scale and offset in lane 0 of the eight.
+// F: float where the values are what the caller gave, double for rotated ones (see above).
+template <typename F>
+__device__ __forceinline__ uint32_t four_bits(const F (&x)[8], uint32_t& pair) {
+  F lo = x[0], hi = x[0];
+  bool odd = false;                        // a NaN or an infinity
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo = x[i] < lo ? x[i] : lo;
+    hi = x[i] > hi ? x[i] : hi;
+    odd |= !(x[i] - x[i] == (F)0);
+  }
+#pragma unroll
+  for (int w = 1; w < 8; w <<= 1) {
+    const F a = __shfl_xor_sync(0xffffffffu, lo, w), b = __shfl_xor_sync(0xffffffffu, hi, w);
+    lo = a < lo ? a : lo;
+    hi = b > hi ? b : hi;
+  }
+  const uint32_t eight = (__ballot_sync(0xffffffffu, odd) >> (threadIdx.x & 24)) & 0xffu;
+  const float zero = __bfloat162float(__float2bfloat16_rn((float)lo));
+  const float scale = __bfloat162float(__float2bfloat16_rn((float)(((double)hi - (double)zero) / 15.0)));
+  if (eight != 0u) {                       // (the offset reads back as NaN whatever the numbers are)
+    pair = 0x7fc07fc0u;
+    return 0u;
+  }
+  pair = (__float_as_uint(scale) >> 16) | (__float_as_uint(zero) & 0xffff0000u);
+  if (!(scale > 0.f)) return 0u;
+  const bool tiny = scale < 1e-36f;        // its reciprocal, or a product with it, may leave the range of fp32
+  const float inv = tiny ? 0.f : 1.f / scale;
+  uint32_t packed = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const F d = x[i] - (F)zero;            // (of two fp32 values: rounded once)
+    const float t = (float)d * inv;        // within 2^-22 of the quotient
+    float n = rintf(t);
+    if (tiny || fabsf(fabsf(t - n) - 0.5f) < 1e-4f) n = (float)rint(((double)x[i] - (double)zero) / (double)scale);
+    n = fminf(fmaxf(n, 0.f), 15.f);
+    packed |= (uint32_t)n << (4 * i);
+  }
+  return packed;
+}
+
+template <typename T, bool FOUR>
+__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const AppendParams p) {
+  kernel_begin();
+  __shared__ float2 s_turn[kMaxTurned / 2];                      // cos, sin of the row's angles
+  __shared__ double2 s_exact[FOUR ? kMaxTurned / 2 : 1];         // the same in 64 bits, for keys that go to 4 bits
+  const int32_t row = blockIdx.x;
+  const int32_t s = sequence_of(p.cu, p.c.n_seq, p.rows, row);
+  if (s < 0) return;                                             // (the same answer in every warp)
+  const int32_t i = row - bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - (row - i);
+  const int32_t place = p.c.lens ? p.c.lens[s] - n + i : i;
+  int32_t page = -1, slot = 0;
+  if (p.c.k) {
+    const int32_t entry = place >= 0 ? place / p.c.page_len : -1;
+    page = page_of(p.c, s, entry);
+    slot = place - entry * p.c.page_len;
+    if (page < 0 && threadIdx.x == 0) report_status(p.status, SP_ERR_SHAPE, s, row);
+  }
+  const int half = p.turned / 2, dh = p.c.dh;
+  if (half > 0) {
+    const double position = (double)(p.positions ? p.positions[row] : place);
+    for (int f = threadIdx.x; f < half; f += kAppendThreads) {
+      const double turns = position * (double)p.inv_freq[f] * 0.15915494309189533577;      // angle / 2 pi
+      double sn, cs;
+      if (FOUR) {
+        sincospi(2.0 * (turns - rint(turns)), &sn, &cs);
+        s_exact[f] = make_double2(cs, sn);
+        s_turn[f] = make_float2((float)cs, (float)sn);
+      } else {
+        float snf, csf;
+        sincospif((float)(2.0 * (turns - rint(turns))), &snf, &csf);
+        s_turn[f] = make_float2(csf, snf);
+      }
+    }
+    __syncthreads();
+  }
+  const int per_head = dh / 8, half8 = half / 8, turned8 = p.turned / 8;
+  // queries: a thread has both chunks of a pair, so that a row may be turned in its place
+  if (p.q) {
+    const T* q = reinterpret_cast<const T*>(p.q) + row * p.ldq;
+    T* out = reinterpret_cast<T*>(p.q_out) + row * p.ldqo;
+    const bool vec = p.q_vec != 0;
+    const int apart = p.neighbours ? 0 : half8;                  // pairs of chunks: chunk and chunk + apart
+    const int units = per_head - apart;
+    for (int e = threadIdx.x; e < p.n_heads * units; e += kAppendThreads) {
+      const int head = e / units, u = e % units;
+      const int chunk = u < apart || apart == 0 ? u : u + apart;
+      const T* src = q + head * dh;
+      T* dst = out + head * dh;
+      float a[8], b[8];
+      load8(src + 8 * chunk, vec, a);
+      if (chunk >= turned8) {
+        put8(dst + 8 * chunk, vec, a);
+      } else if (apart > 0) {
+        load8(src + 8 * (chunk + apart), vec, b);
+        float x[8], y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float2 cs = s_turn[8 * chunk + k];
+          x[k] = fmaf(a[k], cs.x, -b[k] * cs.y);
+          y[k] = fmaf(b[k], cs.x, a[k] * cs.y);
+        }
+        put8(dst + 8 * chunk, vec, x);
+        put8(dst + 8 * (chunk + apart), vec, y);
+      } else {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 cs = s_turn[4 * chunk + k];
+          x[2 * k] = fmaf(a[2 * k], cs.x, -a[2 * k + 1] * cs.y);
+          x[2 * k + 1] = fmaf(a[2 * k + 1], cs.x, a[2 * k] * cs.y);
+        }
+        put8(dst + 8 * chunk, vec, x);
+      }
+    }
+  }
+  // keys: eight channels as they stand side by side in the cache, their partners read beside them; then values
+  const int chunks = p.c.n_kv * per_head, all = (chunks + 31) / 32 * 32;      // (groups of eight lanes stay together)
+  const bool pages = page >= 0;
+  for (int e = threadIdx.x; e < all; e += kAppendThreads) {
+    const bool live = e < chunks;
+    const int head = live ? e / per_head : 0, chunk = live ? e % per_head : 0;
+    const T* src = reinterpret_cast<const T*>(p.k) + row * p.ldk + head * dh;
+    const bool vec = p.k_vec != 0;
+    float a[8], b[8];
+    load8(src + 8 * chunk, vec, a);
+    using F = typename std::conditional<FOUR, double, float>::type;
+    F x[8];
+    if (chunk >= turned8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = (F)a[k];
+    } else {
+      const bool second = !p.neighbours && chunk >= half8;       // the pair's other value stands `half` channels before, or behind
+      if (!p.neighbours) load8(src + 8 * (second ? chunk - half8 : chunk + half8), vec, b);
+      const int f0 = p.neighbours ? 4 * chunk : 8 * (second ? chunk - half8 : chunk);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int f = p.neighbours ? f0 + k / 2 : f0 + k;
+        const float other = p.neighbours ? a[k ^ 1] : b[k];
+        const bool up = p.neighbours ? (k & 1) != 0 : second;
+        F c, w;
+        if constexpr (FOUR) {
+          c = s_exact[f].x; w = s_exact[f].y;
+        } else {
+          c = s_turn[f].x; w = s_turn[f].y;
+        }
+        const F m = (F)other * w;
+        x[k] = fma((F)a[k], c, up ? m : -m);
+      }
+    }
+    if (p.k_out && live) {
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = (float)x[k];
+      put8(reinterpret_cast<T*>(p.k_out) + row * p.ldko + head * dh + 8 * chunk, vec, y);
+    }
+    if (!p.c.k) continue;                                        // (the same in every thread, as `pages`)
+    const int64_t at = (int64_t)head * p.c.page_len + slot;      // (head, token) of the page
+    if constexpr (FOUR) {
+      uint32_t pair;
+      const uint32_t packed = four_bits(x, pair);
+      if (pages && live) {
+        *reinterpret_cast<uint32_t*>(p.c.k + page * p.c.k_step + at * (dh / 2) + 4 * chunk) = packed;
+        if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.ks + page * p.c.ks_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
+      }
+    } else if (pages && live) {
+      put8(reinterpret_cast<__nv_bfloat16*>(p.c.k + page * p.c.k_step) + at * dh + 8 * chunk, true, x);
+    }
+  }
+  if (!p.c.k) return;
+  for (int e = threadIdx.x; e < all; e += kAppendThreads) {
+    const bool live = e < chunks;
+    const int head = live ? e / per_head : 0, chunk = live ? e % per_head : 0;
+    float x[8];
+    load8(reinterpret_cast<const T*>(p.v) + row * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, x);
+    const int64_t at = (int64_t)head * p.c.page_len + slot;
+    if constexpr (FOUR) {
+      uint32_t pair;
+      const uint32_t packed = four_bits(x, pair);
+      if (pages && live) {
+        *reinterpret_cast<uint32_t*>(p.c.v + page * p.c.v_step + at * (dh / 2) + 4 * chunk) = packed;
+        if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.vs + page * p.c.vs_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
+      }
+    } else if (pages && live) {
+      put8(reinterpret_cast<__nv_bfloat16*>(p.c.v + page * p.c.v_step) + at * dh + 8 * chunk, true, x);
+    }
+  }
+}
+
+struct ReadParams {
+  CacheView c;
+  const int32_t* cu;
+  void *k, *v;
+  int64_t ldk, ldv;
+  int32_t rows, whole, k_vec, v_vec;
+  int32_t* status;
+};
+
+// a warp per row: eight channels of keys and of values at a time in every lane
+template <typename T, bool FOUR>
+__global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
+  kernel_begin();
+  const int lane = threadIdx.x & 31;
+  const int32_t row = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= p.rows) return;
+  const int32_t s = sequence_of(p.cu, p.c.n_seq, p.rows, row);
+  if (s < 0) return;
+  const int32_t i = row - bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - (row - i);
+  const int32_t length = p.c.lens[s], place = length - n + i;
+  const int32_t entry = place >= 0 ? place / p.c.page_len : -1;
+  int32_t page = p.whole && n != length ? -1 : page_of(p.c, s, entry);
+  const int32_t slot = place - entry * p.c.page_len;
+  if (page < 0 && lane == 0) report_status(p.status, SP_ERR_SHAPE, s, entry);
+  const int dh = p.c.dh, per_head = dh / 8, chunks = p.c.n_kv * per_head;
+#pragma unroll 2
+  for (int e = lane; e < chunks; e += 32) {
+    const int head = e / per_head, chunk = e % per_head;
+    const int64_t at = (int64_t)head * p.c.page_len + slot;
+    float x[8], y[8];
+    if (page < 0) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = y[k] = NAN;
+    } else if constexpr (FOUR) {
+      const uint32_t a = *reinterpret_cast<const uint32_t*>(p.c.k + page * p.c.k_step + at * (dh / 2) + 4 * chunk);
+      const uint32_t b = *reinterpret_cast<const uint32_t*>(p.c.v + page * p.c.v_step + at * (dh / 2) + 4 * chunk);
+      const int64_t g = (at * (dh / kCacheGroup) + chunk / 8) * 4;
+      const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + page * p.c.ks_step + g);
+      const uint32_t sb = *reinterpret_cast<const uint32_t*>(p.c.vs + page * p.c.vs_step + g);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        x[k] = fmaf((float)((a >> (4 * k)) & 15u), __uint_as_float(sa << 16), __uint_as_float(sa & 0xffff0000u));
+        y[k] = fmaf((float)((b >> (4 * k)) & 15u), __uint_as_float(sb << 16), __uint_as_float(sb & 0xffff0000u));
+      }
+    } else {
+      load8(reinterpret_cast<const __nv_bfloat16*>(p.c.k + page * p.c.k_step) + at * dh + 8 * chunk, true, x);
+      load8(reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.v_step) + at * dh + 8 * chunk, true, y);
+    }
+    put8(reinterpret_cast<T*>(p.k) + row * p.ldk + head * dh + 8 * chunk, p.k_vec != 0, x);
+    put8(reinterpret_cast<T*>(p.v) + row * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, y);
+  }
+}
+
+bool rows_of_16(const void* ptr, int64_t ld, int32_t dtype, int64_t rows) {
+  return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0 && (rows < 2 || ld * (int64_t)dtype_size(dtype) % 16 == 0);
+}
+bool step_fits(int64_t step, int64_t page_bytes, int32_t n_pages) { return step % 16 == 0 && (n_pages < 2 || step >= page_bytes); }
+
+}  // namespace
+
+sp_status check_cache(const sp_kv_cache* c, bool pages) {
+  if (!c) return SP_ERR_INVALID_ARG;
+  if (c->kind != SP_CACHE_BF16 && c->kind != SP_CACHE_4BIT) return SP_ERR_INVALID_ARG;
+  if (c->n_kv_heads < 1 || c->n_kv_heads > (1 << 16) || c->d_head < 1 || c->n_seq < 0) return SP_ERR_SHAPE;
+  if (c->d_head > 128 || c->d_head % (c->kind == SP_CACHE_4BIT ? kCacheGroup : 16) != 0) return SP_ERR_UNSUPPORTED;
+  if (!c->k) return pages ? SP_ERR_INVALID_ARG : SP_OK;
+  const bool four = c->kind == SP_CACHE_4BIT;
+  if (!c->v || (four && (!c->k_scale || !c->v_scale))) return SP_ERR_INVALID_ARG;
+  if (c->n_seq > 0 && (!c->table || !c->lens)) return SP_ERR_INVALID_ARG;
+  if (c->n_pages < 1 || c->page_len < 16 || c->page_len > 65536 || c->page_len % 16 != 0 || c->max_pages < 0 ||
+      (int64_t)c->max_pages * c->page_len > (1 << 30) || (c->n_seq > 1 && c->table_ld < c->max_pages))
+    return SP_ERR_SHAPE;
+  const int64_t tokens = (int64_t)c->n_kv_heads * c->page_len, bytes = tokens * (four ? c->d_head / 2 : 2 * c->d_head);
+  if (!step_fits(c->k_step, bytes, c->n_pages) || !step_fits(c->v_step, bytes, c->n_pages)) return SP_ERR_SHAPE;
+  const int64_t scales = tokens * (c->d_head / kCacheGroup) * 4;
+  if (four && (!step_fits(c->k_scale_step, scales, c->n_pages) || !step_fits(c->v_scale_step, scales, c->n_pages))) return SP_ERR_SHAPE;
+  for (const void* ptr : {c->k, c->v, four ? c->k_scale : nullptr, four ? c->v_scale : nullptr})
+    if (reinterpret_cast<uintptr_t>(ptr) & 15u) return SP_ERR_ALIGNMENT;
+  return SP_OK;
+}
+
+CacheView cache_view(const sp_kv_cache* c) {
+  CacheView w = {};
+  w.k = reinterpret_cast<uint8_t*>(c->k); w.v = reinterpret_cast<uint8_t*>(c->v);
+  w.ks = reinterpret_cast<uint8_t*>(c->k_scale); w.vs = reinterpret_cast<uint8_t*>(c->v_scale);
+  w.k_step = c->k_step; w.v_step = c->v_step; w.ks_step = c->k_scale_step; w.vs_step = c->v_scale_step;
+  w.table = c->table; w.lens = c->lens; w.table_ld = c->table_ld;
+  w.n_pages = c->n_pages; w.page_len = c->page_len; w.max_pages = c->max_pages;
+  w.n_kv = c->n_kv_heads; w.dh = c->d_head; w.n_seq = c->n_seq;
+  return w;
+}
+
+cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
+                       bool whole, int32_t* status, cudaStream_t stream) {
+  ReadParams p = {};
+  p.c = cache_view(c);
+  p.cu = cu;
+  p.k = K; p.v = V; p.ldk = ldk; p.ldv = ldv;
+  p.rows = (int32_t)rows;
+  p.whole = whole ? 1 : 0;
+  p.k_vec = rows_of_16(K, ldk, dtype, rows); p.v_vec = rows_of_16(V, ldv, dtype, rows);
+  p.status = status;
+  count_launch();
+  const dim3 grid((unsigned)ceil_div(rows, (int64_t)8));
+  const bool four = c->kind == SP_CACHE_4BIT;
+  if (dtype == SP_F32)
+    return four ? launch(cache_read_kernel<float, true>, grid, dim3(256), 0, stream, p)
+                : launch(cache_read_kernel<float, false>, grid, dim3(256), 0, stream, p);
+  return four ? launch(cache_read_kernel<__nv_bfloat16, true>, grid, dim3(256), 0, stream, p)
+              : launch(cache_read_kernel<__nv_bfloat16, false>, grid, dim3(256), 0, stream, p);
+}
+
+}  // namespace sp
+
+extern "C" {
+
+sp_status sp_cache_append(const sp_kv_cache* cache, const sp_cache_append_args* a, int32_t* status_dev, void* stream) {
+  using namespace sp;
+  if (!a) return SP_ERR_INVALID_ARG;
+  const sp_status ok = check_cache(cache, false);
+  if (ok != SP_OK) return ok;
+  const int32_t dt = a->K.dtype;
+  if (dt != SP_F32 && dt != SP_BF16) return SP_ERR_DTYPE;
+  const bool pages = cache->k != nullptr;
+  const int64_t N = a->K.rows, kv = (int64_t)cache->n_kv_heads * cache->d_head;
+  if (N < 0 || N > (1 << 30) || a->K.cols != kv || (N > 1 && a->K.ld < kv)) return SP_ERR_SHAPE;
+  if (pages) {
+    if (a->V.dtype != dt) return SP_ERR_DTYPE;
+    if (a->V.rows != N || a->V.cols != kv || (N > 1 && a->V.ld < kv)) return SP_ERR_SHAPE;
+  }
+  const bool queries = a->Q.ptr != nullptr || a->Q_out.ptr != nullptr, keys = a->K_out.ptr != nullptr;
+  if (queries) {
+    if (!a->Q.ptr || !a->Q_out.ptr) return SP_ERR_INVALID_ARG;
+    if (a->Q.dtype != dt || a->Q_out.dtype != dt) return SP_ERR_DTYPE;
+    const int64_t q = (int64_t)a->n_heads * cache->d_head;
+    if (a->n_heads < 1 || a->n_heads > (1 << 16)) return SP_ERR_SHAPE;
+    for (const sp_mat* m : {&a->Q, &a->Q_out})
+      if (m->rows != N || m->cols != q || (N > 1 && m->ld < q)) return SP_ERR_SHAPE;
+    if (a->Q.ptr == a->Q_out.ptr && N > 1 && a->Q.ld != a->Q_out.ld) return SP_ERR_INVALID_ARG;
+  }
+  if (keys) {
+    if (a->K_out.dtype != dt) return SP_ERR_DTYPE;
+    if (a->K_out.rows != N || a->K_out.cols != kv || (N > 1 && a->K_out.ld < kv)) return SP_ERR_SHAPE;
+    if (a->K_out.ptr == a->K.ptr) return SP_ERR_INVALID_ARG;      // (a key's partner may be read after it is written)
+  }
+  if (a->turned < 0 || a->turned > cache->d_head || a->turned % 16 != 0) return SP_ERR_SHAPE;
+  if (a->turned > 0 && !a->inv_freq) return SP_ERR_INVALID_ARG;
+  if (N == 0 || cache->n_seq == 0) return SP_OK;
+  if (!a->K.ptr || !a->cu || (pages && !a->V.ptr)) return SP_ERR_INVALID_ARG;
+  AppendParams p = {};
+  p.c = cache_view(cache);
+  p.q = a->Q.ptr; p.k = a->K.ptr; p.v = a->V.ptr; p.q_out = a->Q_out.ptr; p.k_out = a->K_out.ptr;
+  p.ldq = a->Q.ld; p.ldk = a->K.ld; p.ldv = a->V.ld; p.ldqo = a->Q_out.ld; p.ldko = a->K_out.ld;
+  p.cu = a->cu; p.positions = a->positions; p.inv_freq = a->inv_freq;
+  p.rows = (int32_t)N; p.n_heads = a->n_heads; p.turned = a->turned; p.neighbours = a->neighbours != 0;
+  p.q_vec = queries && rows_of_16(a->Q.ptr, a->Q.ld, dt, N) && rows_of_16(a->Q_out.ptr, a->Q_out.ld, dt, N);
+  p.k_vec = rows_of_16(a->K.ptr, a->K.ld, dt, N) && (!keys || rows_of_16(a->K_out.ptr, a->K_out.ld, dt, N));
+  p.v_vec = pages && rows_of_16(a->V.ptr, a->V.ld, dt, N);
+  p.status = status_dev;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  count_launch();
+  ProfScope prof(PK_ELEMENTWISE, 0.0, 0.0, s);
+  const dim3 grid((unsigned)N);
+  const bool four = pages && cache->kind == SP_CACHE_4BIT;
+  const cudaError_t e = dt == SP_F32 ? (four ? launch(cache_append_kernel<float, true>, grid, dim3(kAppendThreads), 0, s, p)
+                                             : launch(cache_append_kernel<float, false>, grid, dim3(kAppendThreads), 0, s, p))
+                                     : (four ? launch(cache_append_kernel<__nv_bfloat16, true>, grid, dim3(kAppendThreads), 0, s, p)
+                                             : launch(cache_append_kernel<__nv_bfloat16, false>, grid, dim3(kAppendThreads), 0, s, p));
+  return e == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+}
+
+sp_status sp_cache_read(const sp_kv_cache* cache, const int32_t* cu, const sp_mat* K, const sp_mat* V, int32_t* status_dev,
+                        void* stream) {
+  using namespace sp;
+  if (!K || !V) return SP_ERR_INVALID_ARG;
+  const sp_status ok = check_cache(cache, true);
+  if (ok != SP_OK) return ok;
+  if ((K->dtype != SP_F32 && K->dtype != SP_BF16) || V->dtype != K->dtype) return SP_ERR_DTYPE;
+  const int64_t N = K->rows, kv = (int64_t)cache->n_kv_heads * cache->d_head;
+  for (const sp_mat* m : {K, V})
+    if (m->rows != N || m->cols != kv || (N > 1 && m->ld < kv)) return SP_ERR_SHAPE;
+  if (N < 0 || N > (1 << 30)) return SP_ERR_SHAPE;
+  if (N == 0 || cache->n_seq == 0) return SP_OK;
+  if (!cu || !K->ptr || !V->ptr || K->ptr == V->ptr) return SP_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope prof(PK_ELEMENTWISE, 0.0, 0.0, s);
+  return cache_read(cache, cu, N, K->ptr, V->ptr, K->ld, V->ld, K->dtype, false, status_dev, s) == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,938 @@
+// Attention over a paged cache.
+//
+//   O_i = sum_j p_ij V_j, p = softmax(scale Q K^T), keys and values in pages; in 4 bits K_j = s_j n_j + z_j by groups of 64 channels, so that
+//   <Q_i, K_j> = sum_g s_jg sum_c q_ic n_jc + z_jg sum_c q_ic and O_ic = sum_j (p_ij s_jg) n_jc + sum_j p_ij z_jg: the matrix instructions
+//   contract the numbers themselves, and scales and offsets go to logits and probabilities.
+//
+// Few rows (queries x the heads that share a key head) stream the cache past them; what bounds that is reading it once, and in 4 bits as
+// much the instructions that open the numbers.  Each of eight warps brings its own blocks of 16 keys in by 16-byte asynchronous copies, a ring of
+// stages ahead, so that no warp waits for another before the end of an item.  Products are m16n8k16 of bf16, turned so that keys and channels
+// fill them: S^T = K Q^T and O^T += V^T P^T.  The order in which an instruction contracts channels is free, and so is the channel that a row of
+// V^T stands for.  In 4 bits a lane therefore takes whole words of eight numbers as they lie: for K the two words 2 t4, 2 t4 + 1 of a group, for V
+// word g4 of four keys; number n becomes the bf16 16 + n by a shift and one logical operation (for two at a time), and the 16 goes to the offsets.
+// fp32 queries are three bf16 parts that add up to them, as are the probabilities' products with the scales; then sums of 16 keys are added up
+// outside the matrix unit.
+//
+// More rows open the pages into bf16 or fp32 rows in the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor
+// cores' rate, where this form would open them again for every 16 rows.
+#include <math.h>
+
+#include "sp_cache.cuh"
+#include "sp_f32x2.cuh"
+
+namespace sp {
+namespace {
+
+constexpr int kWarps = 8, kBlock = 16, kThreads = kWarps * 32;
+constexpr int kPlanSeqs = 512;             // sequences of a launch
+constexpr int kLeastPart = 256;            // keys of a part, at least
+constexpr int kItemsPerSm = 8;             // items that the parts of a call come to, about
+
+struct PagedParams {
+  CacheView c;
+  const void* q;
+  void* o;
+  int64_t ldq, ldo;
+  float* lse;
+  const int32_t* cu_q;
+  int32_t Nq, n_heads, g, causal;
+  int32_t s0, n_here;                      // sequences of this launch
+  int32_t max_items;                       // what the workspace holds (more only where cu_q decreases)
+  float scale_log2;
+  int32_t* plan;                           // [n_here + 1] first item of each sequence, then the length of a part
+  float* part_o;                           // [item, row, dh]
+  float* part_lse;                         // [item, row] in base 2
+  int32_t* status;
+};
+
+template <int DH, bool FOUR>
+struct Ring {
+  static constexpr int PIECES = DH / 8;                                     // 16-byte pieces of a key's row, bf16
+  static constexpr int PITCH = FOUR ? DH / 2 : (PIECES | 1) * 16;           // bytes from a key to the next (bf16: an odd number of pieces,
+                                                                            // so that eight rows' pieces lie in different banks)
+  static constexpr int TILE = kBlock * PITCH;                               // K or V of a stage
+  static constexpr int G = DH / kCacheGroup;
+  static constexpr int SCALES = FOUR ? kBlock * G * 4 : 0;
+  static constexpr int STAGE = 2 * TILE + 2 * SCALES;
+  static constexpr int STAGES = FOUR ? (DH == 128 ? 5 : 8) : 3;
+  static constexpr int BYTES = STAGES * STAGE;                              // of a warp
+};
+template <int DH, bool FOUR, int ROWS, int PARTS>
+struct PagedCfg {
+  using R = Ring<DH, FOUR>;
+  static constexpr int PITCH = DH + 4;                                      // floats of a row of a warp's O
+  static constexpr int JOIN = ROWS * (PITCH + 2) * 4;                       // a warp's results, in its own ring
+  static constexpr int WARP = (R::BYTES > JOIN ? R::BYTES : JOIN) / 128 * 128 + 128;
+  static constexpr size_t SMEM = (size_t)kWarps * WARP;
+  // of an SM (fp32: three parts of the queries, and of wide heads more registers than two blocks have)
+  static constexpr int CTAS = SMEM > 113 * 1024 || (PARTS > 1 && DH > 64) ? 1 : 2;
+};
+
+__device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {      // zeros where there is nothing to copy
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_turned(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t turned8x8(uint32_t a) {       // 8 x 8 values of two bytes: row g4, columns 2 t4 and 2 t4 + 1
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+  uint32_t r;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(addr) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 r;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(addr) : "memory");
+  return r;
+}
+// The bf16 pair (16 + n_i, 16 + n_{i + 4}) of a word of eight numbers: the mantissa's last bit of 16 .. 31 is 1 / 8, so that a number stands
+// in bits 3 .. 6.  (An offset of 128, numbers in the lowest bits, would leave the sums eight times as large.)
+template <int I>
+__device__ __forceinline__ uint32_t opened(uint32_t w) {
+  const uint32_t at = I == 0 ? w << 3 : w >> (4 * I - 3);
+  return (at & 0x00780078u) | 0x41804180u;
+}
+__device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 e = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&e);
+}
+// PARTS bf16 pairs that add up to (lo, hi): one is the values rounded, three are exact
+template <int PARTS>
+__device__ __forceinline__ void split(float lo, float hi, uint32_t (&r)[PARTS]) {
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) {
+    r[i] = pack_bf16(lo, hi);
+    if (i + 1 < PARTS) {
+      lo -= low(r[i]);
+      hi -= high(r[i]);
+    }
+  }
+}
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// What a sequence brings: its rows of queries and its keys.
+struct Seq {
+  int32_t q0, nq, nk;
+};
+__device__ __forceinline__ Seq seq_at(const PagedParams& p, int32_t s) {
+  Seq r;
+  r.q0 = bounded(p.cu_q[s], p.Nq);
+  r.nq = max(0, bounded(p.cu_q[s + 1], p.Nq) - r.q0);
+  r.nk = r.nq > 0 ? max(0, p.c.lens[s]) : 0;
+  return r;
+}
+template <int ROWS>
+__device__ __forceinline__ int32_t tiles_of(const PagedParams& p, const Seq& s) {
+  return (int32_t)(((int64_t)s.nq * p.g + ROWS - 1) / ROWS);
+}
+// equal parts of whole blocks: their length and number (at least one)
+__device__ __forceinline__ int32_t part_length(int32_t nk, int32_t part) {
+  if (nk <= part) return nk;
+  const int32_t n = (nk - 1) / part + 1;
+  return ((nk - 1) / n + 1 + kBlock - 1) / kBlock * kBlock;
+}
+__device__ __forceinline__ int32_t parts_of(int32_t nk, int32_t part) {
+  return nk <= part ? 1 : (nk - 1) / part_length(nk, part) + 1;
+}
+__device__ __forceinline__ int32_t visible(int32_t nk, int64_t shift, int64_t token) {
+  return (int32_t)max((int64_t)0, min((int64_t)nk, token + shift + 1));
+}
+
+// sum over the block's threads, and what stands before this one's
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_word, int64_t& before) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t upto = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t t = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += t;
+  }
+  __syncthreads();
+  if (lane == 31) s_word[warp] = upto;
+  __syncthreads();
+  int64_t sum = 0, below = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) below += s_word[w];
+    sum += s_word[w];
+  }
+  before = below + upto - v;
+  return sum;
+}
+
+template <typename T, int DH, bool FOUR, int ROWS>
+__global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>::CTAS)) paged_rows_kernel(const PagedParams p) {
+  kernel_begin();
+  using C = PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>;
+  using R = typename C::R;
+  constexpr int H = ROWS / 8, PARTS = sizeof(T) == 4 ? 3 : 1, G = FOUR ? R::G : 1, K16 = DH / 16;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int32_t s_first[kPlanSeqs + 1];
+  __shared__ int64_t s_word[kWarps];
+  __shared__ int s_bad;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g4 = lane >> 2, t4 = lane & 3;
+  const int n_kv = p.c.n_kv, dh = p.c.dh;
+
+  // The plan, the same in every block: a part's length from the work of all sequences, and the first item of each.
+  int32_t part;
+  {
+    int64_t work = 0, before;
+    for (int i = threadIdx.x; i < p.n_here; i += kThreads) {
+      const Seq s = seq_at(p, p.s0 + i);
+      work += (int64_t)tiles_of<ROWS>(p, s) * s.nk;
+    }
+    const int64_t want = (block_scan(work, s_word, before) * n_kv + 148 * kItemsPerSm - 1) / (148 * kItemsPerSm);
+    part = (int32_t)min(max(want, (int64_t)kLeastPart), (int64_t)1 << 30);
+    const int per = (p.n_here + kThreads - 1) / kThreads;        // consecutive sequences of a thread
+    int64_t mine = 0;
+    for (int i = threadIdx.x * per; i < min((int)(threadIdx.x + 1) * per, p.n_here); ++i) {
+      const Seq s = seq_at(p, p.s0 + i);
+      mine += (int64_t)tiles_of<ROWS>(p, s) * n_kv * parts_of(s.nk, part);
+    }
+    block_scan(mine, s_word, before);
+    for (int i = threadIdx.x * per; i < min((int)(threadIdx.x + 1) * per, p.n_here); ++i) {
+      const Seq s = seq_at(p, p.s0 + i);
+      s_first[i] = (int32_t)min(before, (int64_t)p.max_items);
+      before += (int64_t)tiles_of<ROWS>(p, s) * n_kv * parts_of(s.nk, part);
+      if (i == p.n_here - 1) s_first[p.n_here] = (int32_t)min(before, (int64_t)p.max_items);
+    }
+    __syncthreads();
+    if (blockIdx.x == 0) {
+      for (int i = threadIdx.x; i <= p.n_here; i += kThreads) p.plan[i] = s_first[i];
+      if (threadIdx.x == 0) p.plan[p.n_here + 1] = part;
+    }
+  }
+
+  uint8_t* mine = smem + warp * C::WARP;
+  const uint32_t ring = shared_at(mine);
+  float* s_o = reinterpret_cast<float*>(mine);                   // [row][PITCH], after an item's last block
+  for (int32_t item = blockIdx.x; item < s_first[p.n_here]; item += gridDim.x) {
+    // the last sequence whose first item is not behind this one
+    int lo = 0, hi = p.n_here;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (s_first[mid] <= item) lo = mid;
+      else hi = mid;
+    }
+    const int32_t sq = p.s0 + lo;
+    const Seq it = seq_at(p, sq);
+    const int32_t n_parts = parts_of(it.nk, part), len = part_length(it.nk, part);
+    int32_t rest = item - s_first[lo];
+    const int32_t c = rest % n_parts;
+    rest /= n_parts;
+    const int32_t head = rest % n_kv, tile = rest / n_kv;
+    const int64_t r0 = (int64_t)tile * ROWS;
+    const int rows = (int)min((int64_t)ROWS, (int64_t)it.nq * p.g - r0);
+    const int64_t shift = p.causal ? (int64_t)it.nk - it.nq : (int64_t)it.nk;        // query i sees keys j <= i + shift
+    const int32_t sure = visible(it.nk, shift, r0 / p.g);                            // keys that every row sees
+    const int32_t kb = c * len;
+    int32_t seen = visible(it.nk, shift, (r0 + rows - 1) / p.g);                     // keys that some row sees
+    if (seen > kb + len) seen = kb + len;
+    const int32_t blocks = seen > kb ? (seen - kb + kBlock - 1) / kBlock : 0;
+    const int32_t own = blocks > warp ? (blocks - warp - 1) / kWarps + 1 : 0;        // this warp's: warp, warp + 8, ...
+
+    // ---- queries
+    uint32_t q[H][PARTS][K16][2];
+    float qsum[H][G][2];                                         // 4 bits: sums over a group of rows 8 h + 2 t4 + x
+    int32_t lim[H][2];                                           // keys [0, lim) of those rows
+    const T* Q = reinterpret_cast<const T*>(p.q);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const bool valid = 8 * h + g4 < rows;
+      const int64_t rr = valid ? r0 + 8 * h + g4 : r0;
+      const T* src = Q + (it.q0 + rr / p.g) * p.ldq + (head * (int64_t)p.g + rr % p.g) * dh;
+      if constexpr (FOUR) {
+        float sum[G];
+#pragma unroll
+        for (int gr = 0; gr < G; ++gr) {
+          sum[gr] = 0.f;
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              v[i] = valid ? load1(src + 64 * gr + 8 * (2 * t4 + w) + i) : 0.f;
+              sum[gr] += v[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                        // numbers (i, i + 4) of a word stand side by side
+              uint32_t r[PARTS];
+              split<PARTS>(v[i], v[i + 4], r);
+#pragma unroll
+              for (int u = 0; u < PARTS; ++u) q[h][u][4 * gr + 2 * w + i / 2][i & 1] = r[u];
+            }
+          }
+#pragma unroll
+          for (int w = 1; w < 4; w <<= 1) sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], w);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) qsum[h][gr][x] = __shfl_sync(0xffffffffu, sum[gr], (2 * t4 + x) * 4);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < K16; ++j)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int d = 16 * j + 8 * x + 2 * t4;
+            const bool there = valid && d < dh;
+            uint32_t r[PARTS];
+            split<PARTS>(there ? load1(src + d) : 0.f, there ? load1(src + d + 1) : 0.f, r);
+#pragma unroll
+            for (int u = 0; u < PARTS; ++u) q[h][u][j][x] = r[u];
+          }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {                              // (rows that are none: any values, kept to themselves)
+        const int row = 8 * h + 2 * t4 + x;
+        lim[h][x] = row < rows ? min(visible(it.nk, shift, (r0 + row) / p.g), seen) : seen;
+      }
+    }
+    // O: 4 bits: channels 64 (j / 4) + 8 g4 + j % 4 (| + 4) of rows 2 t4 + (x & 1); bf16: channels 16 j + g4 (| + 8)
+    float o[K16][H][4], zero_part[H][G][2], r[H][2], l[H][2];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+#pragma unroll
+      for (int j = 0; j < K16; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[j][h][x] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        r[h][x] = -INFINITY;                                     // reference of the rows' exponents, this lane's part of their sums
+        l[h][x] = 0.f;
+#pragma unroll
+        for (int gr = 0; gr < G; ++gr) zero_part[h][gr][x] = 0.f;
+      }
+    }
+    bool found = false;                                          // bf16: non-finite values behind some row's mask
+
+    // ---- copies: block i of this warp starts at key kb + 16 (warp + 8 i).  Pages of 32 blocks at a time, a lane each.
+    int32_t pages = -1;
+    uint32_t missing = 0u;                                       // a bit per stage: its block has no page
+    const auto fetch = [&](int32_t i) {
+      if (i < own) {
+        if ((i & 31) == 0) {
+          const int32_t at = i + lane;
+          pages = at < own ? page_of(p.c, sq, (kb + kBlock * (warp + kWarps * at)) / p.c.page_len) : -1;
+        }
+        const int32_t page = __shfl_sync(0xffffffffu, pages, i & 31);
+        const int32_t key = kb + kBlock * (warp + kWarps * i), slot = key % p.c.page_len;
+        const bool there = page >= 0;
+        const int64_t at = (int64_t)head * p.c.page_len + slot, pg = there ? page : 0;
+        const uint32_t dst = ring + (uint32_t)(i % R::STAGES) * R::STAGE, bit = 1u << (i % R::STAGES);
+        missing = there ? missing & ~bit : missing | bit;
+        if constexpr (FOUR) {
+          const uint8_t* k = p.c.k + pg * p.c.k_step + at * (DH / 2);
+          const uint8_t* v = p.c.v + pg * p.c.v_step + at * (DH / 2);
+#pragma unroll
+          for (int e = lane; e < DH / 2; e += 32) {              // piece e of the block's 16 rows
+            // 32-byte quarters of a 128-byte line change places with the line's number: the four keys of a half warp's read of K, and the
+            // four pairs of keys of a read of V, lie in different banks
+            const uint32_t byte = 16u * e, to = byte ^ ((byte >> 2) & 0x60u);
+            copy16(dst + to, k + byte, there);
+            copy16(dst + R::TILE + to, v + byte, there);
+          }
+          const int e = lane & 15;
+          if (e < 4 * G) {
+            const uint8_t* src = lane < 16 ? p.c.ks + pg * p.c.ks_step + at * (4 * G) : p.c.vs + pg * p.c.vs_step + at * (4 * G);
+            copy16(dst + 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * e, src + 16 * e, there);
+          }
+        } else {
+          const uint8_t* k = p.c.k + pg * p.c.k_step + at * (2 * dh);
+          const uint8_t* v = p.c.v + pg * p.c.v_step + at * (2 * dh);
+          const int per = dh / 8;
+#pragma unroll
+          for (int e0 = 0; e0 < kBlock * R::PIECES; e0 += 32) {
+            const int e = e0 + lane, row = e / per, piece = e % per;
+            if (e < kBlock * per) {
+              copy16(dst + row * R::PITCH + 16 * piece, k + 16 * e, there);
+              copy16(dst + R::TILE + row * R::PITCH + 16 * piece, v + 16 * e, there);
+            }
+          }
+        }
+      }
+      copies_end();
+    };
+#pragma unroll
+    for (int i = 0; i < R::STAGES - 1; ++i) fetch(i);
+
+    for (int32_t i = 0; i < own; ++i) {
+      const int32_t kt = kb + kBlock * (warp + kWarps * i);
+      fetch(i + R::STAGES - 1);
+      copies_wait<R::STAGES - 1>();
+      __syncwarp();
+      const uint32_t stage = ring + (uint32_t)(i % R::STAGES) * R::STAGE;
+      const bool edge = kt + kBlock > sure;
+      float s[H][4];                                             // keys kt + g4 | + 8, rows 2 t4, 2 t4 + 1
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[h][x] = 0.f;
+      if constexpr (FOUR) {
+        uint32_t pair[2][G];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int gr = 0; gr < G; ++gr) pair[y][gr] = lds32(stage + 2 * R::TILE + ((g4 + 8 * y) * G + gr) * 4);
+#pragma unroll
+        for (int gr = 0; gr < G; ++gr) {
+          float a[H][4];
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) a[h][x] = 0.f;
+          uint2 w[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const uint32_t byte = (uint32_t)((g4 + 8 * y) * (DH / 2) + 32 * gr + 8 * t4);
+            w[y] = lds64(stage + (byte ^ ((byte >> 2) & 0x60u)));
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t lo8 = u == 0 ? w[0].x : w[0].y, hi8 = u == 0 ? w[1].x : w[1].y;
+            const uint32_t a0 = opened<0>(lo8), a1 = opened<0>(hi8), a2 = opened<1>(lo8), a3 = opened<1>(hi8);
+            const uint32_t b0 = opened<2>(lo8), b1 = opened<2>(hi8), b2 = opened<3>(lo8), b3 = opened<3>(hi8);
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+              for (int x = 0; x < PARTS; ++x) {
+                mma(a[h], a0, a1, a2, a3, q[h][x][4 * gr + 2 * u][0], q[h][x][4 * gr + 2 * u][1]);
+                mma(a[h], b0, b1, b2, b3, q[h][x][4 * gr + 2 * u + 1][0], q[h][x][4 * gr + 2 * u + 1][1]);
+              }
+          }
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float scale = low(pair[y][gr]), zero = fmaf(-16.f, scale, high(pair[y][gr]));
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+                s[h][2 * y + x] = fmaf(zero, qsum[h][gr][x], fmaf(scale, a[h][2 * y + x], s[h][2 * y + x]));
+          }
+        }
+      } else {
+        const uint32_t row = stage + (uint32_t)((lane & 7) + 8 * ((lane >> 3) & 1)) * R::PITCH + 16u * (lane >> 4);
+#pragma unroll
+        for (int j = 0; j < K16; ++j) {
+          if (16 * j >= dh) break;
+          uint32_t a[4];                                         // matrices (keys 0-7 | 8-15) x (channels 0-7 | 8-15), keys first
+          ldsm(a, row + 32u * j);
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) mma(s[h], a[0], a[1], a[2], a[3], q[h][x][j][0], q[h][x][j][1]);
+        }
+      }
+      // a block of a page that is none: NaN to every row that sees it
+      if ((missing >> (i % R::STAGES)) & 1u) {
+        if (lane == 0) report_status(p.status, SP_ERR_SHAPE, sq, kt / p.c.page_len);
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[h][x] = NAN;
+      }
+      bool rise = false;
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float& u = s[h][x];
+          u *= p.scale_log2;
+          if (edge && kt + 8 * (x >> 1) + g4 >= lim[h][x & 1]) u = -INFINITY;
+          rise |= u != -INFINITY && !(u - r[h][x & 1] <= 8.f);
+        }
+      if (__any_sync(0xffffffffu, rise)) {                       // seldom: the references follow the maxima of this block
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          float f[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float m = fmaxf(s[h][x], s[h][2 + x]);
+            const bool nan = s[h][x] != s[h][x] || s[h][2 + x] != s[h][2 + x];
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+            if (__ballot_sync(0xffffffffu, nan) & (0x11111111u << t4)) m = NAN;      // (the lanes of these rows)
+            const bool up = m != -INFINITY && !(m - r[h][x] <= 0.f);
+            f[x] = up ? exp2_fast(r[h][x] - m) : 1.f;            // r = -infinity: 0
+            if (up) r[h][x] = m;
+            l[h][x] *= f[x];
+#pragma unroll
+            for (int gr = 0; gr < G; ++gr) zero_part[h][gr][x] *= f[x];
+          }
+#pragma unroll
+          for (int j = 0; j < K16; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[j][h][x] *= f[x & 1];
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float ref = r[h][x & 1];
+          s[h][x] = exp2_fast(s[h][x] - (ref == -INFINITY ? 0.f : ref));      // now probabilities, to the reference
+          l[h][x & 1] += s[h][x];
+        }
+      const uint32_t vtile = stage + R::TILE;
+      if constexpr (FOUR) {
+        uint32_t pair[2][G];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int gr = 0; gr < G; ++gr) pair[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
+#pragma unroll
+        for (int gr = 0; gr < G; ++gr) {
+          uint32_t pb[H][PARTS][2];                              // (P s)^T: keys 2 t4, + 1 | 2 t4 + 8, + 9 of row 8 h + g4
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const float scale = low(pair[y][gr]), zero = high(pair[y][gr]);
+              float ps[2], pz[2];
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const bool hidden = edge && kt + 8 * y + g4 >= lim[h][x];      // (whatever stands in a slot that the row does not see)
+                ps[x] = hidden ? 0.f : s[h][2 * y + x] * scale;
+                pz[x] = hidden ? 0.f : s[h][2 * y + x] * zero;
+              }
+              uint32_t u[PARTS];
+              split<PARTS>(ps[0], ps[1], u);
+              if (PARTS == 1) {                                  // what the product is taken with: its 16s have to go again
+                ps[0] = low(u[0]);
+                ps[1] = high(u[0]);
+              }
+#pragma unroll
+              for (int x = 0; x < 2; ++x) zero_part[h][gr][x] += fmaf(-16.f, ps[x], pz[x]);
+#pragma unroll
+              for (int x = 0; x < PARTS; ++x) pb[h][x][y] = turned8x8(u[x]);
+            }
+          uint32_t w[4];                                         // word g4 of keys 2 t4, + 1, + 8, + 9
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t byte = (uint32_t)((2 * t4 + (x & 1) + 8 * (x >> 1)) * (DH / 2) + 32 * gr + 4 * g4);
+            w[x] = lds32(vtile + (byte ^ ((byte >> 2) & 0x60u)));
+          }
+          // numbers 0 .. 3 and 4 .. 7 of two keys side by side
+          const uint32_t m0 = __byte_perm(w[0], w[1], 0x5410), m1 = __byte_perm(w[0], w[1], 0x7632);
+          const uint32_t m2 = __byte_perm(w[2], w[3], 0x5410), m3 = __byte_perm(w[2], w[3], 0x7632);
+          const uint32_t a[4][4] = {{opened<0>(m0), opened<0>(m1), opened<0>(m2), opened<0>(m3)},
+                                    {opened<1>(m0), opened<1>(m1), opened<1>(m2), opened<1>(m3)},
+                                    {opened<2>(m0), opened<2>(m1), opened<2>(m2), opened<2>(m3)},
+                                    {opened<3>(m0), opened<3>(m1), opened<3>(m2), opened<3>(m3)}};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+              float* acc = o[4 * gr + j][h];
+              if constexpr (PARTS == 1) {
+                mma(o[4 * gr + j][h], a[j][0], a[j][1], a[j][2], a[j][3], pb[h][0][0], pb[h][0][1]);
+              } else {
+                float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = PARTS - 1; x >= 0; --x) mma(t, a[j][0], a[j][1], a[j][2], a[j][3], pb[h][x][0], pb[h][x][1]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) acc[x] += t[x];
+              }
+            }
+        }
+      } else {
+        uint32_t pb[H][PARTS][2];
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            uint32_t u[PARTS];
+            split<PARTS>(s[h][2 * y], s[h][2 * y + 1], u);
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) pb[h][x][y] = turned8x8(u[x]);
+          }
+        const uint32_t row = vtile + (uint32_t)((lane & 7) + 8 * (lane >> 4)) * R::PITCH + 16u * ((lane >> 3) & 1);
+#pragma unroll
+        for (int j = 0; j < K16; ++j) {
+          if (16 * j >= dh) break;
+          uint32_t a[4];                                         // channels first: keys 2 t4, + 1 (a[0], a[1]) | 2 t4 + 8, + 9
+          ldsm_turned(a, row + 32u * j);
+          if (edge) {
+            // Keys that no row sees are cleared.  At one that only some see, a non-finite value is set to zero (0 times it would
+            // be NaN for the others) and given back at the end to the rows that see it; seen by every row, it goes its way.
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int key = kt + 2 * t4 + 8 * (x >> 1);
+              uint32_t clear = (key >= seen ? 0xffffu : 0u) | (key + 1 >= seen ? 0xffff0000u : 0u);
+              const uint32_t b = ((a[x] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u & ~clear;      // all-ones exponents
+              const uint32_t odd = (b & 0x8000u && key >= sure ? 0xffffu : 0u) | (b & 0x80000000u && key + 1 >= sure ? 0xffff0000u : 0u);
+              found |= odd != 0u;
+              a[x] &= ~(clear | odd);
+            }
+          }
+#pragma unroll
+          for (int h = 0; h < H; ++h) {
+            if constexpr (PARTS == 1) {
+              mma(o[j][h], a[0], a[1], a[2], a[3], pb[h][0][0], pb[h][0][1]);
+            } else {
+              float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int x = PARTS - 1; x >= 0; --x) mma(t, a[0], a[1], a[2], a[3], pb[h][x][0], pb[h][x][1]);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) o[j][h][x] += t[x];
+            }
+          }
+        }
+      }
+      __syncwarp();                                              // the stage is read: the next copies may take it
+    }
+    copies_wait<0>();
+    __syncwarp();                                                // (every lane's copies: the ring now holds results)
+    // ---- the warps join
+    if (threadIdx.x == 0) s_bad = 0;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      if constexpr (FOUR) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int gr = 0; gr < G; ++gr) {
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) zero_part[h][gr][x] += __shfl_xor_sync(0xffffffffu, zero_part[h][gr][x], w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              o[4 * gr + j][h][x] += zero_part[h][gr][x];
+              o[4 * gr + j][h][2 + x] += zero_part[h][gr][x];
+            }
+          }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int row = 8 * h + 2 * t4 + x;
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) l[h][x] += __shfl_xor_sync(0xffffffffu, l[h][x], w);
+        float* dst = s_o + row * C::PITCH;
+#pragma unroll
+        for (int j = 0; j < K16; ++j) {
+          const int d = FOUR ? 64 * (j / 4) + 8 * g4 + j % 4 : 16 * j + g4;
+          dst[d] = o[j][h][x];
+          dst[d + (FOUR ? 4 : 8)] = o[j][h][2 + x];
+        }
+        if (g4 == 0) {
+          s_o[ROWS * C::PITCH + row] = r[h][x];
+          s_o[ROWS * (C::PITCH + 1) + row] = l[h][x];
+        }
+      }
+    }
+    __syncthreads();
+    if (found) s_bad = 1;
+    if (!FOUR) __syncthreads();
+    const bool bad = !FOUR && s_bad != 0, cut = n_parts > 1;
+    for (int e = threadIdx.x; e < rows * dh; e += kThreads) {
+      const int row = e / dh, d = e % dh;
+      const int64_t rr = r0 + row, token = rr / p.g, out_row = it.q0 + token;
+      const int out_head = head * p.g + (int)(rr % p.g);
+      const auto of = [&](int w, int at) { return reinterpret_cast<const float*>(smem + w * C::WARP)[at]; };
+      float ref = -INFINITY;                                     // (a NaN of one warp's comes in through its sum)
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) ref = fmaxf(ref, of(w, ROWS * C::PITCH + row));
+      const float base = ref == -INFINITY ? 0.f : ref;
+      float total = 0.f, acc = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = exp2f(of(w, ROWS * C::PITCH + row) - base);      // a warp without keys: 0, and its l and O are 0
+        total = fmaf(of(w, ROWS * (C::PITCH + 1) + row), f, total);
+        acc = fmaf(of(w, row * C::PITCH + d), f, acc);
+      }
+      acc = total == 0.f ? 0.f : acc / total;
+      if (bad) {
+        const int32_t last = min(visible(it.nk, shift, token), seen);
+        for (int32_t key = max(sure, kb); key < last; ++key) {
+          const int32_t page = page_of(p.c, sq, key / p.c.page_len);
+          if (page < 0) continue;
+          const __nv_bfloat16* V = reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.v_step) +
+                                   ((int64_t)head * p.c.page_len + key % p.c.page_len) * dh;
+          const float u = __bfloat162float(V[d]);
+          if (!(fabsf(u) < INFINITY)) acc += u;
+        }
+      }
+      if (cut) p.part_o[((int64_t)item * ROWS + row) * dh + d] = acc;
+      else store1(reinterpret_cast<T*>(p.o) + out_row * p.ldo + (int64_t)out_head * dh + d, acc);
+      if (d == 0) {
+        const float lse2 = total == 0.f ? -INFINITY : base + log2f(total);
+        if (cut) p.part_lse[(int64_t)item * ROWS + row] = lse2;
+        else if (p.lse) p.lse[out_row * p.n_heads + out_head] = lse2 == -INFINITY ? lse2 : lse2 * 0.6931471805599453f;
+      }
+    }
+    __syncthreads();                                             // s_bad and the warps' results are read
+  }
+}
+
+// O_i = sum_c w_c O_ic / sum_c w_c with w_c = 2^(lse_ic - max): one warp per row and head of a sequence that was cut.
+template <typename T, int ROWS>
+__global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
+  kernel_begin();
+  const int lane = threadIdx.x & 31;
+  const int64_t idx = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (idx >= (int64_t)p.Nq * p.n_heads) return;
+  const int32_t row = (int32_t)(idx / p.n_heads), h = (int32_t)(idx % p.n_heads);
+  const int32_t sq = sequence_of(p.cu_q, p.c.n_seq, p.Nq, row);
+  if (sq < p.s0 || sq >= p.s0 + p.n_here) return;
+  const int32_t part = p.plan[p.n_here + 1];
+  const Seq it = seq_at(p, sq);
+  const int32_t parts = parts_of(it.nk, part);
+  if (parts < 2) return;
+  const int dh = p.c.dh;
+  const int64_t rr = (int64_t)(row - it.q0) * p.g + h % p.g, tile = rr / ROWS;
+  const int64_t slot0 = p.plan[sq - p.s0] + (tile * p.c.n_kv + h / p.g) * parts;
+  if (slot0 + parts > p.max_items) return;
+  const float* lses = p.part_lse + slot0 * ROWS + rr % ROWS;
+  float mx = -INFINITY;
+  bool bad = false;                   // (fmaxf passes over a NaN)
+  for (int c = lane; c < parts; c += 32) {
+    const float lc = lses[(int64_t)c * ROWS];
+    mx = fmaxf(mx, lc);
+    bad |= lc != lc;
+  }
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  bad = __any_sync(0xffffffffu, bad);
+  const int d = 4 * lane;             // a lane has channels 4 lane .. (dh is a multiple of 16)
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float total = 0.f;
+  const float* po = p.part_o + (slot0 * ROWS + rr % ROWS) * dh + d;
+  for (int c0 = 0; c0 < parts; c0 += 32) {
+    const float wl = c0 + lane < parts ? exp2f(lses[(int64_t)(c0 + lane) * ROWS] - ref) : 0.f;
+    const int m = min(32, parts - c0);
+#pragma unroll 8
+    for (int c = 0; c < m; ++c) {
+      const float w = __shfl_sync(0xffffffffu, wl, c);
+      total += w;
+      if (d < dh) {
+        const float4 v = *reinterpret_cast<const float4*>(po + (int64_t)(c0 + c) * ROWS * dh);
+        acc.x = fmaf(w, v.x, acc.x);
+        acc.y = fmaf(w, v.y, acc.y);
+        acc.z = fmaf(w, v.z, acc.z);
+        acc.w = fmaf(w, v.w, acc.w);
+      }
+    }
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  if (d < dh) {
+    T* out = reinterpret_cast<T*>(p.o) + (int64_t)row * p.ldo + (int64_t)h * dh + d;
+    store1(out, bad ? NAN : acc.x * inv);
+    store1(out + 1, bad ? NAN : acc.y * inv);
+    store1(out + 2, bad ? NAN : acc.z * inv);
+    store1(out + 3, bad ? NAN : acc.w * inv);
+  }
+  if (lane == 0 && p.lse)
+    p.lse[(int64_t)row * p.n_heads + h] = bad ? NAN : total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
+}
+
+// Items of a launch, at most: parts of at least want keys come to no more than 148 x kItemsPerSm, one more for every tile and key head.
+int64_t most_items(int64_t Nq, int64_t n_seq, int64_t n_kv, int64_t g, int rows) {
+  const int64_t seqs = n_seq < Nq ? n_seq : Nq;
+  return (148 * kItemsPerSm + 1) + (Nq * g / rows + seqs) * n_kv;
+}
+inline int tile_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 8 * n_seq ? 8 : 16; }
+// Rows per sequence, on average, up to which the cache streams past tiles of 16 of them.
+inline bool paged_few_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 64 * n_seq; }
+
+struct RowsPlan {
+  int rows;
+  int64_t items;
+  size_t plan_bytes, o_bytes, lse_bytes;
+  size_t bytes() const { return plan_bytes + o_bytes + lse_bytes; }
+};
+RowsPlan rows_plan(int64_t Nq, int64_t n_seq, int64_t n_kv, int64_t g, int64_t dh) {
+  RowsPlan r;
+  r.rows = tile_rows(Nq, g, n_seq);
+  const int64_t n_here = n_seq < kPlanSeqs ? n_seq : kPlanSeqs;
+  r.items = most_items(Nq, n_here, n_kv, g, r.rows);
+  r.plan_bytes = align_up((size_t)(n_here + 2) * 4, 256);
+  r.o_bytes = align_up((size_t)r.items * r.rows * dh * 4, 256);
+  r.lse_bytes = align_up((size_t)r.items * r.rows * 4, 256);
+  return r;
+}
+
+template <typename T, int DH, bool FOUR, int ROWS>
+cudaError_t launch_rows(const PagedParams& p, cudaStream_t stream) {
+  using C = PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>;
+  static PerDeviceOnce attr_once;
+  const auto kernel = paged_rows_kernel<T, DH, FOUR, ROWS>;
+  cudaError_t e = attr_once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM); });
+  if (e != cudaSuccess) return e;
+  // as many blocks as can be resident and may have work
+  const int64_t seqs = p.n_here < p.Nq ? p.n_here : p.Nq, most = ceil_div((int64_t)p.c.max_pages * p.c.page_len, (int64_t)kLeastPart);
+  const int64_t work = ((int64_t)p.Nq * p.g / ROWS + seqs) * p.c.n_kv * (most > 0 ? most : 1), resident = (int64_t)sm_count() * C::CTAS;
+  count_launch();
+  e = launch(kernel, dim3((unsigned)(work < resident ? work : resident)), dim3(kThreads), C::SMEM, stream, p);
+  if (e != cudaSuccess || most < 2) return e;
+  count_launch();
+  const OverlapScope overlap(true);       // its blocks start while the parts end
+  return launch(paged_join_kernel<T, ROWS>, dim3((unsigned)ceil_div((int64_t)p.Nq * p.n_heads, (int64_t)8)), dim3(256), 0, stream, p);
+}
+template <typename T, int DH, bool FOUR>
+cudaError_t launch_rows(const PagedParams& p, int rows, cudaStream_t stream) {
+  return rows == 8 ? launch_rows<T, DH, FOUR, 8>(p, stream) : launch_rows<T, DH, FOUR, 16>(p, stream);
+}
+template <typename T>
+cudaError_t launch_rows(const PagedParams& p, bool four, int rows, cudaStream_t stream) {
+  if (p.c.dh <= 64) return four ? launch_rows<T, 64, true>(p, rows, stream) : launch_rows<T, 64, false>(p, rows, stream);
+  return four ? launch_rows<T, 128, true>(p, rows, stream) : launch_rows<T, 128, false>(p, rows, stream);
+}
+
+// cu_k of the opened keys: the lengths added up; a sequence that does not fit into max_keys (or has more tokens than its table) gets as many
+// rows as queries at most, which cache_read makes NaN: every query sees one of them.
+__global__ void __launch_bounds__(kThreads) open_plan_kernel(const CacheView c, const int32_t* cu_q, int32_t Nq, int32_t max_keys, int32_t* cu_k,
+                                                             int32_t* status) {
+  kernel_begin();
+  __shared__ int64_t s_word[kWarps];
+  int64_t at = 0, used = 0;               // rows given to the sequences before, and their keys
+  for (int32_t s0 = 0; s0 < c.n_seq; s0 += kThreads) {
+    const int32_t s = s0 + threadIdx.x;
+    int64_t n = 0, before;
+    const int32_t nq = s < c.n_seq ? bounded(cu_q[s + 1], Nq) - bounded(cu_q[s], Nq) : 0;
+    if (nq > 0) n = max(0, c.lens[s]);
+    const int64_t keys = block_scan(n, s_word, before);
+    // (what fits is decided by the sum up to here, whether those before fitted or not: the same answer in any order)
+    const bool fits = n == 0 || (used + before + n <= max_keys && n <= (int64_t)c.max_pages * c.page_len);
+    if (!fits) {
+      report_status(status, SP_ERR_SHAPE, s, -1);
+      n = min(n, (int64_t)nq);
+    }
+    const int64_t rows = block_scan(n, s_word, before);
+    if (s < c.n_seq) cu_k[s] = (int32_t)(at + before);
+    at += rows;
+    used += keys;
+  }
+  if (threadIdx.x == 0) cu_k[c.n_seq] = (int32_t)at;
+}
+
+struct OpenPlan {
+  int64_t rows;
+  size_t cu_bytes, k_bytes, attention;
+  size_t bytes() const { return cu_bytes + 2 * k_bytes + attention; }
+};
+OpenPlan open_plan(int64_t Nq, int64_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype, int64_t max_keys) {
+  OpenPlan r;
+  r.rows = max_keys + Nq;
+  r.cu_bytes = align_up((size_t)(n_seq + 1) * 4, 256);
+  r.k_bytes = align_up((size_t)r.rows * n_kv * dh * dtype_size(dtype), 256);
+  r.attention = sp_attention_workspace_bytes(Nq, r.rows, (int32_t)n_seq, n_heads, n_kv, dh, dtype);
+  return r;
+}
+// max_keys as the caller gave it, or all that the table can hold
+int64_t keys_at_most(int64_t max_keys, int64_t n_seq, int64_t max_pages, int64_t page_len) {
+  const int64_t all = n_seq * max_pages * page_len;
+  return max_keys > 0 && max_keys < all ? max_keys : all;
+}
+
+}  // namespace
+}  // namespace sp
+
+extern "C" {
+
+size_t sp_cache_attention_bytes(int64_t Nq, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t dtype,
+                                int32_t max_pages, int32_t page_len, int64_t max_keys) {
+  using namespace sp;
+  if (Nq < 1 || Nq > (1 << 30) || n_seq < 1 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || d_head < 1 || d_head > 128 ||
+      max_pages < 0 || page_len < 1 || (int64_t)max_pages * page_len > (1 << 30))
+    return 0;
+  const int64_t g = n_heads / n_kv_heads;
+  if (paged_few_rows(Nq, g, n_seq)) {
+    const RowsPlan plan = rows_plan(Nq, n_seq, n_kv_heads, g, d_head);
+    return plan.items > 0x7fffffff ? 0 : plan.bytes();
+  }
+  const int64_t keys = keys_at_most(max_keys, n_seq, max_pages, page_len);
+  if (keys + Nq > (1 << 30)) return 0;
+  return open_plan(Nq, n_seq, n_heads, n_kv_heads, d_head, dtype, keys).bytes();
+}
+
+sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const int32_t* cu_q, int32_t n_heads, int32_t causal, double scale,
+                             int64_t max_keys, const sp_mat* O, float* lse, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream) {
+  using namespace sp;
+  if (!Q || !O) return SP_ERR_INVALID_ARG;
+  const sp_status ok = check_cache(cache, true);
+  if (ok != SP_OK) return ok;
+  const int32_t dt = Q->dtype, n_seq = cache->n_seq, n_kv = cache->n_kv_heads, dh = cache->d_head;
+  if ((dt != SP_F32 && dt != SP_BF16) || O->dtype != dt) return SP_ERR_DTYPE;
+  if (n_heads < 1 || n_heads > (1 << 20) || n_heads % n_kv != 0 || max_keys < 0) return SP_ERR_SHAPE;
+  const int64_t Nq = Q->rows, cols = (int64_t)n_heads * dh;
+  if (Nq < 0 || Nq > (1 << 30) || Q->cols != cols || O->rows != Nq || O->cols != cols) return SP_ERR_SHAPE;
+  if (Nq > 1 && (Q->ld < cols || O->ld < cols)) return SP_ERR_SHAPE;
+  if (Nq * n_heads > ((int64_t)1 << 33)) return SP_ERR_SHAPE;
+  if (!(scale >= 1e-30) || !(scale <= 1e30)) return SP_ERR_INVALID_ARG;
+  if (Nq == 0 || n_seq == 0) return SP_OK;
+  if (!Q->ptr || !O->ptr || !cu_q) return SP_ERR_INVALID_ARG;
+  const int64_t g = n_heads / n_kv;
+  const size_t need = sp_cache_attention_bytes(Nq, n_seq, n_heads, n_kv, dh, dt, cache->max_pages, cache->page_len, max_keys);
+  if (need == 0) return SP_ERR_SHAPE;                            // (more keys than can be opened: max_keys tells how many there are)
+  if (!ws || ws_bytes < need) return SP_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(ws) & 255u) return SP_ERR_ALIGNMENT;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  uint8_t* at = reinterpret_cast<uint8_t*>(ws);
+  ProfScope prof(PK_GEMM_SIMT, 0.0, 0.0, s);
+  if (paged_few_rows(Nq, g, n_seq)) {
+    const RowsPlan plan = rows_plan(Nq, n_seq, n_kv, g, dh);
+    PagedParams p = {};
+    p.c = cache_view(cache);
+    p.q = Q->ptr; p.o = O->ptr;
+    p.ldq = Nq > 1 ? Q->ld : cols; p.ldo = Nq > 1 ? O->ld : cols;
+    p.lse = lse;
+    p.cu_q = cu_q;
+    p.Nq = (int32_t)Nq; p.n_heads = n_heads; p.g = (int32_t)g; p.causal = causal != 0;
+    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    p.plan = reinterpret_cast<int32_t*>(at);
+    p.part_o = reinterpret_cast<float*>(at + plan.plan_bytes);
+    p.part_lse = reinterpret_cast<float*>(at + plan.plan_bytes + plan.o_bytes);
+    p.status = status_dev;
+    p.max_items = (int32_t)plan.items;
+    for (p.s0 = 0; p.s0 < n_seq; p.s0 += kPlanSeqs) {
+      p.n_here = n_seq - p.s0 < kPlanSeqs ? n_seq - p.s0 : kPlanSeqs;
+      const bool four = cache->kind == SP_CACHE_4BIT;
+      const cudaError_t e = dt == SP_F32 ? launch_rows<float>(p, four, plan.rows, s) : launch_rows<__nv_bfloat16>(p, four, plan.rows, s);
+      if (e != cudaSuccess) return SP_ERR_CUDA;
+    }
+    return SP_OK;
+  }
+  const int64_t keys = keys_at_most(max_keys, n_seq, cache->max_pages, cache->page_len);
+  const OpenPlan plan = open_plan(Nq, n_seq, n_heads, n_kv, dh, dt, keys);
+  int32_t* cu_k = reinterpret_cast<int32_t*>(at);
+  uint8_t *K = at + plan.cu_bytes, *V = K + plan.k_bytes;
+  const int64_t kv = (int64_t)n_kv * dh;
+  count_launch();
+  if (launch(open_plan_kernel, dim3(1), dim3(kThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, status_dev) !=
+          cudaSuccess ||
+      cache_read(cache, cu_k, plan.rows, K, V, kv, kv, dt, true, status_dev, s) != cudaSuccess)
+    return SP_ERR_CUDA;
+  sp_attention_args a = {};
+  a.Q = *Q;
+  a.O = *O;
+  a.K = sp_mat{K, dt, 0, plan.rows, kv, kv};
+  a.V = sp_mat{V, dt, 0, plan.rows, kv, kv};
+  a.cu_q = cu_q; a.cu_k = cu_k;
+  a.lse = lse;
+  a.n_seq = n_seq; a.n_heads = n_heads; a.n_kv_heads = n_kv; a.causal = causal;
+  a.scale = scale;
+  return sp_attention(&a, status_dev, V + plan.k_bytes, plan.attention, stream);
+}
+
+}  // extern "C"

@@ -240,7 +240,7 @@ __device__ __forceinline__ void strip_index(const int32_t* idx, int64_t cols, in
 }
 #endif
 
-inline size_t dtype_size(int32_t dt) { return dt == SP_BF16 ? 2 : (dt == SP_F64 ? 8 : 4); }
+inline size_t dtype_size(int32_t dt) { return dt == SP_BF16 ? 2 : dt == SP_F64 ? 8 : dt == SP_E4M3 ? 1 : 4; }
 
 // A strided operand of the SIMT GEMM: element (i, k) lives at ptr[i * s0 + k * s1].
 struct Operand {
@@ -261,6 +261,7 @@ struct OutOperand {
 // What follows a product in sp_linear: v -> act(v + bias[j]); the caller's `other` is then added or multiplied.
 struct LinearEpi {
   const float* bias = nullptr;
+  const float *x_scale = nullptr, *w_scale = nullptr;      // both or none: operands of e4m3, scales of X's and of W's rows
   int32_t act = SP_LINEAR_NONE, combine = SP_COMBINE_ADD;
 };
 #ifdef __CUDACC__
@@ -376,6 +377,9 @@ cudaError_t linear_few(int64_t M, int64_t N, int64_t K, TcOperand A, TcOperand W
 inline bool linear_few_rows_f32(int64_t M, int64_t K) { return M <= 128 || (M <= 512 && K >= 512); }
 cudaError_t linear_few_f32(int64_t M, int64_t N, int64_t K, Operand A, Operand W, const LinearEpi& epi, Operand other, OutOperand C,
                            cudaStream_t stream);
+
+// e4m3 rows of few tokens (sp_linear_e4m3.cu), layouts as sp_linear_e4m3 takes them.
+inline bool linear_few_rows_e4m3(int64_t M, int64_t N) { return M <= 16 || (M <= 192 && M * N <= (1 << 18)); }
 
 struct SolveAssist;
 // fp64 factorisation and solves (sp_linalg.cu), block columns of kCholNB.

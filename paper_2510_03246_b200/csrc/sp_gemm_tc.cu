@@ -137,12 +137,12 @@ __device__ __forceinline__ void tma_reduce_add_5d(const CUtensorMap* map, const 
                ::"l"(map), "r"(c.x[0]), "r"(c.x[1]), "r"(c.x[2]), "r"(c.x[3]), "r"(c.x[4]), "r"(src)
                : "memory");
 }
-// Instruction descriptor of the pair's MMA: 256 x tile_n x 16, bf16 operands, fp32 accumulator.
-__device__ __forceinline__ uint32_t make_instr_desc(bool a_kmajor, bool b_kmajor, int tile_n) {
+// Instruction descriptor of the pair's MMA: 256 x tile_n x 16, bf16 operands (eight: x 32, e4m3), fp32 accumulator.
+__device__ __forceinline__ uint32_t make_instr_desc(bool a_kmajor, bool b_kmajor, int tile_n, bool eight) {
   uint32_t d = 0;
   d |= 1u << 4;                          // accumulator format: fp32
-  d |= 1u << 7;                          // A format: bf16
-  d |= 1u << 10;                         // B format: bf16
+  d |= (eight ? 0u : 1u) << 7;           // A format: bf16 (1 of kind::f16) or e4m3 (0 of kind::f8f6f4)
+  d |= (eight ? 0u : 1u) << 10;          // B format
   d |= (a_kmajor ? 0u : 1u) << 15;       // A major-ness
   d |= (b_kmajor ? 0u : 1u) << 16;       // B major-ness
   d |= (uint32_t)(tile_n >> 3) << 17;    // N
@@ -200,9 +200,17 @@ __device__ __forceinline__ void tc_commit_local(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// act(acc + bias) of a 32-column block: lane l fetches the bias of column gj0 + l, every lane needs all 32.
-__device__ __forceinline__ void linear_block(const TcParams& p, int64_t gj0, uint32_t (&r)[32]) {
+// act(acc + bias) of a 32-column block: lane l fetches the bias of column gj0 + l, every lane needs all 32.  EIGHT: the sums of products
+// of 8-bit values take the scales of their row (a lane's own: row0 + lane) and of their output first.
+template <bool EIGHT>
+__device__ __forceinline__ void linear_block(const TcParams& p, int64_t row0, int64_t gj0, uint32_t (&r)[32]) {
   const int lane = threadIdx.x & 31;
+  if constexpr (EIGHT) {
+    const float xs = row0 + lane < p.M ? p.lin.x_scale[row0 + lane] : 0.f;
+    const float ws = gj0 + lane < p.N ? p.lin.w_scale[gj0 + lane] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * xs * __shfl_sync(0xffffffffu, ws, i));
+  }
   if (p.lin.bias) {
     const float b = gj0 + lane < p.N ? p.lin.bias[gj0 + lane] : 0.f;
 #pragma unroll
@@ -241,7 +249,9 @@ __device__ __forceinline__ void linear_loose_columns(const TcParams& p, int64_t 
 // zeros.  The sum over K runs in the same order either way.
 // LIN: sp_linear's epilogue, act(acc + bias) and then Cin added or multiplied, in each of the epilogue's forms; an instantiation of its
 // own, so that the others carry none of its instructions.
-template <bool BATCHED, int TN, bool LIN = false>
+// EIGHT: operands of e4m3, both K-major.  In bytes a stage, its descriptors and the step of an instruction along K are those of bf16, so
+// that a k-block holds twice the values and an instruction contracts 32 of them; the epilogue applies the scales of rows and outputs.
+template <bool BATCHED, int TN, bool LIN = false, bool EIGHT = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmCin, const TcParams p) {
@@ -250,6 +260,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     wait_for_predecessors();
     if (*p.skip != 0) return;      // the same answer in every CTA: nothing is allocated yet
   }
+  static_assert(!EIGHT || (LIN && !BATCHED), "the 8-bit form is sp_linear_e4m3's");
+  constexpr int KB_VALUES = EIGHT ? 2 * BK : BK;             // values of K in a k-block
   constexpr int BN_LOAD = TN / 2;                            // columns of B loaded per CTA
   constexpr uint32_t LOAD_BYTES = A_BYTES + BN_LOAD * BK * 2;
   extern __shared__ uint8_t smem_raw[];
@@ -319,7 +331,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           const uint32_t a_dst = tiles + s * STAGE_BYTES;
           const uint32_t b_dst = a_dst + A_BYTES;
           const int sg = kb / p.seg_kb;
-          const int kk = (kb - sg * p.seg_kb) * BK;
+          const int kk = (kb - sg * p.seg_kb) * KB_VALUES;
           const int ka = kk + p.seg.a_k[sg], kbb = kk + p.seg.b_k[sg];
           const int am = tm * TILE_M + (int)rank * BM + p.seg.a_mn[sg];
           const int bn = tn * TN + (int)rank * BN_LOAD + p.seg.b_mn[sg];
@@ -366,7 +378,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer (leader CTA only)
     if (lane == 0 && rank == 0) {
-      const uint32_t idesc = make_instr_desc(p.a_kmajor != 0, p.b_kmajor != 0, TN);
+      const uint32_t idesc = make_instr_desc(p.a_kmajor != 0, p.b_kmajor != 0, TN, EIGHT);
       int s = 0;
       uint32_t ph = 0;
       int acc = 0;
@@ -398,7 +410,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             const uint32_t b_off = p.b_kmajor ? (uint32_t)(k * UMMA_K * 2) : (uint32_t)(k * UMMA_K * 128);
             const uint64_t adesc = make_smem_desc(a_src + a_off, p.a_kmajor != 0, 64 * BK * 2);
             const uint64_t bdesc = make_smem_desc(b_src + b_off, p.b_kmajor != 0, 64 * BK * 2);
-            tc_mma_bf16_pair(d_tmem, adesc, bdesc, idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+            if constexpr (EIGHT) tc_mma_e4m3_pair(d_tmem, adesc, bdesc, idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+            else tc_mma_bf16_pair(d_tmem, adesc, bdesc, idesc, (kb > kb0 || k > 0) ? 1u : 0u);
           }
           issued = true;
           tc_commit_pair(empty_bar(s));   // frees the stage in both CTAs once these MMAs have read it
@@ -463,7 +476,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           uint32_t r[32];
           tc_ld32(taddr + (uint32_t)(sl * 32), r);
           tc_wait_ld();
-          if constexpr (LIN) linear_block(p, gj0, r);
+          if constexpr (LIN) linear_block<EIGHT>(p, row0, gj0, r);
           if (rows_ok) {
             if (lane == 0 && sl + 1 < nsl) {     // next block of Cin into the other half (its last reader is done)
               fence_async_smem();
@@ -528,7 +541,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           uint32_t r[32];
           tc_ld32(taddr + (uint32_t)c0, r);
           tc_wait_ld();
-          if constexpr (LIN) linear_block(p, gj0, r);
+          if constexpr (LIN) linear_block<EIGHT>(p, row0, gj0, r);
           if (lane == 0) bulk_wait_read_1();      // the copies that last read this half (two blocks ago) are done
           __syncwarp();
           uint8_t* out_row = wstg_ptr + buf * 4096 + lane * 64;
@@ -577,7 +590,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           uint32_t r[32];
           tc_ld32(taddr + (uint32_t)c0, r);
           tc_wait_ld();
-          if constexpr (LIN) linear_block(p, gj0, r);
+          if constexpr (LIN) linear_block<EIGHT>(p, row0, gj0, r);
           if (lane == 0) bulk_wait_read_1();      // the copy that last read this tile (two blocks ago) is done
           __syncwarp();
           uint8_t* tile = wstg_ptr + buf * 4096 + lane * 128;
@@ -630,7 +643,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           uint32_t r[32];
           tc_ld32(taddr + (uint32_t)c0, r);
           tc_wait_ld();
-          if constexpr (LIN) linear_block(p, gj0, r);
+          if constexpr (LIN) linear_block<EIGHT>(p, row0, gj0, r);
 #pragma unroll
           for (int i = 0; i < 32; ++i) stg[lane][i] = p.alpha * __uint_as_float(r[i]);
           __syncwarp();
@@ -717,6 +730,18 @@ bool make_map(CUtensorMap* map, bool f32, const void* ptr, int64_t inner, int64_
   return r == CUDA_SUCCESS;
 }
 
+// e4m3 [outer, inner], K-major: boxes of 128 bytes x box_outer rows, 128-byte swizzle
+static bool make_map_bytes(CUtensorMap* map, const void* ptr, int64_t inner, int64_t outer, int64_t ld, int box_outer) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+  cuuint64_t strides[1] = {(cuuint64_t)ld};
+  cuuint32_t box[2] = {2 * BK, (cuuint32_t)box_outer};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_map3(CUtensorMap* map, const void* ptr, int64_t n0, int64_t n1, int64_t n2, int64_t ld1, int64_t ld2, int b0, int b1,
                int b2) {
   EncodeTiledFn fn = encode_fn();
@@ -798,6 +823,8 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
                   OutOperand C, bool lower_only, int32_t* status_dev, cudaStream_t stream, const TcSegments* segs,
                   double alg_flops, int max_pairs, const TcBatch* batch, const LinearEpi* lin) {
   const bool batched = batch != nullptr;
+  const bool eight = lin && lin->x_scale != nullptr;      // operands of e4m3
+  if (eight && (!A.kmajor || !B.kmajor || A.ld % 16 != 0 || B.ld % 16 != 0)) return SP_ERR_UNSUPPORTED;
   if (lin && (batched || lower_only || segs || alpha != 1.f || (beta != 0.f && beta != 1.f))) return SP_ERR_INVALID_ARG;
   if (batched && (batch->nb0 < 1 || batch->nb1 < 1 || batch->a_planes < 1 || batch->b_planes < 1))
     return SP_ERR_INVALID_ARG;
@@ -823,7 +850,8 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
 
   int pairs_max = sm_count() / 2;
   if (max_pairs > 0 && max_pairs < pairs_max) pairs_max = max_pairs;
-  const int num_kb = (int)ceil_div(K, BK) * sg.nseg;
+  const int64_t kb_values = eight ? 2 * BK : BK;
+  const int num_kb = (int)ceil_div(K, kb_values) * sg.nseg;
   // The narrow tile where both halves of every wide tile run at once, or N fits it; not where K may be cut instead (see
   // below), and for a lower triangle only where one wide tile covers all columns, so that the same entries are written.
   const int64_t wide_tiles = ceil_div(M, (int64_t)TILE_M) * ceil_div(N, (int64_t)TILE_N) *
@@ -857,6 +885,9 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
                          : make_map5(&tmB, false, B.ptr, b_next, 64, b_kext, B.ld, BK, b_nb0, bt.b_s0, bt.nb1,
                                      bt.b_s1, bt.b_planes, bt.b_plane, false, p.b_ord));
     if (!ok) return SP_ERR_ALIGNMENT;
+  } else if (eight) {
+    if (!make_map_bytes(&tmA, A.ptr, a_kext, a_mext, A.ld, BM) || !make_map_bytes(&tmB, B.ptr, b_kext, b_next, B.ld, tile_n / 2))
+      return SP_ERR_CUDA;
   } else {
     ok = A.kmajor ? make_map(&tmA, false, A.ptr, a_kext, a_mext, A.ld, BK, BM)
                   : make_map(&tmA, false, A.ptr, a_mext, a_kext, A.ld, 64, BK);
@@ -926,7 +957,7 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
       p.epi_mode = EPI_TMA_BF16;
   }
   p.seg = sg;
-  p.seg_kb = (int32_t)ceil_div(K, BK);
+  p.seg_kb = (int32_t)ceil_div(K, kb_values);
   p.tiles_m = (int32_t)ceil_div(M, TILE_M);
   p.tiles_n = (int32_t)ceil_div(N, tile_n);
   // consecutive tiles (which run at the same time on neighbouring SMs) should share the larger operand panel
@@ -996,7 +1027,8 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
   if (attr_once.run([] {
         for (auto k : {gemm_tc_kernel<false, TILE_N>, gemm_tc_kernel<true, TILE_N>, gemm_tc_kernel<false, kNarrowN>,
                        gemm_tc_kernel<true, kNarrowN>, gemm_tc_kernel<false, TILE_N, true>,
-                       gemm_tc_kernel<false, kNarrowN, true>}) {
+                       gemm_tc_kernel<false, kNarrowN, true>, gemm_tc_kernel<false, TILE_N, true, true>,
+                       gemm_tc_kernel<false, kNarrowN, true, true>}) {
           const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES);
           if (e != cudaSuccess) return e;
         }
@@ -1011,7 +1043,8 @@ sp_status gemm_tc(int64_t M, int64_t N, int64_t K, float alpha, TcOperand A, TcO
   ProfScope prof(p.skip != nullptr ? PK_CONDITIONAL : max_pairs > 0 ? PK_GEMM_TC_SHARED : PK_GEMM_TC,
                  p.skip != nullptr ? 0.0 : flops, 0.0, stream);
   const int pairs = p.num_units < pairs_max ? p.num_units : pairs_max;
-  const auto kernel = lin     ? (narrow ? gemm_tc_kernel<false, kNarrowN, true> : gemm_tc_kernel<false, TILE_N, true>)
+  const auto kernel = eight   ? (narrow ? gemm_tc_kernel<false, kNarrowN, true, true> : gemm_tc_kernel<false, TILE_N, true, true>)
+                      : lin   ? (narrow ? gemm_tc_kernel<false, kNarrowN, true> : gemm_tc_kernel<false, TILE_N, true>)
                       : batched ? (narrow ? gemm_tc_kernel<true, kNarrowN> : gemm_tc_kernel<true, TILE_N>)
                               : (narrow ? gemm_tc_kernel<false, kNarrowN> : gemm_tc_kernel<false, TILE_N>);
   // (programmatic launch only for one wave of tiles with the GPU to itself, see launch())
