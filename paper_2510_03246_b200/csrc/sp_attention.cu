@@ -353,19 +353,9 @@ Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_k
 }
 
 }  // namespace
-}  // namespace sp
 
-extern "C" {
-
-size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
-                                    int32_t d_head, int32_t dtype) {
-  if (Nq < 0 || Nk < 0 || Nq > (1 << 30) || Nk > (1 << 30)) return 0;
-  if (n_seq < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || d_head < 1 || d_head > 128) return 0;
-  return sp::plan_cut(Nq, Nk, n_seq, n_heads, n_kv_heads, d_head, dtype).bytes;
-}
-
-sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream) {
-  using namespace sp;
+sp_status attention_forward(const sp_attention_args* a, const void* k_lo, const void* v_lo, int32_t* status_dev, void* ws, size_t ws_bytes,
+                            cudaStream_t s) {
   if (!a) return SP_ERR_INVALID_ARG;
   const int32_t dt = a->Q.dtype;
   if (dt != SP_F32 && dt != SP_BF16) return SP_ERR_DTYPE;
@@ -395,6 +385,7 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
   // (a single row has no pitch: whatever stands there is not used)
   p.ldq = Nq > 1 ? a->Q.ld : a->Q.cols; p.ldk = Nk > 1 ? a->K.ld : a->K.cols;
   p.ldv = Nk > 1 ? a->V.ld : a->V.cols; p.ldo = Nq > 1 ? a->O.ld : a->O.cols;
+  p.k_lo = k_lo; p.v_lo = v_lo;
   p.lse = a->lse;
   p.cu_q = a->cu_q; p.cu_k = a->cu_k;
   p.Nq = (int32_t)Nq; p.Nk = (int32_t)Nk;
@@ -408,7 +399,6 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
                                           align_up((size_t)cut.max_parts * Nq * a->n_heads * dh * 4, 256));
   }
   p.status = status_dev;
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const bool tc = dt == SP_BF16 && attention_tc_supported(p);
   ProfScope prof(tc ? PK_GEMM_TC : PK_GEMM_SIMT, 0.0, 0.0, s);
   count_launch();
@@ -430,6 +420,21 @@ sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws
     if (e != cudaSuccess) return SP_ERR_CUDA;
   }
   return SP_OK;
+}
+
+}  // namespace sp
+
+extern "C" {
+
+size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
+                                    int32_t d_head, int32_t dtype) {
+  if (Nq < 0 || Nk < 0 || Nq > (1 << 30) || Nk > (1 << 30)) return 0;
+  if (n_seq < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || d_head < 1 || d_head > 128) return 0;
+  return sp::plan_cut(Nq, Nk, n_seq, n_heads, n_kv_heads, d_head, dtype).bytes;
+}
+
+sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream) {
+  return sp::attention_forward(a, nullptr, nullptr, status_dev, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

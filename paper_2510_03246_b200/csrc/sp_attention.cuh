@@ -6,6 +6,7 @@ namespace sp {
 
 struct AttnParams {
   const void *q, *k, *v;
+  const void *k_lo, *v_lo;     // tcgen05 form: second bf16 parts of keys and values at their pitches, or null
   void* o;
   int64_t ldq, ldk, ldv, ldo;
   float* lse;
@@ -122,5 +123,8 @@ cudaError_t attention_rows_f32(const AttnParams& p, cudaStream_t stream);
 // tcgen05 form (sp_attention_tc.cu): layouts that tensor maps can describe
 bool attention_tc_supported(const AttnParams& a);
 sp_status attention_tc(const AttnParams& a, cudaStream_t stream);
+// sp_attention; k_lo, v_lo (both or none): what its tcgen05 form adds to keys and values (the other forms read the first parts alone).
+sp_status attention_forward(const sp_attention_args* a, const void* k_lo, const void* v_lo, int32_t* status_dev, void* ws, size_t ws_bytes,
+                            cudaStream_t stream);
 
 }  // namespace sp

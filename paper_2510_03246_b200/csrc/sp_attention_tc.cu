@@ -22,6 +22,8 @@
 // What bounds it: per half and tile 128 exponentials a row (1024 cycles of the pipe that two warps share) between two products (1024 cycles
 // together for heads of 128).  One prompt of 8192, 32 heads of 128 on 8: 488 us after a pause, 531 in a row of calls (power cap); 16 documents of up to
 // 2048 tokens, 32 heads of 64 on 8: 167 and 156 us.  (Figures beside the steps below are of the kernel of that time.)
+// LO: keys and values in two bf16 parts that add up to them (opened from a cache of 4 bits): a key tile is four stages, the parts of K and those of V,
+// and S = Q K^T + Q K_lo^T, O += P V + P V_lo in one accumulator each.
 // Waits for copies, the tensor core and other warps are bounded by a clock budget (SP_ERR_TIMEOUT through status).
 #include <math.h>
 #include <string.h>
@@ -187,13 +189,13 @@ struct Brief {
 };
 constexpr int kBriefs = 8;             // more than the buffers of S: items between the issue of S and of P V
 
-// A walk over the jobs of an item: key tile by key tile, the halves that see the tile.  (Half 1 has the later rows and sees no fewer tiles
+// A walk over the jobs of an item, `per` stages of the ring to a key tile: key tile by key tile, the halves that see the tile.  (Half 1 has the later rows and sees no fewer tiles
 // than half 0; a tile of rows without half 1 is half 0 alone.)
 struct Cursor {
   Brief w;
   int i, h;                            // key tile, half
   int b = 0;                           // buffer of S and P
-  int stage = 0;                       // of the ring: the tile's K, its V is in the next one
+  int stage = 0;                       // of the ring: the tile's K, behind it K's lower part (LO) and V
   bool open = false;
   __device__ __forceinline__ void start(const Brief& of) {
     w = of;
@@ -204,24 +206,25 @@ struct Cursor {
   __device__ __forceinline__ int tiles() const { return w.n0 > w.n1 ? w.n0 : w.n1; }
   __device__ __forceinline__ bool first() const { return h == 0 || w.n0 <= i; }       // of the tile
   __device__ __forceinline__ bool last() const { return h == 1 || w.n1 <= i; }
-  __device__ __forceinline__ void advance(int bufs, int stages) {
+  __device__ __forceinline__ void advance(int bufs, int stages, int per) {
     b = b + 1 == bufs ? 0 : b + 1;
     if (!last()) {
       h = 1;
       return;
     }
     ++i;
-    stage = stage + 2 >= stages ? stage + 2 - stages : stage + 2;
+    stage = stage + per >= stages ? stage + per - stages : stage + per;
     h = w.n0 > i ? 0 : 1;
     open = i < tiles();
   }
 };
 
-template <int DH>
+template <int DH, bool LO>
 __global__ void __launch_bounds__(kThreads, 1)
-attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                    const __grid_constant__ CUtensorMap tmV, const TcAttnParams p) {
+attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                    const __grid_constant__ CUtensorMap tmKlo, const __grid_constant__ CUtensorMap tmVlo, const TcAttnParams p) {
   using C = Cfg<DH>;
+  constexpr int PARTS = LO ? 2 : 1, PER = 2 * PARTS;      // stages of K or V of a key tile, of the tile
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort;
@@ -334,15 +337,17 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               for (int c = 0; c < C::CH; ++c)
                 tma_load_3d(q_smem + h * C::TILE + c * C::CHUNK, &tmQ, c * 64, it.head * p.gp, it.q0 + w.t0 + h * p.tokens, q_full);
           }
-          for (int i = 0; i < 2 * n && ok; ++i) {
+          for (int i = 0; i < PER * n && ok; ++i) {
             const int s = (int)(pos % C::STAGES);
             if (!mbar_wait(empty_bar(s), (pos / C::STAGES + 1) & 1u, abort_flag, budget)) { ok = false; break; }
-            const bool v = i & 1;
-            const uint32_t bar = v && w.edge(i >> 1) ? edge_bar(s) : full_bar(s);
+            const int tile = i / PER, part = i % PER;      // K, (its lower part,) V, (its lower part)
+            const bool v = part >= PARTS;
+            const CUtensorMap* map = v ? (LO && part == 3 ? &tmVlo : &tmV) : (LO && part == 1 ? &tmKlo : &tmK);
+            const uint32_t bar = v && w.edge(tile) ? edge_bar(s) : full_bar(s);
             mbar_expect_tx(bar, C::TILE);
   #pragma unroll
             for (int c = 0; c < C::CH; ++c)
-              tma_load_3d(ring + s * C::TILE + c * C::CHUNK, v ? &tmV : &tmK, c * 64, kvh, it.k0 + w.kb + (i >> 1) * kKeys, bar);
+              tma_load_3d(ring + s * C::TILE + c * C::CHUNK, map, c * 64, kvh, it.k0 + w.kb + tile * kKeys, bar);
             ++pos;
           }
         }
@@ -369,13 +374,26 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         uint32_t full_ph = 0, ready_ph = 0, p_ph = 0;    // phases of the barriers of a stage, of a buffer: a bit each
         int items_s = 0, items_v = 0;                    // items that the cursors have been given
         int ahead = 0;                                   // jobs whose S is issued and whose P V is not
-        bool end = false, issued = false, keys = false;  // keys: K of the next S has been waited for
+        bool end = false, issued = false, keys = false;  // keys: K of the next S (LO: both parts) has been waited for
+        bool upper = false;                              // LO: its upper part has
         Cursor cs, cv;
         long long t0 = 0;                                // since when nothing could be issued (0: something was)
         auto keys_there = [&] {                          // of the next S
           if (!cs.open) return false;
           if (!cs.first() || keys) return true;
           const int s = cs.stage;
+          if constexpr (LO) {
+            const int t = s + 1 == C::STAGES ? 0 : s + 1;
+            if (!upper) {
+              upper = mbar_test(full_bar(s), (full_ph >> s) & 1u);
+              if (upper) full_ph ^= 1u << s;
+            }
+            if (upper) {
+              keys = mbar_test(full_bar(t), (full_ph >> t) & 1u);
+              if (keys) full_ph ^= 1u << t;
+            }
+            return keys;
+          }
           keys = mbar_test(full_bar(s), (full_ph >> s) & 1u);
           if (keys) full_ph ^= 1u << s;
           return keys;
@@ -389,15 +407,25 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
             tc_mma_ss(d, a0 + off, b0 + off, id_s, k > 0);
           }
+          const int t = s + 1 == C::STAGES ? 0 : s + 1;
+          if constexpr (LO) {
+            const uint32_t b1 = desc_low(ring + t * C::TILE, 16);
+#pragma unroll
+            for (int k = 0; k < DH / 16; ++k) {
+              const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
+              tc_mma_ss(d, a0 + off, b1 + off, id_s, 1u);
+            }
+          }
           tc_commit_one(s_full(cs.h, cs.b));
           if (cs.last()) {
             tc_commit_one(empty_bar(s));
+            if constexpr (LO) tc_commit_one(empty_bar(t));
             if (cs.i + 1 == cs.tiles()) tc_commit_one(q_empty);
           }
           issued = true;
-          keys = false;
+          keys = upper = false;
           ++ahead;
-          cs.advance(C::BUFS, C::STAGES);
+          cs.advance(C::BUFS, C::STAGES, PER);
         };
         while (true) {
           if (!cs.open && !end && mbar_test(q_full, (uint32_t)items_s & 1u)) {
@@ -415,35 +443,49 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           if (ahead > 0) {
             if (!cv.open) cv.start(s_brief[items_v++ % kBriefs]);
             if (mbar_test(p_half(cv.b), (p_ph >> cv.b) & 1u)) {
-              const int s = cv.stage + 1 == C::STAGES ? 0 : cv.stage + 1;
+              const auto stage_of = [&](int part) { return cv.stage + part >= C::STAGES ? cv.stage + part - C::STAGES : cv.stage + part; };
+              const int s = stage_of(PARTS);
               if (cv.first()) {
-                if (cv.i >= cv.w.edge) {
-                  ok = mbar_wait(ready_bar(s), (ready_ph >> s) & 1u, abort_flag, budget);
-                  ready_ph ^= 1u << s;
-                } else {
-                  ok = mbar_wait(full_bar(s), (full_ph >> s) & 1u, abort_flag, budget);
-                  full_ph ^= 1u << s;
+#pragma unroll
+                for (int x = 0; x < PARTS; ++x) {
+                  const int t = stage_of(PARTS + x);
+                  if (cv.i >= cv.w.edge) {
+                    ok = ok && mbar_wait(ready_bar(t), (ready_ph >> t) & 1u, abort_flag, budget);
+                    ready_ph ^= 1u << t;
+                  } else {
+                    ok = ok && mbar_wait(full_bar(t), (full_ph >> t) & 1u, abort_flag, budget);
+                    full_ph ^= 1u << t;
+                  }
                 }
                 if (!ok) break;
               }
               // (P of a half's first key tile also says that its warps have read O of the item before)
               const uint32_t d = tmem + C::O_COL + C::O_COLS * cv.h, a0 = tmem + 128u * cv.b;
-              const uint32_t v0 = desc_low(ring + s * C::TILE, C::CHUNK);
+              const uint32_t v0 = desc_low(ring + s * C::TILE, C::CHUNK), v1 = desc_low(ring + stage_of(PER - 1) * C::TILE, C::CHUNK);
               tc_fence_after();
 #pragma unroll
-              for (int k = 0; k < kKeys / 32; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, cv.i > 0 || k > 0);
+              for (int k = 0; k < kKeys / 32; ++k) {
+                tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, cv.i > 0 || k > 0);
+                if constexpr (LO) tc_mma_ts(d, a0 + 8u * k, v1 + 128u * k, id_o, 1u);
+              }
               const bool more = keys_there();            // (before the wait: S of the next job follows the product at once)
               ok = mbar_wait(p_full(cv.b), (p_ph >> cv.b) & 1u, abort_flag, budget);
               p_ph ^= 1u << cv.b;
               if (!ok) break;
               tc_fence_after();
 #pragma unroll
-              for (int k = kKeys / 32; k < kKeys / 16; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, 1u);
+              for (int k = kKeys / 32; k < kKeys / 16; ++k) {
+                tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, 1u);
+                if constexpr (LO) tc_mma_ts(d, a0 + 8u * k, v1 + 128u * k, id_o, 1u);
+              }
               --ahead;
               if (C::BUFS == 2 && more) issue_s();       // (with three: 184 us for the documents)
               tc_commit_one(pv_done(cv.h));
-              if (cv.last()) tc_commit_one(empty_bar(s));
-              cv.advance(C::BUFS, C::STAGES);
+              if (cv.last()) {
+                tc_commit_one(empty_bar(s));
+                if constexpr (LO) tc_commit_one(empty_bar(stage_of(PER - 1)));
+              }
+              cv.advance(C::BUFS, C::STAGES, PER);
               t0 = 0;
               continue;
             }
@@ -481,9 +523,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const int n = w.tiles();
         if (n == 0) continue;
         patience = budget + 20000ll * n;
-        for (int i = 0; i < n && ok; ++i, pos += 2) {
+        for (int x = 0; x < PARTS * n && ok; ++x, pos += x % PARTS == 0 ? PER - PARTS + 1 : 1) {      // (pos: stages before K of the tile, plus x % PARTS)
+          const int i = x / PARTS;
           if (!w.edge(i)) continue;
-          const int s = (int)((pos + 1) % C::STAGES);
+          const int s = (int)((pos + PARTS) % C::STAGES);
           const bool got = mbar_wait(edge_bar(s), (edge_ph >> s) & 1u, abort_flag, patience);
           edge_ph ^= 1u << s;
           ok = __all_sync(0xffffffffu, got);
@@ -497,8 +540,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   #pragma unroll
             for (int c = 0; c < C::CH; ++c)
   #pragma unroll
-              for (int x = 0; x < 8; ++x) {
-                uint4* at = reinterpret_cast<uint4*>(tile + c * C::CHUNK + j * 128 + ((x + j) & 7) * 16);
+              for (int y = 0; y < 8; ++y) {
+                uint4* at = reinterpret_cast<uint4*>(tile + c * C::CHUNK + j * 128 + ((y + j) & 7) * 16);
                 if (clear) {
                   *at = make_uint4(0u, 0u, 0u, 0u);
                 } else {
@@ -754,17 +797,17 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   }
 }
 
-template <int DH>
-sp_status launch_tc(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const TcAttnParams& p, int64_t work,
-                    cudaStream_t stream) {
+template <int DH, bool LO>
+sp_status launch_tc(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmKlo, const CUtensorMap& tmVlo,
+                    const TcAttnParams& p, int64_t work, cudaStream_t stream) {
   static PerDeviceOnce attr_once;
-  const auto kernel = attention_tc_kernel<DH>;
+  const auto kernel = attention_tc_kernel<DH, LO>;
   if (attr_once.run([&] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<DH>::SMEM);
       }) != cudaSuccess)
     return SP_ERR_CUDA;
   const dim3 grid((unsigned)(work < sm_count() ? work : sm_count()));
-  return launch(kernel, grid, dim3(kThreads), Cfg<DH>::SMEM, stream, tmQ, tmK, tmV, p) == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+  return launch(kernel, grid, dim3(kThreads), Cfg<DH>::SMEM, stream, tmQ, tmK, tmV, tmKlo, tmVlo, p) == cudaSuccess ? SP_OK : SP_ERR_CUDA;
 }
 
 }  // namespace
@@ -784,14 +827,20 @@ sp_status attention_tc(const AttnParams& a, cudaStream_t stream) {
   p.tokens = kRows / p.gp;
   p.heads = p.gp == 1 ? a.n_heads : a.n_kv;
   p.vec_out = a.ldo % 8 == 0 && (reinterpret_cast<uintptr_t>(a.o) & 15u) == 0;
-  CUtensorMap tmQ, tmK, tmV;
+  CUtensorMap tmQ, tmK, tmV, tmKlo, tmVlo;
+  memset(&tmKlo, 0, sizeof(tmKlo));
+  memset(&tmVlo, 0, sizeof(tmVlo));
   if (!make_map3(&tmQ, a.q, a.dh, a.n_heads, a.Nq, a.dh, a.ldq, 64, p.gp, p.tokens) ||
       !make_map3(&tmK, a.k, a.dh, a.n_kv, a.Nk, a.dh, a.ldk, 64, 1, kKeys) ||
-      !make_map3(&tmV, a.v, a.dh, a.n_kv, a.Nk, a.dh, a.ldv, 64, 1, kKeys))
+      !make_map3(&tmV, a.v, a.dh, a.n_kv, a.Nk, a.dh, a.ldv, 64, 1, kKeys) ||
+      (a.k_lo && (!make_map3(&tmKlo, a.k_lo, a.dh, a.n_kv, a.Nk, a.dh, a.ldk, 64, 1, kKeys) ||
+                  !make_map3(&tmVlo, a.v_lo, a.dh, a.n_kv, a.Nk, a.dh, a.ldv, 64, 1, kKeys))))
     return SP_ERR_CUDA;
   const int64_t tiles = min((int64_t)a.Nq / (2 * p.tokens) + a.n_seq, (int64_t)a.Nq);
   const int64_t work = tiles * p.heads * (a.part > 0 ? a.max_parts : 1);
-  return a.dh <= 64 ? launch_tc<64>(tmQ, tmK, tmV, p, work, stream) : launch_tc<128>(tmQ, tmK, tmV, p, work, stream);
+  if (a.k_lo)
+    return a.dh <= 64 ? launch_tc<64, true>(tmQ, tmK, tmV, tmKlo, tmVlo, p, work, stream) : launch_tc<128, true>(tmQ, tmK, tmV, tmKlo, tmVlo, p, work, stream);
+  return a.dh <= 64 ? launch_tc<64, false>(tmQ, tmK, tmV, tmKlo, tmVlo, p, work, stream) : launch_tc<128, false>(tmQ, tmK, tmV, tmKlo, tmVlo, p, work, stream);
 }
 
 }  // namespace sp

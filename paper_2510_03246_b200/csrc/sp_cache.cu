@@ -275,10 +275,16 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Appe
   }
 }
 
+// what rounding to bf16 leaves (nothing of a NaN, an infinity, or a value that rounds to one)
+__device__ __forceinline__ float left_of(float x) {
+  const float hi = __bfloat162float(__float2bfloat16_rn(x));
+  return fabsf(hi) < INFINITY ? x - hi : 0.f;
+}
+
 struct ReadParams {
   CacheView c;
   const int32_t* cu;
-  void *k, *v;
+  void *k, *v, *k_lo, *v_lo;
   int64_t ldk, ldv;
   int32_t rows, whole, k_vec, v_vec;
   int32_t* status;
@@ -325,6 +331,15 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
     }
     put8(reinterpret_cast<T*>(p.k) + row * p.ldk + head * dh + 8 * chunk, p.k_vec != 0, x);
     put8(reinterpret_cast<T*>(p.v) + row * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, y);
+    if (p.k_lo) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        x[k] = left_of(x[k]);
+        y[k] = left_of(y[k]);
+      }
+      put8(reinterpret_cast<__nv_bfloat16*>(p.k_lo) + row * p.ldk + head * dh + 8 * chunk, true, x);
+      put8(reinterpret_cast<__nv_bfloat16*>(p.v_lo) + row * p.ldv + head * dh + 8 * chunk, true, y);
+    }
   }
 }
 
@@ -368,11 +383,11 @@ CacheView cache_view(const sp_kv_cache* c) {
 }
 
 cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
-                       bool whole, int32_t* status, cudaStream_t stream) {
+                       bool whole, int32_t* status, cudaStream_t stream, void* K_lo, void* V_lo) {
   ReadParams p = {};
   p.c = cache_view(c);
   p.cu = cu;
-  p.k = K; p.v = V; p.ldk = ldk; p.ldv = ldv;
+  p.k = K; p.v = V; p.k_lo = K_lo; p.v_lo = V_lo; p.ldk = ldk; p.ldv = ldv;
   p.rows = (int32_t)rows;
   p.whole = whole ? 1 : 0;
   p.k_vec = rows_of_16(K, ldk, dtype, rows); p.v_vec = rows_of_16(V, ldv, dtype, rows);

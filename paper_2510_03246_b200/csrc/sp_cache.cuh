@@ -43,7 +43,8 @@ __device__ __forceinline__ int32_t page_of(const CacheView& c, int32_t s, int32_
 sp_status check_cache(const sp_kv_cache* c, bool pages);
 CacheView cache_view(const sp_kv_cache* c);
 // Reads n = cu[s + 1] - cu[s] last tokens of every sequence (sp_cache_read); whole: rows of a sequence with another number of tokens than n are NaN.
+// K_lo, V_lo: bf16 at the pitches of K and V, what the rounding to bf16 has left (4 bits), or null.
 cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
-                       bool whole, int32_t* status, cudaStream_t stream);
+                       bool whole, int32_t* status, cudaStream_t stream, void* K_lo = nullptr, void* V_lo = nullptr);
 
 }  // namespace sp

@@ -14,9 +14,12 @@
 // outside the matrix unit.
 //
 // More rows open the pages into bf16 or fp32 rows in the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor
-// cores' rate, where this form would open them again for every 16 rows.
+// cores' rate, where this form would open them again for every 16 rows.  4 bits are opened into two bf16 parts: rounded to one,
+// logits were off by 2^-9 of |q| |k| (512 queries after 16384 keys, 32 heads of 128 on 8: results 4.2e-3 from the formula), and values of equal
+// scales by the same in every key, which no sum over keys takes away.
 #include <math.h>
 
+#include "sp_attention.cuh"
 #include "sp_cache.cuh"
 #include "sp_f32x2.cuh"
 
@@ -105,10 +108,13 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
 }
 // The bf16 pair (16 + n_i, 16 + n_{i + 4}) of a word of eight numbers: the mantissa's last bit of 16 .. 31 is 1 / 8, so that a number stands
 // in bits 3 .. 6.  (An offset of 128, numbers in the lowest bits, would leave the sums eight times as large.)
-template <int I>
+// C16 false: 24 less, -8 .. 7, for fp32: sums of larger numbers would round by more.
+template <int I, bool C16>
 __device__ __forceinline__ uint32_t opened(uint32_t w) {
-  const uint32_t at = I == 0 ? w << 3 : w >> (4 * I - 3);
-  return (at & 0x00780078u) | 0x41804180u;
+  const uint32_t at = I == 0 ? w << 3 : w >> (4 * I - 3), v = (at & 0x00780078u) | 0x41804180u;
+  if (C16) return v;
+  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __floats2bfloat162_rn(24.f, 24.f));
+  return *reinterpret_cast<const uint32_t*>(&d);
 }
 __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
@@ -189,6 +195,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
   using C = PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>;
   using R = typename C::R;
   constexpr int H = ROWS / 8, PARTS = sizeof(T) == 4 ? 3 : 1, G = FOUR ? R::G : 1, K16 = DH / 16;
+  constexpr bool C16 = PARTS == 1;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int32_t s_first[kPlanSeqs + 1];
   __shared__ int64_t s_word[kWarps];
@@ -402,28 +409,25 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
           for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int x = 0; x < 4; ++x) a[h][x] = 0.f;
-          uint2 w[2];
+          uint2 w[2];                                            // keys g4, g4 + 8
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const uint32_t byte = (uint32_t)((g4 + 8 * y) * (DH / 2) + 32 * gr + 8 * t4);
             w[y] = lds64(stage + (byte ^ ((byte >> 2) & 0x60u)));
           }
+          const uint32_t n[4][4] = {{opened<0, C16>(w[0].x), opened<0, C16>(w[1].x), opened<1, C16>(w[0].x), opened<1, C16>(w[1].x)},
+                                    {opened<2, C16>(w[0].x), opened<2, C16>(w[1].x), opened<3, C16>(w[0].x), opened<3, C16>(w[1].x)},
+                                    {opened<0, C16>(w[0].y), opened<0, C16>(w[1].y), opened<1, C16>(w[0].y), opened<1, C16>(w[1].y)},
+                                    {opened<2, C16>(w[0].y), opened<2, C16>(w[1].y), opened<3, C16>(w[0].y), opened<3, C16>(w[1].y)}};
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const uint32_t lo8 = u == 0 ? w[0].x : w[0].y, hi8 = u == 0 ? w[1].x : w[1].y;
-            const uint32_t a0 = opened<0>(lo8), a1 = opened<0>(hi8), a2 = opened<1>(lo8), a3 = opened<1>(hi8);
-            const uint32_t b0 = opened<2>(lo8), b1 = opened<2>(hi8), b2 = opened<3>(lo8), b3 = opened<3>(hi8);
+          for (int x = PARTS - 1; x >= 0; --x)                   // (small parts first: their sums round less)
 #pragma unroll
-            for (int h = 0; h < H; ++h)
+            for (int u = 0; u < 4; ++u)
 #pragma unroll
-              for (int x = 0; x < PARTS; ++x) {
-                mma(a[h], a0, a1, a2, a3, q[h][x][4 * gr + 2 * u][0], q[h][x][4 * gr + 2 * u][1]);
-                mma(a[h], b0, b1, b2, b3, q[h][x][4 * gr + 2 * u + 1][0], q[h][x][4 * gr + 2 * u + 1][1]);
-              }
-          }
+              for (int h = 0; h < H; ++h) mma(a[h], n[u][0], n[u][1], n[u][2], n[u][3], q[h][x][4 * gr + u][0], q[h][x][4 * gr + u][1]);
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const float scale = low(pair[y][gr]), zero = fmaf(-16.f, scale, high(pair[y][gr]));
+            const float scale = low(pair[y][gr]), zero = fmaf(C16 ? -16.f : 8.f, scale, high(pair[y][gr]));
 #pragma unroll
             for (int h = 0; h < H; ++h)
 #pragma unroll
@@ -441,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
           for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int x = 0; x < PARTS; ++x) mma(s[h], a[0], a[1], a[2], a[3], q[h][x][j][0], q[h][x][j][1]);
+            for (int x = PARTS - 1; x >= 0; --x) mma(s[h], a[0], a[1], a[2], a[3], q[h][x][j][0], q[h][x][j][1]);
         }
       }
       // a block of a page that is none: NaN to every row that sees it
@@ -457,9 +461,8 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
       for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          float& u = s[h][x];
-          u *= p.scale_log2;
-          if (edge && kt + 8 * (x >> 1) + g4 >= lim[h][x & 1]) u = -INFINITY;
+          if (edge && kt + 8 * (x >> 1) + g4 >= lim[h][x & 1]) s[h][x] = -INFINITY;
+          const float u = s[h][x] * p.scale_log2;
           rise |= u != -INFINITY && !(u - r[h][x & 1] <= 8.f);
         }
       if (__any_sync(0xffffffffu, rise)) {                       // seldom: the references follow the maxima of this block
@@ -468,8 +471,9 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
           float f[2];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            float m = fmaxf(s[h][x], s[h][2 + x]);
-            const bool nan = s[h][x] != s[h][x] || s[h][2 + x] != s[h][2 + x];
+            float m = fmaxf(s[h][x], s[h][2 + x]) * p.scale_log2;
+            // (beyond fp32: NaN, too)
+            const bool nan = s[h][x] != s[h][x] || s[h][2 + x] != s[h][2 + x] || m == INFINITY;
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
             if (__ballot_sync(0xffffffffu, nan) & (0x11111111u << t4)) m = NAN;      // (the lanes of these rows)
@@ -491,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const float ref = r[h][x & 1];
-          s[h][x] = exp2_fast(s[h][x] - (ref == -INFINITY ? 0.f : ref));      // now probabilities, to the reference
+          s[h][x] = exp2_fast(fmaf(s[h][x], p.scale_log2, ref == -INFINITY ? 0.f : -ref));      // now probabilities, to the reference
           l[h][x & 1] += s[h][x];
         }
       const uint32_t vtile = stage + R::TILE;
@@ -518,12 +522,16 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
               }
               uint32_t u[PARTS];
               split<PARTS>(ps[0], ps[1], u);
-              if (PARTS == 1) {                                  // what the product is taken with: its 16s have to go again
-                ps[0] = low(u[0]);
-                ps[1] = high(u[0]);
+              // what stands in the product beside the numbers goes again: fp32 16 - 24 = -8.  bf16: 16 of the rounded ps; and of the numbers
+              // themselves their middle 7.5 is taken back with the rounded ps and added with the exact one, so that a rounding only weighs a
+              // number's distance from the middle (16 tokens after 2048 .. 31013 keys: 4.7e-3 from the formula without, 2.0e-3)
+              if constexpr (PARTS == 1) {
+                zero_part[h][gr][0] += fmaf(-23.5f, low(u[0]), fmaf(7.5f, ps[0], pz[0]));
+                zero_part[h][gr][1] += fmaf(-23.5f, high(u[0]), fmaf(7.5f, ps[1], pz[1]));
+              } else {
+                zero_part[h][gr][0] += fmaf(8.f, ps[0], pz[0]);
+                zero_part[h][gr][1] += fmaf(8.f, ps[1], pz[1]);
               }
-#pragma unroll
-              for (int x = 0; x < 2; ++x) zero_part[h][gr][x] += fmaf(-16.f, ps[x], pz[x]);
 #pragma unroll
               for (int x = 0; x < PARTS; ++x) pb[h][x][y] = turned8x8(u[x]);
             }
@@ -536,10 +544,10 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
           // numbers 0 .. 3 and 4 .. 7 of two keys side by side
           const uint32_t m0 = __byte_perm(w[0], w[1], 0x5410), m1 = __byte_perm(w[0], w[1], 0x7632);
           const uint32_t m2 = __byte_perm(w[2], w[3], 0x5410), m3 = __byte_perm(w[2], w[3], 0x7632);
-          const uint32_t a[4][4] = {{opened<0>(m0), opened<0>(m1), opened<0>(m2), opened<0>(m3)},
-                                    {opened<1>(m0), opened<1>(m1), opened<1>(m2), opened<1>(m3)},
-                                    {opened<2>(m0), opened<2>(m1), opened<2>(m2), opened<2>(m3)},
-                                    {opened<3>(m0), opened<3>(m1), opened<3>(m2), opened<3>(m3)}};
+          const uint32_t a[4][4] = {{opened<0, C16>(m0), opened<0, C16>(m1), opened<0, C16>(m2), opened<0, C16>(m3)},
+                                    {opened<1, C16>(m0), opened<1, C16>(m1), opened<1, C16>(m2), opened<1, C16>(m3)},
+                                    {opened<2, C16>(m0), opened<2, C16>(m1), opened<2, C16>(m2), opened<2, C16>(m3)},
+                                    {opened<3, C16>(m0), opened<3, C16>(m1), opened<3, C16>(m2), opened<3, C16>(m3)}};
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -828,14 +836,16 @@ __global__ void __launch_bounds__(kThreads) open_plan_kernel(const CacheView c, 
 
 struct OpenPlan {
   int64_t rows;
-  size_t cu_bytes, k_bytes, attention;
-  size_t bytes() const { return cu_bytes + 2 * k_bytes + attention; }
+  size_t cu_bytes, k_bytes, lo_bytes, attention;
+  size_t bytes() const { return cu_bytes + 2 * k_bytes + 2 * lo_bytes + attention; }
 };
+// (room for the second parts whatever the cache is: the workspace depends on the sizes that its call is given)
 OpenPlan open_plan(int64_t Nq, int64_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype, int64_t max_keys) {
   OpenPlan r;
   r.rows = max_keys + Nq;
   r.cu_bytes = align_up((size_t)(n_seq + 1) * 4, 256);
   r.k_bytes = align_up((size_t)r.rows * n_kv * dh * dtype_size(dtype), 256);
+  r.lo_bytes = dtype == SP_BF16 && dh % kCacheGroup == 0 ? r.k_bytes : 0;
   r.attention = sp_attention_workspace_bytes(Nq, r.rows, (int32_t)n_seq, n_heads, n_kv, dh, dtype);
   return r;
 }
@@ -916,12 +926,14 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   const int64_t keys = keys_at_most(max_keys, n_seq, cache->max_pages, cache->page_len);
   const OpenPlan plan = open_plan(Nq, n_seq, n_heads, n_kv, dh, dt, keys);
   int32_t* cu_k = reinterpret_cast<int32_t*>(at);
-  uint8_t *K = at + plan.cu_bytes, *V = K + plan.k_bytes;
+  uint8_t *K = at + plan.cu_bytes, *V = K + plan.k_bytes, *rest = V + plan.k_bytes + 2 * plan.lo_bytes;
+  const bool parts = dt == SP_BF16 && cache->kind == SP_CACHE_4BIT;
+  uint8_t *K_lo = parts ? V + plan.k_bytes : nullptr, *V_lo = parts ? K_lo + plan.lo_bytes : nullptr;
   const int64_t kv = (int64_t)n_kv * dh;
   count_launch();
   if (launch(open_plan_kernel, dim3(1), dim3(kThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, status_dev) !=
           cudaSuccess ||
-      cache_read(cache, cu_k, plan.rows, K, V, kv, kv, dt, true, status_dev, s) != cudaSuccess)
+      cache_read(cache, cu_k, plan.rows, K, V, kv, kv, dt, true, status_dev, s, K_lo, V_lo) != cudaSuccess)
     return SP_ERR_CUDA;
   sp_attention_args a = {};
   a.Q = *Q;
@@ -932,7 +944,7 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   a.lse = lse;
   a.n_seq = n_seq; a.n_heads = n_heads; a.n_kv_heads = n_kv; a.causal = causal;
   a.scale = scale;
-  return sp_attention(&a, status_dev, V + plan.k_bytes, plan.attention, stream);
+  return attention_forward(&a, K_lo, V_lo, status_dev, rest, plan.attention, s);
 }
 
 }  // extern "C"
