@@ -631,7 +631,7 @@ sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const sp_mat* W,
  * number.  K, V: [N, n_kv_heads * d_head], Q: [N, n_heads * d_head] or none (ptr NULL), one dtype (SP_BF16 or SP_F32), any ld, so that they may be column
  * slices of one matrix.  The first `turned` channels (a multiple of 16, 0 .. d_head) of every query and key head are turned by their position: pair
  * i of channels (i, i + turned / 2), with neighbours != 0 (2 i, 2 i + 1), by the angle position * inv_freq[i], (a, b) -> (a cos - b sin,
- * b cos + a sin); inv_freq: fp32 [turned / 2]; the angle and what goes to 4 bits in fp64, the rest in fp32.  position is p, or positions[row] (int32
+ * b cos + a sin); inv_freq: fp32 [turned / 2]; the angle, its cosine and sine and what goes to 4 bits in fp64, the rest by its steps in fp32.  position is p, or positions[row] (int32
  * [N]) where given.  Q_out [N, n_heads * d_head]: the turned queries, may be Q itself.  K_out: the turned keys, or none; not K itself.
  * A cache without pages (k NULL; then lens may be NULL, p = i, and V is not read) only turns.  Rows of no sequence are left alone.
  * sp_cache_read: the values that the cache holds for the last n = cu[s+1] - cu[s] tokens of every sequence, rows as above, into K, V

@@ -11,6 +11,8 @@
 // 16 bytes of bf16, four bytes of a page in 4 bits; the eight lanes of a group find its bounds by shuffles.
 #include <math.h>
 
+#include <type_traits>
+
 #include "sp_cache.cuh"
 
 namespace sp {
@@ -28,6 +30,7 @@ struct AppendParams {
   const int32_t* positions;
   const float* inv_freq;
   int32_t rows, n_heads, turned, neighbours;
+  int32_t per_block;                       // rows of a block
   int32_t q_vec, k_vec, v_vec;             // rows start on 16 bytes
   int32_t* status;
 };
@@ -85,6 +88,10 @@ __device__ __forceinline__ void put8(float* p, bool vec, const float (&x)[8]) {
   }
 }
 
+// A pair (a, b) turned: three roundings each, so that the values are those of the formula's steps in fp32.
+__device__ __forceinline__ float turned_low(float a, float b, float2 cs) { return __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y)); }
+__device__ __forceinline__ float turned_high(float a, float b, float2 cs) { return __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y)); }
+
 // The eight lanes of a group hold eight channels each: their 4-bit numbers packed, and the group's scale and offset in lane 0 of the eight.
 // F: float where the values are what the caller gave, double for rotated ones (see above).
 template <typename F>
@@ -127,54 +134,62 @@ __device__ __forceinline__ uint32_t four_bits(const F (&x)[8], uint32_t& pair) {
   return packed;
 }
 
+// A block has `per_block` consecutive rows: first their places and angles, a warp to a row, then all their chunks of channels in one walk, two of a
+// thread's in flight.  (One row at a time spends most of a block's life on the way to its first chunk: the sequence, its length, its page, the
+// angles, one after the other; 10584 rows of 48 heads of 128 took 145 us.)
+constexpr int kMaxRows = 8;
+// Angle f of a row: the k-th angles of consecutive chunks side by side, since the lanes of a warp read those.
+__device__ __forceinline__ int placed(int f) { return (f & 7) * (kMaxTurned / 16) + (f >> 3); }
 template <typename T, bool FOUR>
-__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const AppendParams p) {
   kernel_begin();
-  __shared__ float2 s_turn[kMaxTurned / 2];                      // cos, sin of the row's angles
-  __shared__ double2 s_exact[FOUR ? kMaxTurned / 2 : 1];         // the same in 64 bits, for keys that go to 4 bits
-  const int32_t row = blockIdx.x;
-  const int32_t s = sequence_of(p.cu, p.c.n_seq, p.rows, row);
-  if (s < 0) return;                                             // (the same answer in every warp)
-  const int32_t i = row - bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - (row - i);
-  const int32_t place = p.c.lens ? p.c.lens[s] - n + i : i;
-  int32_t page = -1, slot = 0;
-  if (p.c.k) {
-    const int32_t entry = place >= 0 ? place / p.c.page_len : -1;
-    page = page_of(p.c, s, entry);
-    slot = place - entry * p.c.page_len;
-    if (page < 0 && threadIdx.x == 0) report_status(p.status, SP_ERR_SHAPE, s, row);
-  }
+  __shared__ float2 s_turn[kMaxRows][kMaxTurned / 2];                       // cos, sin of a row's angles
+  __shared__ double2 s_exact[FOUR ? kMaxRows : 1][kMaxTurned / 2];          // the same in 64 bits, for keys that go to 4 bits
+  __shared__ int32_t s_page[kMaxRows], s_slot[kMaxRows];                    // -2: a row of no sequence
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int32_t row0 = blockIdx.x * p.per_block, rows = min(p.per_block, p.rows - row0);
   const int half = p.turned / 2, dh = p.c.dh;
-  if (half > 0) {
-    const double position = (double)(p.positions ? p.positions[row] : place);
-    for (int f = threadIdx.x; f < half; f += kAppendThreads) {
-      const double turns = position * (double)p.inv_freq[f] * 0.15915494309189533577;      // angle / 2 pi
-      double sn, cs;
-      if (FOUR) {
+  if (warp < rows) {
+    const int32_t row = row0 + warp, s = sequence_of(p.cu, p.c.n_seq, p.rows, row);
+    int32_t page = -2, slot = 0;
+    if (s >= 0) {
+      const int32_t i = row - bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - (row - i);
+      const int32_t place = p.c.lens ? p.c.lens[s] - n + i : i;
+      page = -1;
+      if (p.c.k) {
+        const int32_t entry = place >= 0 ? place / p.c.page_len : -1;
+        page = page_of(p.c, s, entry);
+        slot = place - entry * p.c.page_len;
+        if (page < 0 && lane == 0) report_status(p.status, SP_ERR_SHAPE, s, row);
+      }
+      const double position = half > 0 ? (double)(p.positions ? p.positions[row] : place) : 0.0;
+      for (int f = lane; f < half; f += 32) {
+        const double turns = position * (double)p.inv_freq[f] * 0.15915494309189533577;      // angle / 2 pi
+        double sn, cs;
         sincospi(2.0 * (turns - rint(turns)), &sn, &cs);
-        s_exact[f] = make_double2(cs, sn);
-        s_turn[f] = make_float2((float)cs, (float)sn);
-      } else {
-        float snf, csf;
-        sincospif((float)(2.0 * (turns - rint(turns))), &snf, &csf);
-        s_turn[f] = make_float2(csf, snf);
+        if (FOUR) s_exact[warp][placed(f)] = make_double2(cs, sn);
+        s_turn[warp][placed(f)] = make_float2((float)cs, (float)sn);
       }
     }
-    __syncthreads();
+    if (lane == 0) {
+      s_page[warp] = page;
+      s_slot[warp] = slot;
+    }
   }
+  __syncthreads();
   const int per_head = dh / 8, half8 = half / 8, turned8 = p.turned / 8;
   // queries: a thread has both chunks of a pair, so that a row may be turned in its place
   if (p.q) {
-    const T* q = reinterpret_cast<const T*>(p.q) + row * p.ldq;
-    T* out = reinterpret_cast<T*>(p.q_out) + row * p.ldqo;
-    const bool vec = p.q_vec != 0;
     const int apart = p.neighbours ? 0 : half8;                  // pairs of chunks: chunk and chunk + apart
-    const int units = per_head - apart;
-    for (int e = threadIdx.x; e < p.n_heads * units; e += kAppendThreads) {
-      const int head = e / units, u = e % units;
+    const int units = per_head - apart, of_row = p.n_heads * units, all = rows * of_row;
+    const bool vec = p.q_vec != 0;
+#pragma unroll 2
+    for (int e = threadIdx.x; e < all; e += kAppendThreads) {
+      const int r = e / of_row, x_ = e - r * of_row, head = x_ / units, u = x_ - head * units;
+      if (s_page[r] == -2) continue;
       const int chunk = u < apart || apart == 0 ? u : u + apart;
-      const T* src = q + head * dh;
-      T* dst = out + head * dh;
+      const T* src = reinterpret_cast<const T*>(p.q) + (row0 + r) * p.ldq + head * dh;
+      T* dst = reinterpret_cast<T*>(p.q_out) + (row0 + r) * p.ldqo + head * dh;
       float a[8], b[8];
       load8(src + 8 * chunk, vec, a);
       if (chunk >= turned8) {
@@ -184,9 +199,9 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Appe
         float x[8], y[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const float2 cs = s_turn[8 * chunk + k];
-          x[k] = fmaf(a[k], cs.x, -b[k] * cs.y);
-          y[k] = fmaf(b[k], cs.x, a[k] * cs.y);
+          const float2 cs = s_turn[r][placed(8 * chunk + k)];
+          x[k] = turned_low(a[k], b[k], cs);
+          y[k] = turned_high(a[k], b[k], cs);
         }
         put8(dst + 8 * chunk, vec, x);
         put8(dst + 8 * (chunk + apart), vec, y);
@@ -194,23 +209,42 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Appe
         float x[8];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float2 cs = s_turn[4 * chunk + k];
-          x[2 * k] = fmaf(a[2 * k], cs.x, -a[2 * k + 1] * cs.y);
-          x[2 * k + 1] = fmaf(a[2 * k + 1], cs.x, a[2 * k] * cs.y);
+          const float2 cs = s_turn[r][placed(4 * chunk + k)];
+          x[2 * k] = turned_low(a[2 * k], a[2 * k + 1], cs);
+          x[2 * k + 1] = turned_high(a[2 * k], a[2 * k + 1], cs);
         }
         put8(dst + 8 * chunk, vec, x);
       }
     }
   }
-  // keys: eight channels as they stand side by side in the cache, their partners read beside them; then values
-  const int chunks = p.c.n_kv * per_head, all = (chunks + 31) / 32 * 32;      // (groups of eight lanes stay together)
-  const bool pages = page >= 0;
-  for (int e = threadIdx.x; e < all; e += kAppendThreads) {
-    const bool live = e < chunks;
-    const int head = live ? e / per_head : 0, chunk = live ? e % per_head : 0;
-    const T* src = reinterpret_cast<const T*>(p.k) + row * p.ldk + head * dh;
+  // keys, then values: eight channels as they stand side by side in the cache, a key's partners read beside them
+  const int chunks = p.c.n_kv * per_head, sides = p.c.k ? 2 : 1, of_row = (chunks + 31) / 32 * 32;      // (groups of eight lanes stay together)
+#pragma unroll 2
+  for (int e = threadIdx.x; e < sides * rows * of_row; e += kAppendThreads) {
+    const bool value = e >= rows * of_row;                       // (the same in a warp, as is r)
+    const int f_ = value ? e - rows * of_row : e, r = f_ / of_row, x_ = f_ - r * of_row;
+    const int page = s_page[r];
+    if (page == -2) continue;
+    const bool live = x_ < chunks;
+    const int head = live ? x_ / per_head : 0, chunk = live ? x_ - head * per_head : 0;
+    const int64_t at = (int64_t)head * p.c.page_len + s_slot[r];      // (head, token) of the page
+    float a[8];
+    if (value) {
+      load8(reinterpret_cast<const T*>(p.v) + (row0 + r) * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, a);
+      if constexpr (FOUR) {
+        uint32_t pair;
+        const uint32_t packed = four_bits(a, pair);
+        if (page >= 0 && live) {
+          *reinterpret_cast<uint32_t*>(p.c.v + page * p.c.v_step + at * (dh / 2) + 4 * chunk) = packed;
+          if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.vs + page * p.c.vs_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
+        }
+      } else if (page >= 0 && live) {
+        put8(reinterpret_cast<__nv_bfloat16*>(p.c.v + page * p.c.v_step) + at * dh + 8 * chunk, true, a);
+      }
+      continue;
+    }
+    const T* src = reinterpret_cast<const T*>(p.k) + (row0 + r) * p.ldk + head * dh;
     const bool vec = p.k_vec != 0;
-    float a[8], b[8];
     load8(src + 8 * chunk, vec, a);
     using F = typename std::conditional<FOUR, double, float>::type;
     F x[8];
@@ -218,6 +252,7 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Appe
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = (F)a[k];
     } else {
+      float b[8];
       const bool second = !p.neighbours && chunk >= half8;       // the pair's other value stands `half` channels before, or behind
       if (!p.neighbours) load8(src + 8 * (second ? chunk - half8 : chunk + half8), vec, b);
       const int f0 = p.neighbours ? 4 * chunk : 8 * (second ? chunk - half8 : chunk);
@@ -226,51 +261,30 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Appe
         const int f = p.neighbours ? f0 + k / 2 : f0 + k;
         const float other = p.neighbours ? a[k ^ 1] : b[k];
         const bool up = p.neighbours ? (k & 1) != 0 : second;
-        F c, w;
         if constexpr (FOUR) {
-          c = s_exact[f].x; w = s_exact[f].y;
+          const double2 cs = s_exact[r][placed(f)];
+          x[k] = fma((double)a[k], cs.x, (double)other * (up ? cs.y : -cs.y));
         } else {
-          c = s_turn[f].x; w = s_turn[f].y;
+          const float2 cs = s_turn[r][placed(f)];
+          x[k] = up ? turned_high(other, a[k], cs) : turned_low(a[k], other, cs);
         }
-        const F m = (F)other * w;
-        x[k] = fma((F)a[k], c, up ? m : -m);
       }
     }
     if (p.k_out && live) {
       float y[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) y[k] = (float)x[k];
-      put8(reinterpret_cast<T*>(p.k_out) + row * p.ldko + head * dh + 8 * chunk, vec, y);
+      put8(reinterpret_cast<T*>(p.k_out) + (row0 + r) * p.ldko + head * dh + 8 * chunk, vec, y);
     }
-    if (!p.c.k) continue;                                        // (the same in every thread, as `pages`)
-    const int64_t at = (int64_t)head * p.c.page_len + slot;      // (head, token) of the page
     if constexpr (FOUR) {
       uint32_t pair;
       const uint32_t packed = four_bits(x, pair);
-      if (pages && live) {
+      if (page >= 0 && live) {
         *reinterpret_cast<uint32_t*>(p.c.k + page * p.c.k_step + at * (dh / 2) + 4 * chunk) = packed;
         if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.ks + page * p.c.ks_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
       }
-    } else if (pages && live) {
+    } else if (page >= 0 && live) {
       put8(reinterpret_cast<__nv_bfloat16*>(p.c.k + page * p.c.k_step) + at * dh + 8 * chunk, true, x);
-    }
-  }
-  if (!p.c.k) return;
-  for (int e = threadIdx.x; e < all; e += kAppendThreads) {
-    const bool live = e < chunks;
-    const int head = live ? e / per_head : 0, chunk = live ? e % per_head : 0;
-    float x[8];
-    load8(reinterpret_cast<const T*>(p.v) + row * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, x);
-    const int64_t at = (int64_t)head * p.c.page_len + slot;
-    if constexpr (FOUR) {
-      uint32_t pair;
-      const uint32_t packed = four_bits(x, pair);
-      if (pages && live) {
-        *reinterpret_cast<uint32_t*>(p.c.v + page * p.c.v_step + at * (dh / 2) + 4 * chunk) = packed;
-        if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.vs + page * p.c.vs_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
-      }
-    } else if (pages && live) {
-      put8(reinterpret_cast<__nv_bfloat16*>(p.c.v + page * p.c.v_step) + at * dh + 8 * chunk, true, x);
     }
   }
 }
@@ -452,7 +466,10 @@ sp_status sp_cache_append(const sp_kv_cache* cache, const sp_cache_append_args* 
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   count_launch();
   ProfScope prof(PK_ELEMENTWISE, 0.0, 0.0, s);
-  const dim3 grid((unsigned)N);
+  // as many rows to a block as leave four blocks for every SM
+  const int64_t most = N / (4 * (int64_t)sm_count());
+  p.per_block = most < 1 ? 1 : most < kMaxRows ? (int32_t)most : kMaxRows;
+  const dim3 grid((unsigned)ceil_div(N, (int64_t)p.per_block));
   const bool four = pages && cache->kind == SP_CACHE_4BIT;
   const cudaError_t e = dt == SP_F32 ? (four ? launch(cache_append_kernel<float, true>, grid, dim3(kAppendThreads), 0, s, p)
                                              : launch(cache_append_kernel<float, false>, grid, dim3(kAppendThreads), 0, s, p))

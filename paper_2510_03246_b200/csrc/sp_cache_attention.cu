@@ -9,14 +9,20 @@
 // stages ahead, so that no warp waits for another before the end of an item.  Products are m16n8k16 of bf16, turned so that keys and channels
 // fill them: S^T = K Q^T and O^T += V^T P^T.  The order in which an instruction contracts channels is free, and so is the channel that a row of
 // V^T stands for.  In 4 bits a lane therefore takes whole words of eight numbers as they lie: for K the two words 2 t4, 2 t4 + 1 of a group, for V
-// word g4 of four keys; number n becomes the bf16 16 + n by a shift and one logical operation (for two at a time), and the 16 goes to the offsets.
-// fp32 queries are three bf16 parts that add up to them, as are the probabilities' products with the scales; then sums of 16 keys are added up
-// outside the matrix unit.
+// word g4 of four keys.
+//   K: the byte of a number n is n / 512 as e4m3 (the values below the first power of two and above it lie equally close), so that a mask opens
+//   four of them for m16n8k32 of e4m3, a faster instruction too.  Queries are two e4m3 parts, eight bits of what a power of two per row takes to
+//   128 .. 255; what is lost lies 2^-17 and more below a row's largest value.
+//   V: number n becomes the bf16 16 + n (or 128 + n) by a shift and one logical operation, two at a time; what was added goes to the offsets.
+// fp32 queries are three bf16 parts that add up to them, as are the probabilities' products with the scales; numbers are bf16 for both products, and
+// sums of 16 keys are added up outside the matrix unit.
 //
 // More rows open the pages into bf16 or fp32 rows in the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor
 // cores' rate, where this form would open them again for every 16 rows.  4 bits are opened into two bf16 parts: rounded to one,
 // logits were off by 2^-9 of |q| |k| (512 queries after 16384 keys, 32 heads of 128 on 8: results 4.2e-3 from the formula), and values of equal
 // scales by the same in every key, which no sum over keys takes away.
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
 #include <math.h>
 
 #include "sp_attention.cuh"
@@ -83,6 +89,12 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -106,15 +118,28 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(addr) : "memory");
   return r;
 }
-// The bf16 pair (16 + n_i, 16 + n_{i + 4}) of a word of eight numbers: the mantissa's last bit of 16 .. 31 is 1 / 8, so that a number stands
-// in bits 3 .. 6.  (An offset of 128, numbers in the lowest bits, would leave the sums eight times as large.)
-// C16 false: 24 less, -8 .. 7, for fp32: sums of larger numbers would round by more.
-template <int I, bool C16>
+// The bf16 pair (k + n_i, k + n_{i + 4}) of a word of eight numbers.  The mantissa's last bit of 16 .. 31 is 1 / 8, so that with k = 16 a
+// number stands in bits 3 .. 6; number 0 stands in the lowest bits already, where k is 128 (kOpened).
+__device__ constexpr float kOpened[4] = {128.f, 16.f, 16.f, 16.f};
+template <int I>
 __device__ __forceinline__ uint32_t opened(uint32_t w) {
-  const uint32_t at = I == 0 ? w << 3 : w >> (4 * I - 3), v = (at & 0x00780078u) | 0x41804180u;
-  if (C16) return v;
+  if constexpr (I == 0) return (w & 0x000f000fu) | 0x43004300u;
+  else return ((w >> (4 * I - 3)) & 0x00780078u) | 0x41804180u;
+}
+// The same with k = -8, for fp32: sums of larger numbers would round by more.
+template <int I>
+__device__ __forceinline__ uint32_t opened_centred(uint32_t w) {
+  const uint32_t at = I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3), v = (at & 0x00780078u) | 0x41804180u;
   const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __floats2bfloat162_rn(24.f, 24.f));
   return *reinterpret_cast<const uint32_t*>(&d);
+}
+// four values as e4m3, the first in the lowest byte
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) |
+         (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
+}
+__device__ __forceinline__ float round_e4m3(float a) {
+  return __half2float(__half(__nv_cvt_fp8_to_halfraw(__nv_cvt_float_to_fp8(a, __NV_SATFINITE, __NV_E4M3), __NV_E4M3)));
 }
 __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
@@ -195,7 +220,6 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
   using C = PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>;
   using R = typename C::R;
   constexpr int H = ROWS / 8, PARTS = sizeof(T) == 4 ? 3 : 1, G = FOUR ? R::G : 1, K16 = DH / 16;
-  constexpr bool C16 = PARTS == 1;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int32_t s_first[kPlanSeqs + 1];
   __shared__ int64_t s_word[kWarps];
@@ -233,6 +257,19 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
     }
   }
 
+  // Where a lane's piece of 16 bytes goes, and where its words stand, in a stage (4 bits; see fetch).  Eight keys further, in rows of 32 bytes,
+  // the line's number has changed by two.
+  constexpr uint32_t kFlip = DH == 64 ? 0x40u : 0u;
+  const uint32_t piece_to = (16u * lane) ^ ((4u * lane) & 0x60u);
+  const uint32_t k_row = (uint32_t)(g4 * (DH / 2) + 8 * t4), k_at = k_row ^ ((k_row >> 2) & 0x60u);
+  uint32_t v_at[2][G];
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int gr = 0; gr < G; ++gr) {
+      const uint32_t byte = (uint32_t)((2 * t4 + x) * (DH / 2) + 32 * gr + 4 * g4);
+      v_at[x][gr] = byte ^ ((byte >> 2) & 0x60u);
+    }
   uint8_t* mine = smem + warp * C::WARP;
   const uint32_t ring = shared_at(mine);
   float* s_o = reinterpret_cast<float*>(mine);                   // [row][PITCH], after an item's last block
@@ -263,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 
     // ---- queries
     uint32_t q[H][PARTS][K16][2];
-    float qsum[H][G][2];                                         // 4 bits: sums over a group of rows 8 h + 2 t4 + x
+    float qsum[H][G][2], to_log2[H][2];                          // rows 8 h + 2 t4 + x: 4 bits: sums over a group; logits to base 2
     int32_t lim[H][2];                                           // keys [0, lim) of those rows
     const T* Q = reinterpret_cast<const T*>(p.q);
 #pragma unroll
@@ -272,30 +309,68 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
       const int64_t rr = valid ? r0 + 8 * h + g4 : r0;
       const T* src = Q + (it.q0 + rr / p.g) * p.ldq + (head * (int64_t)p.g + rr % p.g) * dh;
       if constexpr (FOUR) {
-        float sum[G];
+        float v[G][2][8], sum[G], top = 0.f;
+        bool odd = false;
 #pragma unroll
         for (int gr = 0; gr < G; ++gr) {
           sum[gr] = 0.f;
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            float v[8];
+          for (int w = 0; w < 2; ++w)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              v[i] = valid ? load1(src + 64 * gr + 8 * (2 * t4 + w) + i) : 0.f;
-              sum[gr] += v[i];
+              const float u = valid ? load1(src + 64 * gr + 8 * (2 * t4 + w) + i) : 0.f;
+              v[gr][w][i] = u;
+              sum[gr] += u;
+              top = fmaxf(top, fabsf(u));
+              odd |= !(fabsf(u) < INFINITY);
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {                        // numbers (i, i + 4) of a word stand side by side
-              uint32_t r[PARTS];
-              split<PARTS>(v[i], v[i + 4], r);
-#pragma unroll
-              for (int u = 0; u < PARTS; ++u) q[h][u][4 * gr + 2 * w + i / 2][i & 1] = r[u];
-            }
-          }
 #pragma unroll
           for (int w = 1; w < 4; w <<= 1) sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], w);
+        }
+        float unit = 1.f;                                        // of this row's e4m3 values
+        if constexpr (PARTS == 1) {
 #pragma unroll
-          for (int x = 0; x < 2; ++x) qsum[h][gr][x] = __shfl_sync(0xffffffffu, sum[gr], (2 * t4 + x) * 4);
+          for (int w = 1; w < 4; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+          // 2^(e - 7) of the exponent e of the largest value; NaN where there is one, or an infinity: every logit is then
+          unit = __uint_as_float(max(__float_as_uint(top) >> 23, 20u) - 7u << 23);
+          if (__ballot_sync(0xffffffffu, odd) >> (lane & 28) & 15u) unit = NAN;
+          const float inv = 1.f / unit;
+#pragma unroll
+          for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {                      // numbers x, x + 2, x + 4, x + 6 of a word stand side by side
+                float a[4], b[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  a[i] = v[gr][w][x + 2 * i] * inv;
+                  b[i] = a[i] - round_e4m3(a[i]);
+                }
+                q[h][0][4 * gr + 2 * w][x] = pack_e4m3(a[0], a[1], a[2], a[3]);
+                q[h][0][4 * gr + 2 * w + 1][x] = pack_e4m3(b[0], b[1], b[2], b[3]);
+              }
+        } else {
+#pragma unroll
+          for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {                      // numbers (i, i + 4) of a word stand side by side
+                uint32_t r[PARTS];
+                split<PARTS>(v[gr][w][i], v[gr][w][i + 4], r);
+#pragma unroll
+                for (int u = 0; u < PARTS; ++u) q[h][u][4 * gr + 2 * w + i / 2][i & 1] = r[u];
+              }
+        }
+        // what a lane needs of its rows 2 t4 + x: logits come in units of a row
+        const float of_sum = PARTS == 1 ? 512.f * unit : 1.f;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const float u = __shfl_sync(0xffffffffu, of_sum, (2 * t4 + x) * 4);
+          to_log2[h][x] = u * p.scale_log2;
+#pragma unroll
+          for (int gr = 0; gr < G; ++gr) qsum[h][gr][x] = __shfl_sync(0xffffffffu, sum[gr], (2 * t4 + x) * 4) / u;
         }
       } else {
 #pragma unroll
@@ -309,6 +384,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
             for (int u = 0; u < PARTS; ++u) q[h][u][j][x] = r[u];
           }
+        to_log2[h][0] = to_log2[h][1] = p.scale_log2;
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {                              // (rows that are none: any values, kept to themselves)
@@ -317,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
       }
     }
     // O: 4 bits: channels 64 (j / 4) + 8 g4 + j % 4 (| + 4) of rows 2 t4 + (x & 1); bf16: channels 16 j + g4 (| + 8)
-    float o[K16][H][4], zero_part[H][G][2], r[H][2], l[H][2];
+    float o[K16][H][4], offset[H][G][2], plus[H][G][2], r[H][2], ref[H][2], most[H][2], l[H][2];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
 #pragma unroll
@@ -326,70 +402,71 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
         for (int x = 0; x < 4; ++x) o[j][h][x] = 0.f;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        r[h][x] = -INFINITY;                                     // reference of the rows' exponents, this lane's part of their sums
-        l[h][x] = 0.f;
+        r[h][x] = most[h][x] = -INFINITY;                        // reference of the rows' exponents, the logit up to which it stays
+        ref[h][x] = l[h][x] = 0.f;                               // r, 0 while there is none; this lane's part of the rows' sums
 #pragma unroll
-        for (int gr = 0; gr < G; ++gr) zero_part[h][gr][x] = 0.f;
+        for (int gr = 0; gr < G; ++gr) offset[h][gr][x] = plus[h][gr][x] = 0.f;
       }
     }
     bool found = false;                                          // bf16: non-finite values behind some row's mask
 
-    // ---- copies: block i of this warp starts at key kb + 16 (warp + 8 i).  Pages of 32 blocks at a time, a lane each.
-    int32_t pages = -1;
-    uint32_t missing = 0u;                                       // a bit per stage: its block has no page
+    // ---- copies: block i of this warp starts at key kb + 16 (warp + 8 i).  Pages and places of 32 blocks at a time, a lane each.
+    int32_t pages = -1, slots = 0;
+    uint32_t missing = 0u;                                       // a bit per block fetched, the last one lowest: it has no page
+    uint32_t into = ring;                                        // the stage that is next
+    const int64_t head0 = (int64_t)head * p.c.page_len;
     const auto fetch = [&](int32_t i) {
+      missing <<= 1;
       if (i < own) {
         if ((i & 31) == 0) {
-          const int32_t at = i + lane;
-          pages = at < own ? page_of(p.c, sq, (kb + kBlock * (warp + kWarps * at)) / p.c.page_len) : -1;
+          const int32_t at = i + lane, key = kb + kBlock * (warp + kWarps * at), entry = key / p.c.page_len;
+          pages = at < own ? page_of(p.c, sq, entry) : -1;
+          slots = key - entry * p.c.page_len;
         }
-        const int32_t page = __shfl_sync(0xffffffffu, pages, i & 31);
-        const int32_t key = kb + kBlock * (warp + kWarps * i), slot = key % p.c.page_len;
+        const int32_t page = __shfl_sync(0xffffffffu, pages, i & 31), slot = __shfl_sync(0xffffffffu, slots, i & 31);
         const bool there = page >= 0;
-        const int64_t at = (int64_t)head * p.c.page_len + slot, pg = there ? page : 0;
-        const uint32_t dst = ring + (uint32_t)(i % R::STAGES) * R::STAGE, bit = 1u << (i % R::STAGES);
-        missing = there ? missing & ~bit : missing | bit;
+        const int64_t at = head0 + slot, pg = there ? page : 0;
+        missing |= there ? 0u : 1u;
         if constexpr (FOUR) {
-          const uint8_t* k = p.c.k + pg * p.c.k_step + at * (DH / 2);
-          const uint8_t* v = p.c.v + pg * p.c.v_step + at * (DH / 2);
+          const uint8_t* k = p.c.k + pg * p.c.k_step + at * (DH / 2) + 16 * lane;
+          const uint8_t* v = p.c.v + pg * p.c.v_step + at * (DH / 2) + 16 * lane;
+          const uint8_t* sc = lane < 16 ? p.c.ks + pg * p.c.ks_step : p.c.vs + pg * p.c.vs_step;
 #pragma unroll
-          for (int e = lane; e < DH / 2; e += 32) {              // piece e of the block's 16 rows
+          for (int e = 0; e < DH / 2; e += 32) {                 // pieces of the block's 16 rows
             // 32-byte quarters of a 128-byte line change places with the line's number: the four keys of a half warp's read of K, and the
             // four pairs of keys of a read of V, lie in different banks
-            const uint32_t byte = 16u * e, to = byte ^ ((byte >> 2) & 0x60u);
-            copy16(dst + to, k + byte, there);
-            copy16(dst + R::TILE + to, v + byte, there);
+            copy16(into + 16 * e + piece_to, k + 16 * e, there);
+            copy16(into + R::TILE + 16 * e + piece_to, v + 16 * e, there);
           }
-          const int e = lane & 15;
-          if (e < 4 * G) {
-            const uint8_t* src = lane < 16 ? p.c.ks + pg * p.c.ks_step + at * (4 * G) : p.c.vs + pg * p.c.vs_step + at * (4 * G);
-            copy16(dst + 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * e, src + 16 * e, there);
-          }
+          if ((lane & 15) < 4 * G)
+            copy16(into + 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * (lane & 15), sc + at * (4 * G) + 16 * (lane & 15), there);
         } else {
           const uint8_t* k = p.c.k + pg * p.c.k_step + at * (2 * dh);
           const uint8_t* v = p.c.v + pg * p.c.v_step + at * (2 * dh);
           const int per = dh / 8;
 #pragma unroll
           for (int e0 = 0; e0 < kBlock * R::PIECES; e0 += 32) {
-            const int e = e0 + lane, row = e / per, piece = e % per;
+            const int e = e0 + lane, row = dh == DH ? e / R::PIECES : e / per, piece = e - row * per;
             if (e < kBlock * per) {
-              copy16(dst + row * R::PITCH + 16 * piece, k + 16 * e, there);
-              copy16(dst + R::TILE + row * R::PITCH + 16 * piece, v + 16 * e, there);
+              copy16(into + row * R::PITCH + 16 * piece, k + 16 * e, there);
+              copy16(into + R::TILE + row * R::PITCH + 16 * piece, v + 16 * e, there);
             }
           }
         }
+        into = into + R::STAGE == ring + R::BYTES ? ring : into + R::STAGE;
       }
       copies_end();
     };
 #pragma unroll
     for (int i = 0; i < R::STAGES - 1; ++i) fetch(i);
 
+    uint32_t stage = ring + R::BYTES - R::STAGE;
     for (int32_t i = 0; i < own; ++i) {
       const int32_t kt = kb + kBlock * (warp + kWarps * i);
       fetch(i + R::STAGES - 1);
       copies_wait<R::STAGES - 1>();
       __syncwarp();
-      const uint32_t stage = ring + (uint32_t)(i % R::STAGES) * R::STAGE;
+      stage = stage + R::STAGE == ring + R::BYTES ? ring : stage + R::STAGE;
       const bool edge = kt + kBlock > sure;
       float s[H][4];                                             // keys kt + g4 | + 8, rows 2 t4, 2 t4 + 1
 #pragma unroll
@@ -411,23 +488,34 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
             for (int x = 0; x < 4; ++x) a[h][x] = 0.f;
           uint2 w[2];                                            // keys g4, g4 + 8
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const uint32_t byte = (uint32_t)((g4 + 8 * y) * (DH / 2) + 32 * gr + 8 * t4);
-            w[y] = lds64(stage + (byte ^ ((byte >> 2) & 0x60u)));
+          for (int y = 0; y < 2; ++y) w[y] = lds64(stage + (k_at ^ (32u * gr + kFlip * y)) + 8 * y * (DH / 2));
+          if constexpr (PARTS == 1) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t w0 = u == 0 ? w[0].x : w[0].y, w1 = u == 0 ? w[1].x : w[1].y;
+              const uint32_t a0 = w0 & 0x0f0f0f0fu, a1 = w1 & 0x0f0f0f0fu, a2 = (w0 >> 4) & 0x0f0f0f0fu, a3 = (w1 >> 4) & 0x0f0f0f0fu;
+#pragma unroll
+              for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                  mma_e4m3(a[h], a0, a1, a2, a3, q[h][0][4 * gr + 2 * u + x][0], q[h][0][4 * gr + 2 * u + x][1]);
+            }
+          } else {
+            const uint32_t n[4][4] = {
+                {opened_centred<0>(w[0].x), opened_centred<0>(w[1].x), opened_centred<1>(w[0].x), opened_centred<1>(w[1].x)},
+                {opened_centred<2>(w[0].x), opened_centred<2>(w[1].x), opened_centred<3>(w[0].x), opened_centred<3>(w[1].x)},
+                {opened_centred<0>(w[0].y), opened_centred<0>(w[1].y), opened_centred<1>(w[0].y), opened_centred<1>(w[1].y)},
+                {opened_centred<2>(w[0].y), opened_centred<2>(w[1].y), opened_centred<3>(w[0].y), opened_centred<3>(w[1].y)}};
+#pragma unroll
+            for (int x = PARTS - 1; x >= 0; --x)                 // (small parts first: their sums round less)
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int h = 0; h < H; ++h) mma(a[h], n[u][0], n[u][1], n[u][2], n[u][3], q[h][x][4 * gr + u][0], q[h][x][4 * gr + u][1]);
           }
-          const uint32_t n[4][4] = {{opened<0, C16>(w[0].x), opened<0, C16>(w[1].x), opened<1, C16>(w[0].x), opened<1, C16>(w[1].x)},
-                                    {opened<2, C16>(w[0].x), opened<2, C16>(w[1].x), opened<3, C16>(w[0].x), opened<3, C16>(w[1].x)},
-                                    {opened<0, C16>(w[0].y), opened<0, C16>(w[1].y), opened<1, C16>(w[0].y), opened<1, C16>(w[1].y)},
-                                    {opened<2, C16>(w[0].y), opened<2, C16>(w[1].y), opened<3, C16>(w[0].y), opened<3, C16>(w[1].y)}};
-#pragma unroll
-          for (int x = PARTS - 1; x >= 0; --x)                   // (small parts first: their sums round less)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-              for (int h = 0; h < H; ++h) mma(a[h], n[u][0], n[u][1], n[u][2], n[u][3], q[h][x][4 * gr + u][0], q[h][x][4 * gr + u][1]);
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const float scale = low(pair[y][gr]), zero = fmaf(C16 ? -16.f : 8.f, scale, high(pair[y][gr]));
+            const float scale = low(pair[y][gr]), zero = PARTS == 1 ? high(pair[y][gr]) : fmaf(8.f, scale, high(pair[y][gr]));
 #pragma unroll
             for (int h = 0; h < H; ++h)
 #pragma unroll
@@ -449,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
         }
       }
       // a block of a page that is none: NaN to every row that sees it
-      if ((missing >> (i % R::STAGES)) & 1u) {
+      if ((missing >> (R::STAGES - 1)) & 1u) {
         if (lane == 0) report_status(p.status, SP_ERR_SHAPE, sq, kt / p.c.page_len);
 #pragma unroll
         for (int h = 0; h < H; ++h)
@@ -462,8 +550,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           if (edge && kt + 8 * (x >> 1) + g4 >= lim[h][x & 1]) s[h][x] = -INFINITY;
-          const float u = s[h][x] * p.scale_log2;
-          rise |= u != -INFINITY && !(u - r[h][x & 1] <= 8.f);
+          rise |= !(s[h][x] <= most[h][x & 1]);
         }
       if (__any_sync(0xffffffffu, rise)) {                       // seldom: the references follow the maxima of this block
 #pragma unroll
@@ -471,7 +558,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
           float f[2];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            float m = fmaxf(s[h][x], s[h][2 + x]) * p.scale_log2;
+            float m = fmaxf(s[h][x], s[h][2 + x]) * to_log2[h][x];
             // (beyond fp32: NaN, too)
             const bool nan = s[h][x] != s[h][x] || s[h][2 + x] != s[h][2 + x] || m == INFINITY;
 #pragma unroll
@@ -479,10 +566,16 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
             if (__ballot_sync(0xffffffffu, nan) & (0x11111111u << t4)) m = NAN;      // (the lanes of these rows)
             const bool up = m != -INFINITY && !(m - r[h][x] <= 0.f);
             f[x] = up ? exp2_fast(r[h][x] - m) : 1.f;            // r = -infinity: 0
-            if (up) r[h][x] = m;
+            if (up) {
+              r[h][x] = ref[h][x] = m;
+              most[h][x] = (m + 8.f) / to_log2[h][x];
+            }
             l[h][x] *= f[x];
 #pragma unroll
-            for (int gr = 0; gr < G; ++gr) zero_part[h][gr][x] *= f[x];
+            for (int gr = 0; gr < G; ++gr) {
+              offset[h][gr][x] *= f[x];
+              plus[h][gr][x] *= f[x];
+            }
           }
 #pragma unroll
           for (int j = 0; j < K16; ++j)
@@ -494,8 +587,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
       for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const float ref = r[h][x & 1];
-          s[h][x] = exp2_fast(fmaf(s[h][x], p.scale_log2, ref == -INFINITY ? 0.f : -ref));      // now probabilities, to the reference
+          s[h][x] = exp2_fast(fmaf(s[h][x], to_log2[h][x & 1], -ref[h][x & 1]));      // now probabilities, to the reference
           l[h][x & 1] += s[h][x];
         }
       const uint32_t vtile = stage + R::TILE;
@@ -512,42 +604,45 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
           for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const float scale = low(pair[y][gr]), zero = high(pair[y][gr]);
-              float ps[2], pz[2];
+              // (p s)^T goes into the product with the numbers opened to k + n; offset collects p times what belongs to a key whatever its
+              // number, plus the products' sum, from which k goes again.  bf16: a rounding of p s weighs the number's distance from the middle
+              // 7.5 alone, whose part is taken exactly (16 tokens after 2048 .. 31013 keys: 4.7e-3 from the formula without, 2.3e-3).
+              const float scale = low(pair[y][gr]), zero = fmaf(PARTS == 1 ? 7.5f : 8.f, scale, high(pair[y][gr]));
+              float ps[2];
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
-                const bool hidden = edge && kt + 8 * y + g4 >= lim[h][x];      // (whatever stands in a slot that the row does not see)
-                ps[x] = hidden ? 0.f : s[h][2 * y + x] * scale;
-                pz[x] = hidden ? 0.f : s[h][2 * y + x] * zero;
+                ps[x] = s[h][2 * y + x] * scale;
+                float pz = s[h][2 * y + x] * zero;
+                if (edge && kt + 8 * y + g4 >= lim[h][x]) ps[x] = pz = 0.f;      // (whatever stands in a slot that the row does not see)
+                offset[h][gr][x] += pz;
               }
               uint32_t u[PARTS];
               split<PARTS>(ps[0], ps[1], u);
-              // what stands in the product beside the numbers goes again: fp32 16 - 24 = -8.  bf16: 16 of the rounded ps; and of the numbers
-              // themselves their middle 7.5 is taken back with the rounded ps and added with the exact one, so that a rounding only weighs a
-              // number's distance from the middle (16 tokens after 2048 .. 31013 keys: 4.7e-3 from the formula without, 2.0e-3)
               if constexpr (PARTS == 1) {
-                zero_part[h][gr][0] += fmaf(-23.5f, low(u[0]), fmaf(7.5f, ps[0], pz[0]));
-                zero_part[h][gr][1] += fmaf(-23.5f, high(u[0]), fmaf(7.5f, ps[1], pz[1]));
-              } else {
-                zero_part[h][gr][0] += fmaf(8.f, ps[0], pz[0]);
-                zero_part[h][gr][1] += fmaf(8.f, ps[1], pz[1]);
+                plus[h][gr][0] += low(u[0]);
+                plus[h][gr][1] += high(u[0]);
               }
 #pragma unroll
               for (int x = 0; x < PARTS; ++x) pb[h][x][y] = turned8x8(u[x]);
             }
           uint32_t w[4];                                         // word g4 of keys 2 t4, + 1, + 8, + 9
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t byte = (uint32_t)((2 * t4 + (x & 1) + 8 * (x >> 1)) * (DH / 2) + 32 * gr + 4 * g4);
-            w[x] = lds32(vtile + (byte ^ ((byte >> 2) & 0x60u)));
-          }
+          for (int x = 0; x < 4; ++x) w[x] = lds32(vtile + (v_at[x & 1][gr] ^ (kFlip * (x >> 1))) + 8 * (x >> 1) * (DH / 2));
           // numbers 0 .. 3 and 4 .. 7 of two keys side by side
           const uint32_t m0 = __byte_perm(w[0], w[1], 0x5410), m1 = __byte_perm(w[0], w[1], 0x7632);
           const uint32_t m2 = __byte_perm(w[2], w[3], 0x5410), m3 = __byte_perm(w[2], w[3], 0x7632);
-          const uint32_t a[4][4] = {{opened<0, C16>(m0), opened<0, C16>(m1), opened<0, C16>(m2), opened<0, C16>(m3)},
-                                    {opened<1, C16>(m0), opened<1, C16>(m1), opened<1, C16>(m2), opened<1, C16>(m3)},
-                                    {opened<2, C16>(m0), opened<2, C16>(m1), opened<2, C16>(m2), opened<2, C16>(m3)},
-                                    {opened<3, C16>(m0), opened<3, C16>(m1), opened<3, C16>(m2), opened<3, C16>(m3)}};
+          uint32_t a[4][4];
+          if constexpr (PARTS == 1) {
+            a[0][0] = opened<0>(m0); a[0][1] = opened<0>(m1); a[0][2] = opened<0>(m2); a[0][3] = opened<0>(m3);
+            a[1][0] = opened<1>(m0); a[1][1] = opened<1>(m1); a[1][2] = opened<1>(m2); a[1][3] = opened<1>(m3);
+            a[2][0] = opened<2>(m0); a[2][1] = opened<2>(m1); a[2][2] = opened<2>(m2); a[2][3] = opened<2>(m3);
+            a[3][0] = opened<3>(m0); a[3][1] = opened<3>(m1); a[3][2] = opened<3>(m2); a[3][3] = opened<3>(m3);
+          } else {
+            a[0][0] = opened_centred<0>(m0); a[0][1] = opened_centred<0>(m1); a[0][2] = opened_centred<0>(m2); a[0][3] = opened_centred<0>(m3);
+            a[1][0] = opened_centred<1>(m0); a[1][1] = opened_centred<1>(m1); a[1][2] = opened_centred<1>(m2); a[1][3] = opened_centred<1>(m3);
+            a[2][0] = opened_centred<2>(m0); a[2][1] = opened_centred<2>(m1); a[2][2] = opened_centred<2>(m2); a[2][3] = opened_centred<2>(m3);
+            a[3][0] = opened_centred<3>(m0); a[3][1] = opened_centred<3>(m1); a[3][2] = opened_centred<3>(m2); a[3][3] = opened_centred<3>(m3);
+          }
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -622,11 +717,15 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
           for (int gr = 0; gr < G; ++gr) {
 #pragma unroll
-            for (int w = 4; w < 32; w <<= 1) zero_part[h][gr][x] += __shfl_xor_sync(0xffffffffu, zero_part[h][gr][x], w);
+            for (int w = 4; w < 32; w <<= 1) {
+              offset[h][gr][x] += __shfl_xor_sync(0xffffffffu, offset[h][gr][x], w);
+              if (PARTS == 1) plus[h][gr][x] += __shfl_xor_sync(0xffffffffu, plus[h][gr][x], w);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              o[4 * gr + j][h][x] += zero_part[h][gr][x];
-              o[4 * gr + j][h][2 + x] += zero_part[h][gr][x];
+              const float part = PARTS == 1 ? fmaf(-(7.5f + kOpened[j]), plus[h][gr][x], offset[h][gr][x]) : offset[h][gr][x];
+              o[4 * gr + j][h][x] += part;
+              o[4 * gr + j][h][2 + x] += part;
             }
           }
       }

@@ -283,10 +283,31 @@ struct GradParams {
   float eps;
 };
 
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// a chunk from its 16-byte pieces, `step` bytes apart
+__device__ __forceinline__ void collect(Raw8<__nv_bfloat16>& r, const uint8_t* at, int) { r.a = *reinterpret_cast<const uint4*>(at); }
+__device__ __forceinline__ void collect(Raw8<float>& r, const uint8_t* at, int step) {
+  r.a = *reinterpret_cast<const float4*>(at);
+  r.b = *reinterpret_cast<const float4*>(at + step);
+}
+// Rows in the ring: three of bf16 (24 KB each for 4096 columns; three blocks of an SM), two of wider types, one less where a row has 1024 threads.
+template <typename TY, typename TH, int TPR>
+struct GradRing {
+  static constexpr int CHUNK = (int)(sizeof(TY) + 2 * sizeof(TH)) / 2;      // pieces of a chunk of eight values of dy, h and the stream's gradient
+  static constexpr int PIECES = 2 * CHUNK;
+  static constexpr int STAGES = (CHUNK == 3 ? 3 : 2) - (TPR == 1024 ? 1 : 0);
+  static constexpr int THREADS = TPR < 256 ? 256 : TPR;
+  static constexpr size_t SMEM = (size_t)STAGES * PIECES * THREADS * 16;
+  static_assert(SMEM <= 200 * 1024, "shared memory of a block");
+};
 // Blocks walk over rows, a grid apart; a thread keeps the weight's gradient of its columns in registers from row to row.
 constexpr int kGradChunks = 2;
 template <typename TY, typename TH, int TPR>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_grad_kernel(const GradParams p) {
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 && sizeof(TY) + sizeof(TH) == 4 ? 3 : 1) norm_grad_kernel(const GradParams p) {
   kernel_begin();
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kWarps = TPR / 32;      // rows of a block at a time, warps of a row
   __shared__ float s_red[2][kRows][kWarps][2];
@@ -297,14 +318,46 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_grad_kernel(const 
   for (int c = 0; c < kGradChunks; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
-  int flip = 0;
+  // Whole chunks come through a ring of rows in shared memory, by copies that the thread itself waits for: each has its own places there.
+  extern __shared__ __align__(16) uint8_t smem[];
+  using R = GradRing<TY, TH, TPR>;
+  uint8_t* mine = smem + threadIdx.x * 16;
+  constexpr int kStep = R::THREADS * 16;                         // bytes from a piece of the thread's to its next
+  const auto piece = [&](int stage, int k) { return mine + (stage * R::PIECES + k) * kStep; };
+  const auto bring = [&](int stage, int64_t row) {
+    if (row < p.T) {
+      const TY* dy = reinterpret_cast<const TY*>(p.dy) + row * p.lddy;
+      const TH* h = reinterpret_cast<const TH*>(p.h) + row * p.ldh;
+      const TH* dh = reinterpret_cast<const TH*>(p.dh) + row * p.lddh;
+#pragma unroll
+      for (int c = 0; c < kGradChunks; ++c) {
+        const int j = (c * TPR + t) * 8;
+        if (j + 8 > p.d) continue;
+        int k = c * R::CHUNK;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(TY) / 2; ++i) copy16(piece(stage, k++), dy + j + 4 * i);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(TH) / 2; ++i) copy16(piece(stage, k++), h + j + 4 * i);
+        if (p.dh) {
+#pragma unroll
+          for (int i = 0; i < (int)sizeof(TH) / 2; ++i) copy16(piece(stage, k++), dh + j + 4 * i);
+        }
+      }
+    }
+    copies_end();
+  };
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  {
+    int64_t row = (int64_t)blockIdx.x * kRows + g;
+    for (int k = 0; k < R::STAGES - 1; ++k, row += stride) bring(k, row);
+  }
+  int flip = 0, stage = 0;
   // (all rows of a block go round together: they meet at the sums)
-  for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < p.T; row0 += (int64_t)gridDim.x * kRows, flip ^= 1) {
+  for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < p.T; row0 += stride, flip ^= 1) {
     const int64_t row = row0 + g;
     const bool live = row < p.T;
-    const TY* dy = reinterpret_cast<const TY*>(p.dy) + row * p.lddy;
-    const TH* h = reinterpret_cast<const TH*>(p.h) + row * p.ldh;
-    const TH* dh = reinterpret_cast<const TH*>(p.dh) + row * p.lddh;
+    bring(stage == 0 ? R::STAGES - 1 : stage - 1, row + (R::STAGES - 1) * stride);
+    copies_wait<R::STAGES - 1>();
     Raw8<TY> a[kGradChunks];
     Raw8<TH> b[kGradChunks], e[kGradChunks];
 #pragma unroll
@@ -313,17 +366,18 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_grad_kernel(const 
       a[c] = Raw8<TY>();
       b[c] = e[c] = Raw8<TH>();
       if (live && j + 8 <= p.d) {
-        fetch(a[c], dy + j);
-        fetch(b[c], h + j);
-        if (p.dh) fetch(e[c], dh + j);
+        const int k = c * R::CHUNK;
+        collect(a[c], piece(stage, k), kStep);
+        collect(b[c], piece(stage, k + sizeof(TY) / 2), kStep);
+        if (p.dh) collect(e[c], piece(stage, k + sizeof(TY) / 2 + sizeof(TH) / 2), kStep);
       } else if (live && j < p.d) {
-        fetch_some(a[c], dy + j, p.d - j);
-        fetch_some(b[c], h + j, p.d - j);
-        if (p.dh) fetch_some(e[c], dh + j, p.d - j);
+        fetch_some(a[c], reinterpret_cast<const TY*>(p.dy) + row * p.lddy + j, p.d - j);
+        fetch_some(b[c], reinterpret_cast<const TH*>(p.h) + row * p.ldh + j, p.d - j);
+        if (p.dh) fetch_some(e[c], reinterpret_cast<const TH*>(p.dh) + row * p.lddh + j, p.d - j);
       }
     }
-    float given = 0.f;
-    if (p.rstd && live) given = p.rstd[row];
+    stage = stage + 1 == R::STAGES ? 0 : stage + 1;
+    const float given = p.rstd && live ? p.rstd[row] : 0.f;
     float s = 0.f, ss = 0.f;
 #pragma unroll
     for (int c = 0; c < kGradChunks; ++c) {
@@ -477,16 +531,24 @@ inline int64_t grad_blocks(int64_t T, int64_t d) {
   return want < most ? (want > 0 ? want : 1) : most;
 }
 
+template <typename TY, typename TH, int TPR>
+cudaError_t launch_grad(const GradParams& p, dim3 grid, cudaStream_t s) {
+  using R = GradRing<TY, TH, TPR>;
+  static PerDeviceOnce attr_once;
+  const auto kernel = norm_grad_kernel<TY, TH, TPR>;
+  const cudaError_t e = attr_once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)R::SMEM); });
+  return e == cudaSuccess ? launch(kernel, grid, dim3(R::THREADS), R::SMEM, s, p) : e;
+}
 template <typename TY, typename TH>
 cudaError_t launch_grad(const GradParams& p, bool vec, cudaStream_t s) {
   const dim3 grid((unsigned)grad_blocks(p.T, p.d));
   switch (vec ? grad_threads(p.d) : 0) {
-    case 32: return launch(norm_grad_kernel<TY, TH, 32>, grid, dim3(256), 0, s, p);
-    case 64: return launch(norm_grad_kernel<TY, TH, 64>, grid, dim3(256), 0, s, p);
-    case 128: return launch(norm_grad_kernel<TY, TH, 128>, grid, dim3(256), 0, s, p);
-    case 256: return launch(norm_grad_kernel<TY, TH, 256>, grid, dim3(256), 0, s, p);
-    case 512: return launch(norm_grad_kernel<TY, TH, 512>, grid, dim3(512), 0, s, p);
-    case 1024: return launch(norm_grad_kernel<TY, TH, 1024>, grid, dim3(1024), 0, s, p);
+    case 32: return launch_grad<TY, TH, 32>(p, grid, s);
+    case 64: return launch_grad<TY, TH, 64>(p, grid, s);
+    case 128: return launch_grad<TY, TH, 128>(p, grid, s);
+    case 256: return launch_grad<TY, TH, 256>(p, grid, s);
+    case 512: return launch_grad<TY, TH, 512>(p, grid, s);
+    case 1024: return launch_grad<TY, TH, 1024>(p, grid, s);
     default: return launch(norm_grad_loop_kernel<TY, TH>, grid, dim3(512), 0, s, p);
   }
 }
