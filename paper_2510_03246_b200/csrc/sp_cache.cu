@@ -360,7 +360,9 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
 bool rows_of_16(const void* ptr, int64_t ld, int32_t dtype, int64_t rows) {
   return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0 && (rows < 2 || ld * (int64_t)dtype_size(dtype) % 16 == 0);
 }
-bool step_fits(int64_t step, int64_t page_bytes, int32_t n_pages) { return step % 16 == 0 && (n_pages < 2 || step >= page_bytes); }
+bool step_fits(int64_t step, int64_t page_bytes, int32_t n_pages) {
+  return n_pages < 2 || (step % 16 == 0 && step >= page_bytes && step <= 0xffffffffll);
+}
 
 }  // namespace
 

@@ -6,7 +6,7 @@
 //
 // Few rows (queries x the heads that share a key head) stream the cache past them; what bounds that is reading it once, and in 4 bits as
 // much the instructions that open the numbers.  Each of eight warps brings its own blocks of 16 keys in by 16-byte asynchronous copies, a ring of
-// stages ahead, so that no warp waits for another before the end of an item.  Products are m16n8k16 of bf16, turned so that keys and channels
+// stages ahead, so that no warp waits for another before the end of a piece.  Products are m16n8k16 of bf16, turned so that keys and channels
 // fill them: S^T = K Q^T and O^T += V^T P^T.  The order in which an instruction contracts channels is free, and so is the channel that a row of
 // V^T stands for.  In 4 bits a lane therefore takes whole words of eight numbers as they lie: for K the two words 2 t4, 2 t4 + 1 of a group, for V
 // word g4 of four keys.
@@ -32,10 +32,11 @@
 namespace sp {
 namespace {
 
-constexpr int kWarps = 8, kBlock = 16, kThreads = kWarps * 32;
-constexpr int kPlanSeqs = 512;             // sequences of a launch
-constexpr int kLeastPart = 256;            // keys of a part, at least
-constexpr int kItemsPerSm = 8;             // items that the parts of a call come to, about
+constexpr int kBlock = 16;
+constexpr int kPlanSeqs = 256;             // sequences of a launch
+constexpr int kLeastBlocks = 16;           // blocks of keys to a thread block, at least
+constexpr int kMostCtas = 2 * 148;         // thread blocks of a launch, at most
+constexpr int kPlanThreads = 256;
 
 struct PagedParams {
   CacheView c;
@@ -46,11 +47,10 @@ struct PagedParams {
   const int32_t* cu_q;
   int32_t Nq, n_heads, g, causal;
   int32_t s0, n_here;                      // sequences of this launch
-  int32_t max_items;                       // what the workspace holds (more only where cu_q decreases)
   float scale_log2;
-  int32_t* plan;                           // [n_here + 1] first item of each sequence, then the length of a part
-  float* part_o;                           // [item, row, dh]
-  float* part_lse;                         // [item, row] in base 2
+  int64_t* plan;                           // [n_here + 1] where each sequence's work starts, then the thread blocks that share it
+  float* part_o;                           // [2 kMostCtas, row, dh]
+  float* part_lse;                         // [2 kMostCtas, row] in base 2
   int32_t* status;
 };
 
@@ -72,9 +72,12 @@ struct PagedCfg {
   static constexpr int PITCH = DH + 4;                                      // floats of a row of a warp's O
   static constexpr int JOIN = ROWS * (PITCH + 2) * 4;                       // a warp's results, in its own ring
   static constexpr int WARP = (R::BYTES > JOIN ? R::BYTES : JOIN) / 128 * 128 + 128;
-  static constexpr size_t SMEM = (size_t)kWarps * WARP;
-  // of an SM (fp32: three parts of the queries, and of wide heads more registers than two blocks have)
-  static constexpr int CTAS = SMEM > 113 * 1024 || (PARTS > 1 && DH > 64) ? 1 : 2;
+  // Warps of a block and blocks of an SM: twice 8 (128 registers of a thread), for 16 rows of wide heads in 4 bits once 12 (168), once 8 where
+  // the ring, or three parts of wide queries, need an SM for themselves.
+  static constexpr bool ALONE = 8 * WARP > 113 * 1024 || (PARTS > 1 && DH > 64);
+  static constexpr bool TWELVE = !ALONE && FOUR && DH == 128 && ROWS > 8;
+  static constexpr int W = TWELVE ? 12 : 8, CTAS = ALONE || TWELVE ? 1 : 2, THREADS = 32 * W;
+  static constexpr size_t SMEM = (size_t)W * WARP;
 };
 
 __device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -138,8 +141,10 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) |
          (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
 }
-__device__ __forceinline__ float round_e4m3(float a) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(__nv_cvt_float_to_fp8(a, __NV_SATFINITE, __NV_E4M3), __NV_E4M3)));
+__device__ __forceinline__ uint32_t left_of_e4m3(const float (&a)[4], uint32_t packed) {      // a - packed
+  const __half2 lo = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(packed & 0xffffu), __NV_E4M3));
+  const __half2 hi = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(packed >> 16), __NV_E4M3));
+  return pack_e4m3(a[0] - __low2float(lo), a[1] - __high2float(lo), a[2] - __low2float(hi), a[3] - __high2float(hi));
 }
 __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
@@ -179,20 +184,20 @@ template <int ROWS>
 __device__ __forceinline__ int32_t tiles_of(const PagedParams& p, const Seq& s) {
   return (int32_t)(((int64_t)s.nq * p.g + ROWS - 1) / ROWS);
 }
-// equal parts of whole blocks: their length and number (at least one)
-__device__ __forceinline__ int32_t part_length(int32_t nk, int32_t part) {
-  if (nk <= part) return nk;
-  const int32_t n = (nk - 1) / part + 1;
-  return ((nk - 1) / n + 1 + kBlock - 1) / kBlock * kBlock;
-}
-__device__ __forceinline__ int32_t parts_of(int32_t nk, int32_t part) {
-  return nk <= part ? 1 : (nk - 1) / part_length(nk, part) + 1;
-}
+// blocks of keys of a tile (one at least: a tile without keys has rows to write)
+__device__ __forceinline__ int32_t blocks_of(int32_t nk) { return nk > 0 ? (nk - 1) / kBlock + 1 : 1; }
 __device__ __forceinline__ int32_t visible(int32_t nk, int64_t shift, int64_t token) {
   return (int32_t)max((int64_t)0, min((int64_t)nk, token + shift + 1));
 }
 
+// The work of a launch is a line of blocks: sequence by sequence, of each its tiles of rows, of each the key heads, of each the blocks of
+// keys.  `ctas` thread blocks share it in equal pieces: the b-th has [b total / ctas, (b + 1) total / ctas).  A tile and head that lies in several
+// thread blocks' pieces is joined from what they leave: the one that goes on in it from a predecessor at 2 b, the one that begins it at 2 b + 1.
+__device__ __forceinline__ int64_t first_of(int64_t b, int64_t total, int64_t ctas) { return b * total / ctas; }
+__device__ __forceinline__ int64_t cta_of(int64_t x, int64_t total, int64_t ctas) { return ((x + 1) * ctas - 1) / total; }
+
 // sum over the block's threads, and what stands before this one's
+template <int WARPS>
 __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_word, int64_t& before) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int64_t upto = v;
@@ -206,7 +211,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_word, int64_
   __syncthreads();
   int64_t sum = 0, below = 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
+  for (int w = 0; w < WARPS; ++w) {
     if (w < warp) below += s_word[w];
     sum += s_word[w];
   }
@@ -215,47 +220,47 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_word, int64_
 }
 
 template <typename T, int DH, bool FOUR, int ROWS>
-__global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>::CTAS)) paged_rows_kernel(const PagedParams p) {
+__global__ void __launch_bounds__((PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>::THREADS), (PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>::CTAS))
+paged_rows_kernel(const PagedParams p) {
   kernel_begin();
   using C = PagedCfg<DH, FOUR, ROWS, sizeof(T) == 4 ? 3 : 1>;
   using R = typename C::R;
-  constexpr int H = ROWS / 8, PARTS = sizeof(T) == 4 ? 3 : 1, G = FOUR ? R::G : 1, K16 = DH / 16;
+  constexpr int H = ROWS / 8, PARTS = sizeof(T) == 4 ? 3 : 1, G = FOUR ? R::G : 1, K16 = DH / 16, W = C::W;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int32_t s_first[kPlanSeqs + 1];
-  __shared__ int64_t s_word[kWarps];
+  __shared__ int64_t s_first[kPlanSeqs + 1];
+  __shared__ int64_t s_word[W];
   __shared__ int s_bad;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g4 = lane >> 2, t4 = lane & 3;
-  const int n_kv = p.c.n_kv, dh = p.c.dh;
+  const int n_kv = p.c.n_kv, dh = FOUR ? DH : p.c.dh;
 
-  // The plan, the same in every block: a part's length from the work of all sequences, and the first item of each.
-  int32_t part;
+  // The plan, the same in every block: where the work of each sequence starts.
   {
-    int64_t work = 0, before;
-    for (int i = threadIdx.x; i < p.n_here; i += kThreads) {
+    const int per = (p.n_here + C::THREADS - 1) / C::THREADS;    // consecutive sequences of a thread
+    const int i0 = (int)threadIdx.x * per, i1 = min(i0 + per, p.n_here);
+    int64_t mine = 0, before;
+    for (int i = i0; i < i1; ++i) {
       const Seq s = seq_at(p, p.s0 + i);
-      work += (int64_t)tiles_of<ROWS>(p, s) * s.nk;
+      s_first[i] = (int64_t)tiles_of<ROWS>(p, s) * n_kv * blocks_of(s.nk);
+      mine += s_first[i];
     }
-    const int64_t want = (block_scan(work, s_word, before) * n_kv + 148 * kItemsPerSm - 1) / (148 * kItemsPerSm);
-    part = (int32_t)min(max(want, (int64_t)kLeastPart), (int64_t)1 << 30);
-    const int per = (p.n_here + kThreads - 1) / kThreads;        // consecutive sequences of a thread
-    int64_t mine = 0;
-    for (int i = threadIdx.x * per; i < min((int)(threadIdx.x + 1) * per, p.n_here); ++i) {
-      const Seq s = seq_at(p, p.s0 + i);
-      mine += (int64_t)tiles_of<ROWS>(p, s) * n_kv * parts_of(s.nk, part);
+    const int64_t all = block_scan<W>(mine, s_word, before);
+    for (int i = i0; i < i1; ++i) {
+      const int64_t n = s_first[i];
+      s_first[i] = before;
+      before += n;
     }
-    block_scan(mine, s_word, before);
-    for (int i = threadIdx.x * per; i < min((int)(threadIdx.x + 1) * per, p.n_here); ++i) {
-      const Seq s = seq_at(p, p.s0 + i);
-      s_first[i] = (int32_t)min(before, (int64_t)p.max_items);
-      before += (int64_t)tiles_of<ROWS>(p, s) * n_kv * parts_of(s.nk, part);
-      if (i == p.n_here - 1) s_first[p.n_here] = (int32_t)min(before, (int64_t)p.max_items);
-    }
+    if (threadIdx.x == 0) s_first[p.n_here] = all;
     __syncthreads();
-    if (blockIdx.x == 0) {
-      for (int i = threadIdx.x; i <= p.n_here; i += kThreads) p.plan[i] = s_first[i];
-      if (threadIdx.x == 0) p.plan[p.n_here + 1] = part;
-    }
   }
+  const int64_t total = s_first[p.n_here];
+  const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / kLeastBlocks));
+  if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i <= p.n_here; i += C::THREADS) p.plan[i] = s_first[i];
+    if (threadIdx.x == 0) p.plan[p.n_here + 1] = ctas;
+  }
+  if (blockIdx.x >= ctas) return;
+  int64_t at = first_of(blockIdx.x, total, ctas);
+  const int64_t end = first_of((int64_t)blockIdx.x + 1, total, ctas);
 
   // Where a lane's piece of 16 bytes goes, and where its words stand, in a stage (4 bits; see fetch).  Eight keys further, in rows of 32 bytes,
   // the line's number has changed by two.
@@ -272,31 +277,35 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
     }
   uint8_t* mine = smem + warp * C::WARP;
   const uint32_t ring = shared_at(mine);
-  float* s_o = reinterpret_cast<float*>(mine);                   // [row][PITCH], after an item's last block
-  for (int32_t item = blockIdx.x; item < s_first[p.n_here]; item += gridDim.x) {
-    // the last sequence whose first item is not behind this one
+  float* s_o = reinterpret_cast<float*>(mine);                   // [row][PITCH], after a piece's last block
+  while (at < end) {
+    // the last sequence whose work starts at or before `at`
     int lo = 0, hi = p.n_here;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (s_first[mid] <= item) lo = mid;
+      if (s_first[mid] <= at) lo = mid;
       else hi = mid;
     }
     const int32_t sq = p.s0 + lo;
     const Seq it = seq_at(p, sq);
-    const int32_t n_parts = parts_of(it.nk, part), len = part_length(it.nk, part);
-    int32_t rest = item - s_first[lo];
-    const int32_t c = rest % n_parts;
-    rest /= n_parts;
-    const int32_t head = rest % n_kv, tile = rest / n_kv;
-    const int64_t r0 = (int64_t)tile * ROWS;
-    const int rows = (int)min((int64_t)ROWS, (int64_t)it.nq * p.g - r0);
+    const uint32_t of_tile = (uint32_t)blocks_of(it.nk);
+    const int64_t from_seq = at - s_first[lo], unit_ = from_seq / of_tile;
+    const uint32_t block0 = (uint32_t)(from_seq - unit_ * of_tile);                  // of the tile and head
+    const uint32_t piece = (uint32_t)min((int64_t)(of_tile - block0), end - at);
+    at += piece;
+    const uint32_t tile = (uint32_t)(unit_ / n_kv);
+    const int32_t head = (int32_t)(unit_ - (int64_t)tile * n_kv);
+    const bool cut = piece < of_tile;
+    const int32_t slot_of = 2 * (int32_t)blockIdx.x + (block0 == 0 ? 1 : 0);
+    const uint32_t g = (uint32_t)p.g, r0 = tile * ROWS;
+    const int rows = (int)min((uint32_t)ROWS, (uint32_t)it.nq * g - r0);
     const int64_t shift = p.causal ? (int64_t)it.nk - it.nq : (int64_t)it.nk;        // query i sees keys j <= i + shift
-    const int32_t sure = visible(it.nk, shift, r0 / p.g);                            // keys that every row sees
-    const int32_t kb = c * len;
-    int32_t seen = visible(it.nk, shift, (r0 + rows - 1) / p.g);                     // keys that some row sees
-    if (seen > kb + len) seen = kb + len;
+    const int32_t sure = visible(it.nk, shift, r0 / g);                              // keys that every row sees
+    const int32_t kb = (int32_t)block0 * kBlock;
+    int32_t seen = visible(it.nk, shift, (r0 + rows - 1) / g);                       // keys that some row sees
+    if (seen - kb > (int32_t)piece * kBlock) seen = kb + (int32_t)piece * kBlock;
     const int32_t blocks = seen > kb ? (seen - kb + kBlock - 1) / kBlock : 0;
-    const int32_t own = blocks > warp ? (blocks - warp - 1) / kWarps + 1 : 0;        // this warp's: warp, warp + 8, ...
+    const int32_t own = blocks > warp ? (blocks - warp - 1) / W + 1 : 0;             // this warp's: warp, warp + W, ...
 
     // ---- queries
     uint32_t q[H][PARTS][K16][2];
@@ -306,8 +315,8 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       const bool valid = 8 * h + g4 < rows;
-      const int64_t rr = valid ? r0 + 8 * h + g4 : r0;
-      const T* src = Q + (it.q0 + rr / p.g) * p.ldq + (head * (int64_t)p.g + rr % p.g) * dh;
+      const uint32_t rr = valid ? r0 + 8 * h + g4 : r0, token = rr / g;
+      const T* src = Q + (it.q0 + (int64_t)token) * p.ldq + ((int64_t)head * g + (rr - token * g)) * dh;
       if constexpr (FOUR) {
         float v[G][2][8], sum[G], top = 0.f;
         bool odd = false;
@@ -341,14 +350,12 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
             for (int w = 0; w < 2; ++w)
 #pragma unroll
               for (int x = 0; x < 2; ++x) {                      // numbers x, x + 2, x + 4, x + 6 of a word stand side by side
-                float a[4], b[4];
+                float a[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  a[i] = v[gr][w][x + 2 * i] * inv;
-                  b[i] = a[i] - round_e4m3(a[i]);
-                }
-                q[h][0][4 * gr + 2 * w][x] = pack_e4m3(a[0], a[1], a[2], a[3]);
-                q[h][0][4 * gr + 2 * w + 1][x] = pack_e4m3(b[0], b[1], b[2], b[3]);
+                for (int i = 0; i < 4; ++i) a[i] = v[gr][w][x + 2 * i] * inv;
+                const uint32_t hi = pack_e4m3(a[0], a[1], a[2], a[3]);
+                q[h][0][4 * gr + 2 * w][x] = hi;
+                q[h][0][4 * gr + 2 * w + 1][x] = left_of_e4m3(a, hi);
               }
         } else {
 #pragma unroll
@@ -389,11 +396,11 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
       for (int x = 0; x < 2; ++x) {                              // (rows that are none: any values, kept to themselves)
         const int row = 8 * h + 2 * t4 + x;
-        lim[h][x] = row < rows ? min(visible(it.nk, shift, (r0 + row) / p.g), seen) : seen;
+        lim[h][x] = row < rows ? min(visible(it.nk, shift, (r0 + row) / g), seen) : seen;
       }
     }
     // O: 4 bits: channels 64 (j / 4) + 8 g4 + j % 4 (| + 4) of rows 2 t4 + (x & 1); bf16: channels 16 j + g4 (| + 8)
-    float o[K16][H][4], offset[H][G][2], plus[H][G][2], r[H][2], ref[H][2], most[H][2], l[H][2];
+    float o[K16][H][4], offset[H][G][2], plus[G][H][4], r[H][2], ref[H][2], most[H][2], l[H][2];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
 #pragma unroll
@@ -405,32 +412,39 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
         r[h][x] = most[h][x] = -INFINITY;                        // reference of the rows' exponents, the logit up to which it stays
         ref[h][x] = l[h][x] = 0.f;                               // r, 0 while there is none; this lane's part of the rows' sums
 #pragma unroll
-        for (int gr = 0; gr < G; ++gr) offset[h][gr][x] = plus[h][gr][x] = 0.f;
+        for (int gr = 0; gr < G; ++gr) offset[h][gr][x] = plus[gr][h][x] = plus[gr][h][2 + x] = 0.f;
       }
     }
     bool found = false;                                          // bf16: non-finite values behind some row's mask
 
-    // ---- copies: block i of this warp starts at key kb + 16 (warp + 8 i).  Pages and places of 32 blocks at a time, a lane each.
+    // ---- copies: block i of this warp starts at key kb + 16 (warp + W i).  Pages and places of 32 blocks at a time, a lane each.
     int32_t pages = -1, slots = 0;
     uint32_t missing = 0u;                                       // a bit per block fetched, the last one lowest: it has no page
     uint32_t into = ring;                                        // the stage that is next
+    constexpr int kRow = FOUR ? DH / 2 : 2 * DH, kScales = 4 * G;      // bytes of a key, of its scales
+    const int row_bytes = FOUR ? kRow : 2 * dh;
     const int64_t head0 = (int64_t)head * p.c.page_len;
+    const uint8_t* k_from = p.c.k + head0 * row_bytes + 16 * lane;
+    const uint8_t* v_from = p.c.v + head0 * row_bytes + 16 * lane;
+    const uint8_t* s_from = FOUR ? (lane < 16 ? p.c.ks : p.c.vs) + head0 * kScales + 16 * (lane & 15) : nullptr;
+    const uint32_t s_step = (uint32_t)(lane < 16 ? p.c.ks_step : p.c.vs_step);
     const auto fetch = [&](int32_t i) {
       missing <<= 1;
       if (i < own) {
         if ((i & 31) == 0) {
-          const int32_t at = i + lane, key = kb + kBlock * (warp + kWarps * at), entry = key / p.c.page_len;
-          pages = at < own ? page_of(p.c, sq, entry) : -1;
+          const int32_t at_ = i + lane, key = kb + kBlock * (warp + W * at_), entry = key / p.c.page_len;
+          pages = at_ < own ? page_of(p.c, sq, entry) : -1;
           slots = key - entry * p.c.page_len;
         }
-        const int32_t page = __shfl_sync(0xffffffffu, pages, i & 31), slot = __shfl_sync(0xffffffffu, slots, i & 31);
+        const int32_t page = __shfl_sync(0xffffffffu, pages, i & 31);
+        const uint32_t slot = (uint32_t)__shfl_sync(0xffffffffu, slots, i & 31);
         const bool there = page >= 0;
-        const int64_t at = head0 + slot, pg = there ? page : 0;
+        const uint32_t pg = there ? (uint32_t)page : 0u;
         missing |= there ? 0u : 1u;
+        // (steps below 2^32, rows of a page below 2^16 of at most 256 bytes: one multiplication each)
+        const uint8_t* k = k_from + (uint64_t)pg * (uint32_t)p.c.k_step + slot * (uint32_t)row_bytes;
+        const uint8_t* v = v_from + (uint64_t)pg * (uint32_t)p.c.v_step + slot * (uint32_t)row_bytes;
         if constexpr (FOUR) {
-          const uint8_t* k = p.c.k + pg * p.c.k_step + at * (DH / 2) + 16 * lane;
-          const uint8_t* v = p.c.v + pg * p.c.v_step + at * (DH / 2) + 16 * lane;
-          const uint8_t* sc = lane < 16 ? p.c.ks + pg * p.c.ks_step : p.c.vs + pg * p.c.vs_step;
 #pragma unroll
           for (int e = 0; e < DH / 2; e += 32) {                 // pieces of the block's 16 rows
             // 32-byte quarters of a 128-byte line change places with the line's number: the four keys of a half warp's read of K, and the
@@ -439,18 +453,23 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
             copy16(into + R::TILE + 16 * e + piece_to, v + 16 * e, there);
           }
           if ((lane & 15) < 4 * G)
-            copy16(into + 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * (lane & 15), sc + at * (4 * G) + 16 * (lane & 15), there);
-        } else {
-          const uint8_t* k = p.c.k + pg * p.c.k_step + at * (2 * dh);
-          const uint8_t* v = p.c.v + pg * p.c.v_step + at * (2 * dh);
-          const int per = dh / 8;
+            copy16(into + 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * (lane & 15), s_from + (uint64_t)pg * s_step + slot * kScales, there);
+        } else if (dh == DH) {
 #pragma unroll
-          for (int e0 = 0; e0 < kBlock * R::PIECES; e0 += 32) {
-            const int e = e0 + lane, row = dh == DH ? e / R::PIECES : e / per, piece = e - row * per;
-            if (e < kBlock * per) {
-              copy16(into + row * R::PITCH + 16 * piece, k + 16 * e, there);
-              copy16(into + R::TILE + row * R::PITCH + 16 * piece, v + 16 * e, there);
-            }
+          for (int e = 0; e < kBlock * R::PIECES; e += 32) {
+            const int row = e / R::PIECES + lane / R::PIECES;    // (a power of two, at most 32)
+            const uint32_t to = into + row * R::PITCH + 16 * (lane % R::PIECES);
+            copy16(to, k + 16 * e, there);
+            copy16(to + R::TILE, v + 16 * e, there);
+          }
+        } else {
+          const int per = dh / 8;
+#pragma unroll 1
+          for (int e = lane; e < kBlock * per; e += 32) {
+            const int row = e / per;
+            const uint32_t to = into + row * R::PITCH + 16 * (e - row * per);
+            copy16(to, k + 16 * (e - lane), there);
+            copy16(to + R::TILE, v + 16 * (e - lane), there);
           }
         }
         into = into + R::STAGE == ring + R::BYTES ? ring : into + R::STAGE;
@@ -462,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 
     uint32_t stage = ring + R::BYTES - R::STAGE;
     for (int32_t i = 0; i < own; ++i) {
-      const int32_t kt = kb + kBlock * (warp + kWarps * i);
+      const int32_t kt = kb + kBlock * (warp + W * i);
       fetch(i + R::STAGES - 1);
       copies_wait<R::STAGES - 1>();
       __syncwarp();
@@ -574,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
             for (int gr = 0; gr < G; ++gr) {
               offset[h][gr][x] *= f[x];
-              plus[h][gr][x] *= f[x];
+              plus[gr][h][x] *= f[x];
             }
           }
 #pragma unroll
@@ -597,6 +616,15 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
         for (int y = 0; y < 2; ++y)
 #pragma unroll
           for (int gr = 0; gr < G; ++gr) pair[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
+        // (0 times a scale is 0 unless that is a NaN or an infinity)
+        bool strict = false;
+        if (edge) {
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int gr = 0; gr < G; ++gr) strict |= !(fabsf(low(pair[y][gr])) < 1e37f) || !(fabsf(high(pair[y][gr])) < 1e37f);
+          strict = __any_sync(0xffffffffu, strict);
+        }
 #pragma unroll
         for (int gr = 0; gr < G; ++gr) {
           uint32_t pb[H][PARTS][2];                              // (P s)^T: keys 2 t4, + 1 | 2 t4 + 8, + 9 of row 8 h + g4
@@ -608,20 +636,21 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
               // number, plus the products' sum, from which k goes again.  bf16: a rounding of p s weighs the number's distance from the middle
               // 7.5 alone, whose part is taken exactly (16 tokens after 2048 .. 31013 keys: 4.7e-3 from the formula without, 2.3e-3).
               const float scale = low(pair[y][gr]), zero = fmaf(PARTS == 1 ? 7.5f : 8.f, scale, high(pair[y][gr]));
-              float ps[2];
+              float ps[2], pz[2];
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
                 ps[x] = s[h][2 * y + x] * scale;
-                float pz = s[h][2 * y + x] * zero;
-                if (edge && kt + 8 * y + g4 >= lim[h][x]) ps[x] = pz = 0.f;      // (whatever stands in a slot that the row does not see)
-                offset[h][gr][x] += pz;
+                pz[x] = zero;
               }
+              if (strict) {                                      // whatever stands in a slot that the row does not see
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                  if (kt + 8 * y + g4 >= lim[h][x]) ps[x] = pz[x] = 0.f;
+              }
+#pragma unroll
+              for (int x = 0; x < 2; ++x) offset[h][gr][x] = fmaf(s[h][2 * y + x], pz[x], offset[h][gr][x]);
               uint32_t u[PARTS];
               split<PARTS>(ps[0], ps[1], u);
-              if constexpr (PARTS == 1) {
-                plus[h][gr][0] += low(u[0]);
-                plus[h][gr][1] += high(u[0]);
-              }
 #pragma unroll
               for (int x = 0; x < PARTS; ++x) pb[h][x][y] = turned8x8(u[x]);
             }
@@ -642,6 +671,10 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
             a[1][0] = opened_centred<1>(m0); a[1][1] = opened_centred<1>(m1); a[1][2] = opened_centred<1>(m2); a[1][3] = opened_centred<1>(m3);
             a[2][0] = opened_centred<2>(m0); a[2][1] = opened_centred<2>(m1); a[2][2] = opened_centred<2>(m2); a[2][3] = opened_centred<2>(m3);
             a[3][0] = opened_centred<3>(m0); a[3][1] = opened_centred<3>(m1); a[3][2] = opened_centred<3>(m2); a[3][3] = opened_centred<3>(m3);
+          }
+          if constexpr (PARTS == 1) {                            // sums of the products' operand: a row of ones
+#pragma unroll
+            for (int h = 0; h < H; ++h) mma(plus[gr][h], 0x3f803f80u, 0u, 0x3f803f80u, 0u, pb[h][0][0], pb[h][0][1]);
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j)
@@ -717,13 +750,10 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
 #pragma unroll
           for (int gr = 0; gr < G; ++gr) {
 #pragma unroll
-            for (int w = 4; w < 32; w <<= 1) {
-              offset[h][gr][x] += __shfl_xor_sync(0xffffffffu, offset[h][gr][x], w);
-              if (PARTS == 1) plus[h][gr][x] += __shfl_xor_sync(0xffffffffu, plus[h][gr][x], w);
-            }
+            for (int w = 4; w < 32; w <<= 1) offset[h][gr][x] += __shfl_xor_sync(0xffffffffu, offset[h][gr][x], w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float part = PARTS == 1 ? fmaf(-(7.5f + kOpened[j]), plus[h][gr][x], offset[h][gr][x]) : offset[h][gr][x];
+              const float part = PARTS == 1 ? fmaf(-(7.5f + kOpened[j]), plus[gr][h][x], offset[h][gr][x]) : offset[h][gr][x];
               o[4 * gr + j][h][x] += part;
               o[4 * gr + j][h][2 + x] += part;
             }
@@ -750,24 +780,31 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
     __syncthreads();
     if (found) s_bad = 1;
     if (!FOUR) __syncthreads();
-    const bool bad = !FOUR && s_bad != 0, cut = n_parts > 1;
-    for (int e = threadIdx.x; e < rows * dh; e += kThreads) {
-      const int row = e / dh, d = e % dh;
-      const int64_t rr = r0 + row, token = rr / p.g, out_row = it.q0 + token;
-      const int out_head = head * p.g + (int)(rr % p.g);
-      const auto of = [&](int w, int at) { return reinterpret_cast<const float*>(smem + w * C::WARP)[at]; };
-      float ref = -INFINITY;                                     // (a NaN of one warp's comes in through its sum)
+    const bool bad = !FOUR && s_bad != 0;
+    const uint32_t quads = (uint32_t)dh / 4;                     // a thread has four channels of a row
+    for (uint32_t e = threadIdx.x; e < rows * quads; e += C::THREADS) {
+      const uint32_t row = e / quads, d = 4 * (e - row * quads), rr = r0 + row, token = rr / g;
+      const int64_t out_row = it.q0 + (int64_t)token;
+      const int64_t out_head = (int64_t)head * g + (rr - token * g);
+      const auto of = [&](int w) { return reinterpret_cast<const float*>(smem + w * C::WARP); };
+      float top = -INFINITY;                                     // (a NaN of one warp's comes in through its sum)
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) ref = fmaxf(ref, of(w, ROWS * C::PITCH + row));
-      const float base = ref == -INFINITY ? 0.f : ref;
-      float total = 0.f, acc = 0.f;
+      for (int w = 0; w < W; ++w) top = fmaxf(top, of(w)[ROWS * C::PITCH + row]);
+      const float base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2f(of(w, ROWS * C::PITCH + row) - base);      // a warp without keys: 0, and its l and O are 0
-        total = fmaf(of(w, ROWS * (C::PITCH + 1) + row), f, total);
-        acc = fmaf(of(w, row * C::PITCH + d), f, acc);
+      for (int w = 0; w < W; ++w) {
+        const float f = exp2_fast(of(w)[ROWS * C::PITCH + row] - base);      // a warp without keys: 0, and its l and O are 0
+        sum = fmaf(of(w)[ROWS * (C::PITCH + 1) + row], f, sum);
+        const float4 v = *reinterpret_cast<const float4*>(of(w) + row * C::PITCH + d);
+        acc[0] = fmaf(v.x, f, acc[0]);
+        acc[1] = fmaf(v.y, f, acc[1]);
+        acc[2] = fmaf(v.z, f, acc[2]);
+        acc[3] = fmaf(v.w, f, acc[3]);
       }
-      acc = total == 0.f ? 0.f : acc / total;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[x] *= inv;
       if (bad) {
         const int32_t last = min(visible(it.nk, shift, token), seen);
         for (int32_t key = max(sure, kb); key < last; ++key) {
@@ -775,15 +812,23 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
           if (page < 0) continue;
           const __nv_bfloat16* V = reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.v_step) +
                                    ((int64_t)head * p.c.page_len + key % p.c.page_len) * dh;
-          const float u = __bfloat162float(V[d]);
-          if (!(fabsf(u) < INFINITY)) acc += u;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float u = __bfloat162float(V[d + x]);
+            if (!(fabsf(u) < INFINITY)) acc[x] += u;
+          }
         }
       }
-      if (cut) p.part_o[((int64_t)item * ROWS + row) * dh + d] = acc;
-      else store1(reinterpret_cast<T*>(p.o) + out_row * p.ldo + (int64_t)out_head * dh + d, acc);
+      if (cut) {
+        *reinterpret_cast<float4*>(p.part_o + ((int64_t)slot_of * ROWS + row) * dh + d) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      } else {
+        T* out = reinterpret_cast<T*>(p.o) + out_row * p.ldo + out_head * dh + d;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) store1(out + x, acc[x]);
+      }
       if (d == 0) {
-        const float lse2 = total == 0.f ? -INFINITY : base + log2f(total);
-        if (cut) p.part_lse[(int64_t)item * ROWS + row] = lse2;
+        const float lse2 = sum == 0.f ? -INFINITY : base + log2f(sum);
+        if (cut) p.part_lse[slot_of * ROWS + row] = lse2;
         else if (p.lse) p.lse[out_row * p.n_heads + out_head] = lse2 == -INFINITY ? lse2 : lse2 * 0.6931471805599453f;
       }
     }
@@ -791,7 +836,7 @@ __global__ void __launch_bounds__(kThreads, (PagedCfg<DH, FOUR, ROWS, sizeof(T) 
   }
 }
 
-// O_i = sum_c w_c O_ic / sum_c w_c with w_c = 2^(lse_ic - max): one warp per row and head of a sequence that was cut.
+// O_i = sum_c w_c O_ic / sum_c w_c with w_c = 2^(lse_ic - max) over the pieces of a tile and head: one warp per row and head.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
   kernel_begin();
@@ -801,19 +846,20 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
   const int32_t row = (int32_t)(idx / p.n_heads), h = (int32_t)(idx % p.n_heads);
   const int32_t sq = sequence_of(p.cu_q, p.c.n_seq, p.Nq, row);
   if (sq < p.s0 || sq >= p.s0 + p.n_here) return;
-  const int32_t part = p.plan[p.n_here + 1];
   const Seq it = seq_at(p, sq);
-  const int32_t parts = parts_of(it.nk, part);
-  if (parts < 2) return;
-  const int dh = p.c.dh;
-  const int64_t rr = (int64_t)(row - it.q0) * p.g + h % p.g, tile = rr / ROWS;
-  const int64_t slot0 = p.plan[sq - p.s0] + (tile * p.c.n_kv + h / p.g) * parts;
-  if (slot0 + parts > p.max_items) return;
-  const float* lses = p.part_lse + slot0 * ROWS + rr % ROWS;
+  const int64_t total = p.plan[p.n_here], ctas = p.plan[p.n_here + 1];
+  const int32_t of_tile = blocks_of(it.nk);
+  const uint32_t rr = (uint32_t)(row - it.q0) * p.g + h % p.g;
+  const int64_t first = p.plan[sq - p.s0] + ((int64_t)(rr / ROWS) * p.c.n_kv + h / p.g) * of_tile;
+  const int64_t b0 = cta_of(first, total, ctas), b1 = cta_of(first + of_tile - 1, total, ctas);
+  if (b0 == b1 || b0 < 0 || b1 >= kMostCtas) return;      // (whole; outside only where cu_q decreases)
+  const int parts = (int)(b1 - b0) + 1, dh = p.c.dh;
+  // (the first piece stands at 2 b0 + 1, the others at 2 b)
+  const auto slot = [&](int c) { return 2 * (b0 + c) + (c == 0 ? 1 : 0); };
   float mx = -INFINITY;
   bool bad = false;                   // (fmaxf passes over a NaN)
   for (int c = lane; c < parts; c += 32) {
-    const float lc = lses[(int64_t)c * ROWS];
+    const float lc = p.part_lse[slot(c) * ROWS + rr % ROWS];
     mx = fmaxf(mx, lc);
     bad |= lc != lc;
   }
@@ -823,17 +869,16 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
   bad = __any_sync(0xffffffffu, bad);
   const int d = 4 * lane;             // a lane has channels 4 lane .. (dh is a multiple of 16)
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float total = 0.f;
-  const float* po = p.part_o + (slot0 * ROWS + rr % ROWS) * dh + d;
+  float total_w = 0.f;
   for (int c0 = 0; c0 < parts; c0 += 32) {
-    const float wl = c0 + lane < parts ? exp2f(lses[(int64_t)(c0 + lane) * ROWS] - ref) : 0.f;
+    const float wl = c0 + lane < parts ? exp2f(p.part_lse[slot(c0 + lane) * ROWS + rr % ROWS] - ref) : 0.f;
     const int m = min(32, parts - c0);
 #pragma unroll 8
     for (int c = 0; c < m; ++c) {
       const float w = __shfl_sync(0xffffffffu, wl, c);
-      total += w;
+      total_w += w;
       if (d < dh) {
-        const float4 v = *reinterpret_cast<const float4*>(po + (int64_t)(c0 + c) * ROWS * dh);
+        const float4 v = *reinterpret_cast<const float4*>(p.part_o + (slot(c0 + c) * ROWS + rr % ROWS) * dh + d);
         acc.x = fmaf(w, v.x, acc.x);
         acc.y = fmaf(w, v.y, acc.y);
         acc.z = fmaf(w, v.z, acc.z);
@@ -841,7 +886,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
       }
     }
   }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const float inv = total_w == 0.f ? 0.f : 1.f / total_w;
   if (d < dh) {
     T* out = reinterpret_cast<T*>(p.o) + (int64_t)row * p.ldo + (int64_t)h * dh + d;
     store1(out, bad ? NAN : acc.x * inv);
@@ -850,32 +895,24 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
     store1(out + 3, bad ? NAN : acc.w * inv);
   }
   if (lane == 0 && p.lse)
-    p.lse[(int64_t)row * p.n_heads + h] = bad ? NAN : total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
+    p.lse[(int64_t)row * p.n_heads + h] = bad ? NAN : total_w == 0.f ? -INFINITY : (ref + log2f(total_w)) * 0.6931471805599453f;
 }
 
-// Items of a launch, at most: parts of at least want keys come to no more than 148 x kItemsPerSm, one more for every tile and key head.
-int64_t most_items(int64_t Nq, int64_t n_seq, int64_t n_kv, int64_t g, int rows) {
-  const int64_t seqs = n_seq < Nq ? n_seq : Nq;
-  return (148 * kItemsPerSm + 1) + (Nq * g / rows + seqs) * n_kv;
-}
 inline int tile_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 8 * n_seq ? 8 : 16; }
 // Rows per sequence, on average, up to which the cache streams past tiles of 16 of them.
 inline bool paged_few_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 64 * n_seq; }
 
 struct RowsPlan {
   int rows;
-  int64_t items;
   size_t plan_bytes, o_bytes, lse_bytes;
   size_t bytes() const { return plan_bytes + o_bytes + lse_bytes; }
 };
-RowsPlan rows_plan(int64_t Nq, int64_t n_seq, int64_t n_kv, int64_t g, int64_t dh) {
+RowsPlan rows_plan(int64_t Nq, int64_t n_seq, int64_t g, int64_t dh) {
   RowsPlan r;
   r.rows = tile_rows(Nq, g, n_seq);
-  const int64_t n_here = n_seq < kPlanSeqs ? n_seq : kPlanSeqs;
-  r.items = most_items(Nq, n_here, n_kv, g, r.rows);
-  r.plan_bytes = align_up((size_t)(n_here + 2) * 4, 256);
-  r.o_bytes = align_up((size_t)r.items * r.rows * dh * 4, 256);
-  r.lse_bytes = align_up((size_t)r.items * r.rows * 4, 256);
+  r.plan_bytes = align_up((kPlanSeqs + 2) * sizeof(int64_t), 256);
+  r.o_bytes = align_up((size_t)2 * kMostCtas * r.rows * dh * 4, 256);
+  r.lse_bytes = align_up((size_t)2 * kMostCtas * r.rows * 4, 256);
   return r;
 }
 
@@ -887,13 +924,16 @@ cudaError_t launch_rows(const PagedParams& p, cudaStream_t stream) {
   cudaError_t e = attr_once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM); });
   if (e != cudaSuccess) return e;
   // as many blocks as can be resident and may have work
-  const int64_t seqs = p.n_here < p.Nq ? p.n_here : p.Nq, most = ceil_div((int64_t)p.c.max_pages * p.c.page_len, (int64_t)kLeastPart);
-  const int64_t work = ((int64_t)p.Nq * p.g / ROWS + seqs) * p.c.n_kv * (most > 0 ? most : 1), resident = (int64_t)sm_count() * C::CTAS;
+  const int64_t seqs = p.n_here < p.Nq ? p.n_here : p.Nq, keys = (int64_t)p.c.max_pages * p.c.page_len;
+  const int64_t tiles = ((int64_t)p.Nq * p.g / ROWS + seqs) * p.c.n_kv, work = ceil_div(tiles * (ceil_div(keys, (int64_t)kBlock) + 1), (int64_t)kLeastBlocks);
+  int64_t ctas = (int64_t)sm_count() * C::CTAS;
+  if (ctas > kMostCtas) ctas = kMostCtas;
+  if (ctas > work) ctas = work;
   count_launch();
-  e = launch(kernel, dim3((unsigned)(work < resident ? work : resident)), dim3(kThreads), C::SMEM, stream, p);
-  if (e != cudaSuccess || most < 2) return e;
+  e = launch(kernel, dim3((unsigned)ctas), dim3(C::THREADS), C::SMEM, stream, p);
+  if (e != cudaSuccess || ctas < 2) return e;
   count_launch();
-  const OverlapScope overlap(true);       // its blocks start while the parts end
+  const OverlapScope overlap(true);       // its blocks start while the pieces end
   return launch(paged_join_kernel<T, ROWS>, dim3((unsigned)ceil_div((int64_t)p.Nq * p.n_heads, (int64_t)8)), dim3(256), 0, stream, p);
 }
 template <typename T, int DH, bool FOUR>
@@ -908,24 +948,24 @@ cudaError_t launch_rows(const PagedParams& p, bool four, int rows, cudaStream_t 
 
 // cu_k of the opened keys: the lengths added up; a sequence that does not fit into max_keys (or has more tokens than its table) gets as many
 // rows as queries at most, which cache_read makes NaN: every query sees one of them.
-__global__ void __launch_bounds__(kThreads) open_plan_kernel(const CacheView c, const int32_t* cu_q, int32_t Nq, int32_t max_keys, int32_t* cu_k,
+__global__ void __launch_bounds__(kPlanThreads) open_plan_kernel(const CacheView c, const int32_t* cu_q, int32_t Nq, int32_t max_keys, int32_t* cu_k,
                                                              int32_t* status) {
   kernel_begin();
-  __shared__ int64_t s_word[kWarps];
+  __shared__ int64_t s_word[kPlanThreads / 32];
   int64_t at = 0, used = 0;               // rows given to the sequences before, and their keys
-  for (int32_t s0 = 0; s0 < c.n_seq; s0 += kThreads) {
+  for (int32_t s0 = 0; s0 < c.n_seq; s0 += kPlanThreads) {
     const int32_t s = s0 + threadIdx.x;
     int64_t n = 0, before;
     const int32_t nq = s < c.n_seq ? bounded(cu_q[s + 1], Nq) - bounded(cu_q[s], Nq) : 0;
     if (nq > 0) n = max(0, c.lens[s]);
-    const int64_t keys = block_scan(n, s_word, before);
+    const int64_t keys = block_scan<kPlanThreads / 32>(n, s_word, before);
     // (what fits is decided by the sum up to here, whether those before fitted or not: the same answer in any order)
     const bool fits = n == 0 || (used + before + n <= max_keys && n <= (int64_t)c.max_pages * c.page_len);
     if (!fits) {
       report_status(status, SP_ERR_SHAPE, s, -1);
       n = min(n, (int64_t)nq);
     }
-    const int64_t rows = block_scan(n, s_word, before);
+    const int64_t rows = block_scan<kPlanThreads / 32>(n, s_word, before);
     if (s < c.n_seq) cu_k[s] = (int32_t)(at + before);
     at += rows;
     used += keys;
@@ -966,10 +1006,8 @@ size_t sp_cache_attention_bytes(int64_t Nq, int32_t n_seq, int32_t n_heads, int3
       max_pages < 0 || page_len < 1 || (int64_t)max_pages * page_len > (1 << 30))
     return 0;
   const int64_t g = n_heads / n_kv_heads;
-  if (paged_few_rows(Nq, g, n_seq)) {
-    const RowsPlan plan = rows_plan(Nq, n_seq, n_kv_heads, g, d_head);
-    return plan.items > 0x7fffffff ? 0 : plan.bytes();
-  }
+  if (Nq * g > 0x7fffffff) return 0;
+  if (paged_few_rows(Nq, g, n_seq)) return rows_plan(Nq, n_seq, g, d_head).bytes();
   const int64_t keys = keys_at_most(max_keys, n_seq, max_pages, page_len);
   if (keys + Nq > (1 << 30)) return 0;
   return open_plan(Nq, n_seq, n_heads, n_kv_heads, d_head, dtype, keys).bytes();
@@ -993,14 +1031,14 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   if (!Q->ptr || !O->ptr || !cu_q) return SP_ERR_INVALID_ARG;
   const int64_t g = n_heads / n_kv;
   const size_t need = sp_cache_attention_bytes(Nq, n_seq, n_heads, n_kv, dh, dt, cache->max_pages, cache->page_len, max_keys);
-  if (need == 0) return SP_ERR_SHAPE;                            // (more keys than can be opened: max_keys tells how many there are)
+  if (need == 0) return SP_ERR_SHAPE;                            // (too many rows, or more keys than can be opened: max_keys tells how many there are)
   if (!ws || ws_bytes < need) return SP_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(ws) & 255u) return SP_ERR_ALIGNMENT;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   uint8_t* at = reinterpret_cast<uint8_t*>(ws);
   ProfScope prof(PK_GEMM_SIMT, 0.0, 0.0, s);
   if (paged_few_rows(Nq, g, n_seq)) {
-    const RowsPlan plan = rows_plan(Nq, n_seq, n_kv, g, dh);
+    const RowsPlan plan = rows_plan(Nq, n_seq, g, dh);
     PagedParams p = {};
     p.c = cache_view(cache);
     p.q = Q->ptr; p.o = O->ptr;
@@ -1009,11 +1047,10 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
     p.cu_q = cu_q;
     p.Nq = (int32_t)Nq; p.n_heads = n_heads; p.g = (int32_t)g; p.causal = causal != 0;
     p.scale_log2 = (float)(scale * 1.4426950408889634);
-    p.plan = reinterpret_cast<int32_t*>(at);
+    p.plan = reinterpret_cast<int64_t*>(at);
     p.part_o = reinterpret_cast<float*>(at + plan.plan_bytes);
     p.part_lse = reinterpret_cast<float*>(at + plan.plan_bytes + plan.o_bytes);
     p.status = status_dev;
-    p.max_items = (int32_t)plan.items;
     for (p.s0 = 0; p.s0 < n_seq; p.s0 += kPlanSeqs) {
       p.n_here = n_seq - p.s0 < kPlanSeqs ? n_seq - p.s0 : kPlanSeqs;
       const bool four = cache->kind == SP_CACHE_4BIT;
@@ -1030,7 +1067,7 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   uint8_t *K_lo = parts ? V + plan.k_bytes : nullptr, *V_lo = parts ? K_lo + plan.lo_bytes : nullptr;
   const int64_t kv = (int64_t)n_kv * dh;
   count_launch();
-  if (launch(open_plan_kernel, dim3(1), dim3(kThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, status_dev) !=
+  if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, status_dev) !=
           cudaSuccess ||
       cache_read(cache, cu_k, plan.rows, K, V, kv, kv, dt, true, status_dev, s, K_lo, V_lo) != cudaSuccess)
     return SP_ERR_CUDA;
