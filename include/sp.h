@@ -622,7 +622,8 @@ sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const sp_mat* W,
  *     [n_pages, n_kv_heads, page_len, d_head / 64, 2], scale and zero of every 64 channels: a number n stands for scale n + zero.  d_head 64 or 128.
  *     zero = bf16(least), scale = bf16((largest - zero) / 15), n = (x - zero) / scale rounded to the nearest of 0 .. 15 (halves to even; 0 where
  *     scale is 0).  A group with a NaN or an infinity reads back as NaN.
- * The *_step are the bytes from a page to the next (multiples of 16 below 2^32), so that the pages of several layers may lie in one buffer.
+ * step (a multiple of 128) and scale_step (of 64) are the bytes from a page to the next, in k and v alike, so that the pages of several layers may lie in one
+ * buffer.
  * A token whose place has no page (a place before 0 or behind the table, an entry outside [0, n_pages)) is reported through status_dev (may be
  * NULL) as SP_ERR_SHAPE with the sequence, and nothing outside the pages is touched: it is not appended, reads back as NaN, and makes the queries NaN
  * that see it.  Pages that sequences share may be read by all; one slot that two tokens of a call are put into holds either.
@@ -653,7 +654,7 @@ typedef enum { SP_CACHE_BF16 = 0, SP_CACHE_4BIT = 1 } sp_cache_kind;
 typedef struct {
   void *k, *v;
   void *k_scale, *v_scale;           /* SP_CACHE_4BIT */
-  int64_t k_step, v_step, k_scale_step, v_scale_step;
+  int64_t step, scale_step;          /* bytes from a page to the next, of k and v, of k_scale and v_scale */
   const int32_t* table;              /* [n_seq, max_pages], device */
   const int32_t* lens;               /* [n_seq], device */
   int64_t table_ld;

@@ -103,8 +103,8 @@ class SpAttentionArgs(C.Structure):
 
 
 class SpKvCache(C.Structure):
-    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_step", C.c_int64),
-                ("v_step", C.c_int64), ("k_scale_step", C.c_int64), ("v_scale_step", C.c_int64), ("table", C.c_void_p),
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("step", C.c_int64),
+                ("scale_step", C.c_int64), ("table", C.c_void_p),
                 ("lens", C.c_void_p), ("table_ld", C.c_int64), ("max_pages", C.c_int32), ("n_seq", C.c_int32), ("kind", C.c_int32),
                 ("n_pages", C.c_int32), ("page_len", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32),
                 ("reserved", C.c_int32)]
@@ -738,8 +738,8 @@ def sp_linear_e4m3(X, x_scale, W, w_scale, bias=None, act=SP_LINEAR_NONE, other=
 @dataclass
 class KvPages:
     """Pages of keys and values of one module: bf16 [n_pages, n_kv_heads, page_len, d_head], or 4 bits: uint8 [.., d_head / 2] with
-    bf16 scales [n_pages, n_kv_heads, page_len, d_head / 64, 2] (see sp.h).  A page's entries are contiguous; pages may lie any multiple of 16
-    bytes apart, so that those of several modules can be slices of one buffer."""
+    bf16 scales [n_pages, n_kv_heads, page_len, d_head / 64, 2] (see sp.h).  A page's entries are contiguous; pages may lie any multiple of 128
+    bytes apart (scales: of 64), so that those of several modules can be slices of one buffer."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor | None = None
@@ -782,14 +782,15 @@ class KvPages:
                     raise ValueError("the entries of a page must be contiguous")
                 inner *= shape[i]
             steps.append((stride[0] if n_pages > 1 else inner) * t.element_size())
-        if not four:
-            steps += [0, 0]
+        if n_pages > 1 and (steps[0] != steps[1] or (four and steps[2] != steps[3])):
+            raise ValueError("the pages of k and v lie equally far apart, and so do those of their scales")
         if table.dim() != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and table.shape[1] > 1):
             raise ValueError("table must be int32 [n_seq, pages] with contiguous rows")
         if table.get_device() != dev:
             _elsewhere(table)
         n_seq, max_pages = table.shape
-        return SpKvCache(k.data_ptr(), v.data_ptr(), _ptr(self.k_scale) if four else None, _ptr(self.v_scale) if four else None, *steps,
+        return SpKvCache(k.data_ptr(), v.data_ptr(), _ptr(self.k_scale) if four else None, _ptr(self.v_scale) if four else None, steps[0],
+                         steps[2] if four else 0,
                          table.data_ptr(), _vector(lens, torch.int32, n_seq, dev, "lens"),
                          table.stride(0) if n_seq > 1 else max_pages, max_pages, n_seq, SP_CACHE_4BIT if four else SP_CACHE_BF16,
                          n_pages, page_len, n_kv, d_head, 0)

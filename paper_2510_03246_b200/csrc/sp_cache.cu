@@ -235,11 +235,11 @@ __global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const A
         uint32_t pair;
         const uint32_t packed = four_bits(a, pair);
         if (page >= 0 && live) {
-          *reinterpret_cast<uint32_t*>(p.c.v + page * p.c.v_step + at * (dh / 2) + 4 * chunk) = packed;
-          if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.vs + page * p.c.vs_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
+          *reinterpret_cast<uint32_t*>(p.c.v + page * p.c.step + at * (dh / 2) + 4 * chunk) = packed;
+          if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.vs + page * p.c.scale_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
         }
       } else if (page >= 0 && live) {
-        put8(reinterpret_cast<__nv_bfloat16*>(p.c.v + page * p.c.v_step) + at * dh + 8 * chunk, true, a);
+        put8(reinterpret_cast<__nv_bfloat16*>(p.c.v + page * p.c.step) + at * dh + 8 * chunk, true, a);
       }
       continue;
     }
@@ -280,11 +280,11 @@ __global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const A
       uint32_t pair;
       const uint32_t packed = four_bits(x, pair);
       if (page >= 0 && live) {
-        *reinterpret_cast<uint32_t*>(p.c.k + page * p.c.k_step + at * (dh / 2) + 4 * chunk) = packed;
-        if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.ks + page * p.c.ks_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
+        *reinterpret_cast<uint32_t*>(p.c.k + page * p.c.step + at * (dh / 2) + 4 * chunk) = packed;
+        if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.ks + page * p.c.scale_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
       }
     } else if (page >= 0 && live) {
-      put8(reinterpret_cast<__nv_bfloat16*>(p.c.k + page * p.c.k_step) + at * dh + 8 * chunk, true, x);
+      put8(reinterpret_cast<__nv_bfloat16*>(p.c.k + page * p.c.step) + at * dh + 8 * chunk, true, x);
     }
   }
 }
@@ -329,19 +329,19 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = y[k] = NAN;
     } else if constexpr (FOUR) {
-      const uint32_t a = *reinterpret_cast<const uint32_t*>(p.c.k + page * p.c.k_step + at * (dh / 2) + 4 * chunk);
-      const uint32_t b = *reinterpret_cast<const uint32_t*>(p.c.v + page * p.c.v_step + at * (dh / 2) + 4 * chunk);
+      const uint32_t a = *reinterpret_cast<const uint32_t*>(p.c.k + page * p.c.step + at * (dh / 2) + 4 * chunk);
+      const uint32_t b = *reinterpret_cast<const uint32_t*>(p.c.v + page * p.c.step + at * (dh / 2) + 4 * chunk);
       const int64_t g = (at * (dh / kCacheGroup) + chunk / 8) * 4;
-      const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + page * p.c.ks_step + g);
-      const uint32_t sb = *reinterpret_cast<const uint32_t*>(p.c.vs + page * p.c.vs_step + g);
+      const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + page * p.c.scale_step + g);
+      const uint32_t sb = *reinterpret_cast<const uint32_t*>(p.c.vs + page * p.c.scale_step + g);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         x[k] = fmaf((float)((a >> (4 * k)) & 15u), __uint_as_float(sa << 16), __uint_as_float(sa & 0xffff0000u));
         y[k] = fmaf((float)((b >> (4 * k)) & 15u), __uint_as_float(sb << 16), __uint_as_float(sb & 0xffff0000u));
       }
     } else {
-      load8(reinterpret_cast<const __nv_bfloat16*>(p.c.k + page * p.c.k_step) + at * dh + 8 * chunk, true, x);
-      load8(reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.v_step) + at * dh + 8 * chunk, true, y);
+      load8(reinterpret_cast<const __nv_bfloat16*>(p.c.k + page * p.c.step) + at * dh + 8 * chunk, true, x);
+      load8(reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.step) + at * dh + 8 * chunk, true, y);
     }
     put8(reinterpret_cast<T*>(p.k) + row * p.ldk + head * dh + 8 * chunk, p.k_vec != 0, x);
     put8(reinterpret_cast<T*>(p.v) + row * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, y);
@@ -360,8 +360,8 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
 bool rows_of_16(const void* ptr, int64_t ld, int32_t dtype, int64_t rows) {
   return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0 && (rows < 2 || ld * (int64_t)dtype_size(dtype) % 16 == 0);
 }
-bool step_fits(int64_t step, int64_t page_bytes, int32_t n_pages) {
-  return n_pages < 2 || (step % 16 == 0 && step >= page_bytes && step <= 0xffffffffll);
+bool step_fits(int64_t step, int64_t page_bytes, int64_t unit, int32_t n_pages) {
+  return n_pages < 2 || (step % unit == 0 && step >= page_bytes && step <= (int64_t)0xfffffffe * unit / n_pages);
 }
 
 }  // namespace
@@ -379,9 +379,10 @@ sp_status check_cache(const sp_kv_cache* c, bool pages) {
       (int64_t)c->max_pages * c->page_len > (1 << 30) || (c->n_seq > 1 && c->table_ld < c->max_pages))
     return SP_ERR_SHAPE;
   const int64_t tokens = (int64_t)c->n_kv_heads * c->page_len, bytes = tokens * (four ? c->d_head / 2 : 2 * c->d_head);
-  if (!step_fits(c->k_step, bytes, c->n_pages) || !step_fits(c->v_step, bytes, c->n_pages)) return SP_ERR_SHAPE;
-  const int64_t scales = tokens * (c->d_head / kCacheGroup) * 4;
-  if (four && (!step_fits(c->k_scale_step, scales, c->n_pages) || !step_fits(c->v_scale_step, scales, c->n_pages))) return SP_ERR_SHAPE;
+  // (a place in a page is named by 32 bits in units of 128 bytes, of 64 among the scales)
+  if (!step_fits(c->step, bytes, 128, c->n_pages) ||
+      (four && !step_fits(c->scale_step, tokens * (c->d_head / kCacheGroup) * 4, 64, c->n_pages)))
+    return SP_ERR_SHAPE;
   for (const void* ptr : {c->k, c->v, four ? c->k_scale : nullptr, four ? c->v_scale : nullptr})
     if (reinterpret_cast<uintptr_t>(ptr) & 15u) return SP_ERR_ALIGNMENT;
   return SP_OK;
@@ -391,7 +392,7 @@ CacheView cache_view(const sp_kv_cache* c) {
   CacheView w = {};
   w.k = reinterpret_cast<uint8_t*>(c->k); w.v = reinterpret_cast<uint8_t*>(c->v);
   w.ks = reinterpret_cast<uint8_t*>(c->k_scale); w.vs = reinterpret_cast<uint8_t*>(c->v_scale);
-  w.k_step = c->k_step; w.v_step = c->v_step; w.ks_step = c->k_scale_step; w.vs_step = c->v_scale_step;
+  w.step = c->step; w.scale_step = c->scale_step;
   w.table = c->table; w.lens = c->lens; w.table_ld = c->table_ld;
   w.n_pages = c->n_pages; w.page_len = c->page_len; w.max_pages = c->max_pages;
   w.n_kv = c->n_kv_heads; w.dh = c->d_head; w.n_seq = c->n_seq;

@@ -8,7 +8,7 @@ constexpr int kCacheGroup = SP_CACHE_GROUP;
 
 struct CacheView {
   uint8_t *k, *v, *ks, *vs;                // first page; scales (4 bits): pairs of bf16, scale and offset
-  int64_t k_step, v_step, ks_step, vs_step;      // bytes from a page to the next
+  int64_t step, scale_step;                // bytes from a page to the next
   const int32_t* table;
   const int32_t* lens;
   int64_t table_ld;

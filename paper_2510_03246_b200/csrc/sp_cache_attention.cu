@@ -37,6 +37,7 @@ constexpr int kPlanSeqs = 256;             // sequences of a launch
 constexpr int kLeastBlocks = 16;           // blocks of keys to a thread block, at least
 constexpr int kMostCtas = 2 * 148;         // thread blocks of a launch, at most
 constexpr int kPlanThreads = 256;
+constexpr uint32_t kNoPage = 0xffffffffu;
 
 struct PagedParams {
   CacheView c;
@@ -81,8 +82,8 @@ struct PagedCfg {
 };
 
 __device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {      // zeros where there is nothing to copy
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -417,50 +418,51 @@ paged_rows_kernel(const PagedParams p) {
     }
     bool found = false;                                          // bf16: non-finite values behind some row's mask
 
-    // ---- copies: block i of this warp starts at key kb + 16 (warp + W i).  Pages and places of 32 blocks at a time, a lane each.
-    int32_t pages = -1, slots = 0;
+    // ---- copies: block i of this warp starts at key kb + 16 (warp + W i).  Where 32 of them stand is looked up at a time, a lane each, in
+    // units of 128 bytes (kNoPage: there is none) and of 64 for the scales.
+    uint32_t places = kNoPage, scale_places = 0u;
     uint32_t missing = 0u;                                       // a bit per block fetched, the last one lowest: it has no page
-    uint32_t into = ring;                                        // the stage that is next
-    constexpr int kRow = FOUR ? DH / 2 : 2 * DH, kScales = 4 * G;      // bytes of a key, of its scales
-    const int row_bytes = FOUR ? kRow : 2 * dh;
-    const int64_t head0 = (int64_t)head * p.c.page_len;
-    const uint8_t* k_from = p.c.k + head0 * row_bytes + 16 * lane;
-    const uint8_t* v_from = p.c.v + head0 * row_bytes + 16 * lane;
-    const uint8_t* s_from = FOUR ? (lane < 16 ? p.c.ks : p.c.vs) + head0 * kScales + 16 * (lane & 15) : nullptr;
-    const uint32_t s_step = (uint32_t)(lane < 16 ? p.c.ks_step : p.c.vs_step);
+    uint32_t into = ring + R::BYTES - R::STAGE;                  // the stage that was filled last
+    const int row_bytes = FOUR ? DH / 2 : 2 * dh;
+    const uint8_t *k_from = p.c.k + 16 * lane, *v_from = p.c.v + 16 * lane;
+    const uint8_t* s_from = FOUR ? (lane < 16 ? p.c.ks : p.c.vs) + 16 * (lane & 15) : nullptr;
+    const uint32_t s_to = 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * (lane & 15);
+    const bool has_scale = (lane & 15) < 4 * G;
     const auto fetch = [&](int32_t i) {
       missing <<= 1;
       if (i < own) {
         if ((i & 31) == 0) {
           const int32_t at_ = i + lane, key = kb + kBlock * (warp + W * at_), entry = key / p.c.page_len;
-          pages = at_ < own ? page_of(p.c, sq, entry) : -1;
-          slots = key - entry * p.c.page_len;
+          const int32_t page = at_ < own ? page_of(p.c, sq, entry) : -1;
+          const int64_t token = (int64_t)head * p.c.page_len + (key - entry * p.c.page_len);
+          places = page < 0 ? kNoPage : (uint32_t)((page * p.c.step + token * row_bytes) >> 7);
+          if (FOUR) scale_places = (uint32_t)((page * p.c.scale_step + token * (4 * G)) >> 6);
         }
-        const int32_t page = __shfl_sync(0xffffffffu, pages, i & 31);
-        const uint32_t slot = (uint32_t)__shfl_sync(0xffffffffu, slots, i & 31);
-        const bool there = page >= 0;
-        const uint32_t pg = there ? (uint32_t)page : 0u;
-        missing |= there ? 0u : 1u;
-        // (steps below 2^32, rows of a page below 2^16 of at most 256 bytes: one multiplication each)
-        const uint8_t* k = k_from + (uint64_t)pg * (uint32_t)p.c.k_step + slot * (uint32_t)row_bytes;
-        const uint8_t* v = v_from + (uint64_t)pg * (uint32_t)p.c.v_step + slot * (uint32_t)row_bytes;
+        const uint32_t place = __shfl_sync(0xffffffffu, places, i & 31);
+        into = into + R::STAGE == ring + R::BYTES ? ring : into + R::STAGE;
+        if (place == kNoPage) {                                  // (what stands in the stage only meets probabilities that are NaN)
+          missing |= 1u;
+          copies_end();
+          return;
+        }
+        const uint8_t *k = k_from + (uint64_t)place * 128u, *v = v_from + (uint64_t)place * 128u;
         if constexpr (FOUR) {
 #pragma unroll
           for (int e = 0; e < DH / 2; e += 32) {                 // pieces of the block's 16 rows
             // 32-byte quarters of a 128-byte line change places with the line's number: the four keys of a half warp's read of K, and the
             // four pairs of keys of a read of V, lie in different banks
-            copy16(into + 16 * e + piece_to, k + 16 * e, there);
-            copy16(into + R::TILE + 16 * e + piece_to, v + 16 * e, there);
+            copy16(into + 16 * e + piece_to, k + 16 * e);
+            copy16(into + R::TILE + 16 * e + piece_to, v + 16 * e);
           }
-          if ((lane & 15) < 4 * G)
-            copy16(into + 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * (lane & 15), s_from + (uint64_t)pg * s_step + slot * kScales, there);
+          const uint32_t scale_place = __shfl_sync(0xffffffffu, scale_places, i & 31);
+          if (has_scale) copy16(into + s_to, s_from + (uint64_t)scale_place * 64u);
         } else if (dh == DH) {
 #pragma unroll
           for (int e = 0; e < kBlock * R::PIECES; e += 32) {
             const int row = e / R::PIECES + lane / R::PIECES;    // (a power of two, at most 32)
             const uint32_t to = into + row * R::PITCH + 16 * (lane % R::PIECES);
-            copy16(to, k + 16 * e, there);
-            copy16(to + R::TILE, v + 16 * e, there);
+            copy16(to, k + 16 * e);
+            copy16(to + R::TILE, v + 16 * e);
           }
         } else {
           const int per = dh / 8;
@@ -468,11 +470,10 @@ paged_rows_kernel(const PagedParams p) {
           for (int e = lane; e < kBlock * per; e += 32) {
             const int row = e / per;
             const uint32_t to = into + row * R::PITCH + 16 * (e - row * per);
-            copy16(to, k + 16 * (e - lane), there);
-            copy16(to + R::TILE, v + 16 * (e - lane), there);
+            copy16(to, k + 16 * (e - lane));
+            copy16(to + R::TILE, v + 16 * (e - lane));
           }
         }
-        into = into + R::STAGE == ring + R::BYTES ? ring : into + R::STAGE;
       }
       copies_end();
     };
@@ -616,13 +617,14 @@ paged_rows_kernel(const PagedParams p) {
         for (int y = 0; y < 2; ++y)
 #pragma unroll
           for (int gr = 0; gr < G; ++gr) pair[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
-        // (0 times a scale is 0 unless that is a NaN or an infinity)
+        // (0 times a scale is 0 unless that is a NaN or an infinity; read again here, so that this stays behind the branch)
         bool strict = false;
         if (edge) {
-#pragma unroll
           for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int gr = 0; gr < G; ++gr) strict |= !(fabsf(low(pair[y][gr])) < 1e37f) || !(fabsf(high(pair[y][gr])) < 1e37f);
+            for (int gr = 0; gr < G; ++gr) {
+              const uint32_t w = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
+              strict |= !(fabsf(low(w)) < INFINITY) || !(fabsf(high(w)) < INFINITY);
+            }
           strict = __any_sync(0xffffffffu, strict);
         }
 #pragma unroll
@@ -810,7 +812,7 @@ paged_rows_kernel(const PagedParams p) {
         for (int32_t key = max(sure, kb); key < last; ++key) {
           const int32_t page = page_of(p.c, sq, key / p.c.page_len);
           if (page < 0) continue;
-          const __nv_bfloat16* V = reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.v_step) +
+          const __nv_bfloat16* V = reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.step) +
                                    ((int64_t)head * p.c.page_len + key % p.c.page_len) * dh;
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
