@@ -25,6 +25,8 @@
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "sp_attention.cuh"
 #include "sp_cache.cuh"
 #include "sp_f32x2.cuh"
@@ -170,6 +172,10 @@ __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
+// A value that all lanes of a warp have, as the compiler can know it: loops and addresses then need no lane's registers, and branches no
+// meeting points.
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // What a sequence brings: its rows of queries and its keys.
 struct Seq {
   int32_t q0, nq, nk;
@@ -231,7 +237,7 @@ paged_rows_kernel(const PagedParams p) {
   __shared__ int64_t s_first[kPlanSeqs + 1];
   __shared__ int64_t s_word[W];
   __shared__ int s_bad;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g4 = lane >> 2, t4 = lane & 3;
+  const int lane = threadIdx.x & 31, warp = uniform((int)threadIdx.x >> 5), g4 = lane >> 2, t4 = lane & 3;
   const int n_kv = p.c.n_kv, dh = FOUR ? DH : p.c.dh;
 
   // The plan, the same in every block: where the work of each sequence starts.
@@ -301,10 +307,11 @@ paged_rows_kernel(const PagedParams p) {
     const uint32_t g = (uint32_t)p.g, r0 = tile * ROWS;
     const int rows = (int)min((uint32_t)ROWS, (uint32_t)it.nq * g - r0);
     const int64_t shift = p.causal ? (int64_t)it.nk - it.nq : (int64_t)it.nk;        // query i sees keys j <= i + shift
-    const int32_t sure = visible(it.nk, shift, r0 / g);                              // keys that every row sees
-    const int32_t kb = (int32_t)block0 * kBlock;
+    const int32_t sure = uniform(visible(it.nk, shift, r0 / g));                     // keys that every row sees
+    const int32_t kb = uniform((int32_t)block0 * kBlock);
     int32_t seen = visible(it.nk, shift, (r0 + rows - 1) / g);                       // keys that some row sees
     if (seen - kb > (int32_t)piece * kBlock) seen = kb + (int32_t)piece * kBlock;
+    seen = uniform(seen);
     const int32_t blocks = seen > kb ? (seen - kb + kBlock - 1) / kBlock : 0;
     const int32_t own = blocks > warp ? (blocks - warp - 1) / W + 1 : 0;             // this warp's: warp, warp + W, ...
 
@@ -564,12 +571,19 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
           for (int x = 0; x < 4; ++x) s[h][x] = NAN;
       }
+      if (edge) {
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (kt + 8 * (x >> 1) + g4 >= lim[h][x & 1]) s[h][x] = -INFINITY;
+        __syncwarp();                                            // (keeps this a branch)
+      }
       bool rise = false;
 #pragma unroll
       for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          if (edge && kt + 8 * (x >> 1) + g4 >= lim[h][x & 1]) s[h][x] = -INFINITY;
           rise |= !(s[h][x] <= most[h][x & 1]);
         }
       if (__any_sync(0xffffffffu, rise)) {                       // seldom: the references follow the maxima of this block
@@ -618,15 +632,16 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
           for (int gr = 0; gr < G; ++gr) pair[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
         // (0 times a scale is 0 unless that is a NaN or an infinity; read again here, so that this stays behind the branch)
-        bool strict = false;
+        bool odd_scales = false;
         if (edge) {
           for (int y = 0; y < 2; ++y)
             for (int gr = 0; gr < G; ++gr) {
               const uint32_t w = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
-              strict |= !(fabsf(low(w)) < INFINITY) || !(fabsf(high(w)) < INFINITY);
+              odd_scales |= !(fabsf(low(w)) < INFINITY) || !(fabsf(high(w)) < INFINITY);
             }
-          strict = __any_sync(0xffffffffu, strict);
+          odd_scales = __any_sync(0xffffffffu, odd_scales);
         }
+        const auto add_values = [&](auto strict) {
 #pragma unroll
         for (int gr = 0; gr < G; ++gr) {
           uint32_t pb[H][PARTS][2];                              // (P s)^T: keys 2 t4, + 1 | 2 t4 + 8, + 9 of row 8 h + g4
@@ -644,7 +659,7 @@ paged_rows_kernel(const PagedParams p) {
                 ps[x] = s[h][2 * y + x] * scale;
                 pz[x] = zero;
               }
-              if (strict) {                                      // whatever stands in a slot that the row does not see
+              if constexpr (decltype(strict)::value) {                                      // whatever stands in a slot that the row does not see
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
                   if (kt + 8 * y + g4 >= lim[h][x]) ps[x] = pz[x] = 0.f;
@@ -694,6 +709,9 @@ paged_rows_kernel(const PagedParams p) {
               }
             }
         }
+        };
+        if (odd_scales) add_values(std::true_type());
+        else add_values(std::false_type());
       } else {
         uint32_t pb[H][PARTS][2];
 #pragma unroll
