@@ -654,17 +654,19 @@ def sp_token_logprobs_grad(logits, targets, lse, g_logp, entropy=None, g_entropy
 
 
 # ------------------------------------------------------------- norm, 8-bit projections, paged caches of keys and values
+# These serve single tokens, so their checks, allocations and marshalling are native (csrc/sp_binding.cpp).
 _F8 = torch.float8_e4m3fn
+_native = None
 
 
-def _eight(t, dev, what):
-    """Matrix view of a 2-D e4m3 tensor whose rows are contiguous."""
-    if t.get_device() != dev:
-        _elsewhere(t)
-    if t.dtype != _F8 or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{what} must be a row-major 2-D tensor of float8_e4m3fn")
-    rows, cols = t.shape
-    return SpMat(t.data_ptr(), SP_E4M3, 0, rows, cols, t.stride(0) if rows > 1 else max(cols, t.stride(0)))
+def _binding():
+    """The native binding of the calls below; raises if it is not built."""
+    global _native
+    if _native is None:
+        lib()
+        from . import _binding as native
+        _native = native
+    return _native
 
 
 @dataclass
@@ -679,60 +681,34 @@ def sp_rms_norm(X, weight=None, eps=1e-5, residual=None, h_out=None, out=None, o
     """h = X + residual, y = weight h / sqrt(mean h^2 + eps) (see sp.h).  X [T, d] bf16 or fp32, residual of either, weight fp32 [d].
     h_out: where to write h (residual or X itself: in place; allocated where there is a residual).  out_dtype
     torch.float8_e4m3fn: 8 bits with a scale per row, rows that start on 16 bytes, as sp_linear_e4m3 reads them."""
-    dev = _current_device(X)
-    x = _rows(X, dev, "X")
-    r = None if residual is None else _rows(residual, dev, "residual")
-    if out is None:
-        out = rows_of_16_bytes(x.rows, x.cols, out_dtype or X.dtype, X.device)
-    if h_out is None and residual is not None:
-        h_out = torch.empty(x.rows, x.cols, dtype=residual.dtype, device=X.device)
-    eight = out.dtype == _F8
-    y = _eight(out, dev, "out") if eight else _rows(out, dev, "out")
-    h = None if h_out is None else _rows(h_out, dev, "h_out")
-    scale = torch.empty(x.rows, dtype=torch.float32, device=X.device) if eight else None
-    rstd = torch.empty(x.rows, dtype=torch.float32, device=X.device) if want_rstd else None
-    _check(lib().sp_rms_norm(C.byref(x), None if r is None else C.byref(r), _vector(weight, torch.float32, x.cols, dev, "weight"), eps,
-                             None if h is None else C.byref(h), C.byref(y), _ptr(scale), _ptr(rstd),
-                             torch._C._cuda_getCurrentRawStream(dev)), "sp_rms_norm")
-    return RmsNorm(out, h_out, scale, rstd)
+    if out_dtype is not None and out_dtype != _F8 and out_dtype != X.dtype:
+        raise ValueError("the result is of X's dtype or float8_e4m3fn")
+    code, y, h, scale, rstd = (_native or _binding()).rms_norm(X, weight, eps, residual, h_out, out, out_dtype is _F8, want_rstd)
+    if code:
+        raise SpError(code, "sp_rms_norm")
+    return RmsNorm(y, h, scale, rstd)
 
 
 def sp_rms_norm_grad(dY, H, weight=None, rstd=None, eps=1e-5, d_stream=None, want_weight=True, out=None, ws=None):
     """Gradient of sp_rms_norm with respect to h (so to x and to the residual) and to the weight (see sp.h): dY [T, d] the gradient of
     y, H and rstd as the forward call left them (rstd None: formed again), d_stream the gradient that arrives at h by itself.  out may be
     d_stream.  Returns (dX of H's dtype, dweight fp32 [d] or None)."""
-    dev = _current_device(dY)
-    g, h = _rows(dY, dev, "dY"), _rows(H, dev, "H")
-    if out is None:
-        out = torch.empty(g.rows, g.cols, dtype=H.dtype, device=dY.device)
-    d = None if d_stream is None else _rows(d_stream, dev, "d_stream")
-    dw = torch.empty(g.cols, dtype=torch.float32, device=dY.device) if want_weight else None
-    if ws is None:
-        ws = _ws(lib().sp_rms_norm_grad_bytes(g.rows, g.cols), dY.device) if want_weight else None
-    elif ws.get_device() != dev:
-        _elsewhere(ws)
-    _check(lib().sp_rms_norm_grad(C.byref(g), C.byref(h), _vector(weight, torch.float32, g.cols, dev, "weight"),
-                                  _vector(rstd, torch.float32, g.rows, dev, "rstd"), eps, None if d is None else C.byref(d),
-                                  C.byref(_rows(out, dev, "out")), _ptr(dw), _ptr(ws), ws.nbytes if ws is not None else 0,
-                                  torch._C._cuda_getCurrentRawStream(dev)), "sp_rms_norm_grad")
-    return out, dw
+    code, dx, dw = (_native or _binding()).rms_norm_grad(dY, H, weight, rstd, eps, d_stream, want_weight, out, ws)
+    if code:
+        raise SpError(code, "sp_rms_norm_grad")
+    return dx, dw
 
 
 def sp_linear_e4m3(X, x_scale, W, w_scale, bias=None, act=SP_LINEAR_NONE, other=None, combine=SP_COMBINE_ADD, out=None,
                    out_dtype=torch.bfloat16, status=None):
     """act(x_scale w_scale X W^T + bias), then other added or multiplied (see sp.h).  X [T, in], W [out, in]: float8_e4m3fn, rows that start
     on 16 bytes; x_scale fp32 [T] (sp_rms_norm), w_scale fp32 [out].  The result is bf16 or fp32."""
-    dev = _current_device(X)
-    x, w = _eight(X, dev, "X"), _eight(W, dev, "W")
-    if out is None:
-        out = rows_of_16_bytes(x.rows, w.rows, out_dtype, X.device)
-    o = None if other is None else C.byref(_rows(other, dev, "other"))
-    _check(lib().sp_linear_e4m3(C.byref(x), _vector(x_scale, torch.float32, x.rows, dev, "x_scale"), C.byref(w),
-                                _vector(w_scale, torch.float32, w.rows, dev, "w_scale"),
-                                _vector(bias, torch.float32, w.rows, dev, "bias"), act, o, combine, C.byref(_rows(out, dev, "out")),
-                                _vector(status, torch.int32, 4, dev, "status"), torch._C._cuda_getCurrentRawStream(dev)),
-           "sp_linear_e4m3")
-    return out
+    if out_dtype is not torch.bfloat16 and out_dtype is not torch.float32:
+        raise ValueError("the result is bf16 or fp32")
+    code, y = (_native or _binding()).linear_e4m3(X, x_scale, W, w_scale, bias, act, other, combine, out, out_dtype is torch.float32, status)
+    if code:
+        raise SpError(code, "sp_linear_e4m3")
+    return y
 
 
 @dataclass
@@ -756,45 +732,6 @@ class KvPages:
         return KvPages(of(d_head // 2, dtype=torch.uint8), of(d_head // 2, dtype=torch.uint8), of(g, 2, dtype=torch.bfloat16),
                        of(g, 2, dtype=torch.bfloat16))
 
-    def view(self, dev, table, lens) -> SpKvCache:
-        k, v = self.k, self.v
-        four = k.dtype == torch.uint8
-        if not four and k.dtype != torch.bfloat16:
-            raise ValueError("pages are bf16 or uint8")
-        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
-            raise ValueError("k and v must be [n_pages, n_kv_heads, page_len, d_head] of one shape and dtype")
-        n_pages, n_kv, page_len, d = k.shape
-        d_head = 2 * d if four else d
-        pages = [k, v]
-        if four:
-            want = (n_pages, n_kv, page_len, d_head // SP_CACHE_GROUP, 2)
-            for t in (self.k_scale, self.v_scale):
-                if t is None or t.shape != want or t.dtype != torch.bfloat16:
-                    raise ValueError(f"k_scale and v_scale must be bf16 {list(want)}")
-            pages += [self.k_scale, self.v_scale]
-        steps = []
-        for t in pages:
-            if t.get_device() != dev:
-                _elsewhere(t)
-            inner, stride, shape = 1, t.stride(), t.shape
-            for i in range(len(shape) - 1, 0, -1):
-                if stride[i] != inner and shape[i] > 1:
-                    raise ValueError("the entries of a page must be contiguous")
-                inner *= shape[i]
-            steps.append((stride[0] if n_pages > 1 else inner) * t.element_size())
-        if n_pages > 1 and (steps[0] != steps[1] or (four and steps[2] != steps[3])):
-            raise ValueError("the pages of k and v lie equally far apart, and so do those of their scales")
-        if table.dim() != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and table.shape[1] > 1):
-            raise ValueError("table must be int32 [n_seq, pages] with contiguous rows")
-        if table.get_device() != dev:
-            _elsewhere(table)
-        n_seq, max_pages = table.shape
-        return SpKvCache(k.data_ptr(), v.data_ptr(), _ptr(self.k_scale) if four else None, _ptr(self.v_scale) if four else None, steps[0],
-                         steps[2] if four else 0,
-                         table.data_ptr(), _vector(lens, torch.int32, n_seq, dev, "lens"),
-                         table.stride(0) if n_seq > 1 else max_pages, max_pages, n_seq, SP_CACHE_4BIT if four else SP_CACHE_BF16,
-                         n_pages, page_len, n_kv, d_head, 0)
-
 
 def sp_cache_append(pages, K, V, cu, table, lens, Q=None, inv_freq=None, neighbours=False, positions=None, q_out=None, k_out=None,
                     want_k=False, status=None, d_head=None):
@@ -802,62 +739,30 @@ def sp_cache_append(pages, K, V, cu, table, lens, Q=None, inv_freq=None, neighbo
     [N, n_heads * d_head]) turned by their positions on the way (see sp.h).  table int32 [n_seq, pages of a sequence], lens int32
     [n_seq] with these tokens.  inv_freq fp32 [turned / 2]: frequencies of the turned channels, None: nothing is turned; pairs are halves apart,
     or neighbours.  positions int32 [N]: others than the places.  q_out: where the turned queries go (Q itself: in place; allocated otherwise);
-    k_out, want_k: the turned keys, too.  pages None (then d_head is needed, table and V may be None): turns only.
+    k_out, want_k: the turned keys, too.  pages None (then d_head is needed, table, lens and V may be None): turns only.
     Returns the turned queries (None without Q), and with want_k or k_out (queries, keys)."""
-    dev = _current_device(K)
-    k = _rows(K, dev, "K")
-    N = k.rows
-    n_seq = cu.numel() - 1
-    if n_seq < 0:
-        raise ValueError("cu holds n_seq + 1 offsets")
-    if pages is not None:
-        c = pages.view(dev, table, lens)
-        if c.n_seq != n_seq:
-            raise ValueError("cu, table and lens are of one number of sequences")
-        d_head, v = c.d_head, _rows(V, dev, "V")
+    native = _native or _binding()
+    if pages is None:
+        code, q, k = native.cache_append(None, None, None, None, None, lens, K, None, cu, Q, inv_freq, neighbours, positions, q_out, k_out,
+                                         want_k, status, d_head)
     else:
-        if not d_head or k.cols % d_head:
-            raise ValueError("d_head of the keys")
-        c = SpKvCache(lens=_vector(lens, torch.int32, n_seq, dev, "lens"), n_seq=n_seq, n_kv_heads=k.cols // d_head, d_head=d_head)
-        v = SpMat()
-    q = qo = ko = SpMat()
-    n_heads = 0
-    if Q is not None:
-        if q_out is None:
-            q_out = torch.empty(N, Q.shape[1], dtype=Q.dtype, device=Q.device)
-        q, qo, n_heads = _rows(Q, dev, "Q"), _rows(q_out, dev, "q_out"), Q.shape[1] // max(d_head, 1)
-    if k_out is None and want_k:
-        k_out = torch.empty(N, k.cols, dtype=K.dtype, device=K.device)
-    if k_out is not None:
-        ko = _rows(k_out, dev, "k_out")
-    turned = 0 if inv_freq is None else 2 * inv_freq.numel()
-    args = SpCacheAppendArgs(q, k, v, qo, ko, _vector(cu, torch.int32, n_seq + 1, dev, "cu"),
-                             _vector(positions, torch.int32, N, dev, "positions"),
-                             _vector(inv_freq, torch.float32, turned // 2, dev, "inv_freq") if turned else None, n_heads, turned,
-                             int(bool(neighbours)), 0)
-    _check(lib().sp_cache_append(C.byref(c), C.byref(args), _vector(status, torch.int32, 4, dev, "status"),
-                                 torch._C._cuda_getCurrentRawStream(dev)), "sp_cache_append")
-    return (q_out, k_out) if k_out is not None else q_out
+        code, q, k = native.cache_append(pages.k, pages.v, pages.k_scale, pages.v_scale, table, lens, K, V, cu, Q, inv_freq, neighbours,
+                                         positions, q_out, k_out, want_k, status, None)
+    if code:
+        raise SpError(code, "sp_cache_append")
+    return q if k is None else (q, k)
 
 
 def sp_cache_read(pages, cu, table, lens, rows, dtype=torch.bfloat16, K=None, V=None, status=None):
     """The values that the cache holds for the last cu[s+1] - cu[s] tokens of every sequence (see sp.h).  Returns (K, V) [rows, n_kv_heads *
     d_head] of bf16 or fp32; rows of no sequence stay as they are (in buffers allocated here they are undefined)."""
-    dev = _current_device(pages.k)
-    c = pages.view(dev, table, lens)
-    if cu.numel() - 1 != c.n_seq:
-        raise ValueError("cu, table and lens are of one number of sequences")
-    cols = c.n_kv_heads * c.d_head
-    K, V = (torch.empty(rows, cols, dtype=dtype, device=pages.k.device) if t is None else t for t in (K, V))
-    _check(lib().sp_cache_read(C.byref(c), _vector(cu, torch.int32, c.n_seq + 1, dev, "cu"), C.byref(_rows(K, dev, "K")),
-                               C.byref(_rows(V, dev, "V")), _vector(status, torch.int32, 4, dev, "status"),
-                               torch._C._cuda_getCurrentRawStream(dev)), "sp_cache_read")
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError("values are read as bf16 or fp32")
+    code, K, V = (_native or _binding()).cache_read(pages.k, pages.v, pages.k_scale, pages.v_scale, table, lens, cu, rows, dtype is torch.float32,
+                                                    K, V, status)
+    if code:
+        raise SpError(code, "sp_cache_read")
     return K, V
-
-
-@functools.lru_cache(maxsize=256)
-def _cache_attention_bytes(*sizes):      # (a function of the sizes alone)
-    return int(lib().sp_cache_attention_bytes(*sizes))
 
 
 def sp_cache_attention(Q, pages, cu_q, table, lens, n_heads, causal=True, scale=None, max_keys=0, out=None, lse=None, want_lse=False,
@@ -865,25 +770,10 @@ def sp_cache_attention(Q, pages, cu_q, table, lens, n_heads, causal=True, scale=
     """sp_attention over the keys and values of a paged cache (see sp.h): rows [cu_q[s], cu_q[s+1]) of Q [Nq, n_heads * d_head] against the
     lens[s] tokens of sequence s.  max_keys: how many keys all sequences have together, at most, as the caller knows it (0: as many as the
     table holds); calls with many rows per sequence size their workspace by it.  Returns (O, lse or None)."""
-    dev = _current_device(Q)
-    c = pages.view(dev, table, lens)
-    q = _rows(Q, dev, "Q")
-    if out is None:
-        out = torch.empty(q.rows, q.cols, dtype=Q.dtype, device=Q.device)
-    if lse is None and want_lse:
-        lse = torch.empty(q.rows, n_heads, dtype=torch.float32, device=Q.device)
-    if scale is None:
-        scale = max(c.d_head, 1) ** -0.5
-    if ws is None:
-        need = _cache_attention_bytes(q.rows, c.n_seq, n_heads, c.n_kv_heads, c.d_head, q.dtype, c.max_pages, c.page_len, max_keys)
-        ws = _ws(need, Q.device) if need else None
-    elif ws.get_device() != dev:
-        _elsewhere(ws)
-    _check(lib().sp_cache_attention(C.byref(c), C.byref(q), _vector(cu_q, torch.int32, c.n_seq + 1, dev, "cu_q"), n_heads,
-                                    int(bool(causal)), scale, max_keys, C.byref(_rows(out, dev, "out")),
-                                    _vector(lse, torch.float32, q.rows * n_heads, dev, "lse"),
-                                    _vector(status, torch.int32, 4, dev, "status"), _ptr(ws), ws.nbytes if ws is not None else 0,
-                                    torch._C._cuda_getCurrentRawStream(dev)), "sp_cache_attention")
+    code, out, lse = (_native or _binding()).cache_attention(pages.k, pages.v, pages.k_scale, pages.v_scale, table, lens, Q, cu_q, n_heads, causal,
+                                                             scale, max_keys, out, lse, want_lse, ws, status)
+    if code:
+        raise SpError(code, "sp_cache_attention")
     return out, lse
 
 

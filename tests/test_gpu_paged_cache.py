@@ -481,7 +481,7 @@ def test_captured_and_on_other_streams(four):
     Q = torch.randn(2, heads * dh, generator=gen(23), device=DEV).to(BF)
     want = api.sp_cache_attention(Q, pages, cu, table, lens, heads)[0].clone()
     shorter = api.sp_cache_attention(Q, pages, cu, table, ints([1111, 64]), heads)[0].clone()
-    need = api._cache_attention_bytes(2, 2, heads, kv, dh, api.SP_BF16, table.shape[1], page, 0)
+    need = api.lib().sp_cache_attention_bytes(2, 2, heads, kv, dh, api.SP_BF16, table.shape[1], page, 0)
     graphs = []
     for _ in range(2):
         ws, out, s = torch.empty(need, dtype=torch.uint8, device=DEV), torch.empty_like(Q), torch.cuda.Stream()
