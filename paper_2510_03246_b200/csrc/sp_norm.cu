@@ -294,12 +294,12 @@ __device__ __forceinline__ void collect(Raw8<float>& r, const uint8_t* at, int s
   r.a = *reinterpret_cast<const float4*>(at);
   r.b = *reinterpret_cast<const float4*>(at + step);
 }
-// Rows in the ring: three of bf16 (24 KB each for 4096 columns; three blocks of an SM), two of wider types, one less where a row has 1024 threads.
+// Rows in the ring: four of bf16 (24 KB each for 4096 columns; two blocks of an SM), two of wider types; one where a row has 1024 threads, two of bf16.
 template <typename TY, typename TH, int TPR>
 struct GradRing {
   static constexpr int CHUNK = (int)(sizeof(TY) + 2 * sizeof(TH)) / 2;      // pieces of a chunk of eight values of dy, h and the stream's gradient
   static constexpr int PIECES = 2 * CHUNK;
-  static constexpr int STAGES = (CHUNK == 3 ? 3 : 2) - (TPR == 1024 ? 1 : 0);
+  static constexpr int STAGES = TPR == 1024 ? (CHUNK == 3 ? 2 : 1) : CHUNK == 3 && TPR <= 256 ? 4 : 2;
   static constexpr int THREADS = TPR < 256 ? 256 : TPR;
   static constexpr size_t SMEM = (size_t)STAGES * PIECES * THREADS * 16;
   static_assert(SMEM <= 200 * 1024, "shared memory of a block");
@@ -307,7 +307,7 @@ struct GradRing {
 // Blocks walk over rows, a grid apart; a thread keeps the weight's gradient of its columns in registers from row to row.
 constexpr int kGradChunks = 2;
 template <typename TY, typename TH, int TPR>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 && sizeof(TY) + sizeof(TH) == 4 ? 3 : 1) norm_grad_kernel(const GradParams p) {
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 && sizeof(TY) + sizeof(TH) == 4 ? 2 : 1) norm_grad_kernel(const GradParams p) {
   kernel_begin();
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kWarps = TPR / 32;      // rows of a block at a time, warps of a row
   __shared__ float s_red[2][kRows][kWarps][2];
@@ -347,8 +347,19 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 && sizeof(TY
     copies_end();
   };
   const int64_t stride = (int64_t)gridDim.x * kRows;
+  // (weights stay in registers, and the next row's rstd is on its way: beside the ring little of L1 is left, and waits for L2 in every row
+  // were what bounded this: 8192 x 4096 77 us with them)
+  float w[kGradChunks][8];
+#pragma unroll
+  for (int c = 0; c < kGradChunks; ++c) {
+    const int j = (c * TPR + t) * 8, n = p.d - j < 8 ? p.d - j : 8;
+    if (n > 0) weights8(p.w, j, n, p.w_vec != 0, w[c]);
+  }
+  const auto rstd_of = [&](int64_t row) { return p.rstd && row < p.T ? p.rstd[row] : 0.f; };
+  float next_rstd;
   {
     int64_t row = (int64_t)blockIdx.x * kRows + g;
+    next_rstd = rstd_of(row);
     for (int k = 0; k < R::STAGES - 1; ++k, row += stride) bring(k, row);
   }
   int flip = 0, stage = 0;
@@ -377,19 +388,19 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 && sizeof(TY
       }
     }
     stage = stage + 1 == R::STAGES ? 0 : stage + 1;
-    const float given = p.rstd && live ? p.rstd[row] : 0.f;
+    const float given = next_rstd;
+    next_rstd = rstd_of(row + stride);
     float s = 0.f, ss = 0.f;
 #pragma unroll
     for (int c = 0; c < kGradChunks; ++c) {
       const int j = (c * TPR + t) * 8, n = p.d - j < 8 ? p.d - j : 8;
       if (n <= 0) continue;
-      float w[8], u[8], x[8];
-      weights8(p.w, j, n, p.w_vec != 0, w);
+      float u[8], x[8];
       open8(a[c], u);
       open8(b[c], x);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        s = fmaf(u[i] * w[i], x[i], s);
+        s = fmaf(u[i] * w[c][i], x[i], s);
         if (!p.rstd) ss = fmaf(x[i], x[i], ss);
       }
     }
@@ -419,15 +430,14 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 256 && sizeof(TY
     for (int c = 0; c < kGradChunks; ++c) {
       const int j = (c * TPR + t) * 8, n = p.d - j < 8 ? p.d - j : 8;
       if (!live || n <= 0) continue;
-      float w[8], u[8], x[8], o[8];
-      weights8(p.w, j, n, p.w_vec != 0, w);
+      float u[8], x[8], o[8];
       open8(a[c], u);
       open8(b[c], x);
       open8(e[c], o);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         dw[c][i] = fmaf(u[i], x[i] * rstd, dw[c][i]);
-        const float v = rstd * fmaf(-x[i], f, u[i] * w[i]);
+        const float v = rstd * fmaf(-x[i], f, u[i] * w[c][i]);
         o[i] = p.dh ? v + o[i] : v;
       }
       if (n == 8) store8(dx + j, o);
@@ -522,12 +532,12 @@ inline int grad_threads(int64_t d) {
     if (chunks <= (int64_t)t * kGradChunks) return t;
   return 0;
 }
-// Blocks of the gradient: a wave of 1024 threads for every SM (148, so that the workspace depends on the sizes alone), and at least four
+// Blocks of the gradient: one wave, as many as are resident on 148 SMs (so that the workspace depends on the sizes alone), and at least four
 // rounds of rows for each block, so that its sums' way through memory stays small beside its rows.
 inline int64_t grad_blocks(int64_t T, int64_t d) {
   const int tpr = grad_threads(d);
   const int threads = tpr == 0 ? 512 : tpr < 256 ? 256 : tpr, rows = tpr > 0 && tpr < 256 ? 256 / tpr : 1;
-  const int64_t most = 148 * (1024 / threads), want = ceil_div(T, (int64_t)rows * 4);
+  const int64_t most = 148 * (threads > 256 ? 1 : 2), want = ceil_div(T, (int64_t)rows * 4);
   return want < most ? (want > 0 ? want : 1) : most;
 }
 
