@@ -21,8 +21,17 @@ namespace {
 constexpr int kAppendThreads = 256;
 constexpr int kMaxTurned = 128;
 
+// Quotients by numbers that the host knows: n / d = (n m) >> s with m = ceil(2^s / d), exact for n below 2^20 and d below 2^20 (s = 40).
+struct Divisor {
+  uint64_t m;
+  uint32_t d;
+};
+inline Divisor divisor(int64_t d) { return Divisor{((uint64_t(1) << 40) + (uint64_t)d - 1) / (uint64_t)d, (uint32_t)d}; }
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const Divisor& d) { return (uint32_t)((n * d.m) >> 40); }
+
 struct AppendParams {
   CacheView c;
+  Divisor q_row, q_head, k_row, k_head;    // chunks of a row (queries: pairs of chunks), of a head
   const void *q, *k, *v;
   void *q_out, *k_out;
   int64_t ldq, ldk, ldv, ldqo, ldko;
@@ -35,12 +44,10 @@ struct AppendParams {
   int32_t* status;
 };
 
-// eight values from p on, in fp32
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool vec, float (&x)[8]);
-template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, bool vec, float (&x)[8]) {
-  if (vec) {
+// Eight values from p on, in fp32.  VEC: rows start on 16 bytes in every matrix of the call; else `vec` tells of this one.
+template <bool VEC>
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, bool vec, float (&x)[8]) {
+  if (VEC || vec) {
     const uint4 w = *reinterpret_cast<const uint4*>(p);
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -53,9 +60,9 @@ __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, boo
     for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
   }
 }
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, bool vec, float (&x)[8]) {
-  if (vec) {
+template <bool VEC>
+__device__ __forceinline__ void load8(const float* p, bool vec, float (&x)[8]) {
+  if (VEC || vec) {
     const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
     x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
@@ -64,8 +71,9 @@ __device__ __forceinline__ void load8<float>(const float* p, bool vec, float (&x
     for (int i = 0; i < 8; ++i) x[i] = p[i];
   }
 }
+template <bool VEC>
 __device__ __forceinline__ void put8(__nv_bfloat16* p, bool vec, const float (&x)[8]) {
-  if (vec) {
+  if (VEC || vec) {
     uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -78,8 +86,9 @@ __device__ __forceinline__ void put8(__nv_bfloat16* p, bool vec, const float (&x
     for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(x[i]);
   }
 }
+template <bool VEC>
 __device__ __forceinline__ void put8(float* p, bool vec, const float (&x)[8]) {
-  if (vec) {
+  if (VEC || vec) {
     *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
     *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
   } else {
@@ -93,25 +102,30 @@ __device__ __forceinline__ float turned_low(float a, float b, float2 cs) { retur
 __device__ __forceinline__ float turned_high(float a, float b, float2 cs) { return __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y)); }
 
 // The eight lanes of a group hold eight channels each: their 4-bit numbers packed, and the group's scale and offset in lane 0 of the eight.
-// F: float where the values are what the caller gave, double for rotated ones (see above).
+// F: float where the values are what the caller gave, double for rotated ones (see above).  A quotient in fp32 decides unless it lies near
+// the border of two numbers; what is near takes in how far the values are from zero in steps, by which a difference in fp32 is off.
 template <typename F>
 __device__ __forceinline__ uint32_t four_bits(const F (&x)[8], uint32_t& pair) {
-  F lo = x[0], hi = x[0];
+  float f[8], lo, top = 0.f;
+  F hi = x[0];
   bool odd = false;                        // a NaN or an infinity
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    lo = x[i] < lo ? x[i] : lo;
+    f[i] = (float)x[i];
+    lo = i == 0 ? f[0] : fminf(lo, f[i]);
+    top = fmaxf(top, fabsf(f[i]));
     hi = x[i] > hi ? x[i] : hi;
-    odd |= !(x[i] - x[i] == (F)0);
+    odd |= !(fabsf(f[i]) < INFINITY);
   }
 #pragma unroll
   for (int w = 1; w < 8; w <<= 1) {
-    const F a = __shfl_xor_sync(0xffffffffu, lo, w), b = __shfl_xor_sync(0xffffffffu, hi, w);
-    lo = a < lo ? a : lo;
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, w));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+    const F b = __shfl_xor_sync(0xffffffffu, hi, w);
     hi = b > hi ? b : hi;
   }
   const uint32_t eight = (__ballot_sync(0xffffffffu, odd) >> (threadIdx.x & 24)) & 0xffu;
-  const float zero = __bfloat162float(__float2bfloat16_rn((float)lo));
+  const float zero = __bfloat162float(__float2bfloat16_rn(lo));      // (rounding keeps the order: the least value's)
   const float scale = __bfloat162float(__float2bfloat16_rn((float)(((double)hi - (double)zero) / 15.0)));
   if (eight != 0u) {                       // (the offset reads back as NaN whatever the numbers are)
     pair = 0x7fc07fc0u;
@@ -121,26 +135,34 @@ __device__ __forceinline__ uint32_t four_bits(const F (&x)[8], uint32_t& pair) {
   if (!(scale > 0.f)) return 0u;
   const bool tiny = scale < 1e-36f;        // its reciprocal, or a product with it, may leave the range of fp32
   const float inv = tiny ? 0.f : 1.f / scale;
+  const float near = tiny ? 1.f : fminf(1e-4f + top * inv * 0x1p-21f, 1.f);
+  constexpr float kRound = 12582912.f;     // 1.5 2^23: added, the sum's last bits are the whole number that is nearest
   uint32_t packed = 0u;
+  bool slow = false;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const F d = x[i] - (F)zero;            // (of two fp32 values: rounded once)
-    const float t = (float)d * inv;        // within 2^-22 of the quotient
-    float n = rintf(t);
-    if (tiny || fabsf(fabsf(t - n) - 0.5f) < 1e-4f) n = (float)rint(((double)x[i] - (double)zero) / (double)scale);
-    n = fminf(fmaxf(n, 0.f), 15.f);
-    packed |= (uint32_t)n << (4 * i);
+    const float t = fminf(fmaxf((f[i] - zero) * inv, 0.f), 15.f), u = t + kRound;
+    packed |= (__float_as_uint(u) & 15u) << (4 * i);
+    slow |= fabsf(fabsf(t - (u - kRound)) - 0.5f) < near;
+  }
+  if (slow) {
+    packed = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const double n = rint(((double)x[i] - (double)zero) / (double)scale);
+      packed |= (uint32_t)fmin(fmax(n, 0.0), 15.0) << (4 * i);
+    }
   }
   return packed;
 }
 
-// A block has `per_block` consecutive rows: first their places and angles, a warp to a row, then all their chunks of channels in one walk, two of a
-// thread's in flight.  (One row at a time spends most of a block's life on the way to its first chunk: the sequence, its length, its page, the
+// A block has `per_block` consecutive rows: first their places and angles, a warp to a row, then all their chunks of channels in one walk, several of
+// a thread's in flight.  (One row at a time spends most of a block's life on the way to its first chunk: the sequence, its length, its page, the
 // angles, one after the other; 10584 rows of 48 heads of 128 took 145 us.)
-constexpr int kMaxRows = 8;
+constexpr int kMaxRows = 4;
 // Angle f of a row: the k-th angles of consecutive chunks side by side, since the lanes of a warp read those.
 __device__ __forceinline__ int placed(int f) { return (f & 7) * (kMaxTurned / 16) + (f >> 3); }
-template <typename T, bool FOUR>
+template <typename T, bool FOUR, bool VEC>
 __global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const AppendParams p) {
   kernel_begin();
   __shared__ float2 s_turn[kMaxRows][kMaxTurned / 2];                       // cos, sin of a row's angles
@@ -178,83 +200,81 @@ __global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const A
   }
   __syncthreads();
   const int per_head = dh / 8, half8 = half / 8, turned8 = p.turned / 8;
-  // queries: a thread has both chunks of a pair, so that a row may be turned in its place
+  // queries: a thread has both chunks of a pair, so that a row may be turned in its place; two units of a thread in flight
   if (p.q) {
     const int apart = p.neighbours ? 0 : half8;                  // pairs of chunks: chunk and chunk + apart
-    const int units = per_head - apart, of_row = p.n_heads * units, all = rows * of_row;
+    const uint32_t all = (uint32_t)rows * p.q_row.d;
     const bool vec = p.q_vec != 0;
-#pragma unroll 2
-    for (int e = threadIdx.x; e < all; e += kAppendThreads) {
-      const int r = e / of_row, x_ = e - r * of_row, head = x_ / units, u = x_ - head * units;
-      if (s_page[r] == -2) continue;
-      const int chunk = u < apart || apart == 0 ? u : u + apart;
-      const T* src = reinterpret_cast<const T*>(p.q) + (row0 + r) * p.ldq + head * dh;
-      T* dst = reinterpret_cast<T*>(p.q_out) + (row0 + r) * p.ldqo + head * dh;
-      float a[8], b[8];
-      load8(src + 8 * chunk, vec, a);
-      if (chunk >= turned8) {
-        put8(dst + 8 * chunk, vec, a);
-      } else if (apart > 0) {
-        load8(src + 8 * (chunk + apart), vec, b);
-        float x[8], y[8];
+    for (uint32_t e0 = threadIdx.x; e0 < all; e0 += 2 * kAppendThreads) {
+      float a[2][8], b[2][8];
+      uint32_t r[2], head[2];
+      int chunk[2];
+      bool live[2];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float2 cs = s_turn[r][placed(8 * chunk + k)];
-          x[k] = turned_low(a[k], b[k], cs);
-          y[k] = turned_high(a[k], b[k], cs);
-        }
-        put8(dst + 8 * chunk, vec, x);
-        put8(dst + 8 * (chunk + apart), vec, y);
-      } else {
-        float x[8];
+      for (int y = 0; y < 2; ++y) {
+        const uint32_t e = e0 + y * kAppendThreads;
+        r[y] = quotient(e, p.q_row);
+        live[y] = e < all && s_page[r[y]] != -2;
+        const uint32_t x_ = e - r[y] * p.q_row.d;
+        head[y] = quotient(x_, p.q_head);
+        const int u = (int)(x_ - head[y] * p.q_head.d);
+        chunk[y] = u < apart || apart == 0 ? u : u + apart;
+        if (!live[y]) continue;
+        const T* src = reinterpret_cast<const T*>(p.q) + (row0 + r[y]) * p.ldq + head[y] * dh + 8 * chunk[y];
+        load8<VEC>(src, vec, a[y]);
+        if (apart > 0 && chunk[y] < turned8) load8<VEC>(src + half, vec, b[y]);
+      }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 cs = s_turn[r][placed(4 * chunk + k)];
-          x[2 * k] = turned_low(a[2 * k], a[2 * k + 1], cs);
-          x[2 * k + 1] = turned_high(a[2 * k], a[2 * k + 1], cs);
+      for (int y = 0; y < 2; ++y) {
+        if (!live[y]) continue;
+        T* dst = reinterpret_cast<T*>(p.q_out) + (row0 + r[y]) * p.ldqo + head[y] * dh + 8 * chunk[y];
+        if (chunk[y] >= turned8) {
+          put8<VEC>(dst, vec, a[y]);
+        } else if (apart > 0) {
+          float x[8], z[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float2 cs = s_turn[r[y]][placed(8 * chunk[y] + k)];
+            x[k] = turned_low(a[y][k], b[y][k], cs);
+            z[k] = turned_high(a[y][k], b[y][k], cs);
+          }
+          put8<VEC>(dst, vec, x);
+          put8<VEC>(dst + half, vec, z);
+        } else {
+          float x[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 cs = s_turn[r[y]][placed(4 * chunk[y] + k)];
+            x[2 * k] = turned_low(a[y][2 * k], a[y][2 * k + 1], cs);
+            x[2 * k + 1] = turned_high(a[y][2 * k], a[y][2 * k + 1], cs);
+          }
+          put8<VEC>(dst, vec, x);
         }
-        put8(dst + 8 * chunk, vec, x);
       }
     }
   }
-  // keys, then values: eight channels as they stand side by side in the cache, a key's partners read beside them
-  const int chunks = p.c.n_kv * per_head, sides = p.c.k ? 2 : 1, of_row = (chunks + 31) / 32 * 32;      // (groups of eight lanes stay together)
-#pragma unroll 2
-  for (int e = threadIdx.x; e < sides * rows * of_row; e += kAppendThreads) {
-    const bool value = e >= rows * of_row;                       // (the same in a warp, as is r)
-    const int f_ = value ? e - rows * of_row : e, r = f_ / of_row, x_ = f_ - r * of_row;
-    const int page = s_page[r];
+  // keys and values: eight channels as they stand side by side in the cache, a key's partners read beside them
+  const int chunks = p.c.n_kv * per_head;
+  const uint32_t all = (uint32_t)rows * p.k_row.d;               // (whole warps to a row: groups of eight lanes stay together)
+  for (uint32_t e = threadIdx.x; e < all; e += kAppendThreads) {
+    const uint32_t r = quotient(e, p.k_row);                     // (the same in a warp)
+    const int x_ = (int)(e - r * p.k_row.d), page = s_page[r];
     if (page == -2) continue;
     const bool live = x_ < chunks;
-    const int head = live ? x_ / per_head : 0, chunk = live ? x_ - head * per_head : 0;
-    const int64_t at = (int64_t)head * p.c.page_len + s_slot[r];      // (head, token) of the page
-    float a[8];
-    if (value) {
-      load8(reinterpret_cast<const T*>(p.v) + (row0 + r) * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, a);
-      if constexpr (FOUR) {
-        uint32_t pair;
-        const uint32_t packed = four_bits(a, pair);
-        if (page >= 0 && live) {
-          *reinterpret_cast<uint32_t*>(p.c.v + page * p.c.step + at * (dh / 2) + 4 * chunk) = packed;
-          if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.vs + page * p.c.scale_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
-        }
-      } else if (page >= 0 && live) {
-        put8(reinterpret_cast<__nv_bfloat16*>(p.c.v + page * p.c.step) + at * dh + 8 * chunk, true, a);
-      }
-      continue;
-    }
-    const T* src = reinterpret_cast<const T*>(p.k) + (row0 + r) * p.ldk + head * dh;
-    const bool vec = p.k_vec != 0;
-    load8(src + 8 * chunk, vec, a);
+    const int head = live ? (int)quotient((uint32_t)x_, p.k_head) : 0, chunk = live ? x_ - head * per_head : 0;
+    const bool turns = chunk < turned8, second = !p.neighbours && chunk >= half8;      // the pair's other value stands `half` before, or behind
+    const int64_t column = head * dh + 8 * chunk;
+    const T* src = reinterpret_cast<const T*>(p.k) + (row0 + r) * p.ldk + column;
+    float a[8], b[8], v[8];
+    load8<VEC>(src, p.k_vec != 0, a);
+    if (turns && !p.neighbours) load8<VEC>(second ? src - half : src + half, p.k_vec != 0, b);
+    if (p.c.k) load8<VEC>(reinterpret_cast<const T*>(p.v) + (row0 + r) * p.ldv + column, p.v_vec != 0, v);
     using F = typename std::conditional<FOUR, double, float>::type;
     F x[8];
-    if (chunk >= turned8) {
+    if (!turns) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = (F)a[k];
     } else {
-      float b[8];
-      const bool second = !p.neighbours && chunk >= half8;       // the pair's other value stands `half` channels before, or behind
-      if (!p.neighbours) load8(src + 8 * (second ? chunk - half8 : chunk + half8), vec, b);
       const int f0 = p.neighbours ? 4 * chunk : 8 * (second ? chunk - half8 : chunk);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -274,17 +294,27 @@ __global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const A
       float y[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) y[k] = (float)x[k];
-      put8(reinterpret_cast<T*>(p.k_out) + (row0 + r) * p.ldko + head * dh + 8 * chunk, vec, y);
+      put8<VEC>(reinterpret_cast<T*>(p.k_out) + (row0 + r) * p.ldko + column, p.k_vec != 0, y);
     }
+    if (!p.c.k) continue;
+    const int64_t at = (int64_t)head * p.c.page_len + s_slot[r];      // (head, token) of the page
     if constexpr (FOUR) {
-      uint32_t pair;
-      const uint32_t packed = four_bits(x, pair);
+      uint32_t pair_k, pair_v;
+      const uint32_t packed_k = four_bits(x, pair_k), packed_v = four_bits(v, pair_v);
       if (page >= 0 && live) {
-        *reinterpret_cast<uint32_t*>(p.c.k + page * p.c.step + at * (dh / 2) + 4 * chunk) = packed;
-        if (chunk % 8 == 0) *reinterpret_cast<uint32_t*>(p.c.ks + page * p.c.scale_step + (at * (dh / kCacheGroup) + chunk / 8) * 4) = pair;
+        const int64_t to = page * p.c.step + at * (dh / 2) + 4 * chunk;
+        *reinterpret_cast<uint32_t*>(p.c.k + to) = packed_k;
+        *reinterpret_cast<uint32_t*>(p.c.v + to) = packed_v;
+        if (chunk % 8 == 0) {
+          const int64_t pair_to = page * p.c.scale_step + (at * (dh / kCacheGroup) + chunk / 8) * 4;
+          *reinterpret_cast<uint32_t*>(p.c.ks + pair_to) = pair_k;
+          *reinterpret_cast<uint32_t*>(p.c.vs + pair_to) = pair_v;
+        }
       }
     } else if (page >= 0 && live) {
-      put8(reinterpret_cast<__nv_bfloat16*>(p.c.k + page * p.c.step) + at * dh + 8 * chunk, true, x);
+      const int64_t to = page * p.c.step + (at * dh + 8 * chunk) * 2;
+      put8<true>(reinterpret_cast<__nv_bfloat16*>(p.c.k + to), true, x);
+      put8<true>(reinterpret_cast<__nv_bfloat16*>(p.c.v + to), true, v);
     }
   }
 }
@@ -340,19 +370,19 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
         y[k] = fmaf((float)((b >> (4 * k)) & 15u), __uint_as_float(sb << 16), __uint_as_float(sb & 0xffff0000u));
       }
     } else {
-      load8(reinterpret_cast<const __nv_bfloat16*>(p.c.k + page * p.c.step) + at * dh + 8 * chunk, true, x);
-      load8(reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.step) + at * dh + 8 * chunk, true, y);
+      load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.k + page * p.c.step) + at * dh + 8 * chunk, true, x);
+      load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.step) + at * dh + 8 * chunk, true, y);
     }
-    put8(reinterpret_cast<T*>(p.k) + row * p.ldk + head * dh + 8 * chunk, p.k_vec != 0, x);
-    put8(reinterpret_cast<T*>(p.v) + row * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, y);
+    put8<false>(reinterpret_cast<T*>(p.k) + row * p.ldk + head * dh + 8 * chunk, p.k_vec != 0, x);
+    put8<false>(reinterpret_cast<T*>(p.v) + row * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, y);
     if (p.k_lo) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         x[k] = left_of(x[k]);
         y[k] = left_of(y[k]);
       }
-      put8(reinterpret_cast<__nv_bfloat16*>(p.k_lo) + row * p.ldk + head * dh + 8 * chunk, true, x);
-      put8(reinterpret_cast<__nv_bfloat16*>(p.v_lo) + row * p.ldv + head * dh + 8 * chunk, true, y);
+      put8<true>(reinterpret_cast<__nv_bfloat16*>(p.k_lo) + row * p.ldk + head * dh + 8 * chunk, true, x);
+      put8<true>(reinterpret_cast<__nv_bfloat16*>(p.v_lo) + row * p.ldv + head * dh + 8 * chunk, true, y);
     }
   }
 }
@@ -369,7 +399,7 @@ bool step_fits(int64_t step, int64_t page_bytes, int64_t unit, int32_t n_pages) 
 sp_status check_cache(const sp_kv_cache* c, bool pages) {
   if (!c) return SP_ERR_INVALID_ARG;
   if (c->kind != SP_CACHE_BF16 && c->kind != SP_CACHE_4BIT) return SP_ERR_INVALID_ARG;
-  if (c->n_kv_heads < 1 || c->n_kv_heads > (1 << 16) || c->d_head < 1 || c->n_seq < 0) return SP_ERR_SHAPE;
+  if (c->n_kv_heads < 1 || c->n_kv_heads > (1 << 12) || c->d_head < 1 || c->n_seq < 0) return SP_ERR_SHAPE;
   if (c->d_head > 128 || c->d_head % (c->kind == SP_CACHE_4BIT ? kCacheGroup : 16) != 0) return SP_ERR_UNSUPPORTED;
   if (!c->k) return pages ? SP_ERR_INVALID_ARG : SP_OK;
   const bool four = c->kind == SP_CACHE_4BIT;
@@ -442,7 +472,7 @@ sp_status sp_cache_append(const sp_kv_cache* cache, const sp_cache_append_args* 
     if (!a->Q.ptr || !a->Q_out.ptr) return SP_ERR_INVALID_ARG;
     if (a->Q.dtype != dt || a->Q_out.dtype != dt) return SP_ERR_DTYPE;
     const int64_t q = (int64_t)a->n_heads * cache->d_head;
-    if (a->n_heads < 1 || a->n_heads > (1 << 16)) return SP_ERR_SHAPE;
+    if (a->n_heads < 1 || a->n_heads > (1 << 12)) return SP_ERR_SHAPE;
     for (const sp_mat* m : {&a->Q, &a->Q_out})
       if (m->rows != N || m->cols != q || (N > 1 && m->ld < q)) return SP_ERR_SHAPE;
     if (a->Q.ptr == a->Q_out.ptr && N > 1 && a->Q.ld != a->Q_out.ld) return SP_ERR_INVALID_ARG;
@@ -472,12 +502,19 @@ sp_status sp_cache_append(const sp_kv_cache* cache, const sp_cache_append_args* 
   // as many rows to a block as leave four blocks for every SM
   const int64_t most = N / (4 * (int64_t)sm_count());
   p.per_block = most < 1 ? 1 : most < kMaxRows ? (int32_t)most : kMaxRows;
+  const int64_t per_head = cache->d_head / 8, units = per_head - (p.neighbours ? 0 : p.turned / 16);
+  p.q_head = divisor(units); p.q_row = divisor(queries ? units * a->n_heads : 1);
+  p.k_head = divisor(per_head); p.k_row = divisor((int64_t)align_up((size_t)(per_head * cache->n_kv_heads), 32));
   const dim3 grid((unsigned)ceil_div(N, (int64_t)p.per_block));
   const bool four = pages && cache->kind == SP_CACHE_4BIT;
-  const cudaError_t e = dt == SP_F32 ? (four ? launch(cache_append_kernel<float, true>, grid, dim3(kAppendThreads), 0, s, p)
-                                             : launch(cache_append_kernel<float, false>, grid, dim3(kAppendThreads), 0, s, p))
-                                     : (four ? launch(cache_append_kernel<__nv_bfloat16, true>, grid, dim3(kAppendThreads), 0, s, p)
-                                             : launch(cache_append_kernel<__nv_bfloat16, false>, grid, dim3(kAppendThreads), 0, s, p));
+  const bool vec = (!queries || p.q_vec) && p.k_vec && (!pages || p.v_vec);
+  const auto run = [&](auto t) {
+    using T = decltype(t);
+    const dim3 block(kAppendThreads);
+    if (vec) return four ? launch(cache_append_kernel<T, true, true>, grid, block, 0, s, p) : launch(cache_append_kernel<T, false, true>, grid, block, 0, s, p);
+    return four ? launch(cache_append_kernel<T, true, false>, grid, block, 0, s, p) : launch(cache_append_kernel<T, false, false>, grid, block, 0, s, p);
+  };
+  const cudaError_t e = dt == SP_F32 ? run(float()) : run(__nv_bfloat16());
   return e == cudaSuccess ? SP_OK : SP_ERR_CUDA;
 }
 
