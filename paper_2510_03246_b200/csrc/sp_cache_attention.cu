@@ -35,8 +35,9 @@ namespace sp {
 namespace {
 
 constexpr int kBlock = 16;
-constexpr int kPlanSeqs = 256;             // sequences of a launch
-constexpr int kLeastBlocks = 16;           // blocks of keys to a thread block, at least
+constexpr int kPlanSeqs = 128;             // sequences of a launch
+constexpr int kLead = 64;                  // what a tile and head costs beside its blocks of keys, in those
+constexpr int kLeastShare = 16;            // of the line of work to a thread block, at least
 constexpr int kMostCtas = 2 * 148;         // thread blocks of a launch, at most
 constexpr int kPlanThreads = 256;
 constexpr uint32_t kNoPage = 0xffffffffu;
@@ -197,8 +198,9 @@ __device__ __forceinline__ int32_t visible(int32_t nk, int64_t shift, int64_t to
   return (int32_t)max((int64_t)0, min((int64_t)nk, token + shift + 1));
 }
 
-// The work of a launch is a line of blocks: sequence by sequence, of each its tiles of rows, of each the key heads, of each the blocks of
-// keys.  `ctas` thread blocks share it in equal pieces: the b-th has [b total / ctas, (b + 1) total / ctas).  A tile and head that lies in several
+// The work of a launch is a line of blocks: sequence by sequence, of each its tiles of rows, of each the key heads, of each kLead that stand for
+// its queries and its output (some microseconds; without them 12 texts of 700 .. 11447 keys kept SMs busy for half of the time: 76 us, with 32 52, with
+// 64 46), and the blocks of keys.  `ctas` thread blocks share it in equal pieces: the b-th has [b total / ctas, (b + 1) total / ctas).  A tile and head that lies in several
 // thread blocks' pieces is joined from what they leave: the one that goes on in it from a predecessor at 2 b, the one that begins it at 2 b + 1.
 __device__ __forceinline__ int64_t first_of(int64_t b, int64_t total, int64_t ctas) { return b * total / ctas; }
 __device__ __forceinline__ int64_t cta_of(int64_t x, int64_t total, int64_t ctas) { return ((x + 1) * ctas - 1) / total; }
@@ -235,6 +237,7 @@ paged_rows_kernel(const PagedParams p) {
   constexpr int H = ROWS / 8, PARTS = sizeof(T) == 4 ? 3 : 1, G = FOUR ? R::G : 1, K16 = DH / 16, W = C::W;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int64_t s_first[kPlanSeqs + 1];
+  __shared__ Seq s_seq[kPlanSeqs];
   __shared__ int64_t s_word[W];
   __shared__ int s_bad;
   const int lane = threadIdx.x & 31, warp = uniform((int)threadIdx.x >> 5), g4 = lane >> 2, t4 = lane & 3;
@@ -247,7 +250,8 @@ paged_rows_kernel(const PagedParams p) {
     int64_t mine = 0, before;
     for (int i = i0; i < i1; ++i) {
       const Seq s = seq_at(p, p.s0 + i);
-      s_first[i] = (int64_t)tiles_of<ROWS>(p, s) * n_kv * blocks_of(s.nk);
+      s_seq[i] = s;
+      s_first[i] = (int64_t)tiles_of<ROWS>(p, s) * n_kv * (kLead + blocks_of(s.nk));
       mine += s_first[i];
     }
     const int64_t all = block_scan<W>(mine, s_word, before);
@@ -260,7 +264,7 @@ paged_rows_kernel(const PagedParams p) {
     __syncthreads();
   }
   const int64_t total = s_first[p.n_here];
-  const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / kLeastBlocks));
+  const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / kLeastShare));
   if (blockIdx.x == 0) {
     for (int i = threadIdx.x; i <= p.n_here; i += C::THREADS) p.plan[i] = s_first[i];
     if (threadIdx.x == 0) p.plan[p.n_here + 1] = ctas;
@@ -294,15 +298,17 @@ paged_rows_kernel(const PagedParams p) {
       else hi = mid;
     }
     const int32_t sq = p.s0 + lo;
-    const Seq it = seq_at(p, sq);
-    const uint32_t of_tile = (uint32_t)blocks_of(it.nk);
+    const Seq it = s_seq[lo];
+    const uint32_t all_blocks = (uint32_t)blocks_of(it.nk), of_tile = kLead + all_blocks;
     const int64_t from_seq = at - s_first[lo], unit_ = from_seq / of_tile;
-    const uint32_t block0 = (uint32_t)(from_seq - unit_ * of_tile);                  // of the tile and head
-    const uint32_t piece = (uint32_t)min((int64_t)(of_tile - block0), end - at);
-    at += piece;
+    const uint32_t from = (uint32_t)(from_seq - unit_ * of_tile);                    // of the tile and head
+    const uint32_t to = (uint32_t)min((int64_t)of_tile, from + end - at);
+    at += to - from;
+    if (to <= kLead) continue;                                                       // (no block of keys: the next thread block begins)
+    const uint32_t block0 = from > kLead ? from - kLead : 0u, piece = to - kLead - block0;
     const uint32_t tile = (uint32_t)(unit_ / n_kv);
     const int32_t head = (int32_t)(unit_ - (int64_t)tile * n_kv);
-    const bool cut = piece < of_tile;
+    const bool cut = piece < all_blocks;
     const int32_t slot_of = 2 * (int32_t)blockIdx.x + (block0 == 0 ? 1 : 0);
     const uint32_t g = (uint32_t)p.g, r0 = tile * ROWS;
     const int rows = (int)min((uint32_t)ROWS, (uint32_t)it.nq * g - r0);
@@ -314,6 +320,68 @@ paged_rows_kernel(const PagedParams p) {
     seen = uniform(seen);
     const int32_t blocks = seen > kb ? (seen - kb + kBlock - 1) / kBlock : 0;
     const int32_t own = blocks > warp ? (blocks - warp - 1) / W + 1 : 0;             // this warp's: warp, warp + W, ...
+
+    // ---- copies, on their way before the queries are read: block i of this warp starts at key kb + 16 (warp + W i).  Where 32 of them stand is looked up at a time, a lane each, in
+    // units of 128 bytes (kNoPage: there is none) and of 64 for the scales.
+    uint32_t places = kNoPage, scale_places = 0u;
+    uint32_t missing = 0u;                                       // a bit per block fetched, the last one lowest: it has no page
+    uint32_t into = ring + R::BYTES - R::STAGE;                  // the stage that was filled last
+    const int row_bytes = FOUR ? DH / 2 : 2 * dh;
+    const uint8_t *k_from = p.c.k + 16 * lane, *v_from = p.c.v + 16 * lane;
+    const uint8_t* s_from = FOUR ? (lane < 16 ? p.c.ks : p.c.vs) + 16 * (lane & 15) : nullptr;
+    const uint32_t s_to = 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * (lane & 15);
+    const bool has_scale = (lane & 15) < 4 * G;
+    const auto fetch = [&](int32_t i) {
+      missing <<= 1;
+      if (i < own) {
+        if ((i & 31) == 0) {
+          const int32_t at_ = i + lane, key = kb + kBlock * (warp + W * at_), entry = key / p.c.page_len;
+          const int32_t page = at_ < own ? page_of(p.c, sq, entry) : -1;
+          const int64_t token = (int64_t)head * p.c.page_len + (key - entry * p.c.page_len);
+          places = page < 0 ? kNoPage : (uint32_t)((page * p.c.step + token * row_bytes) >> 7);
+          if (FOUR) scale_places = (uint32_t)((page * p.c.scale_step + token * (4 * G)) >> 6);
+        }
+        const uint32_t place = __shfl_sync(0xffffffffu, places, i & 31);
+        into = into + R::STAGE == ring + R::BYTES ? ring : into + R::STAGE;
+        if (place == kNoPage) {                                  // (what stands in the stage only meets probabilities that are NaN)
+          missing |= 1u;
+          copies_end();
+          return;
+        }
+        const uint8_t *k = k_from + (uint64_t)place * 128u, *v = v_from + (uint64_t)place * 128u;
+        if constexpr (FOUR) {
+#pragma unroll
+          for (int e = 0; e < DH / 2; e += 32) {                 // pieces of the block's 16 rows
+            // 32-byte quarters of a 128-byte line change places with the line's number: the four keys of a half warp's read of K, and the
+            // four pairs of keys of a read of V, lie in different banks
+            copy16(into + 16 * e + piece_to, k + 16 * e);
+            copy16(into + R::TILE + 16 * e + piece_to, v + 16 * e);
+          }
+          const uint32_t scale_place = __shfl_sync(0xffffffffu, scale_places, i & 31);
+          if (has_scale) copy16(into + s_to, s_from + (uint64_t)scale_place * 64u);
+        } else if (dh == DH) {
+#pragma unroll
+          for (int e = 0; e < kBlock * R::PIECES; e += 32) {
+            const int row = e / R::PIECES + lane / R::PIECES;    // (a power of two, at most 32)
+            const uint32_t to = into + row * R::PITCH + 16 * (lane % R::PIECES);
+            copy16(to, k + 16 * e);
+            copy16(to + R::TILE, v + 16 * e);
+          }
+        } else {
+          const int per = dh / 8;
+#pragma unroll 1
+          for (int e = lane; e < kBlock * per; e += 32) {
+            const int row = e / per;
+            const uint32_t to = into + row * R::PITCH + 16 * (e - row * per);
+            copy16(to, k + 16 * (e - lane));
+            copy16(to + R::TILE, v + 16 * (e - lane));
+          }
+        }
+      }
+      copies_end();
+    };
+#pragma unroll
+    for (int i = 0; i < R::STAGES - 1; ++i) fetch(i);
 
     // ---- queries
     uint32_t q[H][PARTS][K16][2];
@@ -424,68 +492,6 @@ paged_rows_kernel(const PagedParams p) {
       }
     }
     bool found = false;                                          // bf16: non-finite values behind some row's mask
-
-    // ---- copies: block i of this warp starts at key kb + 16 (warp + W i).  Where 32 of them stand is looked up at a time, a lane each, in
-    // units of 128 bytes (kNoPage: there is none) and of 64 for the scales.
-    uint32_t places = kNoPage, scale_places = 0u;
-    uint32_t missing = 0u;                                       // a bit per block fetched, the last one lowest: it has no page
-    uint32_t into = ring + R::BYTES - R::STAGE;                  // the stage that was filled last
-    const int row_bytes = FOUR ? DH / 2 : 2 * dh;
-    const uint8_t *k_from = p.c.k + 16 * lane, *v_from = p.c.v + 16 * lane;
-    const uint8_t* s_from = FOUR ? (lane < 16 ? p.c.ks : p.c.vs) + 16 * (lane & 15) : nullptr;
-    const uint32_t s_to = 2 * R::TILE + (lane < 16 ? 0 : R::SCALES) + 16 * (lane & 15);
-    const bool has_scale = (lane & 15) < 4 * G;
-    const auto fetch = [&](int32_t i) {
-      missing <<= 1;
-      if (i < own) {
-        if ((i & 31) == 0) {
-          const int32_t at_ = i + lane, key = kb + kBlock * (warp + W * at_), entry = key / p.c.page_len;
-          const int32_t page = at_ < own ? page_of(p.c, sq, entry) : -1;
-          const int64_t token = (int64_t)head * p.c.page_len + (key - entry * p.c.page_len);
-          places = page < 0 ? kNoPage : (uint32_t)((page * p.c.step + token * row_bytes) >> 7);
-          if (FOUR) scale_places = (uint32_t)((page * p.c.scale_step + token * (4 * G)) >> 6);
-        }
-        const uint32_t place = __shfl_sync(0xffffffffu, places, i & 31);
-        into = into + R::STAGE == ring + R::BYTES ? ring : into + R::STAGE;
-        if (place == kNoPage) {                                  // (what stands in the stage only meets probabilities that are NaN)
-          missing |= 1u;
-          copies_end();
-          return;
-        }
-        const uint8_t *k = k_from + (uint64_t)place * 128u, *v = v_from + (uint64_t)place * 128u;
-        if constexpr (FOUR) {
-#pragma unroll
-          for (int e = 0; e < DH / 2; e += 32) {                 // pieces of the block's 16 rows
-            // 32-byte quarters of a 128-byte line change places with the line's number: the four keys of a half warp's read of K, and the
-            // four pairs of keys of a read of V, lie in different banks
-            copy16(into + 16 * e + piece_to, k + 16 * e);
-            copy16(into + R::TILE + 16 * e + piece_to, v + 16 * e);
-          }
-          const uint32_t scale_place = __shfl_sync(0xffffffffu, scale_places, i & 31);
-          if (has_scale) copy16(into + s_to, s_from + (uint64_t)scale_place * 64u);
-        } else if (dh == DH) {
-#pragma unroll
-          for (int e = 0; e < kBlock * R::PIECES; e += 32) {
-            const int row = e / R::PIECES + lane / R::PIECES;    // (a power of two, at most 32)
-            const uint32_t to = into + row * R::PITCH + 16 * (lane % R::PIECES);
-            copy16(to, k + 16 * e);
-            copy16(to + R::TILE, v + 16 * e);
-          }
-        } else {
-          const int per = dh / 8;
-#pragma unroll 1
-          for (int e = lane; e < kBlock * per; e += 32) {
-            const int row = e / per;
-            const uint32_t to = into + row * R::PITCH + 16 * (e - row * per);
-            copy16(to, k + 16 * (e - lane));
-            copy16(to + R::TILE, v + 16 * (e - lane));
-          }
-        }
-      }
-      copies_end();
-    };
-#pragma unroll
-    for (int i = 0; i < R::STAGES - 1; ++i) fetch(i);
 
     uint32_t stage = ring + R::BYTES - R::STAGE;
     for (int32_t i = 0; i < own; ++i) {
@@ -697,7 +703,6 @@ paged_rows_kernel(const PagedParams p) {
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int h = 0; h < H; ++h) {
-              float* acc = o[4 * gr + j][h];
               if constexpr (PARTS == 1) {
                 mma(o[4 * gr + j][h], a[j][0], a[j][1], a[j][2], a[j][3], pb[h][0][0], pb[h][0][1]);
               } else {
@@ -705,7 +710,7 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
                 for (int x = PARTS - 1; x >= 0; --x) mma(t, a[j][0], a[j][1], a[j][2], a[j][3], pb[h][x][0], pb[h][x][1]);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) acc[x] += t[x];
+                for (int x = 0; x < 4; ++x) o[4 * gr + j][h][x] += t[x];
               }
             }
         }
@@ -870,7 +875,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
   const int64_t total = p.plan[p.n_here], ctas = p.plan[p.n_here + 1];
   const int32_t of_tile = blocks_of(it.nk);
   const uint32_t rr = (uint32_t)(row - it.q0) * p.g + h % p.g;
-  const int64_t first = p.plan[sq - p.s0] + ((int64_t)(rr / ROWS) * p.c.n_kv + h / p.g) * of_tile;
+  const int64_t first = p.plan[sq - p.s0] + ((int64_t)(rr / ROWS) * p.c.n_kv + h / p.g) * (kLead + of_tile) + kLead;
   const int64_t b0 = cta_of(first, total, ctas), b1 = cta_of(first + of_tile - 1, total, ctas);
   if (b0 == b1 || b0 < 0 || b1 >= kMostCtas) return;      // (whole; outside only where cu_q decreases)
   const int parts = (int)(b1 - b0) + 1, dh = p.c.dh;
@@ -918,6 +923,8 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
     p.lse[(int64_t)row * p.n_heads + h] = bad ? NAN : total_w == 0.f ? -INFINITY : (ref + log2f(total_w)) * 0.6931471805599453f;
 }
 
+// Rows of a tile.  (Tiles of 24 or 32 read the cache once for the five drafted tokens of four heads of 64, and took as long: 46 us for 12 texts of
+// 700 .. 11447 keys, 8 heads, 16 bits.)
 inline int tile_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 8 * n_seq ? 8 : 16; }
 // Rows per sequence, on average, up to which the cache streams past tiles of 16 of them.
 inline bool paged_few_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 64 * n_seq; }
@@ -945,7 +952,7 @@ cudaError_t launch_rows(const PagedParams& p, cudaStream_t stream) {
   if (e != cudaSuccess) return e;
   // as many blocks as can be resident and may have work
   const int64_t seqs = p.n_here < p.Nq ? p.n_here : p.Nq, keys = (int64_t)p.c.max_pages * p.c.page_len;
-  const int64_t tiles = ((int64_t)p.Nq * p.g / ROWS + seqs) * p.c.n_kv, work = ceil_div(tiles * (ceil_div(keys, (int64_t)kBlock) + 1), (int64_t)kLeastBlocks);
+  const int64_t tiles = ((int64_t)p.Nq * p.g / ROWS + seqs) * p.c.n_kv, work = ceil_div(tiles * (kLead + 1 + ceil_div(keys, (int64_t)kBlock)), (int64_t)kLeastShare);
   int64_t ctas = (int64_t)sm_count() * C::CTAS;
   if (ctas > kMostCtas) ctas = kMostCtas;
   if (ctas > work) ctas = work;

@@ -532,12 +532,11 @@ inline int grad_threads(int64_t d) {
     if (chunks <= (int64_t)t * kGradChunks) return t;
   return 0;
 }
-// Blocks of the gradient: one wave, as many as are resident on 148 SMs (so that the workspace depends on the sizes alone), and at least four
-// rounds of rows for each block, so that its sums' way through memory stays small beside its rows.
+// Blocks of the gradient: one wave, as many as are resident on 148 SMs (so that the workspace depends on the sizes alone).
 inline int64_t grad_blocks(int64_t T, int64_t d) {
   const int tpr = grad_threads(d);
   const int threads = tpr == 0 ? 512 : tpr < 256 ? 256 : tpr, rows = tpr > 0 && tpr < 256 ? 256 / tpr : 1;
-  const int64_t most = 148 * (threads > 256 ? 1 : 2), want = ceil_div(T, (int64_t)rows * 4);
+  const int64_t most = 148 * (threads > 256 ? 1 : 2), want = ceil_div(T, (int64_t)rows);
   return want < most ? (want > 0 ? want : 1) : most;
 }
 
