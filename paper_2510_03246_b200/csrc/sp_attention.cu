@@ -354,7 +354,7 @@ Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_k
 
 }  // namespace
 
-sp_status attention_forward(const sp_attention_args* a, const void* k_lo, const void* v_lo, int32_t* status_dev, void* ws, size_t ws_bytes,
+sp_status attention_forward(const sp_attention_args* a, const uint32_t* half_tops, int32_t* status_dev, void* ws, size_t ws_bytes,
                             cudaStream_t s) {
   if (!a) return SP_ERR_INVALID_ARG;
   const int32_t dt = a->Q.dtype;
@@ -385,7 +385,7 @@ sp_status attention_forward(const sp_attention_args* a, const void* k_lo, const 
   // (a single row has no pitch: whatever stands there is not used)
   p.ldq = Nq > 1 ? a->Q.ld : a->Q.cols; p.ldk = Nk > 1 ? a->K.ld : a->K.cols;
   p.ldv = Nk > 1 ? a->V.ld : a->V.cols; p.ldo = Nq > 1 ? a->O.ld : a->O.cols;
-  p.k_lo = k_lo; p.v_lo = v_lo;
+  p.half_tops = half_tops;
   p.lse = a->lse;
   p.cu_q = a->cu_q; p.cu_k = a->cu_k;
   p.Nq = (int32_t)Nq; p.Nk = (int32_t)Nk;
@@ -402,7 +402,8 @@ sp_status attention_forward(const sp_attention_args* a, const void* k_lo, const 
   const bool tc = dt == SP_BF16 && attention_tc_supported(p);
   ProfScope prof(tc ? PK_GEMM_TC : PK_GEMM_SIMT, 0.0, 0.0, s);
   count_launch();
-  if (tc && attention_few_rows(Nq, p.g, a->n_seq)) {
+  if (half_tops && !tc) return SP_ERR_UNSUPPORTED;
+  if (tc && !half_tops && attention_few_rows(Nq, p.g, a->n_seq)) {
     const sp_status st = attention_rows(p, s);
     if (st != SP_OK) return st;
   } else if (tc) {
@@ -434,7 +435,7 @@ size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32
 }
 
 sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream) {
-  return sp::attention_forward(a, nullptr, nullptr, status_dev, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+  return sp::attention_forward(a, nullptr, status_dev, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -6,7 +6,6 @@ namespace sp {
 
 struct AttnParams {
   const void *q, *k, *v;
-  const void *k_lo, *v_lo;     // tcgen05 form: second bf16 parts of keys and values at their pitches, or null
   void* o;
   int64_t ldq, ldk, ldv, ldo;
   float* lse;
@@ -21,7 +20,17 @@ struct AttnParams {
   float* part_lse;             // [max_parts, Nq, n_heads]
   int32_t* status;
   long long wait_budget;
+  const uint32_t* half_tops;   // tcgen05 form: operands are fp16 in units (half_unit) of these maxima of queries, keys and values; null: bf16
 };
+
+// fp16 operands opened from a cache of 4 bits: values in units of the power of two that takes the largest one (its fp32 bits) to 2^14 .. 2^15.
+constexpr int kTopQ = 0, kTopK = 1, kTopV = 2;
+#ifdef __CUDACC__
+__device__ __forceinline__ int half_exponent(uint32_t top) { return top == 0u ? 0 : max((int)(top >> 23) - 127, -100) - 14; }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // e in -126 .. 127
+__device__ __forceinline__ float half_unit(uint32_t top) { return power_of_two(half_exponent(top)); }
+__device__ __forceinline__ float half_per_unit(uint32_t top) { return power_of_two(-half_exponent(top)); }
+#endif
 
 // One piece of work: a tile of a sequence's rows (queries x the heads that share a key head, head fastest), one key / value
 // head, one part of the keys.
@@ -123,8 +132,8 @@ cudaError_t attention_rows_f32(const AttnParams& p, cudaStream_t stream);
 // tcgen05 form (sp_attention_tc.cu): layouts that tensor maps can describe
 bool attention_tc_supported(const AttnParams& a);
 sp_status attention_tc(const AttnParams& a, cudaStream_t stream);
-// sp_attention; k_lo, v_lo (both or none): what its tcgen05 form adds to keys and values (the other forms read the first parts alone).
-sp_status attention_forward(const sp_attention_args* a, const void* k_lo, const void* v_lo, int32_t* status_dev, void* ws, size_t ws_bytes,
+// sp_attention (half null), or with fp16 operands in the places and pitches of Q, K and V, always by the tcgen05 form.
+sp_status attention_forward(const sp_attention_args* a, const uint32_t* half_tops, int32_t* status_dev, void* ws, size_t ws_bytes,
                             cudaStream_t stream);
 
 }  // namespace sp

@@ -22,9 +22,10 @@
 // What bounds it: per half and tile 128 exponentials a row (1024 cycles of the pipe that two warps share) between two products (1024 cycles
 // together for heads of 128).  One prompt of 8192, 32 heads of 128 on 8: 488 us after a pause, 531 in a row of calls (power cap); 16 documents of up to
 // 2048 tokens, 32 heads of 64 on 8: 167 and 156 us.  (Figures beside the steps below are of the kernel of that time.)
-// LO: keys and values in two bf16 parts that add up to them (opened from a cache of 4 bits): a key tile is four stages, the parts of K and those of V,
-// and S = Q K^T + Q K_lo^T, O += P V + P V_lo in one accumulator each.
+// HALF: operands opened from a cache of 4 bits, fp16 in units that its maxima give (AttnParams::half_tops): the same instructions with eight times
+// finer roundings, of P as well, whose reference leaves it 2^6 higher so that its small values keep theirs.
 // Waits for copies, the tensor core and other warps are bounded by a clock budget (SP_ERR_TIMEOUT through status).
+#include <cuda_fp16.h>
 #include <math.h>
 #include <string.h>
 
@@ -126,9 +127,9 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {      
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// bf16 operands, fp32 accumulator, 128 x n; B K-major or (V: keys are K, channels contiguous) MN-major
-__device__ __forceinline__ uint32_t instr_desc(bool b_kmajor, int n) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((b_kmajor ? 0u : 1u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+// bf16 or fp16 operands, fp32 accumulator, 128 x n; B K-major or (V: keys are K, channels contiguous) MN-major
+__device__ __forceinline__ uint32_t instr_desc(bool b_kmajor, int n, bool half) {
+  return (1u << 4) | (half ? 0u : (1u << 7) | (1u << 10)) | ((b_kmajor ? 0u : 1u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
 }
 
 struct TcAttnParams {
@@ -189,13 +190,13 @@ struct Brief {
 };
 constexpr int kBriefs = 8;             // more than the buffers of S: items between the issue of S and of P V
 
-// A walk over the jobs of an item, `per` stages of the ring to a key tile: key tile by key tile, the halves that see the tile.  (Half 1 has the later rows and sees no fewer tiles
+// A walk over the jobs of an item: key tile by key tile, the halves that see the tile.  (Half 1 has the later rows and sees no fewer tiles
 // than half 0; a tile of rows without half 1 is half 0 alone.)
 struct Cursor {
   Brief w;
   int i, h;                            // key tile, half
   int b = 0;                           // buffer of S and P
-  int stage = 0;                       // of the ring: the tile's K, behind it K's lower part (LO) and V
+  int stage = 0;                       // of the ring: the tile's K, its V is in the next one
   bool open = false;
   __device__ __forceinline__ void start(const Brief& of) {
     w = of;
@@ -206,25 +207,26 @@ struct Cursor {
   __device__ __forceinline__ int tiles() const { return w.n0 > w.n1 ? w.n0 : w.n1; }
   __device__ __forceinline__ bool first() const { return h == 0 || w.n0 <= i; }       // of the tile
   __device__ __forceinline__ bool last() const { return h == 1 || w.n1 <= i; }
-  __device__ __forceinline__ void advance(int bufs, int stages, int per) {
+  __device__ __forceinline__ void advance(int bufs, int stages) {
     b = b + 1 == bufs ? 0 : b + 1;
     if (!last()) {
       h = 1;
       return;
     }
     ++i;
-    stage = stage + per >= stages ? stage + per - stages : stage + per;
+    stage = stage + 2 >= stages ? stage + 2 - stages : stage + 2;
     h = w.n0 > i ? 0 : 1;
     open = i < tiles();
   }
 };
 
-template <int DH, bool LO>
+constexpr float kHalfLift = 6.f;       // HALF: P and its sums by 2^6
+
+template <int DH, bool HALF>
 __global__ void __launch_bounds__(kThreads, 1)
-attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                    const __grid_constant__ CUtensorMap tmKlo, const __grid_constant__ CUtensorMap tmVlo, const TcAttnParams p) {
+attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                    const __grid_constant__ CUtensorMap tmV, const TcAttnParams p) {
   using C = Cfg<DH>;
-  constexpr int PARTS = LO ? 2 : 1, PER = 2 * PARTS;      // stages of K or V of a key tile, of the tile
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort;
@@ -337,17 +339,15 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               for (int c = 0; c < C::CH; ++c)
                 tma_load_3d(q_smem + h * C::TILE + c * C::CHUNK, &tmQ, c * 64, it.head * p.gp, it.q0 + w.t0 + h * p.tokens, q_full);
           }
-          for (int i = 0; i < PER * n && ok; ++i) {
+          for (int i = 0; i < 2 * n && ok; ++i) {
             const int s = (int)(pos % C::STAGES);
             if (!mbar_wait(empty_bar(s), (pos / C::STAGES + 1) & 1u, abort_flag, budget)) { ok = false; break; }
-            const int tile = i / PER, part = i % PER;      // K, (its lower part,) V, (its lower part)
-            const bool v = part >= PARTS;
-            const CUtensorMap* map = v ? (LO && part == 3 ? &tmVlo : &tmV) : (LO && part == 1 ? &tmKlo : &tmK);
-            const uint32_t bar = v && w.edge(tile) ? edge_bar(s) : full_bar(s);
+            const bool v = i & 1;
+            const uint32_t bar = v && w.edge(i >> 1) ? edge_bar(s) : full_bar(s);
             mbar_expect_tx(bar, C::TILE);
   #pragma unroll
             for (int c = 0; c < C::CH; ++c)
-              tma_load_3d(ring + s * C::TILE + c * C::CHUNK, map, c * 64, kvh, it.k0 + w.kb + tile * kKeys, bar);
+              tma_load_3d(ring + s * C::TILE + c * C::CHUNK, v ? &tmV : &tmK, c * 64, kvh, it.k0 + w.kb + (i >> 1) * kKeys, bar);
             ++pos;
           }
         }
@@ -370,30 +370,17 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       // for both halves was better than a warp for each, whose instructions alternate (519 us, 189).
       bool ok = true;
       if (elect_one()) {
-        const uint32_t id_s = instr_desc(true, kKeys), id_o = instr_desc(false, DH);
+        const uint32_t id_s = instr_desc(true, kKeys, HALF), id_o = instr_desc(false, DH, HALF);
         uint32_t full_ph = 0, ready_ph = 0, p_ph = 0;    // phases of the barriers of a stage, of a buffer: a bit each
         int items_s = 0, items_v = 0;                    // items that the cursors have been given
         int ahead = 0;                                   // jobs whose S is issued and whose P V is not
-        bool end = false, issued = false, keys = false;  // keys: K of the next S (LO: both parts) has been waited for
-        bool upper = false;                              // LO: its upper part has
+        bool end = false, issued = false, keys = false;  // keys: K of the next S has been waited for
         Cursor cs, cv;
         long long t0 = 0;                                // since when nothing could be issued (0: something was)
         auto keys_there = [&] {                          // of the next S
           if (!cs.open) return false;
           if (!cs.first() || keys) return true;
           const int s = cs.stage;
-          if constexpr (LO) {
-            const int t = s + 1 == C::STAGES ? 0 : s + 1;
-            if (!upper) {
-              upper = mbar_test(full_bar(s), (full_ph >> s) & 1u);
-              if (upper) full_ph ^= 1u << s;
-            }
-            if (upper) {
-              keys = mbar_test(full_bar(t), (full_ph >> t) & 1u);
-              if (keys) full_ph ^= 1u << t;
-            }
-            return keys;
-          }
           keys = mbar_test(full_bar(s), (full_ph >> s) & 1u);
           if (keys) full_ph ^= 1u << s;
           return keys;
@@ -407,25 +394,15 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
             tc_mma_ss(d, a0 + off, b0 + off, id_s, k > 0);
           }
-          const int t = s + 1 == C::STAGES ? 0 : s + 1;
-          if constexpr (LO) {
-            const uint32_t b1 = desc_low(ring + t * C::TILE, 16);
-#pragma unroll
-            for (int k = 0; k < DH / 16; ++k) {
-              const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
-              tc_mma_ss(d, a0 + off, b1 + off, id_s, 1u);
-            }
-          }
           tc_commit_one(s_full(cs.h, cs.b));
           if (cs.last()) {
             tc_commit_one(empty_bar(s));
-            if constexpr (LO) tc_commit_one(empty_bar(t));
             if (cs.i + 1 == cs.tiles()) tc_commit_one(q_empty);
           }
           issued = true;
-          keys = upper = false;
+          keys = false;
           ++ahead;
-          cs.advance(C::BUFS, C::STAGES, PER);
+          cs.advance(C::BUFS, C::STAGES);
         };
         while (true) {
           if (!cs.open && !end && mbar_test(q_full, (uint32_t)items_s & 1u)) {
@@ -443,49 +420,35 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           if (ahead > 0) {
             if (!cv.open) cv.start(s_brief[items_v++ % kBriefs]);
             if (mbar_test(p_half(cv.b), (p_ph >> cv.b) & 1u)) {
-              const auto stage_of = [&](int part) { return cv.stage + part >= C::STAGES ? cv.stage + part - C::STAGES : cv.stage + part; };
-              const int s = stage_of(PARTS);
+              const int s = cv.stage + 1 == C::STAGES ? 0 : cv.stage + 1;
               if (cv.first()) {
-#pragma unroll
-                for (int x = 0; x < PARTS; ++x) {
-                  const int t = stage_of(PARTS + x);
-                  if (cv.i >= cv.w.edge) {
-                    ok = ok && mbar_wait(ready_bar(t), (ready_ph >> t) & 1u, abort_flag, budget);
-                    ready_ph ^= 1u << t;
-                  } else {
-                    ok = ok && mbar_wait(full_bar(t), (full_ph >> t) & 1u, abort_flag, budget);
-                    full_ph ^= 1u << t;
-                  }
+                if (cv.i >= cv.w.edge) {
+                  ok = mbar_wait(ready_bar(s), (ready_ph >> s) & 1u, abort_flag, budget);
+                  ready_ph ^= 1u << s;
+                } else {
+                  ok = mbar_wait(full_bar(s), (full_ph >> s) & 1u, abort_flag, budget);
+                  full_ph ^= 1u << s;
                 }
                 if (!ok) break;
               }
               // (P of a half's first key tile also says that its warps have read O of the item before)
               const uint32_t d = tmem + C::O_COL + C::O_COLS * cv.h, a0 = tmem + 128u * cv.b;
-              const uint32_t v0 = desc_low(ring + s * C::TILE, C::CHUNK), v1 = desc_low(ring + stage_of(PER - 1) * C::TILE, C::CHUNK);
+              const uint32_t v0 = desc_low(ring + s * C::TILE, C::CHUNK);
               tc_fence_after();
 #pragma unroll
-              for (int k = 0; k < kKeys / 32; ++k) {
-                tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, cv.i > 0 || k > 0);
-                if constexpr (LO) tc_mma_ts(d, a0 + 8u * k, v1 + 128u * k, id_o, 1u);
-              }
+              for (int k = 0; k < kKeys / 32; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, cv.i > 0 || k > 0);
               const bool more = keys_there();            // (before the wait: S of the next job follows the product at once)
               ok = mbar_wait(p_full(cv.b), (p_ph >> cv.b) & 1u, abort_flag, budget);
               p_ph ^= 1u << cv.b;
               if (!ok) break;
               tc_fence_after();
 #pragma unroll
-              for (int k = kKeys / 32; k < kKeys / 16; ++k) {
-                tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, 1u);
-                if constexpr (LO) tc_mma_ts(d, a0 + 8u * k, v1 + 128u * k, id_o, 1u);
-              }
+              for (int k = kKeys / 32; k < kKeys / 16; ++k) tc_mma_ts(d, a0 + 8u * k, v0 + 128u * k, id_o, 1u);
               --ahead;
               if (C::BUFS == 2 && more) issue_s();       // (with three: 184 us for the documents)
               tc_commit_one(pv_done(cv.h));
-              if (cv.last()) {
-                tc_commit_one(empty_bar(s));
-                if constexpr (LO) tc_commit_one(empty_bar(stage_of(PER - 1)));
-              }
-              cv.advance(C::BUFS, C::STAGES, PER);
+              if (cv.last()) tc_commit_one(empty_bar(s));
+              cv.advance(C::BUFS, C::STAGES);
               t0 = 0;
               continue;
             }
@@ -523,10 +486,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const int n = w.tiles();
         if (n == 0) continue;
         patience = budget + 20000ll * n;
-        for (int x = 0; x < PARTS * n && ok; ++x, pos += x % PARTS == 0 ? PER - PARTS + 1 : 1) {      // (pos: stages before K of the tile, plus x % PARTS)
-          const int i = x / PARTS;
+        for (int i = 0; i < n && ok; ++i, pos += 2) {
           if (!w.edge(i)) continue;
-          const int s = (int)((pos + PARTS) % C::STAGES);
+          const int s = (int)((pos + 1) % C::STAGES);
           const bool got = mbar_wait(edge_bar(s), (edge_ph >> s) & 1u, abort_flag, patience);
           edge_ph ^= 1u << s;
           ok = __all_sync(0xffffffffu, got);
@@ -540,14 +502,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   #pragma unroll
             for (int c = 0; c < C::CH; ++c)
   #pragma unroll
-              for (int y = 0; y < 8; ++y) {
-                uint4* at = reinterpret_cast<uint4*>(tile + c * C::CHUNK + j * 128 + ((y + j) & 7) * 16);
+              for (int x = 0; x < 8; ++x) {
+                uint4* at = reinterpret_cast<uint4*>(tile + c * C::CHUNK + j * 128 + ((x + j) & 7) * 16);
                 if (clear) {
                   *at = make_uint4(0u, 0u, 0u, 0u);
                 } else {
                   const uint4 v = *at;
-                  // a bf16 of all-ones exponent: its magnitude plus 0x80 reaches the sign bit
-                  auto mark = [](uint32_t u) { return ((u & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; };
+                  // a bf16 (fp16) of all-ones exponent: its magnitude plus 0x80 (0x400) reaches the sign bit
+                  auto mark = [](uint32_t u) { return ((u & 0x7fff7fffu) + (HALF ? 0x04000400u : 0x00800080u)) & 0x80008000u; };
                   if (mark(v.x) | mark(v.y) | mark(v.z) | mark(v.w)) {
                     auto fix = [&](uint32_t u) {
                       const uint32_t b = mark(u);
@@ -575,7 +537,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const int row = q * 32 + lane;                   // of the half, and lane of tensor memory
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     const uint32_t t_o = tmem + C::O_COL + C::O_COLS * h + lanes;
-    const float c = p.a.scale_log2;
+    const float c = HALF ? p.a.scale_log2 * half_unit(p.a.half_tops[kTopQ]) * half_unit(p.a.half_tops[kTopK]) : p.a.scale_log2;
     uint32_t s_ph = 0, pv_ph = 0, jobs = 0;          // (of a buffer: a bit each; jobs of the items before)
     bool ok = true;
     const uint64_t c2 = pack2(c, c);
@@ -656,7 +618,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               }
             }
           }
-          const float shift = r == -INFINITY ? 0.f : -r * c;
+          const float shift = r == -INFINITY ? 0.f : HALF ? fmaf(-r, c, kHalfLift) : -r * c;
           const uint64_t shift2 = pack2(shift, shift);
           uint64_t l2[2] = {pack2(l, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
@@ -670,8 +632,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               e0 = exp2_fast(e0);
               e1 = exp2_fast(e1);
               l2[j & 1] = add2(l2[j & 1], pack2(e0, e1));
-              const __nv_bfloat162 e = __floats2bfloat162_rn(e0, e1);
-              w16[j] = *reinterpret_cast<const uint32_t*>(&e);
+              if constexpr (HALF) {
+                const __half2 e = __floats2half2_rn(e0, e1);
+                w16[j] = *reinterpret_cast<const uint32_t*>(&e);
+              } else {
+                const __nv_bfloat162 e = __floats2bfloat162_rn(e0, e1);
+                w16[j] = *reinterpret_cast<const uint32_t*>(&e);
+              }
             }
             if (b < 2) tc_st16(t_s + 16u * b, w16);
             if (b == 2) {                            // the tensor core starts on the first half (stored while this quarter was computed)
@@ -705,8 +672,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const bool cut = p.a.part > 0 && it.nk > p.a.part;
       // no key seen: no reference r.  With one, 2^(c (x - r)) of the row's largest logit is 1 or more, unless c r is beyond fp32: then the row is NaN.
       const bool none = r == -INFINITY;
-      const float inv = l == 0.f ? NAN : 1.f / l;
-      const float lse2 = none ? -INFINITY : l == 0.f ? NAN : fmaf(r, c, log2f(l));
+      const float unit = HALF ? half_unit(p.a.half_tops[kTopV]) : 1.f;
+      const float inv = l == 0.f ? NAN : unit / l;
+      const float lse2 = none ? -INFINITY : l == 0.f ? NAN : fmaf(r, c, log2f(l) - (HALF ? kHalfLift : 0.f));
       __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.o) + out_row * p.a.ldo + (int64_t)head * p.a.dh;
       float* part = cut ? p.a.part_o + ((int64_t)it.c * p.a.Nq + out_row) * ((int64_t)p.a.n_heads * p.a.dh) + (int64_t)head * p.a.dh
                         : nullptr;
@@ -742,7 +710,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             for (int key = max(w.sure, w.kb); key < lim; ++key)
 #pragma unroll 1
               for (int j = 0; j < 32 && 32 * b + j < p.a.dh; ++j) {
-                const float v = __bfloat162float(V[((int64_t)it.k0 + key) * p.a.ldv + j]);
+                const float v = HALF ? __half2float(reinterpret_cast<const __half*>(V)[((int64_t)it.k0 + key) * p.a.ldv + j])
+                                     : __bfloat162float(V[((int64_t)it.k0 + key) * p.a.ldv + j]);
                 if (!(fabsf(v) < INFINITY)) {
 #pragma unroll
                   for (int y = 0; y < 32; ++y)
@@ -797,17 +766,17 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   }
 }
 
-template <int DH, bool LO>
-sp_status launch_tc(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmKlo, const CUtensorMap& tmVlo,
-                    const TcAttnParams& p, int64_t work, cudaStream_t stream) {
+template <int DH, bool HALF>
+sp_status launch_tc(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const TcAttnParams& p, int64_t work,
+                    cudaStream_t stream) {
   static PerDeviceOnce attr_once;
-  const auto kernel = attention_tc_kernel<DH, LO>;
+  const auto kernel = attention_tc_kernel<DH, HALF>;
   if (attr_once.run([&] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<DH>::SMEM);
       }) != cudaSuccess)
     return SP_ERR_CUDA;
   const dim3 grid((unsigned)(work < sm_count() ? work : sm_count()));
-  return launch(kernel, grid, dim3(kThreads), Cfg<DH>::SMEM, stream, tmQ, tmK, tmV, tmKlo, tmVlo, p) == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+  return launch(kernel, grid, dim3(kThreads), Cfg<DH>::SMEM, stream, tmQ, tmK, tmV, p) == cudaSuccess ? SP_OK : SP_ERR_CUDA;
 }
 
 }  // namespace
@@ -827,20 +796,15 @@ sp_status attention_tc(const AttnParams& a, cudaStream_t stream) {
   p.tokens = kRows / p.gp;
   p.heads = p.gp == 1 ? a.n_heads : a.n_kv;
   p.vec_out = a.ldo % 8 == 0 && (reinterpret_cast<uintptr_t>(a.o) & 15u) == 0;
-  CUtensorMap tmQ, tmK, tmV, tmKlo, tmVlo;
-  memset(&tmKlo, 0, sizeof(tmKlo));
-  memset(&tmVlo, 0, sizeof(tmVlo));
+  CUtensorMap tmQ, tmK, tmV;
   if (!make_map3(&tmQ, a.q, a.dh, a.n_heads, a.Nq, a.dh, a.ldq, 64, p.gp, p.tokens) ||
       !make_map3(&tmK, a.k, a.dh, a.n_kv, a.Nk, a.dh, a.ldk, 64, 1, kKeys) ||
-      !make_map3(&tmV, a.v, a.dh, a.n_kv, a.Nk, a.dh, a.ldv, 64, 1, kKeys) ||
-      (a.k_lo && (!make_map3(&tmKlo, a.k_lo, a.dh, a.n_kv, a.Nk, a.dh, a.ldk, 64, 1, kKeys) ||
-                  !make_map3(&tmVlo, a.v_lo, a.dh, a.n_kv, a.Nk, a.dh, a.ldv, 64, 1, kKeys))))
+      !make_map3(&tmV, a.v, a.dh, a.n_kv, a.Nk, a.dh, a.ldv, 64, 1, kKeys))
     return SP_ERR_CUDA;
   const int64_t tiles = min((int64_t)a.Nq / (2 * p.tokens) + a.n_seq, (int64_t)a.Nq);
   const int64_t work = tiles * p.heads * (a.part > 0 ? a.max_parts : 1);
-  if (a.k_lo)
-    return a.dh <= 64 ? launch_tc<64, true>(tmQ, tmK, tmV, tmKlo, tmVlo, p, work, stream) : launch_tc<128, true>(tmQ, tmK, tmV, tmKlo, tmVlo, p, work, stream);
-  return a.dh <= 64 ? launch_tc<64, false>(tmQ, tmK, tmV, tmKlo, tmVlo, p, work, stream) : launch_tc<128, false>(tmQ, tmK, tmV, tmKlo, tmVlo, p, work, stream);
+  if (a.half_tops) return a.dh <= 64 ? launch_tc<64, true>(tmQ, tmK, tmV, p, work, stream) : launch_tc<128, true>(tmQ, tmK, tmV, p, work, stream);
+  return a.dh <= 64 ? launch_tc<64, false>(tmQ, tmK, tmV, p, work, stream) : launch_tc<128, false>(tmQ, tmK, tmV, p, work, stream);
 }
 
 }  // namespace sp

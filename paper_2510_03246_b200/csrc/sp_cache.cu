@@ -9,10 +9,12 @@
 //
 // Both kernels are bound by memory (append: 16384 x (32 + 2 x 8) heads of 128: 200 MB in, 150 MB out); a thread has eight channels at a time,
 // 16 bytes of bf16, four bytes of a page in 4 bits; the eight lanes of a group find its bounds by shuffles.
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include <type_traits>
 
+#include "sp_attention.cuh"
 #include "sp_cache.cuh"
 
 namespace sp {
@@ -319,22 +321,26 @@ __global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const A
   }
 }
 
-// what rounding to bf16 leaves (nothing of a NaN, an infinity, or a value that rounds to one)
-__device__ __forceinline__ float left_of(float x) {
-  const float hi = __bfloat162float(__float2bfloat16_rn(x));
-  return fabsf(hi) < INFINITY ? x - hi : 0.f;
-}
-
 struct ReadParams {
   CacheView c;
   const int32_t* cu;
-  void *k, *v, *k_lo, *v_lo;
+  void *k, *v;
   int64_t ldk, ldv;
   int32_t rows, whole, k_vec, v_vec;
+  const uint32_t* tops;
   int32_t* status;
 };
+__device__ __forceinline__ void put8_half(__half* p, const float (&x)[8], float f) {
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 e = __floats2half2_rn(x[2 * i] * f, x[2 * i + 1] * f);
+    u[i] = *reinterpret_cast<const uint32_t*>(&e);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+}
 
-// a warp per row: eight channels of keys and of values at a time in every lane
+// a warp per row: eight channels of keys and of values at a time in every lane.  T of fp16: contiguous rows in units of tops.
 template <typename T, bool FOUR>
 __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
   kernel_begin();
@@ -346,9 +352,11 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
   const int32_t i = row - bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - (row - i);
   const int32_t length = p.c.lens[s], place = length - n + i;
   const int32_t entry = place >= 0 ? place / p.c.page_len : -1;
-  int32_t page = p.whole && n != length ? -1 : page_of(p.c, s, entry);
+  const int32_t page = p.whole && n != length ? -1 : page_of(p.c, s, entry);
   const int32_t slot = place - entry * p.c.page_len;
   if (page < 0 && lane == 0) report_status(p.status, SP_ERR_SHAPE, s, entry);
+  constexpr bool HALF = std::is_same<T, __half>::value;
+  const float fk = HALF ? half_per_unit(p.tops[kTopK]) : 1.f, fv = HALF ? half_per_unit(p.tops[kTopV]) : 1.f;
   const int dh = p.c.dh, per_head = dh / 8, chunks = p.c.n_kv * per_head;
 #pragma unroll 2
   for (int e = lane; e < chunks; e += 32) {
@@ -359,32 +367,86 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = y[k] = NAN;
     } else if constexpr (FOUR) {
-      const uint32_t a = *reinterpret_cast<const uint32_t*>(p.c.k + page * p.c.step + at * (dh / 2) + 4 * chunk);
-      const uint32_t b = *reinterpret_cast<const uint32_t*>(p.c.v + page * p.c.step + at * (dh / 2) + 4 * chunk);
-      const int64_t g = (at * (dh / kCacheGroup) + chunk / 8) * 4;
-      const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + page * p.c.scale_step + g);
-      const uint32_t sb = *reinterpret_cast<const uint32_t*>(p.c.vs + page * p.c.scale_step + g);
+      const int64_t from = page * p.c.step + at * (dh / 2) + 4 * chunk, g = page * p.c.scale_step + (at * (dh / kCacheGroup) + chunk / 8) * 4;
+      const uint32_t a = *reinterpret_cast<const uint32_t*>(p.c.k + from), b = *reinterpret_cast<const uint32_t*>(p.c.v + from);
+      const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + g), sb = *reinterpret_cast<const uint32_t*>(p.c.vs + g);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         x[k] = fmaf((float)((a >> (4 * k)) & 15u), __uint_as_float(sa << 16), __uint_as_float(sa & 0xffff0000u));
         y[k] = fmaf((float)((b >> (4 * k)) & 15u), __uint_as_float(sb << 16), __uint_as_float(sb & 0xffff0000u));
       }
     } else {
-      load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.k + page * p.c.step) + at * dh + 8 * chunk, true, x);
-      load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.v + page * p.c.step) + at * dh + 8 * chunk, true, y);
+      const int64_t from = page * p.c.step + (at * dh + 8 * chunk) * 2;
+      load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.k + from), true, x);
+      load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.v + from), true, y);
     }
-    put8<false>(reinterpret_cast<T*>(p.k) + row * p.ldk + head * dh + 8 * chunk, p.k_vec != 0, x);
-    put8<false>(reinterpret_cast<T*>(p.v) + row * p.ldv + head * dh + 8 * chunk, p.v_vec != 0, y);
-    if (p.k_lo) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        x[k] = left_of(x[k]);
-        y[k] = left_of(y[k]);
-      }
-      put8<true>(reinterpret_cast<__nv_bfloat16*>(p.k_lo) + row * p.ldk + head * dh + 8 * chunk, true, x);
-      put8<true>(reinterpret_cast<__nv_bfloat16*>(p.v_lo) + row * p.ldv + head * dh + 8 * chunk, true, y);
+    const int64_t column = head * dh + 8 * chunk;
+    if constexpr (HALF) {
+      put8_half(reinterpret_cast<__half*>(p.k) + row * p.ldk + column, x, fk);
+      put8_half(reinterpret_cast<__half*>(p.v) + row * p.ldv + column, y, fv);
+    } else {
+      put8<false>(reinterpret_cast<T*>(p.k) + row * p.ldk + column, p.k_vec != 0, x);
+      put8<false>(reinterpret_cast<T*>(p.v) + row * p.ldv + column, p.v_vec != 0, y);
     }
   }
+}
+
+// Largest finite |value| of the queries, and bounds 15 |scale| + |zero| of the keys and values of the rows that cache_open opens.  The first
+// `q_blocks` blocks take the queries, a row to a warp, the others keys.  (A maximum is the same in any order.)
+struct TopsParams {
+  CacheView c;
+  const int32_t* cu;
+  const __nv_bfloat16* q;
+  int64_t ldq, q_rows;
+  int32_t q_cols, q_blocks, rows;
+  uint32_t* tops;
+};
+__global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
+  kernel_begin();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float a = 0.f, b = 0.f;
+  const auto take = [](float& top, float v) {
+    if (v < INFINITY) top = fmaxf(top, v);                       // (not a NaN either)
+  };
+  const bool queries = (int)blockIdx.x < p.q_blocks;
+  if (queries) {
+    for (int64_t row = (int64_t)blockIdx.x * 8 + warp; row < p.q_rows; row += (int64_t)p.q_blocks * 8)
+      for (int j = lane; j < p.q_cols; j += 32) take(a, fabsf(__bfloat162float(p.q[row * p.ldq + j])));
+  } else {
+    const int blocks = (int)gridDim.x - p.q_blocks;
+    const int groups = p.c.n_kv * (p.c.dh / kCacheGroup), per_head = p.c.dh / kCacheGroup;
+    for (int32_t row = ((int)blockIdx.x - p.q_blocks) * 8 + warp; row < p.rows; row += blocks * 8) {
+      const int32_t s = sequence_of(p.cu, p.c.n_seq, p.rows, row);
+      if (s < 0) continue;
+      const int32_t place = row - bounded(p.cu[s], p.rows), entry = place / p.c.page_len, page = page_of(p.c, s, entry);
+      if (page < 0) continue;
+      for (int e = lane; e < groups; e += 32) {
+        const int head = e / per_head, g = e - head * per_head;
+        const int64_t at = page * p.c.scale_step + (((int64_t)head * p.c.page_len + place - entry * p.c.page_len) * per_head + g) * 4;
+        const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + at), sb = *reinterpret_cast<const uint32_t*>(p.c.vs + at);
+        take(a, fmaf(15.f, fabsf(__uint_as_float(sa << 16)), fabsf(__uint_as_float(sa & 0xffff0000u))));
+        take(b, fmaf(15.f, fabsf(__uint_as_float(sb << 16)), fabsf(__uint_as_float(sb & 0xffff0000u))));
+      }
+    }
+  }
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) {
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, w));
+    b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, w));
+  }
+  if (lane == 0) {
+    atomicMax(p.tops + (queries ? kTopQ : kTopK), __float_as_uint(a));
+    if (!queries) atomicMax(p.tops + kTopV, __float_as_uint(b));
+  }
+}
+__global__ void __launch_bounds__(256) queries_to_half_kernel(const __nv_bfloat16* q, int64_t ldq, int64_t rows, int32_t cols, __half* out,
+                                                              const uint32_t* tops) {
+  kernel_begin();
+  const float f = half_per_unit(tops[kTopQ]);
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+#pragma unroll 4
+  for (int j = threadIdx.x & 31; j < cols; j += 32) out[row * cols + j] = __float2half_rn(__bfloat162float(q[row * ldq + j]) * f);
 }
 
 bool rows_of_16(const void* ptr, int64_t ld, int32_t dtype, int64_t rows) {
@@ -429,24 +491,56 @@ CacheView cache_view(const sp_kv_cache* c) {
   return w;
 }
 
-cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
-                       bool whole, int32_t* status, cudaStream_t stream, void* K_lo, void* V_lo) {
+namespace {
+cudaError_t read_rows(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype, bool whole,
+                      const uint32_t* tops, int32_t* status, cudaStream_t stream) {
   ReadParams p = {};
   p.c = cache_view(c);
   p.cu = cu;
-  p.k = K; p.v = V; p.k_lo = K_lo; p.v_lo = V_lo; p.ldk = ldk; p.ldv = ldv;
+  p.k = K; p.v = V; p.ldk = ldk; p.ldv = ldv;
   p.rows = (int32_t)rows;
   p.whole = whole ? 1 : 0;
   p.k_vec = rows_of_16(K, ldk, dtype, rows); p.v_vec = rows_of_16(V, ldv, dtype, rows);
+  p.tops = tops;
   p.status = status;
   count_launch();
   const dim3 grid((unsigned)ceil_div(rows, (int64_t)8));
   const bool four = c->kind == SP_CACHE_4BIT;
+  if (tops) return launch(cache_read_kernel<__half, true>, grid, dim3(256), 0, stream, p);
   if (dtype == SP_F32)
     return four ? launch(cache_read_kernel<float, true>, grid, dim3(256), 0, stream, p)
                 : launch(cache_read_kernel<float, false>, grid, dim3(256), 0, stream, p);
   return four ? launch(cache_read_kernel<__nv_bfloat16, true>, grid, dim3(256), 0, stream, p)
               : launch(cache_read_kernel<__nv_bfloat16, false>, grid, dim3(256), 0, stream, p);
+}
+}  // namespace
+
+cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
+                       int32_t* status, cudaStream_t stream) {
+  return read_rows(c, cu, rows, K, V, ldk, ldv, dtype, false, nullptr, status, stream);
+}
+cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int32_t dtype, const uint32_t* tops, int32_t* status,
+                       cudaStream_t stream) {
+  const int64_t ld = (int64_t)c->n_kv_heads * c->d_head;
+  return read_rows(c, cu, rows, K, V, ld, ld, dtype, true, tops, status, stream);
+}
+cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, const sp_mat* Q, uint32_t* tops, cudaStream_t stream) {
+  TopsParams p = {};
+  p.c = cache_view(c);
+  p.cu = cu;
+  p.q = reinterpret_cast<const __nv_bfloat16*>(Q->ptr);
+  p.ldq = Q->ld; p.q_rows = Q->rows; p.q_cols = (int32_t)Q->cols;
+  p.rows = (int32_t)rows;
+  p.tops = tops;
+  const int64_t most = 2 * (int64_t)sm_count(), q = ceil_div(Q->rows, (int64_t)8), k = ceil_div(rows, (int64_t)8);
+  p.q_blocks = (int32_t)(q < most ? q : most);
+  count_launch();
+  return launch(cache_tops_kernel, dim3((unsigned)(p.q_blocks + (k < most ? k : most))), dim3(256), 0, stream, p);
+}
+cudaError_t queries_to_half(const sp_mat* Q, void* Q_half, const uint32_t* tops, cudaStream_t stream) {
+  count_launch();
+  return launch(queries_to_half_kernel, dim3((unsigned)ceil_div(Q->rows, (int64_t)8)), dim3(256), 0, stream,
+                reinterpret_cast<const __nv_bfloat16*>(Q->ptr), Q->ld, Q->rows, (int32_t)Q->cols, reinterpret_cast<__half*>(Q_half), tops);
 }
 
 }  // namespace sp
@@ -533,7 +627,7 @@ sp_status sp_cache_read(const sp_kv_cache* cache, const int32_t* cu, const sp_ma
   if (!cu || !K->ptr || !V->ptr || K->ptr == V->ptr) return SP_ERR_INVALID_ARG;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   ProfScope prof(PK_ELEMENTWISE, 0.0, 0.0, s);
-  return cache_read(cache, cu, N, K->ptr, V->ptr, K->ld, V->ld, K->dtype, false, status_dev, s) == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+  return cache_read(cache, cu, N, K->ptr, V->ptr, K->ld, V->ld, K->dtype, status_dev, s) == cudaSuccess ? SP_OK : SP_ERR_CUDA;
 }
 
 }  // extern "C"

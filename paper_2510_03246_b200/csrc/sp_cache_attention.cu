@@ -17,10 +17,10 @@
 // fp32 queries are three bf16 parts that add up to them, as are the probabilities' products with the scales; numbers are bf16 for both products, and
 // sums of 16 keys are added up outside the matrix unit.
 //
-// More rows open the pages into bf16 or fp32 rows in the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor
-// cores' rate, where this form would open them again for every 16 rows.  4 bits are opened into two bf16 parts: rounded to one,
-// logits were off by 2^-9 of |q| |k| (512 queries after 16384 keys, 32 heads of 128 on 8: results 4.2e-3 from the formula), and values of equal
-// scales by the same in every key, which no sum over keys takes away.
+// More rows open the pages into rows of the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor cores' rate, where this
+// form would open them again for every 16 rows.  4 bits are opened into fp16 in units of the call's maxima (bf16 queries alike): rounded to bf16,
+// results were 4.2e-3 from the formula (512 queries after 16384 keys, 32 heads of 128 on 8), 2.3e-3 as two bf16 parts each, in 312 us instead of
+// XXX, and values of equal scales all off by the same, which no sum over keys takes away.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>
@@ -976,8 +976,9 @@ cudaError_t launch_rows(const PagedParams& p, bool four, int rows, cudaStream_t 
 // cu_k of the opened keys: the lengths added up; a sequence that does not fit into max_keys (or has more tokens than its table) gets as many
 // rows as queries at most, which cache_read makes NaN: every query sees one of them.
 __global__ void __launch_bounds__(kPlanThreads) open_plan_kernel(const CacheView c, const int32_t* cu_q, int32_t Nq, int32_t max_keys, int32_t* cu_k,
-                                                             int32_t* status) {
+                                                             uint32_t* tops, int32_t* status) {
   kernel_begin();
+  if (tops && threadIdx.x < 3) tops[threadIdx.x] = 0u;
   __shared__ int64_t s_word[kPlanThreads / 32];
   int64_t at = 0, used = 0;               // rows given to the sequences before, and their keys
   for (int32_t s0 = 0; s0 < c.n_seq; s0 += kPlanThreads) {
@@ -1002,16 +1003,16 @@ __global__ void __launch_bounds__(kPlanThreads) open_plan_kernel(const CacheView
 
 struct OpenPlan {
   int64_t rows;
-  size_t cu_bytes, k_bytes, lo_bytes, attention;
-  size_t bytes() const { return cu_bytes + 2 * k_bytes + 2 * lo_bytes + attention; }
+  size_t cu_bytes, k_bytes, q_bytes, attention;
+  size_t bytes() const { return cu_bytes + 2 * k_bytes + q_bytes + attention; }
 };
-// (room for the second parts whatever the cache is: the workspace depends on the sizes that its call is given)
+// (room for the queries in fp16 whatever the cache is: the workspace depends on the sizes that its call is given)
 OpenPlan open_plan(int64_t Nq, int64_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype, int64_t max_keys) {
   OpenPlan r;
   r.rows = max_keys + Nq;
-  r.cu_bytes = align_up((size_t)(n_seq + 1) * 4, 256);
+  r.cu_bytes = align_up((size_t)(n_seq + 1) * 4 + 16, 256);      // and the three maxima behind the offsets
   r.k_bytes = align_up((size_t)r.rows * n_kv * dh * dtype_size(dtype), 256);
-  r.lo_bytes = dtype == SP_BF16 && dh % kCacheGroup == 0 ? r.k_bytes : 0;
+  r.q_bytes = dtype == SP_BF16 && dh % kCacheGroup == 0 ? align_up((size_t)Nq * n_heads * dh * 2, 256) : 0;
   r.attention = sp_attention_workspace_bytes(Nq, r.rows, (int32_t)n_seq, n_heads, n_kv, dh, dtype);
   return r;
 }
@@ -1089,17 +1090,19 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   const int64_t keys = keys_at_most(max_keys, n_seq, cache->max_pages, cache->page_len);
   const OpenPlan plan = open_plan(Nq, n_seq, n_heads, n_kv, dh, dt, keys);
   int32_t* cu_k = reinterpret_cast<int32_t*>(at);
-  uint8_t *K = at + plan.cu_bytes, *V = K + plan.k_bytes, *rest = V + plan.k_bytes + 2 * plan.lo_bytes;
-  const bool parts = dt == SP_BF16 && cache->kind == SP_CACHE_4BIT;
-  uint8_t *K_lo = parts ? V + plan.k_bytes : nullptr, *V_lo = parts ? K_lo + plan.lo_bytes : nullptr;
+  uint8_t *K = at + plan.cu_bytes, *V = K + plan.k_bytes, *Qh = V + plan.k_bytes, *rest = Qh + plan.q_bytes;
   const int64_t kv = (int64_t)n_kv * dh;
+  const bool half = dt == SP_BF16 && cache->kind == SP_CACHE_4BIT;
+  uint32_t* tops = half ? reinterpret_cast<uint32_t*>(cu_k + n_seq + 1) : nullptr;
   count_launch();
-  if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, status_dev) !=
-          cudaSuccess ||
-      cache_read(cache, cu_k, plan.rows, K, V, kv, kv, dt, true, status_dev, s, K_lo, V_lo) != cudaSuccess)
+  if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, tops, status_dev) !=
+      cudaSuccess)
     return SP_ERR_CUDA;
+  if (half && (cache_tops(cache, cu_k, plan.rows, Q, tops, s) != cudaSuccess || queries_to_half(Q, Qh, tops, s) != cudaSuccess))
+    return SP_ERR_CUDA;
+  if (cache_open(cache, cu_k, plan.rows, K, V, dt, tops, status_dev, s) != cudaSuccess) return SP_ERR_CUDA;
   sp_attention_args a = {};
-  a.Q = *Q;
+  a.Q = half ? sp_mat{Qh, dt, 0, Nq, cols, cols} : *Q;
   a.O = *O;
   a.K = sp_mat{K, dt, 0, plan.rows, kv, kv};
   a.V = sp_mat{V, dt, 0, plan.rows, kv, kv};
@@ -1107,7 +1110,7 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   a.lse = lse;
   a.n_seq = n_seq; a.n_heads = n_heads; a.n_kv_heads = n_kv; a.causal = causal;
   a.scale = scale;
-  return attention_forward(&a, K_lo, V_lo, status_dev, rest, plan.attention, s);
+  return attention_forward(&a, tops, status_dev, rest, plan.attention, s);
 }
 
 }  // extern "C"
