@@ -392,13 +392,13 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
 }
 
 // Largest finite |value| of the queries, and bounds 15 |scale| + |zero| of the keys and values of the rows that cache_open opens.  The first
-// `q_blocks` blocks take the queries, a row to a warp, the others keys.  (A maximum is the same in any order.)
+// `q_blocks` blocks take the queries, the others keys, a row to a warp.  (A maximum is the same in any order.)
 struct TopsParams {
   CacheView c;
   const int32_t* cu;
   const __nv_bfloat16* q;
   int64_t ldq, q_rows;
-  int32_t q_cols, q_blocks, rows;
+  int32_t q_cols, q_blocks, q_vec, rows;
   uint32_t* tops;
 };
 __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
@@ -410,8 +410,14 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
   };
   const bool queries = (int)blockIdx.x < p.q_blocks;
   if (queries) {
-    for (int64_t row = (int64_t)blockIdx.x * 8 + warp; row < p.q_rows; row += (int64_t)p.q_blocks * 8)
-      for (int j = lane; j < p.q_cols; j += 32) take(a, fabsf(__bfloat162float(p.q[row * p.ldq + j])));
+    const int64_t chunks = p.q_rows * (p.q_cols / 8);            // (heads are whole chunks)
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < chunks; e += (int64_t)p.q_blocks * 256) {
+      const int64_t row = e / (p.q_cols / 8), j = e - row * (p.q_cols / 8);
+      float x[8];
+      load8<false>(p.q + row * p.ldq + 8 * j, p.q_vec != 0, x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) take(a, fabsf(x[k]));
+    }
   } else {
     const int blocks = (int)gridDim.x - p.q_blocks;
     const int groups = p.c.n_kv * (p.c.dh / kCacheGroup), per_head = p.c.dh / kCacheGroup;
@@ -439,14 +445,15 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
     if (!queries) atomicMax(p.tops + kTopV, __float_as_uint(b));
   }
 }
-__global__ void __launch_bounds__(256) queries_to_half_kernel(const __nv_bfloat16* q, int64_t ldq, int64_t rows, int32_t cols, __half* out,
+__global__ void __launch_bounds__(256) queries_to_half_kernel(const __nv_bfloat16* q, int64_t ldq, int64_t rows, int32_t cols, int32_t vec, __half* out,
                                                               const uint32_t* tops) {
   kernel_begin();
   const float f = half_per_unit(tops[kTopQ]);
-  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, row = e / (cols / 8), j = e - row * (cols / 8);
   if (row >= rows) return;
-#pragma unroll 4
-  for (int j = threadIdx.x & 31; j < cols; j += 32) out[row * cols + j] = __float2half_rn(__bfloat162float(q[row * ldq + j]) * f);
+  float x[8];
+  load8<false>(q + row * ldq + 8 * j, vec != 0, x);
+  put8_half(out + row * cols + 8 * j, x, f);
 }
 
 bool rows_of_16(const void* ptr, int64_t ld, int32_t dtype, int64_t rows) {
@@ -532,15 +539,17 @@ cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, co
   p.ldq = Q->ld; p.q_rows = Q->rows; p.q_cols = (int32_t)Q->cols;
   p.rows = (int32_t)rows;
   p.tops = tops;
-  const int64_t most = 2 * (int64_t)sm_count(), q = ceil_div(Q->rows, (int64_t)8), k = ceil_div(rows, (int64_t)8);
+  p.q_vec = rows_of_16(Q->ptr, Q->ld, SP_BF16, Q->rows);
+  const int64_t most = 8 * (int64_t)sm_count(), q = ceil_div(Q->rows * (Q->cols / 8), (int64_t)512), k = ceil_div(rows, (int64_t)8);
   p.q_blocks = (int32_t)(q < most ? q : most);
   count_launch();
   return launch(cache_tops_kernel, dim3((unsigned)(p.q_blocks + (k < most ? k : most))), dim3(256), 0, stream, p);
 }
 cudaError_t queries_to_half(const sp_mat* Q, void* Q_half, const uint32_t* tops, cudaStream_t stream) {
   count_launch();
-  return launch(queries_to_half_kernel, dim3((unsigned)ceil_div(Q->rows, (int64_t)8)), dim3(256), 0, stream,
-                reinterpret_cast<const __nv_bfloat16*>(Q->ptr), Q->ld, Q->rows, (int32_t)Q->cols, reinterpret_cast<__half*>(Q_half), tops);
+  return launch(queries_to_half_kernel, dim3((unsigned)ceil_div(Q->rows * (Q->cols / 8), (int64_t)256)), dim3(256), 0, stream,
+                reinterpret_cast<const __nv_bfloat16*>(Q->ptr), Q->ld, Q->rows, (int32_t)Q->cols,
+                (int32_t)rows_of_16(Q->ptr, Q->ld, SP_BF16, Q->rows), reinterpret_cast<__half*>(Q_half), tops);
 }
 
 }  // namespace sp

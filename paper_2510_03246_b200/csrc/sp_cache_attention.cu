@@ -13,7 +13,8 @@
 //   K: the byte of a number n is n / 512 as e4m3 (the values below the first power of two and above it lie equally close), so that a mask opens
 //   four of them for m16n8k32 of e4m3, a faster instruction too.  Queries are two e4m3 parts, eight bits of what a power of two per row takes to
 //   128 .. 255; what is lost lies 2^-17 and more below a row's largest value.
-//   V: number n becomes the bf16 16 + n (or 128 + n) by a shift and one logical operation, two at a time; what was added goes to the offsets.
+//   V: number n becomes the bf16 16 + n (or 128 + n) by a shift and one logical operation, two at a time; a second instruction with a constant takes
+//   what was added, and 8, away again.
 // fp32 queries are three bf16 parts that add up to them, as are the probabilities' products with the scales; numbers are bf16 for both products, and
 // sums of 16 keys are added up outside the matrix unit.
 //
@@ -126,8 +127,7 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   return r;
 }
 // The bf16 pair (k + n_i, k + n_{i + 4}) of a word of eight numbers.  The mantissa's last bit of 16 .. 31 is 1 / 8, so that with k = 16 a
-// number stands in bits 3 .. 6; number 0 stands in the lowest bits already, where k is 128 (kOpened).
-__device__ constexpr float kOpened[4] = {128.f, 16.f, 16.f, 16.f};
+// number stands in bits 3 .. 6; number 0 stands in the lowest bits already, where k is 128.
 template <int I>
 __device__ __forceinline__ uint32_t opened(uint32_t w) {
   if constexpr (I == 0) return (w & 0x000f000fu) | 0x43004300u;
@@ -476,7 +476,7 @@ paged_rows_kernel(const PagedParams p) {
       }
     }
     // O: 4 bits: channels 64 (j / 4) + 8 g4 + j % 4 (| + 4) of rows 2 t4 + (x & 1); bf16: channels 16 j + g4 (| + 8)
-    float o[K16][H][4], offset[H][G][2], plus[G][H][4], r[H][2], ref[H][2], most[H][2], l[H][2];
+    float o[K16][H][4], offset[H][G][2], r[H][2], ref[H][2], most[H][2], l[H][2];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
 #pragma unroll
@@ -488,7 +488,7 @@ paged_rows_kernel(const PagedParams p) {
         r[h][x] = most[h][x] = -INFINITY;                        // reference of the rows' exponents, the logit up to which it stays
         ref[h][x] = l[h][x] = 0.f;                               // r, 0 while there is none; this lane's part of the rows' sums
 #pragma unroll
-        for (int gr = 0; gr < G; ++gr) offset[h][gr][x] = plus[gr][h][x] = plus[gr][h][2 + x] = 0.f;
+        for (int gr = 0; gr < G; ++gr) offset[h][gr][x] = 0.f;
       }
     }
     bool found = false;                                          // bf16: non-finite values behind some row's mask
@@ -612,10 +612,7 @@ paged_rows_kernel(const PagedParams p) {
             }
             l[h][x] *= f[x];
 #pragma unroll
-            for (int gr = 0; gr < G; ++gr) {
-              offset[h][gr][x] *= f[x];
-              plus[gr][h][x] *= f[x];
-            }
+            for (int gr = 0; gr < G; ++gr) offset[h][gr][x] *= f[x];
           }
 #pragma unroll
           for (int j = 0; j < K16; ++j)
@@ -655,10 +652,9 @@ paged_rows_kernel(const PagedParams p) {
           for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              // (p s)^T goes into the product with the numbers opened to k + n; offset collects p times what belongs to a key whatever its
-              // number, plus the products' sum, from which k goes again.  bf16: a rounding of p s weighs the number's distance from the middle
-              // 7.5 alone, whose part is taken exactly (16 tokens after 2048 .. 31013 keys: 4.7e-3 from the formula without, 2.3e-3).
-              const float scale = low(pair[y][gr]), zero = fmaf(PARTS == 1 ? 7.5f : 8.f, scale, high(pair[y][gr]));
+              // (p s)^T goes into the product with n - 8, the rest into offset, so that a rounding of p s weighs a number's distance from the
+              // middle alone (16 tokens after 2048 .. 31013 keys: 4.7e-3 from the formula with n as it is).
+              const float scale = low(pair[y][gr]), zero = fmaf(8.f, scale, high(pair[y][gr]));
               float ps[2], pz[2];
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
@@ -695,15 +691,14 @@ paged_rows_kernel(const PagedParams p) {
             a[2][0] = opened_centred<2>(m0); a[2][1] = opened_centred<2>(m1); a[2][2] = opened_centred<2>(m2); a[2][3] = opened_centred<2>(m3);
             a[3][0] = opened_centred<3>(m0); a[3][1] = opened_centred<3>(m1); a[3][2] = opened_centred<3>(m2); a[3][3] = opened_centred<3>(m3);
           }
-          if constexpr (PARTS == 1) {                            // sums of the products' operand: a row of ones
-#pragma unroll
-            for (int h = 0; h < H; ++h) mma(plus[gr][h], 0x3f803f80u, 0u, 0x3f803f80u, 0u, pb[h][0][0], pb[h][0][1]);
-          }
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int h = 0; h < H; ++h) {
               if constexpr (PARTS == 1) {
+                // (what opening has added, and 8, goes block by block: at the end it would be hundreds of times what is left)
+                const uint32_t back = j == 0 ? 0xc308c308u : 0xc1c0c1c0u;      // -136, -24
+                mma(o[4 * gr + j][h], back, back, back, back, pb[h][0][0], pb[h][0][1]);
                 mma(o[4 * gr + j][h], a[j][0], a[j][1], a[j][2], a[j][3], pb[h][0][0], pb[h][0][1]);
               } else {
                 float t[4] = {0.f, 0.f, 0.f, 0.f};
@@ -778,9 +773,8 @@ paged_rows_kernel(const PagedParams p) {
             for (int w = 4; w < 32; w <<= 1) offset[h][gr][x] += __shfl_xor_sync(0xffffffffu, offset[h][gr][x], w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float part = PARTS == 1 ? fmaf(-(7.5f + kOpened[j]), plus[gr][h][x], offset[h][gr][x]) : offset[h][gr][x];
-              o[4 * gr + j][h][x] += part;
-              o[4 * gr + j][h][2 + x] += part;
+              o[4 * gr + j][h][x] += offset[h][gr][x];
+              o[4 * gr + j][h][2 + x] += offset[h][gr][x];
             }
           }
       }
