@@ -13,8 +13,9 @@
 //   K: the byte of a number n is n / 512 as e4m3 (the values below the first power of two and above it lie equally close), so that a mask opens
 //   four of them for m16n8k32 of e4m3, a faster instruction too.  Queries are two e4m3 parts, eight bits of what a power of two per row takes to
 //   128 .. 255; what is lost lies 2^-17 and more below a row's largest value.
-//   V: number n becomes the bf16 16 + n (or 128 + n) by a shift and one logical operation, two at a time; a second instruction with a constant takes
-//   what was added, and 8, away again.
+//   V: number n becomes the fp16 64 + n by a shift and one logical operation, two at a time; a second instruction with a constant takes 72 away
+//   again, so that n - 8 is left.  Probabilities times scales are fp16 as well, in units of a power of two that follows the scales (vunit): with bf16
+//   their roundings left 2.4e-3 of the result's norm (16 tokens after 2048 .. 31013 keys), with fp16 1.7e-3, the result's own.
 // fp32 queries are three bf16 parts that add up to them, as are the probabilities' products with the scales; numbers are bf16 for both products, and
 // sums of 16 keys are added up outside the matrix unit.
 //
@@ -97,6 +98,12 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_half(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -126,14 +133,14 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(addr) : "memory");
   return r;
 }
-// The bf16 pair (k + n_i, k + n_{i + 4}) of a word of eight numbers.  The mantissa's last bit of 16 .. 31 is 1 / 8, so that with k = 16 a
-// number stands in bits 3 .. 6; number 0 stands in the lowest bits already, where k is 128.
+// The fp16 pair (64 + n_i, 64 + n_{i + 4}) of a word of eight numbers: the mantissa's last bit of 64 .. 127 is 1 / 16, so that a number stands in
+// bits 4 .. 7, where number 1 stands already.
 template <int I>
 __device__ __forceinline__ uint32_t opened(uint32_t w) {
-  if constexpr (I == 0) return (w & 0x000f000fu) | 0x43004300u;
-  else return ((w >> (4 * I - 3)) & 0x00780078u) | 0x41804180u;
+  const uint32_t at = I == 0 ? w * 16u : w >> (I == 0 ? 0 : 4 * I - 4);
+  return (at & 0x00f000f0u) | 0x54005400u;
 }
-// The same with k = -8, for fp32: sums of larger numbers would round by more.
+// The same as bf16 and n - 8, for fp32: sums of larger numbers would round by more.
 template <int I>
 __device__ __forceinline__ uint32_t opened_centred(uint32_t w) {
   const uint32_t at = I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3), v = (at & 0x00780078u) | 0x41804180u;
@@ -167,6 +174,10 @@ __device__ __forceinline__ void split(float lo, float hi, uint32_t (&r)[PARTS]) 
       hi -= high(r[i]);
     }
   }
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  const __half2 e = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&e);
 }
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
@@ -475,8 +486,12 @@ paged_rows_kernel(const PagedParams p) {
         lim[h][x] = row < rows ? min(visible(it.nk, shift, (r0 + row) / g), seen) : seen;
       }
     }
+    // 4 bits, bf16: probabilities are taken 2^kLift higher, and O holds them in units of vunit, half of a power of two that no scale has passed yet.
+    // (fp16: at most 2^(8 + kLift) 4, and small ones keep ten bits down to 2^-20 of the reference.)
+    constexpr bool HALF = FOUR && PARTS == 1;
+    constexpr float kLift = HALF ? 5.f : 0.f;
     // O: 4 bits: channels 64 (j / 4) + 8 g4 + j % 4 (| + 4) of rows 2 t4 + (x & 1); bf16: channels 16 j + g4 (| + 8)
-    float o[K16][H][4], offset[H][G][2], r[H][2], ref[H][2], most[H][2], l[H][2];
+    float o[K16][H][4], offset[H][G][2], vunit = 0.f, per_vunit = 0.f, r[H][2], ref[H][2], most[H][2], l[H][2];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
 #pragma unroll
@@ -586,13 +601,48 @@ paged_rows_kernel(const PagedParams p) {
         __syncwarp();                                            // (keeps this a branch)
       }
       bool rise = false;
+      uint32_t pair_v[2][G];                                     // 4 bits: scales of V of keys g4 | + 8
 #pragma unroll
       for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           rise |= !(s[h][x] <= most[h][x & 1]);
         }
+      if constexpr (HALF) {
+        float top = 0.f;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int gr = 0; gr < G; ++gr) {
+            pair_v[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
+            if (!edge || kt + 8 * y + g4 < seen) top = fmaxf(top, fabsf(low(pair_v[y][gr])));      // (not of slots that hold nothing)
+          }
+        rise |= top > 2.f * vunit;
+      }
       if (__any_sync(0xffffffffu, rise)) {                       // seldom: the references follow the maxima of this block
+        if constexpr (HALF) {
+          float top = 0.f;
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int gr = 0; gr < G; ++gr) {
+              const float u = fabsf(low(pair_v[y][gr]));
+              if (u < INFINITY && kt + 8 * y + g4 < seen) top = fmaxf(top, u);
+            }
+#pragma unroll
+          for (int w = 1; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+          if (top > 2.f * vunit) {
+            const float now = __uint_as_float(min(max(__float_as_uint(top) >> 23, 20u), 240u) << 23), f = vunit / now;
+            vunit = now;
+            per_vunit = 1.f / now;
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+              for (int j = 0; j < K16; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[j][h][x] *= f;
+          }
+        }
 #pragma unroll
         for (int h = 0; h < H; ++h) {
           float f[2];
@@ -607,7 +657,8 @@ paged_rows_kernel(const PagedParams p) {
             const bool up = m != -INFINITY && !(m - r[h][x] <= 0.f);
             f[x] = up ? exp2_fast(r[h][x] - m) : 1.f;            // r = -infinity: 0
             if (up) {
-              r[h][x] = ref[h][x] = m;
+              r[h][x] = m;
+              ref[h][x] = m - kLift;
               most[h][x] = (m + 8.f) / to_log2[h][x];
             }
             l[h][x] *= f[x];
@@ -629,18 +680,20 @@ paged_rows_kernel(const PagedParams p) {
         }
       const uint32_t vtile = stage + R::TILE;
       if constexpr (FOUR) {
-        uint32_t pair[2][G];
+        if constexpr (!HALF) {
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+          for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int gr = 0; gr < G; ++gr) pair[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
-        // (0 times a scale is 0 unless that is a NaN or an infinity; read again here, so that this stays behind the branch)
+            for (int gr = 0; gr < G; ++gr) pair_v[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
+        }
+        // (0 times a scale, and what comes of it, is 0 unless it is beyond what the keys that are seen have; read again here, so that this stays behind
+        // the branch)
         bool odd_scales = false;
         if (edge) {
           for (int y = 0; y < 2; ++y)
             for (int gr = 0; gr < G; ++gr) {
               const uint32_t w = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
-              odd_scales |= !(fabsf(low(w)) < INFINITY) || !(fabsf(high(w)) < INFINITY);
+              odd_scales |= !(fabsf(low(w)) <= (HALF ? 2.f * vunit : 1e37f)) || !(fabsf(high(w)) < 1e38f);
             }
           odd_scales = __any_sync(0xffffffffu, odd_scales);
         }
@@ -654,11 +707,11 @@ paged_rows_kernel(const PagedParams p) {
             for (int y = 0; y < 2; ++y) {
               // (p s)^T goes into the product with n - 8, the rest into offset, so that a rounding of p s weighs a number's distance from the
               // middle alone (16 tokens after 2048 .. 31013 keys: 4.7e-3 from the formula with n as it is).
-              const float scale = low(pair[y][gr]), zero = fmaf(8.f, scale, high(pair[y][gr]));
+              const float scale = low(pair_v[y][gr]), zero = fmaf(8.f, scale, high(pair_v[y][gr]));
               float ps[2], pz[2];
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
-                ps[x] = s[h][2 * y + x] * scale;
+                ps[x] = s[h][2 * y + x] * (HALF ? scale * per_vunit : scale);
                 pz[x] = zero;
               }
               if constexpr (decltype(strict)::value) {                                      // whatever stands in a slot that the row does not see
@@ -669,7 +722,8 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
               for (int x = 0; x < 2; ++x) offset[h][gr][x] = fmaf(s[h][2 * y + x], pz[x], offset[h][gr][x]);
               uint32_t u[PARTS];
-              split<PARTS>(ps[0], ps[1], u);
+              if constexpr (HALF) u[0] = pack_half(ps[0], ps[1]);
+              else split<PARTS>(ps[0], ps[1], u);
 #pragma unroll
               for (int x = 0; x < PARTS; ++x) pb[h][x][y] = turned8x8(u[x]);
             }
@@ -696,10 +750,9 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
             for (int h = 0; h < H; ++h) {
               if constexpr (PARTS == 1) {
-                // (what opening has added, and 8, goes block by block: at the end it would be hundreds of times what is left)
-                const uint32_t back = j == 0 ? 0xc308c308u : 0xc1c0c1c0u;      // -136, -24
-                mma(o[4 * gr + j][h], back, back, back, back, pb[h][0][0], pb[h][0][1]);
-                mma(o[4 * gr + j][h], a[j][0], a[j][1], a[j][2], a[j][3], pb[h][0][0], pb[h][0][1]);
+                // (the 72 go block by block: at the end they would be hundreds of times what is left)
+                mma_half(o[4 * gr + j][h], 0xd480d480u, 0xd480d480u, 0xd480d480u, 0xd480d480u, pb[h][0][0], pb[h][0][1]);
+                mma_half(o[4 * gr + j][h], a[j][0], a[j][1], a[j][2], a[j][3], pb[h][0][0], pb[h][0][1]);
               } else {
                 float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -773,8 +826,9 @@ paged_rows_kernel(const PagedParams p) {
             for (int w = 4; w < 32; w <<= 1) offset[h][gr][x] += __shfl_xor_sync(0xffffffffu, offset[h][gr][x], w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              o[4 * gr + j][h][x] += offset[h][gr][x];
-              o[4 * gr + j][h][2 + x] += offset[h][gr][x];
+              const float f = HALF ? vunit : 1.f;
+              o[4 * gr + j][h][x] = fmaf(o[4 * gr + j][h][x], f, offset[h][gr][x]);
+              o[4 * gr + j][h][2 + x] = fmaf(o[4 * gr + j][h][2 + x], f, offset[h][gr][x]);
             }
           }
       }
@@ -846,7 +900,7 @@ paged_rows_kernel(const PagedParams p) {
         for (int x = 0; x < 4; ++x) store1(out + x, acc[x]);
       }
       if (d == 0) {
-        const float lse2 = sum == 0.f ? -INFINITY : base + log2f(sum);
+        const float lse2 = sum == 0.f ? -INFINITY : base + (log2f(sum) - kLift);
         if (cut) p.part_lse[slot_of * ROWS + row] = lse2;
         else if (p.lse) p.lse[out_row * p.n_heads + out_head] = lse2 == -INFINITY ? lse2 : lse2 * 0.6931471805599453f;
       }

@@ -530,3 +530,29 @@ def test_four_bits_lose_no_more_than_their_roundings(q_len, k_len):
         want[cu[s]:cu[s + 1]] = torch.einsum("agij,jad->iagd", torch.softmax(z, 3), V).flatten(1, 2)
     roundings = 2 if sum(q_len) * (heads // kv) <= 64 * len(q_len) else 3
     assert (got.double() - want.flatten(1)).norm() <= (roundings / 3) ** 0.5 * 2.0 ** -8 * want.norm()
+
+
+@pytest.mark.parametrize("q_len, k_len", [([1], [900]), ([3, 1], [40, 700]), ([200], [500])])
+def test_scales_of_very_different_sizes(q_len, k_len):
+    """Scales of V that grow a thousandfold on the way, and leftovers of any size in slots that hold no token of the text."""
+    heads, kv, dh, page = 4, 2, 64, 16
+    table, n_pages = table_for(k_len, page, 41)
+    pages = filled(n_pages, kv, page, dh, True, 42)
+    for s, n in enumerate(k_len):
+        for j in range(n):
+            pg, slot = int(table[s, j // page]), j % page
+            if j % 37 == 0:
+                pages.v_scale[pg, :, slot] *= 2.0 ** (10 * j / n) if j % 2 else 2.0 ** -9
+    want, want_lse = check_attention(q_len, k_len, heads, kv, dh, page, BF, True, pages=pages, table=table, seed=43)
+    check_attention(q_len, k_len, heads, kv, dh, page, F32, True, pages=pages, table=table, seed=43)
+    left = api.KvPages(*(x.clone() for x in (pages.k, pages.v, pages.k_scale, pages.v_scale)))
+    for s, n in enumerate(k_len):
+        for j in range(n, -(-n // page) * page):
+            pg, slot = int(table[s, j // page]), j % page
+            for x in (left.k_scale, left.v_scale):
+                x[pg, :, slot] = 3e38 if j % 2 else -2e38
+    for dtype in (BF, F32):
+        Q = torch.randn(sum(q_len), heads * dh, generator=gen(45), device=DEV).to(dtype)
+        a = api.sp_cache_attention(Q, pages, ints(offsets(q_len)), table, ints(k_len), heads, want_lse=True)
+        b = api.sp_cache_attention(Q, left, ints(offsets(q_len)), table, ints(k_len), heads, want_lse=True)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
