@@ -8,7 +8,8 @@ built from the library calls only (argument marshalling and loop control; all ar
 
 attention_head_outputs, prune_attention_module, kept_ffn_weights, ffn_forward and token_loss carry activations through (pruned)
 modules and score the model's predictions: they give a module its calibration input from the module before, and the
-perplexity of Section 4.
+perplexity of Section 4.  KvCache, cached_attention and layer_forward do the same token by token, or by chunks of prompts, with keys and values in a
+cache of pages (16 or 4 bits), so that a pruned model writes text.
 
 plan_distribute covers Steps 1 and 2 of the "-distribute" variant (importances from weight statistics, attention and
 MLP modules allocated separately by inverse weighting).
@@ -235,12 +236,15 @@ class _Status:
 
 
 def attention_head_outputs(X: torch.Tensor, Wqkv: torch.Tensor, cu: torch.Tensor, n_heads: int, n_kv_heads: int | None = None,
-                           bias: torch.Tensor | None = None, causal: bool = True, status: torch.Tensor | None = None) -> torch.Tensor:
+                           bias: torch.Tensor | None = None, causal: bool = True, status: torch.Tensor | None = None,
+                           inv_freq: torch.Tensor | None = None, neighbours: bool = False) -> torch.Tensor:
     """Concatenated head outputs H [N, n_heads * d_head] of an attention module over packed sequences (cu: int32 offsets [n_seq + 1]
     on the device, X [N, d] token-major): the input of its output projection, and what prune_attention_heads takes.
     Wqkv [(n_heads + 2 n_kv_heads) d_head, d]: the rows of W_Q, W_K, W_V one below the other, in X's dtype; bias fp32 or None.
     Rows of X before the first and behind the last sequence (padding; whatever stands there) have zero rows in H: nothing in sums over tokens.
-    Two library calls, and no probabilities in memory (sp_mha_init, which the auxiliary variables of Algorithm 2 start from, keeps
+    inv_freq (fp32, half as many as the channels of a head that are turned): queries and keys are turned by their position in their sequence,
+    pairs of channels halves apart, or neighbours (sp_cache_append).
+    Two or three library calls, and no probabilities in memory (sp_mha_init, which the auxiliary variables of Algorithm 2 start from, keeps
     n_seq * n_heads * T * T of them).  status: int32 [4] (api.new_status) that the calls report through; without one the function waits for them
     and raises SpError itself."""
     n_kv = n_heads if n_kv_heads is None else n_kv_heads
@@ -249,18 +253,22 @@ def attention_head_outputs(X: torch.Tensor, Wqkv: torch.Tensor, cu: torch.Tensor
         qkv = api.sp_linear(X, Wqkv, bias=bias, status=word)
         q, k = n_heads * d_head, n_kv * d_head
         H = torch.zeros(X.shape[0], q, dtype=X.dtype, device=X.device)
-        api.sp_attention(qkv[:, :q], qkv[:, q:q + k], qkv[:, q + k:q + 2 * k], cu, cu, n_heads, n_kv, causal=causal, out=H, status=word)
+        Q, K = qkv[:, :q], qkv[:, q:q + k]
+        if inv_freq is not None:
+            Q, K = api.sp_cache_append(None, K, None, cu, None, None, Q=Q, inv_freq=inv_freq, neighbours=neighbours, q_out=Q, want_k=True,
+                                       status=word, d_head=d_head)
+        api.sp_attention(Q, K, qkv[:, q + k:q + 2 * k], cu, cu, n_heads, n_kv, causal=causal, out=H, status=word)
     return H
 
 
 def prune_attention_module(X: torch.Tensor, Wqkv: torch.Tensor, W_O: torch.Tensor, cu: torch.Tensor, n_heads: int, k_heads: int,
                            rho: float = 0.1, token_chunk: int = 32768, bias: torch.Tensor | None = None, causal: bool = True,
-                           status: torch.Tensor | None = None):
+                           status: torch.Tensor | None = None, inv_freq: torch.Tensor | None = None, neighbours: bool = False):
     """Head pruning of an attention module from its input (every head with a key head of its own): the head outputs over the packed
     calibration sequences, the pre-trained module output Ypre = H W_O^T, then prune_attention_heads.  W_O fp32 [d, n_heads * d_head].
-    status as attention_head_outputs.  Returns (mask, W_O_new, scores, H, Ypre)."""
+    status, inv_freq and neighbours as attention_head_outputs.  Returns (mask, W_O_new, scores, H, Ypre)."""
     with _Status(status, X.device) as word:
-        H = attention_head_outputs(X, Wqkv, cu, n_heads, bias=bias, causal=causal, status=word)
+        H = attention_head_outputs(X, Wqkv, cu, n_heads, bias=bias, causal=causal, status=word, inv_freq=inv_freq, neighbours=neighbours)
         Ypre = api.sp_linear(H, W_O.to(X.dtype), status=word)
         mask, W_new, scores = prune_attention_heads(H, Ypre, W_O, n_heads, k_heads, rho, token_chunk, status=word)
     return mask, W_new, scores, H, Ypre
@@ -298,6 +306,145 @@ def ffn_forward(X: torch.Tensor, W1: torch.Tensor, W2: torch.Tensor, Wg: torch.T
         return api.sp_linear(A, W2, bias=b2, other=residual, status=word)
 
 
+class KvCache:
+    """Pages for the keys and values of the texts that `n_layers` attention modules work on, and who has which.  One page table serves all layers:
+    page p of a text is page p in each.  The bookkeeping is the host's (a step's lengths are known there); what the kernels read of it goes to the
+    device once per step, in one copy."""
+
+    def __init__(self, n_layers: int, n_pages: int, page_len: int, n_kv_heads: int, d_head: int, four_bits: bool = False, device="cuda"):
+        self.layers = [api.KvPages.empty(n_pages, n_kv_heads, page_len, d_head, four_bits, device) for _ in range(n_layers)]
+        self.page_len, self.device = page_len, device
+        self._free = list(range(n_pages - 1, -1, -1))
+        self._pages: dict[object, list[int]] = {}
+        self._tokens: dict[object, int] = {}
+
+    def __len__(self) -> int:
+        """Pages that no text has."""
+        return len(self._free)
+
+    def tokens(self, text) -> int:
+        return self._tokens.get(text, 0)
+
+    def close(self, text):
+        """The text's pages are free again (a text that has none: nothing to do)."""
+        self._free.extend(reversed(self._pages.pop(text, [])))
+        self._tokens.pop(text, None)
+
+    def step(self, texts, new_tokens) -> "CacheStep":
+        """Room for new_tokens[i] more tokens of texts[i] (any hashable names, each once; one that is new starts empty).  Nothing is taken where the
+        free pages do not suffice (MemoryError)."""
+        texts, new_tokens = list(texts), [int(n) for n in new_tokens]
+        if len(texts) != len(new_tokens) or len(set(texts)) != len(texts) or any(n < 0 for n in new_tokens):
+            raise ValueError("a number of tokens, not negative, for every text, and every text once")
+        after = [self.tokens(t) + n for t, n in zip(texts, new_tokens)]
+        need = [-(-a // self.page_len) - len(self._pages.get(t, ())) for t, a in zip(texts, after)]
+        if sum(need) > len(self._free):
+            raise MemoryError(f"{sum(need)} pages are needed, {len(self._free)} are free")
+        fresh = all(self.tokens(t) == 0 for t in texts)
+        for t, a, n in zip(texts, after, need):
+            self._pages.setdefault(t, []).extend(self._free.pop() for _ in range(n))
+            self._tokens[t] = a
+        width = max([len(self._pages[t]) for t in texts], default=0)
+        cu = [0]
+        for n in new_tokens:
+            cu.append(cu[-1] + n)
+        flat = cu + after
+        for t in texts:
+            flat += self._pages[t] + [-1] * (width - len(self._pages[t]))
+        flat = torch.tensor(flat, dtype=torch.int32)
+        if torch.device(self.device).type == "cuda":
+            flat = flat.pin_memory().to(self.device, non_blocking=True)
+        n = len(texts)
+        return CacheStep(flat[:n + 1], flat[n + 1:2 * n + 1], flat[2 * n + 1:].view(n, width), sum(a for a, k in zip(after, new_tokens) if k > 0), fresh)
+
+
+@dataclass
+class CacheStep:
+    """What the calls of one step read: rows [cu[s], cu[s+1]) are the new tokens of text s, which has lens[s] with them on the pages table[s]."""
+    cu: torch.Tensor            # int32 [n + 1]
+    lens: torch.Tensor          # int32 [n]
+    table: torch.Tensor         # int32 [n, pages]
+    keys: int                   # keys of all texts with new tokens
+    fresh: bool                 # no text had tokens before
+
+
+def cached_attention(qkv: torch.Tensor, pages: api.KvPages, step: CacheStep, n_heads: int, n_kv_heads: int, inv_freq: torch.Tensor | None = None,
+                     neighbours: bool = False, status: torch.Tensor | None = None) -> torch.Tensor:
+    """Concatenated head outputs [N, n_heads * d_head] of an attention module for the new tokens of a step, from its projections qkv [N, (n_heads +
+    2 n_kv_heads) d_head] (whose queries are turned in their place): keys and values go into the module's pages, and the queries attend to all that is
+    there.  Prompts of texts that were empty read their own keys and values as the projection left them, 4 bits or not.  Rows behind the step's last are
+    zero.  status as attention_head_outputs."""
+    d_head = qkv.shape[1] // (n_heads + 2 * n_kv_heads)
+    q, k = n_heads * d_head, n_kv_heads * d_head
+    Q, K, V = qkv[:, :q], qkv[:, q:q + k], qkv[:, q + k:q + 2 * k]
+    H = torch.zeros(qkv.shape[0], q, dtype=qkv.dtype, device=qkv.device)
+    with _Status(status, qkv.device) as word:
+        turned = api.sp_cache_append(pages, K, V, step.cu, step.table, step.lens, Q=Q, inv_freq=inv_freq, neighbours=neighbours, q_out=Q,
+                                     want_k=step.fresh, status=word)
+        if step.fresh:
+            api.sp_attention(Q, turned[1], V, step.cu, step.cu, n_heads, n_kv_heads, out=H, status=word)
+        else:
+            api.sp_cache_attention(Q, pages, step.cu, step.table, step.lens, n_heads, max_keys=step.keys, out=H, status=word)
+    return H
+
+
+def weights_8bit(W: torch.Tensor):
+    """(W8 float8_e4m3fn [out, in] with rows that start on 16 bytes, scale fp32 [out]): a projection's weight as sp_linear_e4m3 reads it, laid out
+    once."""
+    scale = W.float().abs().amax(1).clamp_min(1e-30) / 448.0
+    W8 = api.rows_of_16_bytes(*W.shape, torch.float8_e4m3fn, W.device)
+    W8.copy_((W.float() / scale[:, None]).clamp(-448.0, 448.0))
+    return W8, scale.contiguous()
+
+
+@dataclass
+class LayerWeights:
+    """One layer: norms, attention module and FFN module on their kept heads and channels.  Projections that read a norm may be held in 8 bits (pairs
+    of weights_8bit); the others are of the activations' dtype."""
+    norm_attn: torch.Tensor                 # fp32 [d]
+    wqkv: torch.Tensor | tuple              # [(n_heads + 2 n_kv_heads) d_head, d]
+    wo: torch.Tensor                        # [d, n_heads * d_head]
+    norm_ffn: torch.Tensor                  # fp32 [d]
+    up: torch.Tensor | tuple                # [k, d]
+    down: torch.Tensor                      # [d, k] (kept_ffn_weights)
+    gate: torch.Tensor | tuple | None       # [k, d]: silu(gate) * up, None: relu(up)
+    n_heads: int
+    n_kv_heads: int
+    inv_freq: torch.Tensor | None = None    # fp32, positions turn queries and keys
+    neighbours: bool = False
+    eps: float = 1e-5
+
+
+def layer_forward(x: torch.Tensor, h: torch.Tensor | None, w: LayerWeights, pages: api.KvPages, step: CacheStep,
+                  status: torch.Tensor | None = None):
+    """One layer for the new tokens of a step: x [N, d] is what the module before adds to the residual stream h [N, d] (None: x is the stream's
+    beginning).  Returns (x, h) of the same meaning, x the FFN module's output that is still to be added; the next layer's first norm adds it, or
+    sp_rms_norm(x, weight, residual=h) before the head.  h is not changed in its place.  status as attention_head_outputs."""
+    eight = torch.float8_e4m3fn
+    with _Status(status, x.device) as word:
+        def project(r: api.RmsNorm, weight, **kw):
+            if isinstance(weight, tuple):
+                return api.sp_linear_e4m3(r.Y, r.scale, *weight, out_dtype=x.dtype, status=word, **kw)
+            return api.sp_linear(r.Y, weight, status=word, **kw)
+
+        def norm(x, weight, h, reads):
+            if any(isinstance(m, tuple) != isinstance(reads[0], tuple) for m in reads):
+                raise ValueError("gate and up are both held in 8 bits, or neither")
+            # (a stream that begins is the first module's input itself)
+            return api.sp_rms_norm(x, weight, w.eps, residual=h, out_dtype=eight if isinstance(reads[0], tuple) else None)
+
+        r = norm(x, w.norm_attn, h, (w.wqkv,))
+        h = x if h is None else r.H
+        H = cached_attention(project(r, w.wqkv), pages, step, w.n_heads, w.n_kv_heads, w.inv_freq, w.neighbours, status=word)
+        r = norm(api.sp_linear(H, w.wo, status=word), w.norm_ffn, h, (w.up,) if w.gate is None else (w.up, w.gate))
+        if w.gate is None:
+            A = project(r, w.up, act=api.SP_LINEAR_RELU)
+        else:
+            A = project(r, w.up)
+            A = project(r, w.gate, act=api.SP_LINEAR_SILU, other=A, combine=api.SP_COMBINE_MUL, out=A)
+        return api.sp_linear(A, w.down, status=word), r.H
+
+
 @dataclass
 class TokenLoss:
     nll: float                          # sum of -log p over the scored tokens
@@ -305,6 +452,7 @@ class TokenLoss:
     logp: torch.Tensor                  # fp32 [N], 0 where not scored
     d_hidden: torch.Tensor | None       # gradient of nll / tokens, dtype of hidden
     d_W: torch.Tensor | None            # the same, fp32
+    d_norm: torch.Tensor | None = None  # of the norm before the head, fp32
 
     @property
     def perplexity(self) -> float:
@@ -317,13 +465,19 @@ class TokenLoss:
             return math.inf
 
 
-def token_loss(hidden: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor, token_chunk: int = 8192, with_grad: bool = False) -> TokenLoss:
+def token_loss(hidden: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor, token_chunk: int = 8192, with_grad: bool = False,
+               norm_weight: torch.Tensor | None = None, norm_eps: float = 1e-5) -> TokenLoss:
     """Negative log likelihood of the target tokens under logits = hidden W_lm^T, chunk by chunk (one chunk of logits in memory):
     the measure of Section 4 is its perplexity.  hidden [N, d], W_lm [V, d] of one dtype, to which the logits are rounded (bf16: half a step is 0.03
     of a logit between 8 and 16, 0.06 of one up to 32; log p is off by as much at the target, on average by far less); targets int64 [N], negative:
     not scored.  with_grad: also the gradient of the mean with respect to hidden and W_lm, written over the logits of each chunk and
-    multiplied from there."""
+    multiplied from there.  norm_weight (fp32 [d]): logits = sp_rms_norm(hidden, norm_weight, norm_eps) W_lm^T, hidden is the stream
+    after the last layer, and the gradients are those of it and of the weight."""
     N, d = hidden.shape
+    stream, normed = hidden, None
+    if norm_weight is not None:
+        normed = api.sp_rms_norm(stream, norm_weight, norm_eps, want_rstd=with_grad)
+        hidden = normed.Y
     V = W_lm.shape[0]
     tokens = int((targets >= 0).sum().item())
     logp = torch.empty(N, dtype=torch.float32, device=hidden.device)
@@ -344,8 +498,11 @@ def token_loss(hidden: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor, 
             api.sp_token_logprobs_grad(x, t, r.lse, g[:n], out=x)
             api.sp_gemm(x, W_lm, d_hidden[t0:t0 + n], use_tensor_cores=tc, status=status)
             api.sp_gemm(x, h, d_W, transA=True, beta=1.0, use_tensor_cores=tc, status=status)
+    d_norm = None
+    if with_grad and normed is not None:
+        d_hidden, d_norm = api.sp_rms_norm_grad(d_hidden, stream, norm_weight, normed.rstd, norm_eps)
     api.raise_status(status, "token of its chunk, or of a wait the block,")
-    return TokenLoss(-float(logp.double().sum().item()), tokens, logp, d_hidden, d_W)
+    return TokenLoss(-float(logp.double().sum().item()), tokens, logp, d_hidden, d_W, d_norm)
 
 
 def mha_outer_iterations(mod: api.MhaModule, head_mask: torch.Tensor, iters: int, params: api.MhaParams | None = None,
