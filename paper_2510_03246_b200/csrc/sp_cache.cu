@@ -392,7 +392,9 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
 }
 
 // Largest finite |value| of the queries, and bounds 15 |scale| + |zero| of the keys and values of the rows that cache_open opens.  The first
-// `q_blocks` blocks take the queries, the others keys, a row to a warp.  (A maximum is the same in any order.)
+// `q_blocks` blocks take the queries, the others keys: a warp takes one key head of 32 rows, a row to a lane, since a head's scales of the rows of a
+// page stand side by side; with a row to a warp every 8 bytes come in a sector of their own.  A block's maxima meet in shared memory: an atomic of
+// each warp queues at three words.  (A maximum is the same in any order.)
 struct TopsParams {
   CacheView c;
   const int32_t* cu;
@@ -419,17 +421,26 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
       for (int k = 0; k < 8; ++k) take(a, fabsf(x[k]));
     }
   } else {
-    const int blocks = (int)gridDim.x - p.q_blocks;
-    const int groups = p.c.n_kv * (p.c.dh / kCacheGroup), per_head = p.c.dh / kCacheGroup;
-    for (int32_t row = ((int)blockIdx.x - p.q_blocks) * 8 + warp; row < p.rows; row += blocks * 8) {
-      const int32_t s = sequence_of(p.cu, p.c.n_seq, p.rows, row);
-      if (s < 0) continue;
-      const int32_t place = row - bounded(p.cu[s], p.rows), entry = place / p.c.page_len, page = page_of(p.c, s, entry);
+    const int per_head = p.c.dh / kCacheGroup;
+    const int64_t items = ceil_div((int64_t)p.rows, (int64_t)32) * p.c.n_kv, step = ((int64_t)gridDim.x - p.q_blocks) * 8;
+    for (int64_t item = ((int64_t)blockIdx.x - p.q_blocks) * 8 + warp; item < items; item += step) {
+      const int64_t row = item / p.c.n_kv * 32 + lane;
+      const int head = (int)(item % p.c.n_kv);
+      if (row >= p.rows) continue;
+      int32_t s = 0;                                             // the last one that starts no later (cu[0] is 0)
+      for (int32_t len = p.c.n_seq; len > 1;) {
+        const int32_t half = len / 2;
+        const bool there = bounded(p.cu[s + half], p.rows) <= row;
+        s += there ? half : 0;
+        len = there ? len - half : half;
+      }
+      if (row >= bounded(p.cu[s + 1], p.rows)) continue;
+      const int32_t place = (int32_t)row - bounded(p.cu[s], p.rows), entry = place / p.c.page_len, page = page_of(p.c, s, entry);
       if (page < 0) continue;
-      for (int e = lane; e < groups; e += 32) {
-        const int head = e / per_head, g = e - head * per_head;
-        const int64_t at = page * p.c.scale_step + (((int64_t)head * p.c.page_len + place - entry * p.c.page_len) * per_head + g) * 4;
-        const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + at), sb = *reinterpret_cast<const uint32_t*>(p.c.vs + at);
+      const int64_t at = page * p.c.scale_step + ((int64_t)head * p.c.page_len + place - entry * p.c.page_len) * per_head * 4;
+#pragma unroll 2
+      for (int g = 0; g < per_head; ++g) {
+        const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + at + 4 * g), sb = *reinterpret_cast<const uint32_t*>(p.c.vs + at + 4 * g);
         take(a, fmaf(15.f, fabsf(__uint_as_float(sa << 16)), fabsf(__uint_as_float(sa & 0xffff0000u))));
         take(b, fmaf(15.f, fabsf(__uint_as_float(sb << 16)), fabsf(__uint_as_float(sb & 0xffff0000u))));
       }
@@ -440,9 +451,17 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
     a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, w));
     b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, w));
   }
+  __shared__ float s_top[2][8];
   if (lane == 0) {
-    atomicMax(p.tops + (queries ? kTopQ : kTopK), __float_as_uint(a));
-    if (!queries) atomicMax(p.tops + kTopV, __float_as_uint(b));
+    s_top[0][warp] = a;
+    s_top[1][warp] = b;
+  }
+  __syncthreads();
+  if (threadIdx.x < (queries ? 1 : 2)) {
+    float top = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, s_top[threadIdx.x][w]);
+    atomicMax(p.tops + (queries ? kTopQ : threadIdx.x == 0 ? kTopK : kTopV), __float_as_uint(top));
   }
 }
 __global__ void __launch_bounds__(256) queries_to_half_kernel(const __nv_bfloat16* q, int64_t ldq, int64_t rows, int32_t cols, int32_t vec, __half* out,
@@ -540,7 +559,8 @@ cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, co
   p.rows = (int32_t)rows;
   p.tops = tops;
   p.q_vec = rows_of_16(Q->ptr, Q->ld, SP_BF16, Q->rows);
-  const int64_t most = 8 * (int64_t)sm_count(), q = ceil_div(Q->rows * (Q->cols / 8), (int64_t)512), k = ceil_div(rows, (int64_t)8);
+  const int64_t most = 4 * (int64_t)sm_count(), q = ceil_div(Q->rows * (Q->cols / 8), (int64_t)1024);
+  const int64_t k = ceil_div(ceil_div(rows, (int64_t)32) * c->n_kv_heads, (int64_t)8);
   p.q_blocks = (int32_t)(q < most ? q : most);
   count_launch();
   return launch(cache_tops_kernel, dim3((unsigned)(p.q_blocks + (k < most ? k : most))), dim3(256), 0, stream, p);
