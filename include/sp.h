@@ -632,22 +632,25 @@ sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const sp_mat* W,
  * number.  K, V: [N, n_kv_heads * d_head], Q: [N, n_heads * d_head] or none (ptr NULL), one dtype (SP_BF16 or SP_F32), any ld, so that they may be column
  * slices of one matrix.  The first `turned` channels (a multiple of 16, 0 .. d_head) of every query and key head are turned by their position: pair
  * i of channels (i, i + turned / 2), with neighbours != 0 (2 i, 2 i + 1), by the angle position * inv_freq[i], (a, b) -> (a cos - b sin,
- * b cos + a sin); inv_freq: fp32 [turned / 2]; the angle, its cosine and sine and what goes to 4 bits in fp64, the rest by its steps in fp32.  position is p, or positions[row] (int32
- * [N]) where given.  Q_out [N, n_heads * d_head]: the turned queries, may be Q itself.  K_out: the turned keys, or none; not K itself.
+ * b cos + a sin); inv_freq: fp32 [turned / 2]; the angle, its cosine and sine and what goes to 4 bits in fp64, the rest by its steps in fp32.
+ * position is p, or positions[row] (int32 [N]) where given.  Q_out [N, n_heads * d_head]: the turned queries, may be Q itself.  K_out: the turned keys, or none; not K itself.
  * A cache without pages (k NULL; then lens may be NULL, p = i, and V is not read) only turns.  Rows of no sequence are left alone.
  * sp_cache_read: the values that the cache holds for the last n = cu[s+1] - cu[s] tokens of every sequence, rows as above, into K, V
  * [N, n_kv_heads * d_head] (SP_BF16: rounded, or SP_F32).
  * sp_cache_attention: sp_attention with the keys and values [0, lens[s]) of the cache: rows [cu_q[s], cu_q[s+1]) of Q and O, [Nq, n_heads * d_head], query i
  * of n_q sees keys j <= i + lens[s] - n_q (causal != 0) or all.  d_head and head h / g of a query head as there, a query without a visible key gets
  * O = 0 and lse = -infinity, rows of no sequence are left as they were, and what stands in slots that a query does not see does not reach it.
- * 4 bits or 16, the values are those the cache stands for, products in fp32 of them (SP_BF16: probabilities, or their products with the scales, are
- * rounded to bf16; with many rows per sequence the values themselves, too).  Softmax and sums in fp32.  Equal calls give equal bits.
- * Many rows per sequence (more than 64 queries x heads of a key head, on average) open the pages in the workspace: max_keys tells how many keys all
- * sequences with queries have at most (0: as many as the table holds); sequences that do not fit are reported like tokens without a page.
+ * 4 bits or 16, the values are those that the cache stands for.  Softmax and sums in fp32.  Roundings: SP_F32 none but those of fp32 products and
+ * sums.  SP_BF16 with 16 bits: probabilities to bf16.  SP_BF16 with 4 bits: probabilities times scales to fp16; queries (2^-16 of a row's
+ * largest value is kept at least); with many rows probabilities, queries and opened values to fp16 in units of powers of two that the largest of the
+ * call sets (values below 2^-28 of that lose bits).  Equal calls give equal bits.
+ * Many bf16 rows per sequence (more than 32 to 128 queries x heads of a key head, on average) open the pages in the workspace: max_keys tells how
+ * many keys all sequences with queries have at most (0: as many as the table holds); sequences that do not fit are reported like tokens without a page.
  * Workspace: sp_cache_attention_bytes of the same numbers, scratch of this call alone.
  * Errors: SP_ERR_INVALID_ARG (null pointers, unknown kind, scale outside [1e-30, 1e30], K_out in K's place), SP_ERR_SHAPE (sizes that do not match, ld or
- * a step too small or odd, page_len, turned, more than 2^30 rows, tokens of a table or opened keys), SP_ERR_DTYPE, SP_ERR_UNSUPPORTED (d_head),
- * SP_ERR_ALIGNMENT (pages and scales on 16 bytes, workspace on 256), SP_ERR_WORKSPACE.
+ * a step too small or odd, page_len not a multiple of 16 up to 65536, turned, more than 2^30 rows, tokens of a table or opened keys, more than 4096
+ * key heads, or heads of an appended query, queries x heads of a key head above 2^31 - 1), SP_ERR_DTYPE, SP_ERR_UNSUPPORTED (d_head), SP_ERR_ALIGNMENT
+ * (pages and scales on 16 bytes, workspace on 256), SP_ERR_WORKSPACE.
  */
 typedef enum { SP_CACHE_BF16 = 0, SP_CACHE_4BIT = 1 } sp_cache_kind;
 #define SP_CACHE_GROUP 64

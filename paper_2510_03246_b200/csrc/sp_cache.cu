@@ -545,10 +545,10 @@ cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, vo
                        int32_t* status, cudaStream_t stream) {
   return read_rows(c, cu, rows, K, V, ldk, ldv, dtype, false, nullptr, status, stream);
 }
-cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int32_t dtype, const uint32_t* tops, int32_t* status,
+cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, const uint32_t* tops, int32_t* status,
                        cudaStream_t stream) {
   const int64_t ld = (int64_t)c->n_kv_heads * c->d_head;
-  return read_rows(c, cu, rows, K, V, ld, ld, dtype, true, tops, status, stream);
+  return read_rows(c, cu, rows, K, V, ld, ld, SP_BF16, true, tops, status, stream);
 }
 cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, const sp_mat* Q, uint32_t* tops, cudaStream_t stream) {
   TopsParams p = {};

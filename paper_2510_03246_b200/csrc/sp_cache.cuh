@@ -45,10 +45,10 @@ CacheView cache_view(const sp_kv_cache* c);
 // Reads n = cu[s + 1] - cu[s] last tokens of every sequence (sp_cache_read).
 cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
                        int32_t* status, cudaStream_t stream);
-// The same for whole sequences into contiguous rows (those of a sequence with another number of tokens than n are NaN); with tops as fp16 in units
-// of these maxima of keys and values (sp_attention.cuh), which cache_tops has found among the scales of the same rows and the queries Q, and
+// The same for whole sequences into contiguous rows of bf16 (those of a sequence with another number of tokens than n are NaN); with tops as fp16 in
+// units of these maxima of keys and values (sp_attention.cuh), which cache_tops has found among the scales of the same rows and the queries Q, and
 // Q_half [Nq, n_heads * d_head] takes the queries alike.
-cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int32_t dtype, const uint32_t* tops, int32_t* status,
+cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, const uint32_t* tops, int32_t* status,
                        cudaStream_t stream);
 cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, const sp_mat* Q, uint32_t* tops, cudaStream_t stream);
 cudaError_t queries_to_half(const sp_mat* Q, void* Q_half, const uint32_t* tops, cudaStream_t stream);

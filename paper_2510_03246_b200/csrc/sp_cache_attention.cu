@@ -19,10 +19,10 @@
 // fp32 queries are three bf16 parts that add up to them, as are the probabilities' products with the scales; numbers are bf16 for both products, and
 // sums of 16 keys are added up outside the matrix unit.
 //
-// More rows open the pages into rows of the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor cores' rate, where this
+// More rows of bf16 open the pages into rows of the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor cores' rate, where this
 // form would open them again for every 16 rows.  4 bits are opened into fp16 in units of the call's maxima (bf16 queries alike): rounded to bf16,
-// results were 4.2e-3 from the formula (512 queries after 16384 keys, 32 heads of 128 on 8), 2.3e-3 as two bf16 parts each, in 312 us instead of
-// XXX, and values of equal scales all off by the same, which no sum over keys takes away.
+// results were 4.2e-3 from the formula (512 queries after 16384 keys, 32 heads of 128 on 8), and as two bf16 parts each 2.3e-3, in 312 us instead of
+// 186; in fp16 they are 1.7e-3 from it.  (Rounded values of equal scales are all off by the same, which no sum over keys takes away.)
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>
@@ -974,8 +974,17 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
 // Rows of a tile.  (Tiles of 24 or 32 read the cache once for the five drafted tokens of four heads of 64, and took as long: 46 us for 12 texts of
 // 700 .. 11447 keys, 8 heads, 16 bits.)
 inline int tile_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 8 * n_seq ? 8 : 16; }
-// Rows per sequence, on average, up to which the cache streams past tiles of 16 of them.
-inline bool paged_few_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 64 * n_seq; }
+// Whether the cache streams past tiles of 16 rows: up to a number of rows per sequence, on average, that is the larger the fewer sequences and key
+// heads there are, since the other form's tiles of 128 rows then leave most of the device idle.  This / the other form in 4 bits (16 take about as long),
+// heads of 128, us.  Sequences x heads 8: 1 x 16384 keys 128 rows 92 / 97, 192 rows 128 / 107; 12: 12 x 4096 keys 160 rows 59 / 61;
+// 16: 2 x 4096 keys 80 rows 45 / 49, 96 rows 51 / 48; 32: 4 x 4096 keys 80 rows 73 / 80, 96 rows 83 / 77; 48: 6 x 4096 keys 80 rows 100 / 100;
+// 64: 8 x 2048 keys 48 rows 176 / 204, 64 rows 228 / 190; 96: 12 x 4096 keys 32 rows 84 / 135, 64 rows 149 / 139; 512: 64 x 1024 keys 32 rows
+// 162 / 175, 64 rows 308 / 177.  In fp32 this form is always faster, since only it takes the tensor cores: 64 x 1024 keys 16 rows 104 / 541, 256 rows
+// 1378 / 2663; 1 x 16384 keys 256 rows 235 / 989.
+inline bool paged_few_rows(int32_t dtype, int64_t Nq, int64_t g, int64_t n_seq, int64_t n_kv) {
+  const int64_t streams = n_seq * n_kv;
+  return dtype == SP_F32 || Nq * g <= (streams <= 12 ? 128 : streams <= 48 ? 80 : streams <= 128 ? 48 : 32) * n_seq;
+}
 
 struct RowsPlan {
   int rows;
@@ -1055,13 +1064,13 @@ struct OpenPlan {
   size_t bytes() const { return cu_bytes + 2 * k_bytes + q_bytes + attention; }
 };
 // (room for the queries in fp16 whatever the cache is: the workspace depends on the sizes that its call is given)
-OpenPlan open_plan(int64_t Nq, int64_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype, int64_t max_keys) {
+OpenPlan open_plan(int64_t Nq, int64_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int64_t max_keys) {
   OpenPlan r;
   r.rows = max_keys + Nq;
   r.cu_bytes = align_up((size_t)(n_seq + 1) * 4 + 16, 256);      // and the three maxima behind the offsets
-  r.k_bytes = align_up((size_t)r.rows * n_kv * dh * dtype_size(dtype), 256);
-  r.q_bytes = dtype == SP_BF16 && dh % kCacheGroup == 0 ? align_up((size_t)Nq * n_heads * dh * 2, 256) : 0;
-  r.attention = sp_attention_workspace_bytes(Nq, r.rows, (int32_t)n_seq, n_heads, n_kv, dh, dtype);
+  r.k_bytes = align_up((size_t)r.rows * n_kv * dh * 2, 256);
+  r.q_bytes = dh % kCacheGroup == 0 ? align_up((size_t)Nq * n_heads * dh * 2, 256) : 0;
+  r.attention = sp_attention_workspace_bytes(Nq, r.rows, (int32_t)n_seq, n_heads, n_kv, dh, SP_BF16);
   return r;
 }
 // max_keys as the caller gave it, or all that the table can hold
@@ -1083,10 +1092,10 @@ size_t sp_cache_attention_bytes(int64_t Nq, int32_t n_seq, int32_t n_heads, int3
     return 0;
   const int64_t g = n_heads / n_kv_heads;
   if (Nq * g > 0x7fffffff) return 0;
-  if (paged_few_rows(Nq, g, n_seq)) return rows_plan(Nq, n_seq, g, d_head).bytes();
+  if (paged_few_rows(dtype, Nq, g, n_seq, n_kv_heads)) return rows_plan(Nq, n_seq, g, d_head).bytes();
   const int64_t keys = keys_at_most(max_keys, n_seq, max_pages, page_len);
   if (keys + Nq > (1 << 30)) return 0;
-  return open_plan(Nq, n_seq, n_heads, n_kv_heads, d_head, dtype, keys).bytes();
+  return open_plan(Nq, n_seq, n_heads, n_kv_heads, d_head, keys).bytes();
 }
 
 sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const int32_t* cu_q, int32_t n_heads, int32_t causal, double scale,
@@ -1113,7 +1122,7 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   uint8_t* at = reinterpret_cast<uint8_t*>(ws);
   ProfScope prof(PK_GEMM_SIMT, 0.0, 0.0, s);
-  if (paged_few_rows(Nq, g, n_seq)) {
+  if (paged_few_rows(dt, Nq, g, n_seq, n_kv)) {
     const RowsPlan plan = rows_plan(Nq, n_seq, g, dh);
     PagedParams p = {};
     p.c = cache_view(cache);
@@ -1136,11 +1145,11 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
     return SP_OK;
   }
   const int64_t keys = keys_at_most(max_keys, n_seq, cache->max_pages, cache->page_len);
-  const OpenPlan plan = open_plan(Nq, n_seq, n_heads, n_kv, dh, dt, keys);
+  const OpenPlan plan = open_plan(Nq, n_seq, n_heads, n_kv, dh, keys);
   int32_t* cu_k = reinterpret_cast<int32_t*>(at);
   uint8_t *K = at + plan.cu_bytes, *V = K + plan.k_bytes, *Qh = V + plan.k_bytes, *rest = Qh + plan.q_bytes;
   const int64_t kv = (int64_t)n_kv * dh;
-  const bool half = dt == SP_BF16 && cache->kind == SP_CACHE_4BIT;
+  const bool half = cache->kind == SP_CACHE_4BIT;
   uint32_t* tops = half ? reinterpret_cast<uint32_t*>(cu_k + n_seq + 1) : nullptr;
   count_launch();
   if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, tops, status_dev) !=
@@ -1148,7 +1157,7 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
     return SP_ERR_CUDA;
   if (half && (cache_tops(cache, cu_k, plan.rows, Q, tops, s) != cudaSuccess || queries_to_half(Q, Qh, tops, s) != cudaSuccess))
     return SP_ERR_CUDA;
-  if (cache_open(cache, cu_k, plan.rows, K, V, dt, tops, status_dev, s) != cudaSuccess) return SP_ERR_CUDA;
+  if (cache_open(cache, cu_k, plan.rows, K, V, tops, status_dev, s) != cudaSuccess) return SP_ERR_CUDA;
   sp_attention_args a = {};
   a.Q = half ? sp_mat{Qh, dt, 0, Nq, cols, cols} : *Q;
   a.O = *O;

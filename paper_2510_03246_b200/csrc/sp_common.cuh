@@ -378,8 +378,10 @@ inline bool linear_few_rows_f32(int64_t M, int64_t K) { return M <= 128 || (M <=
 cudaError_t linear_few_f32(int64_t M, int64_t N, int64_t K, Operand A, Operand W, const LinearEpi& epi, Operand other, OutOperand C,
                            cudaStream_t stream);
 
-// e4m3 rows of few tokens (sp_linear_e4m3.cu), layouts as sp_linear_e4m3 takes them.
-inline bool linear_few_rows_e4m3(int64_t M, int64_t N) { return M <= 16 || (M <= 192 && M * N <= (1 << 18)); }
+// e4m3 rows of few tokens (sp_linear_e4m3.cu), layouts as sp_linear_e4m3 takes them.  This / the tensor-core form, us: 768 -> 768 1 row 2.3 / 9.0,
+// 256 rows 5.9 / 9.1; 4096 -> 1024 256 rows 13.6 / 18.4; 1024 -> 4096 64 rows 7.0 / 9.9, 128 rows 11.5 / 10.1; 4096 -> 6144 16 rows 9.0 / 19.1,
+// 32 rows 14.2 / 19.1, 48 rows 19.4 / 19.1; 4096 -> 32000 16 rows 30.6 / 42.4, 32 rows 47.3 / 38.5.
+inline bool linear_few_rows_e4m3(int64_t M, int64_t N) { return M <= 16 || (M <= 256 && M * N <= (1 << 18)); }
 
 struct SolveAssist;
 // fp64 factorisation and solves (sp_linalg.cu), block columns of kCholNB.
