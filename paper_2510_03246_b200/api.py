@@ -683,6 +683,8 @@ def sp_rms_norm(X, weight=None, eps=1e-5, residual=None, h_out=None, out=None, o
     torch.float8_e4m3fn: 8 bits with a scale per row, rows that start on 16 bytes, as sp_linear_e4m3 reads them."""
     if out_dtype is not None and out_dtype != _F8 and out_dtype != X.dtype:
         raise ValueError("the result is of X's dtype or float8_e4m3fn")
+    if out_dtype is not None and out is not None and out.dtype != out_dtype:
+        raise ValueError("out is of another dtype than out_dtype")
     code, y, h, scale, rstd = (_native or _binding()).rms_norm(X, weight, eps, residual, h_out, out, out_dtype is _F8, want_rstd)
     if code:
         raise SpError(code, "sp_rms_norm")

@@ -7,6 +7,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/sp.h"
@@ -86,7 +87,6 @@ at::Tensor rows_of_16_bytes(int64_t n, int64_t cols, at::ScalarType type, int de
   at::Tensor t = empty({n, wide}, type, dev);
   return wide == cols ? t : t.narrow(1, 0, cols);
 }
-at::Tensor given_or(PyObject* o, const char* what, at::Tensor other) { return o == Py_None ? other : tensor(o, what); }
 struct Workspace {
   at::Tensor t;
   void* ptr = nullptr;
@@ -343,14 +343,13 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     PyErr_Format(PyExc_TypeError, "%d arguments, not %zd", N, n);
     return nullptr;
   }
+  HANDLE_TH_ERRORS                         // (an allocation that fails is torch's own error)
   try {
     return F(args);
   } catch (const Raised&) {
     return nullptr;
-  } catch (const std::exception& e) {      // (an allocation, say)
-    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
   }
+  END_HANDLE_TH_ERRORS
 }
 template <PyObject* (*F)(PyObject* const*), int N>
 PyMethodDef method(const char* name) {

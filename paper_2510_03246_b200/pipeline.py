@@ -344,7 +344,7 @@ class KvCache:
         for t, a, n in zip(texts, after, need):
             self._pages.setdefault(t, []).extend(self._free.pop() for _ in range(n))
             self._tokens[t] = a
-        width = max([len(self._pages[t]) for t in texts], default=0)
+        width = max([max(1, len(self._pages[t])) for t in texts], default=0)
         cu = [0]
         for n in new_tokens:
             cu.append(cu[-1] + n)
@@ -374,8 +374,10 @@ def cached_attention(qkv: torch.Tensor, pages: api.KvPages, step: CacheStep, n_h
     2 n_kv_heads) d_head] (whose queries are turned in their place): keys and values go into the module's pages, and the queries attend to all that is
     there.  Prompts of texts that were empty read their own keys and values as the projection left them, 4 bits or not.  Rows behind the step's last are
     zero.  status as attention_head_outputs."""
-    d_head = qkv.shape[1] // (n_heads + 2 * n_kv_heads)
+    d_head = pages.k.shape[3] * (2 if pages.k.dtype == torch.uint8 else 1)
     q, k = n_heads * d_head, n_kv_heads * d_head
+    if qkv.shape[1] != q + 2 * k:
+        raise ValueError(f"qkv has {qkv.shape[1]} columns, {n_heads} heads of queries and 2 x {n_kv_heads} of {d_head} channels have {q + 2 * k}")
     Q, K, V = qkv[:, :q], qkv[:, q:q + k], qkv[:, q + k:q + 2 * k]
     H = torch.zeros(qkv.shape[0], q, dtype=qkv.dtype, device=qkv.device)
     with _Status(status, qkv.device) as word:

@@ -259,3 +259,40 @@ def test_calls_on_another_stream_than_the_tensors_own():
     torch.cuda.synchronize()
     for x in got:
         assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_steps_without_tokens(four):
+    cache = pipeline.KvCache(1, 4, 16, 2, 64, four)
+    for texts, new in (([], []), (["a"], [0]), (["a", "b"], [0, 0])):
+        H = pipeline.cached_attention(torch.zeros(0, 512, device=DEV), cache.layers[0], cache.step(texts, new), 4, 2, freqs(64))
+        assert H.shape == (0, 256)
+    qkv = torch.randn(5, 512, generator=gen(80), device=DEV)
+    pipeline.cached_attention(qkv.clone(), cache.layers[0], cache.step(["a", "b"], [0, 5]), 4, 2, freqs(64))
+    for texts, new in ((["b"], [0]), (["a", "b"], [0, 0]), ([], [])):
+        H = pipeline.cached_attention(torch.zeros(2, 512, device=DEV), cache.layers[0], cache.step(texts, new), 4, 2, freqs(64))
+        assert H.shape == (2, 256) and (H == 0).all()
+
+
+def test_an_output_of_another_dtype_is_refused():
+    X = torch.randn(4, 64, device=DEV).to(BF)
+    for asked, given in ((torch.float8_e4m3fn, BF), (BF, torch.float8_e4m3fn)):
+        with pytest.raises(ValueError, match="out_dtype"):
+            api.sp_rms_norm(X, out_dtype=asked, out=torch.empty(4, 64, dtype=given, device=DEV))
+    assert api.sp_rms_norm(X, out=torch.empty(4, 64, dtype=torch.float8_e4m3fn, device=DEV)).scale.shape == (4,)
+
+
+def test_loss_of_a_normed_stream_in_bf16():
+    """bf16: the normed rows, the logits' and the gradients' roundings, half a step of 2^-8 each at most and uniform: below 2^-7 of a gradient's norm
+    in all, as the norm's own gradient comes from the rounded d_hidden."""
+    N, d, V = 64, 128, 300
+    h = torch.randn(N, d, generator=gen(90), device=DEV).to(BF)
+    W = (torch.randn(V, d, generator=gen(91), device=DEV) / d ** 0.5).to(BF)
+    w = 1 + 0.2 * torch.randn(d, generator=gen(92), device=DEV)
+    t = torch.randint(0, V, (N,), generator=gen(93), device=DEV)
+    r = pipeline.token_loss(h, W, t, with_grad=True, norm_weight=w)
+    a, b, c = (x.double().requires_grad_() for x in (h, W, w))
+    y = a / (a.square().mean(1, keepdim=True) + 1e-5).sqrt() * c
+    torch.nn.functional.cross_entropy(y @ b.t(), t).backward()
+    for got, want in ((r.d_hidden, a.grad), (r.d_W, b.grad), (r.d_norm, c.grad)):
+        assert ((got.double() - want).norm() / want.norm()).item() <= 2.0 ** -7

@@ -72,3 +72,11 @@ def test_weights_in_8_bits():
     assert W8.dtype == torch.float8_e4m3fn and W8.stride(0) % 16 == 0 and scale.dtype == torch.float32
     back = W8.float() * scale[:, None]
     assert ((back - W).abs() <= W.abs() * 2.0 ** -4 + scale[:, None] * 2.0 ** -10 + 1e-7 * W.abs()).all()
+
+
+def test_projections_of_other_heads_are_refused():
+    cache = pipeline.KvCache(1, 4, 16, 2, 64, device="cpu")
+    step = cache.step(["a"], [3])
+    for heads, kv, cols in ((4, 2, 8 * 64 + 16), (4, 2, 7 * 64), (8, 2, 8 * 64)):
+        with pytest.raises(ValueError, match="columns"):
+            pipeline.cached_attention(torch.zeros(3, cols), cache.layers[0], step, heads, kv)
