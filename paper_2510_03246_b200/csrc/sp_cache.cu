@@ -4,8 +4,7 @@
 // Rotation: channels (a, b) of a pair with frequency f become (a cos - b sin, b cos + a sin), angle p f.  The angle is taken in 64 bits and
 // in whole turns away first: at p = 10^5 an angle in 32 bits would be off by 10^-2.
 // 4 bits: of every 64 channels of a head, zero = bf16(least), scale = bf16((largest - zero) / 15), n = (x - zero) / scale rounded to the
-// nearest of 0 .. 15.  Rotated keys are kept in 64 bits up to there: a value next to the border of two steps falls on the side on which the
-// formula has it, whatever order the sums were taken in.
+// nearest of 0 .. 15.  A value next to the border of two steps, a rotated one too, falls on the side on which the formula in 64 bits has it.
 //
 // Both kernels are bound by memory (append: 16384 x (32 + 2 x 8) heads of 128: 200 MB in, 150 MB out); a thread has eight channels at a time,
 // 16 bytes of bf16, four bytes of a page in 4 bits; the eight lanes of a group find its bounds by shuffles.
@@ -103,59 +102,87 @@ __device__ __forceinline__ void put8(float* p, bool vec, const float (&x)[8]) {
 __device__ __forceinline__ float turned_low(float a, float b, float2 cs) { return __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y)); }
 __device__ __forceinline__ float turned_high(float a, float b, float2 cs) { return __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y)); }
 
-// The eight lanes of a group hold eight channels each: their 4-bit numbers packed, and the group's scale and offset in lane 0 of the eight.
-// F: float where the values are what the caller gave, double for rotated ones (see above).  A quotient in fp32 decides unless it lies near
-// the border of two numbers; what is near takes in how far the values are from zero in steps, by which a difference in fp32 is off.
-template <typename F>
-__device__ __forceinline__ uint32_t four_bits(const F (&x)[8], uint32_t& pair) {
-  float f[8], lo, top = 0.f;
-  F hi = x[0];
-  bool odd = false;                        // a NaN or an infinity
+// The eight lanes of a group hold eight channels each: their 4-bit numbers packed, and the group's scale and offset.  f: the values in fp32, at most `off`
+// from the exact ones (OFF; else they are those), which exact() makes in 64 bits.  fp32 decides where it can: something that its error could round
+// elsewhere takes the formula in 64 bits, one warp in a hundred.  (10584 rows of 32, 8 and 8 heads of 128: 74 us, all in 64 bits 85.)
+template <bool OFF, typename E>
+__device__ __forceinline__ uint32_t four_bits(const float (&f)[8], float off, const E& exact, uint32_t& pair) {
+  float lo = f[0], hi = f[0], none = 0.f;  // none: NaN with a NaN or an infinity
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    f[i] = (float)x[i];
-    lo = i == 0 ? f[0] : fminf(lo, f[i]);
-    top = fmaxf(top, fabsf(f[i]));
-    hi = x[i] > hi ? x[i] : hi;
-    odd |= !(fabsf(f[i]) < INFINITY);
+    lo = fminf(lo, f[i]);
+    hi = fmaxf(hi, f[i]);
+    none = fmaf(f[i], 0.f, none);
   }
 #pragma unroll
   for (int w = 1; w < 8; w <<= 1) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, w));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-    const F b = __shfl_xor_sync(0xffffffffu, hi, w);
-    hi = b > hi ? b : hi;
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, w));
+    if (OFF) off = fmaxf(off, __shfl_xor_sync(0xffffffffu, off, w));
   }
-  const uint32_t eight = (__ballot_sync(0xffffffffu, odd) >> (threadIdx.x & 24)) & 0xffu;
-  const float zero = __bfloat162float(__float2bfloat16_rn(lo));      // (rounding keeps the order: the least value's)
-  const float scale = __bfloat162float(__float2bfloat16_rn((float)(((double)hi - (double)zero) / 15.0)));
-  if (eight != 0u) {                       // (the offset reads back as NaN whatever the numbers are)
-    pair = 0x7fc07fc0u;
-    return 0u;
-  }
-  pair = (__float_as_uint(scale) >> 16) | (__float_as_uint(zero) & 0xffff0000u);
-  if (!(scale > 0.f)) return 0u;
-  const bool tiny = scale < 1e-36f;        // its reciprocal, or a product with it, may leave the range of fp32
-  const float inv = tiny ? 0.f : 1.f / scale;
-  const float near = tiny ? 1.f : fminf(1e-4f + top * inv * 0x1p-21f, 1.f);
-  constexpr float kRound = 12582912.f;     // 1.5 2^23: added, the sum's last bits are the whole number that is nearest
-  uint32_t packed = 0u;
-  bool slow = false;
+  const bool odd = ((__ballot_sync(0xffffffffu, none != none) >> (threadIdx.x & 24)) & 0xffu) != 0u;
+  float zero = __bfloat162float(__float2bfloat16_rn(lo));            // (rounding keeps the order: the least value's)
+  bool unsure = OFF && __bfloat162float(__float2bfloat16_rn(lo - off)) != __bfloat162float(__float2bfloat16_rn(lo + off));
+  // hi - zero, its product with 1 / 15 and that constant are rounded: 3 x 2^-24 of the quotient
+  const float fifteenth = (hi - zero) * (1.f / 15.f), about = fabsf(fifteenth) * 0x1p-22f + (OFF ? off : 0.f);
+  float scale = __bfloat162float(__float2bfloat16_rn(fifteenth));
+  unsure |= __bfloat162float(__float2bfloat16_rn(fifteenth - about)) != __bfloat162float(__float2bfloat16_rn(fifteenth + about));
+  unsure |= fabsf(fifteenth) < 1e-30f && hi != zero;                 // its reciprocal, or a product with it, may leave the range of fp32
+  const float inv = scale > 0.f ? __fdividef(1.f, scale) * (1.f / 15.f) : 0.f;
+  // in steps: the difference, the reciprocal, the constant and two products are rounded, 16 x 6 x 2^-24 together
+  const float near = OFF ? fmaf(16.f * off, inv, 1e-5f) : 1e-5f;
+  constexpr float kRound = 12582912.f;     // 1.5 2^23: added, what is left behind the point is rounded away
+  float edge = 0.f, sum[2] = {8388608.f, 8388608.f};                 // (2^23: the sums of four numbers times 16^i stand in its last bits)
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float t = fminf(fmaxf((f[i] - zero) * inv, 0.f), 15.f), u = t + kRound;
-    packed |= (__float_as_uint(u) & 15u) << (4 * i);
-    slow |= fabsf(fabsf(t - (u - kRound)) - 0.5f) < near;
+    const float t = __saturatef((f[i] - zero) * inv), n = fmaf(t, 15.f, kRound) - kRound;
+    edge = fmaxf(edge, fabsf(fmaf(t, 15.f, -n)));
+    sum[i / 4] = fmaf(n, (float)(1 << (4 * (i & 3))), sum[i / 4]);
   }
-  if (slow) {
+  uint32_t packed = __byte_perm(__float_as_uint(sum[0]), __float_as_uint(sum[1]), 0x5410);
+  const bool border = edge > 0.5f - near;
+  if (OFF) {
+    unsure |= border;
+  } else if (__any_sync(0xffffffffu, border)) {
+    // Values of few bits often lie between two steps exactly.  Their difference from there has the sign of d - (n + 1/2) scale, whose product has 13
+    // bits, with what d = f - zero leaves.
     packed = 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const double n = rint(((double)x[i] - (double)zero) / (double)scale);
+      const float d = f[i] - zero, back = d - f[i], left = (f[i] - (d - back)) - (zero + back);
+      const float below = floorf(__saturatef(d * inv) * 15.f), side = fmaf(-(below + 0.5f), scale, d) + left;
+      const int n = (int)below;
+      packed |= (uint32_t)(side > 0.f || (side == 0.f && (n & 1)) ? n + 1 : n) << (4 * i);
+    }
+  }
+  if (__any_sync(0xffffffffu, unsure && !odd)) {
+    double x[8];
+    exact(x);
+    double top = x[0];
+    lo = (float)x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+      lo = fminf(lo, (float)x[i]);
+      top = x[i] > top ? x[i] : top;
+    }
+#pragma unroll
+    for (int w = 1; w < 8; w <<= 1) {
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, w));
+      const double other = __shfl_xor_sync(0xffffffffu, top, w);
+      top = other > top ? other : top;
+    }
+    zero = __bfloat162float(__float2bfloat16_rn(lo));
+    scale = __bfloat162float(__float2bfloat16_rn((float)((top - (double)zero) / 15.0)));
+    packed = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const double n = rint((x[i] - (double)zero) / (double)scale);
       packed |= (uint32_t)fmin(fmax(n, 0.0), 15.0) << (4 * i);
     }
   }
-  return packed;
+  // (with a NaN or an infinity the offset reads back as NaN whatever the numbers are)
+  pair = odd ? 0x7fc07fc0u : (__float_as_uint(scale) >> 16) | (__float_as_uint(zero) & 0xffff0000u);
+  return odd || !(scale > 0.f) ? 0u : packed;
 }
 
 // A block has `per_block` consecutive rows: first their places and angles, a warp to a row, then all their chunks of channels in one walk, several of
@@ -271,38 +298,55 @@ __global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const A
     load8<VEC>(src, p.k_vec != 0, a);
     if (turns && !p.neighbours) load8<VEC>(second ? src - half : src + half, p.k_vec != 0, b);
     if (p.c.k) load8<VEC>(reinterpret_cast<const T*>(p.v) + (row0 + r) * p.ldv + column, p.v_vec != 0, v);
-    using F = typename std::conditional<FOUR, double, float>::type;
-    F x[8];
+    // x = a cos + b sin, b with the sign that it has in the pair
+    float x[8];
+    const float sign = second ? 1.f : -1.f;
     if (!turns) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = (F)a[k];
-    } else {
-      const int f0 = p.neighbours ? 4 * chunk : 8 * (second ? chunk - half8 : chunk);
+      for (int k = 0; k < 8; ++k) {
+        x[k] = a[k];
+        b[k] = 0.f;
+      }
+    } else if (p.neighbours) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int f = p.neighbours ? f0 + k / 2 : f0 + k;
-        const float other = p.neighbours ? a[k ^ 1] : b[k];
-        const bool up = p.neighbours ? (k & 1) != 0 : second;
-        if constexpr (FOUR) {
-          const double2 cs = s_exact[r][placed(f)];
-          x[k] = fma((double)a[k], cs.x, (double)other * (up ? cs.y : -cs.y));
-        } else {
-          const float2 cs = s_turn[r][placed(f)];
-          x[k] = up ? turned_high(other, a[k], cs) : turned_low(a[k], other, cs);
-        }
+        const float2 cs = s_turn[r][placed(4 * chunk + k / 2)];
+        b[k] = k & 1 ? a[k - 1] : -a[k + 1];
+        x[k] = __fadd_rn(__fmul_rn(a[k], cs.x), __fmul_rn(b[k], cs.y));
+      }
+    } else {
+      const float2* turn = s_turn[r] + placed(8 * (second ? chunk - half8 : chunk));
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float2 cs = turn[placed(k)];
+        x[k] = fmaf(__fmul_rn(b[k], cs.y), sign, __fmul_rn(a[k], cs.x));      // (a product with 1 or -1 is exact: the sum is rounded, as above)
       }
     }
-    if (p.k_out && live) {
-      float y[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = (float)x[k];
-      put8<VEC>(reinterpret_cast<T*>(p.k_out) + (row0 + r) * p.ldko + column, p.k_vec != 0, y);
-    }
+    if (p.k_out && live) put8<VEC>(reinterpret_cast<T*>(p.k_out) + (row0 + r) * p.ldko + column, p.k_vec != 0, x);
     if (!p.c.k) continue;
     const int64_t at = (int64_t)head * p.c.page_len + s_slot[r];      // (head, token) of the page
     if constexpr (FOUR) {
+      // a turned value's cosine, sine, products and sum are rounded: 3 x 2^-24 of |a| + |b|
+      float off = 0.f;
+      if (turns) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) off = fmaxf(off, fabsf(a[k]) + fabsf(b[k]));
+        off *= 0x1p-22f;
+      }
       uint32_t pair_k, pair_v;
-      const uint32_t packed_k = four_bits(x, pair_k), packed_v = four_bits(v, pair_v);
+      const uint32_t packed_k = four_bits<true>(x, off, [&](double (&y)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          y[k] = (double)a[k];
+          if (!turns) continue;
+          const double2 cs = s_exact[r][placed(p.neighbours ? 4 * chunk + k / 2 : 8 * (second ? chunk - half8 : chunk) + k)];
+          y[k] = fma((double)a[k], cs.x, (double)b[k] * (p.neighbours || second ? cs.y : -cs.y));
+        }
+      }, pair_k);
+      const uint32_t packed_v = four_bits<false>(v, 0.f, [&](double (&y)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = (double)v[k];
+      }, pair_v);
       if (page >= 0 && live) {
         const int64_t to = page * p.c.step + at * (dh / 2) + 4 * chunk;
         *reinterpret_cast<uint32_t*>(p.c.k + to) = packed_k;
