@@ -371,20 +371,38 @@ struct ReadParams {
   void *k, *v;
   int64_t ldk, ldv;
   int32_t rows, whole, k_vec, v_vec;
+  Divisor head;                            // chunks of a head
   const uint32_t* tops;
   int32_t* status;
 };
-__device__ __forceinline__ void put8_half(__half* p, const float (&x)[8], float f) {
-  uint32_t u[4];
+// The eight values of a word of numbers, one rounding each: scale n + zero.  A number is put in the place of a mantissa's bits of 2^23, 2^19 ..,
+// which are taken away again: conversions of integers have a sixteenth of the rate of that.
+__device__ __forceinline__ void open8(uint32_t w, uint32_t pair, float (&x)[8]) {
+  const float scale = __uint_as_float(pair << 16), zero = __uint_as_float(pair & 0xffff0000u);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t from = k < 4 ? w : w >> 16;
+    const int at = 4 * (k & 3);
+    x[k] = fmaf(__uint_as_float((from & (15u << at)) | ((150u - at) << 23)) - (float)(1 << (23 - at)), scale, zero);
+  }
+}
+// The same in fp16, in units of 1 / f: scales and offsets fit into it but for what lies 2^-28 below the largest.
+__device__ __forceinline__ void open8_half(__half* p, uint32_t w, uint32_t pair, float f) {
+  const __half2 scale = __float2half2_rn(__uint_as_float(pair << 16) * f), zero = __float2half2_rn(__uint_as_float(pair & 0xffff0000u) * f);
+  __half2 x[4];                            // channels i and i + 4
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const __half2 e = __floats2half2_rn(x[2 * i] * f, x[2 * i + 1] * f);
-    u[i] = *reinterpret_cast<const uint32_t*>(&e);
+    const uint32_t m = ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u;             // 1024 + n
+    x[i] = __hfma2(__hsub2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x6400u))), scale, zero);
   }
-  *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+  const __half2 y[4] = {__lows2half2(x[0], x[1]), __lows2half2(x[2], x[3]), __highs2half2(x[0], x[1]), __highs2half2(x[2], x[3])};
+  *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(y);
 }
 
-// a warp per row: eight channels of keys and of values at a time in every lane.  T of fp16: contiguous rows in units of tops.
+constexpr uint32_t kNan2 = 0x7fff7fffu;   // two of fp16
+
+// a warp per row: eight channels of keys and of values at a time in every lane (more warps at once are worth more than two chunks of a lane in
+// flight: 17k rows of 8 heads of 128 to fp16 20 us, unrolled 23).  T of fp16: contiguous rows in units of tops.
 template <typename T, bool FOUR>
 __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
   kernel_begin();
@@ -401,36 +419,38 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
   if (page < 0 && lane == 0) report_status(p.status, SP_ERR_SHAPE, s, entry);
   constexpr bool HALF = std::is_same<T, __half>::value;
   const float fk = HALF ? half_per_unit(p.tops[kTopK]) : 1.f, fv = HALF ? half_per_unit(p.tops[kTopV]) : 1.f;
-  const int dh = p.c.dh, per_head = dh / 8, chunks = p.c.n_kv * per_head;
-#pragma unroll 2
+  const int dh = p.c.dh, chunks = p.c.n_kv * (dh / 8);
+  T *k_row = reinterpret_cast<T*>(p.k) + row * p.ldk, *v_row = reinterpret_cast<T*>(p.v) + row * p.ldv;
+#pragma unroll 1
   for (int e = lane; e < chunks; e += 32) {
-    const int head = e / per_head, chunk = e % per_head;
+    const int head = (int)quotient((uint32_t)e, p.head), chunk = e - head * (int)p.head.d;       // (heads are whole chunks: they go to 8 e)
     const int64_t at = (int64_t)head * p.c.page_len + slot;
     float x[8], y[8];
     if (page < 0) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = y[k] = NAN;
+      for (int k = 0; k < 8; ++k) x[k] = y[k] = NAN;       // (fp16: below)
     } else if constexpr (FOUR) {
       const int64_t from = page * p.c.step + at * (dh / 2) + 4 * chunk, g = page * p.c.scale_step + (at * (dh / kCacheGroup) + chunk / 8) * 4;
       const uint32_t a = *reinterpret_cast<const uint32_t*>(p.c.k + from), b = *reinterpret_cast<const uint32_t*>(p.c.v + from);
       const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + g), sb = *reinterpret_cast<const uint32_t*>(p.c.vs + g);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        x[k] = fmaf((float)((a >> (4 * k)) & 15u), __uint_as_float(sa << 16), __uint_as_float(sa & 0xffff0000u));
-        y[k] = fmaf((float)((b >> (4 * k)) & 15u), __uint_as_float(sb << 16), __uint_as_float(sb & 0xffff0000u));
+      if constexpr (HALF) {
+        open8_half(k_row + 8 * e, a, sa, fk);
+        open8_half(v_row + 8 * e, b, sb, fv);
+        continue;
+      } else {
+        open8(a, sa, x);
+        open8(b, sb, y);
       }
     } else {
       const int64_t from = page * p.c.step + (at * dh + 8 * chunk) * 2;
       load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.k + from), true, x);
       load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.v + from), true, y);
     }
-    const int64_t column = head * dh + 8 * chunk;
     if constexpr (HALF) {
-      put8_half(reinterpret_cast<__half*>(p.k) + row * p.ldk + column, x, fk);
-      put8_half(reinterpret_cast<__half*>(p.v) + row * p.ldv + column, y, fv);
+      *reinterpret_cast<uint4*>(k_row + 8 * e) = *reinterpret_cast<uint4*>(v_row + 8 * e) = make_uint4(kNan2, kNan2, kNan2, kNan2);
     } else {
-      put8<false>(reinterpret_cast<T*>(p.k) + row * p.ldk + column, p.k_vec != 0, x);
-      put8<false>(reinterpret_cast<T*>(p.v) + row * p.ldv + column, p.v_vec != 0, y);
+      put8<false>(k_row + 8 * e, p.k_vec != 0, x);
+      put8<false>(v_row + 8 * e, p.v_vec != 0, y);
     }
   }
 }
@@ -516,7 +536,13 @@ __global__ void __launch_bounds__(256) queries_to_half_kernel(const __nv_bfloat1
   if (row >= rows) return;
   float x[8];
   load8<false>(q + row * ldq + 8 * j, vec != 0, x);
-  put8_half(out + row * cols + 8 * j, x, f);
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 y = __floats2half2_rn(x[2 * i] * f, x[2 * i + 1] * f);
+    u[i] = *reinterpret_cast<const uint32_t*>(&y);
+  }
+  *reinterpret_cast<uint4*>(out + row * cols + 8 * j) = make_uint4(u[0], u[1], u[2], u[3]);
 }
 
 bool rows_of_16(const void* ptr, int64_t ld, int32_t dtype, int64_t rows) {
@@ -570,6 +596,7 @@ cudaError_t read_rows(const sp_kv_cache* c, const int32_t* cu, int64_t rows, voi
   p.k = K; p.v = V; p.ldk = ldk; p.ldv = ldv;
   p.rows = (int32_t)rows;
   p.whole = whole ? 1 : 0;
+  p.head = divisor(c->d_head / 8);
   p.k_vec = rows_of_16(K, ldk, dtype, rows); p.v_vec = rows_of_16(V, ldv, dtype, rows);
   p.tops = tops;
   p.status = status;
