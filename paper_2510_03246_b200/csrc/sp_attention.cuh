@@ -132,8 +132,10 @@ cudaError_t attention_rows_f32(const AttnParams& p, cudaStream_t stream);
 // tcgen05 form (sp_attention_tc.cu): layouts that tensor maps can describe
 bool attention_tc_supported(const AttnParams& a);
 sp_status attention_tc(const AttnParams& a, cudaStream_t stream);
-// sp_attention (half null), or with fp16 operands in the places and pitches of Q, K and V, always by the tcgen05 form.
-sp_status attention_forward(const sp_attention_args* a, const uint32_t* half_tops, int32_t* status_dev, void* ws, size_t ws_bytes,
+// sp_attention (half_tops null), or with fp16 operands in the places and pitches of Q, K and V, always by the tcgen05 form.  keys: how many of K's
+// rows a single sequence has, as the caller knows it; 0: not known.  Both calls get the same.
+size_t attention_workspace(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype, int64_t keys);
+sp_status attention_forward(const sp_attention_args* a, const uint32_t* half_tops, int64_t keys, int32_t* status_dev, void* ws, size_t ws_bytes,
                             cudaStream_t stream);
 
 }  // namespace sp

@@ -975,15 +975,19 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
 // 700 .. 11447 keys, 8 heads, 16 bits.)
 inline int tile_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 8 * n_seq ? 8 : 16; }
 // Whether the cache streams past tiles of 16 rows: up to a number of rows per sequence, on average, that is the larger the fewer sequences and key
-// heads there are, since the other form's tiles of 128 rows then leave most of the device idle.  This / the other form in 4 bits (16 take about as long),
-// heads of 128, us.  Sequences x heads 8: 1 x 16384 keys 128 rows 92 / 97, 192 rows 128 / 107; 12: 12 x 4096 keys 160 rows 59 / 61;
-// 16: 2 x 4096 keys 80 rows 45 / 49, 96 rows 51 / 48; 32: 4 x 4096 keys 80 rows 73 / 80, 96 rows 83 / 77; 48: 6 x 4096 keys 80 rows 100 / 100;
-// 64: 8 x 2048 keys 48 rows 176 / 204, 64 rows 228 / 190; 96: 12 x 4096 keys 32 rows 84 / 135, 64 rows 149 / 139; 512: 64 x 1024 keys 32 rows
-// 162 / 175, 64 rows 308 / 177.  In fp32 this form is always faster, since only it takes the tensor cores: 64 x 1024 keys 16 rows 104 / 541, 256 rows
-// 1378 / 2663; 1 x 16384 keys 256 rows 235 / 989.
+// heads there are, since the other form's tiles of 128 rows then leave more of the device idle (less of it where a single sequence is cut to
+// fit).  This / the other form in 4 bits (16 take about as long), heads of 128, us.  A single sequence, by key heads: 1 head 16384 keys 160 rows 33 / 55;
+// 4 heads 8192 keys 128 rows 39 / 40; 8 heads 2048 keys 96 rows 28 / 29, 32768 keys 48 rows 73 / 86, 64 rows 91 / 83; 32 heads 8192 keys 48 rows
+// 77 / 82, 64 rows 96 / 79; 40 heads 4096 keys 48 rows 59 / 67, 80 rows 86 / 69.  Several, by sequences x heads: 12: 12 x 4096 keys 160 rows
+// 59 / 61; 16: 2 x 4096 keys 80 rows 45 / 49, 96 rows 51 / 48; 32: 4 x 4096 keys 80 rows 73 / 80, 96 rows 83 / 77; 48: 6 x 4096 keys 80 rows
+// 100 / 100; 64: 8 x 2048 keys 48 rows 176 / 204, 64 rows 228 / 190; 96: 12 x 4096 keys 32 rows 84 / 135, 64 rows 149 / 139; 512: 64 x 1024 keys 32
+// rows 162 / 175, 64 rows 308 / 177.  In fp32 this form is always faster, since only it takes the tensor cores: 64 x 1024 keys 16 rows 104 / 541,
+// 256 rows 1378 / 2663; 1 x 16384 keys 256 rows 235 / 989.
 inline bool paged_few_rows(int32_t dtype, int64_t Nq, int64_t g, int64_t n_seq, int64_t n_kv) {
+  if (dtype == SP_F32) return true;
   const int64_t streams = n_seq * n_kv;
-  return dtype == SP_F32 || Nq * g <= (streams <= 12 ? 128 : streams <= 48 ? 80 : streams <= 128 ? 48 : 32) * n_seq;
+  const int64_t most = n_seq == 1 ? (streams <= 4 ? 128 : streams <= 12 ? 64 : 48) : streams <= 12 ? 128 : streams <= 48 ? 80 : streams <= 128 ? 48 : 32;
+  return Nq * g <= most * n_seq;
 }
 
 struct RowsPlan {
@@ -1070,7 +1074,7 @@ OpenPlan open_plan(int64_t Nq, int64_t n_seq, int32_t n_heads, int32_t n_kv, int
   r.cu_bytes = align_up((size_t)(n_seq + 1) * 4 + 16, 256);      // and the three maxima behind the offsets
   r.k_bytes = align_up((size_t)r.rows * n_kv * dh * 2, 256);
   r.q_bytes = dh % kCacheGroup == 0 ? align_up((size_t)Nq * n_heads * dh * 2, 256) : 0;
-  r.attention = sp_attention_workspace_bytes(Nq, r.rows, (int32_t)n_seq, n_heads, n_kv, dh, SP_BF16);
+  r.attention = attention_workspace(Nq, r.rows, (int32_t)n_seq, n_heads, n_kv, dh, SP_BF16, max_keys);
   return r;
 }
 // max_keys as the caller gave it, or all that the table can hold
@@ -1167,7 +1171,7 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   a.lse = lse;
   a.n_seq = n_seq; a.n_heads = n_heads; a.n_kv_heads = n_kv; a.causal = causal;
   a.scale = scale;
-  return attention_forward(&a, tops, status_dev, rest, plan.attention, s);
+  return attention_forward(&a, tops, keys, status_dev, rest, plan.attention, s);
 }
 
 }  // extern "C"
