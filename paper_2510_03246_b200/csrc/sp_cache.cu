@@ -145,14 +145,15 @@ __device__ __forceinline__ uint32_t four_bits(const float (&f)[8], float off, co
     unsure |= border;
   } else if (__any_sync(0xffffffffu, border)) {
     // Values of few bits often lie between two steps exactly.  Their difference from there has the sign of d - (n + 1/2) scale, whose product has 13
-    // bits, with what d = f - zero leaves.
+    // bits, with what d = f - zero leaves; a rest that 64 bits would lose is left to them.
     packed = 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float d = f[i] - zero, back = d - f[i], left = (f[i] - (d - back)) - (zero + back);
-      const float below = floorf(__saturatef(d * inv) * 15.f), side = fmaf(-(below + 0.5f), scale, d) + left;
+      const float below = floorf(__saturatef(d * inv) * 15.f), at = fmaf(-(below + 0.5f), scale, d), side = at + left;
       const int n = (int)below;
       packed |= (uint32_t)(side > 0.f || (side == 0.f && (n & 1)) ? n + 1 : n) << (4 * i);
+      unsure |= at == 0.f && left != 0.f && fabsf(left) < d * 0x1p-50f;
     }
   }
   if (__any_sync(0xffffffffu, unsure && !odd)) {
