@@ -556,3 +556,19 @@ def test_scales_of_very_different_sizes(q_len, k_len):
         a = api.sp_cache_attention(Q, pages, ints(offsets(q_len)), table, ints(k_len), heads, want_lse=True)
         b = api.sp_cache_attention(Q, left, ints(offsets(q_len)), table, ints(k_len), heads, want_lse=True)
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("q_len, k_len, heads, kv", [([16], [3000], 32, 8), ([17], [3000], 32, 8), ([12], [700], 128, 32), ([13], [700], 128, 32),
+                                                      ([20, 20], [900, 30], 32, 8), ([22, 19], [900, 300], 32, 8), ([128], [2000], 2, 2)])
+def test_on_both_sides_of_few_rows(q_len, k_len, heads, kv, four):
+    check_attention(q_len, k_len, heads, kv, 64, 16, BF, four, seed=41, max_keys=sum(k_len))
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("max_keys", [0, 5003, 60000])
+def test_a_chunk_of_one_text_whose_keys_are_cut(max_keys, causal, four):
+    """Parts by what the caller says, right, too large or not at all: the text's length comes from the device."""
+    check_attention([130], [5003], 8, 2, 128, 64, BF, four, causal, tail=2, seed=42, max_keys=max_keys)
+    check_attention([3, 300], [60, 4000], 8, 2, 64, 16, BF, four, causal, seed=43, max_keys=max_keys)
