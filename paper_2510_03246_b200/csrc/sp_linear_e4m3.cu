@@ -38,11 +38,13 @@ struct FewParams {
   int32_t y_f32;
 };
 
-// NT: groups of eight rows of X
-template <int NT>
-__global__ void __launch_bounds__(kWarps * 32, NT > 1 ? 2 : 3) linear_e4m3_few_kernel(const FewParams p) {
+// NT: groups of eight rows of X.  CTAS: blocks that an SM holds.  Two groups have four pieces of a warp in flight in two blocks, or two pieces in three:
+// faster where there are more blocks than fit at once by two.  Two / three blocks, us, 16 rows: 4096 -> 6144 9.0 / 7.8, 4096 -> 32000 30.3 / 29.5,
+// 8192 -> 2048 8.1 / 10.2, 4096 -> 1024 4.8 / 5.9.
+template <int NT, int CTAS>
+__global__ void __launch_bounds__(kWarps * 32, CTAS) linear_e4m3_few_kernel(const FewParams p) {
   kernel_begin();
-  constexpr int kUnroll = NT > 2 ? 2 : 4;
+  constexpr int kUnroll = NT > 2 || (NT == 2 && CTAS > 2) ? 2 : 4;
   __shared__ float s_acc[kWarps][NT * 8][kOut + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g4 = lane >> 2, t4 = lane & 3;
   const int64_t o0 = (int64_t)blockIdx.x * kOut, t0 = (int64_t)blockIdx.y * (NT * 8);
@@ -161,8 +163,9 @@ extern "C" sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const
   count_launch();
   ProfScope prof(PK_GEMM_SIMT, 2.0 * (double)T * (double)N * (double)K, 0.0, s);
   const dim3 grid((unsigned)ceil_div(N, (int64_t)kOut), (unsigned)ceil_div(T, (int64_t)32));
-  const cudaError_t e = T <= 8    ? launch(linear_e4m3_few_kernel<1>, grid, dim3(kWarps * 32), 0, s, p)
-                        : T <= 16 ? launch(linear_e4m3_few_kernel<2>, grid, dim3(kWarps * 32), 0, s, p)
-                                  : launch(linear_e4m3_few_kernel<4>, grid, dim3(kWarps * 32), 0, s, p);
+  const auto kernel = T <= 8 ? linear_e4m3_few_kernel<1, 3>
+                      : T > 16 ? linear_e4m3_few_kernel<4, 2>
+                      : (int64_t)grid.x > 2 * (int64_t)sm_count() ? linear_e4m3_few_kernel<2, 3> : linear_e4m3_few_kernel<2, 2>;
+  const cudaError_t e = launch(kernel, grid, dim3(kWarps * 32), 0, s, p);
   return e == cudaSuccess ? SP_OK : SP_ERR_CUDA;
 }
