@@ -211,8 +211,8 @@ __device__ __forceinline__ int32_t visible(int32_t nk, int64_t shift, int64_t to
 
 // The work of a launch is a line of blocks: sequence by sequence, of each its tiles of rows, of each the key heads, of each kLead that stand for
 // its queries and its output (some microseconds; without them 12 texts of 700 .. 11447 keys kept SMs busy for half of the time: 76 us, with 32 52, with
-// 64 46), and the blocks of keys.  `ctas` thread blocks share it in equal pieces: the b-th has [b total / ctas, (b + 1) total / ctas).  A tile and head that lies in several
-// thread blocks' pieces is joined from what they leave: the one that goes on in it from a predecessor at 2 b, the one that begins it at 2 b + 1.
+// 64 46), and the blocks of keys.  `ctas` thread blocks share it in equal pieces: the b-th has [b total / ctas, (b + 1) total / ctas).  A tile and head
+// that lies in several thread blocks' pieces is joined from what they leave: the one that goes on in it from a predecessor at 2 b, the one that begins it at 2 b + 1.
 __device__ __forceinline__ int64_t first_of(int64_t b, int64_t total, int64_t ctas) { return b * total / ctas; }
 __device__ __forceinline__ int64_t cta_of(int64_t x, int64_t total, int64_t ctas) { return ((x + 1) * ctas - 1) / total; }
 
@@ -332,8 +332,8 @@ paged_rows_kernel(const PagedParams p) {
     const int32_t blocks = seen > kb ? (seen - kb + kBlock - 1) / kBlock : 0;
     const int32_t own = blocks > warp ? (blocks - warp - 1) / W + 1 : 0;             // this warp's: warp, warp + W, ...
 
-    // ---- copies, on their way before the queries are read: block i of this warp starts at key kb + 16 (warp + W i).  Where 32 of them stand is looked up at a time, a lane each, in
-    // units of 128 bytes (kNoPage: there is none) and of 64 for the scales.
+    // ---- copies, on their way before the queries are read: block i of this warp starts at key kb + 16 (warp + W i).  Where 32 of them stand is looked
+    // up at a time, a lane each, in units of 128 bytes (kNoPage: there is none) and of 64 for the scales.
     uint32_t places = kNoPage, scale_places = 0u;
     uint32_t missing = 0u;                                       // a bit per block fetched, the last one lowest: it has no page
     uint32_t into = ring + R::BYTES - R::STAGE;                  // the stage that was filled last
