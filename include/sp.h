@@ -642,8 +642,9 @@ sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const sp_mat* W,
  * O = 0 and lse = -infinity, rows of no sequence are left as they were, and what stands in slots that a query does not see does not reach it.
  * 4 bits or 16, the values are those that the cache stands for.  Softmax and sums in fp32.  Roundings: SP_F32 none but those of fp32 products and
  * sums.  SP_BF16 with 16 bits: probabilities to bf16.  SP_BF16 with 4 bits: probabilities times scales to fp16; queries (2^-16 of a row's
- * largest value is kept at least); with many rows probabilities, queries and opened values to fp16 in units of powers of two that the largest of the
- * call sets (values below 2^-28 of that lose bits).  Equal calls give equal bits.
+ * largest value is kept at least); with many rows probabilities and opened values to fp16 in units of powers of two of a text's key head, queries in units of
+ * a row and head (2^-28 of the largest keep all bits), or all three to bf16 where the sizes of a text's key head, by groups of 64 channels, lie
+ * further apart than 2^20.  Equal calls give equal bits, and no bit of a text's rows depends on another text's pages.
  * Many bf16 rows per sequence (more than 32 to 128 queries x heads of a key head, on average) open the pages in the workspace: max_keys tells how
  * many keys all sequences with queries have at most (0: as many as the table holds); sequences that do not fit are reported like tokens without a page.
  * Workspace: sp_cache_attention_bytes of the same numbers, scratch of this call alone.

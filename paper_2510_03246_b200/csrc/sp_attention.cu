@@ -380,8 +380,8 @@ Cut plan_cut(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_k
 size_t attention_workspace(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype, int64_t keys) {
   return plan_cut(Nq, Nk, n_seq, n_heads, n_kv, dh, dtype, keys).bytes;
 }
-sp_status attention_forward(const sp_attention_args* a, const uint32_t* half_tops, int64_t keys, int32_t* status_dev, void* ws, size_t ws_bytes,
-                            cudaStream_t s) {
+sp_status attention_forward(const sp_attention_args* a, const HalfTops* half_tops, const float* half_q, int64_t keys, int32_t* status_dev, void* ws,
+                            size_t ws_bytes, cudaStream_t s) {
   if (!a) return SP_ERR_INVALID_ARG;
   const int32_t dt = a->Q.dtype;
   if (dt != SP_F32 && dt != SP_BF16) return SP_ERR_DTYPE;
@@ -411,7 +411,7 @@ sp_status attention_forward(const sp_attention_args* a, const uint32_t* half_top
   // (a single row has no pitch: whatever stands there is not used)
   p.ldq = Nq > 1 ? a->Q.ld : a->Q.cols; p.ldk = Nk > 1 ? a->K.ld : a->K.cols;
   p.ldv = Nk > 1 ? a->V.ld : a->V.cols; p.ldo = Nq > 1 ? a->O.ld : a->O.cols;
-  p.half_tops = half_tops;
+  p.half_tops = half_tops; p.half_q = half_q;
   p.lse = a->lse;
   p.cu_q = a->cu_q; p.cu_k = a->cu_k;
   p.Nq = (int32_t)Nq; p.Nk = (int32_t)Nk;
@@ -461,7 +461,7 @@ size_t sp_attention_workspace_bytes(int64_t Nq, int64_t Nk, int32_t n_seq, int32
 }
 
 sp_status sp_attention(const sp_attention_args* a, int32_t* status_dev, void* ws, size_t ws_bytes, void* stream) {
-  return sp::attention_forward(a, nullptr, 0, status_dev, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+  return sp::attention_forward(a, nullptr, nullptr, 0, status_dev, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -4,6 +4,33 @@
 
 namespace sp {
 
+// fp16 operands opened from a cache of 4 bits: values in units of a power of two that takes the largest one to 2^14 .. 2^15.  Queries have a unit
+// for every row and head; keys and values one for every text and key head, by the least and the largest size that their groups of 64 channels may reach
+// there (fp32 bits; groups of zeros and non-finite ones do not count).  Sizes that lie further apart than 2^kHalfSpan would leave fp16: that text's head is
+// then opened in bf16, its queries and probabilities are bf16 too, and all units are 1.  (At 2^20 the least group's values are still off by no more
+// than 2^-15 of its size, beside 2^-9 of a value in bf16.)  What another text, another head or a key that a query does not see
+// holds thus never takes a value's bits.
+struct alignas(16) HalfTops {
+  uint32_t k_top, k_low, v_top, v_low;
+};
+struct HalfUnits {
+  float k, v;                  // values of a unit
+  int32_t half;                // 0: bf16
+};
+constexpr int kHalfSpan = 20;
+constexpr uint32_t kNoLow = 0x7f800000u;       // of a text without keys, beside a top of 0
+#ifdef __CUDACC__
+__device__ __forceinline__ int half_exponent(uint32_t top) { return top == 0u ? 0 : max((int)(top >> 23) - 127, -100) - 14; }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // e in -126 .. 127
+__device__ __forceinline__ bool half_holds(const HalfTops& t) {
+  return (int)(t.k_top >> 23) - (int)(t.k_low >> 23) <= kHalfSpan && (int)(t.v_top >> 23) - (int)(t.v_low >> 23) <= kHalfSpan;
+}
+__device__ __forceinline__ HalfUnits half_units(const HalfTops& t) {
+  if (!half_holds(t)) return HalfUnits{1.f, 1.f, 0};
+  return HalfUnits{power_of_two(half_exponent(t.k_top)), power_of_two(half_exponent(t.v_top)), 1};
+}
+#endif
+
 struct AttnParams {
   const void *q, *k, *v;
   void* o;
@@ -20,23 +47,16 @@ struct AttnParams {
   float* part_lse;             // [max_parts, Nq, n_heads]
   int32_t* status;
   long long wait_budget;
-  const uint32_t* half_tops;   // tcgen05 form: operands are fp16 in units (half_unit) of these maxima of queries, keys and values; null: bf16
+  const HalfTops* half_tops;   // tcgen05 form: operands opened from 4 bits, [n_seq, n_kv]; null: bf16
+  const float* half_q;         // [Nq, n_heads] units of the queries
 };
-
-// fp16 operands opened from a cache of 4 bits: values in units of the power of two that takes the largest one (its fp32 bits) to 2^14 .. 2^15.
-constexpr int kTopQ = 0, kTopK = 1, kTopV = 2;
-#ifdef __CUDACC__
-__device__ __forceinline__ int half_exponent(uint32_t top) { return top == 0u ? 0 : max((int)(top >> 23) - 127, -100) - 14; }
-__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // e in -126 .. 127
-__device__ __forceinline__ float half_unit(uint32_t top) { return power_of_two(half_exponent(top)); }
-__device__ __forceinline__ float half_per_unit(uint32_t top) { return power_of_two(-half_exponent(top)); }
-#endif
 
 // One piece of work: a tile of a sequence's rows (queries x the heads that share a key head, head fastest), one key / value
 // head, one part of the keys.
 struct AttnItem {
   int32_t q0, nq, k0, nk;           // first row of the sequence in Q and K, their numbers
   int32_t head, tile, c;            // key / value head, tile of rows, part of keys
+  int32_t s;                        // sequence
 };
 
 // Deals the items of a call in a fixed order: 32 sequences at a time; among them, tiles of rows from the last to the first (by number: with the
@@ -110,6 +130,7 @@ struct AttnDealer {
         const int of_parts = __shfl_sync(0xffffffffu, parts, l);
         rest -= __shfl_sync(0xffffffffu, upto - mine, l);
         it.tile = level;
+        it.s = base + l;
         it.head = (int)quotient(rest, of_parts);
         it.c = (int)(rest - (int64_t)it.head * of_parts);
         return true;
@@ -132,10 +153,10 @@ cudaError_t attention_rows_f32(const AttnParams& p, cudaStream_t stream);
 // tcgen05 form (sp_attention_tc.cu): layouts that tensor maps can describe
 bool attention_tc_supported(const AttnParams& a);
 sp_status attention_tc(const AttnParams& a, cudaStream_t stream);
-// sp_attention (half_tops null), or with fp16 operands in the places and pitches of Q, K and V, always by the tcgen05 form.  keys: how many of K's
+// sp_attention (half_tops null), or with operands opened from 4 bits in the places and pitches of Q, K and V, always by the tcgen05 form.  keys: how many of K's
 // rows a single sequence has, as the caller knows it; 0: not known.  Both calls get the same.
 size_t attention_workspace(int64_t Nq, int64_t Nk, int32_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int32_t dtype, int64_t keys);
-sp_status attention_forward(const sp_attention_args* a, const uint32_t* half_tops, int64_t keys, int32_t* status_dev, void* ws, size_t ws_bytes,
-                            cudaStream_t stream);
+sp_status attention_forward(const sp_attention_args* a, const HalfTops* half_tops, const float* half_q, int64_t keys, int32_t* status_dev, void* ws,
+                            size_t ws_bytes, cudaStream_t stream);
 
 }  // namespace sp

@@ -22,12 +22,15 @@
 // What bounds it: per half and tile 128 exponentials a row (1024 cycles of the pipe that two warps share) between two products (1024 cycles
 // together for heads of 128).  One prompt of 8192, 32 heads of 128 on 8: 488 us after a pause, 531 in a row of calls (power cap); 16 documents of up to
 // 2048 tokens, 32 heads of 64 on 8: 167 and 156 us.  (Figures beside the steps below are of the kernel of that time.)
-// HALF: operands opened from a cache of 4 bits, fp16 in units that its maxima give (AttnParams::half_tops): the same instructions with eight times
-// finer roundings, of P as well, whose reference leaves it 2^6 higher so that its small values keep theirs.
+// HALF: operands opened from a cache of 4 bits, fp16 in units of a text's key head and of a row's queries (HalfTops): the same instructions with
+// eight times finer roundings, of P as well, whose reference leaves it 2^6 higher so that its small values keep theirs.  A text's head whose
+// sizes leave fp16 comes in bf16: the format is an item's.
 // Waits for copies, the tensor core and other warps are bounded by a clock budget (SP_ERR_TIMEOUT through status).
 #include <cuda_fp16.h>
 #include <math.h>
 #include <string.h>
+
+#include <type_traits>
 
 #include "sp_attention.cuh"
 #include "sp_f32x2.cuh"
@@ -127,9 +130,10 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {      
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// bf16 or fp16 operands, fp32 accumulator, 128 x n; B K-major or (V: keys are K, channels contiguous) MN-major
-__device__ __forceinline__ uint32_t instr_desc(bool b_kmajor, int n, bool half) {
-  return (1u << 4) | (half ? 0u : (1u << 7) | (1u << 10)) | ((b_kmajor ? 0u : 1u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+// fp16 or (kBf16) bf16 operands, fp32 accumulator, 128 x n; B K-major or (V: keys are K, channels contiguous) MN-major
+constexpr uint32_t kBf16 = (1u << 7) | (1u << 10);
+__device__ __forceinline__ uint32_t instr_desc(bool b_kmajor, int n) {
+  return (1u << 4) | ((b_kmajor ? 0u : 1u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
 }
 
 struct TcAttnParams {
@@ -187,6 +191,7 @@ __device__ __forceinline__ int64_t item_of(int k) {
 // this in shared memory before the item's Q): key tiles of each half, 0 and 0 behind the last item, and the first edge tile.
 struct Brief {
   int n0, n1, edge;
+  uint32_t type;             // of the operands: 0, kBf16
 };
 constexpr int kBriefs = 8;             // more than the buffers of S: items between the issue of S and of P V
 
@@ -232,6 +237,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   __shared__ int s_abort;
   __shared__ Brief s_brief[kBriefs];
   __shared__ AttnItem s_item[kItems];    // tile < 0: no more
+  __shared__ HalfUnits s_units[HALF ? kItems : 1];
   __shared__ int s_bad[kBadSlots];       // slot of an item: its number where V had non-finite values behind the mask
 
   const uint32_t raw = smem_u32(smem_raw);
@@ -317,9 +323,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       for (int k = 0;; ++k) {
         const bool more = dealer.find(p.a, item_of(k), 2 * p.tokens, 1, p.heads, it);
         if (!more) it.tile = -1;
+        const int kvh = p.gp == 1 ? it.head / p.a.g : it.head;
+        HalfUnits units = {1.f, 1.f, 0};
+        if (HALF && more && lane == 0) units = half_units(p.a.half_tops[(int64_t)it.s * p.a.n_kv + kvh]);
         if (lane == 0) {
           if (k >= kItems) ok = mbar_wait(item_empty(k), (uint32_t)(k / kItems - 1) & 1u, abort_flag, budget);
           s_item[k % kItems] = it;
+          if (HALF) s_units[k % kItems] = units;
           if (ok) mbar_arrive(item_full(k));
         }
         ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
@@ -328,11 +338,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const int n = w.tiles();
         if (n == 0) continue;
         if (lane == 0) {
-          const int kvh = p.gp == 1 ? it.head / p.a.g : it.head;
           if (loaded > 0) ok = mbar_wait(q_empty, (uint32_t)(loaded - 1) & 1u, abort_flag, budget);
           if (ok) {
             const int halves = w.alone ? 1 : 2;
-            s_brief[loaded % kBriefs] = Brief{w.n[0], w.n[1], w.sure > w.kb ? (w.sure - w.kb) / kKeys : 0};
+            s_brief[loaded % kBriefs] = Brief{w.n[0], w.n[1], w.sure > w.kb ? (w.sure - w.kb) / kKeys : 0, HALF && units.half ? 0u : kBf16};
             mbar_expect_tx(q_full, (uint32_t)(halves * C::CH * p.gp * p.tokens * 128));
             for (int h = 0; h < halves; ++h)
   #pragma unroll
@@ -357,7 +366,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       }
       if (ok && lane == 0) {      // no more
         if (loaded > 0) ok = mbar_wait(q_empty, (uint32_t)(loaded - 1) & 1u, abort_flag, budget);
-        s_brief[loaded % kBriefs] = Brief{0, 0, 0};
+        s_brief[loaded % kBriefs] = Brief{0, 0, 0, 0u};
         if (ok) mbar_arrive(q_full);
       }
       if (!ok && lane == 0) report_status(p.a.status, SP_ERR_TIMEOUT, (int32_t)blockIdx.x, 11);
@@ -370,7 +379,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       // for both halves was better than a warp for each, whose instructions alternate (519 us, 189).
       bool ok = true;
       if (elect_one()) {
-        const uint32_t id_s = instr_desc(true, kKeys, HALF), id_o = instr_desc(false, DH, HALF);
+        const uint32_t id_s0 = instr_desc(true, kKeys), id_o0 = instr_desc(false, DH);
         uint32_t full_ph = 0, ready_ph = 0, p_ph = 0;    // phases of the barriers of a stage, of a buffer: a bit each
         int items_s = 0, items_v = 0;                    // items that the cursors have been given
         int ahead = 0;                                   // jobs whose S is issued and whose P V is not
@@ -388,7 +397,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         auto issue_s = [&] {
           const int s = cs.stage;
           const uint32_t a0 = desc_low(q_smem + cs.h * C::TILE, 16), b0 = desc_low(ring + s * C::TILE, 16);
-          const uint32_t d = tmem + 128u * cs.b;
+          const uint32_t d = tmem + 128u * cs.b, id_s = id_s0 | (HALF ? cs.w.type : kBf16);
 #pragma unroll
           for (int k = 0; k < DH / 16; ++k) {
             const uint32_t off = (uint32_t)((k / 4) * C::CHUNK + (k % 4) * 32) >> 4;
@@ -432,7 +441,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (!ok) break;
               }
               // (P of a half's first key tile also says that its warps have read O of the item before)
-              const uint32_t d = tmem + C::O_COL + C::O_COLS * cv.h, a0 = tmem + 128u * cv.b;
+              const uint32_t d = tmem + C::O_COL + C::O_COLS * cv.h, a0 = tmem + 128u * cv.b, id_o = id_o0 | (HALF ? cv.w.type : kBf16);
               const uint32_t v0 = desc_low(ring + s * C::TILE, C::CHUNK);
               tc_fence_after();
 #pragma unroll
@@ -481,6 +490,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       bool ok = true;
       long long patience = budget;                     // (these warps wait for as long as the others work on an item)
       for (int k = 0; ok && next_item(k, ok, patience); ++k) {
+        // a bf16 (fp16) of all-ones exponent: its magnitude plus this reaches the sign bit
+        const uint32_t to_sign = HALF && s_units[k % kItems].half ? 0x04000400u : 0x00800080u;
         item_read(k);
         const Work w = work_of(p, it);
         const int n = w.tiles();
@@ -508,8 +519,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                   *at = make_uint4(0u, 0u, 0u, 0u);
                 } else {
                   const uint4 v = *at;
-                  // a bf16 (fp16) of all-ones exponent: its magnitude plus 0x80 (0x400) reaches the sign bit
-                  auto mark = [](uint32_t u) { return ((u & 0x7fff7fffu) + (HALF ? 0x04000400u : 0x00800080u)) & 0x80008000u; };
+                  auto mark = [to_sign](uint32_t u) { return ((u & 0x7fff7fffu) + to_sign) & 0x80008000u; };
                   if (mark(v.x) | mark(v.y) | mark(v.z) | mark(v.w)) {
                     auto fix = [&](uint32_t u) {
                       const uint32_t b = mark(u);
@@ -537,14 +547,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const int row = q * 32 + lane;                   // of the half, and lane of tensor memory
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     const uint32_t t_o = tmem + C::O_COL + C::O_COLS * h + lanes;
-    const float c = HALF ? p.a.scale_log2 * half_unit(p.a.half_tops[kTopQ]) * half_unit(p.a.half_tops[kTopK]) : p.a.scale_log2;
     uint32_t s_ph = 0, pv_ph = 0, jobs = 0;          // (of a buffer: a bit each; jobs of the items before)
     bool ok = true;
-    const uint64_t c2 = pack2(c, c);
     int waits = 0;                                   // key tiles of the item before: half 1 waits for as long as half 0 works on one alone
     for (int k = 0; ok && next_item(k, ok, budget + 20000ll * waits); ++k) {
       int lim, n, n0, kb;                            // (a row of S leaves few registers: the rest is derived again for the output)
       bool alone, busy;
+      float c = p.a.scale_log2;                      // of a value of S to base 2
       {
         const Work w = work_of(p, it);
         const int token = w.t0 + h * p.tokens + row / p.gp;
@@ -555,7 +564,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         n = h ? w.n[1] : n0;
         kb = w.kb;
         alone = w.alone;
+        if (HALF) {
+          const int head = p.gp == 1 ? it.head : it.head * p.gp + row % p.gp;
+          c *= s_units[k % kItems].k * (valid ? p.a.half_q[((int64_t)it.q0 + token) * p.a.n_heads + head] : 1.f);
+          if (c < 1.2e-38f) c = 1.2e-38f;            // (0 times the mask's -infinity would be NaN; S is below 2^38)
+        }
       }
+      const uint64_t c2 = pack2(c, c);
       float r = -INFINITY, l = 0.f;                  // reference (not yet times c) and sum
       for (int i = 0; i < n; ++i) {
         const int b_ = (int)((jobs + (alone ? i : i < n0 ? 2 * i + h : n0 + i)) % C::BUFS);      // the buffer of the job
@@ -621,6 +636,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           const float shift = r == -INFINITY ? 0.f : HALF ? fmaf(-r, c, kHalfLift) : -r * c;
           const uint64_t shift2 = pack2(shift, shift);
           uint64_t l2[2] = {pack2(l, 0.f), pack2(0.f, 0.f)};
+          const auto put_p = [&](auto fp16) {
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             uint32_t w16[16];
@@ -632,7 +648,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               e0 = exp2_fast(e0);
               e1 = exp2_fast(e1);
               l2[j & 1] = add2(l2[j & 1], pack2(e0, e1));
-              if constexpr (HALF) {
+              if constexpr (decltype(fp16)::value) {
                 const __half2 e = __floats2half2_rn(e0, e1);
                 w16[j] = *reinterpret_cast<const uint32_t*>(&e);
               } else {
@@ -649,6 +665,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
             if (b >= 2) tc_st16(t_s + 16u * b, w16);
           }
+          };
+          if (HALF && s_units[k % kItems].half) put_p(std::integral_constant<bool, HALF>());
+          else put_p(std::false_type());
           float l0, l1;
           unpack2(add2(l2[0], l2[1]), l0, l1);
           l = l0 + l1;
@@ -672,7 +691,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const bool cut = p.a.part > 0 && it.nk > p.a.part;
       // no key seen: no reference r.  With one, 2^(c (x - r)) of the row's largest logit is 1 or more, unless c r is beyond fp32: then the row is NaN.
       const bool none = r == -INFINITY;
-      const float unit = HALF ? half_unit(p.a.half_tops[kTopV]) : 1.f;
+      const bool half = HALF && s_units[k % kItems].half;
+      const float unit = HALF ? s_units[k % kItems].v : 1.f;
       const float inv = l == 0.f ? NAN : unit / l;
       const float lse2 = none ? -INFINITY : l == 0.f ? NAN : fmaf(r, c, log2f(l) - (HALF ? kHalfLift : 0.f));
       __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.o) + out_row * p.a.ldo + (int64_t)head * p.a.dh;
@@ -710,7 +730,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             for (int key = max(w.sure, w.kb); key < lim; ++key)
 #pragma unroll 1
               for (int j = 0; j < 32 && 32 * b + j < p.a.dh; ++j) {
-                const float v = HALF ? __half2float(reinterpret_cast<const __half*>(V)[((int64_t)it.k0 + key) * p.a.ldv + j])
+                const float v = half ? __half2float(reinterpret_cast<const __half*>(V)[((int64_t)it.k0 + key) * p.a.ldv + j])
                                      : __bfloat162float(V[((int64_t)it.k0 + key) * p.a.ldv + j]);
                 if (!(fabsf(v) < INFINITY)) {
 #pragma unroll

@@ -373,7 +373,7 @@ struct ReadParams {
   int64_t ldk, ldv;
   int32_t rows, whole, k_vec, v_vec;
   Divisor head;                            // chunks of a head
-  const uint32_t* tops;
+  const HalfTops* tops;
   int32_t* status;
 };
 // The eight values of a word of numbers, one rounding each: scale n + zero.  A number is put in the place of a mantissa's bits of 2^23, 2^19 ..,
@@ -387,7 +387,7 @@ __device__ __forceinline__ void open8(uint32_t w, uint32_t pair, float (&x)[8]) 
     x[k] = fmaf(__uint_as_float((from & (15u << at)) | ((150u - at) << 23)) - (float)(1 << (23 - at)), scale, zero);
   }
 }
-// The same in fp16, in units of 1 / f: scales and offsets fit into it but for what lies 2^-28 below the largest.
+// The same in fp16, in units of 1 / f: scales and offsets fit into it but for what lies 2^-28 below the largest of the text's head.
 __device__ __forceinline__ void open8_half(__half* p, uint32_t w, uint32_t pair, float f) {
   const __half2 scale = __float2half2_rn(__uint_as_float(pair << 16) * f), zero = __float2half2_rn(__uint_as_float(pair & 0xffff0000u) * f);
   __half2 x[4];                            // channels i and i + 4
@@ -400,10 +400,10 @@ __device__ __forceinline__ void open8_half(__half* p, uint32_t w, uint32_t pair,
   *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(y);
 }
 
-constexpr uint32_t kNan2 = 0x7fff7fffu;   // two of fp16
+constexpr uint32_t kNan2 = 0x7fff7fffu;   // two of fp16, or of bf16
 
 // a warp per row: eight channels of keys and of values at a time in every lane (more warps at once are worth more than two chunks of a lane in
-// flight: 17k rows of 8 heads of 128 to fp16 20 us, unrolled 23).  T of fp16: contiguous rows in units of tops.
+// flight: 17k rows of 8 heads of 128 to fp16 20 us, unrolled 23).  T of fp16: contiguous rows in the units that tops give, or of bf16.
 template <typename T, bool FOUR>
 __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
   kernel_begin();
@@ -419,7 +419,6 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
   const int32_t slot = place - entry * p.c.page_len;
   if (page < 0 && lane == 0) report_status(p.status, SP_ERR_SHAPE, s, entry);
   constexpr bool HALF = std::is_same<T, __half>::value;
-  const float fk = HALF ? half_per_unit(p.tops[kTopK]) : 1.f, fv = HALF ? half_per_unit(p.tops[kTopV]) : 1.f;
   const int dh = p.c.dh, chunks = p.c.n_kv * (dh / 8);
   T *k_row = reinterpret_cast<T*>(p.k) + row * p.ldk, *v_row = reinterpret_cast<T*>(p.v) + row * p.ldv;
 #pragma unroll 1
@@ -435,20 +434,27 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
       const uint32_t a = *reinterpret_cast<const uint32_t*>(p.c.k + from), b = *reinterpret_cast<const uint32_t*>(p.c.v + from);
       const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + g), sb = *reinterpret_cast<const uint32_t*>(p.c.vs + g);
       if constexpr (HALF) {
-        open8_half(k_row + 8 * e, a, sa, fk);
-        open8_half(v_row + 8 * e, b, sb, fv);
-        continue;
-      } else {
-        open8(a, sa, x);
-        open8(b, sb, y);
+        const HalfTops t = p.tops[(int64_t)s * p.c.n_kv + head];
+        if (half_holds(t)) {
+          open8_half(k_row + 8 * e, a, sa, power_of_two(-half_exponent(t.k_top)));
+          open8_half(v_row + 8 * e, b, sb, power_of_two(-half_exponent(t.v_top)));
+          continue;
+        }
       }
+      open8(a, sa, x);
+      open8(b, sb, y);
     } else {
       const int64_t from = page * p.c.step + (at * dh + 8 * chunk) * 2;
       load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.k + from), true, x);
       load8<true>(reinterpret_cast<const __nv_bfloat16*>(p.c.v + from), true, y);
     }
     if constexpr (HALF) {
-      *reinterpret_cast<uint4*>(k_row + 8 * e) = *reinterpret_cast<uint4*>(v_row + 8 * e) = make_uint4(kNan2, kNan2, kNan2, kNan2);
+      if (page < 0) {
+        *reinterpret_cast<uint4*>(k_row + 8 * e) = *reinterpret_cast<uint4*>(v_row + 8 * e) = make_uint4(kNan2, kNan2, kNan2, kNan2);
+      } else {
+        put8<true>(reinterpret_cast<__nv_bfloat16*>(k_row) + 8 * e, true, x);
+        put8<true>(reinterpret_cast<__nv_bfloat16*>(v_row) + 8 * e, true, y);
+      }
     } else {
       put8<false>(k_row + 8 * e, p.k_vec != 0, x);
       put8<false>(v_row + 8 * e, p.v_vec != 0, y);
@@ -456,94 +462,127 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
   }
 }
 
-// Largest finite |value| of the queries, and bounds 15 |scale| + |zero| of the keys and values of the rows that cache_open opens.  The first
-// `q_blocks` blocks take the queries, the others keys: a warp takes one key head of 32 rows, a row to a lane, since a head's scales of the rows of a
-// page stand side by side; with a row to a warp every 8 bytes come in a sector of their own.  A block's maxima meet in shared memory: an atomic of
-// each warp queues at three words.  (A maximum is the same in any order.)
+// Least and largest bound 15 |scale| + |zero| of the keys and of the values of every text and key head, among the rows that cache_open opens.  A block
+// takes one key head of 256 rows at a time, a row to a thread, since a head's scales of the rows of a page stand side by side; with a row to a
+// warp every 8 bytes come in a sector of their own.  A block's bounds of one text meet in shared memory: an atomic of each warp queues at
+// a few words.  (Maxima and minima are the same in any order.)
 struct TopsParams {
   CacheView c;
   const int32_t* cu;
-  const __nv_bfloat16* q;
-  int64_t ldq, q_rows;
-  int32_t q_cols, q_blocks, q_vec, rows;
-  uint32_t* tops;
+  int32_t rows, strips;
+  HalfTops* tops;
 };
 __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
   kernel_begin();
+  __shared__ int s_seq;
+  __shared__ HalfTops s_tops[8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float a = 0.f, b = 0.f;
-  const auto take = [](float& top, float v) {
-    if (v < INFINITY) top = fmaxf(top, v);                       // (not a NaN either)
+  const int32_t head = (int32_t)(blockIdx.x % (uint32_t)p.c.n_kv), strip = (int32_t)(blockIdx.x / (uint32_t)p.c.n_kv);
+  const int per_head = p.c.dh / kCacheGroup;
+  const HalfTops none = {0u, kNoLow, 0u, kNoLow};
+  HalfTops mine = none;
+  int32_t seq = -1;                        // the text that `mine` is of
+  const auto leave = [&](int32_t s, const HalfTops& t) {
+    HalfTops* to = p.tops + (int64_t)s * p.c.n_kv + head;
+    if (t.k_top != 0u) atomicMax(&to->k_top, t.k_top);
+    if (t.k_low != kNoLow) atomicMin(&to->k_low, t.k_low);
+    if (t.v_top != 0u) atomicMax(&to->v_top, t.v_top);
+    if (t.v_low != kNoLow) atomicMin(&to->v_low, t.v_low);
   };
-  const bool queries = (int)blockIdx.x < p.q_blocks;
-  if (queries) {
-    const int64_t chunks = p.q_rows * (p.q_cols / 8);            // (heads are whole chunks)
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < chunks; e += (int64_t)p.q_blocks * 256) {
-      const int64_t row = e / (p.q_cols / 8), j = e - row * (p.q_cols / 8);
-      float x[8];
-      load8<false>(p.q + row * p.ldq + 8 * j, p.q_vec != 0, x);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) take(a, fabsf(x[k]));
+  const auto take = [](uint32_t& top, uint32_t& low, uint32_t pair) {
+    const float scale = fabsf(__uint_as_float(pair << 16)), zero = fabsf(__uint_as_float(pair & 0xffff0000u));
+    if (!(scale < INFINITY) || !(zero < INFINITY)) return;                // (a NaN either)
+    const uint32_t bits = __float_as_uint(fminf(fmaf(15.f, scale, zero), 3.402823466e38f));
+    top = max(top, bits);
+    if (bits != 0u) low = min(low, bits);
+  };
+  for (int64_t row = (int64_t)strip * 256 + threadIdx.x; row < p.rows; row += (int64_t)p.strips * 256) {
+    const int32_t s = sequence_near(p.cu, p.c.n_seq, p.rows, row);        // (cu[0] is 0)
+    const int32_t first = bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - first;
+    if (row >= first + n || n != p.c.lens[s]) continue;
+    const int32_t place = (int32_t)row - first, entry = place / p.c.page_len, page = page_of(p.c, s, entry);
+    if (page < 0) continue;
+    if (s != seq) {
+      if (seq >= 0) leave(seq, mine);
+      mine = none;
+      seq = s;
     }
-  } else {
-    const int per_head = p.c.dh / kCacheGroup;
-    const int64_t items = ceil_div((int64_t)p.rows, (int64_t)32) * p.c.n_kv, step = ((int64_t)gridDim.x - p.q_blocks) * 8;
-    for (int64_t item = ((int64_t)blockIdx.x - p.q_blocks) * 8 + warp; item < items; item += step) {
-      const int64_t row = item / p.c.n_kv * 32 + lane;
-      const int head = (int)(item % p.c.n_kv);
-      if (row >= p.rows) continue;
-      int32_t s = 0;                                             // the last one that starts no later (cu[0] is 0)
-      for (int32_t len = p.c.n_seq; len > 1;) {
-        const int32_t half = len / 2;
-        const bool there = bounded(p.cu[s + half], p.rows) <= row;
-        s += there ? half : 0;
-        len = there ? len - half : half;
-      }
-      if (row >= bounded(p.cu[s + 1], p.rows)) continue;
-      const int32_t place = (int32_t)row - bounded(p.cu[s], p.rows), entry = place / p.c.page_len, page = page_of(p.c, s, entry);
-      if (page < 0) continue;
-      const int64_t at = page * p.c.scale_step + ((int64_t)head * p.c.page_len + place - entry * p.c.page_len) * per_head * 4;
+    const int64_t at = page * p.c.scale_step + ((int64_t)head * p.c.page_len + place - entry * p.c.page_len) * per_head * 4;
 #pragma unroll 2
-      for (int g = 0; g < per_head; ++g) {
-        const uint32_t sa = *reinterpret_cast<const uint32_t*>(p.c.ks + at + 4 * g), sb = *reinterpret_cast<const uint32_t*>(p.c.vs + at + 4 * g);
-        take(a, fmaf(15.f, fabsf(__uint_as_float(sa << 16)), fabsf(__uint_as_float(sa & 0xffff0000u))));
-        take(b, fmaf(15.f, fabsf(__uint_as_float(sb << 16)), fabsf(__uint_as_float(sb & 0xffff0000u))));
-      }
+    for (int g = 0; g < per_head; ++g) {
+      take(mine.k_top, mine.k_low, *reinterpret_cast<const uint32_t*>(p.c.ks + at + 4 * g));
+      take(mine.v_top, mine.v_low, *reinterpret_cast<const uint32_t*>(p.c.vs + at + 4 * g));
     }
   }
-#pragma unroll
-  for (int w = 16; w > 0; w >>= 1) {
-    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, w));
-    b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, w));
-  }
-  __shared__ float s_top[2][8];
-  if (lane == 0) {
-    s_top[0][warp] = a;
-    s_top[1][warp] = b;
-  }
+  // the lanes that have the same text, then the warps where all of the block has
+  const uint32_t peers = __match_any_sync(0xffffffffu, seq);
+  mine.k_top = __reduce_max_sync(peers, mine.k_top);
+  mine.k_low = __reduce_min_sync(peers, mine.k_low);
+  mine.v_top = __reduce_max_sync(peers, mine.v_top);
+  mine.v_low = __reduce_min_sync(peers, mine.v_low);
+  if (threadIdx.x == 0) s_seq = -1;
   __syncthreads();
-  if (threadIdx.x < (queries ? 1 : 2)) {
-    float top = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, s_top[threadIdx.x][w]);
-    atomicMax(p.tops + (queries ? kTopQ : threadIdx.x == 0 ? kTopK : kTopV), __float_as_uint(top));
+  if (seq >= 0) atomicMax(&s_seq, seq);
+  if (lane == 0) s_tops[warp] = none;
+  __syncthreads();
+  const int32_t text = s_seq;
+  const bool whole = __syncthreads_and(seq < 0 || seq == text) != 0, first = seq >= 0 && lane == __ffs(peers) - 1;
+  if (!whole) {
+    if (first) leave(seq, mine);
+    return;
   }
+  if (first) s_tops[warp] = mine;
+  __syncthreads();
+  if (threadIdx.x != 0 || text < 0) return;
+  HalfTops all = none;
+  for (int w = 0; w < 8; ++w) {
+    all.k_top = max(all.k_top, s_tops[w].k_top);
+    all.k_low = min(all.k_low, s_tops[w].k_low);
+    all.v_top = max(all.v_top, s_tops[w].v_top);
+    all.v_low = min(all.v_low, s_tops[w].v_low);
+  }
+  leave(text, all);
 }
-__global__ void __launch_bounds__(256) queries_to_half_kernel(const __nv_bfloat16* q, int64_t ldq, int64_t rows, int32_t cols, int32_t vec, __half* out,
-                                                              const uint32_t* tops) {
+struct QueriesParams {
+  const __nv_bfloat16* q;
+  const int32_t* cu_q;
+  const HalfTops* tops;
+  __half* out;
+  float* unit;
+  int64_t ldq, rows;
+  int32_t n_heads, n_kv, dh, n_seq, vec;
+};
+// eight channels to a thread, the 8 or 16 threads of a head side by side in a warp
+__global__ void __launch_bounds__(256) queries_to_half_kernel(const QueriesParams p) {
   kernel_begin();
-  const float f = half_per_unit(tops[kTopQ]);
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, row = e / (cols / 8), j = e - row * (cols / 8);
-  if (row >= rows) return;
-  float x[8];
-  load8<false>(q + row * ldq + 8 * j, vec != 0, x);
+  const int32_t per_head = p.dh / 8, per_row = p.n_heads * per_head;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = min(e / per_row, p.rows - 1);              // (lanes behind the end stay for the shuffles)
+  const int32_t j = (int32_t)(e % per_row), head = j / per_head;
+  float x[8], top = 0.f;
+  load8<false>(p.q + row * p.ldq + 8 * j, p.vec != 0, x);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (fabsf(x[k]) < INFINITY) top = fmaxf(top, fabsf(x[k]));
+  for (int w = 1; w < per_head; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+  if (e >= p.rows * per_row) return;
+  const int32_t s = sequence_near(p.cu_q, p.n_seq, (int32_t)p.rows, row);
+  const bool half = half_holds(p.tops[(int64_t)s * p.n_kv + head / (p.n_heads / p.n_kv)]);
+  const int unit = half ? half_exponent(__float_as_uint(top)) : 0;
+  if (j % per_head == 0) p.unit[row * p.n_heads + head] = power_of_two(unit);
+  __half* to = p.out + row * ((int64_t)p.n_heads * p.dh) + 8 * j;
+  if (!half) {
+    put8<true>(reinterpret_cast<__nv_bfloat16*>(to), true, x);
+    return;
+  }
+  const float f = power_of_two(-unit);
   uint32_t u[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const __half2 y = __floats2half2_rn(x[2 * i] * f, x[2 * i + 1] * f);
     u[i] = *reinterpret_cast<const uint32_t*>(&y);
   }
-  *reinterpret_cast<uint4*>(out + row * cols + 8 * j) = make_uint4(u[0], u[1], u[2], u[3]);
+  *reinterpret_cast<uint4*>(to) = make_uint4(u[0], u[1], u[2], u[3]);
 }
 
 bool rows_of_16(const void* ptr, int64_t ld, int32_t dtype, int64_t rows) {
@@ -590,7 +629,7 @@ CacheView cache_view(const sp_kv_cache* c) {
 
 namespace {
 cudaError_t read_rows(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype, bool whole,
-                      const uint32_t* tops, int32_t* status, cudaStream_t stream) {
+                      const HalfTops* tops, int32_t* status, cudaStream_t stream) {
   ReadParams p = {};
   p.c = cache_view(c);
   p.cu = cu;
@@ -617,31 +656,35 @@ cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, vo
                        int32_t* status, cudaStream_t stream) {
   return read_rows(c, cu, rows, K, V, ldk, ldv, dtype, false, nullptr, status, stream);
 }
-cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, const uint32_t* tops, int32_t* status,
+cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, const HalfTops* tops, int32_t* status,
                        cudaStream_t stream) {
   const int64_t ld = (int64_t)c->n_kv_heads * c->d_head;
   return read_rows(c, cu, rows, K, V, ld, ld, SP_BF16, true, tops, status, stream);
 }
-cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, const sp_mat* Q, uint32_t* tops, cudaStream_t stream) {
+cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, HalfTops* tops, cudaStream_t stream) {
   TopsParams p = {};
   p.c = cache_view(c);
   p.cu = cu;
-  p.q = reinterpret_cast<const __nv_bfloat16*>(Q->ptr);
-  p.ldq = Q->ld; p.q_rows = Q->rows; p.q_cols = (int32_t)Q->cols;
   p.rows = (int32_t)rows;
   p.tops = tops;
-  p.q_vec = rows_of_16(Q->ptr, Q->ld, SP_BF16, Q->rows);
-  const int64_t most = 4 * (int64_t)sm_count(), q = ceil_div(Q->rows * (Q->cols / 8), (int64_t)1024);
-  const int64_t k = ceil_div(ceil_div(rows, (int64_t)32) * c->n_kv_heads, (int64_t)8);
-  p.q_blocks = (int32_t)(q < most ? q : most);
+  const int64_t most = ceil_div(4 * (int64_t)sm_count(), (int64_t)c->n_kv_heads), strips = ceil_div(rows, (int64_t)256);
+  p.strips = (int32_t)(strips < most ? strips : most);
   count_launch();
-  return launch(cache_tops_kernel, dim3((unsigned)(p.q_blocks + (k < most ? k : most))), dim3(256), 0, stream, p);
+  return launch(cache_tops_kernel, dim3((unsigned)(p.strips * c->n_kv_heads)), dim3(256), 0, stream, p);
 }
-cudaError_t queries_to_half(const sp_mat* Q, void* Q_half, const uint32_t* tops, cudaStream_t stream) {
+cudaError_t queries_to_half(const sp_kv_cache* c, const sp_mat* Q, const int32_t* cu_q, void* Q_half, float* q_unit, const HalfTops* tops,
+                            cudaStream_t stream) {
+  QueriesParams p = {};
+  p.q = reinterpret_cast<const __nv_bfloat16*>(Q->ptr);
+  p.cu_q = cu_q;
+  p.tops = tops;
+  p.out = reinterpret_cast<__half*>(Q_half);
+  p.unit = q_unit;
+  p.ldq = Q->ld; p.rows = Q->rows;
+  p.n_heads = (int32_t)(Q->cols / c->d_head); p.n_kv = c->n_kv_heads; p.dh = c->d_head; p.n_seq = c->n_seq;
+  p.vec = rows_of_16(Q->ptr, Q->ld, SP_BF16, Q->rows);
   count_launch();
-  return launch(queries_to_half_kernel, dim3((unsigned)ceil_div(Q->rows * (Q->cols / 8), (int64_t)256)), dim3(256), 0, stream,
-                reinterpret_cast<const __nv_bfloat16*>(Q->ptr), Q->ld, Q->rows, (int32_t)Q->cols,
-                (int32_t)rows_of_16(Q->ptr, Q->ld, SP_BF16, Q->rows), reinterpret_cast<__half*>(Q_half), tops);
+  return launch(queries_to_half_kernel, dim3((unsigned)ceil_div(Q->rows * (Q->cols / 8), (int64_t)256)), dim3(256), 0, stream, p);
 }
 
 }  // namespace sp

@@ -31,6 +31,17 @@ __device__ __forceinline__ int32_t sequence_of(const int32_t* cu, int32_t n_seq,
     if (step == 1) return lo < n_seq ? lo : -1;
   }
 }
+// The same of every lane for itself, and any row: the last one that starts at or before it (the first one if none does).
+__device__ __forceinline__ int32_t sequence_near(const int32_t* cu, int32_t n_seq, int32_t rows, int64_t row) {
+  int32_t s = 0;
+  for (int32_t len = n_seq; len > 1;) {
+    const int32_t half = len / 2;
+    const bool there = bounded(cu[s + half], rows) <= row;
+    s += there ? half : 0;
+    len = there ? len - half : half;
+  }
+  return s;
+}
 // Page of a sequence's token, -1 where there is none: no such entry of the table, or one that names no page.
 __device__ __forceinline__ int32_t page_of(const CacheView& c, int32_t s, int32_t entry) {
   if (entry < 0 || entry >= c.max_pages) return -1;
@@ -46,11 +57,13 @@ CacheView cache_view(const sp_kv_cache* c);
 cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
                        int32_t* status, cudaStream_t stream);
 // The same for whole sequences into contiguous rows of bf16 (those of a sequence with another number of tokens than n are NaN); with tops as fp16 in
-// units of these maxima of keys and values (sp_attention.cuh), which cache_tops has found among the scales of the same rows and the queries Q, and
-// Q_half [Nq, n_heads * d_head] takes the queries alike.
-cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, const uint32_t* tops, int32_t* status,
+// the units that these give a text's key head, or bf16 (HalfTops, sp_attention.cuh).  cache_tops finds them among the scales of the same rows, and Q_half
+// [Nq, n_heads * d_head] takes the queries alike, q_unit [Nq, n_heads] their units.
+struct HalfTops;
+cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, const HalfTops* tops, int32_t* status,
                        cudaStream_t stream);
-cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, const sp_mat* Q, uint32_t* tops, cudaStream_t stream);
-cudaError_t queries_to_half(const sp_mat* Q, void* Q_half, const uint32_t* tops, cudaStream_t stream);
+cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, HalfTops* tops, cudaStream_t stream);
+cudaError_t queries_to_half(const sp_kv_cache* c, const sp_mat* Q, const int32_t* cu_q, void* Q_half, float* q_unit, const HalfTops* tops,
+                            cudaStream_t stream);
 
 }  // namespace sp

@@ -20,7 +20,7 @@
 // sums of 16 keys are added up outside the matrix unit.
 //
 // More rows of bf16 open the pages into rows of the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor cores' rate, where this
-// form would open them again for every 16 rows.  4 bits are opened into fp16 in units of the call's maxima (bf16 queries alike): rounded to bf16,
+// form would open them again for every 16 rows.  4 bits are opened into fp16 in units of a text's key head (bf16 queries in those of a row): rounded to bf16,
 // results were 4.2e-3 from the formula (512 queries after 16384 keys, 32 heads of 128 on 8), and as two bf16 parts each 2.3e-3, in 312 us instead of
 // 186; in fp16 they are 1.7e-3 from it.  (Rounded values of equal scales are all off by the same, which no sum over keys takes away.)
 #include <cuda_fp16.h>
@@ -1037,9 +1037,10 @@ cudaError_t launch_rows(const PagedParams& p, bool four, int rows, cudaStream_t 
 // cu_k of the opened keys: the lengths added up; a sequence that does not fit into max_keys (or has more tokens than its table) gets as many
 // rows as queries at most, which cache_read makes NaN: every query sees one of them.
 __global__ void __launch_bounds__(kPlanThreads) open_plan_kernel(const CacheView c, const int32_t* cu_q, int32_t Nq, int32_t max_keys, int32_t* cu_k,
-                                                             uint32_t* tops, int32_t* status) {
+                                                             HalfTops* tops, int32_t* status) {
   kernel_begin();
-  if (tops && threadIdx.x < 3) tops[threadIdx.x] = 0u;
+  if (tops)
+    for (int64_t i = threadIdx.x; i < (int64_t)c.n_seq * c.n_kv; i += kPlanThreads) tops[i] = HalfTops{0u, kNoLow, 0u, kNoLow};
   __shared__ int64_t s_word[kPlanThreads / 32];
   int64_t at = 0, used = 0;               // rows given to the sequences before, and their keys
   for (int32_t s0 = 0; s0 < c.n_seq; s0 += kPlanThreads) {
@@ -1064,16 +1065,19 @@ __global__ void __launch_bounds__(kPlanThreads) open_plan_kernel(const CacheView
 
 struct OpenPlan {
   int64_t rows;
-  size_t cu_bytes, k_bytes, q_bytes, attention;
-  size_t bytes() const { return cu_bytes + 2 * k_bytes + q_bytes + attention; }
+  size_t cu_bytes, tops_bytes, k_bytes, q_bytes, unit_bytes, attention;
+  size_t bytes() const { return cu_bytes + tops_bytes + 2 * k_bytes + q_bytes + unit_bytes + attention; }
 };
-// (room for the queries in fp16 whatever the cache is: the workspace depends on the sizes that its call is given)
+// (room for what 4 bits need whatever the cache is: the workspace depends on the sizes that its call is given)
 OpenPlan open_plan(int64_t Nq, int64_t n_seq, int32_t n_heads, int32_t n_kv, int32_t dh, int64_t max_keys) {
   OpenPlan r;
   r.rows = max_keys + Nq;
-  r.cu_bytes = align_up((size_t)(n_seq + 1) * 4 + 16, 256);      // and the three maxima behind the offsets
+  const bool four = dh % kCacheGroup == 0;
+  r.cu_bytes = align_up((size_t)(n_seq + 1) * 4, 256);
+  r.tops_bytes = four ? align_up((size_t)n_seq * n_kv * sizeof(HalfTops), 256) : 0;
   r.k_bytes = align_up((size_t)r.rows * n_kv * dh * 2, 256);
-  r.q_bytes = dh % kCacheGroup == 0 ? align_up((size_t)Nq * n_heads * dh * 2, 256) : 0;
+  r.q_bytes = four ? align_up((size_t)Nq * n_heads * dh * 2, 256) : 0;
+  r.unit_bytes = four ? align_up((size_t)Nq * n_heads * 4, 256) : 0;
   r.attention = attention_workspace(Nq, r.rows, (int32_t)n_seq, n_heads, n_kv, dh, SP_BF16, max_keys);
   return r;
 }
@@ -1151,15 +1155,18 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   const int64_t keys = keys_at_most(max_keys, n_seq, cache->max_pages, cache->page_len);
   const OpenPlan plan = open_plan(Nq, n_seq, n_heads, n_kv, dh, keys);
   int32_t* cu_k = reinterpret_cast<int32_t*>(at);
-  uint8_t *K = at + plan.cu_bytes, *V = K + plan.k_bytes, *Qh = V + plan.k_bytes, *rest = Qh + plan.q_bytes;
+  uint8_t *K = at + plan.cu_bytes + plan.tops_bytes, *V = K + plan.k_bytes, *Qh = V + plan.k_bytes, *units = Qh + plan.q_bytes;
+  uint8_t* rest = units + plan.unit_bytes;
   const int64_t kv = (int64_t)n_kv * dh;
   const bool half = cache->kind == SP_CACHE_4BIT;
-  uint32_t* tops = half ? reinterpret_cast<uint32_t*>(cu_k + n_seq + 1) : nullptr;
+  HalfTops* tops = half ? reinterpret_cast<HalfTops*>(at + plan.cu_bytes) : nullptr;
+  float* q_unit = half ? reinterpret_cast<float*>(units) : nullptr;
   count_launch();
   if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, tops, status_dev) !=
       cudaSuccess)
     return SP_ERR_CUDA;
-  if (half && (cache_tops(cache, cu_k, plan.rows, Q, tops, s) != cudaSuccess || queries_to_half(Q, Qh, tops, s) != cudaSuccess))
+  if (half && (cache_tops(cache, cu_k, plan.rows, tops, s) != cudaSuccess ||
+               queries_to_half(cache, Q, cu_q, Qh, q_unit, tops, s) != cudaSuccess))
     return SP_ERR_CUDA;
   if (cache_open(cache, cu_k, plan.rows, K, V, tops, status_dev, s) != cudaSuccess) return SP_ERR_CUDA;
   sp_attention_args a = {};
@@ -1171,7 +1178,7 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   a.lse = lse;
   a.n_seq = n_seq; a.n_heads = n_heads; a.n_kv_heads = n_kv; a.causal = causal;
   a.scale = scale;
-  return attention_forward(&a, tops, keys, status_dev, rest, plan.attention, s);
+  return attention_forward(&a, tops, q_unit, keys, status_dev, rest, plan.attention, s);
 }
 
 }  // extern "C"

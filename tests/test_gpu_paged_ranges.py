@@ -1,0 +1,154 @@
+"""sp_cache_attention over 4-bit pages whose values have very different sizes: what another text, another head, another query or a key that a query
+does not see holds costs its result nothing.
+
+Tolerances count roundings.  fp16 is off by 2^-11 of a value at most, bf16 by 2^-8, sums in fp32 by 2^-19 of their terms' sizes (128 channels, and the
+partial sums of a tile).  With many rows keys are opened in one rounding, a query's values are exact; probabilities and opened values have one rounding each.  With few
+rows a query's values may lose 2^-16 of the row's largest, the numbers are exact, probabilities times scales have one rounding.  The result has half a step of bf16."""
+import math
+
+import pytest
+import torch
+
+from paper_2510_03246_b200 import api
+from tests.test_gpu_paged_cache import filled, gathered, gen, ints, offsets, table_for, values
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF = torch.bfloat16
+
+
+def copied(pages):
+    return api.KvPages(*(None if x is None else x.clone() for x in (pages.k, pages.v, pages.k_scale, pages.v_scale)))
+
+
+def call(Q, pages, q_len, table, k_len, heads, **kw):
+    status = api.new_status()
+    out, lse = api.sp_cache_attention(Q, pages, ints(offsets(q_len)), table, ints(k_len), heads, want_lse=True, status=status, **kw)
+    assert status.tolist() == [0, 0, 0, 0]
+    return out, lse
+
+
+def within(got, lse, Q, pages, q_len, table, k_len, heads, page, rounding, few, rows=None):
+    """Every value (of rows and heads [Nq, n_heads]) against the formula in 64 bits.  rounding: of probabilities and opened values."""
+    kv = pages.k.shape[1]
+    (k64, k_size), (v64, v_size) = values(pages)
+    dh, g, cu = k64.shape[3], heads // kv, offsets(q_len)
+    for s, (nq, nk) in enumerate(zip(q_len, k_len)):
+        if nq == 0:
+            continue
+        q = Q[cu[s]:cu[s + 1]].double().view(nq, kv, g, dh)
+        K, V, KS, VS = (gathered(x, table, page, s, nk) for x in (k64, v64, k_size, v_size))
+        hidden = torch.arange(nk, device=DEV)[None, :] > torch.arange(nq, device=DEV)[:, None] + nk - nq
+        z = (torch.einsum("iagd,jad->agij", q, K) * dh ** -0.5).masked_fill(hidden, -math.inf)
+        size = torch.einsum("iagd,jad->agij", q.abs(), KS) * 2.0 ** -19
+        if few:
+            size = size + torch.einsum("iag,ja->agij", q.abs().amax(3), KS.sum(2)) * 2.0 ** -16
+        else:
+            size = size + torch.einsum("iagd,jad->agij", q.abs(), K.abs()) * rounding
+        size = (size * dh ** -0.5).masked_fill(hidden, 0.0)
+        want_lse = torch.logsumexp(z, 3)
+        p = torch.where(want_lse[..., None] == -math.inf, 0.0, (z - want_lse[..., None]).exp())
+        want = torch.einsum("agij,jad->iagd", p, V)
+        moved = torch.expm1(size.clamp(max=1.0)) + torch.expm1((p * size).sum(3).clamp(max=1.0))[..., None]
+        off = torch.einsum("agij,jad->iagd", p * (moved + 2.0 ** -19 + rounding * (1 if few else 2)), VS) + 2.0 ** -8 * want.abs() + 1e-7
+        o = got[cu[s]:cu[s + 1]].double().view(nq, kv, g, dh)
+        of = torch.ones(nq, heads, dtype=torch.bool, device=DEV) if rows is None else rows[cu[s]:cu[s + 1]]
+        of = of.view(nq, kv, g)
+        assert ((o - want).abs() <= off)[of].all(), (s, ((o - want).abs() / off)[of].max().item())
+        have = lse[cu[s]:cu[s + 1]].double().view(nq, kv, g).permute(1, 2, 0)
+        of, none = of.permute(1, 2, 0), want_lse == -math.inf
+        assert torch.equal((have == -math.inf)[of], none[of])
+        assert ((have - want_lse).abs() <= size.amax(3) + 2.0 ** -19 * (1 + want_lse.abs()))[~none & of].all()
+
+
+FORMS = {"few": ([4, 1], [200, 90]), "many": ([140, 100], [400, 130])}
+
+
+def setup(rows, seed, heads=4, kv=2, dh=128, page=16):
+    q_len, k_len = FORMS[rows]
+    table, n_pages = table_for(k_len, page, seed)
+    pages = filled(n_pages, kv, page, dh, True, seed + 1)
+    Q = torch.randn(sum(q_len), heads * dh, generator=gen(seed + 2), device=DEV).to(BF)
+    return q_len, k_len, table, pages, Q, heads, page
+
+
+def at(table, s, j, page):
+    return int(table[s, j // page]), j % page
+
+
+@pytest.mark.parametrize("size", [1e9, 1e30])
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("rows", ["few", "many"])
+def test_another_text(rows, which, size):
+    """A large scale, a large offset of another text: not a bit."""
+    q_len, k_len, table, pages, Q, heads, page = setup(rows, 1)
+    want, lse = call(Q, pages, q_len, table, k_len, heads)
+    within(want, lse, Q, pages, q_len, table, k_len, heads, page, 2.0 ** -11, rows == "few")
+    for entry in (0, 1):
+        bad = copied(pages)
+        pg, slot = at(table, 1, 20, page)
+        (bad.k_scale if which == "k" else bad.v_scale)[pg, :, slot, 0, entry] = size
+        got, other = call(Q, bad, q_len, table, k_len, heads)
+        assert torch.equal(got[:q_len[0]], want[:q_len[0]]) and torch.equal(other[:q_len[0]], lse[:q_len[0]])
+
+
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("rows", ["few", "many"])
+def test_another_head(rows, which):
+    q_len, k_len, table, pages, Q, heads, page = setup(rows, 4)
+    want, lse = call(Q, pages, q_len, table, k_len, heads)
+    bad = copied(pages)
+    for s in (0, 1):
+        pg, slot = at(table, s, 33, page)
+        (bad.k_scale if which == "k" else bad.v_scale)[pg, 1, slot] = 1e30
+    got, other = call(Q, bad, q_len, table, k_len, heads)
+    half = want.shape[1] // 2                                    # (the query heads of key head 0)
+    assert torch.equal(got[:, :half], want[:, :half]) and torch.equal(other[:, :heads // 2], lse[:, :heads // 2])
+
+
+@pytest.mark.parametrize("rows", ["few", "many"])
+def test_another_query(rows):
+    """Not a bit where a row has its own units and reference (many rows); the references of a tile of few rows rise together."""
+    q_len, k_len, table, pages, Q, heads, page = setup(rows, 7)
+    want, lse = call(Q, pages, q_len, table, k_len, heads)
+    big, dh = Q.clone(), Q.shape[1] // heads
+    big[2] *= 1e20
+    big[1, dh:2 * dh] = 1e25
+    got, other = call(big, pages, q_len, table, k_len, heads)
+    same = torch.ones(Q.shape[0], heads, dtype=torch.bool, device=DEV)
+    same[2], same[1, 1] = False, False
+    within(got, other, big, pages, q_len, table, k_len, heads, page, 2.0 ** -11, rows == "few", same)
+    if rows == "many":
+        assert torch.equal(got.view(-1, heads, dh)[same], want.view(-1, heads, dh)[same]) and torch.equal(other[same], lse[same])
+
+
+@pytest.mark.parametrize("size", [300.0, 1e9, 1e30])
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("rows", ["many"])
+def test_a_key_that_only_later_queries_see(rows, which, size):
+    q_len, k_len, table, pages, Q, heads, page = setup(rows, 10)
+    bad = copied(pages)
+    key = k_len[0] - 1
+    pg, slot = at(table, 0, key, page)
+    (bad.k_scale if which == "k" else bad.v_scale)[pg, :, slot, :, 0] = size
+    got, lse = call(Q, bad, q_len, table, k_len, heads)
+    # all but the last query of the first text, which alone sees the key
+    n = q_len[0] - 1
+    keep = [i for i in range(sum(q_len)) if i != n]
+    within(got[keep], lse[keep], Q[keep], bad, [n, q_len[1]], table, [k_len[0] - 1, k_len[1]], heads, page, 2.0 ** -11 if size < 1e6 else 2.0 ** -8, rows == "few")
+    assert got[n].isfinite().all() or size > 1e6                # (logits beyond 2^31 leave its own exponents nothing)
+
+
+@pytest.mark.parametrize("rows", ["many"])
+@pytest.mark.parametrize("far", [2.0 ** 19, 2.0 ** 24, 2.0 ** 60])
+def test_a_large_value_of_no_weight(rows, far):
+    """A key whose probability vanishes may hold values of any size: the others keep theirs.  (Offsets: K of the key is far below, so that its logit is.)"""
+    q_len, k_len, table, pages, Q, heads, page = setup(rows, 13)
+    Q = Q.abs()
+    bad = copied(pages)
+    for s in (0, 1):
+        pg, slot = at(table, s, 5, page)
+        bad.k_scale[pg, :, slot, :, 1] = -40.0                   # logits of -40 sum |q| / sqrt 128: some -350
+        bad.v_scale[pg, :, slot] *= far
+    got, lse = call(Q, bad, q_len, table, k_len, heads)
+    within(got, lse, Q, bad, q_len, table, k_len, heads, page, 2.0 ** -8, rows == "few")
