@@ -14,7 +14,7 @@
 //   four of them for m16n8k32 of e4m3, a faster instruction too.  Queries are two e4m3 parts, eight bits of what a power of two per row takes to
 //   128 .. 255; what is lost lies 2^-17 and more below a row's largest value.
 //   V: number n becomes the fp16 64 + n by a shift and one logical operation, two at a time; a second instruction with a constant takes 72 away
-//   again, so that n - 8 is left.  Probabilities times scales are fp16 as well, in units of a power of two that follows the scales (vunit): with bf16
+//   again, so that n - 8 is left.  Probabilities times scales are fp16 as well, in units of a power of two that follows the scales: with bf16
 //   their roundings left 2.4e-3 of the result's norm (16 tokens after 2048 .. 31013 keys), with fp16 1.7e-3, the result's own.
 // fp32 queries are three bf16 parts that add up to them, as are the probabilities' products with the scales; numbers are bf16 for both products, and
 // sums of 16 keys are added up outside the matrix unit.
@@ -141,12 +141,13 @@ __device__ __forceinline__ uint32_t opened(uint32_t w) {
   return (at & 0x00f000f0u) | 0x54005400u;
 }
 // The same as bf16 and n - 8, for fp32: sums of larger numbers would round by more.
-template <int I>
-__device__ __forceinline__ uint32_t opened_centred(uint32_t w) {
-  const uint32_t at = I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3), v = (at & 0x00780078u) | 0x41804180u;
+__device__ __forceinline__ uint32_t opened_centred(uint32_t w, int i) {
+  const uint32_t at = i == 0 ? w << 3 : w >> (4 * i - 3), v = (at & 0x00780078u) | 0x41804180u;
   const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __floats2bfloat162_rn(24.f, 24.f));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
+template <int I>
+__device__ __forceinline__ uint32_t opened_centred(uint32_t w) { return opened_centred(w, I); }
 // four values as e4m3, the first in the lowest byte
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) |
@@ -486,12 +487,16 @@ paged_rows_kernel(const PagedParams p) {
         lim[h][x] = row < rows ? min(visible(it.nk, shift, (r0 + row) / g), seen) : seen;
       }
     }
-    // 4 bits, bf16: probabilities are taken 2^kLift higher, and O holds them in units of vunit, half of a power of two that no scale has passed yet.
-    // (fp16: at most 2^(8 + kLift) 4, and small ones keep ten bits down to 2^-20 of the reference.)
+    // 4 bits, bf16: probabilities are taken 2^kLift higher, and O holds them in units of 1 / per_vunit, half of a power of two that no scale has passed
+    // yet.  (fp16: at most 2^(8 + kLift) 4, and small ones keep ten bits down to 2^-20 of the reference.)  A scale below 2^-20 of the unit
+    // would lose its own: from such a block on, probabilities times scales are three bf16 parts, as for fp32, in units that no longer move.  So a
+    // scale of any size, at a key that few rows see or that has no weight, takes nothing from the others.
+    constexpr uint32_t kWide = 0x7f807f80u;                      // as vhigh: such a block has been met
+    // vhigh: twice the unit, vlow: less one, 2^-20 of it, as bits of bf16, in both halves of a word: two scales are compared at once.
     constexpr bool HALF = FOUR && PARTS == 1;
-    constexpr float kLift = HALF ? 5.f : 0.f;
+    constexpr float kLift = HALF ? 5.f : 0.f, kWideUnit = 16777216.f;      // (2^24: no finite scale times a lifted probability leaves fp32)
     // O: 4 bits: channels 64 (j / 4) + 8 g4 + j % 4 (| + 4) of rows 2 t4 + (x & 1); bf16: channels 16 j + g4 (| + 8)
-    float o[K16][H][4], offset[H][G][2], vunit = 0.f, per_vunit = 0.f, r[H][2], ref[H][2], most[H][2], l[H][2];
+    float o[K16][H][4], offset[H][G][2], per_vunit = 0.f, r[H][2], ref[H][2], most[H][2], l[H][2];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
 #pragma unroll
@@ -506,8 +511,76 @@ paged_rows_kernel(const PagedParams p) {
         for (int gr = 0; gr < G; ++gr) offset[h][gr][x] = 0.f;
       }
     }
+    uint32_t vhigh = 0u, vlow = 0u;
     bool found = false;                                          // bf16: non-finite values behind some row's mask
 
+    // The values of a block for probabilities s (HALF, scales of any size): O stands in local memory meanwhile and everything goes step by step, so that
+    // a path that is seldom taken costs the others no registers.
+    const auto add_wide = [&](int32_t kt, uint32_t stage, const float (&s)[H][4]) {
+      float held[H * K16 * 4], held_offset[H * G * 2];
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+#pragma unroll
+        for (int j = 0; j < K16; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) held[(h * K16 + j) * 4 + x] = o[j][h][x];
+#pragma unroll
+        for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) held_offset[(h * G + gr) * 2 + x] = offset[h][gr][x];
+      }
+#pragma unroll 1
+      for (int gr = 0; gr < G; ++gr) {
+        uint32_t w[4];                                           // as in add_values
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t byte = (uint32_t)((2 * t4 + (x & 1)) * (DH / 2) + 32 * gr + 4 * g4);
+          w[x] = lds32(stage + R::TILE + ((byte ^ ((byte >> 2) & 0x60u)) ^ (kFlip * (x >> 1))) + 8 * (x >> 1) * (DH / 2));
+        }
+        const uint32_t m[4] = {__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x5410),
+                               __byte_perm(w[2], w[3], 0x7632)};
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          uint32_t pb[3][2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const uint32_t pair = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
+            const float scale = low(pair), zero = fmaf(8.f, scale, high(pair));
+            float ps[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const bool sees = kt + 8 * y + g4 < lim[h][x];
+              ps[x] = sees ? s[h][2 * y + x] * (scale * per_vunit) : 0.f;
+              if (sees) held_offset[(h * G + gr) * 2 + x] = fmaf(s[h][2 * y + x], zero, held_offset[(h * G + gr) * 2 + x]);
+            }
+            uint32_t u[3];
+            split<3>(ps[0], ps[1], u);
+#pragma unroll
+            for (int x = 0; x < 3; ++x) pb[x][y] = turned8x8(u[x]);
+          }
+#pragma unroll 1
+          for (int j = 0; j < 4; ++j) {
+            uint32_t a[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) a[x] = opened_centred(m[x], j);
+            float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 2; x >= 0; --x) mma(t, a[0], a[1], a[2], a[3], pb[x][0], pb[x][1]);
+            for (int x = 0; x < 4; ++x) held[(h * K16 + 4 * gr + j) * 4 + x] += t[x];
+          }
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+#pragma unroll
+        for (int j = 0; j < K16; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[j][h][x] = held[(h * K16 + j) * 4 + x];
+#pragma unroll
+        for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) offset[h][gr][x] = held_offset[(h * G + gr) * 2 + x];
+      }
+    };
     uint32_t stage = ring + R::BYTES - R::STAGE;
     for (int32_t i = 0; i < own; ++i) {
       const int32_t kt = kb + kBlock * (warp + W * i);
@@ -609,31 +682,48 @@ paged_rows_kernel(const PagedParams p) {
           rise |= !(s[h][x] <= most[h][x & 1]);
         }
       if constexpr (HALF) {
-        float top = 0.f;
+        uint32_t top = vhigh, least = vlow, mask = 0x7fff7fffu;
+        if (edge) mask = (kt + g4 < seen ? 0x7fffu : 0u) | (kt + 8 + g4 < seen ? 0x7fff0000u : 0u);      // (not of slots that hold nothing)
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+        for (int gr = 0; gr < G; ++gr) {
 #pragma unroll
-          for (int gr = 0; gr < G; ++gr) {
-            pair_v[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
-            if (!edge || kt + 8 * y + g4 < seen) top = fmaxf(top, fabsf(low(pair_v[y][gr])));      // (not of slots that hold nothing)
-          }
-        rise |= top > 2.f * vunit;
+          for (int y = 0; y < 2; ++y) pair_v[y][gr] = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
+          const uint32_t both = __byte_perm(pair_v[0][gr], pair_v[1][gr], 0x5410) & mask;
+          top = __vmaxu2(top, both);
+          least = __vminu2(least, both - 0x00010001u);           // (a scale of 0 counts as none; beside one, the upper may count a bit too low)
+        }
+        rise |= top != vhigh || least != vlow;
       }
+      bool wide = false;
       if (__any_sync(0xffffffffu, rise)) {                       // seldom: the references follow the maxima of this block
         if constexpr (HALF) {
-          float top = 0.f;
+          float top = 0.f, least = INFINITY;
 #pragma unroll
           for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int gr = 0; gr < G; ++gr) {
               const float u = fabsf(low(pair_v[y][gr]));
-              if (u < INFINITY && kt + 8 * y + g4 < seen) top = fmaxf(top, u);
+              if (u < INFINITY && kt + 8 * y + g4 < seen) {
+                top = fmaxf(top, u);
+                least = fminf(least, u > 0.f ? u : INFINITY);
+              }
             }
 #pragma unroll
-          for (int w = 1; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-          if (top > 2.f * vunit) {
-            const float now = __uint_as_float(min(max(__float_as_uint(top) >> 23, 20u), 240u) << 23), f = vunit / now;
-            vunit = now;
+          for (int w = 1; w < 32; w <<= 1) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+            least = fminf(least, __shfl_xor_sync(0xffffffffu, least, w));
+          }
+          const float twice = low(vhigh);
+          if (vhigh != kWide && (top > twice || (least < INFINITY && least < 0x1p-21f * twice))) {
+            float now = top > twice ? __uint_as_float(min(max(__float_as_uint(top) >> 23, 20u), 240u) << 23) : 0.5f * twice;
+            vhigh = (__float_as_uint(2.f * now) >> 16) * 0x00010001u;
+            vlow = ((__float_as_uint(0x1p-20f * now) >> 16) - 1u) * 0x00010001u;
+            if (least < 0x1p-20f * now || now * per_vunit > 0x1p40f) {                   // (what O holds would leave fp32 by such a step)
+              now = kWideUnit;
+              vhigh = kWide;
+              vlow = 0xffffffffu;                                // (every block but one of zeros comes here)
+            }
+            const float f = per_vunit > 0.f ? (1.f / per_vunit) / now : 0.f;
             per_vunit = 1.f / now;
 #pragma unroll
             for (int h = 0; h < H; ++h)
@@ -642,6 +732,8 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x) o[j][h][x] *= f;
           }
+          // (a vote, and within this branch: with a branch of its own on vhigh 16 tokens after 2048 .. 31013 keys took 130 us, not 121)
+          wide = __any_sync(0xffffffffu, vhigh == kWide);
         }
 #pragma unroll
         for (int h = 0; h < H; ++h) {
@@ -693,7 +785,7 @@ paged_rows_kernel(const PagedParams p) {
           for (int y = 0; y < 2; ++y)
             for (int gr = 0; gr < G; ++gr) {
               const uint32_t w = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
-              odd_scales |= !(fabsf(low(w)) <= (HALF ? 2.f * vunit : 1e37f)) || !(fabsf(high(w)) < 1e38f);
+              odd_scales |= !(fabsf(low(w)) <= (HALF ? low(vhigh) : 1e37f)) || !(fabsf(high(w)) < 1e38f);
             }
           odd_scales = __any_sync(0xffffffffu, odd_scales);
         }
@@ -763,8 +855,12 @@ paged_rows_kernel(const PagedParams p) {
             }
         }
         };
-        if (odd_scales) add_values(std::true_type());
-        else add_values(std::false_type());
+        if (odd_scales || wide) {
+          if (wide) add_wide(kt, stage, s);
+          else add_values(std::true_type());
+        } else {
+          add_values(std::false_type());
+        }
       } else {
         uint32_t pb[H][PARTS][2];
 #pragma unroll
@@ -826,7 +922,7 @@ paged_rows_kernel(const PagedParams p) {
             for (int w = 4; w < 32; w <<= 1) offset[h][gr][x] += __shfl_xor_sync(0xffffffffu, offset[h][gr][x], w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float f = HALF ? vunit : 1.f;
+              const float f = !HALF ? 1.f : per_vunit > 0.f ? 1.f / per_vunit : 0.f;
               o[4 * gr + j][h][x] = fmaf(o[4 * gr + j][h][x], f, offset[h][gr][x]);
               o[4 * gr + j][h][2 + x] = fmaf(o[4 * gr + j][h][2 + x], f, offset[h][gr][x]);
             }

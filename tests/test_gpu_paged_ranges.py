@@ -124,7 +124,7 @@ def test_another_query(rows):
 
 @pytest.mark.parametrize("size", [300.0, 1e9, 1e30])
 @pytest.mark.parametrize("which", ["k", "v"])
-@pytest.mark.parametrize("rows", ["many"])
+@pytest.mark.parametrize("rows", ["few", "many"])
 def test_a_key_that_only_later_queries_see(rows, which, size):
     q_len, k_len, table, pages, Q, heads, page = setup(rows, 10)
     bad = copied(pages)
@@ -139,7 +139,7 @@ def test_a_key_that_only_later_queries_see(rows, which, size):
     assert got[n].isfinite().all() or size > 1e6                # (logits beyond 2^31 leave its own exponents nothing)
 
 
-@pytest.mark.parametrize("rows", ["many"])
+@pytest.mark.parametrize("rows", ["few", "many"])
 @pytest.mark.parametrize("far", [2.0 ** 19, 2.0 ** 24, 2.0 ** 60])
 def test_a_large_value_of_no_weight(rows, far):
     """A key whose probability vanishes may hold values of any size: the others keep theirs.  (Offsets: K of the key is far below, so that its logit is.)"""
@@ -152,3 +152,18 @@ def test_a_large_value_of_no_weight(rows, far):
         bad.v_scale[pg, :, slot] *= far
     got, lse = call(Q, bad, q_len, table, k_len, heads)
     within(got, lse, Q, bad, q_len, table, k_len, heads, page, 2.0 ** -8, rows == "few")
+
+
+@pytest.mark.parametrize("rows", ["few", "many"])
+@pytest.mark.parametrize("by", [2.0 ** -30, 2.0 ** 30, 2.0 ** 90])
+def test_values_that_change_by_steps(rows, by):
+    """The scales of V change once on the way, so far that no unit holds both sides, and one group of 64 channels differs from the other."""
+    q_len, k_len, table, pages, Q, heads, page = setup(rows, 16)
+    bad = copied(pages)
+    for s in (0, 1):
+        for j in range(k_len[s] // 2, k_len[s]):
+            pg, slot = at(table, s, j, page)
+            bad.v_scale[pg, 0, slot] *= by
+            bad.v_scale[pg, 1, slot, 1] *= by
+    got, lse = call(Q, bad, q_len, table, k_len, heads)
+    within(got, lse, Q, bad, q_len, table, k_len, heads, page, 2.0 ** -8 if rows == "many" else 2.0 ** -11, rows == "few")
