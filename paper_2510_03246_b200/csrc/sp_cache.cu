@@ -371,7 +371,8 @@ struct ReadParams {
   const int32_t* cu;
   void *k, *v;
   int64_t ldk, ldv;
-  int32_t rows, whole, k_vec, v_vec;
+  const int32_t* whole;                    // null: any last tokens
+  int32_t rows, k_vec, v_vec;
   Divisor head;                            // chunks of a head
   const HalfTops* tops;
   int32_t* status;
@@ -415,7 +416,7 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
   const int32_t i = row - bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - (row - i);
   const int32_t length = p.c.lens[s], place = length - n + i;
   const int32_t entry = place >= 0 ? place / p.c.page_len : -1;
-  const int32_t page = p.whole && n != length ? -1 : page_of(p.c, s, entry);
+  const int32_t page = p.whole && n != p.whole[s] ? -1 : page_of(p.c, s, entry);
   const int32_t slot = place - entry * p.c.page_len;
   if (page < 0 && lane == 0) report_status(p.status, SP_ERR_SHAPE, s, entry);
   constexpr bool HALF = std::is_same<T, __half>::value;
@@ -468,7 +469,7 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
 // a few words.  (Maxima and minima are the same in any order.)
 struct TopsParams {
   CacheView c;
-  const int32_t* cu;
+  const int32_t *cu, *whole;
   int32_t rows, strips;
   HalfTops* tops;
 };
@@ -499,7 +500,7 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
   for (int64_t row = (int64_t)strip * 256 + threadIdx.x; row < p.rows; row += (int64_t)p.strips * 256) {
     const int32_t s = sequence_near(p.cu, p.c.n_seq, p.rows, row);        // (cu[0] is 0)
     const int32_t first = bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - first;
-    if (row >= first + n || n != p.c.lens[s]) continue;
+    if (row >= first + n || n != p.whole[s]) continue;
     const int32_t place = (int32_t)row - first, entry = place / p.c.page_len, page = page_of(p.c, s, entry);
     if (page < 0) continue;
     if (s != seq) {
@@ -628,14 +629,14 @@ CacheView cache_view(const sp_kv_cache* c) {
 }
 
 namespace {
-cudaError_t read_rows(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype, bool whole,
-                      const HalfTops* tops, int32_t* status, cudaStream_t stream) {
+cudaError_t read_rows(const sp_kv_cache* c, const int32_t* cu, const int32_t* whole, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv,
+                      int32_t dtype, const HalfTops* tops, int32_t* status, cudaStream_t stream) {
   ReadParams p = {};
   p.c = cache_view(c);
   p.cu = cu;
   p.k = K; p.v = V; p.ldk = ldk; p.ldv = ldv;
   p.rows = (int32_t)rows;
-  p.whole = whole ? 1 : 0;
+  p.whole = whole;
   p.head = divisor(c->d_head / 8);
   p.k_vec = rows_of_16(K, ldk, dtype, rows); p.v_vec = rows_of_16(V, ldv, dtype, rows);
   p.tops = tops;
@@ -654,17 +655,17 @@ cudaError_t read_rows(const sp_kv_cache* c, const int32_t* cu, int64_t rows, voi
 
 cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
                        int32_t* status, cudaStream_t stream) {
-  return read_rows(c, cu, rows, K, V, ldk, ldv, dtype, false, nullptr, status, stream);
+  return read_rows(c, cu, nullptr, rows, K, V, ldk, ldv, dtype, nullptr, status, stream);
 }
-cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, const HalfTops* tops, int32_t* status,
-                       cudaStream_t stream) {
+cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, const int32_t* whole, int64_t rows, void* K, void* V, const HalfTops* tops,
+                       int32_t* status, cudaStream_t stream) {
   const int64_t ld = (int64_t)c->n_kv_heads * c->d_head;
-  return read_rows(c, cu, rows, K, V, ld, ld, SP_BF16, true, tops, status, stream);
+  return read_rows(c, cu, whole, rows, K, V, ld, ld, SP_BF16, tops, status, stream);
 }
-cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, HalfTops* tops, cudaStream_t stream) {
+cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, const int32_t* whole, int64_t rows, HalfTops* tops, cudaStream_t stream) {
   TopsParams p = {};
   p.c = cache_view(c);
-  p.cu = cu;
+  p.cu = cu; p.whole = whole;
   p.rows = (int32_t)rows;
   p.tops = tops;
   const int64_t most = ceil_div(4 * (int64_t)sm_count(), (int64_t)c->n_kv_heads), strips = ceil_div(rows, (int64_t)256);

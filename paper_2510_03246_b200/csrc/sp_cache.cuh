@@ -56,13 +56,13 @@ CacheView cache_view(const sp_kv_cache* c);
 // Reads n = cu[s + 1] - cu[s] last tokens of every sequence (sp_cache_read).
 cudaError_t cache_read(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, int64_t ldk, int64_t ldv, int32_t dtype,
                        int32_t* status, cudaStream_t stream);
-// The same for whole sequences into contiguous rows of bf16 (those of a sequence with another number of tokens than n are NaN); with tops as fp16 in
+// The same for whole sequences, whole[s] tokens, into contiguous rows of bf16 (those of a sequence with another number than n are NaN); with tops as fp16 in
 // the units that these give a text's key head, or bf16 (HalfTops, sp_attention.cuh).  cache_tops finds them among the scales of the same rows, and Q_half
 // [Nq, n_heads * d_head] takes the queries alike, q_unit [Nq, n_heads] their units.
 struct HalfTops;
-cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, int64_t rows, void* K, void* V, const HalfTops* tops, int32_t* status,
-                       cudaStream_t stream);
-cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, int64_t rows, HalfTops* tops, cudaStream_t stream);
+cudaError_t cache_open(const sp_kv_cache* c, const int32_t* cu, const int32_t* whole, int64_t rows, void* K, void* V, const HalfTops* tops,
+                       int32_t* status, cudaStream_t stream);
+cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, const int32_t* whole, int64_t rows, HalfTops* tops, cudaStream_t stream);
 cudaError_t queries_to_half(const sp_kv_cache* c, const sp_mat* Q, const int32_t* cu_q, void* Q_half, float* q_unit, const HalfTops* tops,
                             cudaStream_t stream);
 

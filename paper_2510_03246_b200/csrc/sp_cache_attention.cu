@@ -1135,9 +1135,9 @@ cudaError_t launch_rows(const PagedParams& p, bool four, int rows, cudaStream_t 
 }
 
 // cu_k of the opened keys: the lengths added up; a sequence that does not fit into max_keys (or has more tokens than its table) gets as many
-// rows as queries at most, which cache_read makes NaN: every query sees one of them.
+// rows as queries at most, of which every query sees one that it would see, and no number of tokens in `whole`, which makes those NaN.
 __global__ void __launch_bounds__(kPlanThreads) open_plan_kernel(const CacheView c, const int32_t* cu_q, int32_t Nq, int32_t max_keys, int32_t* cu_k,
-                                                             HalfTops* tops, int32_t* status) {
+                                                             int32_t* whole, HalfTops* tops, int32_t* status) {
   kernel_begin();
   if (tops)
     for (int64_t i = threadIdx.x; i < (int64_t)c.n_seq * c.n_kv; i += kPlanThreads) tops[i] = HalfTops{0u, kNoLow, 0u, kNoLow};
@@ -1156,7 +1156,10 @@ __global__ void __launch_bounds__(kPlanThreads) open_plan_kernel(const CacheView
       n = min(n, (int64_t)nq);
     }
     const int64_t rows = block_scan<kPlanThreads / 32>(n, s_word, before);
-    if (s < c.n_seq) cu_k[s] = (int32_t)(at + before);
+    if (s < c.n_seq) {
+      cu_k[s] = (int32_t)(at + before);
+      whole[s] = fits ? (int32_t)n : -1;
+    }
     at += rows;
     used += keys;
   }
@@ -1173,7 +1176,7 @@ OpenPlan open_plan(int64_t Nq, int64_t n_seq, int32_t n_heads, int32_t n_kv, int
   OpenPlan r;
   r.rows = max_keys + Nq;
   const bool four = dh % kCacheGroup == 0;
-  r.cu_bytes = align_up((size_t)(n_seq + 1) * 4, 256);
+  r.cu_bytes = align_up((size_t)(2 * n_seq + 1) * 4, 256);       // and the lengths behind the offsets
   r.tops_bytes = four ? align_up((size_t)n_seq * n_kv * sizeof(HalfTops), 256) : 0;
   r.k_bytes = align_up((size_t)r.rows * n_kv * dh * 2, 256);
   r.q_bytes = four ? align_up((size_t)Nq * n_heads * dh * 2, 256) : 0;
@@ -1254,7 +1257,7 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   }
   const int64_t keys = keys_at_most(max_keys, n_seq, cache->max_pages, cache->page_len);
   const OpenPlan plan = open_plan(Nq, n_seq, n_heads, n_kv, dh, keys);
-  int32_t* cu_k = reinterpret_cast<int32_t*>(at);
+  int32_t *cu_k = reinterpret_cast<int32_t*>(at), *whole = cu_k + n_seq + 1;
   uint8_t *K = at + plan.cu_bytes + plan.tops_bytes, *V = K + plan.k_bytes, *Qh = V + plan.k_bytes, *units = Qh + plan.q_bytes;
   uint8_t* rest = units + plan.unit_bytes;
   const int64_t kv = (int64_t)n_kv * dh;
@@ -1262,13 +1265,13 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   HalfTops* tops = half ? reinterpret_cast<HalfTops*>(at + plan.cu_bytes) : nullptr;
   float* q_unit = half ? reinterpret_cast<float*>(units) : nullptr;
   count_launch();
-  if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, tops, status_dev) !=
+  if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, whole, tops, status_dev) !=
       cudaSuccess)
     return SP_ERR_CUDA;
-  if (half && (cache_tops(cache, cu_k, plan.rows, tops, s) != cudaSuccess ||
+  if (half && (cache_tops(cache, cu_k, whole, plan.rows, tops, s) != cudaSuccess ||
                queries_to_half(cache, Q, cu_q, Qh, q_unit, tops, s) != cudaSuccess))
     return SP_ERR_CUDA;
-  if (cache_open(cache, cu_k, plan.rows, K, V, tops, status_dev, s) != cudaSuccess) return SP_ERR_CUDA;
+  if (cache_open(cache, cu_k, whole, plan.rows, K, V, tops, status_dev, s) != cudaSuccess) return SP_ERR_CUDA;
   sp_attention_args a = {};
   a.Q = half ? sp_mat{Qh, dt, 0, Nq, cols, cols} : *Q;
   a.O = *O;

@@ -1,0 +1,35 @@
+"""sp_cache_attention at the ends of what a call may say: texts beyond max_keys, logits beyond fp32, scales at the ends of their range."""
+import math
+
+import pytest
+import torch
+
+from paper_2510_03246_b200 import api
+from tests.test_gpu_paged_cache import filled, gen, ints, offsets, table_for
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("causal", [False, True])
+def test_texts_beyond_max_keys_are_nan_whatever_their_length(four, causal):
+    """The first chunk of a prompt (as many keys as queries), one with fewer keys than queries, one with more: reported, and NaN wherever a key is seen."""
+    q_len, k_len, heads, kv, dh, page = [100, 120, 90, 90], [300, 120, 50, 200], 4, 2, 64, 16
+    table, n_pages = table_for(k_len, page, 61)
+    pages = filled(n_pages, kv, page, dh, four, 62)
+    Q = torch.randn(sum(q_len), heads * dh, generator=gen(63), device=DEV).to(BF)
+    cu = offsets(q_len)
+    want, _ = api.sp_cache_attention(Q, pages, ints(cu), table, ints(k_len), heads, causal=causal, max_keys=sum(k_len))
+    for left in range(len(k_len)):
+        status = api.new_status()
+        got, lse = api.sp_cache_attention(Q, pages, ints(cu), table, ints(k_len), heads, causal=causal, max_keys=sum(k_len[:left]) + k_len[left] - 1,
+                                          want_lse=True, status=status)
+        assert status.tolist()[0] == 2 and status.tolist()[1] >= left
+        assert got[:cu[left]].isfinite().all()
+        for s in range(left, len(k_len)):
+            blind = max(0, q_len[s] - k_len[s]) if causal else 0             # queries before the first key
+            assert (got[cu[s]:cu[s] + blind] == 0).all() and (lse[cu[s]:cu[s] + blind] == -math.inf).all()
+            assert got[cu[s] + blind:cu[s + 1]].isnan().all() and lse[cu[s] + blind:cu[s + 1]].isnan().all()
+    assert want.isfinite().all()
