@@ -975,7 +975,9 @@ paged_rows_kernel(const PagedParams p) {
         acc[2] = fmaf(v.z, f, acc[2]);
         acc[3] = fmaf(v.w, f, acc[3]);
       }
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      // (keys seen, and all logits beyond fp32 below: nothing can be told; a piece of a row's keys may be of no weight)
+      const bool lost = sum == 0.f && !cut && visible(it.nk, shift, token) > 0;
+      const float inv = sum == 0.f ? (lost ? NAN : 0.f) : 1.f / sum;
 #pragma unroll
       for (int x = 0; x < 4; ++x) acc[x] *= inv;
       if (bad) {
@@ -1000,7 +1002,7 @@ paged_rows_kernel(const PagedParams p) {
         for (int x = 0; x < 4; ++x) store1(out + x, acc[x]);
       }
       if (d == 0) {
-        const float lse2 = sum == 0.f ? -INFINITY : base + (log2f(sum) - kLift);
+        const float lse2 = sum == 0.f ? (lost ? NAN : -INFINITY) : base + (log2f(sum) - kLift);
         if (cut) p.part_lse[slot_of * ROWS + row] = lse2;
         else if (p.lse) p.lse[out_row * p.n_heads + out_head] = lse2 == -INFINITY ? lse2 : lse2 * 0.6931471805599453f;
       }
@@ -1059,6 +1061,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
       }
     }
   }
+  if (total_w == 0.f) bad |= visible(it.nk, p.causal ? (int64_t)it.nk - it.nq : (int64_t)it.nk, row - it.q0) > 0;      // (as above)
   const float inv = total_w == 0.f ? 0.f : 1.f / total_w;
   if (d < dh) {
     T* out = reinterpret_cast<T*>(p.o) + (int64_t)row * p.ldo + (int64_t)h * dh + d;

@@ -33,3 +33,22 @@ def test_texts_beyond_max_keys_are_nan_whatever_their_length(four, causal):
             assert (got[cu[s]:cu[s] + blind] == 0).all() and (lse[cu[s]:cu[s] + blind] == -math.inf).all()
             assert got[cu[s] + blind:cu[s + 1]].isnan().all() and lse[cu[s] + blind:cu[s + 1]].isnan().all()
     assert want.isfinite().all()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("q_len, k_len", [([1, 2], [40, 700]), ([1], [30000]), ([300], [300])])
+def test_scaled_logits_beyond_fp32_are_not_taken_for_a_mask(q_len, k_len, sign, dtype, four):
+    """scale <q, k> = +-2^136 at every key: no probability can be told, so the rows are NaN, not 0, which says that a row sees no key."""
+    heads, kv, dh, page = 4, 2, 64, 16
+    table, n_pages = table_for(k_len, page, 64)
+    pages = filled(n_pages, kv, page, dh, four, 65)
+    if four:
+        pages.k_scale[..., 0], pages.k_scale[..., 1] = 0.0, sign * 2.0 ** 66
+    else:
+        pages.k[:] = sign * 2.0 ** 66
+    Q = torch.zeros(sum(q_len), heads * dh, dtype=dtype, device=DEV)
+    Q[:, ::64] = 2.0 ** 60
+    o, lse = api.sp_cache_attention(Q, pages, ints(offsets(q_len)), table, ints(k_len), heads, scale=2.0 ** 10, want_lse=True)
+    assert o.isnan().all() and not (lse == -math.inf).any()
