@@ -463,7 +463,8 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const float u = __shfl_sync(0xffffffffu, of_sum, (2 * t4 + x) * 4);
-          to_log2[h][x] = u * p.scale_log2;
+          const float f = u * p.scale_log2;
+          to_log2[h][x] = f < 1.2e-38f ? 1.2e-38f : f;           // (0 times the mask's -infinity would be NaN)
 #pragma unroll
           for (int gr = 0; gr < G; ++gr) qsum[h][gr][x] = __shfl_sync(0xffffffffu, sum[gr], (2 * t4 + x) * 4) / u;
         }

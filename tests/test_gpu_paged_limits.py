@@ -52,3 +52,20 @@ def test_scaled_logits_beyond_fp32_are_not_taken_for_a_mask(q_len, k_len, sign, 
     Q[:, ::64] = 2.0 ** 60
     o, lse = api.sp_cache_attention(Q, pages, ints(offsets(q_len)), table, ints(k_len), heads, scale=2.0 ** 10, want_lse=True)
     assert o.isnan().all() and not (lse == -math.inf).any()
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("size", [0.0, 1e-30, 1e-20])
+@pytest.mark.parametrize("q_len, k_len", [([1, 2], [40, 701]), ([300], [300])])
+def test_logits_too_small_for_fp32_are_equal(q_len, k_len, size, dtype, four):
+    """Queries of (nearly) nothing times a scale of 1e-30: all keys that a query sees weigh the same."""
+    heads, kv, dh, page = 4, 2, 64, 16
+    table, n_pages = table_for(k_len, page, 66)
+    pages = filled(n_pages, kv, page, dh, four, 67)
+    Q = torch.full((sum(q_len), heads * dh), size, device=DEV).to(dtype)
+    o, lse = api.sp_cache_attention(Q, pages, ints(offsets(q_len)), table, ints(k_len), heads, scale=1e-30, want_lse=True)
+    cu = offsets(q_len)
+    for s, (nq, nk) in enumerate(zip(q_len, k_len)):
+        seen = torch.arange(nk - nq + 1, nk + 1, device=DEV).double()
+        assert ((lse[cu[s]:cu[s + 1]].double() - seen.log()[:, None]).abs() <= 2.0 ** -18 * 10).all()
+    assert o.isfinite().all()
