@@ -332,7 +332,7 @@ class KvCache:
 
     def step(self, texts, new_tokens) -> "CacheStep":
         """Room for new_tokens[i] more tokens of texts[i] (any hashable names, each once; one that is new starts empty).  Nothing is taken where the
-        free pages do not suffice (MemoryError)."""
+        free pages do not suffice (MemoryError).  Prompts that are to read their own unrounded keys and values take a step without texts that go on."""
         texts, new_tokens = list(texts), [int(n) for n in new_tokens]
         if len(texts) != len(new_tokens) or len(set(texts)) != len(texts) or any(n < 0 for n in new_tokens):
             raise ValueError("a number of tokens, not negative, for every text, and every text once")
@@ -340,7 +340,7 @@ class KvCache:
         need = [-(-a // self.page_len) - len(self._pages.get(t, ())) for t, a in zip(texts, after)]
         if sum(need) > len(self._free):
             raise MemoryError(f"{sum(need)} pages are needed, {len(self._free)} are free")
-        fresh = all(self.tokens(t) == 0 for t in texts)
+        fresh = all(self.tokens(t) == 0 for t, n in zip(texts, new_tokens) if n > 0)
         for t, a, n in zip(texts, after, need):
             self._pages.setdefault(t, []).extend(self._free.pop() for _ in range(n))
             self._tokens[t] = a
@@ -365,15 +365,16 @@ class CacheStep:
     lens: torch.Tensor          # int32 [n]
     table: torch.Tensor         # int32 [n, pages]
     keys: int                   # keys of all texts with new tokens
-    fresh: bool                 # no text had tokens before
+    fresh: bool                 # no text with new tokens had any before: prompts need not read what the pages hold (cached_attention)
 
 
 def cached_attention(qkv: torch.Tensor, pages: api.KvPages, step: CacheStep, n_heads: int, n_kv_heads: int, inv_freq: torch.Tensor | None = None,
                      neighbours: bool = False, status: torch.Tensor | None = None) -> torch.Tensor:
     """Concatenated head outputs [N, n_heads * d_head] of an attention module for the new tokens of a step, from its projections qkv [N, (n_heads +
     2 n_kv_heads) d_head] (whose queries are turned in their place): keys and values go into the module's pages, and the queries attend to all that is
-    there.  Prompts of texts that were empty read their own keys and values as the projection left them, 4 bits or not.  Rows behind the step's last are
-    zero.  status as attention_head_outputs."""
+    there, as the pages hold it.  A step of nothing but prompts of texts that were empty (step.fresh) reads the keys and values as the projection left
+    them instead, 4 bits or not; beside a text that goes on, a prompt reads the pages like it, and differs by what they round.  Rows behind the step's
+    last are zero.  status as attention_head_outputs."""
     d_head = pages.k.shape[3] * (2 if pages.k.dtype == torch.uint8 else 1)
     q, k = n_heads * d_head, n_kv_heads * d_head
     if qkv.shape[1] != q + 2 * k:
