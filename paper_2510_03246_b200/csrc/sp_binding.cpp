@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -78,14 +79,12 @@ T* vector(PyObject* o, at::ScalarType type, int64_t n, int dev, const char* what
   }
   return (T*)t.data_ptr();
 }
-at::Tensor empty(at::IntArrayRef size, at::ScalarType type, int dev) {
-  return at::empty(size, at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, (c10::DeviceIndex)dev)));
-}
-// [n, cols] whose rows start on 16 bytes
+at::TensorOptions on(at::ScalarType type, int dev) { return at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, (c10::DeviceIndex)dev)); }
+at::Tensor empty(at::IntArrayRef size, at::ScalarType type, int dev) { return at::empty(size, on(type, dev)); }
+// [n, cols] whose rows start on 16 bytes (a slice of a wider matrix would be the same, 3 us later)
 at::Tensor rows_of_16_bytes(int64_t n, int64_t cols, at::ScalarType type, int dev) {
   const int64_t per = 16 / (int64_t)c10::elementSize(type), wide = (cols + per - 1) / per * per;
-  at::Tensor t = empty({n, wide}, type, dev);
-  return wide == cols ? t : t.narrow(1, 0, cols);
+  return wide == cols ? empty({n, cols}, type, dev) : at::empty_strided({n, cols}, {wide, 1}, on(type, dev));
 }
 struct Workspace {
   at::Tensor t;
@@ -147,7 +146,7 @@ PyObject* rms_norm(PyObject* const* a) {
   at::Tensor H;
   if (a[3] != Py_None) {
     r = rows(a[3], dev, "residual");
-    H = a[4] == Py_None ? empty({x.rows, x.cols}, tensor(a[3], "residual").scalar_type(), dev) : tensor(a[4], "h_out");
+    H = a[4] == Py_None ? rows_of_16_bytes(x.rows, x.cols, tensor(a[3], "residual").scalar_type(), dev) : tensor(a[4], "h_out");
   } else if (a[4] != Py_None) {
     H = tensor(a[4], "h_out");
   }
@@ -168,7 +167,7 @@ PyObject* rms_norm(PyObject* const* a) {
 PyObject* rms_norm_grad(PyObject* const* a) {
   const int dev = current_device(a[0], "dY");
   const sp_mat g = rows(a[0], dev, "dY"), h = rows(a[1], dev, "H");
-  at::Tensor X = a[7] == Py_None ? empty({g.rows, g.cols}, tensor(a[1], "H").scalar_type(), dev) : tensor(a[7], "out");
+  at::Tensor X = a[7] == Py_None ? rows_of_16_bytes(g.rows, g.cols, tensor(a[1], "H").scalar_type(), dev) : tensor(a[7], "out");
   const sp_mat x = rows(X, dev, "out");
   sp_mat d{};
   if (a[5] != Py_None) d = rows(a[5], dev, "d_stream");
