@@ -532,10 +532,11 @@ inline int grad_threads(int64_t d) {
     if (chunks <= (int64_t)t * kGradChunks) return t;
   return 0;
 }
-// Blocks of the gradient: one wave, as many as are resident on 148 SMs (so that the workspace depends on the sizes alone).
-inline int64_t grad_blocks(int64_t T, int64_t d) {
+// Blocks of the gradient: one wave, as many as are resident on 148 SMs (so that the workspace depends on the sizes alone).  loop: of the looping
+// kernel, whose blocks have a row at a time: never fewer than of the other.
+inline int64_t grad_blocks(int64_t T, int64_t d, bool loop) {
   const int tpr = grad_threads(d);
-  const int threads = tpr == 0 ? 512 : tpr < 256 ? 256 : tpr, rows = tpr > 0 && tpr < 256 ? 256 / tpr : 1;
+  const int threads = tpr == 0 ? 512 : tpr < 256 ? 256 : tpr, rows = !loop && tpr > 0 && tpr < 256 ? 256 / tpr : 1;
   const int64_t most = 148 * (threads > 256 ? 1 : 2), want = ceil_div(T, (int64_t)rows);
   return want < most ? (want > 0 ? want : 1) : most;
 }
@@ -550,7 +551,7 @@ cudaError_t launch_grad(const GradParams& p, dim3 grid, cudaStream_t s) {
 }
 template <typename TY, typename TH>
 cudaError_t launch_grad(const GradParams& p, bool vec, cudaStream_t s) {
-  const dim3 grid((unsigned)grad_blocks(p.T, p.d));
+  const dim3 grid((unsigned)grad_blocks(p.T, p.d, !vec));
   switch (vec ? grad_threads(p.d) : 0) {
     case 32: return launch_grad<TY, TH, 32>(p, grid, s);
     case 64: return launch_grad<TY, TH, 64>(p, grid, s);
@@ -622,7 +623,7 @@ sp_status sp_rms_norm(const sp_mat* X, const sp_mat* R, const float* weight, dou
 
 size_t sp_rms_norm_grad_bytes(int64_t T, int64_t d) {
   if (T < 1 || d < 1 || T > 0x7fffffff || d > (1 << 30)) return 0;
-  return (size_t)sp::grad_blocks(T, d) * (size_t)d * sizeof(float);
+  return (size_t)sp::grad_blocks(T, d, true) * (size_t)d * sizeof(float);
 }
 
 sp_status sp_rms_norm_grad(const sp_mat* dY, const sp_mat* H, const float* weight, const float* rstd, double eps, const sp_mat* dH,
@@ -663,7 +664,7 @@ sp_status sp_rms_norm_grad(const sp_mat* dY, const sp_mat* H, const float* weigh
     count_launch();
     const OverlapScope overlap(true);      // its blocks start while the rows' end
     e = launch(norm_grad_join_kernel, dim3((unsigned)ceil_div(d, (int64_t)32)), dim3(256), 0, s, (const float*)p.part,
-               (int32_t)grad_blocks(T, d), p.d, dweight);
+               (int32_t)grad_blocks(T, d, !vec), p.d, dweight);
   }
   return e == cudaSuccess ? SP_OK : SP_ERR_CUDA;
 }

@@ -44,3 +44,22 @@ def test_rows_that_end_inside_a_chunk(d, T, dy, dh):
     assert ((dw.double() - terms.sum(0)).abs() <= terms.abs().sum(0) * (T + 4) * 2.0 ** -24 + 1e-30).all()
     none, again = api.sp_rms_norm_grad(G, r.H, w, r.rstd, d_stream=S)
     assert torch.equal(dX, none) and torch.equal(dw, again)
+
+
+@pytest.mark.parametrize("T, d", [(1, 64), (7, 97), (295, 333), (296, 333), (297, 64), (3000, 97), (149, 9000)])
+def test_gradient_of_rows_on_any_address(T, d):
+    """One row of a block at a time, more rows than blocks: the weight's gradient of all of them."""
+    G, H = (torch.randn(T, d + 1, generator=torch.Generator(device=DEV).manual_seed(s), device=DEV)[:, 1:] for s in (5, 6))
+    w = 1 + 0.2 * torch.randn(d, device=DEV)
+    need = api.lib().sp_rms_norm_grad_bytes(T, d)
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device=DEV)
+    dX, dw = api.sp_rms_norm_grad(G, H, w, ws=ws[:need])
+    assert (ws[need:] == 255).all()
+    h, g = H.double(), G.double()
+    rstd = (h.square().mean(1, keepdim=True) + 1e-5).rsqrt()
+    u = g * w.double()
+    want = rstd * (u - h * rstd.square() * (u * h).mean(1, keepdim=True))
+    near = rstd * (u.abs() * (4 + d / 512 + 64) + h.abs() * rstd.square() * (u * h).abs().mean(1, keepdim=True) * (68 + d / 512)) * 2.0 ** -24
+    assert ((dX.double() - want).abs() <= want.abs() * 2.0 ** -24 + 3 * near).all()
+    terms = (g * h * rstd).abs().sum(0)
+    assert ((dw.double() - (g * h * rstd).sum(0)).abs() <= terms * (T + 4 + d / 512 + 64) * 2.0 ** -24 + 1e-30).all()
