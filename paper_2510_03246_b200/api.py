@@ -664,7 +664,10 @@ def _binding():
     global _native
     if _native is None:
         lib()
-        from . import _binding as native
+        try:
+            from . import _binding as native
+        except ImportError as e:
+            raise RuntimeError("_binding.so is missing: run `python -m paper_2510_03246_b200.build` with Python's and torch's headers at hand") from e
         _native = native
     return _native
 

@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -32,23 +33,35 @@ def _binding_command(out: str) -> list:
             "-c", os.path.join(CSRC, "sp_binding.cpp"), "-o", out]
 
 
-def _stale() -> bool:
-    if not os.path.exists(OUT) or not os.path.exists(BINDING):
-        return True
-    t = min(os.path.getmtime(OUT), os.path.getmtime(BINDING))
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "sp.h")]
-    return any(os.path.getmtime(d) > t for d in deps)
+def _binding_link(obj: str) -> list:
+    import torch
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return ["g++", "-shared", "-o", BINDING, obj, OUT, f"-L{lib}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN",
+            f"-Wl,-rpath,{lib}"]
+
+
+def _older(path: str, sources) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(s) > os.path.getmtime(path) for s in sources)
+
+
+def _stale() -> tuple[bool, bool]:
+    """Whether libsp.so and _binding.so are missing or older than what they are made of."""
+    header, binding = os.path.join(HERE, "..", "include", "sp.h"), os.path.join(CSRC, "sp_binding.cpp")
+    library = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != "sp_binding.cpp"]
+    return _older(OUT, [header, *library]), _older(BINDING, [header, binding])
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Build libsp.so if it is missing or older than its sources; returns its path."""
-    if not force and not _stale():
+    """Build libsp.so, and _binding.so, if they are missing or older than their sources; returns the library's path.  Without Python's or torch's
+    headers there is no _binding.so: a warning says so, and the calls that need it raise (api._binding); all others need libsp.so alone."""
+    library, binding = (True, True) if force else _stale()
+    if not library and not binding:
         return OUT
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     objs = []
     procs = []
-    for src in SOURCES:
+    for src in SOURCES if library else ():
         obj = os.path.join(objdir, src.replace(".cu", ".o"))
         cmd = [_nvcc(), *NVCC_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
@@ -56,22 +69,34 @@ def build(force: bool = False, verbose: bool = False) -> str:
             cmd.insert(2, "-v")
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
-    binding = os.path.join(objdir, "sp_binding.o")
-    procs.append(("sp_binding.cpp", subprocess.Popen(_binding_command(binding), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    obj = os.path.join(objdir, "sp_binding.o")
+    compiled, log = None, ""
+    if binding:
+        try:
+            compiled = subprocess.Popen(_binding_command(obj), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        except (OSError, ImportError) as e:          # (no compiler, no torch)
+            log = str(e)
     failed = False
     for src, p in procs:
         out, _ = p.communicate()
         if verbose or p.returncode != 0:
             sys.stderr.write(f"--- {src}\n{out}\n")
         failed |= p.returncode != 0
+    if compiled:
+        log, _ = compiled.communicate()
     if failed:
         raise RuntimeError("nvcc failed")
-    link = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-Xlinker", "-soname=libsp.so", "-o", OUT, *objs]
-    subprocess.run(link, check=True)
-    import torch
-    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    subprocess.run(["g++", "-shared", "-o", BINDING, binding, OUT, f"-L{lib}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
-                    "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{lib}"], check=True)
+    if library:
+        link = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-Xlinker", "-soname=libsp.so", "-o", OUT, *objs]
+        subprocess.run(link, check=True)
+    if binding:
+        linked = compiled is not None and compiled.returncode == 0 and subprocess.run(_binding_link(obj)).returncode == 0
+        if verbose or not linked:
+            sys.stderr.write(f"--- sp_binding.cpp\n{log}\n")
+        if not linked:
+            if os.path.exists(BINDING):
+                os.remove(BINDING)                   # (of another header or source)
+            warnings.warn("_binding.so could not be built: sp_rms_norm, sp_linear_e4m3, sp_cache_* and what calls them will raise")
     return OUT
 
 
