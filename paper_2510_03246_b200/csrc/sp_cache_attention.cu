@@ -1236,8 +1236,8 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   if (reinterpret_cast<uintptr_t>(ws) & 255u) return SP_ERR_ALIGNMENT;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   uint8_t* at = reinterpret_cast<uint8_t*>(ws);
-  ProfScope prof(PK_GEMM_SIMT, 0.0, 0.0, s);
   if (paged_few_rows(dt, Nq, g, n_seq, n_kv)) {
+    ProfScope prof(PK_GEMM_TC, 0.0, 0.0, s);
     const RowsPlan plan = rows_plan(Nq, n_seq, g, dh);
     PagedParams p = {};
     p.c = cache_view(cache);
@@ -1268,14 +1268,17 @@ sp_status sp_cache_attention(const sp_kv_cache* cache, const sp_mat* Q, const in
   const bool half = cache->kind == SP_CACHE_4BIT;
   HalfTops* tops = half ? reinterpret_cast<HalfTops*>(at + plan.cu_bytes) : nullptr;
   float* q_unit = half ? reinterpret_cast<float*>(units) : nullptr;
-  count_launch();
-  if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, whole, tops, status_dev) !=
-      cudaSuccess)
-    return SP_ERR_CUDA;
-  if (half && (cache_tops(cache, cu_k, whole, plan.rows, tops, s) != cudaSuccess ||
-               queries_to_half(cache, Q, cu_q, Qh, q_unit, tops, s) != cudaSuccess))
-    return SP_ERR_CUDA;
-  if (cache_open(cache, cu_k, whole, plan.rows, K, V, tops, status_dev, s) != cudaSuccess) return SP_ERR_CUDA;
+  {
+    ProfScope prof(PK_ELEMENTWISE, 0.0, 0.0, s);                   // (the products have a scope of their own)
+    count_launch();
+    if (launch(open_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, cache_view(cache), cu_q, (int32_t)Nq, (int32_t)keys, cu_k, whole, tops, status_dev) !=
+        cudaSuccess)
+      return SP_ERR_CUDA;
+    if (half && (cache_tops(cache, cu_k, whole, plan.rows, tops, s) != cudaSuccess ||
+                 queries_to_half(cache, Q, cu_q, Qh, q_unit, tops, s) != cudaSuccess))
+      return SP_ERR_CUDA;
+    if (cache_open(cache, cu_k, whole, plan.rows, K, V, tops, status_dev, s) != cudaSuccess) return SP_ERR_CUDA;
+  }
   sp_attention_args a = {};
   a.Q = half ? sp_mat{Qh, dt, 0, Nq, cols, cols} : *Q;
   a.O = *O;
