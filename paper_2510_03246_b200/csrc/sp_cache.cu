@@ -464,13 +464,13 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const ReadParams p) {
 }
 
 // Least and largest bound 15 |scale| + |zero| of the keys and of the values of every text and key head, among the rows that cache_open opens.  A block
-// takes one key head of 256 rows at a time, a row to a thread, since a head's scales of the rows of a page stand side by side; with a row to a
-// warp every 8 bytes come in a sector of their own.  A block's bounds of one text meet in shared memory: an atomic of each warp queues at
-// a few words.  (Maxima and minima are the same in any order.)
+// takes one key head of consecutive rows, 256 at a time, a row to a thread, since a head's scales of the rows of a page stand side by side; with a row
+// to a warp every 8 bytes come in a sector of their own.  A warp leaves its bounds where a text ends, and what a block has of one text at its end
+// meets in shared memory: an atomic of each warp queues at a few words, one of each thread all the more.  (Maxima and minima are the same in any order.)
 struct TopsParams {
   CacheView c;
   const int32_t *cu, *whole;
-  int32_t rows, strips;
+  int32_t rows, per_strip;
   HalfTops* tops;
 };
 __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
@@ -478,7 +478,8 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
   __shared__ int s_seq;
   __shared__ HalfTops s_tops[8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int32_t head = (int32_t)(blockIdx.x % (uint32_t)p.c.n_kv), strip = (int32_t)(blockIdx.x / (uint32_t)p.c.n_kv);
+  const int32_t head = (int32_t)(blockIdx.x % (uint32_t)p.c.n_kv);
+  const int64_t begin = (int64_t)(blockIdx.x / (uint32_t)p.c.n_kv) * p.per_strip, end = min(begin + p.per_strip, (int64_t)p.rows);
   const int per_head = p.c.dh / kCacheGroup;
   const HalfTops none = {0u, kNoLow, 0u, kNoLow};
   HalfTops mine = none;
@@ -490,6 +491,15 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
     if (t.v_top != 0u) atomicMax(&to->v_top, t.v_top);
     if (t.v_low != kNoLow) atomicMin(&to->v_low, t.v_low);
   };
+  // bounds of the lanes that have this lane's text; whether this lane speaks for them
+  const auto meet = [&] {
+    const uint32_t peers = __match_any_sync(0xffffffffu, seq);
+    mine.k_top = __reduce_max_sync(peers, mine.k_top);
+    mine.k_low = __reduce_min_sync(peers, mine.k_low);
+    mine.v_top = __reduce_max_sync(peers, mine.v_top);
+    mine.v_low = __reduce_min_sync(peers, mine.v_low);
+    return seq >= 0 && lane == __ffs(peers) - 1;
+  };
   const auto take = [](uint32_t& top, uint32_t& low, uint32_t pair) {
     const float scale = fabsf(__uint_as_float(pair << 16)), zero = fabsf(__uint_as_float(pair & 0xffff0000u));
     if (!(scale < INFINITY) || !(zero < INFINITY)) return;                // (a NaN either)
@@ -497,17 +507,23 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
     top = max(top, bits);
     if (bits != 0u) low = min(low, bits);
   };
-  for (int64_t row = (int64_t)strip * 256 + threadIdx.x; row < p.rows; row += (int64_t)p.strips * 256) {
-    const int32_t s = sequence_near(p.cu, p.c.n_seq, p.rows, row);        // (cu[0] is 0)
-    const int32_t first = bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - first;
-    if (row >= first + n || n != p.whole[s]) continue;
-    const int32_t place = (int32_t)row - first, entry = place / p.c.page_len, page = page_of(p.c, s, entry);
-    if (page < 0) continue;
-    if (s != seq) {
-      if (seq >= 0) leave(seq, mine);
-      mine = none;
-      seq = s;
+  for (int64_t row0 = begin; row0 < end; row0 += 256) {
+    const int64_t row = row0 + threadIdx.x;
+    int32_t s = -1, place = 0, entry = 0, page = -1;
+    if (row < end) {
+      s = sequence_near(p.cu, p.c.n_seq, p.rows, row);                    // (cu[0] is 0)
+      const int32_t first = bounded(p.cu[s], p.rows), n = bounded(p.cu[s + 1], p.rows) - first;
+      place = (int32_t)row - first;
+      entry = place / p.c.page_len;
+      if (place < n && n == p.whole[s]) page = page_of(p.c, s, entry);
     }
+    if (__any_sync(0xffffffffu, page >= 0 && seq >= 0 && s != seq)) {
+      if (meet()) leave(seq, mine);
+      mine = none;
+      seq = -1;
+    }
+    if (page < 0) continue;
+    seq = s;
     const int64_t at = page * p.c.scale_step + ((int64_t)head * p.c.page_len + place - entry * p.c.page_len) * per_head * 4;
 #pragma unroll 2
     for (int g = 0; g < per_head; ++g) {
@@ -515,20 +531,15 @@ __global__ void __launch_bounds__(256) cache_tops_kernel(const TopsParams p) {
       take(mine.v_top, mine.v_low, *reinterpret_cast<const uint32_t*>(p.c.vs + at + 4 * g));
     }
   }
-  // the lanes that have the same text, then the warps where all of the block has
-  const uint32_t peers = __match_any_sync(0xffffffffu, seq);
-  mine.k_top = __reduce_max_sync(peers, mine.k_top);
-  mine.k_low = __reduce_min_sync(peers, mine.k_low);
-  mine.v_top = __reduce_max_sync(peers, mine.v_top);
-  mine.v_low = __reduce_min_sync(peers, mine.v_low);
+  __syncwarp();
+  const bool first = meet();
   if (threadIdx.x == 0) s_seq = -1;
   __syncthreads();
   if (seq >= 0) atomicMax(&s_seq, seq);
   if (lane == 0) s_tops[warp] = none;
   __syncthreads();
   const int32_t text = s_seq;
-  const bool whole = __syncthreads_and(seq < 0 || seq == text) != 0, first = seq >= 0 && lane == __ffs(peers) - 1;
-  if (!whole) {
+  if (!__syncthreads_and(seq < 0 || seq == text)) {
     if (first) leave(seq, mine);
     return;
   }
@@ -668,10 +679,10 @@ cudaError_t cache_tops(const sp_kv_cache* c, const int32_t* cu, const int32_t* w
   p.cu = cu; p.whole = whole;
   p.rows = (int32_t)rows;
   p.tops = tops;
-  const int64_t most = ceil_div(4 * (int64_t)sm_count(), (int64_t)c->n_kv_heads), strips = ceil_div(rows, (int64_t)256);
-  p.strips = (int32_t)(strips < most ? strips : most);
+  const int64_t most = ceil_div(4 * (int64_t)sm_count(), (int64_t)c->n_kv_heads);
+  p.per_strip = (int32_t)align_up((size_t)ceil_div(rows, most), 256);
   count_launch();
-  return launch(cache_tops_kernel, dim3((unsigned)(p.strips * c->n_kv_heads)), dim3(256), 0, stream, p);
+  return launch(cache_tops_kernel, dim3((unsigned)(ceil_div(rows, (int64_t)p.per_strip) * c->n_kv_heads)), dim3(256), 0, stream, p);
 }
 cudaError_t queries_to_half(const sp_kv_cache* c, const sp_mat* Q, const int32_t* cu_q, void* Q_half, float* q_unit, const HalfTops* tops,
                             cudaStream_t stream) {

@@ -22,7 +22,7 @@
 // More rows of bf16 open the pages into rows of the workspace and take sp_attention: a tile of 128 rows reads opened keys at the tensor cores' rate, where this
 // form would open them again for every 16 rows.  4 bits are opened into fp16 in units of a text's key head (bf16 queries in those of a row): rounded to bf16,
 // results were 4.2e-3 from the formula (512 queries after 16384 keys, 32 heads of 128 on 8), and as two bf16 parts each 2.3e-3, in 312 us instead of
-// 186; in fp16 they are 1.7e-3 from it.  (Rounded values of equal scales are all off by the same, which no sum over keys takes away.)
+// 192; in fp16 they are 1.7e-3 from it.  (Rounded values of equal scales are all off by the same, which no sum over keys takes away.)
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>
@@ -1080,13 +1080,15 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
 inline int tile_rows(int64_t Nq, int64_t g, int64_t n_seq) { return Nq * g <= 8 * n_seq ? 8 : 16; }
 // Whether the cache streams past tiles of 16 rows: up to a number of rows per sequence, on average, that is the larger the fewer sequences and key
 // heads there are, since the other form's tiles of 128 rows then leave more of the device idle (less of it where a single sequence is cut to
-// fit).  This / the other form in 4 bits (16 take about as long), heads of 128, us.  A single sequence, by key heads: 1 head 16384 keys 160 rows 33 / 55;
-// 4 heads 8192 keys 128 rows 39 / 40; 8 heads 2048 keys 96 rows 28 / 29, 32768 keys 48 rows 73 / 86, 64 rows 91 / 83; 32 heads 8192 keys 48 rows
-// 77 / 82, 64 rows 96 / 79; 40 heads 4096 keys 48 rows 59 / 67, 80 rows 86 / 69.  Several, by sequences x heads: 12: 12 x 4096 keys 160 rows
-// 59 / 61; 16: 2 x 4096 keys 80 rows 45 / 49, 96 rows 51 / 48; 32: 4 x 4096 keys 80 rows 73 / 80, 96 rows 83 / 77; 48: 6 x 4096 keys 80 rows
-// 100 / 100; 64: 8 x 2048 keys 48 rows 176 / 204, 64 rows 228 / 190; 96: 12 x 4096 keys 32 rows 84 / 135, 64 rows 149 / 139; 512: 64 x 1024 keys 32
-// rows 162 / 175, 64 rows 308 / 177.  In fp32 this form is always faster, since only it takes the tensor cores: 64 x 1024 keys 16 rows 104 / 541,
-// 256 rows 1378 / 2663; 1 x 16384 keys 256 rows 235 / 989.
+// fit).  This / the other form in 4 bits and in 16, heads of 128, us.  A single sequence, by key heads: 1 head 16384 keys 160 rows 34 / 56 and 33 / 49; 4 heads
+// 8192 keys 128 rows 38 / 40 and 37 / 33, 160 rows 43 / 43 and 42 / 35; 8 heads 2048 keys 64 rows 24 / 29 and 23 / 22, 32768 keys 48 rows 73 / 92 and
+// 91 / 86, 64 rows 90 / 90 and 92 / 84, 80 rows 107 / 92 and 122 / 86; 32 heads 8192 keys 48 rows 76 / 95 and 87 / 91, 64 rows 95 / 92 and 99 / 89;
+// 40 heads 4096 keys 48 rows 58 / 72 and 62 / 64, 64 rows 71 / 69 and 74 / 62.  Several, by sequences x heads: 12: 12 x 4096 keys 128 rows 51 / 61 and
+// 49 / 47; 16: 2 x 4096 keys 80 rows 45 / 50 and 44 / 43, 96 rows 51 / 50 and 49 / 41; 32: 4 x 4096 keys 80 rows 72 / 83 and 70 / 73, 96 rows 83 / 80
+// and 80 / 71; 48: 6 x 4096 keys 80 rows 99 / 102 and 99 / 87; 64: 8 x 2048 keys 48 rows 57 / 78 and 55 / 68, 64 rows 70 / 75 and 66 / 67; 96: 12 x 4096
+// keys 48 rows 115 / 147 and 117 / 134, 64 rows 149 / 138 and 148 / 127; 512: 64 x 1024 keys 32 rows 161 / 175 and 169 / 157, 48 rows 234 / 187 and
+// 254 / 166.  In fp32 this form is always faster, since only it takes the tensor cores: 64 x 1024 keys 16 rows 104 / 541, 256 rows 1378 / 2663; 1 x 16384
+// keys 256 rows 235 / 989.
 inline bool paged_few_rows(int32_t dtype, int64_t Nq, int64_t g, int64_t n_seq, int64_t n_kv) {
   if (dtype == SP_F32) return true;
   const int64_t streams = n_seq * n_kv;

@@ -167,3 +167,21 @@ def test_values_that_change_by_steps(rows, by):
             bad.v_scale[pg, 1, slot, 1] *= by
     got, lse = call(Q, bad, q_len, table, k_len, heads)
     within(got, lse, Q, bad, q_len, table, k_len, heads, page, 2.0 ** -8 if rows == "many" else 2.0 ** -11, rows == "few")
+
+
+def test_many_long_texts_each_with_values_of_its_own_size():
+    """More rows than the blocks that look for the sizes take at once, texts that end inside a warp's rows and behind them."""
+    q_len, k_len, heads, kv, dh, page = [40] * 13, [2048 + 37 * i for i in range(12)] + [41], 4, 2, 64, 16
+    table, n_pages = table_for(k_len, page, 19)
+    pages = filled(n_pages, kv, page, dh, True, 20)
+    for s, n in enumerate(k_len):                                # 2^-50 .. 2^55 for V, beside 1 for K
+        pg = table[s, :-(-n // page)].long()
+        pages.v_scale[pg] *= 2.0 ** (-50 + 8 * s + s % 2)
+    Q = torch.randn(sum(q_len), heads * dh, generator=gen(21), device=DEV).to(BF)
+    got, lse = call(Q, pages, q_len, table, k_len, heads, max_keys=sum(k_len))
+    cu = offsets(q_len)
+    for s, n in enumerate(k_len):
+        back = copied(pages)
+        back.v_scale[table[s, :-(-n // page)].long()] *= 2.0 ** (50 - 8 * s - s % 2)
+        rows = slice(cu[s], cu[s + 1])
+        within(got[rows] * 2.0 ** (50 - 8 * s - s % 2), lse[rows], Q[rows], back, q_len[s:s + 1], table[s:s + 1], [n], heads, page, 2.0 ** -11, False)
