@@ -42,6 +42,7 @@ constexpr int kLead = 64;                  // what a tile and head costs beside 
 constexpr int kLeastShare = 16;            // of the line of work to a thread block, at least
 constexpr int kMostCtas = 2 * 148;         // thread blocks of a launch, at most
 constexpr int kPlanThreads = 256;
+constexpr float kNoWeight = -3.402823466e38f;      // lse of a piece whose keys are seen and have none
 constexpr uint32_t kNoPage = 0xffffffffu;
 
 struct PagedParams {
@@ -976,9 +977,9 @@ paged_rows_kernel(const PagedParams p) {
         acc[2] = fmaf(v.z, f, acc[2]);
         acc[3] = fmaf(v.w, f, acc[3]);
       }
-      // (keys seen, and all logits beyond fp32 below: nothing can be told; a piece of a row's keys may be of no weight)
-      const bool lost = sum == 0.f && !cut && visible(it.nk, shift, token) > 0;
-      const float inv = sum == 0.f ? (lost ? NAN : 0.f) : 1.f / sum;
+      // (keys seen, and all logits beyond fp32 below: nothing can be told, unless other pieces of the row's keys have weight)
+      const bool lost = sum == 0.f && visible(it.nk, shift, token) > kb;
+      const float inv = sum == 0.f ? (lost && !cut ? NAN : 0.f) : 1.f / sum;
 #pragma unroll
       for (int x = 0; x < 4; ++x) acc[x] *= inv;
       if (bad) {
@@ -1003,7 +1004,7 @@ paged_rows_kernel(const PagedParams p) {
         for (int x = 0; x < 4; ++x) store1(out + x, acc[x]);
       }
       if (d == 0) {
-        const float lse2 = sum == 0.f ? (lost ? NAN : -INFINITY) : base + (log2f(sum) - kLift);
+        const float lse2 = sum == 0.f ? (!lost ? -INFINITY : cut ? kNoWeight : NAN) : base + (log2f(sum) - kLift);
         if (cut) p.part_lse[slot_of * ROWS + row] = lse2;
         else if (p.lse) p.lse[out_row * p.n_heads + out_head] = lse2 == -INFINITY ? lse2 : lse2 * 0.6931471805599453f;
       }
@@ -1042,7 +1043,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
 #pragma unroll
   for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
   const float ref = mx == -INFINITY ? 0.f : mx;
-  bad = __any_sync(0xffffffffu, bad);
+  bad = __any_sync(0xffffffffu, bad) || mx == kNoWeight;
   const int d = 4 * lane;             // a lane has channels 4 lane .. (dh is a multiple of 16)
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float total_w = 0.f;
@@ -1062,7 +1063,6 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
       }
     }
   }
-  if (total_w == 0.f) bad |= visible(it.nk, p.causal ? (int64_t)it.nk - it.nq : (int64_t)it.nk, row - it.q0) > 0;      // (as above)
   const float inv = total_w == 0.f ? 0.f : 1.f / total_w;
   if (d < dh) {
     T* out = reinterpret_cast<T*>(p.o) + (int64_t)row * p.ldo + (int64_t)h * dh + d;

@@ -69,3 +69,29 @@ def test_logits_too_small_for_fp32_are_equal(q_len, k_len, size, dtype, four):
         seen = torch.arange(nk - nq + 1, nk + 1, device=DEV).double()
         assert ((lse[cu[s]:cu[s + 1]].double() - seen.log()[:, None]).abs() <= 2.0 ** -18 * 10).all()
     assert o.isfinite().all()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("where", [0, 15000, 29000])
+def test_keys_of_no_weight_beside_others(where, dtype, four):
+    """Logits of -2^136 at all keys but a thousand, whose logits are 0: the mean of their values, whichever pieces of the text hold them."""
+    heads, kv, dh, page, n = 4, 2, 64, 16, 30000
+    table, n_pages = table_for([n], page, 68)
+    pages = filled(n_pages, kv, page, dh, four, 69)
+    some = table[0, where // page:where // page + 62].long()
+    if four:
+        pages.k_scale[..., 0], pages.k_scale[..., 1] = 0.0, -2.0 ** 66
+        pages.k_scale[some] = 0.0
+    else:
+        pages.k[:] = -2.0 ** 66
+        pages.k[some] = 0.0
+    Q = torch.zeros(1, heads * dh, dtype=dtype, device=DEV)
+    Q[:, ::64] = 2.0 ** 60
+    o, lse = api.sp_cache_attention(Q, pages, ints([0, 1]), table, ints([n]), heads, scale=2.0 ** 10, want_lse=True)
+    from tests.test_gpu_paged_cache import values
+    v = values(pages)[1][0][some].transpose(1, 2).flatten(0, 1)                   # [keys, kv, dh]
+    want = v.mean(0).repeat_interleave(heads // kv, 0).flatten()
+    assert ((lse.double() - math.log(v.shape[0])).abs() <= 1e-5).all()
+    size = v.abs().mean(0).repeat_interleave(heads // kv, 0).flatten()
+    assert ((o[0].double() - want).abs() <= (2.0 ** -8 if dtype == BF else 2.0 ** -20) * want.abs() + 2.0 ** (-11 if dtype == BF else -18) * 2 * size).all()
