@@ -585,7 +585,8 @@ sp_status sp_token_logprobs_grad(const sp_mat* logits, const int64_t* targets, d
  * itself, and has R's dtype.  Y: [T, d] of X's dtype, or SP_E4M3: y8 = e4m3(y / scale) with scale[t] = max_j |y_j| / 448 (a row's maximum counts as
  * at least 1e-30): operands of sp_linear_e4m3.  Y may be X itself.  weight: fp32 [d] or NULL (ones).  scale: fp32 [T], given exactly with SP_E4M3.
  * rstd: fp32 [T] or NULL.  Every dtype, ld and alignment of SP_BF16 and SP_F32; widths up to 32768 with 16-byte rows read each value once, others
- * again for each pass.  y comes from the unrounded sum h.  Sums in fp32: a row whose sum of squares leaves its range has rstd 0.
+ * again for each pass.  y comes from the unrounded sum h.  Sums in fp32: a row whose sum of squares leaves its range has rstd 0 (above it, or
+ * infinity below it where eps is 0).
  * A NaN or an infinity in a row makes its y NaN where the formula does.
  * sp_rms_norm_grad: dX = rstd (weight dy - h rstd^2 mean(weight dy h)) + dH: the gradient of x and of r alike.  H as sp_rms_norm left it;
  * rstd as it left it, or NULL (then formed again from H).  dH: the gradient that arrives at h through the stream itself, or NULL.  dX may be dH, or
@@ -639,7 +640,8 @@ sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const sp_mat* W,
  * [N, n_kv_heads * d_head] (SP_BF16: rounded, or SP_F32).
  * sp_cache_attention: sp_attention with the keys and values [0, lens[s]) of the cache: rows [cu_q[s], cu_q[s+1]) of Q and O, [Nq, n_heads * d_head], query i
  * of n_q sees keys j <= i + lens[s] - n_q (causal != 0) or all.  d_head and head h / g of a query head as there, a query without a visible key gets
- * O = 0 and lse = -infinity, rows of no sequence are left as they were, and what stands in slots that a query does not see does not reach it.
+ * O = 0 and lse = -infinity, rows of no sequence are left as they were, and what stands in slots that a query does not see does not reach it.  An infinite
+ * value that it sees makes its channel infinite or NaN; a row whose scaled logits leave fp32 is NaN.
  * 4 bits or 16, the values are those that the cache stands for.  Softmax and sums in fp32.  Roundings: SP_F32 none but those of fp32 products and
  * sums.  SP_BF16 with 16 bits: probabilities to two bf16 parts (2^-16), with many rows to bf16.  SP_BF16 with 4 bits: probabilities times scales to fp16, or to three bf16 parts where the scales
  * of values that a tile of rows meets lie further apart than 2^20; queries (2^-16 of a row's

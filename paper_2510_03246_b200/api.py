@@ -682,7 +682,8 @@ class RmsNorm:
 
 def sp_rms_norm(X, weight=None, eps=1e-5, residual=None, h_out=None, out=None, out_dtype=None, want_rstd=False) -> RmsNorm:
     """h = X + residual, y = weight h / sqrt(mean h^2 + eps) (see sp.h).  X [T, d] bf16 or fp32, residual of either, weight fp32 [d].
-    h_out: where to write h (residual or X itself: in place; allocated where there is a residual).  out_dtype
+    h_out: where to write h (residual or X itself: in place; allocated where there is a residual).  Results allocated here have rows that start on
+    16 bytes (a pitch wider than d where d needs it).  out_dtype
     torch.float8_e4m3fn: 8 bits with a scale per row, rows that start on 16 bytes, as sp_linear_e4m3 reads them."""
     if out_dtype is not None and out_dtype != _F8 and out_dtype != X.dtype:
         raise ValueError("the result is of X's dtype or float8_e4m3fn")
@@ -697,7 +698,7 @@ def sp_rms_norm(X, weight=None, eps=1e-5, residual=None, h_out=None, out=None, o
 def sp_rms_norm_grad(dY, H, weight=None, rstd=None, eps=1e-5, d_stream=None, want_weight=True, out=None, ws=None):
     """Gradient of sp_rms_norm with respect to h (so to x and to the residual) and to the weight (see sp.h): dY [T, d] the gradient of
     y, H and rstd as the forward call left them (rstd None: formed again), d_stream the gradient that arrives at h by itself.  out may be
-    d_stream.  Returns (dX of H's dtype, dweight fp32 [d] or None)."""
+    d_stream; allocated here, its rows start on 16 bytes.  Returns (dX of H's dtype, dweight fp32 [d] or None)."""
     code, dx, dw = (_native or _binding()).rms_norm_grad(dY, H, weight, rstd, eps, d_stream, want_weight, out, ws)
     if code:
         raise SpError(code, "sp_rms_norm_grad")

@@ -185,3 +185,42 @@ def test_many_long_texts_each_with_values_of_its_own_size():
         back.v_scale[table[s, :-(-n // page)].long()] *= 2.0 ** (50 - 8 * s - s % 2)
         rows = slice(cu[s], cu[s + 1])
         within(got[rows] * 2.0 ** (50 - 8 * s - s % 2), lse[rows], Q[rows], back, q_len[s:s + 1], table[s:s + 1], [n], heads, page, 2.0 ** -11, False)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("heads, kv, q_len, k_len", [(8, 2, [4, 3], [200, 90]), (4, 4, [1, 1], [700, 33]), (16, 1, [1], [3000]), (3, 1, [5, 1, 2], [60, 9000, 17])])
+@pytest.mark.parametrize("by", [2.0 ** 30, 2.0 ** -40])
+def test_few_rows_of_every_tile_and_width(by, heads, kv, q_len, k_len, dh):
+    """Scales of V that change by steps in every third block, pieces of a long text that meet them and others that do not."""
+    page = 16
+    table, n_pages = table_for(k_len, page, 22)
+    pages = filled(n_pages, kv, page, dh, True, 23)
+    for s, n in enumerate(k_len):
+        for e in range(1, -(-n // page), 3):
+            pages.v_scale[int(table[s, e]), :, ::5] *= by
+    Q = torch.randn(sum(q_len), heads * dh, generator=gen(24), device=DEV).to(BF)
+    got, lse = call(Q, pages, q_len, table, k_len, heads)
+    within(got, lse, Q, pages, q_len, table, k_len, heads, page, 2.0 ** -11, True)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("heads, kv", [(4, 4), (70, 1)])
+def test_formats_of_items_side_by_side(heads, kv, dh):
+    """More items than SMs, fp16 and bf16 in turn; heads of a group that go one by one (more than 64 share a key head)."""
+    n, page = (60, 16) if kv == 4 else (12, 16)
+    q_len, k_len = [64 if kv == 4 else 40] * n, [65 + 17 * (i % 20) for i in range(n)]
+    table, n_pages = table_for(k_len, page, 25)
+    pages = filled(n_pages, kv, page, dh, True, 26)
+    wide = torch.zeros(n, kv, dtype=torch.bool)
+    for s in range(n):
+        for h in range(kv):
+            if (s + h) % 3 == 0:
+                wide[s, h] = True
+                pages.v_scale[int(table[s, 1]), h, 3] *= 2.0 ** 26
+                if (s + h) % 2:
+                    pages.k_scale[int(table[s, 0]), h, 7] *= 2.0 ** -24
+    Q = torch.randn(sum(q_len), heads * dh, generator=gen(27), device=DEV).to(BF)
+    got, lse = call(Q, pages, q_len, table, k_len, heads, max_keys=sum(k_len))
+    rows = wide.repeat_interleave(heads // kv, 1).repeat_interleave(torch.tensor(q_len), 0).to(DEV)
+    within(got, lse, Q, pages, q_len, table, k_len, heads, page, 2.0 ** -8, False, rows)
+    within(got, lse, Q, pages, q_len, table, k_len, heads, page, 2.0 ** -11, False, ~rows)
