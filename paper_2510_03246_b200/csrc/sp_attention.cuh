@@ -8,8 +8,8 @@ namespace sp {
 // for every row and head; keys and values one for every text and key head, by the least and the largest size that their groups of 64 channels may reach
 // there (fp32 bits; groups of zeros and non-finite ones do not count).  Sizes that lie further apart than 2^kHalfSpan would leave fp16: that text's head is
 // then opened in bf16, its queries and probabilities are bf16 too, and all units are 1.  (At 2^20 the least group's values are still off by no more
-// than 2^-15 of its size, beside 2^-9 of a value in bf16.)  What another text, another head or a key that a query does not see
-// holds thus never takes a value's bits.
+// than 2^-14 of its size: scale, offset and value each by half of 2^-24 units, of which the size is 2^-6.  In bf16 it is 2^-8 of a value.)  What another
+// text, another head or a key that a query does not see holds thus never takes a value's bits.
 struct alignas(16) HalfTops {
   uint32_t k_top, k_low, v_top, v_low;
 };

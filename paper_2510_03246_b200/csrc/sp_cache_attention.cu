@@ -497,6 +497,7 @@ paged_rows_kernel(const PagedParams p) {
     // vhigh: twice the unit, vlow: less one, 2^-20 of it, as bits of bf16, in both halves of a word: two scales are compared at once.
     constexpr bool HALF = FOUR && PARTS == 1;
     constexpr float kLift = HALF ? 5.f : 0.f, kWideUnit = 16777216.f;      // (2^24: no finite scale times a lifted probability leaves fp32)
+    constexpr float kOffsetPer = HALF ? 1.f / kWideUnit : 1.f;   // sums of offsets, and what warps join, are in such units for the same reason
     // O: 4 bits: channels 64 (j / 4) + 8 g4 + j % 4 (| + 4) of rows 2 t4 + (x & 1); bf16: channels 16 j + g4 (| + 8)
     float o[K16][H][4], offset[H][G][2], per_vunit = 0.f, r[H][2], ref[H][2], most[H][2], l[H][2];
 #pragma unroll
@@ -546,7 +547,7 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const uint32_t pair = lds32(stage + 2 * R::TILE + R::SCALES + ((g4 + 8 * y) * G + gr) * 4);
-            const float scale = low(pair), zero = fmaf(8.f, scale, high(pair));
+            const float scale = low(pair), zero = fmaf(8.f * kOffsetPer, scale, kOffsetPer * high(pair));
             float ps[2];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -720,7 +721,8 @@ paged_rows_kernel(const PagedParams p) {
             float now = top > twice ? __uint_as_float(min(max(__float_as_uint(top) >> 23, 20u), 240u) << 23) : 0.5f * twice;
             vhigh = (__float_as_uint(2.f * now) >> 16) * 0x00010001u;
             vlow = ((__float_as_uint(0x1p-20f * now) >> 16) - 1u) * 0x00010001u;
-            if (least < 0x1p-20f * now || now * per_vunit > 0x1p40f) {                   // (what O holds would leave fp32 by such a step)
+            // (what O holds would leave fp32 by a large step; scales beyond the largest unit would leave fp16)
+            if (least < 0x1p-20f * now || now * per_vunit > 0x1p40f || top >= 0x1p114f) {
               now = kWideUnit;
               vhigh = kWide;
               vlow = 0xffffffffu;                                // (every block but one of zeros comes here)
@@ -801,7 +803,7 @@ paged_rows_kernel(const PagedParams p) {
             for (int y = 0; y < 2; ++y) {
               // (p s)^T goes into the product with n - 8, the rest into offset, so that a rounding of p s weighs a number's distance from the
               // middle alone (16 tokens after 2048 .. 31013 keys: 4.7e-3 from the formula with n as it is).
-              const float scale = low(pair_v[y][gr]), zero = fmaf(8.f, scale, high(pair_v[y][gr]));
+              const float scale = low(pair_v[y][gr]), zero = fmaf(8.f * kOffsetPer, scale, kOffsetPer * high(pair_v[y][gr]));
               float ps[2], pz[2];
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
@@ -928,7 +930,7 @@ paged_rows_kernel(const PagedParams p) {
             for (int w = 4; w < 32; w <<= 1) offset[h][gr][x] += __shfl_xor_sync(0xffffffffu, offset[h][gr][x], w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float f = !HALF ? 1.f : per_vunit > 0.f ? 1.f / per_vunit : 0.f;
+              const float f = !HALF ? 1.f : per_vunit > 0.f ? kOffsetPer / per_vunit : 0.f;
               o[4 * gr + j][h][x] = fmaf(o[4 * gr + j][h][x], f, offset[h][gr][x]);
               o[4 * gr + j][h][2 + x] = fmaf(o[4 * gr + j][h][2 + x], f, offset[h][gr][x]);
             }
@@ -979,7 +981,7 @@ paged_rows_kernel(const PagedParams p) {
       }
       // (keys seen, and all logits beyond fp32 below: nothing can be told, unless other pieces of the row's keys have weight)
       const bool lost = sum == 0.f && visible(it.nk, shift, token) > kb;
-      const float inv = sum == 0.f ? (lost && !cut ? NAN : 0.f) : 1.f / sum;
+      const float inv = sum == 0.f ? (lost && !cut ? NAN : 0.f) : 1.f / kOffsetPer / sum;
 #pragma unroll
       for (int x = 0; x < 4; ++x) acc[x] *= inv;
       if (bad) {

@@ -224,3 +224,14 @@ def test_formats_of_items_side_by_side(heads, kv, dh):
     rows = wide.repeat_interleave(heads // kv, 1).repeat_interleave(torch.tensor(q_len), 0).to(DEV)
     within(got, lse, Q, pages, q_len, table, k_len, heads, page, 2.0 ** -8, False, rows)
     within(got, lse, Q, pages, q_len, table, k_len, heads, page, 2.0 ** -11, False, ~rows)
+
+
+@pytest.mark.parametrize("rows", ["few", "many"])
+@pytest.mark.parametrize("by", [2.0 ** 100, 2.0 ** 116, 2.0 ** 121, 2.0 ** -60])
+def test_values_at_the_ends_of_the_range(rows, by):
+    """V's scales and offsets times a power of two: so is the result, to 2^127."""
+    q_len, k_len, table, pages, Q, heads, page = setup(rows, 28)
+    far = copied(pages)
+    far.v_scale *= by
+    got, lse = call(Q, far, q_len, table, k_len, heads)
+    within((got.double() / by).float(), lse, Q, pages, q_len, table, k_len, heads, page, 2.0 ** -11, rows == "few")
