@@ -641,9 +641,9 @@ sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const sp_mat* W,
  * sp_cache_attention: sp_attention with the keys and values [0, lens[s]) of the cache: rows [cu_q[s], cu_q[s+1]) of Q and O, [Nq, n_heads * d_head], query i
  * of n_q sees keys j <= i + lens[s] - n_q (causal != 0) or all.  d_head and head h / g of a query head as there, a query without a visible key gets
  * O = 0 and lse = -infinity, rows of no sequence are left as they were, and what stands in slots that a query does not see does not reach it.  An infinite
- * value that it sees makes its channel infinite or NaN; a row whose scaled logits leave fp32 is NaN.
+ * value that it sees makes its channel infinite (SP_F32, or from a group of 4 bits: infinite or NaN); a row whose scaled logits leave fp32 is NaN.
  * 4 bits or 16, the values are those that the cache stands for.  Softmax and sums in fp32.  Roundings: SP_F32 none but those of fp32 products and
- * sums.  SP_BF16 with 16 bits: probabilities to two bf16 parts (2^-16), with many rows to bf16.  SP_BF16 with 4 bits: probabilities times scales to fp16, or to three bf16 parts where the scales
+ * sums.  SP_BF16 with 16 bits: probabilities to two bf16 parts (2^-15), with many rows to bf16.  SP_BF16 with 4 bits: probabilities times scales to fp16, or to three bf16 parts where the scales
  * of values that a tile of rows meets lie further apart than 2^20; queries (2^-16 of a row's
  * largest value is kept at least); with many rows probabilities and opened values to fp16 in units of powers of two of a text's key head, queries in units of
  * a row and head (2^-28 of the largest keep all bits), or all three to bf16 where the sizes of a text's key head, by groups of 64 channels, lie

@@ -177,6 +177,13 @@ __device__ __forceinline__ void split(float lo, float hi, uint32_t (&r)[PARTS]) 
     }
   }
 }
+// Two parts of numbers that are not negative, both above 0 where the number is: times an infinite value they are infinite, not NaN.  (Less its last
+// bit a number is cut to bf16; the rest is rounded: 2^-15 of the number.)
+__device__ __forceinline__ void split_above_zero(float lo, float hi, uint32_t (&r)[2]) {
+  constexpr float kBelow = 0x1.fffffep-1f;
+  r[0] = __byte_perm(__float_as_uint(lo * kBelow), __float_as_uint(hi * kBelow), 0x7632);
+  r[1] = pack_bf16(lo - low(r[0]), hi - high(r[0]));
+}
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   const __half2 e = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&e);
@@ -875,7 +882,8 @@ paged_rows_kernel(const PagedParams p) {
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             uint32_t u[VPARTS];
-            split<VPARTS>(s[h][2 * y], s[h][2 * y + 1], u);
+            if constexpr (PARTS == 1) split_above_zero(s[h][2 * y], s[h][2 * y + 1], u);
+            else split<VPARTS>(s[h][2 * y], s[h][2 * y + 1], u);
 #pragma unroll
             for (int x = 0; x < VPARTS; ++x) pb[h][x][y] = turned8x8(u[x]);
           }

@@ -95,3 +95,24 @@ def test_keys_of_no_weight_beside_others(where, dtype, four):
     assert ((lse.double() - math.log(v.shape[0])).abs() <= 1e-5).all()
     size = v.abs().mean(0).repeat_interleave(heads // kv, 0).flatten()
     assert ((o[0].double() - want).abs() <= (2.0 ** -8 if dtype == BF else 2.0 ** -20) * want.abs() + 2.0 ** (-11 if dtype == BF else -18) * 2 * size).all()
+
+
+@pytest.mark.parametrize("q_len, k_len", [([1], [40]), ([1, 3], [5000, 33]), ([300], [500])])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_an_infinite_value_makes_its_channel_infinite(sign, q_len, k_len):
+    """16 bits, bf16: at a key that all see, one that has the largest weight, and at the last one."""
+    heads, kv, dh, page = 4, 2, 64, 16
+    table, n_pages = table_for(k_len, page, 70)
+    pages = filled(n_pages, kv, page, dh, False, 71)
+    Q = torch.randn(sum(q_len), heads * dh, generator=gen(72), device=DEV).to(BF)
+    for s, n in enumerate(k_len):
+        for j, channel in ((0, 3), (n - 1, 5)):
+            pages.v[int(table[s, j // page]), :, j % page, channel] = sign * math.inf
+        pages.k[int(table[s, 0]), :, 0] = 0.0
+    o, lse = api.sp_cache_attention(Q, pages, ints(offsets(q_len)), table, ints(k_len), heads, want_lse=True)
+    o = o.view(-1, heads, dh)
+    assert (o[..., 3] == sign * math.inf).all() and lse.isfinite().all()
+    last = [c - 1 for c in offsets(q_len)[1:]]
+    assert (o[last][..., 5] == sign * math.inf).all()
+    others = [c for c in range(dh) if c not in (3, 5)]
+    assert o[..., others].isfinite().all()
