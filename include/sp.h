@@ -644,7 +644,7 @@ sp_status sp_linear_e4m3(const sp_mat* X, const float* x_scale, const sp_mat* W,
  * value that it sees makes its channel infinite (SP_F32, or from a group of 4 bits: infinite or NaN); a row whose scaled logits leave fp32 is NaN.
  * 4 bits or 16, the values are those that the cache stands for.  Softmax and sums in fp32.  Roundings: SP_F32 none but those of fp32 products and
  * sums.  SP_BF16 with 16 bits: probabilities to two bf16 parts (2^-15), with many rows to bf16.  SP_BF16 with 4 bits: probabilities times scales to fp16, or to three bf16 parts where the scales
- * of values that a tile of rows meets lie further apart than 2^20; queries (2^-16 of a row's
+ * of values that a tile of rows meets lie further apart than 2^20; queries (2^-21 of a row's
  * largest value is kept at least); with many rows probabilities and opened values to fp16 in units of powers of two of a text's key head, queries in units of
  * a row and head (2^-28 of the largest keep all bits), or all three to bf16 where the sizes of a text's key head, by groups of 64 channels, lie
  * further apart than 2^20.  Equal calls give equal bits, and no bit of a text's rows depends on another text's pages.

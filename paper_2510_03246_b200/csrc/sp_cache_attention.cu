@@ -12,7 +12,8 @@
 // word g4 of four keys.
 //   K: the byte of a number n is n / 512 as e4m3 (the values below the first power of two and above it lie equally close), so that a mask opens
 //   four of them for m16n8k32 of e4m3, a faster instruction too.  Queries are two e4m3 parts, eight bits of what a power of two per row takes to
-//   128 .. 255; what is lost lies 2^-17 and more below a row's largest value.
+//   128 .. 255, the second 2^5 times as large, with sums of its own; what is lost lies 2^-22 and more below a row's largest value.  (In one unit it was 2^-17, and
+//   lse off by 2e-6 of its size.)
 //   V: number n becomes the fp16 64 + n by a shift and one logical operation, two at a time; a second instruction with a constant takes 72 away
 //   again, so that n - 8 is left.  Probabilities times scales are fp16 as well, in units of a power of two that follows the scales: with bf16
 //   their roundings left 2.4e-3 of the result's norm (16 tokens after 2048 .. 31013 keys), with fp16 1.7e-3, the result's own.
@@ -154,10 +155,13 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) |
          (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
 }
-__device__ __forceinline__ uint32_t left_of_e4m3(const float (&a)[4], uint32_t packed) {      // a - packed
+// kLeftUnits (a - packed): of a value below 2^8 at most 2^3 is left, so that 2^5 of it stay below 448
+constexpr float kLeftUnits = 32.f;
+__device__ __forceinline__ uint32_t left_of_e4m3(const float (&a)[4], uint32_t packed) {
   const __half2 lo = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(packed & 0xffffu), __NV_E4M3));
   const __half2 hi = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(packed >> 16), __NV_E4M3));
-  return pack_e4m3(a[0] - __low2float(lo), a[1] - __high2float(lo), a[2] - __low2float(hi), a[3] - __high2float(hi));
+  return pack_e4m3(kLeftUnits * (a[0] - __low2float(lo)), kLeftUnits * (a[1] - __high2float(lo)), kLeftUnits * (a[2] - __low2float(hi)),
+                   kLeftUnits * (a[3] - __high2float(hi)));
 }
 __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
@@ -612,11 +616,11 @@ paged_rows_kernel(const PagedParams p) {
           for (int gr = 0; gr < G; ++gr) pair[y][gr] = lds32(stage + 2 * R::TILE + ((g4 + 8 * y) * G + gr) * 4);
 #pragma unroll
         for (int gr = 0; gr < G; ++gr) {
-          float a[H][4];
+          float a[H][4], left[H][4];                             // (left: e4m3 queries' second part)
 #pragma unroll
           for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) a[h][x] = 0.f;
+            for (int x = 0; x < 4; ++x) a[h][x] = left[h][x] = 0.f;
           uint2 w[2];                                            // keys g4, g4 + 8
 #pragma unroll
           for (int y = 0; y < 2; ++y) w[y] = lds64(stage + (k_at ^ (32u * gr + kFlip * y)) + 8 * y * (DH / 2));
@@ -626,11 +630,15 @@ paged_rows_kernel(const PagedParams p) {
               const uint32_t w0 = u == 0 ? w[0].x : w[0].y, w1 = u == 0 ? w[1].x : w[1].y;
               const uint32_t a0 = w0 & 0x0f0f0f0fu, a1 = w1 & 0x0f0f0f0fu, a2 = (w0 >> 4) & 0x0f0f0f0fu, a3 = (w1 >> 4) & 0x0f0f0f0fu;
 #pragma unroll
-              for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                  mma_e4m3(a[h], a0, a1, a2, a3, q[h][0][4 * gr + 2 * u + x][0], q[h][0][4 * gr + 2 * u + x][1]);
+              for (int h = 0; h < H; ++h) {
+                mma_e4m3(a[h], a0, a1, a2, a3, q[h][0][4 * gr + 2 * u][0], q[h][0][4 * gr + 2 * u][1]);
+                mma_e4m3(left[h], a0, a1, a2, a3, q[h][0][4 * gr + 2 * u + 1][0], q[h][0][4 * gr + 2 * u + 1][1]);
+              }
             }
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) a[h][x] = fmaf(left[h][x], 1.f / kLeftUnits, a[h][x]);
           } else {
             const uint32_t n[4][4] = {
                 {opened_centred<0>(w[0].x), opened_centred<0>(w[1].x), opened_centred<1>(w[0].x), opened_centred<1>(w[1].x)},

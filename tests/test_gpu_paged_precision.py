@@ -51,3 +51,48 @@ def test_roundings_in_the_mean(four, lengths, roundings, dh):
     expected = (step.square().mean() / 12 + sum(u * u for u in roundings) / 3 * want.square().mean()).sqrt()
     error = (got.double() - want).square().mean().sqrt()
     assert error <= expected * (1 + 2.5 * (3 / want.numel()) ** 0.5), (error / expected).item()
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("four", [True, False])
+@pytest.mark.parametrize("lengths", [([1] * 40, [5 + 53 * i for i in range(40)]), ([4] * 10, [20 + 300 * i for i in range(10)])])
+def test_lse_in_the_mean(lengths, four, dh):
+    """Few rows.  A logit is a sum of some 16 partial sums in fp32 of terms <= T (by groups of 64 channels: scale <q, n> and offset sum q where 4 bits are
+    opened so), each off by 2^-24 T / sqrt 3 in the mean at most; of a query's values 2^-22 of the row's largest are lost at most, 2^-22 / sqrt 3 in the mean,
+    over the channels' numbers as squares.  lse averages the logits' errors, so it has no more than one logit's in the mean."""
+    q_len, k_len = lengths
+    heads, kv, page = 4, 2, 16
+    table, n_pages = table_for(k_len, page, 53)
+    g = gen(54)
+    pages = api.KvPages.empty(n_pages, kv, page, dh, four)
+    for x, s in ((pages.k, pages.k_scale), (pages.v, pages.v_scale)):
+        if four:
+            x.copy_(torch.randint(0, 256, x.shape, generator=g, device=DEV))
+            s[..., 0] = 0.1 + 0.3 * torch.rand(s.shape[:-1], generator=g, device=DEV)
+            s[..., 1] = -7.5 * s[..., 0]
+        else:
+            x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+    Q = torch.randn(sum(q_len), heads * dh, generator=g, device=DEV)
+    Q[:, ::16] *= 8.0                                             # strong channels: the others lie below a row's largest
+    Q = Q.to(BF)
+    _, lse = api.sp_cache_attention(Q, pages, ints(offsets(q_len)), table, ints(k_len), heads, want_lse=True)
+    (k64, k_size), _ = values(pages)
+    cu, wrong, allowed = offsets(q_len), 0.0, 0.0
+    for s, (nq, nk) in enumerate(zip(q_len, k_len)):
+        K, KS = gathered(k64, table, page, s, nk), gathered(k_size, table, page, s, nk)
+        q = Q[cu[s]:cu[s + 1]].double().view(nq, kv, heads // kv, dh)
+        z = torch.einsum("iagd,jad->agij", q, K) * dh ** -0.5
+        hidden = torch.arange(nk, device=DEV)[None, :] > torch.arange(nq, device=DEV)[:, None] + nk - nq
+        want = torch.logsumexp(z.masked_fill(hidden, -math.inf), 3)
+        got = lse[cu[s]:cu[s + 1]].double().view(nq, kv, heads // kv).permute(1, 2, 0)
+        wrong += (got - want).square().sum().item()
+        if four:                                                   # |sum q| |offset| by groups, twice: the numbers' part is about as large
+            off = (pages.k_scale[table[s, :-(-nk // page)].long()][..., 1].double().transpose(1, 2).flatten(0, 1)[:nk]).abs()
+            T = 2 * torch.einsum("iagu,jau->agij", q.unflatten(3, (-1, 64)).sum(4).abs(), off)
+            lost = torch.einsum("iag,ja->agij", q.abs().amax(3), KS.square().sum(2).sqrt()) * 2.0 ** -22
+        else:
+            T = torch.einsum("iagd,jad->agij", q.abs(), K.abs())
+            lost = torch.zeros_like(T)
+        one = ((16 * (T * 2.0 ** -24).square() + lost.square()) / 3 / dh).masked_fill(hidden, 0.0)
+        allowed += one.amax(3).sum().item() + (2.0 ** -23 * want).square().sum().item()        # and lse's own last roundings
+    assert wrong <= allowed, (wrong / allowed) ** 0.5
